@@ -386,6 +386,77 @@ int hif8_pts_search(const void* A, const void* W, int dtype, int w_is_nk, const 
 size_t hif8_pts_workspace_bytes(int M, int N, int K, int n_exp);
 int hif8_pts_status(const void* workspace, hif8_stream_t stream);
 
+/*
+ * Key/value cache in HiF8, paged.  (Section 4.1 keeps to GEMM inputs; the keys and values of attention are the other tensors of
+ * inference that are read again and again, here with one power-of-two scale for each block of tokens and head.)
+ *
+ * A cache is device memory of the caller's:
+ *   k_pages, v_pages  [n_pages][kv_heads][page_tokens][head_dim] bytes, 16-byte aligned
+ *   k_exp, v_exp      [n_pages][kv_heads] ints: the scale exponent e of each block (one page's tokens of one head); a code stands for
+ *                     value(code) * 2^-e.  Exponents are taken within [-HIF8_CACHE_EXP_MAX, HIF8_CACHE_EXP_MAX].
+ *   page_table        ints, row s (of table_stride entries) lists the pages of sequence s in order: token t lies in slot t % page_tokens
+ *                     of page page_table[s * table_stride + t / page_tokens].
+ * page_tokens: 16, 32, 64 or 128; head_dim: 64, 128 or 256; kv_heads: 1 .. HIF8_CACHE_MAX_HEADS; up to HIF8_CACHE_MAX_SEQS sequences a call
+ * (HIF8_ERR_SHAPE otherwise).  Lengths are taken within what a row can name (table_stride * page_tokens tokens) and starts within the
+ * number of tokens given.  An entry that is no page number (negative, n_pages or more) names no page: its tokens are not written, not
+ * attended to, and read back as zeros.  Sequences may share pages that no call of append writes to.
+ * A ragged batch of tokens (new ones, queries, ones to read) lies sequence by sequence; d_*_start [n_seqs + 1] says where each begins,
+ * in ascending order, and the last entry where the last one ends.  Tokens and heads of such a batch are token_stride and head_stride elements
+ * apart, those of a head contiguous.  16-byte aligned pointers and strides take the vectorised path, others a slower one with identical results.
+ */
+#define HIF8_CACHE_MAX_SEQS 4096
+#define HIF8_CACHE_MAX_HEADS 128
+#define HIF8_CACHE_EXP_MAX 48
+
+/*
+ * New tokens into the cache: those of sequence s take the positions from d_lengths[s] (the tokens it has) on.
+ *   A block whose first slot is written by the call gets its exponent from the largest finite magnitude among the tokens of the call that it
+ *   receives: clamp(target_exp - floor(log2 amax)), 0 for zeros.  A block that has tokens keeps its exponent.  target_exp in [-22, 15]: 3 puts the values
+ *   from amax down to amax / 128 where the format has three mantissa bits, and leaves later tokens of the block 2^12 times that before they overflow.
+ *   code = To_HiF8_<rnd>(x * 2^e), rnd one of HIF8_RND_TA, _HR, _SSR, _TE (HIF8_ERR_ROUND for _SR: what a cache holds does not depend on draws).
+ * k, v: [n_new tokens][kv_heads][head_dim] of src_dtype.  The pages and exponents of the tokens are written, nothing else; d_lengths stays as it is.
+ * No page may receive tokens of two sequences of the same call.
+ */
+int hif8_cache_append(const void* k, const void* v, int src_dtype, int64_t token_stride, int64_t head_stride, const int* d_new_start,
+                      const int* d_lengths, int n_seqs, int n_new, uint8_t* k_pages, uint8_t* v_pages, int* k_exp, int* v_exp, int n_pages,
+                      int kv_heads, int page_tokens, int head_dim, const int* page_table, int64_t table_stride, int target_exp, int rnd,
+                      unsigned flags, hif8_stream_t stream);
+
+/*
+ * Tokens out of the cache: those of sequence s from position d_first[s] on, d_out_start[s + 1] - d_out_start[s] of them, as
+ * value(code) * 2^-e rounded to nearest-even in dst_dtype, to k, v [n_out tokens][kv_heads][head_dim] (rows must not share elements: HIF8_ERR_SHAPE).
+ */
+int hif8_cache_read(const uint8_t* k_pages, const uint8_t* v_pages, const int* k_exp, const int* v_exp, int n_pages, int kv_heads,
+                    int page_tokens, int head_dim, const int* page_table, int64_t table_stride, const int* d_first, const int* d_out_start,
+                    int n_seqs, int n_out, void* k, void* v, int dst_dtype, int64_t token_stride, int64_t head_stride, hif8_stream_t stream);
+
+/*
+ * Sequences that continue from others' pages (beam search, several samples of a prompt): row i of table_out (n_children rows, table_out_stride entries
+ * apart) becomes row d_parent[i] of page_table as far as that sequence has tokens, -1 behind, and d_lengths_out[i] its length.  Where the last page is
+ * partly filled and d_new_page[i] is a page, its contents and exponents are copied there and the child's row names the copy; full pages are shared, and so
+ * is the last one where d_new_page[i] is none (or d_new_page NULL): for the child that keeps it.  Of children that name the same new page the first gets it.
+ * New pages must be free: no page of a row.  table_out and d_lengths_out must not overlap page_table and d_lengths (HIF8_ERR_OVERLAP), so that any child
+ * may continue any parent.  A parent that is none (outside 0 .. n_seqs - 1) gives an empty child.  A length beyond table_out_stride pages is cut there.
+ */
+int hif8_cache_fork(uint8_t* k_pages, uint8_t* v_pages, int* k_exp, int* v_exp, int n_pages, int kv_heads, int page_tokens, int head_dim,
+                    const int* page_table, int64_t table_stride, const int* d_lengths, int n_seqs, const int* d_parent, const int* d_new_page,
+                    int n_children, int* table_out, int64_t table_out_stride, int* d_lengths_out, hif8_stream_t stream);
+
+/*
+ * The pages in use, and the others.  A page is live when a row names it within its sequence's length (a sequence is freed by setting its length to 0; a
+ * page that several rows name is live until the last of them goes).  *d_n_live: the number of live pages.
+ *   move != 0: live pages with numbers from *d_n_live on move (contents and exponents) to the free ones below, the lowest to the lowest, and the rows name their
+ *              new places; pages 0 .. *d_n_live - 1 are then the live ones.  Contents of pages left behind stay as they are.
+ *   move == 0: nothing moves.
+ * d_free_pages [n_pages]: the free pages (after the move) in ascending order, -1 behind them.
+ * workspace: hif8_cache_compact_workspace_bytes(n_pages) bytes, 256-byte aligned, contents irrelevant on entry and undefined on return.
+ */
+int hif8_cache_compact(uint8_t* k_pages, uint8_t* v_pages, int* k_exp, int* v_exp, int n_pages, int kv_heads, int page_tokens, int head_dim,
+                       int* page_table, int64_t table_stride, const int* d_lengths, int n_seqs, int move, int* d_n_live, int* d_free_pages,
+                       void* workspace, size_t workspace_bytes, hif8_stream_t stream);
+size_t hif8_cache_compact_workspace_bytes(int n_pages);
+
+
 /* bytes of device workspace a call needs (which = HIF8_WS_*; n = element count; for HIF8_WS_GEMM: 0 for the
  * minimum, or M*K + K*N for the decode-once path) */
 size_t hif8_workspace_bytes(int which, size_t n);

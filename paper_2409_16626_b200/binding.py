@@ -21,13 +21,15 @@ WS_AMAX_SCALE_ENCODE, WS_FAKE_QUANT, WS_GEMM = 0, 1, 2
 OK = 0
 SCALE_STATE_BYTES, SCALE_HISTORY_MAX = 1024, 32
 ALS_STATE_BYTES = 64
+CACHE_MAX_SEQS, CACHE_MAX_HEADS, CACHE_EXP_MAX = 4096, 128, 48
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libhif8.so")
 EXPORTS = ["hif8_encode", "hif8_decode", "hif8_amax", "hif8_amax_scale_encode", "hif8_fake_quant", "hif8_gemm", "hif8_gemm_status", "hif8_pts_search", "hif8_pts_workspace_bytes",
            "hif8_pts_status", "hif8_selftest_wait_timeout", "hif8_channel_amax_scale_encode", "hif8_gemm_channel_scaled",
            "hif8_scale_state_init", "hif8_delayed_scale_encode", "hif8_gemm_ex", "hif8_encode_transpose", "hif8_als_state_init", "hif8_als_update", "hif8_check_finite", "hif8_encode_from_amax",
-           "hif8_amax_scale_encode_static", "hif8_encode_f32_patterns", "hif8_last_device_status", "hif8_selftest_host_caches", "hif8_gemm_path_policy", "hif8_workspace_bytes", "hif8_status_string", "hif8_launch_count"]
+           "hif8_amax_scale_encode_static", "hif8_encode_f32_patterns", "hif8_last_device_status", "hif8_selftest_host_caches", "hif8_cache_append", "hif8_cache_read", "hif8_cache_fork", "hif8_cache_compact",
+           "hif8_cache_compact_workspace_bytes", "hif8_gemm_path_policy", "hif8_workspace_bytes", "hif8_status_string", "hif8_launch_count"]
 
 for _path in (LIB_PATH, CALL_PATH):
     if not os.path.exists(_path):
@@ -88,6 +90,17 @@ lib.hif8_check_finite.argtypes = [_vp, _i, _sz, _vp, _vp]
 lib.hif8_check_finite.restype = _i
 lib.hif8_encode_from_amax.argtypes = [_vp, _i, _vp, _sz, _i, _i, _u, _u64, _vp, _vp, _vp, _vp]
 lib.hif8_encode_from_amax.restype = _i
+_cache = [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp, _i64]  # pages, exponents, page count, heads, page tokens, head size, page table, its stride
+lib.hif8_cache_append.argtypes = [_vp, _vp, _i, _i64, _i64, _vp, _vp, _i, _i] + _cache + [_i, _i, _u, _vp]
+lib.hif8_cache_append.restype = _i
+lib.hif8_cache_read.argtypes = _cache + [_vp, _vp, _i, _i, _vp, _vp, _i, _i64, _i64, _vp]
+lib.hif8_cache_read.restype = _i
+lib.hif8_cache_fork.argtypes = _cache + [_vp, _i, _vp, _vp, _i, _vp, _i64, _vp, _vp]
+lib.hif8_cache_fork.restype = _i
+lib.hif8_cache_compact.argtypes = _cache + [_vp, _i, _i, _vp, _vp, _vp, _sz, _vp]
+lib.hif8_cache_compact.restype = _i
+lib.hif8_cache_compact_workspace_bytes.argtypes = [_i]
+lib.hif8_cache_compact_workspace_bytes.restype = _sz
 lib.hif8_workspace_bytes.argtypes = [_i, _sz]
 lib.hif8_workspace_bytes.restype = _sz
 lib.hif8_status_string.argtypes = [_i]
@@ -308,6 +321,46 @@ def hif8_encode_from_amax(src, src_dtype, dst, n, target_exp, rnd, flags, seed, 
     args = (src, src_dtype, dst, n, target_exp, rnd, flags, seed, d_amax, d_scale_exp_out, d_scale_out, stream)
     rc = _c.hif8_encode_from_amax(*args)
     return _check(_via_ctypes("hif8_encode_from_amax", args) if rc is None else rc, check)
+
+
+def hif8_cache_append(k, v, src_dtype, token_stride, head_stride, d_new_start, d_lengths, n_seqs, n_new, k_pages, v_pages, k_exp, v_exp, n_pages,
+                      kv_heads, page_tokens, head_dim, page_table, table_stride, target_exp=3, rnd=RND_TA, flags=0, stream=None, check=True):
+    """New tokens' K and V into the pages of a cache (see the header for the cache's layout)."""
+    args = (k, v, src_dtype, token_stride, head_stride, d_new_start, d_lengths, n_seqs, n_new, k_pages, v_pages, k_exp, v_exp, n_pages, kv_heads,
+            page_tokens, head_dim, page_table, table_stride, target_exp, rnd, flags, stream)
+    rc = _c.hif8_cache_append(*args)
+    return _check(_via_ctypes("hif8_cache_append", args) if rc is None else rc, check)
+
+
+def hif8_cache_read(k_pages, v_pages, k_exp, v_exp, n_pages, kv_heads, page_tokens, head_dim, page_table, table_stride, d_first, d_out_start,
+                    n_seqs, n_out, k, v, dst_dtype, token_stride, head_stride, stream=None, check=True):
+    """Cached tokens' K and V back to high precision."""
+    args = (k_pages, v_pages, k_exp, v_exp, n_pages, kv_heads, page_tokens, head_dim, page_table, table_stride, d_first, d_out_start, n_seqs, n_out,
+            k, v, dst_dtype, token_stride, head_stride, stream)
+    rc = _c.hif8_cache_read(*args)
+    return _check(_via_ctypes("hif8_cache_read", args) if rc is None else rc, check)
+
+
+def hif8_cache_fork(k_pages, v_pages, k_exp, v_exp, n_pages, kv_heads, page_tokens, head_dim, page_table, table_stride, d_lengths, n_seqs, d_parent,
+                    d_new_page, n_children, table_out, table_out_stride, d_lengths_out, stream=None, check=True):
+    """Sequences that continue from others' pages: their rows of a new page table, partly filled last pages copied."""
+    args = (k_pages, v_pages, k_exp, v_exp, n_pages, kv_heads, page_tokens, head_dim, page_table, table_stride, d_lengths, n_seqs, d_parent, d_new_page,
+            n_children, table_out, table_out_stride, d_lengths_out, stream)
+    rc = _c.hif8_cache_fork(*args)
+    return _check(_via_ctypes("hif8_cache_fork", args) if rc is None else rc, check)
+
+
+def hif8_cache_compact_workspace_bytes(n_pages):
+    return int(lib.hif8_cache_compact_workspace_bytes(n_pages))
+
+
+def hif8_cache_compact(k_pages, v_pages, k_exp, v_exp, n_pages, kv_heads, page_tokens, head_dim, page_table, table_stride, d_lengths, n_seqs, move,
+                       d_n_live, d_free_pages, workspace, workspace_bytes, stream=None, check=True):
+    """The live pages counted and (move) brought together at the front of the pool, the free ones listed."""
+    args = (k_pages, v_pages, k_exp, v_exp, n_pages, kv_heads, page_tokens, head_dim, page_table, table_stride, d_lengths, n_seqs, int(move), d_n_live,
+            d_free_pages, workspace, workspace_bytes, stream)
+    rc = _c.hif8_cache_compact(*args)
+    return _check(_via_ctypes("hif8_cache_compact", args) if rc is None else rc, check)
 
 
 # the names that the package itself offers (see the package's __getattr__)

@@ -118,6 +118,7 @@ PyMethodDef methods[] = {
     HIF8_ENTRY(hif8_amax_scale_encode_static), HIF8_ENTRY(hif8_fake_quant), HIF8_ENTRY(hif8_gemm), HIF8_ENTRY(hif8_gemm_ex),
     HIF8_ENTRY(hif8_gemm_channel_scaled), HIF8_ENTRY(hif8_channel_amax_scale_encode), HIF8_ENTRY(hif8_delayed_scale_encode),
     HIF8_ENTRY(hif8_encode_transpose), HIF8_ENTRY(hif8_encode_from_amax), HIF8_ENTRY(hif8_als_update), HIF8_ENTRY(hif8_check_finite),
+    HIF8_ENTRY(hif8_cache_append), HIF8_ENTRY(hif8_cache_read), HIF8_ENTRY(hif8_cache_fork), HIF8_ENTRY(hif8_cache_compact),
     {"set_up", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&set_up)), METH_FASTCALL, nullptr},
     {"set_cuda_ready", &set_cuda_ready, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
