@@ -397,7 +397,7 @@ int hif8_pts_status(const void* workspace, hif8_stream_t stream);
  *   page_table        ints, row s (of table_stride entries) lists the pages of sequence s in order: token t lies in slot t % page_tokens
  *                     of page page_table[s * table_stride + t / page_tokens].
  * page_tokens: 16, 32, 64 or 128; head_dim: 64, 128 or 256; kv_heads: 1 .. HIF8_CACHE_MAX_HEADS; up to HIF8_CACHE_MAX_SEQS sequences a call
- * (HIF8_ERR_SHAPE otherwise).  Lengths are taken within what a row can name (table_stride * page_tokens tokens) and starts within the
+ * (HIF8_ERR_SHAPE otherwise).  Lengths are taken within what a row can name (table_stride * page_tokens tokens, at most 2^30) and starts within the
  * number of tokens given.  An entry that is no page number (negative, n_pages or more) names no page: its tokens are not written, not
  * attended to, and read back as zeros.  Sequences may share pages that no call of append writes to.
  * A ragged batch of tokens (new ones, queries, ones to read) lies sequence by sequence; d_*_start [n_seqs + 1] says where each begins,
@@ -406,6 +406,7 @@ int hif8_pts_status(const void* workspace, hif8_stream_t stream);
  */
 #define HIF8_CACHE_MAX_SEQS 4096
 #define HIF8_CACHE_MAX_HEADS 128
+#define HIF8_CACHE_MAX_GROUP 64
 #define HIF8_CACHE_EXP_MAX 48
 
 /*
@@ -429,6 +430,29 @@ int hif8_cache_append(const void* k, const void* v, int src_dtype, int64_t token
 int hif8_cache_read(const uint8_t* k_pages, const uint8_t* v_pages, const int* k_exp, const int* v_exp, int n_pages, int kv_heads,
                     int page_tokens, int head_dim, const int* page_table, int64_t table_stride, const int* d_first, const int* d_out_start,
                     int n_seqs, int n_out, void* k, void* v, int dst_dtype, int64_t token_stride, int64_t head_stride, hif8_stream_t stream);
+
+/*
+ * Attention of queries over the cache: q [n_q queries][heads][head_dim] of `dtype` (HIF8_BF16 or HIF8_F16), out likewise, lse [n_q][heads] floats or NULL.
+ * Query head h looks at key head h / (heads / kv_heads); heads is a multiple of kv_heads, up to HIF8_CACHE_MAX_GROUP times as many (HIF8_ERR_SHAPE).
+ *   s_ij = softmax_scale * sum_d q_i[d] k_j[d],  out_i = sum_j softmax_j(s_ij) v_j,  lse_i = ln sum_j exp(s_ij)
+ * d_lengths[s]: tokens of sequence s in the cache, those of its own queries among them (append first).  The n queries of a sequence stand at its last n
+ * positions: query i at p_i = d_lengths[s] - n + i.  It looks at the cached tokens j
+ *   causal != 0: j <= p_i;  causal == 0: all;   window > 0: only j > p_i - window (window == 0: no such limit).
+ * A query that sees no token (an empty cache, a position below 0, scores that are all -Inf) gives zeros and lse = -Inf.  Tokens that a query does not see never
+ * reach its result, Inf and NaN among them, nor do slots behind a sequence's length.  Inf and NaN that it does see propagate as in IEEE arithmetic.
+ * Products of codes are exact and sums are FP32; the weights of the softmax are rounded to FP16.  softmax_scale: positive and finite (HIF8_ERR_SCALE_RANGE).
+ * max_q and max_length: upper bounds of a sequence's queries and tokens, known to the host.  They have to hold (where they do not, results may be wrong, but no
+ * memory beside the arguments' is touched).
+ * out must not overlap q or the pages.  workspace: at least hif8_cache_attention_workspace_bytes(...) bytes, 256-byte aligned, contents irrelevant on entry and
+ * undefined on return, for one call at a time (two captured graphs that may run at the same time need one each).  Its first int is a device status word as for hif8_gemm
+ * (hif8_gemm_status, hif8_last_device_status).  Where the sum over a sequence's tokens is shared, the parts are added in a fixed order: results are reproducible.
+ */
+int hif8_cache_attention(const void* q, int dtype, int64_t q_token_stride, int64_t q_head_stride, const int* d_q_start, const int* d_lengths,
+                         int n_seqs, int n_q, int max_q, int max_length, const uint8_t* k_pages, const uint8_t* v_pages, const int* k_exp,
+                         const int* v_exp, int n_pages, int kv_heads, int page_tokens, int head_dim, const int* page_table, int64_t table_stride,
+                         int heads, float softmax_scale, int causal, int window, void* out, int64_t out_token_stride, int64_t out_head_stride,
+                         float* lse, void* workspace, size_t workspace_bytes, hif8_stream_t stream);
+size_t hif8_cache_attention_workspace_bytes(int n_seqs, int n_q, int max_q, int max_length, int heads, int kv_heads, int head_dim);
 
 /*
  * Sequences that continue from others' pages (beam search, several samples of a prompt): row i of table_out (n_children rows, table_out_stride entries

@@ -21,14 +21,14 @@ WS_AMAX_SCALE_ENCODE, WS_FAKE_QUANT, WS_GEMM = 0, 1, 2
 OK = 0
 SCALE_STATE_BYTES, SCALE_HISTORY_MAX = 1024, 32
 ALS_STATE_BYTES = 64
-CACHE_MAX_SEQS, CACHE_MAX_HEADS, CACHE_EXP_MAX = 4096, 128, 48
+CACHE_MAX_SEQS, CACHE_MAX_HEADS, CACHE_MAX_GROUP, CACHE_EXP_MAX = 4096, 128, 64, 48
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libhif8.so")
 EXPORTS = ["hif8_encode", "hif8_decode", "hif8_amax", "hif8_amax_scale_encode", "hif8_fake_quant", "hif8_gemm", "hif8_gemm_status", "hif8_pts_search", "hif8_pts_workspace_bytes",
            "hif8_pts_status", "hif8_selftest_wait_timeout", "hif8_channel_amax_scale_encode", "hif8_gemm_channel_scaled",
            "hif8_scale_state_init", "hif8_delayed_scale_encode", "hif8_gemm_ex", "hif8_encode_transpose", "hif8_als_state_init", "hif8_als_update", "hif8_check_finite", "hif8_encode_from_amax",
-           "hif8_amax_scale_encode_static", "hif8_encode_f32_patterns", "hif8_last_device_status", "hif8_selftest_host_caches", "hif8_cache_append", "hif8_cache_read", "hif8_cache_fork", "hif8_cache_compact",
+           "hif8_amax_scale_encode_static", "hif8_encode_f32_patterns", "hif8_last_device_status", "hif8_selftest_host_caches", "hif8_cache_append", "hif8_cache_read", "hif8_cache_attention", "hif8_cache_attention_workspace_bytes", "hif8_cache_fork", "hif8_cache_compact",
            "hif8_cache_compact_workspace_bytes", "hif8_gemm_path_policy", "hif8_workspace_bytes", "hif8_status_string", "hif8_launch_count"]
 
 for _path in (LIB_PATH, CALL_PATH):
@@ -95,6 +95,10 @@ lib.hif8_cache_append.argtypes = [_vp, _vp, _i, _i64, _i64, _vp, _vp, _i, _i] + 
 lib.hif8_cache_append.restype = _i
 lib.hif8_cache_read.argtypes = _cache + [_vp, _vp, _i, _i, _vp, _vp, _i, _i64, _i64, _vp]
 lib.hif8_cache_read.restype = _i
+lib.hif8_cache_attention.argtypes = [_vp, _i, _i64, _i64, _vp, _vp, _i, _i, _i, _i] + _cache + [_i, C.c_float, _i, _i, _vp, _i64, _i64, _vp, _vp, _sz, _vp]
+lib.hif8_cache_attention.restype = _i
+lib.hif8_cache_attention_workspace_bytes.argtypes = [_i] * 7
+lib.hif8_cache_attention_workspace_bytes.restype = _sz
 lib.hif8_cache_fork.argtypes = _cache + [_vp, _i, _vp, _vp, _i, _vp, _i64, _vp, _vp]
 lib.hif8_cache_fork.restype = _i
 lib.hif8_cache_compact.argtypes = _cache + [_vp, _i, _i, _vp, _vp, _vp, _sz, _vp]
@@ -339,6 +343,21 @@ def hif8_cache_read(k_pages, v_pages, k_exp, v_exp, n_pages, kv_heads, page_toke
             k, v, dst_dtype, token_stride, head_stride, stream)
     rc = _c.hif8_cache_read(*args)
     return _check(_via_ctypes("hif8_cache_read", args) if rc is None else rc, check)
+
+
+def hif8_cache_attention_workspace_bytes(n_seqs, n_q, max_q, max_length, heads, kv_heads, head_dim):
+    return int(lib.hif8_cache_attention_workspace_bytes(n_seqs, n_q, max_q, max_length, heads, kv_heads, head_dim))
+
+
+def hif8_cache_attention(q, dtype, q_token_stride, q_head_stride, d_q_start, d_lengths, n_seqs, n_q, max_q, max_length, k_pages, v_pages, k_exp, v_exp,
+                         n_pages, kv_heads, page_tokens, head_dim, page_table, table_stride, heads, softmax_scale, causal, window, out,
+                         out_token_stride, out_head_stride, lse, workspace, workspace_bytes, stream=None, check=True):
+    """Attention of a ragged batch of queries over the cache."""
+    args = (q, dtype, q_token_stride, q_head_stride, d_q_start, d_lengths, n_seqs, n_q, max_q, max_length, k_pages, v_pages, k_exp, v_exp, n_pages, kv_heads,
+            page_tokens, head_dim, page_table, table_stride, heads, softmax_scale, int(causal), window, out, out_token_stride, out_head_stride, lse,
+            workspace, workspace_bytes, stream)
+    rc = _c.hif8_cache_attention(*args)
+    return _check(_via_ctypes("hif8_cache_attention", args) if rc is None else rc, check)
 
 
 def hif8_cache_fork(k_pages, v_pages, k_exp, v_exp, n_pages, kv_heads, page_tokens, head_dim, page_table, table_stride, d_lengths, n_seqs, d_parent,

@@ -32,8 +32,8 @@ struct CacheView {
         const int p = table[(long long)seq * table_stride + block];
         return (unsigned)p < (unsigned)pages ? p : -1;
     }
-    // most tokens that a row of the table can name, and a length within that
-    __host__ __device__ int capacity() const { return table_stride >= (0x7FFFFFFF >> shift) ? 0x7FFFFFFF >> shift << shift : (int)table_stride << shift; }
+    // most tokens that a row of the table can name (up to 2^30), and a length within that
+    __host__ __device__ int capacity() const { return table_stride >= (1 << 30) >> shift ? 1 << 30 : (int)table_stride << shift; }
     __device__ int length(int n) const { return max(0, min(n, capacity())); }
 };
 

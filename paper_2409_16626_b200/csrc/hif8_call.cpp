@@ -65,6 +65,11 @@ bool convert(PyObject* o, T* out)
         if (!to_address(o, &p)) return false;
         *out = static_cast<T>(p);
         return true;
+    } else if constexpr (std::is_floating_point_v<T>) {
+        const double v = PyFloat_AsDouble(o);
+        if (v == -1.0 && PyErr_Occurred()) return false;
+        *out = static_cast<T>(v);
+        return true;
     } else {
         if (PyFloat_Check(o)) return false;
         const unsigned long long v = PyLong_AsUnsignedLongLongMask(o);  // (wraps, as a ctypes integer argument does)
@@ -118,7 +123,7 @@ PyMethodDef methods[] = {
     HIF8_ENTRY(hif8_amax_scale_encode_static), HIF8_ENTRY(hif8_fake_quant), HIF8_ENTRY(hif8_gemm), HIF8_ENTRY(hif8_gemm_ex),
     HIF8_ENTRY(hif8_gemm_channel_scaled), HIF8_ENTRY(hif8_channel_amax_scale_encode), HIF8_ENTRY(hif8_delayed_scale_encode),
     HIF8_ENTRY(hif8_encode_transpose), HIF8_ENTRY(hif8_encode_from_amax), HIF8_ENTRY(hif8_als_update), HIF8_ENTRY(hif8_check_finite),
-    HIF8_ENTRY(hif8_cache_append), HIF8_ENTRY(hif8_cache_read), HIF8_ENTRY(hif8_cache_fork), HIF8_ENTRY(hif8_cache_compact),
+    HIF8_ENTRY(hif8_cache_append), HIF8_ENTRY(hif8_cache_read), HIF8_ENTRY(hif8_cache_attention), HIF8_ENTRY(hif8_cache_fork), HIF8_ENTRY(hif8_cache_compact),
     {"set_up", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&set_up)), METH_FASTCALL, nullptr},
     {"set_cuda_ready", &set_cuda_ready, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
