@@ -404,7 +404,7 @@ int hif8_pts_status(const void* workspace, hif8_stream_t stream);
  * in ascending order, and the last entry where the last one ends.  Tokens and heads of such a batch are token_stride and head_stride elements
  * apart, those of a head contiguous.  16-byte aligned pointers and strides take the vectorised path, others a slower one with identical results.
  */
-#define HIF8_CACHE_MAX_SEQS 4096
+#define HIF8_CACHE_MAX_SEQS 2048
 #define HIF8_CACHE_MAX_HEADS 128
 #define HIF8_CACHE_MAX_GROUP 64
 #define HIF8_CACHE_EXP_MAX 48
@@ -441,6 +441,7 @@ int hif8_cache_read(const uint8_t* k_pages, const uint8_t* v_pages, const int* k
  * A query that sees no token (an empty cache, a position below 0, scores that are all -Inf) gives zeros and lse = -Inf.  Tokens that a query does not see never
  * reach its result, Inf and NaN among them, nor do slots behind a sequence's length.  Inf and NaN that it does see propagate as in IEEE arithmetic.
  * Products of codes are exact and sums are FP32; the weights of the softmax are rounded to FP16.  softmax_scale: positive and finite (HIF8_ERR_SCALE_RANGE).
+ * The pool must have a page and less than 2^31 rows (n_pages * kv_heads * page_tokens), and n_q * heads / kv_heads must stay below 2^30 (HIF8_ERR_SHAPE).
  * max_q and max_length: upper bounds of a sequence's queries and tokens, known to the host.  They have to hold (where they do not, results may be wrong, but no
  * memory beside the arguments' is touched).
  * out must not overlap q or the pages.  workspace: at least hif8_cache_attention_workspace_bytes(...) bytes, 256-byte aligned, contents irrelevant on entry and

@@ -21,7 +21,7 @@ WS_AMAX_SCALE_ENCODE, WS_FAKE_QUANT, WS_GEMM = 0, 1, 2
 OK = 0
 SCALE_STATE_BYTES, SCALE_HISTORY_MAX = 1024, 32
 ALS_STATE_BYTES = 64
-CACHE_MAX_SEQS, CACHE_MAX_HEADS, CACHE_MAX_GROUP, CACHE_EXP_MAX = 4096, 128, 64, 48
+CACHE_MAX_SEQS, CACHE_MAX_HEADS, CACHE_MAX_GROUP, CACHE_EXP_MAX = 2048, 128, 64, 48
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libhif8.so")

@@ -8,11 +8,13 @@
 //   P_ij = 2^(x_ij - m_i + 8),   out_i = sum_j P_ij code_v(j) / sum_j P_ij 2^(e_v(j)),
 // so P <= 2^8 whatever the blocks' spreads are, and nothing is rounded but P (to FP16, 11 bits; products and sums are FP32).  The 2^8 keeps P in the
 // normal range of FP16 down to 2^-22 of the largest.  Exponents lie within +-48, so the denominator stays far inside FP32.
+#include <cuda.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
 #include <atomic>
 #include <cstdint>
+#include <mutex>
 
 #include "hif8.h"
 #include "hif8_cache.cuh"
@@ -101,17 +103,68 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v)
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
     return r;
 }
-__device__ __forceinline__ uint4 ld_stream_v4(const uint8_t* p)
+__device__ __forceinline__ uint4 lds_v4(uint32_t addr)
 {
     uint4 v;
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
     return v;
 }
-__device__ __forceinline__ uint2 ld_stream_v2(const uint8_t* p)
+__device__ __forceinline__ uint2 lds_v2(uint32_t addr)
 {
     uint2 v;
-    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p) : "memory");
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
     return v;
+}
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t e;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+    return e != 0;
+}
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ unsigned long long global_ns()
+{
+    unsigned long long t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+    return t;
+}
+constexpr unsigned long long kWaitLimitNs = 2000000000ull;  // 2 s a wait
+// Bounded wait: false when the barrier did not complete in time, or someone else of the block gave up.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int where)
+{
+    if (mbar_try_wait(bar, parity)) return true;
+    const unsigned long long t0 = global_ns();
+    for (uint32_t it = 1;; it++) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((it & 63u) == 0) {
+            if (*abort_flag) return false;
+            if (global_ns() - t0 > kWaitLimitNs) {
+                *abort_flag = 1;
+                atomicCAS(status, 0, where);
+                return false;
+            }
+        }
+    }
+}
+// a copy that nobody waited for lands before the block's shared memory becomes another's
+__device__ __forceinline__ void wait_landed(uint32_t bar, uint32_t parity)
+{
+    const unsigned long long t0 = global_ns();
+    while (!mbar_try_wait(bar, parity) && global_ns() - t0 < kWaitLimitNs) {}
+}
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1) : "memory");
 }
 // bytes that hold Inf or NaN codes (0x6F, 0xEF, 0x80) become zero
 __device__ __forceinline__ uint32_t finite_codes(uint32_t w)
@@ -145,11 +198,13 @@ __device__ __forceinline__ int lo_of(const AttentionParams& p, const SeqView& v,
 // ---------------------------------------------------------------------------------------------------------
 // Few query rows (decoding, drafted tokens): bound by reading the cache once.
 //
-// A warp multiplies 16 tokens at a time on mma.sync with the tokens as the 16 rows of the A operand and up to 8 NT query rows as columns, so K and V
-// bytes go from global memory to registers, through the lookup, into the operand: S^T = K Q^T, O^T += V^T P^T.  Which of the 16 tokens or 64 elements
-// meet in a product is the operands' own business as long as both agree, so every thread's bytes come in 16-byte loads.  A table of the 256 FP16
-// values with a copy for every lane takes a byte permute and a conflict-free lookup a code.  The tensor-memory path would write every decoded
-// value to shared memory and read it again: eight bytes of shared-memory traffic a code instead of four, and that traffic is what comes next after DRAM here.
+// A warp multiplies 16 tokens at a time on mma.sync with the tokens as the 16 rows of the A operand and up to 8 NT query rows as columns: S^T = K Q^T,
+// O^T += V^T P^T.  Bytes come through a ring of TMA copies of the warp's own, and from there through the lookup into the operands: a table of the 256 FP16
+// values with a copy for every lane takes a byte permute and a conflict-free lookup a code.  The tensor-memory path would write every decoded value to
+// shared memory and read it again, and shared-memory traffic is what comes next after DRAM here.  (Loads straight into registers, a tile ahead, did not
+// cover the latency: 8 sequences of up to 131072 tokens, 64/8 heads of 128: 480 us, 400 of them without any lookup.)
+// Which of the 16 tokens or the elements meet in a product is the operands' own business as long as both agree: a thread's bytes are read 16 at a time, and
+// tokens and pieces are dealt to the threads so that the reads of a swizzled tile never meet in a bank (see token_of_row, piece_of).
 //
 // Chunks of 64 tokens of a (sequence, key head, row tile) are dealt out evenly: group g of four warps takes the chunks [T g / G, T (g + 1) / G) of all
 // T, in order.  A unit whose chunks lie in several groups leaves partial sums in the workspace, which a second kernel adds in a fixed order.
@@ -157,21 +212,55 @@ __device__ __forceinline__ int lo_of(const AttentionParams& p, const SeqView& v,
 constexpr int kGroupWarps = 4, kChunk = 16 * kGroupWarps;
 constexpr uint32_t kLutBytes = 65536;  // rows of 256 bytes on a 64 KiB boundary: the address is one byte permute away from the code
 
+// groups of a block: what registers and shared memory leave room for (128 elements, NT = 1: three groups of 168 registers a thread 351 us where four take 341)
+constexpr int groups_of(int dim, int nt) { return dim == 256 ? 2 : dim == 128 && nt == 2 ? 3 : 4; }
+
+// Shared memory: [prefix sums, maxima and denominators, barriers, rings] table [rings].  The table lies on a 64 KiB boundary; a block's memory begins
+// 1 KiB behind one.
 template <int D, int NT>
 struct RowsShape {
-    static constexpr int kGroups = D == 256 ? 2 : (D == 128 && NT == 2 ? 3 : 4);  // what the registers leave room for
-    static constexpr int kThreads = kGroups * kGroupWarps * 32;
+    static constexpr int kGroups = groups_of(D, NT), kWarps = kGroups * kGroupWarps, kThreads = kWarps * 32;
     static constexpr int kRows = 8 * NT;
-    static constexpr int kPitch = D + 4;                                 // floats of a row of the warps' sums
-    static constexpr uint32_t kSumBytes = kGroupWarps * kRows * kPitch * 4;  // of a group
+    static constexpr int kStages = D == 64 ? 4 : 2;
+    static constexpr uint32_t kTile = 16 * D;                            // bytes of 16 tokens of K or V
+    static constexpr uint32_t kRing = kStages * 2 * kTile;               // of a warp; at a segment's end its sums lie there
+    static constexpr int kBackWarps = 98304 / kRing, kFrontWarps = kWarps > kBackWarps ? kWarps - kBackWarps : 0;  // rings behind / in front of the table
     static constexpr int kRecord = kRows * (D + 2);                      // floats of a partial result: sums, maxima, denominators
-    static constexpr uint32_t kFront = (HIF8_CACHE_MAX_SEQS + 2) * 8 + kGroups * (kGroupWarps * kRows * 8) + 32 * 8 + 16;
-    // what lies in front of the table's boundary (a block's shared memory begins 1 KiB into its window), the table, the sums
-    static constexpr uint32_t kSmem = 2 * kLutBytes - 1024 + kGroups * kSumBytes;
-    static_assert(kFront <= kLutBytes - 2048 && kSmem <= 227 * 1024, "shared memory");
+    // offsets from the block's first byte, which is 1024 modulo 65536
+    static constexpr uint32_t kMl = (HIF8_CACHE_MAX_SEQS + 2) * 8, kScan = kMl + kWarps * kRows * 8, kBars = kScan + 32 * 8, kFlag = kBars + kWarps * kStages * 16;
+    static constexpr uint32_t kFrontRing = kLutBytes - 1024 - kFrontWarps * kRing, kLut = kLutBytes - 1024, kBackRing = kLut + kLutBytes;
+    static constexpr uint32_t kSmem = kBackRing + (kWarps < kBackWarps ? kWarps : kBackWarps) * kRing;
+    static_assert(kFlag + 16 <= kFrontRing && kSmem <= 227 * 1024 && kRows * D * 4 <= kRing, "shared memory");
+    __device__ static uint32_t ring(uint32_t raw, int w) { return raw + (w < kBackWarps ? kBackRing + w * kRing : kFrontRing + (w - kBackWarps) * kRing); }
 };
 
+// token (of a tile's 16) in row r of the A operand: with rows 2 t and 2 t + 1 the tokens that thread t of a column of threads reads V of
+template <int D> __device__ __forceinline__ int token_of_row(int r)
+{
+    const int x = (r & 7) >> 1;
+    return D == 64 ? (x & 1) + 4 * (x >> 1) + 2 * (r & 1) + (r & 8) : x + 4 * (r & 1) + (r & 8);
+}
+// piece of a value row (16 bytes, 8 for D = 64) that the threads of operand row g take
+template <int D> __device__ __forceinline__ int piece_of(int g) { return D == 64 ? g : (g >> 1) | (g & 1) << 2; }
+// byte offset of a 16-byte chunk of a token in a swizzled tile (rows of 128 bytes; of 64 for D = 64; halves of 128 bytes one behind the other for D = 256)
+template <int D> __device__ __forceinline__ uint32_t chunk_at(int token, int chunk)
+{
+    if (D == 64) return (uint32_t)(token * 64 + ((chunk ^ ((token >> 1) & 3)) << 4));
+    return (uint32_t)((chunk >> 3) * 2048 + token * 128 + (((chunk & 7) ^ (token & 7)) << 4));
+}
+// place of float4 number f of row `row` in a warp's sums: neither writing them from the products' layout nor reading rows meets in a bank
+template <int D> __device__ __forceinline__ int sum_at(int row, int f) { return row * (D / 4) + (f ^ ((row >> 1) & 3) ^ (((f >> (D == 64 ? 1 : 4)) & 1) << 2)); }
+
 __device__ __forceinline__ void group_sync(int group) { asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(kGroupWarps * 32) : "memory"); }
+// ... and whether `any` holds in one of the group's threads
+__device__ __forceinline__ bool group_any(int group, bool any)
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %3, 0;\n\tbarrier.cta.red.or.pred q, %1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"(group + 1), "r"(kGroupWarps * 32), "r"((uint32_t)any) : "memory");
+    return r != 0;
+}
+__device__ __forceinline__ long long div_small(long long a, int b) { return a >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b); }
 
 // first chunk of group g
 __host__ __device__ __forceinline__ long long share_of(long long chunks, int g, int groups) { return chunks * g / groups; }
@@ -208,35 +297,43 @@ __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? kN
 __device__ __forceinline__ float part_factor(float m, float top) { return m == kNegInf ? 0.f : exp2_approx(m - top); }
 
 template <int D, int NT, int DT>
-__global__ void __launch_bounds__(RowsShape<D, NT>::kThreads, 1) cache_attention_rows_kernel(const AttentionParams p)
+__global__ void __launch_bounds__(RowsShape<D, NT>::kThreads, 1)
+cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const AttentionParams p)
 {
     using S = RowsShape<D, NT>;
     constexpr int J = D / 64;                       // blocks of 64 elements of a key
-    constexpr int VB = D / 8;                       // bytes of a value row that a thread holds
+    constexpr int VB = D / 8;                       // bytes of a value row that a thread takes
     constexpr int MT = D / 16;                      // m16 tiles of the output
     extern __shared__ unsigned char smem_raw[];
-    const uint32_t raw = smem_u32(smem_raw), lut_base = (raw + kLutBytes - 1) & ~(kLutBytes - 1);
-    long long* s_prefix = reinterpret_cast<long long*>(smem_raw + ((0u - raw) & 15u));
-    float2* s_ml = reinterpret_cast<float2*>(s_prefix + HIF8_CACHE_MAX_SEQS + 2);  // [group][warp][row]
-    long long* s_warp = reinterpret_cast<long long*>(s_ml + S::kGroups * kGroupWarps * S::kRows);
-    float* s_sum = reinterpret_cast<float*>(smem_raw + (lut_base - raw) + kLutBytes);
-    if (lut_base + kLutBytes + S::kGroups * S::kSumBytes > raw + S::kSmem || raw + S::kFront > lut_base) {  // (the same answer in every thread of the grid)
+    const uint32_t raw = smem_u32(smem_raw);
+    long long* s_prefix = reinterpret_cast<long long*>(smem_raw);
+    const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int grp = warp / kGroupWarps, gw = warp % kGroupWarps;
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_raw + S::kFlag);
+    if ((raw & (kLutBytes - 1)) != 1024) {  // (the same answer in every thread of the grid)
         pdl_wait_prior_grid();
         if (blockIdx.x == 0 && threadIdx.x == 0) { *p.status = 7; p.prefix[p.n_seqs] = 0; }
         return;
     }
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int grp = warp / kGroupWarps, gw = warp % kGroupWarps;
-    uint32_t* lut_words = reinterpret_cast<uint32_t*>(smem_raw + (lut_base - raw));
-    for (int i = threadIdx.x; i < 256 * 8; i += S::kThreads) {
-        const uint32_t v = g_f16_of_code.v[i >> 3];
-        *reinterpret_cast<uint4*>(lut_words + (i >> 3) * 64 + (i & 7) * 4) = make_uint4(v, v, v, v);
+    {
+        uint32_t* lut_words = reinterpret_cast<uint32_t*>(smem_raw + S::kLut);
+        for (int i = threadIdx.x; i < 256 * 8; i += S::kThreads) {
+            const uint32_t v = g_f16_of_code.v[i >> 3];
+            *reinterpret_cast<uint4*>(lut_words + (i >> 3) * 64 + (i & 7) * 4) = make_uint4(v, v, v, v);
+        }
     }
+    const uint32_t bars = raw + S::kBars + warp * S::kStages * 16;  // of stage x: keys at 16 x, values at 16 x + 8
+    if (lane == 0) {
+        for (int x = 0; x < 2 * S::kStages; x++) mbar_init(bars + 8 * x, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (threadIdx.x == 0) *abort_flag = 0;
     pdl_wait_prior_grid();
     pdl_launch_dependents();
 
     // chunks in front of each sequence: every thread takes consecutive sequences
     {
+        long long* s_warp = reinterpret_cast<long long*>(smem_raw + S::kScan);
         const int each = (p.n_seqs + S::kThreads - 1) / S::kThreads, s0 = min(p.n_seqs, (int)threadIdx.x * each), s1 = min(p.n_seqs, s0 + each);
         long long mine = 0;
         for (int s = s0; s < s1; s++) {
@@ -269,9 +366,15 @@ __global__ void __launch_bounds__(RowsShape<D, NT>::kThreads, 1) cache_attention
     if (me >= groups) return;
     long long x0 = share_of(chunks, me, groups);
     const long long x_end = share_of(chunks, me + 1, groups);
-    const uint32_t lut = lut_base + 4u * lane;
-    float* my_sum = s_sum + (size_t)grp * (S::kSumBytes / 4);
-    float2* my_ml = s_ml + grp * kGroupWarps * S::kRows;
+    const uint32_t lut = raw + S::kLut + 4u * lane;
+    const uint32_t ring = S::ring(raw, warp);
+    float* my_sum = reinterpret_cast<float*>(smem_raw + (ring - raw));
+    float2* all_ml = reinterpret_cast<float2*>(smem_raw + S::kMl) + grp * kGroupWarps * S::kRows;
+    const int slot_mask = (1 << p.c.shift) - 1;
+    // where this thread reads its bytes of a tile: keys of operand rows g and g + 8, the 16-byte chunks t, t + 4, ..; values of four tokens
+    const int tok_k = token_of_row<D>(g), piece = piece_of<D>(g);
+    uint32_t use = 0;  // uses of the ring by this warp: stage use % kStages, parity (use / kStages) & 1
+    bool ok = true;
 
     while (x0 < x_end) {
         int s = 0;
@@ -282,24 +385,63 @@ __global__ void __launch_bounds__(RowsShape<D, NT>::kThreads, 1) cache_attention
         }
         const SeqView v = seq_view(p, s);
         const SeqChunks k(p, v, S::kRows);
-        const long long in_seq = x0 - s_prefix[s], unit = in_seq / k.per_unit;
+        const long long in_seq = x0 - s_prefix[s], unit = div_small(in_seq, k.per_unit);
         const int c0 = (int)(in_seq - unit * k.per_unit), c1 = (int)min((long long)k.per_unit, c0 + (x_end - x0));
-        const int head = (int)(unit / k.tiles), r0 = (int)(unit - (long long)head * k.tiles) * S::kRows;
+        const int head = (int)div_small(unit, k.tiles), r0 = (int)(unit - (long long)head * k.tiles) * S::kRows;
         const int n_rows = (int)min((long long)S::kRows, (long long)v.n_q * p.group - r0);
-        const int ia = r0 / p.group, ib = (r0 + n_rows - 1) / p.group;  // first and last query of the tile
-        const int hi_min = min(v.len, hi_of(p, v, ia)), hi_max = min(v.len, hi_of(p, v, ib)), lo_min = lo_of(p, v, ia), lo_max = lo_of(p, v, ib);
+        const int q0 = r0 / p.group, h0 = r0 - q0 * p.group;  // query and head of the tile's first row
+        const uint32_t magic = 65536u / (uint32_t)p.group + 1u;  // x / group = x magic >> 16 for the x < group + 16 that come up
+        auto query_of = [&](int row) -> int { return q0 + (int)((uint32_t)(h0 + row) * magic >> 16); };
+        auto head_of = [&](int row) -> int { return head * p.group + h0 + row - (int)((uint32_t)(h0 + row) * magic >> 16) * p.group; };
+        const int ib = query_of(n_rows - 1);
+        const int hi_min = min(v.len, hi_of(p, v, q0)), hi_max = min(v.len, hi_of(p, v, ib)), lo_min = lo_of(p, v, q0), lo_max = lo_of(p, v, ib);
+
+        // Tiles of this warp: lane n holds page row and exponents of that of the n-th chunk of a batch of 32; a tile without a page, or with no token
+        // that a row sees, is left out.  Tiles are asked for kStages ahead; `ahead` holds first tokens and exponents of those on their way.
+        int b_row = -1, b_exps = 0, b_first = c0;
+        uint32_t b_live = 0;
+        auto load_batch = [&](int c) {
+            b_first = c;
+            const int at = k.lo + (c + lane) * kChunk + 16 * gw;  // (below 2^31: a length, at most 2^30, and less than 2^12 more)
+            const int page = c + lane < c1 && at < hi_max && at + 16 > lo_min ? p.c.page_of(s, at >> p.c.shift) : -1;
+            const long long e = (long long)max(page, 0) * p.c.heads + head;
+            b_exps = page >= 0 ? (clamp_cache_exp(p.c.k_exp[e]) & 0xFF) | clamp_cache_exp(p.c.v_exp[e]) << 8 : 0;
+            b_row = (int)(e << p.c.shift) + (at & slot_mask);  // (rows of a pool number less than 2^31)
+            b_live = __ballot_sync(0xFFFFFFFFu, page >= 0);
+        };
+        int ahead_t0[S::kStages], ahead_exps[S::kStages];
+        auto ask = [&](uint32_t n, int& t0, int& exps) {  // the next tile into the place of use n; t0 = -1: there is none
+            while (!b_live && b_first + 32 < c1) load_batch(b_first + 32);
+            t0 = -1;
+            if (!b_live || !ok) return;
+            const int i = __ffs(b_live) - 1, row = __shfl_sync(0xFFFFFFFFu, b_row, i);
+            exps = __shfl_sync(0xFFFFFFFFu, b_exps, i);
+            t0 = k.lo + (b_first + i) * kChunk + 16 * gw;
+            b_live &= b_live - 1;
+            const uint32_t st = n % S::kStages, at = ring + st * 2 * S::kTile, bar = bars + 16 * st;
+            __syncwarp();  // every lane has read what the stage held
+            if (elect_one()) {
+                mbar_expect(bar, S::kTile);
+                tma_load_2d(at, &map_k, 0, row, bar);
+                if (D == 256) tma_load_2d(at + 2048, &map_k, 128, row, bar);
+                mbar_expect(bar + 8, S::kTile);
+                tma_load_2d(at + S::kTile, &map_v, 0, row, bar + 8);
+                if (D == 256) tma_load_2d(at + S::kTile + 2048, &map_v, 128, row, bar + 8);
+            }
+            __syncwarp();
+        };
+        load_batch(c0);
+#pragma unroll
+        for (int x = 0; x < S::kStages; x++) ask(use + x, ahead_t0[x], ahead_exps[x]);
 
         // queries: column g of n8 tile i is row r0 + 8 i + g; a thread takes the elements 64 j + 16 t .. + 15
         uint32_t qb[NT][J][4][2];
         float row_mul[NT][2];
-        int row_lo[NT][2], row_hi[NT][2];
 #pragma unroll
         for (int i = 0; i < NT; i++) {
-            const int r = r0 + 8 * i + g;
             uint32_t w[J][8];
             if (8 * i + g < n_rows) {
-                const int qi = r / p.group;
-                const long long at = (long long)(v.first + qi) * p.q_token + (long long)(head * p.group + r - qi * p.group) * p.q_head + 16 * t;
+                const long long at = (long long)(v.first + query_of(8 * i + g)) * p.q_token + (long long)head_of(8 * i + g) * p.q_head + 16 * t;
                 const unsigned short* src = reinterpret_cast<const unsigned short*>(p.q) + at;
 #pragma unroll
                 for (int j = 0; j < J; j++) {
@@ -339,13 +481,8 @@ __global__ void __launch_bounds__(RowsShape<D, NT>::kThreads, 1) cache_attention
 #pragma unroll
                 for (int st = 0; st < 4; st++) { qb[i][j][st][0] = w[j][2 * st]; qb[i][j][st][1] = w[j][2 * st + 1]; }
 #pragma unroll
-            for (int b = 0; b < 2; b++) {  // the scores' columns of this thread: rows 2 t and 2 t + 1 of the tile
-                const int re = __shfl_sync(0xFFFFFFFFu, e, 4 * (2 * t + b)), row = 8 * i + 2 * t + b;
-                const int qi = (r0 + row) / p.group;
-                row_mul[i][b] = fminf(p.scale_log2 * pow2_clamped(-re), 3.0e38f);
-                row_hi[i][b] = row < n_rows ? min(v.len, hi_of(p, v, qi)) : v.len;  // (columns without a row compute something that nobody reads)
-                row_lo[i][b] = row < n_rows ? lo_of(p, v, qi) : 0;
-            }
+            for (int b = 0; b < 2; b++)  // the scores' columns of this thread: rows 2 t and 2 t + 1 of the tile
+                row_mul[i][b] = fminf(p.scale_log2 * pow2_clamped(-__shfl_sync(0xFFFFFFFFu, e, 4 * (2 * t + b))), 3.0e38f);
         }
 
         float m[NT][2], l[NT][2], o[NT][MT][4];
@@ -359,165 +496,139 @@ __global__ void __launch_bounds__(RowsShape<D, NT>::kThreads, 1) cache_attention
                 for (int y = 0; y < 4; y++) o[i][x][y] = 0.f;
         }
 
-        // pages and exponents of this warp's tiles: lane n holds those of the n-th chunk of a batch of 32
-        int b_page = -1, b_ke = 0, b_ve = 0, b_first = c0;
-        auto load_batch = [&](int c) {
-            b_first = c;
-            const int at = k.lo + (c + lane) * kChunk + 16 * gw;  // (below 2^31: a length, at most 2^30, and less than 2^12 more)
-            b_page = c + lane < c1 && at < v.len ? p.c.page_of(s, at >> p.c.shift) : -1;
-            const long long e = (long long)max(b_page, 0) * p.c.heads + head;
-            b_ke = b_page >= 0 ? clamp_cache_exp(p.c.k_exp[e]) : 0;
-            b_ve = b_page >= 0 ? clamp_cache_exp(p.c.v_exp[e]) : 0;
-        };
-        uint4 kw[2][J];       // rows g and g + 8
-        uint32_t vw[4][VB / 4];  // tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9
-        auto tile_of = [&](int c) -> int { return k.lo + c * kChunk + 16 * gw; };
-        auto load_k = [&](int page, int t0) {
+        while (ahead_t0[0] >= 0) {
+            const int t0 = ahead_t0[0], exps = ahead_exps[0];
+            const uint32_t st = use % S::kStages, parity = (use / S::kStages) & 1u, at_k = ring + st * 2 * S::kTile, at_v = at_k + S::kTile, bar = bars + 16 * st;
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag, p.status, 61));
+            if (!ok) break;
+            // scores, transposed: operand row g (+ 8) x rows 2 t, 2 t + 1.  (Two sums, so that a product does not wait for the one in front of it.)
+            float sc[NT][4], sd[NT][4];
 #pragma unroll
-            for (int h = 0; h < 2; h++) {
-                const int tok = t0 + g + 8 * h;
-                const bool in = page >= 0 && tok >= lo_min && tok < hi_max;
-                const uint8_t* src = p.c.k + p.c.block_at(max(page, 0), head) + (long long)(tok & ((1 << p.c.shift) - 1)) * D + 16 * t;
-#pragma unroll
-                for (int j = 0; j < J; j++) kw[h][j] = in ? ld_stream_v4(src + 64 * j) : make_uint4(0, 0, 0, 0);
+            for (int i = 0; i < NT; i++) {
+                sc[i][0] = sc[i][1] = sc[i][2] = sc[i][3] = 0.f;
+                sd[i][0] = sd[i][1] = sd[i][2] = sd[i][3] = 0.f;
             }
-        };
-        auto load_v = [&](int page, int t0) {
+#pragma unroll
+            for (int j = 0; j < J; j++) {
+                const uint4 ka = lds_v4(at_k + chunk_at<D>(tok_k, 4 * j + t)), kb = lds_v4(at_k + chunk_at<D>(tok_k + 8, 4 * j + t));
+                const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
+#pragma unroll
+                for (int q = 0; q < 4; q++) {
+                    const uint32_t a0 = __byte_perm(lds_u32(__byte_perm(wa[q], lut, 0x7604)), lds_u32(__byte_perm(wa[q], lut, 0x7614)), 0x5410);
+                    const uint32_t a2 = __byte_perm(lds_u32(__byte_perm(wa[q], lut, 0x7624)), lds_u32(__byte_perm(wa[q], lut, 0x7634)), 0x5410);
+                    const uint32_t a1 = __byte_perm(lds_u32(__byte_perm(wb[q], lut, 0x7604)), lds_u32(__byte_perm(wb[q], lut, 0x7614)), 0x5410);
+                    const uint32_t a3 = __byte_perm(lds_u32(__byte_perm(wb[q], lut, 0x7624)), lds_u32(__byte_perm(wb[q], lut, 0x7634)), 0x5410);
+#pragma unroll
+                    for (int i = 0; i < NT; i++) mma_16816_f16(q & 1 ? sd[i] : sc[i], a0, a1, a2, a3, qb[i][j][q][0], qb[i][j][q][1]);
+                }
+            }
+            const bool whole = t0 >= lo_max && t0 + 16 <= hi_min;  // every row sees every token
+            const int ke = (int)(signed char)(exps & 0xFF), ve = exps >> 8;
+            const float k_mul = pow2f(-ke), v_mul = pow2f(ve), v_add = (float)-ve;
+            float top[NT][2];
+            bool grows = false;
+#pragma unroll
+            for (int i = 0; i < NT; i++) {
+#pragma unroll
+                for (int b = 0; b < 2; b++) {
+                    const float f = fminf(row_mul[i][b] * k_mul, 3.0e38f);
+#pragma unroll
+                    for (int h = 0; h < 2; h++) sc[i][2 * h + b] = fmaf(sc[i][2 * h + b] + sd[i][2 * h + b], f, v_add);
+                    if (!whole) {
+                        const int row = 8 * i + 2 * t + b, qi = query_of(row);
+                        const int hi = row < n_rows ? min(v.len, hi_of(p, v, qi)) : v.len, lo = row < n_rows ? lo_of(p, v, qi) : 0;  // (nobody reads columns without a row)
+#pragma unroll
+                        for (int h = 0; h < 2; h++) {
+                            const int tok = t0 + tok_k + 8 * h;
+                            if (tok < lo || tok >= hi) sc[i][2 * h + b] = kNegInf;
+                        }
+                    }
+                    float a = fmaxf(sc[i][b], sc[i][2 + b]);
+                    a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 4));
+                    a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 8));
+                    a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 16));
+                    top[i][b] = a;
+                    grows |= a > m[i][b];
+                }
+            }
+            if (__any_sync(0xFFFFFFFFu, grows)) {
+#pragma unroll
+                for (int i = 0; i < NT; i++)
+#pragma unroll
+                    for (int b = 0; b < 2; b++) {
+                        const float n = fmaxf(m[i][b], top[i][b]), f = part_factor(m[i][b], n);
+                        m[i][b] = n;
+                        l[i][b] *= f;
+#pragma unroll
+                        for (int x = 0; x < MT; x++) { o[i][x][b] *= f; o[i][x][2 + b] *= f; }
+                    }
+            }
+            uint32_t pb[NT][2];
+#pragma unroll
+            for (int i = 0; i < NT; i++) {
+                float e[4];
+#pragma unroll
+                for (int b = 0; b < 2; b++) {
+                    const float base = m[i][b] == kNegInf ? 0.f : m[i][b];
+                    e[b] = exp2_approx(sc[i][b] - base + kPShift);  // (the difference is exact where it counts; base - 8 is not for large scores)
+                    e[2 + b] = exp2_approx(sc[i][2 + b] - base + kPShift);
+                    l[i][b] = fmaf(e[b] + e[2 + b], v_mul, l[i][b]);
+                }
+                pb[i][0] = transpose_8x8(pack_f16(e[0], e[1]));
+                pb[i][1] = transpose_8x8(pack_f16(e[2], e[3]));
+            }
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar + 8, parity, abort_flag, p.status, 62));
+            if (!ok) break;
+            uint32_t vw[4][VB / 4];  // of the tokens in operand rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9
 #pragma unroll
             for (int h = 0; h < 4; h++) {
-                const int tok = t0 + 2 * t + (h & 1) + 8 * (h >> 1);
-                const bool in = page >= 0 && tok >= lo_min && tok < hi_max;
-                const uint8_t* src = p.c.v + p.c.block_at(max(page, 0), head) + (long long)(tok & ((1 << p.c.shift) - 1)) * D;
+                const int tok = token_of_row<D>(2 * t + (h & 1) + 8 * (h >> 1));
                 if (D == 64) {
-                    const uint2 a = in ? ld_stream_v2(src + 8 * g) : make_uint2(0, 0);
+                    const uint2 a = lds_v2(at_v + chunk_at<D>(tok, piece >> 1) + 8 * (piece & 1));
                     vw[h][0] = a.x; vw[h][1] = a.y;
                 } else {
 #pragma unroll
                     for (int y = 0; y < VB / 16; y++) {
-                        const uint4 a = in ? ld_stream_v4(src + 128 * y + 16 * g) : make_uint4(0, 0, 0, 0);
+                        const uint4 a = lds_v4(at_v + chunk_at<D>(tok, 8 * y + piece));
                         vw[h][4 * y] = a.x; vw[h][4 * y + 1] = a.y; vw[h][(4 * y + 2) % (VB / 4)] = a.z; vw[h][(4 * y + 3) % (VB / 4)] = a.w;
                     }
                 }
-            }
-        };
-
-        load_batch(c0);
-        int page = __shfl_sync(0xFFFFFFFFu, b_page, 0), ke = __shfl_sync(0xFFFFFFFFu, b_ke, 0), ve = __shfl_sync(0xFFFFFFFFu, b_ve, 0);
-        load_k(page, tile_of(c0));
-        load_v(page, tile_of(c0));
-        for (int c = c0; c < c1; c++) {
-            const int t0 = tile_of(c);
-            // scores, transposed: token g (+ 8) x rows 2 t, 2 t + 1
-            float sc[NT][4];
+                // What no row sees is not there; of what some rows see and others do not, Inf and NaN are left out, since 0 times them would reach the
+                // others: cache_attention_specials_kernel adds them to the rows that do see them.
+                if (!whole) {
+                    const bool in = t0 + tok >= lo_min && t0 + tok < hi_max;
+                    const bool mixed = t0 + tok >= hi_min || t0 + tok < lo_max;
 #pragma unroll
-            for (int i = 0; i < NT; i++) sc[i][0] = sc[i][1] = sc[i][2] = sc[i][3] = 0.f;
-#pragma unroll
-            for (int j = 0; j < J; j++) {
-                const uint32_t wa[4] = {kw[0][j].x, kw[0][j].y, kw[0][j].z, kw[0][j].w}, wb[4] = {kw[1][j].x, kw[1][j].y, kw[1][j].z, kw[1][j].w};
-#pragma unroll
-                for (int st = 0; st < 4; st++) {
-                    const uint32_t a0 = __byte_perm(lds_u32(__byte_perm(wa[st], lut, 0x7604)), lds_u32(__byte_perm(wa[st], lut, 0x7614)), 0x5410);
-                    const uint32_t a2 = __byte_perm(lds_u32(__byte_perm(wa[st], lut, 0x7624)), lds_u32(__byte_perm(wa[st], lut, 0x7634)), 0x5410);
-                    const uint32_t a1 = __byte_perm(lds_u32(__byte_perm(wb[st], lut, 0x7604)), lds_u32(__byte_perm(wb[st], lut, 0x7614)), 0x5410);
-                    const uint32_t a3 = __byte_perm(lds_u32(__byte_perm(wb[st], lut, 0x7624)), lds_u32(__byte_perm(wb[st], lut, 0x7634)), 0x5410);
-#pragma unroll
-                    for (int i = 0; i < NT; i++) mma_16816_f16(sc[i], a0, a1, a2, a3, qb[i][j][st][0], qb[i][j][st][1]);
+                    for (int y = 0; y < VB / 4; y++) vw[h][y] = !in ? 0u : mixed ? finite_codes(vw[h][y]) : vw[h][y];
                 }
             }
-            // the next tile's keys are on their way while this one's values are multiplied
-            int n_page = -1, n_ke = 0, n_ve = 0;
-            if (c + 1 < c1) {
-                if (c + 1 - b_first == 32) load_batch(c + 1);
-                n_page = __shfl_sync(0xFFFFFFFFu, b_page, c + 1 - b_first);
-                n_ke = __shfl_sync(0xFFFFFFFFu, b_ke, c + 1 - b_first);
-                n_ve = __shfl_sync(0xFFFFFFFFu, b_ve, c + 1 - b_first);
-                load_k(n_page, tile_of(c + 1));
-            }
-            const bool whole = page >= 0 && t0 >= lo_max && t0 + 16 <= hi_min;  // every row sees every token
-            const float k_mul = pow2f(-ke), v_mul = pow2f(ve), v_add = (float)-ve;
-            if (page >= 0 && t0 < hi_max && t0 + 16 > lo_min) {  // (the same in the whole warp)
-                float top[NT][2];
-                bool grows = false;
 #pragma unroll
-                for (int i = 0; i < NT; i++) {
+            for (int x = 0; x < MT; x++) {  // element pair x of the thread's bytes: row g the first, row g + 8 the second
+                const int wd = x / 2;
+                uint32_t a[4];
 #pragma unroll
-                    for (int b = 0; b < 2; b++) {
-                        const float f = fminf(row_mul[i][b] * k_mul, 3.0e38f);
+                for (int b = 0; b < 2; b++)
 #pragma unroll
-                        for (int h = 0; h < 2; h++) {
-                            float x = fmaf(sc[i][2 * h + b], f, v_add);
-                            if (!whole) {
-                                const int tok = t0 + g + 8 * h;
-                                if (tok < row_lo[i][b] || tok >= row_hi[i][b]) x = kNegInf;
-                            }
-                            sc[i][2 * h + b] = x;
-                        }
-                        float a = fmaxf(sc[i][b], sc[i][2 + b]);
-                        a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 4));
-                        a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 8));
-                        a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 16));
-                        top[i][b] = a;
-                        grows |= a > m[i][b];
+                    for (int h = 0; h < 2; h++) {
+                        const uint32_t sel = 0x7604u + 0x10u * (uint32_t)(2 * (x & 1) + b);
+                        a[2 * h + b] = __byte_perm(lds_u32(__byte_perm(vw[2 * h][wd], lut, sel)), lds_u32(__byte_perm(vw[2 * h + 1][wd], lut, sel)), 0x5410);
                     }
-                }
-                if (__any_sync(0xFFFFFFFFu, grows)) {
 #pragma unroll
-                    for (int i = 0; i < NT; i++)
-#pragma unroll
-                        for (int b = 0; b < 2; b++) {
-                            const float n = fmaxf(m[i][b], top[i][b]), f = part_factor(m[i][b], n);
-                            m[i][b] = n;
-                            l[i][b] *= f;
-#pragma unroll
-                            for (int x = 0; x < MT; x++) { o[i][x][b] *= f; o[i][x][2 + b] *= f; }
-                        }
-                }
-                uint32_t pb[NT][2];
-#pragma unroll
-                for (int i = 0; i < NT; i++) {
-                    float e[4];
-#pragma unroll
-                    for (int b = 0; b < 2; b++) {
-                        const float base = m[i][b] == kNegInf ? 0.f : m[i][b];
-                        e[b] = exp2_approx(sc[i][b] - base + kPShift);  // (the difference is exact where it counts; base - 8 is not for large scores)
-                        e[2 + b] = exp2_approx(sc[i][2 + b] - base + kPShift);
-                        l[i][b] = fmaf(e[b] + e[2 + b], v_mul, l[i][b]);
-                    }
-                    pb[i][0] = transpose_8x8(pack_f16(e[0], e[1]));
-                    pb[i][1] = transpose_8x8(pack_f16(e[2], e[3]));
-                }
-                if (!whole && (hi_min < hi_max || lo_min < lo_max)) {
-                    // Some rows see a token that others do not, and 0 times an Inf or NaN would reach those: such codes are left out here, and
-                    // cache_attention_specials_kernel adds them to the rows that do see them.
-                    const bool mixed = t0 + 16 > hi_min || t0 < lo_max;
-                    if (mixed) {
-#pragma unroll
-                        for (int h = 0; h < 4; h++)
-#pragma unroll
-                            for (int y = 0; y < VB / 4; y++) vw[h][y] = finite_codes(vw[h][y]);
-                    }
-                }
-#pragma unroll
-                for (int x = 0; x < MT; x++) {  // element pair x of the thread's bytes: row g the first, row g + 8 the second
-                    const int wd = x / 2;
-                    uint32_t a[4];
-#pragma unroll
-                    for (int b = 0; b < 2; b++)
-#pragma unroll
-                        for (int h = 0; h < 2; h++) {
-                            const int by = 2 * (x & 1) + b;
-                            const uint32_t sel = 0x7604u + 0x10u * (uint32_t)by;
-                            a[2 * h + b] = __byte_perm(lds_u32(__byte_perm(vw[2 * h][wd], lut, sel)), lds_u32(__byte_perm(vw[2 * h + 1][wd], lut, sel)), 0x5410);
-                        }
-#pragma unroll
-                    for (int i = 0; i < NT; i++) mma_16816_f16(o[i][x], a[0], a[1], a[2], a[3], pb[i][0], pb[i][1]);
-                }
+                for (int i = 0; i < NT; i++) mma_16816_f16(o[i][x], a[0], a[1], a[2], a[3], pb[i][0], pb[i][1]);
             }
-            if (c + 1 < c1) load_v(n_page, tile_of(c + 1));
-            page = n_page; ke = n_ke; ve = n_ve;
+#pragma unroll
+            for (int x = 0; x + 1 < S::kStages; x++) { ahead_t0[x] = ahead_t0[x + 1]; ahead_exps[x] = ahead_exps[x + 1]; }
+            ask(use + S::kStages, ahead_t0[S::kStages - 1], ahead_exps[S::kStages - 1]);
+            use++;
+        }
+        if (!ok) {  // copies on their way land before the ring is used for anything else
+            for (int x = 0; x < S::kStages; x++)
+                if (ahead_t0[x] >= 0)
+                    for (int y = 0; y < 2; y++) wait_landed(bars + 16 * ((use + x) % S::kStages) + 8 * y, ((use + x) / S::kStages) & 1u);
+            __syncwarp();
         }
 
-        // ---- the four warps' sums of the segment
+        // ---- the four warps' sums of the segment, each in its own ring
 #pragma unroll
         for (int i = 0; i < NT; i++)
 #pragma unroll
@@ -525,54 +636,44 @@ __global__ void __launch_bounds__(RowsShape<D, NT>::kThreads, 1) cache_attention
                 l[i][b] += __shfl_xor_sync(0xFFFFFFFFu, l[i][b], 4);
                 l[i][b] += __shfl_xor_sync(0xFFFFFFFFu, l[i][b], 8);
                 l[i][b] += __shfl_xor_sync(0xFFFFFFFFu, l[i][b], 16);
-                if (g == 0) my_ml[gw * S::kRows + 8 * i + 2 * t + b] = make_float2(m[i][b], l[i][b]);
-            }
-        group_sync(grp);
-#pragma unroll
-        for (int i = 0; i < NT; i++)
-#pragma unroll
-            for (int b = 0; b < 2; b++) {
                 const int row = 8 * i + 2 * t + b;
-                float top = kNegInf;
-#pragma unroll
-                for (int w = 0; w < kGroupWarps; w++) top = fmaxf(top, my_ml[w * S::kRows + row].x);
-                const float f = part_factor(m[i][b], top);
-                float* to = my_sum + (gw * S::kRows + row) * S::kPitch;
+                if (g == 0) all_ml[gw * S::kRows + row] = make_float2(m[i][b], l[i][b]);
 #pragma unroll
                 for (int x = 0; x < MT; x += 2) {
-                    const int d = D == 64 ? 8 * g + 2 * x : 128 * (x / 8) + 16 * g + 2 * (x % 8);
-                    *reinterpret_cast<float4*>(to + d) = make_float4(o[i][x][b] * f, o[i][x][2 + b] * f, o[i][x + 1][b] * f, o[i][x + 1][2 + b] * f);
+                    const int d = D == 64 ? 8 * piece + 2 * x : 128 * (x / 8) + 16 * piece + 2 * (x % 8);
+                    reinterpret_cast<float4*>(my_sum)[sum_at<D>(row, d / 4)] = make_float4(o[i][x][b], o[i][x][2 + b], o[i][x + 1][b], o[i][x + 1][2 + b]);
                 }
             }
         group_sync(grp);
         const bool is_whole = c0 == 0 && c1 == k.per_unit;
         float* record = p.partial + (size_t)(2 * me + (c0 == 0 ? 1 : 0)) * S::kRecord;
         for (int i = gw * 32 + lane; i < n_rows * (D / 4); i += kGroupWarps * 32) {
-            const int row = i / (D / 4), d = (i - row * (D / 4)) * 4;
-            float top = kNegInf, den = 0.f;
+            const int row = i / (D / 4), f = i % (D / 4);
+            float2 ml[kGroupWarps];
+            float top = kNegInf, den = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < kGroupWarps; w++) top = fmaxf(top, my_ml[w * S::kRows + row].x);
-#pragma unroll
-            for (int w = 0; w < kGroupWarps; w++) den += my_ml[w * S::kRows + row].y * part_factor(my_ml[w * S::kRows + row].x, top);
-            float x[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int w = 0; w < kGroupWarps; w++) { ml[w] = all_ml[w * S::kRows + row]; top = fmaxf(top, ml[w].x); }
 #pragma unroll
             for (int w = 0; w < kGroupWarps; w++) {
-                const float4 a = *reinterpret_cast<const float4*>(my_sum + (w * S::kRows + row) * S::kPitch + d);
-                x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w;
+                const float h = part_factor(ml[w].x, top);
+                den += ml[w].y * h;
+                const float4 a = reinterpret_cast<const float4*>(smem_raw + (S::ring(raw, grp * kGroupWarps + w) - raw))[sum_at<D>(row, f)];
+                x[0] += a.x * h; x[1] += a.y * h; x[2] += a.z * h; x[3] += a.w * h;
             }
             if (is_whole) {
-                const int r = r0 + row, qi = r / p.group, h = head * p.group + r - qi * p.group;
+                const int qi = query_of(row), h = head_of(row);
                 const float inv = den == 0.f ? 0.f : 1.f / den;
 #pragma unroll
                 for (int y = 0; y < 4; y++) x[y] *= inv;
-                store_out4<DT>(p, (long long)(v.first + qi) * p.out_token + (long long)h * p.out_head + d, x);
-                if (p.lse && d == 0) p.lse[(long long)(v.first + qi) * p.heads + h] = lse_of(top, den);
+                store_out4<DT>(p, (long long)(v.first + qi) * p.out_token + (long long)h * p.out_head + 4 * f, x);
+                if (p.lse && f == 0) p.lse[(long long)(v.first + qi) * p.heads + h] = lse_of(top, den);
             } else {
-                *reinterpret_cast<float4*>(record + row * D + d) = make_float4(x[0], x[1], x[2], x[3]);
-                if (d == 0) { record[S::kRows * D + 2 * row] = top; record[S::kRows * D + 2 * row + 1] = den; }
+                *reinterpret_cast<float4*>(record + row * D + 4 * f) = make_float4(x[0], x[1], x[2], x[3]);
+                if (f == 0) *reinterpret_cast<float2*>(record + S::kRows * D + 2 * row) = make_float2(top, den);
             }
         }
-        group_sync(grp);  // the sums' place is free again
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the ring is the copies' again
+        if (group_any(grp, !ok)) break;
         x0 += c1 - c0;
     }
 }
@@ -607,6 +708,7 @@ __global__ void __launch_bounds__(kCombineThreads) cache_attention_combine_kerne
     for (int i = threadIdx.x; i < n_rows * (D / 4); i += kCombineThreads) {
         const int row = i / (D / 4), d = (i - row * (D / 4)) * 4;
         float top = kNegInf, den = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
         for (int j = 0; j < parts; j++) {
             const float* r = record(j);
             const float2 ml = *reinterpret_cast<const float2*>(r + S::kRows * D + 2 * row);
@@ -673,7 +775,7 @@ __global__ void __launch_bounds__(kThreads) cache_attention_specials_kernel(cons
 // ---------------------------------------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------------------------------------
-constexpr int kMaxGroups = 148 * 4;
+constexpr int kMaxBlocks = 148;
 constexpr size_t kHeadBytes = 256 + ((size_t)HIF8_CACHE_MAX_SEQS + 1) * 8 + 248;  // status word, chunks in front of each sequence
 static_assert(kHeadBytes % 256 == 0, "what follows is aligned");
 
@@ -684,8 +786,32 @@ int row_tiles_of(int max_q, int group, int dim) { return (long long)max_q * grou
 
 size_t partial_bytes(int dim, int nt)
 {
-    const int per_cta = dim == 256 ? 2 : (dim == 128 && nt == 2 ? 3 : 4);
-    return round_up_256((size_t)2 * (kMaxGroups / 4 * per_cta) * 8 * nt * (dim + 2) * 4);
+    return round_up_256((size_t)2 * (kMaxBlocks * groups_of(dim, nt)) * 8 * nt * (dim + 2) * 4);
+}
+
+// The pool of K or V as rows of head_dim bytes, boxes of 16 tokens (128 bytes of each at most), swizzled.  Encoded anew in every call: it holds no more than
+// the address and the sizes.
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_tiled_fn()
+{
+    static EncodeTiledFn fn = nullptr;
+    static std::once_flag once;
+    std::call_once(once, [] {
+        void* sym = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess) fn = reinterpret_cast<EncodeTiledFn>(sym);
+    });
+    return fn;
+}
+bool pool_map(CUtensorMap* map, const void* pool, const CacheView& c)
+{
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)c.dim, (cuuint64_t)c.pages * c.heads << c.shift}, strides[1] = {(cuuint64_t)c.dim};
+    const cuuint32_t box[2] = {(cuuint32_t)(c.dim < 128 ? c.dim : 128), 16}, one[2] = {1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(pool), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              c.dim == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 struct DeviceSetup {
@@ -712,7 +838,7 @@ cudaError_t launch_rows(const AttentionParams& p, int sms, cudaStream_t st)
 {
     using S = RowsShape<D, NT>;
     cudaLaunchConfig_t cfg{};
-    const int ctas = sms < kMaxGroups / 4 ? sms : kMaxGroups / 4;
+    const int ctas = sms < kMaxBlocks ? sms : kMaxBlocks;
     cfg.gridDim = dim3((unsigned)ctas);
     cfg.blockDim = dim3(S::kThreads);
     cfg.dynamicSmemBytes = S::kSmem;
@@ -722,7 +848,9 @@ cudaError_t launch_rows(const AttentionParams& p, int sms, cudaStream_t st)
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    cudaError_t rc = cudaLaunchKernelEx(&cfg, cache_attention_rows_kernel<D, NT, DT>, p);
+    CUtensorMap map_k, map_v;
+    if (!pool_map(&map_k, p.c.k, p.c) || !pool_map(&map_v, p.c.v, p.c)) return cudaErrorInvalidValue;
+    cudaError_t rc = cudaLaunchKernelEx(&cfg, cache_attention_rows_kernel<D, NT, DT>, map_k, map_v, p);
     if (rc != cudaSuccess) return rc;
     const int groups = ctas * S::kGroups;
     rc = launch_pdl_threads(kCombineThreads, cache_attention_combine_kernel<D, NT, DT>, dim3((unsigned)(groups - 1)), st, p, groups);
@@ -761,8 +889,9 @@ extern "C" int hif8_cache_attention(const void* q, int dtype, int64_t q_token_st
     if (int rc = check_cache(k_pages, v_pages, k_exp, v_exp, n_pages, kv_heads, page_tokens, head_dim, page_table, table_stride, &p.c)) return rc;
     if (heads < 1 || heads % kv_heads || heads / kv_heads > HIF8_CACHE_MAX_GROUP) return HIF8_ERR_SHAPE;
     if (!(softmax_scale > 0.f) || !(softmax_scale <= 3.4e38f)) return HIF8_ERR_SCALE_RANGE;
-    if ((int64_t)n_q * (heads / kv_heads) > 0x3FFFFFFF) return HIF8_ERR_SHAPE;
+    if ((int64_t)n_q * (heads / kv_heads) > 0x3FFFFFFF || ((int64_t)n_pages * kv_heads << p.c.shift) > 0x7FFFFFFF) return HIF8_ERR_SHAPE;
     if (n_seqs == 0 || n_q == 0) return HIF8_OK;
+    if (n_pages == 0) return HIF8_ERR_SHAPE;
     if (!q || !out || !d_q_start || !d_lengths) return HIF8_ERR_NULL;
     if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 1u) return HIF8_ERR_ALIGN;
     if ((reinterpret_cast<uintptr_t>(d_q_start) | reinterpret_cast<uintptr_t>(d_lengths) | reinterpret_cast<uintptr_t>(lse)) & 3u) return HIF8_ERR_ALIGN;

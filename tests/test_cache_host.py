@@ -21,7 +21,7 @@ EVERY = [(dict(n_pages=-1), SHAPE), (dict(kv_heads=0), SHAPE), (dict(kv_heads=12
 OWN = {
     "attention": [(dict(dtype=H.F32), DTYPE), (dict(dtype=5), DTYPE), (dict(n_seqs=4097), SHAPE), (dict(n_q=-1), SHAPE), (dict(max_q=-1), SHAPE), (dict(max_length=-1), SHAPE),
                   (dict(window=-1), SHAPE), (dict(heads=3), SHAPE), (dict(heads=0), SHAPE), (dict(heads=130), SHAPE), (dict(q_token_stride=-1), SHAPE),
-                  (dict(out_token_stride=0), SHAPE), (dict(out_head_stride=63), SHAPE), (dict(out_token_stride=192), SHAPE), (dict(n_q=1 << 30), SHAPE),
+                  (dict(out_token_stride=0), SHAPE), (dict(out_head_stride=63), SHAPE), (dict(out_token_stride=192), SHAPE), (dict(n_q=1 << 30), SHAPE), (dict(n_pages=0), SHAPE), (dict(n_pages=1 << 27), SHAPE),
                   (dict(softmax_scale=0.0), RANGE), (dict(softmax_scale=-1.0), RANGE), (dict(softmax_scale=float("nan")), RANGE), (dict(softmax_scale=float("inf")), RANGE),
                   (dict(q=None), NULL), (dict(out=None), NULL), (dict(d_q_start=None), NULL), (dict(d_lengths=None), NULL), (dict(q=64 * M + 1), ALIGN), (dict(lse=67 * M + 2), ALIGN),
                   (dict(out=64 * M + 64), OVERLAP), (dict(out=16 * M), OVERLAP), (dict(out=32 * M), OVERLAP), (dict(workspace=None), WORKSPACE),
