@@ -11,7 +11,6 @@
 #include "hif8.h"
 
 namespace hif8 {
-namespace {
 
 struct CacheView {
     uint8_t* k;             // [pages, heads, page tokens, dim]
@@ -36,6 +35,8 @@ struct CacheView {
     __host__ __device__ int capacity() const { return table_stride >= (1 << 30) >> shift ? 1 << 30 : (int)table_stride << shift; }
     __device__ int length(int n) const { return max(0, min(n, capacity())); }
 };
+
+namespace {
 
 __device__ __forceinline__ int clamp_cache_exp(int e) { return max(-HIF8_CACHE_EXP_MAX, min(HIF8_CACHE_EXP_MAX, e)); }
 

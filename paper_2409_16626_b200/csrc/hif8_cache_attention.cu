@@ -8,90 +8,13 @@
 //   P_ij = 2^(x_ij - m_i + 8),   out_i = sum_j P_ij code_v(j) / sum_j P_ij 2^(e_v(j)),
 // so P <= 2^8 whatever the blocks' spreads are, and nothing is rounded but P (to FP16, 11 bits; products and sums are FP32).  The 2^8 keeps P in the
 // normal range of FP16 down to 2^-22 of the largest.  Exponents lie within +-48, so the denominator stays far inside FP32.
-#include <cuda.h>
-#include <cuda_fp16.h>
-#include <cuda_runtime.h>
-
-#include <atomic>
-#include <cstdint>
-#include <mutex>
-
-#include "hif8.h"
-#include "hif8_cache.cuh"
-#include "hif8_device.cuh"
-#include "hif8_host_cache.h"
-#include "hif8_internal.cuh"
+#include "hif8_cache_attention.cuh"
 
 namespace hif8 {
-extern std::atomic<uint64_t> g_launches;
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kPShift = 8.f;
-constexpr float kNegInf = -__builtin_huge_valf();
 
-struct AttentionParams {
-    CacheView c;
-    const void* q;
-    long long q_token, q_head;  // strides in elements
-    const int* q_start;
-    const int* lengths;
-    int n_seqs, n_q, heads, group;  // group: query heads to a key head
-    int vectors;                    // q and out take 16-byte accesses
-    float scale_log2;               // softmax scale / ln 2
-    int causal, window;
-    void* out;
-    long long out_token, out_head;
-    float* lse;
-    int* status;
-    long long* prefix;              // chunks in front of each sequence
-    float* partial;
-};
-
-// FP16 bits of one code (Eq. 1, Eq. 2, specials)
-constexpr uint32_t f16_bits_of_code(uint32_t c)
-{
-    const uint32_t sign = (c & 0x80u) << 8, m = c & 0x7Fu;
-    if (m == 0) return sign ? 0x7E00u : 0u;
-    if (m == 0x6F) return sign | 0x7C00u;
-    if (m < 8) return sign | (1u << (m + 1));  // 2^(m - 23) in units of 2^-24
-    int E = 0; uint32_t M = m & 7u, w = 3;
-    if (m >= 0x60) { E = (int)(8u | ((m >> 1) & 7u)); M = m & 1u; w = 1; }
-    else if (m >= 0x40) { E = (int)(4u | ((m >> 2) & 3u)); M = m & 3u; w = 2; }
-    else if (m >= 0x20) E = (int)(2u | ((m >> 3) & 1u));
-    else if (m >= 0x10) E = 1;
-    if (m >= 0x20 ? (m & 0x10u) != 0 : m >= 0x10 && (m & 8u)) E = -E;
-    if (E < -14) return sign | (512u + ((M << 9) >> w));  // E == -15: subnormal
-    return sign | (uint32_t)(E + 15) << 10 | (M << (10 - w));
-}
-struct F16OfCode { uint16_t v[256]; };
-constexpr F16OfCode make_f16_of_code()
-{
-    F16OfCode t{};
-    for (uint32_t c = 0; c < 256; c++) t.v[c] = (uint16_t)f16_bits_of_code(c);
-    return t;
-}
-__device__ const F16OfCode g_f16_of_code = make_f16_of_code();
-
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ uint32_t lds_u32(uint32_t addr)
-{
-    uint32_t v;
-    asm("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr));
-    return v;
-}
-__device__ __forceinline__ float exp2_approx(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
-{
-    uint32_t r;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
 __device__ __forceinline__ void mma_16816_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -103,98 +26,6 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v)
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
     return r;
 }
-__device__ __forceinline__ uint4 lds_v4(uint32_t addr)
-{
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint2 lds_v2(uint32_t addr)
-{
-    uint2 v;
-    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
-    return v;
-}
-__device__ __forceinline__ bool elect_one()
-{
-    uint32_t e;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
-    return e != 0;
-}
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
-__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0;
-}
-__device__ __forceinline__ unsigned long long global_ns()
-{
-    unsigned long long t;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-    return t;
-}
-constexpr unsigned long long kWaitLimitNs = 2000000000ull;  // 2 s a wait
-// Bounded wait: false when the barrier did not complete in time, or someone else of the block gave up.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int where)
-{
-    if (mbar_try_wait(bar, parity)) return true;
-    const unsigned long long t0 = global_ns();
-    for (uint32_t it = 1;; it++) {
-        if (mbar_try_wait(bar, parity)) return true;
-        if ((it & 63u) == 0) {
-            if (*abort_flag) return false;
-            if (global_ns() - t0 > kWaitLimitNs) {
-                *abort_flag = 1;
-                atomicCAS(status, 0, where);
-                return false;
-            }
-        }
-    }
-}
-// a copy that nobody waited for lands before the block's shared memory becomes another's
-__device__ __forceinline__ void wait_landed(uint32_t bar, uint32_t parity)
-{
-    const unsigned long long t0 = global_ns();
-    while (!mbar_try_wait(bar, parity) && global_ns() - t0 < kWaitLimitNs) {}
-}
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1) : "memory");
-}
-// bytes that hold Inf or NaN codes (0x6F, 0xEF, 0x80) become zero
-__device__ __forceinline__ uint32_t finite_codes(uint32_t w)
-{
-    const uint32_t special = __vcmpeq4(w & 0x7F7F7F7Fu, 0x6F6F6F6Fu) | __vcmpeq4(w, 0x80808080u);
-    return w & ~special;
-}
-// 2^a for integers of any size, within the finite floats and not below 2^-126
-__device__ __forceinline__ float pow2_clamped(int a) { return pow2f(max(-126, min(126, a))); }
-
-// exponent that brings a row of queries with that largest finite magnitude into FP16: amax to [2^14, 2^15).  What then lies below FP16's subnormals
-// is below 2^-38 of it.
-__device__ __forceinline__ int query_exp(float amax) { return scale_exp_from_amax(__float_as_uint(amax), 14); }
-
-// What query rows may look at.  A row is a query and one of the heads that share a key head: row r of a sequence's n_q * group belongs to query r / group.
-struct SeqView {
-    int first, n_q, len;  // first query of the batch, queries, tokens in the cache
-    __device__ int pos(int i) const { return len - n_q + i; }  // position of query i
-};
-__device__ __forceinline__ SeqView seq_view(const AttentionParams& p, int s)
-{
-    SeqView v;
-    v.first = start_at(p.q_start, s, p.n_q);
-    v.n_q = max(0, start_at(p.q_start, s + 1, p.n_q) - v.first);
-    v.len = p.c.length(p.lengths[s]);
-    return v;
-}
-__device__ __forceinline__ int hi_of(const AttentionParams& p, const SeqView& v, int i) { return p.causal ? max(0, v.pos(i) + 1) : v.len; }
-__device__ __forceinline__ int lo_of(const AttentionParams& p, const SeqView& v, int i) { return p.window ? max(0, v.pos(i) - p.window + 1) : 0; }
-
 // ---------------------------------------------------------------------------------------------------------
 // Few query rows (decoding, drafted tokens): bound by reading the cache once.
 //
@@ -262,9 +93,6 @@ __device__ __forceinline__ bool group_any(int group, bool any)
 }
 __device__ __forceinline__ long long div_small(long long a, int b) { return a >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b); }
 
-// first chunk of group g
-__host__ __device__ __forceinline__ long long share_of(long long chunks, int g, int groups) { return chunks * g / groups; }
-
 // The work of one sequence in chunks
 struct SeqChunks {
     int lo, per_unit, tiles;  // first token (on a chunk), chunks of a unit, row tiles
@@ -275,26 +103,6 @@ struct SeqChunks {
         tiles = (int)(((long long)v.n_q * p.group + rows - 1) / rows);
     }
 };
-
-template <int DT> __device__ __forceinline__ float q_value(uint32_t half_word) { return DT == HIF8_BF16 ? __uint_as_float(half_word << 16) : __half2float(__ushort_as_half((unsigned short)half_word)); }
-
-template <int DT> __device__ __forceinline__ uint32_t pack_out(float a, float b)
-{
-    uint32_t r;
-    if (DT == HIF8_BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
-    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
-    return r;
-}
-// four consecutive results of a row
-template <int DT> __device__ __forceinline__ void store_out4(const AttentionParams& p, long long at, const float (&x)[4])
-{
-    unsigned short* out = reinterpret_cast<unsigned short*>(p.out) + at;
-    const uint2 w = make_uint2(pack_out<DT>(x[0], x[1]), pack_out<DT>(x[2], x[3]));
-    if (p.vectors) *reinterpret_cast<uint2*>(out) = w;
-    else { out[0] = (unsigned short)w.x; out[1] = (unsigned short)(w.x >> 16); out[2] = (unsigned short)w.y; out[3] = (unsigned short)(w.y >> 16); }
-}
-__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? kNegInf : (m - kPShift + log2f(l)) * kLn2; }
-__device__ __forceinline__ float part_factor(float m, float top) { return m == kNegInf ? 0.f : exp2_approx(m - top); }
 
 template <int D, int NT, int DT>
 __global__ void __launch_bounds__(RowsShape<D, NT>::kThreads, 1)
@@ -666,7 +474,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
 #pragma unroll
                 for (int y = 0; y < 4; y++) x[y] *= inv;
                 store_out4<DT>(p, (long long)(v.first + qi) * p.out_token + (long long)h * p.out_head + 4 * f, x);
-                if (p.lse && f == 0) p.lse[(long long)(v.first + qi) * p.heads + h] = lse_of(top, den);
+                if (p.lse && f == 0) p.lse[(long long)(v.first + qi) * p.heads + h] = lse_of(top, den, kPShift);
             } else {
                 *reinterpret_cast<float4*>(record + row * D + 4 * f) = make_float4(x[0], x[1], x[2], x[3]);
                 if (f == 0) *reinterpret_cast<float2*>(record + S::kRows * D + 2 * row) = make_float2(top, den);
@@ -723,7 +531,7 @@ __global__ void __launch_bounds__(kCombineThreads) cache_attention_combine_kerne
 #pragma unroll
         for (int y = 0; y < 4; y++) o[y] *= inv;
         store_out4<DT>(p, (long long)(v.first + qi) * p.out_token + (long long)h * p.out_head + d, o);
-        if (p.lse && d == 0) p.lse[(long long)(v.first + qi) * p.heads + h] = lse_of(top, den);
+        if (p.lse && d == 0) p.lse[(long long)(v.first + qi) * p.heads + h] = lse_of(top, den, kPShift);
     }
 }
 
@@ -775,11 +583,8 @@ __global__ void __launch_bounds__(kThreads) cache_attention_specials_kernel(cons
 // ---------------------------------------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------------------------------------
-constexpr int kMaxBlocks = 148;
 constexpr size_t kHeadBytes = 256 + ((size_t)HIF8_CACHE_MAX_SEQS + 1) * 8 + 248;  // status word, chunks in front of each sequence
 static_assert(kHeadBytes % 256 == 0, "what follows is aligned");
-
-size_t round_up_256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // n8 tiles of query rows that a warp takes: two where the rows fill more than one and the registers allow it
 int row_tiles_of(int max_q, int group, int dim) { return (long long)max_q * group > 8 && dim <= 128 ? 2 : 1; }
@@ -791,19 +596,6 @@ size_t partial_bytes(int dim, int nt)
 
 // The pool of K or V as rows of head_dim bytes, boxes of 16 tokens (128 bytes of each at most), swizzled.  Encoded anew in every call: it holds no more than
 // the address and the sizes.
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
-                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiledFn encode_tiled_fn()
-{
-    static EncodeTiledFn fn = nullptr;
-    static std::once_flag once;
-    std::call_once(once, [] {
-        void* sym = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess) fn = reinterpret_cast<EncodeTiledFn>(sym);
-    });
-    return fn;
-}
 bool pool_map(CUtensorMap* map, const void* pool, const CacheView& c)
 {
     EncodeTiledFn fn = encode_tiled_fn();
@@ -873,7 +665,8 @@ using namespace hif8;
 extern "C" size_t hif8_cache_attention_workspace_bytes(int n_seqs, int n_q, int max_q, int max_length, int heads, int kv_heads, int head_dim)
 {
     if (n_seqs < 0 || n_q < 0 || max_q < 0 || max_length < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads || (head_dim != 64 && head_dim != 128 && head_dim != 256)) return 0;
-    return kHeadBytes + partial_bytes(head_dim, row_tiles_of(max_q, heads / kv_heads, head_dim));
+    const size_t rows = partial_bytes(head_dim, row_tiles_of(max_q, heads / kv_heads, head_dim)), tiles = prefill_workspace_bytes(n_seqs, n_q, max_q, max_length, heads, kv_heads, head_dim);
+    return kHeadBytes + (rows > tiles ? rows : tiles);
 }
 
 extern "C" int hif8_cache_attention(const void* q, int dtype, int64_t q_token_stride, int64_t q_head_stride, const int* d_q_start, const int* d_lengths, int n_seqs, int n_q,
@@ -923,7 +716,10 @@ extern "C" int hif8_cache_attention(const void* q, int dtype, int64_t q_token_st
     p.prefix = reinterpret_cast<long long*>(ws + 256);
     p.partial = reinterpret_cast<float*>(ws + kHeadBytes);
     cudaStream_t st = (cudaStream_t)stream;
-    cudaError_t rc = dtype == HIF8_BF16 ? launch_rows_of<HIF8_BF16>(p, nt, sms, st) : launch_rows_of<HIF8_F16>(p, nt, sms, st);
+    const size_t tiles = prefill_workspace_bytes(n_seqs, n_q, max_q, max_length, heads, kv_heads, head_dim);
+    cudaError_t rc;
+    if (tiles && workspace_bytes >= kHeadBytes + tiles) rc = launch_prefill(p, dtype, max_length, ws + kHeadBytes, sms, st);
+    else rc = dtype == HIF8_BF16 ? launch_rows_of<HIF8_BF16>(p, nt, sms, st) : launch_rows_of<HIF8_F16>(p, nt, sms, st);
     if (rc == cudaSuccess && max_q > 1 && (p.causal || p.window)) {
         const dim3 grid((unsigned)(head_dim / 16), (unsigned)kv_heads, (unsigned)n_seqs);
         rc = dtype == HIF8_BF16 ? launch_pdl(cache_attention_specials_kernel<HIF8_BF16>, grid, st, p) : launch_pdl(cache_attention_specials_kernel<HIF8_F16>, grid, st, p);

@@ -1,0 +1,771 @@
+// Attention over the HiF8 key/value cache for many query rows (chunks of prompts): bound by the products, so it runs on the tensor cores (tcgen05).
+//
+// Three steps.  (1) plan: where each sequence's tokens lie in the workspace, and how many tiles of 128 tokens each pair of row tiles has to look at.
+// (2) expand: the codes of K and V that are looked at and the queries become FP16 tiles in the workspace (exact, see hif8_cache_attention.cu; the queries
+// packed by key head, with the power of two they are scaled by aside), once for all rows that use them: 5 bytes of traffic a code, 3 % of the time of
+// a chunk of 2048 queries against 16 K tokens.  Decoding inside the product kernel was not built: with 256 query rows to a tile of keys its lookups and stores
+// would take 1500 cycles of shared memory beside the 1500 that the products' operands take, and a tile's products take 2048.
+// (3) attention: a block holds two tiles of 128 query rows.  For each, S = Q K^T goes to tensor memory, four warps (a thread a row) turn it into P = 2^(x - m + 4) in
+// FP16, written over S, and O += P V accumulates in tensor memory; while one tile's warps work, the tensor cores do the other tile's products.  O is only
+// rescaled when a row's maximum has grown by more than 2^8 (P stays below 2^12), by the warps themselves: the next scores' barrier says that the sums are not in use.
+// The tiles of all units are dealt out evenly over the blocks; a unit that several blocks share leaves FP32 parts, which a last kernel joins in a fixed order.
+#include "hif8_cache_attention.cuh"
+
+namespace hif8 {
+namespace {
+
+constexpr int kTileRows = 128, kPairRows = 256, kTileTokens = 128;
+constexpr float kShift = 4.f, kLazy = 8.f;
+constexpr int kStages = 4;
+constexpr int kTmaWarp = 8, kMmaWarp = 9, kThreadsA = 10 * 32;
+
+struct PrefillParams {
+    AttentionParams a;
+    __half* kx;            // [heads][cap_blocks * 128][dim]
+    __half* vx;
+    __half* qx;            // [heads][n_q * group][dim]
+    float* q_mul;          // [heads][n_q * group]: softmax scale / ln 2 times the inverse of the power of two of the row
+    float4* meta;          // [heads][cap_blocks * 8]: of 16 tokens: 2^-e_k, -e_v (-Inf: no page), 2^e_v
+    int* block_at;         // [n_seqs + 1] first 128-token block of each sequence
+    long long* tiles_at;   // [pairs + 1] tiles in front of each pair of row tiles (of one head)
+    int* pair_seq;         // [pairs]
+    int cap_blocks, pairs;
+    long long rows;        // n_q * group
+};
+
+// pairs of row tiles of the sequence, and their numbers: from first_pair on (see Piece: no sums over the batch)
+__device__ __forceinline__ long long first_pair(const PrefillParams& p, int s) { return ((long long)start_at(p.a.q_start, s, p.a.n_q) * p.a.group) / kPairRows + s; }
+
+struct PairView {
+    int seq, r0, n_rows, base, j0, tiles;  // rows r0 .. of the sequence; first token of its blocks in the workspace; first tile, tiles
+    int lo_min, lo_max, hi_min, hi_max;    // what the rows look at
+    SeqView v;
+};
+__device__ __forceinline__ PairView pair_view(const PrefillParams& p, int seq, long long number)
+{
+    PairView u;
+    u.seq = seq;
+    u.v = seq_view(p.a, seq);
+    const long long i = number - first_pair(p, seq), rows = (long long)u.v.n_q * p.a.group;
+    u.base = lo_of(p.a, u.v, 0) / kTileTokens * kTileTokens;
+    u.r0 = (int)(i * kPairRows);
+    u.n_rows = i < 0 || i * kPairRows >= rows ? 0 : (int)min((long long)kPairRows, rows - i * kPairRows);
+    if (!u.n_rows) { u.r0 = u.j0 = u.tiles = u.lo_min = u.lo_max = u.hi_min = u.hi_max = 0; return u; }
+    const int qa = u.r0 / p.a.group, qb = (u.r0 + u.n_rows - 1) / p.a.group;
+    u.lo_min = lo_of(p.a, u.v, qa); u.lo_max = lo_of(p.a, u.v, qb);
+    u.hi_min = min(u.v.len, hi_of(p.a, u.v, qa)); u.hi_max = min(u.v.len, hi_of(p.a, u.v, qb));
+    u.j0 = min(u.lo_min, max(u.v.len - 1, 0)) / kTileTokens - u.base / kTileTokens;
+    u.tiles = max(1, (u.hi_max - u.base + kTileTokens - 1) / kTileTokens - u.j0);
+    return u;
+}
+
+// ---------------------------------------------------------------------------------------------------------
+// Plan
+// ---------------------------------------------------------------------------------------------------------
+constexpr int kPlanThreads = 1024;
+__device__ __forceinline__ long long plan_prefix(long long v, long long* total, long long* s_warp)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    long long x = v;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const long long y = __shfl_up_sync(0xFFFFFFFFu, x, d);
+        if (lane >= d) x += y;
+    }
+    __syncthreads();
+    if (lane == 31) s_warp[warp] = x;
+    __syncthreads();
+    long long w = s_warp[lane];  // (32 warps)
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const long long y = __shfl_up_sync(0xFFFFFFFFu, w, d);
+        if (lane >= d) w += y;
+    }
+    *total = __shfl_sync(0xFFFFFFFFu, w, 31);
+    const long long before = __shfl_sync(0xFFFFFFFFu, w, warp ? warp - 1 : 0);
+    return (warp ? before : 0) + x - v;
+}
+
+__global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const PrefillParams p)
+{
+    __shared__ long long s_warp[32];
+    pdl_wait_prior_grid();
+    pdl_launch_dependents();
+    if (threadIdx.x == 0) *p.a.status = 0;
+    long long carry = 0, total;
+    for (int s0 = 0; s0 < p.a.n_seqs; s0 += kPlanThreads) {
+        const int s = s0 + threadIdx.x;
+        long long n = 0;
+        if (s < p.a.n_seqs) {
+            const SeqView v = seq_view(p.a, s);
+            const int base = lo_of(p.a, v, 0) / kTileTokens * kTileTokens;
+            n = v.n_q ? max(1, (v.len - base + kTileTokens - 1) / kTileTokens) : 0;
+        }
+        const long long before = carry + plan_prefix(n, &total, s_warp);
+        if (s < p.a.n_seqs) p.block_at[s] = (int)min(before, (long long)p.cap_blocks);
+        carry += total;
+    }
+    if (threadIdx.x == 0) p.block_at[p.a.n_seqs] = (int)min(carry, (long long)p.cap_blocks);
+    carry = 0;
+    for (int x0 = 0; x0 < p.pairs; x0 += kPlanThreads) {
+        const int x = x0 + threadIdx.x;
+        long long n = 0;
+        if (x < p.pairs) {
+            int s = 0;
+            for (int k = p.a.n_seqs; k > 1;) {
+                const int half = k >> 1;
+                if (first_pair(p, s + half) <= x) { s += half; k -= half; }
+                else k = half;
+            }
+            p.pair_seq[x] = s;
+            n = pair_view(p, s, x).tiles;
+        }
+        const long long before = carry + plan_prefix(n, &total, s_warp);
+        if (x < p.pairs) p.tiles_at[x] = before;
+        carry += total;
+    }
+    if (threadIdx.x == 0) p.tiles_at[p.pairs] = carry;
+}
+
+// ---------------------------------------------------------------------------------------------------------
+// Expand
+// ---------------------------------------------------------------------------------------------------------
+template <int D, int DT>
+__global__ void __launch_bounds__(kThreads) cache_expand_kernel(const PrefillParams p, int code_blocks)
+{
+    __shared__ __align__(16) uint32_t table[kLaneTableWords];
+    const bool codes = (int)blockIdx.x < code_blocks;
+    if (codes) {
+        fill_lane_table(table, g_f16_of_code.v[threadIdx.x]);  // kThreads == 256 codes
+        __syncthreads();
+    }
+    pdl_wait_prior_grid();
+    pdl_launch_dependents();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const CacheView& c = p.a.c;
+    if (codes) {  // a block takes 128 tokens of one head of K or V, a warp 16 of them, which lie in one page
+        const int n_blocks = p.block_at[p.a.n_seqs];
+        const long long units = 2ll * n_blocks * c.heads;
+        for (long long u = blockIdx.x; u < units; u += code_blocks) {
+            const int part = (int)(u % (2 * c.heads)), head = part >> 1, blk = (int)(u / (2 * c.heads));
+            const bool is_v = part & 1;
+            int s = 0;
+            for (int k = p.a.n_seqs; k > 1;) {  // (sequences without blocks share their start with the next)
+                const int half = k >> 1;
+                if (p.block_at[s + half] <= blk) { s += half; k -= half; }
+                else k = half;
+            }
+            const SeqView v = seq_view(p.a, s);
+            const int base = lo_of(p.a, v, 0) / kTileTokens * kTileTokens, t0 = base + (blk - p.block_at[s]) * kTileTokens + 16 * warp;
+            const int hi0 = min(v.len, hi_of(p.a, v, 0)), hi1 = min(v.len, hi_of(p.a, v, v.n_q - 1)), lo0 = lo_of(p.a, v, 0), lo1 = lo_of(p.a, v, v.n_q - 1);
+            const bool seen = t0 < hi1 && t0 + 16 > lo0;
+            const int page = seen ? c.page_of(s, t0 >> c.shift) : -1;
+            const long long row = ((long long)head * p.cap_blocks + blk) * kTileTokens + 16 * warp;
+            if (!is_v && lane == 0) {
+                const long long e = (long long)max(page, 0) * c.heads + head;
+                const int ke = page >= 0 ? clamp_cache_exp(c.k_exp[e]) : 0, ve = page >= 0 ? clamp_cache_exp(c.v_exp[e]) : 0;
+                p.meta[row >> 4] = make_float4(pow2f(-ke), page >= 0 ? (float)-ve : kNegInf, pow2f(ve), 0.f);
+            }
+            const uint8_t* src = (is_v ? c.v : c.k) + c.block_at(max(page, 0), head) + (long long)(t0 & ((1 << c.shift) - 1)) * D;
+            uint4* dst = reinterpret_cast<uint4*>((is_v ? p.vx : p.kx) + row * D);
+            constexpr int kSteps = 16 * D / 8 / 32;  // eight codes a lane and step
+            uint2 w[kSteps];
+#pragma unroll
+            for (int i = 0; i < kSteps; i++) w[i] = page >= 0 ? __ldg(reinterpret_cast<const uint2*>(src) + lane + 32 * i) : make_uint2(0, 0);
+#pragma unroll
+            for (int i = 0; i < kSteps; i++) {
+                // tokens that no query sees are not there; of V where only some queries see them, Inf and NaN are left to cache_attention_specials_kernel
+                const int tok = t0 + (lane + 32 * i) * 8 / D;
+                if (tok < lo0 || tok >= hi1) w[i] = make_uint2(0, 0);
+                else if (is_v && (tok >= hi0 || tok < lo1)) w[i] = make_uint2(finite_codes(w[i].x), finite_codes(w[i].y));
+                const uint2 a = lane_lookup4(table, w[i].x, 4u * lane), b = lane_lookup4(table, w[i].y, 4u * lane);
+                dst[lane + 32 * i] = make_uint4(a.x, a.y, b.x, b.y);
+            }
+        }
+        return;
+    }
+    // query rows, a warp each: four elements (two for 64) a lane
+    constexpr int E = D / 32;
+    const long long rows = (long long)p.a.n_q * p.a.heads;
+    for (long long r = (long long)(blockIdx.x - code_blocks) * (kThreads / 32) + warp; r < rows; r += (long long)(gridDim.x - code_blocks) * (kThreads / 32)) {
+        const int tok = (int)(r / p.a.heads), h = (int)(r - (long long)tok * p.a.heads), head = h / p.a.group;
+        const long long to = head * p.rows + (long long)tok * p.a.group + (h - head * p.a.group);
+        const unsigned short* src = reinterpret_cast<const unsigned short*>(p.a.q) + (long long)tok * p.a.q_token + (long long)h * p.a.q_head + E * lane;
+        uint32_t w[E / 2];
+#pragma unroll
+        for (int x = 0; x < E / 2; x++) {
+            if (p.a.vectors) w[x] = __ldg(reinterpret_cast<const uint32_t*>(src) + x);
+            else w[x] = (uint32_t)src[2 * x] | ((uint32_t)src[2 * x + 1] << 16);
+        }
+        int e = 0;
+        if (DT == HIF8_BF16) {
+            uint32_t acc = 0;
+#pragma unroll
+            for (int x = 0; x < E / 2; x++) acc = amax_word<DT>(acc, w[x]);
+            e = query_exp(__uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax_value<DT>(acc)))));
+            const float f = pow2f(e);
+#pragma unroll
+            for (int x = 0; x < E / 2; x++) w[x] = pack_f16(q_value<DT>(w[x] & 0xFFFFu) * f, q_value<DT>(w[x] >> 16) * f);
+        }
+        uint32_t* out = reinterpret_cast<uint32_t*>(p.qx + to * D) + E / 2 * lane;
+#pragma unroll
+        for (int x = 0; x < E / 2; x++) out[x] = w[x];
+        if (lane == 0) p.q_mul[to] = fminf(p.a.scale_log2 * pow2_clamped(-e), 3.0e38f);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------
+// Attention
+// ---------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void tc_commit(uint32_t bar) { asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void tc_mma_f16(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// A (128 rows) in tensor memory: row i in lane i, two FP16 a column
+__device__ __forceinline__ void tc_mma_f16_a_tmem(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// shared-memory matrix descriptor: start address, leading / stride byte offsets (16-byte units), version 1, 128-byte swizzle
+__device__ __forceinline__ uint64_t make_smem_desc(uint32_t saddr, uint32_t lbo_bytes, uint32_t sbo_bytes)
+{
+    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)((lbo_bytes >> 4) & 0x3FFFu) << 16 | (uint64_t)((sbo_bytes >> 4) & 0x3FFFu) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+__device__ __forceinline__ void tmem_ld_x32(uint32_t taddr, uint32_t* r)
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+          "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t* r)
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+          "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]),
+          "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t* r)
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+          "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ bool warp_all(bool x) { return __all_sync(0xFFFFFFFFu, x); }
+__device__ __forceinline__ bool warp_any(bool x) { return __any_sync(0xFFFFFFFFu, x); }
+
+template <int D>
+struct PrefillSmem {
+    static constexpr uint32_t kQ = kTileRows * D * 2, kStage = kTileTokens * D * 2;
+    static constexpr uint32_t q = 0, stages = 2 * kQ, bars = stages + kStages * kStage;
+    // barriers: queries there / free, stages full / empty, scores there [2], weights there [2], sums complete, sums read, all products ended (after a wait that gave up)
+    static constexpr uint32_t q_full = bars, q_empty = bars + 8, full = bars + 16, empty = full + 8 * kStages, s_full = empty + 8 * kStages, p_full = s_full + 16, o_full = p_full + 16,
+                              o_empty = o_full + 8, drain = o_empty + 8, tmem_slot = drain + 8, abort_flag = tmem_slot + 4, total = abort_flag + 4;
+    static constexpr uint32_t kBytes = total + 1024;
+    static_assert(kBytes <= 227 * 1024, "shared memory");
+};
+
+constexpr int kRecordRows = kPairRows;
+template <int D> struct Record { static constexpr size_t floats = (size_t)kRecordRows * (D + 2); };
+
+// a segment: tiles c0 .. c1 of a unit
+struct Segment {
+    PairView u;
+    int head, c0, c1;
+    __device__ Segment(const PrefillParams& p, long long x0, long long x_end)
+    {
+        const long long per_head = p.tiles_at[p.pairs];
+        head = (int)(x0 / per_head);
+        const long long x = x0 - head * per_head;
+        int a = 0;  // last pair that starts at or before x (empty ones share their start with the next)
+        for (int n = p.pairs; n > 1;) {
+            const int half = n >> 1;
+            if (p.tiles_at[a + half] <= x) { a += half; n -= half; }
+            else n = half;
+        }
+        u = pair_view(p, p.pair_seq[a], a);
+        c0 = (int)(x - p.tiles_at[a]);
+        c1 = (int)min((long long)u.tiles, c0 + (x_end - x0));
+    }
+};
+
+template <int D, int DT>
+__global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                                                                             const __grid_constant__ CUtensorMap map_v, const PrefillParams p)
+{
+    using L = PrefillSmem<D>;
+    extern __shared__ unsigned char smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    unsigned char* sm = smem_raw + (base - smem_u32(smem_raw));
+    const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + L::abort_flag);
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sm + L::tmem_slot);
+    auto bar = [&](uint32_t at, int i = 0) { return base + at + 8u * i; };
+    if (threadIdx.x == 0) {
+        mbar_init(bar(L::q_full), 1); mbar_init(bar(L::q_empty), 1);
+        for (int i = 0; i < kStages; i++) { mbar_init(bar(L::full, i), 1); mbar_init(bar(L::empty, i), 1); }
+        for (int i = 0; i < 2; i++) { mbar_init(bar(L::s_full, i), 1); mbar_init(bar(L::p_full, i), 4); }
+        mbar_init(bar(L::o_full), 1); mbar_init(bar(L::o_empty), 8); mbar_init(bar(L::drain), 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == kMmaWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + L::tmem_slot), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    pdl_wait_prior_grid();
+    pdl_launch_dependents();
+
+    const long long all = p.tiles_at[p.pairs] * p.a.c.heads;
+    const int blocks = (int)min((long long)gridDim.x, all), me = blockIdx.x;
+    long long x0 = me < blocks ? share_of(all, me, blocks) : 0;
+    const long long x_end = me < blocks ? share_of(all, me + 1, blocks) : 0;
+    // tensor memory: scores (and weights over them) of the two tiles at columns 0 and 128, sums at 256 and 384
+    bool ok = true;
+    uint32_t seg = 0;  // segments so far
+
+    if (warp == kTmaWarp) {
+        uint32_t n = 0, q_loads = 0;  // copies into the ring; loads of queries
+        while (x0 < x_end && ok) {
+            const Segment g(p, x0, x_end);
+            const bool two = g.u.n_rows > kTileRows;
+            if (seg) ok = warp_all(mbar_wait(bar(L::q_empty), (seg - 1) & 1u, abort_flag, p.a.status, 71));
+            if (!ok) break;
+            const int q_row = (int)(g.head * p.rows + (long long)g.u.v.first * p.a.group + g.u.r0);
+            if (elect_one()) {
+                mbar_expect(bar(L::q_full), two ? 2 * L::kQ : L::kQ);
+                for (int i = 0; i < (two ? 2 : 1); i++)
+#pragma unroll
+                    for (int c = 0; c < D / 64; c++) tma_load_2d(base + L::q + i * L::kQ + c * (kTileRows * 128), &map_q, c * 64, q_row + i * kTileRows, bar(L::q_full));
+            }
+            __syncwarp();
+            q_loads++;
+            const long long row0 = ((long long)g.head * p.cap_blocks + p.block_at[g.u.seq] + g.u.j0) * kTileTokens;
+            for (int j = g.c0; j < g.c1 && ok; j++)
+                for (int kv = 0; kv < 2; kv++, n++) {
+                    const uint32_t st = n % kStages;
+                    if (n >= kStages) ok = warp_all(mbar_wait(bar(L::empty, st), (n / kStages - 1) & 1u, abort_flag, p.a.status, 72));
+                    if (!ok) break;
+                    if (elect_one()) {
+                        const uint32_t to = base + L::stages + st * L::kStage;
+                        mbar_expect(bar(L::full, st), L::kStage);
+#pragma unroll
+                        for (int c = 0; c < D / 64; c++) tma_load_2d(to + c * (kTileTokens * 128), kv ? &map_v : &map_k, c * 64, (int)(row0 + (long long)j * kTileTokens), bar(L::full, st));
+                    }
+                    __syncwarp();
+                }
+            seg++;
+            x0 += g.c1 - g.c0;
+        }
+        if (!ok || warp_any(*abort_flag)) {  // copies on their way land before the block's shared memory becomes another's
+            if (q_loads) wait_landed(bar(L::q_full), (q_loads - 1) & 1u);
+            for (uint32_t i = n > kStages ? n - kStages : 0; i < n; i++) wait_landed(bar(L::full, i % kStages), (i / kStages) & 1u);
+        }
+    } else if (warp == kMmaWarp) {
+        const uint32_t id_s = (1u << 4) | ((uint32_t)(kTileTokens >> 3) << 17) | ((uint32_t)(kTileRows >> 4) << 24);                 // FP16 x FP16 -> FP32, both K-major
+        const uint32_t id_o = (1u << 4) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTileRows >> 4) << 24);              // B (the values) MN-major
+        uint32_t n = 0, uses[2] = {0, 0}, o_uses = 0;  // ring; weights taken of each tile
+        while (x0 < x_end && ok) {
+            const Segment g(p, x0, x_end);
+            const int both = g.u.n_rows > kTileRows ? 2 : 1, tiles = g.c1 - g.c0;
+            ok = warp_all(mbar_wait(bar(L::q_full), seg & 1u, abort_flag, p.a.status, 73));
+            if (!ok) break;
+            auto scores = [&](int i, uint32_t st) {
+                if (elect_one()) {
+                    const uint64_t da = make_smem_desc(base + L::q + i * L::kQ, 16, 1024), db = make_smem_desc(base + L::stages + st * L::kStage, 16, 1024);
+#pragma unroll
+                    for (int kk = 0; kk < D / 16; kk++) {
+                        const uint64_t off = (uint64_t)((kk / 4) * (kTileRows * 128 / 16) + (kk % 4) * 2);
+                        tc_mma_f16(tmem + i * 128, da + off, db + off, id_s, kk > 0);
+                    }
+                    tc_commit(bar(L::s_full, i));
+                }
+                __syncwarp();
+            };
+            // keys of the first tile
+            uint32_t st = n % kStages;
+            ok = warp_all(mbar_wait(bar(L::full, st), (n / kStages) & 1u, abort_flag, p.a.status, 74));
+            if (!ok) break;
+            tc_fence_after();
+            for (int i = 0; i < both; i++) scores(i, st);
+            if (elect_one()) tc_commit(bar(L::empty, st));
+            __syncwarp();
+            n++;
+            if (o_uses) ok = warp_all(mbar_wait(bar(L::o_empty), (o_uses - 1) & 1u, abort_flag, p.a.status, 75));  // the segment in front of this one has read its sums
+            for (int j = 0; j < tiles && ok; j++) {
+                const uint32_t sv = n % kStages, sk = (n + 1) % kStages;
+                ok = warp_all(mbar_wait(bar(L::full, sv), (n / kStages) & 1u, abort_flag, p.a.status, 76));
+                if (ok && j + 1 < tiles) ok = warp_all(mbar_wait(bar(L::full, sk), ((n + 1) / kStages) & 1u, abort_flag, p.a.status, 77));
+                for (int i = 0; i < both && ok; i++) {
+                    ok = warp_all(mbar_wait(bar(L::p_full, i), uses[i] & 1u, abort_flag, p.a.status, 78));
+                    if (!ok) break;
+                    uses[i]++;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint64_t dv = make_smem_desc(base + L::stages + sv * L::kStage, kTileTokens * 128, 1024);
+#pragma unroll
+                        for (int kk = 0; kk < kTileTokens / 16; kk++)
+                            tc_mma_f16_a_tmem(tmem + 256 + i * 128, tmem + i * 128 + kk * 8, dv + (uint64_t)(kk * 128), id_o, j > 0 || kk > 0);
+                    }
+                    __syncwarp();
+                    if (j + 1 < tiles) scores(i, sk);
+                }
+                if (!ok) break;
+                if (elect_one()) {
+                    tc_commit(bar(L::empty, sv));
+                    if (j + 1 < tiles) tc_commit(bar(L::empty, sk));
+                    else { tc_commit(bar(L::o_full)); tc_commit(bar(L::q_empty)); }
+                }
+                __syncwarp();
+                n += j + 1 < tiles ? 2 : 1;
+            }
+            if (!ok) break;
+            o_uses++;
+            seg++;
+            x0 += tiles;
+        }
+        if (!ok) {  // products on their way end before the block's memory becomes another's: a commit of its own behind them
+            if (elect_one()) {
+                tc_commit(bar(L::drain));
+                wait_landed(bar(L::drain), 0);
+            }
+            __syncwarp();
+        }
+    } else {
+        const int i = warp >> 2, row = (warp & 3) * 32 + lane;  // tile, row
+        const uint32_t t_s = tmem + i * 128 + ((uint32_t)((warp & 3) * 32) << 16), t_o = t_s + 256;
+        uint32_t uses = 0;
+        while (x0 < x_end && ok) {
+            const Segment g(p, x0, x_end);
+            const PairView& u = g.u;
+            const int tiles = g.c1 - g.c0;
+            const bool works = i * kTileRows < u.n_rows, mine = i * kTileRows + row < u.n_rows;  // the tile, this row
+            const int r = u.r0 + min(i * kTileRows + row, u.n_rows - 1), qi = r / p.a.group, gi = r - qi * p.a.group;
+            const int hi = min(u.v.len, hi_of(p.a, u.v, qi)), lo = lo_of(p.a, u.v, qi);
+            const long long q_row = g.head * p.rows + (long long)u.v.first * p.a.group + r;
+            float m = kNegInf, l = 0.f;
+            if (works) {
+                const float mul = p.q_mul[q_row];
+                const int block0 = p.block_at[u.seq] + u.j0 + g.c0;
+                for (int j = 0; j < tiles; j++) {
+                    const float4* meta = p.meta + ((long long)g.head * p.cap_blocks + min(block0 + j, p.cap_blocks - 1)) * (kTileTokens / 16);  // (beyond: lengths above max_length)
+                    float4 mt[8];
+#pragma unroll
+                    for (int x = 0; x < 8; x++) mt[x] = __ldg(meta + x);
+                    const int t0 = u.base + (u.j0 + g.c0 + j) * kTileTokens;
+                    ok = warp_all(mbar_wait(bar(L::s_full, i), uses & 1u, abort_flag, p.a.status, 79));
+                    if (!ok) break;
+                    uses++;
+                    tc_fence_after();
+                    // Two passes over the scores, each reading them from tensor memory: held from one to the other they take more registers than there are.
+                    const bool masked = t0 < u.lo_max || t0 + kTileTokens > u.hi_min;  // some row does not see some token
+                    const int lo_c = lo - t0, hi_c = hi - t0;
+                    uint32_t sr[2][32];
+                    float f[8], top = kNegInf;
+                    tmem_ld_x32(t_s, sr[0]);
+#pragma unroll
+                    for (int c = 0; c < 4; c++) {
+                        tmem_ld_wait();
+                        if (c < 3) tmem_ld_x32(t_s + 32 * (c + 1), sr[(c + 1) & 1]);
+                        if (masked) {
+#pragma unroll
+                            for (int y = 0; y < 32; y++)
+                                if (32 * c + y < lo_c || 32 * c + y >= hi_c) sr[c & 1][y] = __float_as_uint(kNegInf);
+                        }
+#pragma unroll
+                        for (int x = 2 * c; x < 2 * c + 2; x++) {
+                            f[x] = fmaxf(fminf(mul * mt[x].x, 3.0e38f), 1.0e-36f);
+                            float a = __uint_as_float(sr[c & 1][16 * (x & 1)]);
+#pragma unroll
+                            for (int y = 1; y < 16; y++) a = fmaxf(a, __uint_as_float(sr[c & 1][16 * (x & 1) + y]));
+                            top = fmaxf(top, fmaf(a, f[x], mt[x].y));
+                        }
+                    }
+                    const bool grows = top > m + kLazy || (m == kNegInf && top > kNegInf);
+                    if (__any_sync(0xFFFFFFFFu, grows)) {
+                        const float next = grows ? top : m, h = part_factor(m, next);
+                        if (j > 0) {
+#pragma unroll
+                            for (int c = 0; c < D / 32; c++) {
+                                uint32_t o[32];
+                                tmem_ld_x32(t_o + 32 * c, o);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int y = 0; y < 32; y++) o[y] = __float_as_uint(__uint_as_float(o[y]) * (grows ? h : 1.f));
+                                tmem_st_x32(t_o + 32 * c, o);
+                            }
+                        }
+                        if (grows) { l *= h; m = next; }
+                    }
+                    const float base_m = m == kNegInf ? 0.f : m;
+                    const bool far = __any_sync(0xFFFFFFFFu, fabsf(base_m) > 131072.f);  // (there -m + 4 + e would lose its last bits)
+                    tmem_ld_x32(t_s, sr[0]);
+#pragma unroll
+                    for (int c = 0; c < 4; c++) {
+                        tmem_ld_wait();
+                        if (c < 3) tmem_ld_x32(t_s + 32 * (c + 1), sr[(c + 1) & 1]);
+                        if (masked) {
+#pragma unroll
+                            for (int y = 0; y < 32; y++)
+                                if (32 * c + y < lo_c || 32 * c + y >= hi_c) sr[c & 1][y] = __float_as_uint(kNegInf);
+                        }
+                        uint32_t pr[16];
+#pragma unroll
+                        for (int x = 2 * c; x < 2 * c + 2; x++) {
+                            float sum = 0.f;
+                            const float add = mt[x].y - base_m + kShift;
+                            if (far) {
+#pragma unroll
+                                for (int y = 0; y < 16; y++) {
+                                    uint32_t& v = sr[c & 1][16 * (x & 1) + y];
+                                    v = __float_as_uint(exp2_approx(fmaf(__uint_as_float(v), f[x], mt[x].y) - base_m + kShift));
+                                }
+                            } else {
+#pragma unroll
+                                for (int y = 0; y < 16; y++) {
+                                    uint32_t& v = sr[c & 1][16 * (x & 1) + y];
+                                    v = __float_as_uint(exp2_approx(fmaf(__uint_as_float(v), f[x], add)));
+                                }
+                            }
+#pragma unroll
+                            for (int y = 0; y < 16; y += 2) {
+                                const float e0 = __uint_as_float(sr[c & 1][16 * (x & 1) + y]), e1 = __uint_as_float(sr[c & 1][16 * (x & 1) + y + 1]);
+                                sum += e0 + e1;
+                                pr[8 * (x & 1) + y / 2] = pack_f16(e0, e1);
+                            }
+                            l = fmaf(sum, mt[x].z, l);
+                        }
+                        tmem_st_x16(t_s + 16 * c, pr);  // over scores that have been read: those on their way lie from column 32 c + 32 on
+                    }
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(L::p_full, i));
+                }
+            }
+            if (!ok) break;
+            ok = warp_all(mbar_wait(bar(L::o_full), seg & 1u, abort_flag, p.a.status, 80));
+            if (!ok) break;
+            tc_fence_after();
+            const bool whole = g.c0 == 0 && g.c1 == u.tiles;
+            if (works) {
+                float* record = p.a.partial + (size_t)(2 * me + (g.c0 == 0 ? 1 : 0)) * Record<D>::floats + (size_t)(i * kTileRows + row) * D;
+                const int h = g.head * p.a.group + gi;
+                const long long tok = u.v.first + qi;
+                const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+#pragma unroll
+                for (int c = 0; c < D / 32; c++) {
+                    uint32_t o[32];
+                    tmem_ld_x32(t_o + 32 * c, o);
+                    tmem_ld_wait();
+                    if (mine) {
+                        if (whole) {
+#pragma unroll
+                            for (int y = 0; y < 32; y += 4) {
+                                const float x[4] = {__uint_as_float(o[y]) * inv, __uint_as_float(o[y + 1]) * inv, __uint_as_float(o[y + 2]) * inv, __uint_as_float(o[y + 3]) * inv};
+                                store_out4<DT>(p.a, tok * p.a.out_token + (long long)h * p.a.out_head + 32 * c + y, x);
+                            }
+                        } else {
+#pragma unroll
+                            for (int y = 0; y < 32; y += 4) *reinterpret_cast<uint4*>(record + 32 * c + y) = make_uint4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+                        }
+                    }
+                }
+                if (mine) {
+                    if (!whole) {
+                        float* ml = p.a.partial + (size_t)(2 * me + (g.c0 == 0 ? 1 : 0)) * Record<D>::floats + (size_t)kRecordRows * D + 2 * (i * kTileRows + row);
+                        *reinterpret_cast<float2*>(ml) = make_float2(m, l);
+                    } else if (p.a.lse) p.a.lse[tok * p.a.heads + h] = lse_of(m, l, kShift);
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(L::o_empty));
+            seg++;
+            x0 += tiles;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == kMmaWarp) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    }
+}
+
+// Joins the unit that the boundary between blocks b - 1 and b cuts first; a block of threads takes 16 of its 256 rows.
+constexpr int kJoinRows = 16;
+template <int D, int DT>
+__global__ void __launch_bounds__(kThreads) cache_attention_join_kernel(const PrefillParams p, int grid_blocks)
+{
+    pdl_wait_prior_grid();
+    pdl_launch_dependents();
+    const long long per_head = p.tiles_at[p.pairs], all = per_head * p.a.c.heads;
+    const int blocks = (int)min((long long)grid_blocks, all), b = (int)blockIdx.x + 1;
+    if (b >= blocks) return;
+    const long long x = share_of(all, b, blocks);
+    const Segment g(p, x, x + 1);
+    const long long begin = x - g.c0, end = begin + g.u.tiles;
+    if (g.c0 == 0 || share_of(all, b - 1, blocks) > begin) return;
+    int parts = 2;
+    while (b - 1 + parts < blocks && share_of(all, b - 1 + parts, blocks) < end) parts++;
+    for (int i = threadIdx.x; i < kJoinRows * (D / 4); i += kThreads) {
+        const int row = (int)blockIdx.y * kJoinRows + i / (D / 4), d = i % (D / 4) * 4;
+        if (row >= g.u.n_rows) continue;
+        float top = kNegInf, den = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < parts; j++) {
+            const float* rec = p.a.partial + (size_t)(2 * (b - 1 + j) + (j == 0 ? 1 : 0)) * Record<D>::floats;
+            const float2 ml = *reinterpret_cast<const float2*>(rec + (size_t)kRecordRows * D + 2 * row);
+            const float4 a = *reinterpret_cast<const float4*>(rec + (size_t)row * D + d);
+            const float n = fmaxf(top, ml.x), f = part_factor(top, n), h = part_factor(ml.x, n);
+            den = den * f + ml.y * h;
+            o[0] = o[0] * f + a.x * h; o[1] = o[1] * f + a.y * h; o[2] = o[2] * f + a.z * h; o[3] = o[3] * f + a.w * h;
+            top = n;
+        }
+        const int r = g.u.r0 + row, qi = r / p.a.group, h = g.head * p.a.group + r - qi * p.a.group;
+        const float inv = den == 0.f ? 0.f : 1.f / den;
+#pragma unroll
+        for (int y = 0; y < 4; y++) o[y] *= inv;
+        store_out4<DT>(p.a, (long long)(g.u.v.first + qi) * p.a.out_token + (long long)h * p.a.out_head + d, o);
+        if (p.a.lse && d == 0) p.a.lse[(long long)(g.u.v.first + qi) * p.a.heads + h] = lse_of(top, den, kShift);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------------------------------------
+struct Sizes {
+    int cap_blocks, pairs;
+    size_t block_at, tiles_at, pair_seq, partial, meta, q_mul, kx, vx, qx, total;  // offsets
+};
+Sizes sizes_of(int n_seqs, int n_q, int max_length, int heads, int kv_heads, int dim)
+{
+    Sizes z;
+    const int group = heads / kv_heads;
+    const long long cap = (long long)n_seqs * ((max_length + kTileTokens - 1) / kTileTokens + 1);
+    z.cap_blocks = (int)(cap < (1 << 22) ? cap : 1 << 22);
+    z.pairs = (int)((long long)n_q * group / kPairRows) + n_seqs;
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t here = at; at += round_up_256(bytes); return here; };
+    z.block_at = take((size_t)(n_seqs + 1) * 4);
+    z.tiles_at = take((size_t)(z.pairs + 1) * 8);
+    z.pair_seq = take((size_t)z.pairs * 4);
+    z.partial = take((size_t)2 * kMaxBlocks * kRecordRows * (dim + 2) * 4);
+    z.meta = take((size_t)kv_heads * z.cap_blocks * 8 * 16);
+    z.q_mul = take((size_t)n_q * heads * 4);
+    z.kx = take((size_t)kv_heads * z.cap_blocks * kTileTokens * dim * 2);
+    z.vx = take((size_t)kv_heads * z.cap_blocks * kTileTokens * dim * 2);
+    z.qx = take((size_t)n_q * heads * dim * 2);
+    z.total = at;
+    return z;
+}
+
+struct PrefillSetup { cudaError_t rc; };
+PerDevice<PrefillSetup> g_prefill_setup;
+
+bool fp16_map(CUtensorMap* map, const void* at, int dim, long long rows)
+{
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)dim, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)dim * 2};
+    const cuuint32_t box[2] = {64, 128}, one[2] = {1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(at), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, int DT>
+cudaError_t launch_of(const PrefillParams& p, int sms, cudaStream_t st)
+{
+    cudaError_t rc = launch_pdl_threads(kPlanThreads, cache_plan_kernel, dim3(1), st, p);
+    if (rc != cudaSuccess) return rc;
+    // blocks that expand codes and blocks that expand queries, in proportion to their bytes; six fit on an SM
+    const long long q_blocks = ((long long)p.a.n_q * p.a.heads + kThreads / 32 - 1) / (kThreads / 32), c_blocks = 2ll * p.cap_blocks * p.a.c.heads;
+    const int nq = (int)(q_blocks < sms ? q_blocks : sms), nc = (int)(c_blocks < 5ll * sms ? c_blocks : 5ll * sms);
+    rc = launch_pdl(cache_expand_kernel<D, DT>, dim3((unsigned)(nc + nq)), st, p, nc);
+    if (rc != cudaSuccess) return rc;
+    CUtensorMap mq, mk, mv;
+    const long long kv_rows = (long long)p.a.c.heads * p.cap_blocks * kTileTokens;
+    if (!fp16_map(&mq, p.qx, D, p.rows * p.a.c.heads) || !fp16_map(&mk, p.kx, D, kv_rows) || !fp16_map(&mv, p.vx, D, kv_rows)) return cudaErrorInvalidValue;
+    const int blocks = sms < kMaxBlocks ? sms : kMaxBlocks;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3(kThreadsA);
+    cfg.dynamicSmemBytes = PrefillSmem<D>::kBytes;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    rc = cudaLaunchKernelEx(&cfg, cache_attention_tiles_kernel<D, DT>, mq, mk, mv, p);
+    if (rc != cudaSuccess) return rc;
+    rc = launch_pdl(cache_attention_join_kernel<D, DT>, dim3((unsigned)(blocks > 1 ? blocks - 1 : 1), kPairRows / kJoinRows), st, p, blocks);
+    g_launches.fetch_add(4, std::memory_order_relaxed);
+    return rc;
+}
+
+}  // namespace
+
+size_t prefill_workspace_bytes(int n_seqs, int n_q, int max_q, int max_length, int heads, int kv_heads, int dim)
+{
+    if ((long long)max_q * (heads / kv_heads) < 64 || dim > 128) return 0;
+    const Sizes z = sizes_of(n_seqs, n_q, max_length, heads, kv_heads, dim);
+    if ((long long)kv_heads * z.cap_blocks * kTileTokens > 0x7FFFFFFF || (long long)n_q * heads > 0x7FFFFFFF) return 0;  // (rows of a tensor map)
+    return z.total;
+}
+
+cudaError_t launch_prefill(AttentionParams a, int dtype, int max_length, uint8_t* ws, int sms, cudaStream_t st)
+{
+    int dev = 0;
+    cudaError_t rc = cudaGetDevice(&dev);
+    if (rc != cudaSuccess) return rc;
+    const PrefillSetup* setup = g_prefill_setup.get(dev, [](int, PrefillSetup* o) {
+        const void* k[4] = {(const void*)cache_attention_tiles_kernel<64, HIF8_BF16>, (const void*)cache_attention_tiles_kernel<64, HIF8_F16>,
+                            (const void*)cache_attention_tiles_kernel<128, HIF8_BF16>, (const void*)cache_attention_tiles_kernel<128, HIF8_F16>};
+        const int bytes[4] = {(int)PrefillSmem<64>::kBytes, (int)PrefillSmem<64>::kBytes, (int)PrefillSmem<128>::kBytes, (int)PrefillSmem<128>::kBytes};
+        o->rc = cudaSuccess;
+        for (int i = 0; i < 4 && o->rc == cudaSuccess; i++) o->rc = cudaFuncSetAttribute(k[i], cudaFuncAttributeMaxDynamicSharedMemorySize, bytes[i]);
+    });
+    if (!setup || setup->rc != cudaSuccess) return cudaErrorInvalidValue;
+    PrefillParams p;
+    p.a = a;
+    const Sizes z = sizes_of(a.n_seqs, a.n_q, max_length, a.heads, a.c.heads, a.c.dim);
+    p.block_at = reinterpret_cast<int*>(ws + z.block_at);
+    p.tiles_at = reinterpret_cast<long long*>(ws + z.tiles_at);
+    p.pair_seq = reinterpret_cast<int*>(ws + z.pair_seq);
+    p.a.partial = reinterpret_cast<float*>(ws + z.partial);
+    p.meta = reinterpret_cast<float4*>(ws + z.meta);
+    p.q_mul = reinterpret_cast<float*>(ws + z.q_mul);
+    p.kx = reinterpret_cast<__half*>(ws + z.kx);
+    p.vx = reinterpret_cast<__half*>(ws + z.vx);
+    p.qx = reinterpret_cast<__half*>(ws + z.qx);
+    p.cap_blocks = z.cap_blocks;
+    p.pairs = z.pairs;
+    p.rows = (long long)a.n_q * a.group;
+    if (a.c.dim == 64) return dtype == HIF8_BF16 ? launch_of<64, HIF8_BF16>(p, sms, st) : launch_of<64, HIF8_F16>(p, sms, st);
+    return dtype == HIF8_BF16 ? launch_of<128, HIF8_BF16>(p, sms, st) : launch_of<128, HIF8_F16>(p, sms, st);
+}
+
+}  // namespace hif8

@@ -70,14 +70,16 @@ def reference(c, q, counts, group, scale, causal, window):
     return out, lse, tol_out, tol_lse
 
 
-def attend(c, q, counts, heads, causal=1, window=0, scale=None, out=None, lse=True, stream=None, max_q=None, extra=0):
+def attend(c, q, counts, heads, causal=1, window=0, scale=None, out=None, lse=True, stream=None, max_q=None, small=False):
     n = q.shape[0]
     scale = q.shape[2] ** -0.5 if scale is None else scale
     out = torch.full_like(q, 9.0) if out is None else out
     lse = torch.full((n, heads), 9.0, device="cuda") if lse else None
     max_q = max(counts, default=0) if max_q is None else max_q
     longest = max(c.lengths, default=0)
-    size = H.hif8_cache_attention_workspace_bytes(len(counts), n, max_q, longest, heads, c.shape[1], c.shape[3]) + extra
+    group = heads // c.shape[1]
+    # (small: the least that the call takes, without room for expanded tiles: as much as for fewer than 64 rows of a key head)
+    size = H.hif8_cache_attention_workspace_bytes(len(counts), n, min(max_q, 63 // group) if small else max_q, longest, heads, c.shape[1], c.shape[3])
     ws = torch.full((size + 256,), 0xA5, dtype=torch.uint8, device="cuda")
     H.hif8_cache_attention(q, c.dtype, q.stride(0), q.stride(1), starts(counts), c.d_lengths, len(counts), n, max_q, longest, *c.args(), heads, scale, causal, window,
                            out, out.stride(0), out.stride(1), lse, ws, size, stream)
@@ -136,6 +138,32 @@ def test_several_queries(counts, causal, window, heads, kv_heads, dim):
     close(c, q, counts, heads, causal, window)
 
 
+@pytest.mark.parametrize("lengths,counts", [([300], [128]), ([129, 64, 1], [129, 64, 1]), ([3000, 0, 700, 40], [300, 0, 700, 33]), ([5000, 260], [65, 260]), ([50, 20], [70, 90])])
+@pytest.mark.parametrize("causal,window", [(1, 0), (0, 0), (1, 200), (1, 3), (0, 129)])
+@pytest.mark.parametrize("heads,kv_heads,dim,dtype", [(8, 2, 128, BF16), (3, 3, 64, F16), (7, 1, 64, BF16), (5, 5, 128, F16)])
+def test_chunks(lengths, counts, causal, window, heads, kv_heads, dim, dtype):
+    c, q = make(lengths, counts, heads, kv_heads, 16 if window else 128, dim, dtype, seed=len(lengths) + window)
+    close(c, q, counts, heads, causal, window)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_chunks_without_room_for_tiles(dim):
+    c, q = make([700, 90], [100, 90], 8, 2, 64, dim, BF16)
+    close(c, q, [100, 90], 8)
+    close(c, q, [100, 90], 8, small=True)
+
+
+def test_chunks_of_a_large_head():
+    c, q = make([400, 33], [70, 33], 4, 2, 32, 256, BF16)
+    close(c, q, [70, 33], 4)
+
+
+def test_many_short_prompts():
+    counts = [(i * 31) % 90 for i in range(60)]
+    c, q = make([n + (i % 3) * 40 for i, n in enumerate(counts)], counts, 8, 4, 32, 64, BF16)
+    close(c, q, counts, 8)
+
+
 def test_rows_that_see_nothing():
     # an empty cache, more queries than tokens, and a window that has moved past pages which were given up
     c, q = make([0, 3, 100], [2, 6, 4], 4, 2, 16, 64, BF16)
@@ -167,7 +195,8 @@ def test_a_length_beyond_the_row_is_cut():
 
 @pytest.mark.parametrize("counts", [[1, 1], [6, 3], [40, 200]])
 @pytest.mark.parametrize("causal,window", [(1, 0), (1, 20), (0, 0)])
-def test_inf_and_nan_where_they_are_not_seen(counts, causal, window):
+@pytest.mark.parametrize("small", [False, True])
+def test_inf_and_nan_where_they_are_not_seen(counts, causal, window, small):
     """Stale slots behind the length, tokens before the window, and a later query's tokens hold Inf and NaN in K and V; those that a query sees propagate."""
     lengths = [250, 333]
     c, q = make(lengths, counts, 8, 2, 16, 64, BF16, seed=5)
@@ -185,31 +214,34 @@ def test_inf_and_nan_where_they_are_not_seen(counts, causal, window):
     for p in set(range(c.shape[0] + 1)) - set(c.table[c.table >= 0].tolist()):
         c.h["v"][p] = 0x80
     c.upload()
-    close(c, q, counts, 8, causal, window)
+    close(c, q, counts, 8, causal, window, small=small)
 
 
-def test_scores_and_spreads_at_the_ends():
+@pytest.mark.parametrize("counts", [[1, 2], [1, 40]])
+def test_scores_and_spreads_at_the_ends(counts):
     """Large scores (one token takes all), queries and blocks of very different magnitudes, exponents beyond the limit."""
-    c, q = make([400, 90], [1, 2], 8, 2, 16, 128, BF16, seed=3)
-    q = (q.float() * torch.exp2(torch.arange(3 * 8).view(3, 8, 1).cuda().float() * 2 - 20)).bfloat16()
-    close(c, q, [1, 2], 8, scale=0.5)
+    c, q = make([400, 90], counts, 8, 2, 16, 128, BF16, seed=3)
+    n = sum(counts)
+    q = (q.float() * torch.exp2((torch.arange(n * 8) % 24).view(n, 8, 1).cuda().float() * 2 - 20)).bfloat16()
+    close(c, q, counts, 8, scale=0.5)
     rng = np.random.default_rng(2)
     c.h["k_exp"] = rng.integers(-12, 13, size=c.h["k_exp"].shape).astype(np.int32)
     c.h["v_exp"] = rng.integers(-60, 61, size=c.h["v_exp"].shape).astype(np.int32)
     c.upload()
-    _, q = make([400, 90], [1, 2], 8, 2, 16, 128, BF16, seed=3)
-    close(c, q, [1, 2], 8, scale=0.01)
+    _, q = make([400, 90], counts, 8, 2, 16, 128, BF16, seed=3)
+    close(c, q, counts, 8, scale=0.01)
     zero = torch.zeros_like(q)
-    close(c, zero, [1, 2], 8)
+    close(c, zero, counts, 8)
 
 
 @pytest.mark.parametrize("bad", [float("inf"), float("nan")])
-def test_inf_and_nan_queries_stay_in_their_rows(bad):
-    c, q = make([100], [2], 4, 2, 16, 64, BF16)
+@pytest.mark.parametrize("n", [2, 50])
+def test_inf_and_nan_queries_stay_in_their_rows(bad, n):
+    c, q = make([100], [n], 4, 2, 16, 64, BF16)
     q[0, 1, 3] = bad
-    out, lse = attend(c, q, [2], 4)
-    clean, _ = attend(c, torch.where(torch.isfinite(q), q, 0.0), [2], 4)
-    keep = torch.ones(2, 4, dtype=torch.bool)
+    out, lse = attend(c, q, [n], 4)
+    clean, _ = attend(c, torch.where(torch.isfinite(q), q, 0.0), [n], 4)
+    keep = torch.ones(n, 4, dtype=torch.bool)
     keep[0, 1] = False
     assert torch.isnan(out[0, 1]).all() and torch.equal(out[keep], clean[keep])
 
