@@ -91,7 +91,6 @@ __device__ __forceinline__ bool group_any(int group, bool any)
                  : "=r"(r) : "r"(group + 1), "r"(kGroupWarps * 32), "r"((uint32_t)any) : "memory");
     return r != 0;
 }
-__device__ __forceinline__ long long div_small(long long a, int b) { return a >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b); }
 
 // The work of one sequence in chunks
 struct SeqChunks {
@@ -516,7 +515,7 @@ __global__ void __launch_bounds__(kCombineThreads) cache_attention_combine_kerne
     for (int i = threadIdx.x; i < n_rows * (D / 4); i += kCombineThreads) {
         const int row = i / (D / 4), d = (i - row * (D / 4)) * 4;
         float top = kNegInf, den = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
+#pragma unroll 2
         for (int j = 0; j < parts; j++) {
             const float* r = record(j);
             const float2 ml = *reinterpret_cast<const float2*>(r + S::kRows * D + 2 * row);
@@ -543,6 +542,7 @@ __global__ void __launch_bounds__(kThreads) cache_attention_specials_kernel(cons
     pdl_wait_prior_grid();
     pdl_launch_dependents();
     const int slice = blockIdx.x, head = blockIdx.y, s = blockIdx.z;
+    if (p.special_flag && !*p.special_flag) return;
     const SeqView v = seq_view(p, s);
     if (v.n_q < 2) return;
     // tokens that the last query sees or the first, and not both
@@ -718,8 +718,11 @@ extern "C" int hif8_cache_attention(const void* q, int dtype, int64_t q_token_st
     cudaStream_t st = (cudaStream_t)stream;
     const size_t tiles = prefill_workspace_bytes(n_seqs, n_q, max_q, max_length, heads, kv_heads, head_dim);
     cudaError_t rc;
-    if (tiles && workspace_bytes >= kHeadBytes + tiles) rc = launch_prefill(p, dtype, max_length, ws + kHeadBytes, sms, st);
-    else rc = dtype == HIF8_BF16 ? launch_rows_of<HIF8_BF16>(p, nt, sms, st) : launch_rows_of<HIF8_F16>(p, nt, sms, st);
+    p.special_flag = nullptr;
+    if (tiles && workspace_bytes >= kHeadBytes + tiles) {
+        p.special_flag = p.status + 1;
+        rc = launch_prefill(p, dtype, max_length, ws + kHeadBytes, sms, st);
+    } else rc = dtype == HIF8_BF16 ? launch_rows_of<HIF8_BF16>(p, nt, sms, st) : launch_rows_of<HIF8_F16>(p, nt, sms, st);
     if (rc == cudaSuccess && max_q > 1 && (p.causal || p.window)) {
         const dim3 grid((unsigned)(head_dim / 16), (unsigned)kv_heads, (unsigned)n_seqs);
         rc = dtype == HIF8_BF16 ? launch_pdl(cache_attention_specials_kernel<HIF8_BF16>, grid, st, p) : launch_pdl(cache_attention_specials_kernel<HIF8_F16>, grid, st, p);

@@ -31,6 +31,7 @@ struct AttentionParams {
     long long out_token, out_head;
     float* lse;
     int* status;
+    int* special_flag;              // chunks: whether cache_attention_specials_kernel has anything to do; NULL: it looks for itself
     long long* prefix;              // chunks in front of each sequence
     float* partial;
 };
@@ -181,6 +182,7 @@ __device__ __forceinline__ SeqView seq_view(const AttentionParams& p, int s)
 __device__ __forceinline__ int hi_of(const AttentionParams& p, const SeqView& v, int i) { return p.causal ? max(0, v.pos(i) + 1) : v.len; }
 __device__ __forceinline__ int lo_of(const AttentionParams& p, const SeqView& v, int i) { return p.window ? max(0, v.pos(i) - p.window + 1) : 0; }
 
+__device__ __forceinline__ long long div_small(long long a, int b) { return a >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b); }
 // first chunk of group g
 __host__ __device__ __forceinline__ long long share_of(long long chunks, int g, int groups) { return chunks * g / groups; }
 

@@ -17,7 +17,11 @@ namespace {
 constexpr int kTileRows = 128, kPairRows = 256, kTileTokens = 128;
 constexpr float kShift = 4.f, kLazy = 8.f;
 constexpr int kStages = 4;
-constexpr int kTmaWarp = 8, kMmaWarp = 9, kThreadsA = 10 * 32;
+constexpr int kTmaWarp = 8, kMmaWarp = 9, kThreadsA = 12 * 32;
+// Registers: 168 a thread at launch, 64512 in all; the eight warps that hold rows of scores take 208, the third group of four warps (two of them idle) 88.
+constexpr int kRegsRows = 208, kRegsOther = 88;
+static_assert(256 * kRegsRows + 128 * kRegsOther <= kThreadsA * 168, "no more than the block has");
+constexpr int kMetaRing = 8, kSegRing = 4;
 
 struct PrefillParams {
     AttentionParams a;
@@ -29,6 +33,8 @@ struct PrefillParams {
     int* block_at;         // [n_seqs + 1] first 128-token block of each sequence
     long long* tiles_at;   // [pairs + 1] tiles in front of each pair of row tiles (of one head)
     int* pair_seq;         // [pairs]
+    int4* cut;             // [blocks] pair, sequence, key head and first tile of the block's first segment
+    int* specials;         // set when some token that only some queries see holds Inf or NaN in V
     int cap_blocks, pairs;
     long long rows;        // n_q * group
 };
@@ -91,7 +97,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const PrefillP
     __shared__ long long s_warp[32];
     pdl_wait_prior_grid();
     pdl_launch_dependents();
-    if (threadIdx.x == 0) *p.a.status = 0;
+    if (threadIdx.x == 0) { *p.a.status = 0; *p.specials = 0; }
     long long carry = 0, total;
     for (int s0 = 0; s0 < p.a.n_seqs; s0 += kPlanThreads) {
         const int s = s0 + threadIdx.x;
@@ -130,24 +136,23 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const PrefillP
 // ---------------------------------------------------------------------------------------------------------
 // Expand
 // ---------------------------------------------------------------------------------------------------------
+// A block takes units in turn: 128 tokens of one head of K or V, and behind all of those 32 KiB of query rows.
 template <int D, int DT>
-__global__ void __launch_bounds__(kThreads) cache_expand_kernel(const PrefillParams p, int code_blocks)
+__global__ void __launch_bounds__(kThreads) cache_expand_kernel(const PrefillParams p)
 {
     __shared__ __align__(16) uint32_t table[kLaneTableWords];
-    const bool codes = (int)blockIdx.x < code_blocks;
-    if (codes) {
-        fill_lane_table(table, g_f16_of_code.v[threadIdx.x]);  // kThreads == 256 codes
-        __syncthreads();
-    }
+    fill_lane_table(table, g_f16_of_code.v[threadIdx.x]);  // kThreads == 256 codes
+    __syncthreads();
     pdl_wait_prior_grid();
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const CacheView& c = p.a.c;
-    if (codes) {  // a block takes 128 tokens of one head of K or V, a warp 16 of them, which lie in one page
-        const int n_blocks = p.block_at[p.a.n_seqs];
-        const long long units = 2ll * n_blocks * c.heads;
-        for (long long u = blockIdx.x; u < units; u += code_blocks) {
-            const int part = (int)(u % (2 * c.heads)), head = part >> 1, blk = (int)(u / (2 * c.heads));
+    constexpr int kLanes = D / 8, kRowsWarp = 32 / kLanes, kUnroll4 = 4, kRowsUnit = 8 * kRowsWarp * kUnroll4;  // lanes to a query row, rows of a warp at a time, rows of a unit
+    const int n_blocks = p.block_at[p.a.n_seqs];
+    const long long code_units = 2ll * n_blocks * c.heads, rows = (long long)p.a.n_q * p.a.heads, units = code_units + (rows + kRowsUnit - 1) / kRowsUnit;
+    for (long long u = blockIdx.x; u < units; u += gridDim.x) {
+        if (u < code_units) {  // a warp takes 16 tokens, which lie in one page
+            const int blk = (int)(div_small(u, 2 * c.heads)), part = (int)(u - (long long)blk * 2 * c.heads), head = part >> 1;
             const bool is_v = part & 1;
             int s = 0;
             for (int k = p.a.n_seqs; k > 1;) {  // (sequences without blocks share their start with the next)
@@ -161,56 +166,70 @@ __global__ void __launch_bounds__(kThreads) cache_expand_kernel(const PrefillPar
             const bool seen = t0 < hi1 && t0 + 16 > lo0;
             const int page = seen ? c.page_of(s, t0 >> c.shift) : -1;
             const long long row = ((long long)head * p.cap_blocks + blk) * kTileTokens + 16 * warp;
-            if (!is_v && lane == 0) {
-                const long long e = (long long)max(page, 0) * c.heads + head;
-                const int ke = page >= 0 ? clamp_cache_exp(c.k_exp[e]) : 0, ve = page >= 0 ? clamp_cache_exp(c.v_exp[e]) : 0;
-                p.meta[row >> 4] = make_float4(pow2f(-ke), page >= 0 ? (float)-ve : kNegInf, pow2f(ve), 0.f);
-            }
             const uint8_t* src = (is_v ? c.v : c.k) + c.block_at(max(page, 0), head) + (long long)(t0 & ((1 << c.shift) - 1)) * D;
             uint4* dst = reinterpret_cast<uint4*>((is_v ? p.vx : p.kx) + row * D);
             constexpr int kSteps = 16 * D / 8 / 32;  // eight codes a lane and step
             uint2 w[kSteps];
 #pragma unroll
             for (int i = 0; i < kSteps; i++) w[i] = page >= 0 ? __ldg(reinterpret_cast<const uint2*>(src) + lane + 32 * i) : make_uint2(0, 0);
+            if (!is_v && lane == 0) {
+                const long long e = (long long)max(page, 0) * c.heads + head;
+                const int ke = page >= 0 ? clamp_cache_exp(c.k_exp[e]) : 0, ve = page >= 0 ? clamp_cache_exp(c.v_exp[e]) : 0;
+                p.meta[row >> 4] = make_float4(pow2f(-ke), page >= 0 ? (float)-ve : kNegInf, pow2f(ve), 0.f);
+            }
 #pragma unroll
             for (int i = 0; i < kSteps; i++) {
                 // tokens that no query sees are not there; of V where only some queries see them, Inf and NaN are left to cache_attention_specials_kernel
                 const int tok = t0 + (lane + 32 * i) * 8 / D;
                 if (tok < lo0 || tok >= hi1) w[i] = make_uint2(0, 0);
-                else if (is_v && (tok >= hi0 || tok < lo1)) w[i] = make_uint2(finite_codes(w[i].x), finite_codes(w[i].y));
+                else if (is_v && (tok >= hi0 || tok < lo1)) {
+                    const uint2 f = make_uint2(finite_codes(w[i].x), finite_codes(w[i].y));
+                    if (f.x != w[i].x || f.y != w[i].y) *p.specials = 1;
+                    w[i] = f;
+                }
                 const uint2 a = lane_lookup4(table, w[i].x, 4u * lane), b = lane_lookup4(table, w[i].y, 4u * lane);
                 dst[lane + 32 * i] = make_uint4(a.x, a.y, b.x, b.y);
             }
+            continue;
         }
-        return;
-    }
-    // query rows, a warp each: four elements (two for 64) a lane
-    constexpr int E = D / 32;
-    const long long rows = (long long)p.a.n_q * p.a.heads;
-    for (long long r = (long long)(blockIdx.x - code_blocks) * (kThreads / 32) + warp; r < rows; r += (long long)(gridDim.x - code_blocks) * (kThreads / 32)) {
-        const int tok = (int)(r / p.a.heads), h = (int)(r - (long long)tok * p.a.heads), head = h / p.a.group;
-        const long long to = head * p.rows + (long long)tok * p.a.group + (h - head * p.a.group);
-        const unsigned short* src = reinterpret_cast<const unsigned short*>(p.a.q) + (long long)tok * p.a.q_token + (long long)h * p.a.q_head + E * lane;
-        uint32_t w[E / 2];
+        // query rows: eight elements a lane
+        uint4 w[kUnroll4];
+        long long r[kUnroll4], to[kUnroll4];
 #pragma unroll
-        for (int x = 0; x < E / 2; x++) {
-            if (p.a.vectors) w[x] = __ldg(reinterpret_cast<const uint32_t*>(src) + x);
-            else w[x] = (uint32_t)src[2 * x] | ((uint32_t)src[2 * x + 1] << 16);
+        for (int x = 0; x < kUnroll4; x++) {
+            r[x] = (u - code_units) * kRowsUnit + (x * 8 + warp) * kRowsWarp + lane / kLanes;
+            w[x] = make_uint4(0, 0, 0, 0);
+            to[x] = 0;
+            if (r[x] < rows) {
+                const int tok = (int)div_small(r[x], p.a.heads), h = (int)(r[x] - (long long)tok * p.a.heads), head = h / p.a.group;
+                to[x] = head * p.rows + (long long)tok * p.a.group + (h - head * p.a.group);
+                const unsigned short* src = reinterpret_cast<const unsigned short*>(p.a.q) + (long long)tok * p.a.q_token + (long long)h * p.a.q_head + 8 * (lane % kLanes);
+                if (p.a.vectors) w[x] = __ldcs(reinterpret_cast<const uint4*>(src));
+                else {
+                    uint32_t a[4];
+#pragma unroll
+                    for (int y = 0; y < 4; y++) a[y] = (uint32_t)src[2 * y] | ((uint32_t)src[2 * y + 1] << 16);
+                    w[x] = make_uint4(a[0], a[1], a[2], a[3]);
+                }
+            }
         }
-        int e = 0;
-        if (DT == HIF8_BF16) {
-            uint32_t acc = 0;
 #pragma unroll
-            for (int x = 0; x < E / 2; x++) acc = amax_word<DT>(acc, w[x]);
-            e = query_exp(__uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax_value<DT>(acc)))));
-            const float f = pow2f(e);
+        for (int x = 0; x < kUnroll4; x++) {
+            int e = 0;
+            if (DT == HIF8_BF16) {
+                float a = amax_value<DT>(amax_vector<DT>(0u, w[x]));
 #pragma unroll
-            for (int x = 0; x < E / 2; x++) w[x] = pack_f16(q_value<DT>(w[x] & 0xFFFFu) * f, q_value<DT>(w[x] >> 16) * f);
+                for (int d = 1; d < kLanes; d *= 2) a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, d));
+                e = query_exp(a);
+                const float f = pow2f(e);
+                w[x] = make_uint4(pack_f16(q_value<DT>(w[x].x & 0xFFFFu) * f, q_value<DT>(w[x].x >> 16) * f), pack_f16(q_value<DT>(w[x].y & 0xFFFFu) * f, q_value<DT>(w[x].y >> 16) * f),
+                                  pack_f16(q_value<DT>(w[x].z & 0xFFFFu) * f, q_value<DT>(w[x].z >> 16) * f), pack_f16(q_value<DT>(w[x].w & 0xFFFFu) * f, q_value<DT>(w[x].w >> 16) * f));
+            }
+            if (r[x] < rows) {
+                *reinterpret_cast<uint4*>(p.qx + to[x] * D + 8 * (lane % kLanes)) = w[x];
+                if (lane % kLanes == 0) p.q_mul[to[x]] = fminf(p.a.scale_log2 * pow2_clamped(-e), 3.0e38f);
+            }
         }
-        uint32_t* out = reinterpret_cast<uint32_t*>(p.qx + to * D) + E / 2 * lane;
-#pragma unroll
-        for (int x = 0; x < E / 2; x++) out[x] = w[x];
-        if (lane == 0) p.q_mul[to] = fminf(p.a.scale_log2 * pow2_clamped(-e), 3.0e38f);
     }
 }
 
@@ -248,16 +267,13 @@ __device__ __forceinline__ void tmem_ld_x32(uint32_t taddr, uint32_t* r)
           "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(taddr) : "memory");
 }
-__device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t* r)
+__device__ __forceinline__ void tmem_ld_x16(uint32_t taddr, uint32_t* r)
 {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
-          "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]),
-          "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-        : "memory");
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+          "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t* r)
 {
@@ -272,13 +288,22 @@ __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.
 __device__ __forceinline__ bool warp_all(bool x) { return __all_sync(0xFFFFFFFFu, x); }
 __device__ __forceinline__ bool warp_any(bool x) { return __any_sync(0xFFFFFFFFu, x); }
 
+// What the copying warp tells the others of a segment: tiles c0 .. c1 of a unit (a pair of row tiles of a sequence and key head).  tiles == 0: there is no other.
+struct SegmentInfo {
+    int tiles, head, first, n_q, len, r0, n_rows, t0, lo_max, hi_min, whole, from_start;  // t0: first token of the first tile; whole: c0 == 0 and c1 the unit's tiles
+    int pad[4];
+};
+static_assert(sizeof(SegmentInfo) == 64, "read in 16-byte pieces");
+
 template <int D>
 struct PrefillSmem {
     static constexpr uint32_t kQ = kTileRows * D * 2, kStage = kTileTokens * D * 2;
-    static constexpr uint32_t q = 0, stages = 2 * kQ, bars = stages + kStages * kStage;
-    // barriers: queries there / free, stages full / empty, scores there [2], weights there [2], sums complete, sums read, all products ended (after a wait that gave up)
-    static constexpr uint32_t q_full = bars, q_empty = bars + 8, full = bars + 16, empty = full + 8 * kStages, s_full = empty + 8 * kStages, p_full = s_full + 16, o_full = p_full + 16,
-                              o_empty = o_full + 8, drain = o_empty + 8, tmem_slot = drain + 8, abort_flag = tmem_slot + 4, total = abort_flag + 4;
+    static constexpr uint32_t q = 0, stages = 2 * kQ, meta = stages + kStages * kStage, seg = meta + kMetaRing * 128, bars = seg + kSegRing * 64;
+    // barriers: queries there / free, stages full / empty, factors of a tile there, segment told, scores there [2], weights there [2], sums complete, sums read,
+    // all products ended (after a wait that gave up)
+    static constexpr uint32_t q_full = bars, q_empty = bars + 8, full = bars + 16, empty = full + 8 * kStages, meta_full = empty + 8 * kStages, seg_full = meta_full + 8 * kMetaRing,
+                              s_full = seg_full + 8 * kSegRing, p_full = s_full + 16, o_full = p_full + 16, o_empty = o_full + 8, drain = o_empty + 8, tmem_slot = drain + 8,
+                              abort_flag = tmem_slot + 4, total = abort_flag + 4;
     static constexpr uint32_t kBytes = total + 1024;
     static_assert(kBytes <= 227 * 1024, "shared memory");
 };
@@ -289,7 +314,7 @@ template <int D> struct Record { static constexpr size_t floats = (size_t)kRecor
 // a segment: tiles c0 .. c1 of a unit
 struct Segment {
     PairView u;
-    int head, c0, c1;
+    int pair, head, c0, c1;
     __device__ Segment(const PrefillParams& p, long long x0, long long x_end)
     {
         const long long per_head = p.tiles_at[p.pairs];
@@ -301,11 +326,49 @@ struct Segment {
             if (p.tiles_at[a + half] <= x) { a += half; n -= half; }
             else n = half;
         }
+        pair = a;
         u = pair_view(p, p.pair_seq[a], a);
         c0 = (int)(x - p.tiles_at[a]);
         c1 = (int)min((long long)u.tiles, c0 + (x_end - x0));
     }
 };
+
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t pack2(float a, float b)
+{
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ void unpack2(uint64_t d, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(d)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ float4 lds_f4(uint32_t addr)
+{
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+// `bytes` (a multiple of 16) from global to shared memory
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
 
 template <int D, int DT>
 __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
@@ -322,6 +385,8 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
     if (threadIdx.x == 0) {
         mbar_init(bar(L::q_full), 1); mbar_init(bar(L::q_empty), 1);
         for (int i = 0; i < kStages; i++) { mbar_init(bar(L::full, i), 1); mbar_init(bar(L::empty, i), 1); }
+        for (int i = 0; i < kMetaRing; i++) mbar_init(bar(L::meta_full, i), 1);
+        for (int i = 0; i < kSegRing; i++) mbar_init(bar(L::seg_full, i), 1);
         for (int i = 0; i < 2; i++) { mbar_init(bar(L::s_full, i), 1); mbar_init(bar(L::p_full, i), 4); }
         mbar_init(bar(L::o_full), 1); mbar_init(bar(L::o_empty), 8); mbar_init(bar(L::drain), 1);
         *abort_flag = 0;
@@ -338,18 +403,46 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
     pdl_wait_prior_grid();
     pdl_launch_dependents();
 
-    const long long all = p.tiles_at[p.pairs] * p.a.c.heads;
-    const int blocks = (int)min((long long)gridDim.x, all), me = blockIdx.x;
-    long long x0 = me < blocks ? share_of(all, me, blocks) : 0;
-    const long long x_end = me < blocks ? share_of(all, me + 1, blocks) : 0;
     // tensor memory: scores (and weights over them) of the two tiles at columns 0 and 128, sums at 256 and 384
+    const int me = blockIdx.x;
     bool ok = true;
     uint32_t seg = 0;  // segments so far
+    // the next segment, as the copying warp tells it (four are kept: it is at most one ahead of the products, those one ahead of the rows' warps)
+    auto next_segment = [&](SegmentInfo& g, int where) -> bool {
+        ok = warp_all(mbar_wait(bar(L::seg_full, seg % kSegRing), (seg / kSegRing) & 1u, abort_flag, p.a.status, where));
+        if (!ok) return false;
+        const int4* from = reinterpret_cast<const int4*>(sm + L::seg + (seg % kSegRing) * 64);
+        const int4 a = from[0], b = from[1], c = from[2];
+        g.tiles = a.x; g.head = a.y; g.first = a.z; g.n_q = a.w; g.len = b.x; g.r0 = b.y; g.n_rows = b.z; g.t0 = b.w; g.lo_max = c.x; g.hi_min = c.y; g.whole = c.z; g.from_start = c.w;
+        return g.tiles > 0;
+    };
 
+    // (each branch sets its own count of registers: the compiler works by the smallest that reaches a place)
+    if (warp >= kTmaWarp) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
     if (warp == kTmaWarp) {
-        uint32_t n = 0, q_loads = 0;  // copies into the ring; loads of queries
-        while (x0 < x_end && ok) {
+        const long long all = p.tiles_at[p.pairs] * p.a.c.heads;
+        const int blocks = (int)min((long long)gridDim.x, all);
+        long long x0 = me < blocks ? share_of(all, me, blocks) : 0;
+        const long long x_end = me < blocks ? share_of(all, me + 1, blocks) : 0;
+        uint32_t n = 0, tile = 0;  // copies into the ring; tiles so far
+        auto tell = [&](const SegmentInfo& g) {
+            if (lane == 0) {
+                int4* to = reinterpret_cast<int4*>(sm + L::seg + (seg % kSegRing) * 64);
+                to[0] = make_int4(g.tiles, g.head, g.first, g.n_q);
+                to[1] = make_int4(g.len, g.r0, g.n_rows, g.t0);
+                to[2] = make_int4(g.lo_max, g.hi_min, g.whole, g.from_start);
+                mbar_arrive(bar(L::seg_full, seg % kSegRing));
+            }
+            __syncwarp();
+        };
+        SegmentInfo t;
+        while (x0 < x_end) {
             const Segment g(p, x0, x_end);
+            if (seg == 0 && lane == 0) p.cut[me] = make_int4(g.pair, g.u.seq, g.head, g.c0);
+            t.tiles = g.c1 - g.c0; t.head = g.head; t.first = g.u.v.first; t.n_q = g.u.v.n_q; t.len = g.u.v.len; t.r0 = g.u.r0; t.n_rows = g.u.n_rows;
+            t.t0 = g.u.base + (g.u.j0 + g.c0) * kTileTokens; t.lo_max = g.u.lo_max; t.hi_min = g.u.hi_min; t.whole = g.c0 == 0 && g.c1 == g.u.tiles; t.from_start = g.c0 == 0;
+            tell(t);
             const bool two = g.u.n_rows > kTileRows;
             if (seg) ok = warp_all(mbar_wait(bar(L::q_empty), (seg - 1) & 1u, abort_flag, p.a.status, 71));
             if (!ok) break;
@@ -361,9 +454,11 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                     for (int c = 0; c < D / 64; c++) tma_load_2d(base + L::q + i * L::kQ + c * (kTileRows * 128), &map_q, c * 64, q_row + i * kTileRows, bar(L::q_full));
             }
             __syncwarp();
-            q_loads++;
-            const long long row0 = ((long long)g.head * p.cap_blocks + p.block_at[g.u.seq] + g.u.j0) * kTileTokens;
-            for (int j = g.c0; j < g.c1 && ok; j++)
+            seg++;
+            const int block0 = p.block_at[g.u.seq] + g.u.j0 + g.c0;
+            for (int j = 0; j < t.tiles && ok; j++, tile++) {
+                const int blk = min(block0 + j, p.cap_blocks - 1);  // (beyond: lengths above max_length)
+                const int row = (int)(((long long)g.head * p.cap_blocks + blk) * kTileTokens);
                 for (int kv = 0; kv < 2; kv++, n++) {
                     const uint32_t st = n % kStages;
                     if (n >= kStages) ok = warp_all(mbar_wait(bar(L::empty, st), (n / kStages - 1) & 1u, abort_flag, p.a.status, 72));
@@ -372,24 +467,32 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                         const uint32_t to = base + L::stages + st * L::kStage;
                         mbar_expect(bar(L::full, st), L::kStage);
 #pragma unroll
-                        for (int c = 0; c < D / 64; c++) tma_load_2d(to + c * (kTileTokens * 128), kv ? &map_v : &map_k, c * 64, (int)(row0 + (long long)j * kTileTokens), bar(L::full, st));
+                        for (int c = 0; c < D / 64; c++) tma_load_2d(to + c * (kTileTokens * 128), kv ? &map_v : &map_k, c * 64, row, bar(L::full, st));
+                        if (!kv) {  // (eight tiles are kept: keys of tile x are only asked for when the scores of tile x - 2 are there, so the rows are at x - 3 at least)
+                            mbar_expect(bar(L::meta_full, tile % kMetaRing), 128);
+                            bulk_load(base + L::meta + (tile % kMetaRing) * 128, p.meta + (row >> 4), 128, bar(L::meta_full, tile % kMetaRing));
+                        }
                     }
                     __syncwarp();
                 }
-            seg++;
-            x0 += g.c1 - g.c0;
+            }
+            if (!ok) break;
+            x0 += t.tiles;
         }
+        if (ok) { t.tiles = 0; tell(t); }
         if (!ok || warp_any(*abort_flag)) {  // copies on their way land before the block's shared memory becomes another's
-            if (q_loads) wait_landed(bar(L::q_full), (q_loads - 1) & 1u);
+            if (seg) wait_landed(bar(L::q_full), (seg - 1) & 1u);
             for (uint32_t i = n > kStages ? n - kStages : 0; i < n; i++) wait_landed(bar(L::full, i % kStages), (i / kStages) & 1u);
+            const uint32_t asked = (n + 1) / 2;  // tiles whose keys, and with them factors, were asked for
+            for (uint32_t i = asked > kMetaRing ? asked - kMetaRing : 0; i < asked; i++) wait_landed(bar(L::meta_full, i % kMetaRing), (i / kMetaRing) & 1u);
         }
     } else if (warp == kMmaWarp) {
-        const uint32_t id_s = (1u << 4) | ((uint32_t)(kTileTokens >> 3) << 17) | ((uint32_t)(kTileRows >> 4) << 24);                 // FP16 x FP16 -> FP32, both K-major
-        const uint32_t id_o = (1u << 4) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTileRows >> 4) << 24);              // B (the values) MN-major
-        uint32_t n = 0, uses[2] = {0, 0}, o_uses = 0;  // ring; weights taken of each tile
-        while (x0 < x_end && ok) {
-            const Segment g(p, x0, x_end);
-            const int both = g.u.n_rows > kTileRows ? 2 : 1, tiles = g.c1 - g.c0;
+        const uint32_t id_s = (1u << 4) | ((uint32_t)(kTileTokens >> 3) << 17) | ((uint32_t)(kTileRows >> 4) << 24);     // FP16 x FP16 -> FP32, both K-major
+        const uint32_t id_o = (1u << 4) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTileRows >> 4) << 24);  // B (the values) MN-major
+        uint32_t n = 0, uses[2] = {0, 0};  // ring; weights taken of each tile
+        SegmentInfo g;
+        while (next_segment(g, 81)) {
+            const int both = g.n_rows > kTileRows ? 2 : 1, tiles = g.tiles;
             ok = warp_all(mbar_wait(bar(L::q_full), seg & 1u, abort_flag, p.a.status, 73));
             if (!ok) break;
             auto scores = [&](int i, uint32_t st) {
@@ -413,7 +516,7 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
             if (elect_one()) tc_commit(bar(L::empty, st));
             __syncwarp();
             n++;
-            if (o_uses) ok = warp_all(mbar_wait(bar(L::o_empty), (o_uses - 1) & 1u, abort_flag, p.a.status, 75));  // the segment in front of this one has read its sums
+            if (seg) ok = warp_all(mbar_wait(bar(L::o_empty), (seg - 1) & 1u, abort_flag, p.a.status, 75));  // the segment in front of this one has read its sums
             for (int j = 0; j < tiles && ok; j++) {
                 const uint32_t sv = n % kStages, sk = (n + 1) % kStages;
                 ok = warp_all(mbar_wait(bar(L::full, sv), (n / kStages) & 1u, abort_flag, p.a.status, 76));
@@ -442,9 +545,7 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                 n += j + 1 < tiles ? 2 : 1;
             }
             if (!ok) break;
-            o_uses++;
             seg++;
-            x0 += tiles;
         }
         if (!ok) {  // products on their way end before the block's memory becomes another's: a commit of its own behind them
             if (elect_one()) {
@@ -453,111 +554,93 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
             }
             __syncwarp();
         }
+    }
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsRows));
         const int i = warp >> 2, row = (warp & 3) * 32 + lane;  // tile, row
         const uint32_t t_s = tmem + i * 128 + ((uint32_t)((warp & 3) * 32) << 16), t_o = t_s + 256;
-        uint32_t uses = 0;
-        while (x0 < x_end && ok) {
-            const Segment g(p, x0, x_end);
-            const PairView& u = g.u;
-            const int tiles = g.c1 - g.c0;
-            const bool works = i * kTileRows < u.n_rows, mine = i * kTileRows + row < u.n_rows;  // the tile, this row
-            const int r = u.r0 + min(i * kTileRows + row, u.n_rows - 1), qi = r / p.a.group, gi = r - qi * p.a.group;
-            const int hi = min(u.v.len, hi_of(p.a, u.v, qi)), lo = lo_of(p.a, u.v, qi);
-            const long long q_row = g.head * p.rows + (long long)u.v.first * p.a.group + r;
+        uint32_t uses = 0, tile = 0;  // scores of this row tile, tiles of tokens
+        SegmentInfo g;
+        while (next_segment(g, 82)) {
+            const bool works = i * kTileRows < g.n_rows, mine = i * kTileRows + row < g.n_rows;  // the tile, this row
+            const int r = g.r0 + min(i * kTileRows + row, g.n_rows - 1), qi = r / p.a.group;
+            SeqView v;
+            v.first = g.first; v.n_q = g.n_q; v.len = g.len;
             float m = kNegInf, l = 0.f;
             if (works) {
-                const float mul = p.q_mul[q_row];
-                const int block0 = p.block_at[u.seq] + u.j0 + g.c0;
-                for (int j = 0; j < tiles; j++) {
-                    const float4* meta = p.meta + ((long long)g.head * p.cap_blocks + min(block0 + j, p.cap_blocks - 1)) * (kTileTokens / 16);  // (beyond: lengths above max_length)
-                    float4 mt[8];
-#pragma unroll
-                    for (int x = 0; x < 8; x++) mt[x] = __ldg(meta + x);
-                    const int t0 = u.base + (u.j0 + g.c0 + j) * kTileTokens;
-                    ok = warp_all(mbar_wait(bar(L::s_full, i), uses & 1u, abort_flag, p.a.status, 79));
+                const int hi = min(v.len, hi_of(p.a, v, qi)), lo = lo_of(p.a, v, qi);
+                const float mul = p.q_mul[g.head * p.rows + (long long)g.first * p.a.group + r];
+                int t0 = g.t0;
+                for (int j = 0; j < g.tiles; j++, t0 += kTileTokens) {
+                    const uint32_t mt = base + L::meta + ((tile + j) % kMetaRing) * 128;
+                    ok = warp_all(mbar_wait(bar(L::s_full, i), uses & 1u, abort_flag, p.a.status, 79) &&
+                                  mbar_wait(bar(L::meta_full, (tile + j) % kMetaRing), ((tile + j) / kMetaRing) & 1u, abort_flag, p.a.status, 83));
                     if (!ok) break;
                     uses++;
                     tc_fence_after();
-                    // Two passes over the scores, each reading them from tensor memory: held from one to the other they take more registers than there are.
-                    const bool masked = t0 < u.lo_max || t0 + kTileTokens > u.hi_min;  // some row does not see some token
-                    const int lo_c = lo - t0, hi_c = hi - t0;
-                    uint32_t sr[2][32];
-                    float f[8], top = kNegInf;
-                    tmem_ld_x32(t_s, sr[0]);
+                    uint32_t sr[128];
 #pragma unroll
-                    for (int c = 0; c < 4; c++) {
-                        tmem_ld_wait();
-                        if (c < 3) tmem_ld_x32(t_s + 32 * (c + 1), sr[(c + 1) & 1]);
-                        if (masked) {
+                    for (int c = 0; c < 4; c++) tmem_ld_x32(t_s + 32 * c, sr + 32 * c);
+                    tmem_ld_wait();
+                    if (t0 < g.lo_max || t0 + kTileTokens > g.hi_min) {  // some row does not see some token
+                        const int lo_c = lo - t0, hi_c = hi - t0;
 #pragma unroll
-                            for (int y = 0; y < 32; y++)
-                                if (32 * c + y < lo_c || 32 * c + y >= hi_c) sr[c & 1][y] = __float_as_uint(kNegInf);
-                        }
+                        for (int c = 0; c < 128; c++)
+                            if (c < lo_c || c >= hi_c) sr[c] = __float_as_uint(kNegInf);
+                    }
+                    float top = kNegInf;
 #pragma unroll
-                        for (int x = 2 * c; x < 2 * c + 2; x++) {
-                            f[x] = fmaxf(fminf(mul * mt[x].x, 3.0e38f), 1.0e-36f);
-                            float a = __uint_as_float(sr[c & 1][16 * (x & 1)]);
-#pragma unroll
-                            for (int y = 1; y < 16; y++) a = fmaxf(a, __uint_as_float(sr[c & 1][16 * (x & 1) + y]));
-                            top = fmaxf(top, fmaf(a, f[x], mt[x].y));
-                        }
+                    for (int x = 0; x < 8; x++) {
+                        const float4 k = lds_f4(mt + 16 * x);
+                        auto a = [&](int y) { return __uint_as_float(sr[16 * x + y]); };
+                        const float b0 = max3(a(0), a(1), a(2)), b1 = max3(a(3), a(4), a(5)), b2 = max3(a(6), a(7), a(8)), b3 = max3(a(9), a(10), a(11)), b4 = max3(a(12), a(13), a(14));
+                        const float c = max3(max3(b0, b1, a(15)), max3(b2, b3, b4), kNegInf);
+                        top = fmaxf(top, fmaf(c, fmaxf(fminf(mul * k.x, 3.0e38f), 1.0e-36f), k.y));
                     }
                     const bool grows = top > m + kLazy || (m == kNegInf && top > kNegInf);
                     if (__any_sync(0xFFFFFFFFu, grows)) {
-                        const float next = grows ? top : m, h = part_factor(m, next);
+                        const float next = grows ? top : m, h = grows ? part_factor(m, next) : 1.f;
                         if (j > 0) {
-#pragma unroll
-                            for (int c = 0; c < D / 32; c++) {
-                                uint32_t o[32];
-                                tmem_ld_x32(t_o + 32 * c, o);
+#pragma unroll 1
+                            for (int c = 0; c < D / 16; c++) {
+                                uint32_t o[16];
+                                tmem_ld_x16(t_o + 16 * c, o);
                                 tmem_ld_wait();
 #pragma unroll
-                                for (int y = 0; y < 32; y++) o[y] = __float_as_uint(__uint_as_float(o[y]) * (grows ? h : 1.f));
-                                tmem_st_x32(t_o + 32 * c, o);
+                                for (int y = 0; y < 16; y++) o[y] = __float_as_uint(__uint_as_float(o[y]) * h);
+                                tmem_st_x16(t_o + 16 * c, o);
                             }
                         }
-                        if (grows) { l *= h; m = next; }
+                        l *= h;
+                        m = next;
                     }
                     const float base_m = m == kNegInf ? 0.f : m;
                     const bool far = __any_sync(0xFFFFFFFFu, fabsf(base_m) > 131072.f);  // (there -m + 4 + e would lose its last bits)
-                    tmem_ld_x32(t_s, sr[0]);
 #pragma unroll
                     for (int c = 0; c < 4; c++) {
-                        tmem_ld_wait();
-                        if (c < 3) tmem_ld_x32(t_s + 32 * (c + 1), sr[(c + 1) & 1]);
-                        if (masked) {
-#pragma unroll
-                            for (int y = 0; y < 32; y++)
-                                if (32 * c + y < lo_c || 32 * c + y >= hi_c) sr[c & 1][y] = __float_as_uint(kNegInf);
-                        }
                         uint32_t pr[16];
 #pragma unroll
                         for (int x = 2 * c; x < 2 * c + 2; x++) {
-                            float sum = 0.f;
-                            const float add = mt[x].y - base_m + kShift;
-                            if (far) {
-#pragma unroll
-                                for (int y = 0; y < 16; y++) {
-                                    uint32_t& v = sr[c & 1][16 * (x & 1) + y];
-                                    v = __float_as_uint(exp2_approx(fmaf(__uint_as_float(v), f[x], mt[x].y) - base_m + kShift));
-                                }
-                            } else {
-#pragma unroll
-                                for (int y = 0; y < 16; y++) {
-                                    uint32_t& v = sr[c & 1][16 * (x & 1) + y];
-                                    v = __float_as_uint(exp2_approx(fmaf(__uint_as_float(v), f[x], add)));
-                                }
-                            }
+                            const float4 k = lds_f4(mt + 16 * x);
+                            const float f = fmaxf(fminf(mul * k.x, 3.0e38f), 1.0e-36f), add = k.y - base_m + kShift;
+                            const uint64_t f2 = pack2(f, f), a2 = pack2(add, add);
+                            uint64_t sum2 = 0;
 #pragma unroll
                             for (int y = 0; y < 16; y += 2) {
-                                const float e0 = __uint_as_float(sr[c & 1][16 * (x & 1) + y]), e1 = __uint_as_float(sr[c & 1][16 * (x & 1) + y + 1]);
-                                sum += e0 + e1;
+                                const float s0 = __uint_as_float(sr[16 * x + y]), s1 = __uint_as_float(sr[16 * x + y + 1]);
+                                float e0, e1;
+                                unpack2(fma2(pack2(s0, s1), f2, a2), e0, e1);
+                                if (far) { e0 = fmaf(s0, f, k.y) - base_m + kShift; e1 = fmaf(s1, f, k.y) - base_m + kShift; }
+                                e0 = exp2_approx(e0);
+                                e1 = exp2_approx(e1);
+                                sum2 = y ? add2(sum2, pack2(e0, e1)) : pack2(e0, e1);
                                 pr[8 * (x & 1) + y / 2] = pack_f16(e0, e1);
                             }
-                            l = fmaf(sum, mt[x].z, l);
+                            float u0, u1;
+                            unpack2(sum2, u0, u1);
+                            l = fmaf(u0 + u1, k.z, l);
                         }
-                        tmem_st_x16(t_s + 16 * c, pr);  // over scores that have been read: those on their way lie from column 32 c + 32 on
+                        tmem_st_x16(t_s + 16 * c, pr);
                     }
                     tmem_st_wait();
                     tc_fence_before();
@@ -566,22 +649,22 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                 }
             }
             if (!ok) break;
+            tile += g.tiles;
             ok = warp_all(mbar_wait(bar(L::o_full), seg & 1u, abort_flag, p.a.status, 80));
             if (!ok) break;
             tc_fence_after();
-            const bool whole = g.c0 == 0 && g.c1 == u.tiles;
             if (works) {
-                float* record = p.a.partial + (size_t)(2 * me + (g.c0 == 0 ? 1 : 0)) * Record<D>::floats + (size_t)(i * kTileRows + row) * D;
-                const int h = g.head * p.a.group + gi;
-                const long long tok = u.v.first + qi;
-                const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
-#pragma unroll
+                float* record = p.a.partial + (size_t)(2 * me + (g.from_start ? 1 : 0)) * Record<D>::floats;
+                const int h = g.head * p.a.group + r - qi * p.a.group;
+                const long long tok = g.first + qi;
+                const float inv = g.whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+#pragma unroll 1
                 for (int c = 0; c < D / 32; c++) {
                     uint32_t o[32];
                     tmem_ld_x32(t_o + 32 * c, o);
                     tmem_ld_wait();
                     if (mine) {
-                        if (whole) {
+                        if (g.whole) {
 #pragma unroll
                             for (int y = 0; y < 32; y += 4) {
                                 const float x[4] = {__uint_as_float(o[y]) * inv, __uint_as_float(o[y + 1]) * inv, __uint_as_float(o[y + 2]) * inv, __uint_as_float(o[y + 3]) * inv};
@@ -589,22 +672,20 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                             }
                         } else {
 #pragma unroll
-                            for (int y = 0; y < 32; y += 4) *reinterpret_cast<uint4*>(record + 32 * c + y) = make_uint4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+                            for (int y = 0; y < 32; y += 4)
+                                *reinterpret_cast<uint4*>(record + (size_t)(i * kTileRows + row) * D + 32 * c + y) = make_uint4(o[y], o[y + 1], o[y + 2], o[y + 3]);
                         }
                     }
                 }
                 if (mine) {
-                    if (!whole) {
-                        float* ml = p.a.partial + (size_t)(2 * me + (g.c0 == 0 ? 1 : 0)) * Record<D>::floats + (size_t)kRecordRows * D + 2 * (i * kTileRows + row);
-                        *reinterpret_cast<float2*>(ml) = make_float2(m, l);
-                    } else if (p.a.lse) p.a.lse[tok * p.a.heads + h] = lse_of(m, l, kShift);
+                    if (!g.whole) *reinterpret_cast<float2*>(record + (size_t)kRecordRows * D + 2 * (i * kTileRows + row)) = make_float2(m, l);
+                    else if (p.a.lse) p.a.lse[tok * p.a.heads + h] = lse_of(m, l, kShift);
                 }
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(L::o_empty));
             seg++;
-            x0 += tiles;
         }
     }
     tc_fence_before();
@@ -626,14 +707,17 @@ __global__ void __launch_bounds__(kThreads) cache_attention_join_kernel(const Pr
     const int blocks = (int)min((long long)grid_blocks, all), b = (int)blockIdx.x + 1;
     if (b >= blocks) return;
     const long long x = share_of(all, b, blocks);
-    const Segment g(p, x, x + 1);
-    const long long begin = x - g.c0, end = begin + g.u.tiles;
-    if (g.c0 == 0 || share_of(all, b - 1, blocks) > begin) return;
+    const int4 cut = p.cut[b];  // the unit that the boundary cuts
+    const long long begin = x - cut.w;
+    if (cut.w == 0 || share_of(all, b - 1, blocks) > begin) return;
+    const PairView u = pair_view(p, cut.y, cut.x);
+    const int head = cut.z;
+    const long long end = begin + u.tiles;
     int parts = 2;
     while (b - 1 + parts < blocks && share_of(all, b - 1 + parts, blocks) < end) parts++;
     for (int i = threadIdx.x; i < kJoinRows * (D / 4); i += kThreads) {
         const int row = (int)blockIdx.y * kJoinRows + i / (D / 4), d = i % (D / 4) * 4;
-        if (row >= g.u.n_rows) continue;
+        if (row >= u.n_rows) continue;
         float top = kNegInf, den = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
         for (int j = 0; j < parts; j++) {
             const float* rec = p.a.partial + (size_t)(2 * (b - 1 + j) + (j == 0 ? 1 : 0)) * Record<D>::floats;
@@ -644,12 +728,12 @@ __global__ void __launch_bounds__(kThreads) cache_attention_join_kernel(const Pr
             o[0] = o[0] * f + a.x * h; o[1] = o[1] * f + a.y * h; o[2] = o[2] * f + a.z * h; o[3] = o[3] * f + a.w * h;
             top = n;
         }
-        const int r = g.u.r0 + row, qi = r / p.a.group, h = g.head * p.a.group + r - qi * p.a.group;
+        const int r = u.r0 + row, qi = r / p.a.group, h = head * p.a.group + r - qi * p.a.group;
         const float inv = den == 0.f ? 0.f : 1.f / den;
 #pragma unroll
         for (int y = 0; y < 4; y++) o[y] *= inv;
-        store_out4<DT>(p.a, (long long)(g.u.v.first + qi) * p.a.out_token + (long long)h * p.a.out_head + d, o);
-        if (p.a.lse && d == 0) p.a.lse[(long long)(g.u.v.first + qi) * p.a.heads + h] = lse_of(top, den, kShift);
+        store_out4<DT>(p.a, (long long)(u.v.first + qi) * p.a.out_token + (long long)h * p.a.out_head + d, o);
+        if (p.a.lse && d == 0) p.a.lse[(long long)(u.v.first + qi) * p.a.heads + h] = lse_of(top, den, kShift);
     }
 }
 
@@ -658,7 +742,7 @@ __global__ void __launch_bounds__(kThreads) cache_attention_join_kernel(const Pr
 // ---------------------------------------------------------------------------------------------------------
 struct Sizes {
     int cap_blocks, pairs;
-    size_t block_at, tiles_at, pair_seq, partial, meta, q_mul, kx, vx, qx, total;  // offsets
+    size_t cut, block_at, tiles_at, pair_seq, partial, meta, q_mul, kx, vx, qx, total;  // offsets
 };
 Sizes sizes_of(int n_seqs, int n_q, int max_length, int heads, int kv_heads, int dim)
 {
@@ -669,6 +753,7 @@ Sizes sizes_of(int n_seqs, int n_q, int max_length, int heads, int kv_heads, int
     z.pairs = (int)((long long)n_q * group / kPairRows) + n_seqs;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += round_up_256(bytes); return here; };
+    z.cut = take((size_t)kMaxBlocks * 16);
     z.block_at = take((size_t)(n_seqs + 1) * 4);
     z.tiles_at = take((size_t)(z.pairs + 1) * 8);
     z.pair_seq = take((size_t)z.pairs * 4);
@@ -700,10 +785,8 @@ cudaError_t launch_of(const PrefillParams& p, int sms, cudaStream_t st)
 {
     cudaError_t rc = launch_pdl_threads(kPlanThreads, cache_plan_kernel, dim3(1), st, p);
     if (rc != cudaSuccess) return rc;
-    // blocks that expand codes and blocks that expand queries, in proportion to their bytes; six fit on an SM
-    const long long q_blocks = ((long long)p.a.n_q * p.a.heads + kThreads / 32 - 1) / (kThreads / 32), c_blocks = 2ll * p.cap_blocks * p.a.c.heads;
-    const int nq = (int)(q_blocks < sms ? q_blocks : sms), nc = (int)(c_blocks < 5ll * sms ? c_blocks : 5ll * sms);
-    rc = launch_pdl(cache_expand_kernel<D, DT>, dim3((unsigned)(nc + nq)), st, p, nc);
+    const long long units = 2ll * p.cap_blocks * p.a.c.heads + ((long long)p.a.n_q * p.a.heads + 127) / 128, most = 6ll * sms;  // (six blocks fit on an SM)
+    rc = launch_pdl(cache_expand_kernel<D, DT>, dim3((unsigned)(units < most ? units : most)), st, p);
     if (rc != cudaSuccess) return rc;
     CUtensorMap mq, mk, mv;
     const long long kv_rows = (long long)p.a.c.heads * p.cap_blocks * kTileTokens;
@@ -752,6 +835,8 @@ cudaError_t launch_prefill(AttentionParams a, int dtype, int max_length, uint8_t
     PrefillParams p;
     p.a = a;
     const Sizes z = sizes_of(a.n_seqs, a.n_q, max_length, a.heads, a.c.heads, a.c.dim);
+    p.specials = a.special_flag;
+    p.cut = reinterpret_cast<int4*>(ws + z.cut);
     p.block_at = reinterpret_cast<int*>(ws + z.block_at);
     p.tiles_at = reinterpret_cast<long long*>(ws + z.tiles_at);
     p.pair_seq = reinterpret_cast<int*>(ws + z.pair_seq);
