@@ -299,10 +299,10 @@ template <int D>
 struct PrefillSmem {
     static constexpr uint32_t kQ = kTileRows * D * 2, kStage = kTileTokens * D * 2;
     static constexpr uint32_t q = 0, stages = 2 * kQ, meta = stages + kStages * kStage, seg = meta + kMetaRing * 128, bars = seg + kSegRing * 64;
-    // barriers: queries there / free, stages full / empty, factors of a tile there, segment told, scores there [2], weights there [2], sums complete, sums read,
+    // barriers: queries there / free, stages full / empty, factors of a tile there, segment told, scores there [2], weights there (half of them, all) [2], sums complete, sums read,
     // all products ended (after a wait that gave up)
     static constexpr uint32_t q_full = bars, q_empty = bars + 8, full = bars + 16, empty = full + 8 * kStages, meta_full = empty + 8 * kStages, seg_full = meta_full + 8 * kMetaRing,
-                              s_full = seg_full + 8 * kSegRing, p_full = s_full + 16, o_full = p_full + 16, o_empty = o_full + 8, drain = o_empty + 8, tmem_slot = drain + 8,
+                              s_full = seg_full + 8 * kSegRing, p_half = s_full + 16, p_full = p_half + 16, o_full = p_full + 16, o_empty = o_full + 8, drain = o_empty + 8, tmem_slot = drain + 8,
                               abort_flag = tmem_slot + 4, total = abort_flag + 4;
     static constexpr uint32_t kBytes = total + 1024;
     static_assert(kBytes <= 227 * 1024, "shared memory");
@@ -387,7 +387,7 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
         for (int i = 0; i < kStages; i++) { mbar_init(bar(L::full, i), 1); mbar_init(bar(L::empty, i), 1); }
         for (int i = 0; i < kMetaRing; i++) mbar_init(bar(L::meta_full, i), 1);
         for (int i = 0; i < kSegRing; i++) mbar_init(bar(L::seg_full, i), 1);
-        for (int i = 0; i < 2; i++) { mbar_init(bar(L::s_full, i), 1); mbar_init(bar(L::p_full, i), 4); }
+        for (int i = 0; i < 2; i++) { mbar_init(bar(L::s_full, i), 1); mbar_init(bar(L::p_half, i), 4); mbar_init(bar(L::p_full, i), 4); }
         mbar_init(bar(L::o_full), 1); mbar_init(bar(L::o_empty), 8); mbar_init(bar(L::drain), 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -522,17 +522,21 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                 ok = warp_all(mbar_wait(bar(L::full, sv), (n / kStages) & 1u, abort_flag, p.a.status, 76));
                 if (ok && j + 1 < tiles) ok = warp_all(mbar_wait(bar(L::full, sk), ((n + 1) / kStages) & 1u, abort_flag, p.a.status, 77));
                 for (int i = 0; i < both && ok; i++) {
-                    ok = warp_all(mbar_wait(bar(L::p_full, i), uses[i] & 1u, abort_flag, p.a.status, 78));
+                    const uint64_t dv = make_smem_desc(base + L::stages + sv * L::kStage, kTileTokens * 128, 1024);
+#pragma unroll
+                    for (int h = 0; h < 2; h++) {  // as the weights come: those of the first 64 tokens, and the others
+                        ok = warp_all(mbar_wait(bar(h ? L::p_full : L::p_half, i), uses[i] & 1u, abort_flag, p.a.status, 78));
+                        if (!ok) break;
+                        tc_fence_after();
+                        if (elect_one()) {
+#pragma unroll
+                            for (int kk = 4 * h; kk < 4 * h + 4; kk++)
+                                tc_mma_f16_a_tmem(tmem + 256 + i * 128, tmem + i * 128 + kk * 8, dv + (uint64_t)(kk * 128), id_o, j > 0 || kk > 0);
+                        }
+                        __syncwarp();
+                    }
                     if (!ok) break;
                     uses[i]++;
-                    tc_fence_after();
-                    if (elect_one()) {
-                        const uint64_t dv = make_smem_desc(base + L::stages + sv * L::kStage, kTileTokens * 128, 1024);
-#pragma unroll
-                        for (int kk = 0; kk < kTileTokens / 16; kk++)
-                            tc_mma_f16_a_tmem(tmem + 256 + i * 128, tmem + i * 128 + kk * 8, dv + (uint64_t)(kk * 128), id_o, j > 0 || kk > 0);
-                    }
-                    __syncwarp();
                     if (j + 1 < tiles) scores(i, sk);
                 }
                 if (!ok) break;
@@ -615,22 +619,29 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                         m = next;
                     }
                     const float base_m = m == kNegInf ? 0.f : m;
-                    const bool far = __any_sync(0xFFFFFFFFu, fabsf(base_m) > 131072.f);  // (there -m + 4 + e would lose its last bits)
+                    const bool far = __any_sync(0xFFFFFFFFu, fabsf(base_m) > 131072.f);
+                    if (far) {  // there -m + 4 - e would lose its last bits: the differences first
+#pragma unroll
+                        for (int x = 0; x < 8; x++) {
+                            const float4 k = lds_f4(mt + 16 * x);
+                            const float f = fmaxf(fminf(mul * k.x, 3.0e38f), 1.0e-36f);
+#pragma unroll
+                            for (int y = 0; y < 16; y++) sr[16 * x + y] = __float_as_uint(fmaf(__uint_as_float(sr[16 * x + y]), f, k.y) - base_m);
+                        }
+                    }
 #pragma unroll
                     for (int c = 0; c < 4; c++) {
                         uint32_t pr[16];
 #pragma unroll
                         for (int x = 2 * c; x < 2 * c + 2; x++) {
                             const float4 k = lds_f4(mt + 16 * x);
-                            const float f = fmaxf(fminf(mul * k.x, 3.0e38f), 1.0e-36f), add = k.y - base_m + kShift;
+                            const float f = far ? 1.f : fmaxf(fminf(mul * k.x, 3.0e38f), 1.0e-36f), add = far ? kShift : k.y - base_m + kShift;
                             const uint64_t f2 = pack2(f, f), a2 = pack2(add, add);
                             uint64_t sum2 = 0;
 #pragma unroll
                             for (int y = 0; y < 16; y += 2) {
-                                const float s0 = __uint_as_float(sr[16 * x + y]), s1 = __uint_as_float(sr[16 * x + y + 1]);
                                 float e0, e1;
-                                unpack2(fma2(pack2(s0, s1), f2, a2), e0, e1);
-                                if (far) { e0 = fmaf(s0, f, k.y) - base_m + kShift; e1 = fmaf(s1, f, k.y) - base_m + kShift; }
+                                unpack2(fma2(pack2(__uint_as_float(sr[16 * x + y]), __uint_as_float(sr[16 * x + y + 1])), f2, a2), e0, e1);
                                 e0 = exp2_approx(e0);
                                 e1 = exp2_approx(e1);
                                 sum2 = y ? add2(sum2, pack2(e0, e1)) : pack2(e0, e1);
@@ -641,6 +652,12 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                             l = fmaf(u0 + u1, k.z, l);
                         }
                         tmem_st_x16(t_s + 16 * c, pr);
+                        if (c == 1) {  // the products with the first 64 tokens may start
+                            tmem_st_wait();
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(bar(L::p_half, i));
+                        }
                     }
                     tmem_st_wait();
                     tc_fence_before();
