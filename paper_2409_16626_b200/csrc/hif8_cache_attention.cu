@@ -57,8 +57,10 @@ struct RowsShape {
     static constexpr uint32_t kRing = kStages * 2 * kTile;               // of a warp; at a segment's end its sums lie there
     static constexpr int kBackWarps = 98304 / kRing, kFrontWarps = kWarps > kBackWarps ? kWarps - kBackWarps : 0;  // rings behind / in front of the table
     static constexpr int kRecord = kRows * (D + 2);                      // floats of a partial result: sums, maxima, denominators
+    // where a warp's sums fit in one stage of its ring, the next segment's first tiles are on their way in the others while the sums are joined
+    static constexpr int kEarly = kRows * D * 4 <= 2 * (int)kTile ? kStages - 1 : 0;
     // offsets from the block's first byte, which is 1024 modulo 65536
-    static constexpr uint32_t kMl = (HIF8_CACHE_MAX_SEQS + 2) * 8, kScan = kMl + kWarps * kRows * 8, kBars = kScan + 32 * 8, kFlag = kBars + kWarps * kStages * 16;
+    static constexpr uint32_t kMl = (HIF8_CACHE_MAX_SEQS + 2) * 8, kScan = kMl + kWarps * kRows * 8, kPlace = kScan + 32 * 8, kBars = kPlace + kWarps * 8, kFlag = kBars + kWarps * kStages * 16;
     static constexpr uint32_t kFrontRing = kLutBytes - 1024 - kFrontWarps * kRing, kLut = kLutBytes - 1024, kBackRing = kLut + kLutBytes;
     static constexpr uint32_t kSmem = kBackRing + (kWarps < kBackWarps ? kWarps : kBackWarps) * kRing;
     static_assert(kFlag + 16 <= kFrontRing && kSmem <= 227 * 1024 && kRows * D * 4 <= kRing, "shared memory");
@@ -119,7 +121,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_raw + S::kFlag);
     if ((raw & (kLutBytes - 1)) != 1024) {  // (the same answer in every thread of the grid)
         pdl_wait_prior_grid();
-        if (blockIdx.x == 0 && threadIdx.x == 0) { *p.status = 7; p.prefix[p.n_seqs] = 0; }
+        if (blockIdx.x == 0 && threadIdx.x == 0) { *p.status = 7; *p.chunks = 0; }
         return;
     }
     {
@@ -162,10 +164,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
         for (int s = s0; s < s1; s++) s_prefix[s] += before;
         if (threadIdx.x == S::kThreads - 1) s_prefix[p.n_seqs] = before + mine;
         __syncthreads();
-        if (blockIdx.x == 0) {
-            for (int s = threadIdx.x; s <= p.n_seqs; s += S::kThreads) p.prefix[s] = s_prefix[s];
-            if (threadIdx.x == 0) *p.status = 0;
-        }
+        if (blockIdx.x == 0 && threadIdx.x == 0) { *p.chunks = s_prefix[p.n_seqs]; *p.status = 0; }
     }
     const long long chunks = s_prefix[p.n_seqs];
     const int groups = (int)min((long long)gridDim.x * S::kGroups, chunks);
@@ -175,71 +174,86 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
     const long long x_end = share_of(chunks, me + 1, groups);
     const uint32_t lut = raw + S::kLut + 4u * lane;
     const uint32_t ring = S::ring(raw, warp);
-    float* my_sum = reinterpret_cast<float*>(smem_raw + (ring - raw));
     float2* all_ml = reinterpret_cast<float2*>(smem_raw + S::kMl) + grp * kGroupWarps * S::kRows;
+    uint32_t* all_place = reinterpret_cast<uint32_t*>(smem_raw + S::kPlace) + grp * kGroupWarps;  // where the warps' sums lie
     const int slot_mask = (1 << p.c.shift) - 1;
     // where this thread reads its bytes of a tile: keys of operand rows g and g + 8, the 16-byte chunks t, t + 4, ..; values of four tokens
     const int tok_k = token_of_row<D>(g), piece = piece_of<D>(g);
     uint32_t use = 0;  // uses of the ring by this warp: stage use % kStages, parity (use / kStages) & 1
     bool ok = true;
+    const uint32_t magic = 65536u / (uint32_t)p.group + 1u;  // x / group = x magic >> 16 for the x < group + 16 that come up
 
-    while (x0 < x_end) {
-        int s = 0;
+    // ---- a segment: chunks c0 .. c1 of a unit
+    int s, head, r0, n_rows, q0, h0, c0, c1, per_unit, hi_min, hi_max, lo_min, lo_max, lo_chunk;
+    SeqView v;
+    // Tiles of this warp: lane n holds pool row and exponents of that of the n-th chunk of a batch of 32; a tile without a page, or with no token
+    // that a row sees, is left out.  Tiles are asked for ahead; `ahead` holds first tokens and exponents of those on their way.
+    int b_row = -1, b_exps = 0, b_first = 0;
+    uint32_t b_live = 0;
+    int ahead_t0[S::kStages], ahead_exps[S::kStages];
+    auto load_batch = [&](int c) {
+        b_first = c;
+        const int at = lo_chunk + (c + lane) * kChunk + 16 * gw;  // (below 2^31: a length, at most 2^30, and less than 2^12 more)
+        const int page = c + lane < c1 && at < hi_max && at + 16 > lo_min ? p.c.page_of(s, at >> p.c.shift) : -1;
+        const long long e = (long long)max(page, 0) * p.c.heads + head;
+        b_exps = page >= 0 ? (clamp_cache_exp(p.c.k_exp[e]) & 0xFF) | clamp_cache_exp(p.c.v_exp[e]) << 8 : 0;
+        b_row = (int)(e << p.c.shift) + (at & slot_mask);  // (rows of a pool number less than 2^31)
+        b_live = __ballot_sync(0xFFFFFFFFu, page >= 0);
+    };
+    auto ask = [&](uint32_t n, int& t0, int& exps) {  // the next tile into the place of use n; t0 = -1: there is none
+        while (!b_live && b_first + 32 < c1) load_batch(b_first + 32);
+        t0 = -1;
+        if (!b_live || !ok) return;
+        const int i = __ffs(b_live) - 1, row = __shfl_sync(0xFFFFFFFFu, b_row, i);
+        t0 = lo_chunk + (b_first + i) * kChunk + 16 * gw;
+        b_live &= b_live - 1;
+        const uint32_t st = n % S::kStages, at = ring + st * 2 * S::kTile, bar = bars + 16 * st;
+        __syncwarp();  // every lane has read what the stage held
+        if (elect_one()) {
+            mbar_expect(bar, S::kTile);
+            tma_load_2d(at, &map_k, 0, row, bar);
+            if (D == 256) tma_load_2d(at + 2048, &map_k, 128, row, bar);
+            mbar_expect(bar + 8, S::kTile);
+            tma_load_2d(at + S::kTile, &map_v, 0, row, bar + 8);
+            if (D == 256) tma_load_2d(at + S::kTile + 2048, &map_v, 128, row, bar + 8);
+        }
+        __syncwarp();
+        exps = __shfl_sync(0xFFFFFFFFu, b_exps, i);  // (behind the copies, which need not wait for them)
+    };
+    auto open = [&]() {  // the segment at x0, its first tiles
+        s = 0;
         for (int n = p.n_seqs; n > 1;) {  // last sequence that starts at or before x0 (those without chunks share their start with the next)
             const int half = n >> 1;
             if (s_prefix[s + half] <= x0) { s += half; n -= half; }
             else n = half;
         }
-        const SeqView v = seq_view(p, s);
+        v = seq_view(p, s);
         const SeqChunks k(p, v, S::kRows);
         const long long in_seq = x0 - s_prefix[s], unit = div_small(in_seq, k.per_unit);
-        const int c0 = (int)(in_seq - unit * k.per_unit), c1 = (int)min((long long)k.per_unit, c0 + (x_end - x0));
-        const int head = (int)div_small(unit, k.tiles), r0 = (int)(unit - (long long)head * k.tiles) * S::kRows;
-        const int n_rows = (int)min((long long)S::kRows, (long long)v.n_q * p.group - r0);
-        const int q0 = r0 / p.group, h0 = r0 - q0 * p.group;  // query and head of the tile's first row
-        const uint32_t magic = 65536u / (uint32_t)p.group + 1u;  // x / group = x magic >> 16 for the x < group + 16 that come up
-        auto query_of = [&](int row) -> int { return q0 + (int)((uint32_t)(h0 + row) * magic >> 16); };
-        auto head_of = [&](int row) -> int { return head * p.group + h0 + row - (int)((uint32_t)(h0 + row) * magic >> 16) * p.group; };
-        const int ib = query_of(n_rows - 1);
-        const int hi_min = min(v.len, hi_of(p, v, q0)), hi_max = min(v.len, hi_of(p, v, ib)), lo_min = lo_of(p, v, q0), lo_max = lo_of(p, v, ib);
-
-        // Tiles of this warp: lane n holds page row and exponents of that of the n-th chunk of a batch of 32; a tile without a page, or with no token
-        // that a row sees, is left out.  Tiles are asked for kStages ahead; `ahead` holds first tokens and exponents of those on their way.
-        int b_row = -1, b_exps = 0, b_first = c0;
-        uint32_t b_live = 0;
-        auto load_batch = [&](int c) {
-            b_first = c;
-            const int at = k.lo + (c + lane) * kChunk + 16 * gw;  // (below 2^31: a length, at most 2^30, and less than 2^12 more)
-            const int page = c + lane < c1 && at < hi_max && at + 16 > lo_min ? p.c.page_of(s, at >> p.c.shift) : -1;
-            const long long e = (long long)max(page, 0) * p.c.heads + head;
-            b_exps = page >= 0 ? (clamp_cache_exp(p.c.k_exp[e]) & 0xFF) | clamp_cache_exp(p.c.v_exp[e]) << 8 : 0;
-            b_row = (int)(e << p.c.shift) + (at & slot_mask);  // (rows of a pool number less than 2^31)
-            b_live = __ballot_sync(0xFFFFFFFFu, page >= 0);
-        };
-        int ahead_t0[S::kStages], ahead_exps[S::kStages];
-        auto ask = [&](uint32_t n, int& t0, int& exps) {  // the next tile into the place of use n; t0 = -1: there is none
-            while (!b_live && b_first + 32 < c1) load_batch(b_first + 32);
-            t0 = -1;
-            if (!b_live || !ok) return;
-            const int i = __ffs(b_live) - 1, row = __shfl_sync(0xFFFFFFFFu, b_row, i);
-            exps = __shfl_sync(0xFFFFFFFFu, b_exps, i);
-            t0 = k.lo + (b_first + i) * kChunk + 16 * gw;
-            b_live &= b_live - 1;
-            const uint32_t st = n % S::kStages, at = ring + st * 2 * S::kTile, bar = bars + 16 * st;
-            __syncwarp();  // every lane has read what the stage held
-            if (elect_one()) {
-                mbar_expect(bar, S::kTile);
-                tma_load_2d(at, &map_k, 0, row, bar);
-                if (D == 256) tma_load_2d(at + 2048, &map_k, 128, row, bar);
-                mbar_expect(bar + 8, S::kTile);
-                tma_load_2d(at + S::kTile, &map_v, 0, row, bar + 8);
-                if (D == 256) tma_load_2d(at + S::kTile + 2048, &map_v, 128, row, bar + 8);
-            }
-            __syncwarp();
-        };
+        per_unit = k.per_unit; lo_chunk = k.lo;
+        c0 = (int)(in_seq - unit * k.per_unit); c1 = (int)min((long long)k.per_unit, c0 + (x_end - x0));
+        head = (int)div_small(unit, k.tiles); r0 = (int)(unit - (long long)head * k.tiles) * S::kRows;
+        n_rows = (int)min((long long)S::kRows, (long long)v.n_q * p.group - r0);
+        q0 = r0 / p.group; h0 = r0 - q0 * p.group;  // query and head of the tile's first row
+        const int qb = q0 + (int)((uint32_t)(h0 + n_rows - 1) * magic >> 16);
+        hi_min = min(v.len, hi_of(p, v, q0)); hi_max = min(v.len, hi_of(p, v, qb)); lo_min = lo_of(p, v, q0); lo_max = lo_of(p, v, qb);
         load_batch(c0);
 #pragma unroll
-        for (int x = 0; x < S::kStages; x++) ask(use + x, ahead_t0[x], ahead_exps[x]);
+        for (int x = 0; x < S::kEarly; x++) ask(use + x, ahead_t0[x], ahead_exps[x]);
+    };
+    open();
+    // (what the joining kernel has to know of the unit that this group's first chunk lies in)
+    if (gw == 0 && lane == 0) {
+        int4* cut = p.cut + 2 * me;
+        cut[0] = make_int4(head, r0, c0, per_unit);
+        cut[1] = make_int4(v.first, n_rows, 0, 0);
+    }
+
+    while (true) {
+#pragma unroll
+        for (int x = S::kEarly; x < S::kStages; x++) ask(use + x, ahead_t0[x], ahead_exps[x]);
+        auto query_of = [&](int row) -> int { return q0 + (int)((uint32_t)(h0 + row) * magic >> 16); };
+        auto head_of = [&](int row) -> int { return head * p.group + h0 + row - (int)((uint32_t)(h0 + row) * magic >> 16) * p.group; };
 
         // queries: column g of n8 tile i is row r0 + 8 i + g; a thread takes the elements 64 j + 16 t .. + 15
         uint32_t qb[NT][J][4][2];
@@ -342,7 +356,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
 #pragma unroll
                     for (int h = 0; h < 2; h++) sc[i][2 * h + b] = fmaf(sc[i][2 * h + b] + sd[i][2 * h + b], f, v_add);
                     if (!whole) {
-                        const int row = 8 * i + 2 * t + b, qi = query_of(row);
+                        const int row = 8 * i + 2 * t + b, qi = query_of(min(row, n_rows - 1));
                         const int hi = row < n_rows ? min(v.len, hi_of(p, v, qi)) : v.len, lo = row < n_rows ? lo_of(p, v, qi) : 0;  // (nobody reads columns without a row)
 #pragma unroll
                         for (int h = 0; h < 2; h++) {
@@ -429,13 +443,24 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
             use++;
         }
         if (!ok) {  // copies on their way land before the ring is used for anything else
+#pragma unroll
             for (int x = 0; x < S::kStages; x++)
                 if (ahead_t0[x] >= 0)
                     for (int y = 0; y < 2; y++) wait_landed(bars + 16 * ((use + x) % S::kStages) + 8 * y, ((use + x) / S::kStages) & 1u);
             __syncwarp();
         }
 
-        // ---- the four warps' sums of the segment, each in its own ring
+        // ---- the four warps' sums of the segment, each in its own ring; the next segment's first tiles are asked for before
+        const int done_rows = n_rows, done_q0 = q0, done_h0 = h0, done_head = head, done_first = v.first;
+        const bool is_whole = c0 == 0 && c1 == per_unit;
+        float* record = p.partial + (size_t)(2 * me + (c0 == 0 ? 1 : 0)) * S::kRecord;
+        x0 += c1 - c0;
+        const bool more = x0 < x_end;
+        const uint32_t place = ring - raw + (S::kEarly ? (use + S::kStages - 1) % S::kStages * 2 * S::kTile : 0u);
+#pragma unroll
+        for (int x = 0; x < S::kStages; x++) ahead_t0[x] = -1;
+        __syncwarp();
+        if (more) open();
 #pragma unroll
         for (int i = 0; i < NT; i++)
 #pragma unroll
@@ -448,13 +473,12 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
 #pragma unroll
                 for (int x = 0; x < MT; x += 2) {
                     const int d = D == 64 ? 8 * piece + 2 * x : 128 * (x / 8) + 16 * piece + 2 * (x % 8);
-                    reinterpret_cast<float4*>(my_sum)[sum_at<D>(row, d / 4)] = make_float4(o[i][x][b], o[i][x][2 + b], o[i][x + 1][b], o[i][x + 1][2 + b]);
+                    reinterpret_cast<float4*>(smem_raw + place)[sum_at<D>(row, d / 4)] = make_float4(o[i][x][b], o[i][x][2 + b], o[i][x + 1][b], o[i][x + 1][2 + b]);
                 }
             }
+        if (lane == 0) all_place[gw] = place;
         group_sync(grp);
-        const bool is_whole = c0 == 0 && c1 == k.per_unit;
-        float* record = p.partial + (size_t)(2 * me + (c0 == 0 ? 1 : 0)) * S::kRecord;
-        for (int i = gw * 32 + lane; i < n_rows * (D / 4); i += kGroupWarps * 32) {
+        for (int i = gw * 32 + lane; i < done_rows * (D / 4); i += kGroupWarps * 32) {
             const int row = i / (D / 4), f = i % (D / 4);
             float2 ml[kGroupWarps];
             float top = kNegInf, den = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
@@ -464,24 +488,30 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
             for (int w = 0; w < kGroupWarps; w++) {
                 const float h = part_factor(ml[w].x, top);
                 den += ml[w].y * h;
-                const float4 a = reinterpret_cast<const float4*>(smem_raw + (S::ring(raw, grp * kGroupWarps + w) - raw))[sum_at<D>(row, f)];
+                const float4 a = reinterpret_cast<const float4*>(smem_raw + all_place[w])[sum_at<D>(row, f)];
                 x[0] += a.x * h; x[1] += a.y * h; x[2] += a.z * h; x[3] += a.w * h;
             }
             if (is_whole) {
-                const int qi = query_of(row), h = head_of(row);
+                const int step = (int)((uint32_t)(done_h0 + row) * magic >> 16), h = done_head * p.group + done_h0 + row - step * p.group;
+                const long long tok = done_first + done_q0 + step;
                 const float inv = den == 0.f ? 0.f : 1.f / den;
 #pragma unroll
                 for (int y = 0; y < 4; y++) x[y] *= inv;
-                store_out4<DT>(p, (long long)(v.first + qi) * p.out_token + (long long)h * p.out_head + 4 * f, x);
-                if (p.lse && f == 0) p.lse[(long long)(v.first + qi) * p.heads + h] = lse_of(top, den, kPShift);
+                store_out4<DT>(p, tok * p.out_token + (long long)h * p.out_head + 4 * f, x);
+                if (p.lse && f == 0) p.lse[tok * p.heads + h] = lse_of(top, den, kPShift);
             } else {
                 *reinterpret_cast<float4*>(record + row * D + 4 * f) = make_float4(x[0], x[1], x[2], x[3]);
                 if (f == 0) *reinterpret_cast<float2*>(record + S::kRows * D + 2 * row) = make_float2(top, den);
             }
         }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the ring is the copies' again
-        if (group_any(grp, !ok)) break;
-        x0 += c1 - c0;
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the sums' place is the copies' again
+        if (group_any(grp, !ok) || !more) break;
+    }
+    if (!ok || *abort_flag) {
+#pragma unroll
+        for (int x = 0; x < S::kEarly; x++)
+            if (ahead_t0[x] >= 0)
+                for (int y = 0; y < 2; y++) wait_landed(bars + 16 * ((use + x) % S::kStages) + 8 * y, ((use + x) / S::kStages) & 1u);
     }
 }
 
@@ -493,24 +523,16 @@ __global__ void __launch_bounds__(kCombineThreads) cache_attention_combine_kerne
     using S = RowsShape<D, NT>;
     pdl_wait_prior_grid();
     pdl_launch_dependents();
-    const long long chunks = p.prefix[p.n_seqs];
-    const int groups = (int)min((long long)all_groups, chunks), b = (int)blockIdx.x + 1;
+    const int b = (int)blockIdx.x + 1;
+    const long long chunks = *p.chunks;
+    const int4 cut = p.cut[2 * b], of = p.cut[2 * b + 1];  // (of a group that has no chunks: not looked at)
+    const int groups = (int)min((long long)all_groups, chunks);
     if (b >= groups) return;
-    const long long x = share_of(chunks, b, groups);
-    int s = 0;
-    for (int n = p.n_seqs; n > 1;) {
-        const int half = n >> 1;
-        if (p.prefix[s + half] <= x) { s += half; n -= half; }
-        else n = half;
-    }
-    const SeqView v = seq_view(p, s);
-    const SeqChunks k(p, v, S::kRows);
-    const long long in_seq = x - p.prefix[s], unit = in_seq / k.per_unit, begin = p.prefix[s] + unit * k.per_unit, end = begin + k.per_unit;
-    if (x == begin || share_of(chunks, b - 1, groups) > begin) return;
+    const long long begin = share_of(chunks, b, groups) - cut.z, end = begin + cut.w;
+    if (cut.z == 0 || share_of(chunks, b - 1, groups) > begin) return;
     int parts = 2;  // groups b - 1 .. b - 2 + parts
     while (b - 1 + parts < groups && share_of(chunks, b - 1 + parts, groups) < end) parts++;
-    const int head = (int)(unit / k.tiles), r0 = (int)(unit - (long long)head * k.tiles) * S::kRows;
-    const int n_rows = (int)min((long long)S::kRows, (long long)v.n_q * p.group - r0);
+    const int head = cut.x, r0 = cut.y, first = of.x, n_rows = of.y;
     auto record = [&](int i) { return p.partial + (size_t)(2 * (b - 1 + i) + (i == 0 ? 1 : 0)) * S::kRecord; };
     for (int i = threadIdx.x; i < n_rows * (D / 4); i += kCombineThreads) {
         const int row = i / (D / 4), d = (i - row * (D / 4)) * 4;
@@ -529,8 +551,8 @@ __global__ void __launch_bounds__(kCombineThreads) cache_attention_combine_kerne
         const float inv = den == 0.f ? 0.f : 1.f / den;
 #pragma unroll
         for (int y = 0; y < 4; y++) o[y] *= inv;
-        store_out4<DT>(p, (long long)(v.first + qi) * p.out_token + (long long)h * p.out_head + d, o);
-        if (p.lse && d == 0) p.lse[(long long)(v.first + qi) * p.heads + h] = lse_of(top, den, kPShift);
+        store_out4<DT>(p, (long long)(first + qi) * p.out_token + (long long)h * p.out_head + d, o);
+        if (p.lse && d == 0) p.lse[(long long)(first + qi) * p.heads + h] = lse_of(top, den, kPShift);
     }
 }
 
@@ -583,15 +605,15 @@ __global__ void __launch_bounds__(kThreads) cache_attention_specials_kernel(cons
 // ---------------------------------------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------------------------------------
-constexpr size_t kHeadBytes = 256 + ((size_t)HIF8_CACHE_MAX_SEQS + 1) * 8 + 248;  // status word, chunks in front of each sequence
-static_assert(kHeadBytes % 256 == 0, "what follows is aligned");
+constexpr size_t kHeadBytes = 256;  // status word, flag of specials, chunks in all
 
 // n8 tiles of query rows that a warp takes: two where the rows fill more than one and the registers allow it
 int row_tiles_of(int max_q, int group, int dim) { return (long long)max_q * group > 8 && dim <= 128 ? 2 : 1; }
 
 size_t partial_bytes(int dim, int nt)
 {
-    return round_up_256((size_t)2 * (kMaxBlocks * groups_of(dim, nt)) * 8 * nt * (dim + 2) * 4);
+    const size_t groups = (size_t)kMaxBlocks * groups_of(dim, nt);
+    return round_up_256(groups * 32) + round_up_256(2 * groups * 8 * nt * (dim + 2) * 4);
 }
 
 // The pool of K or V as rows of head_dim bytes, boxes of 16 tokens (128 bytes of each at most), swizzled.  Encoded anew in every call: it holds no more than
@@ -713,8 +735,9 @@ extern "C" int hif8_cache_attention(const void* q, int dtype, int64_t q_token_st
     p.out = out; p.out_token = out_token_stride; p.out_head = out_head_stride; p.lse = lse;
     uint8_t* ws = reinterpret_cast<uint8_t*>(workspace);
     p.status = reinterpret_cast<int*>(ws);
-    p.prefix = reinterpret_cast<long long*>(ws + 256);
-    p.partial = reinterpret_cast<float*>(ws + kHeadBytes);
+    p.chunks = reinterpret_cast<long long*>(ws + 8);
+    p.cut = reinterpret_cast<int4*>(ws + kHeadBytes);
+    p.partial = reinterpret_cast<float*>(ws + kHeadBytes + round_up_256((size_t)kMaxBlocks * groups_of(head_dim, nt) * 32));
     cudaStream_t st = (cudaStream_t)stream;
     const size_t tiles = prefill_workspace_bytes(n_seqs, n_q, max_q, max_length, heads, kv_heads, head_dim);
     cudaError_t rc;

@@ -32,7 +32,8 @@ struct AttentionParams {
     float* lse;
     int* status;
     int* special_flag;              // chunks: whether cache_attention_specials_kernel has anything to do; NULL: it looks for itself
-    long long* prefix;              // chunks in front of each sequence
+    long long* chunks;              // few rows: chunks in all
+    int4* cut;                      // two of each group: key head, first row, chunk, chunks of the unit that its first chunk lies in; first query, rows
     float* partial;
 };
 
