@@ -13,7 +13,7 @@
 namespace hif8 {
 namespace {
 
-constexpr float kPShift = 8.f;
+constexpr float kPShift = 8.f, kPLimit = 14.f;  // weights are 2^(x - m + 8) with m an earlier maximum, up to 2^14 of FP16's 2^16
 
 __device__ __forceinline__ void mma_16816_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
@@ -60,7 +60,7 @@ struct RowsShape {
     // where a warp's sums fit in one stage of its ring, the next segment's first tiles are on their way in the others while the sums are joined
     static constexpr int kEarly = kRows * D * 4 <= 2 * (int)kTile ? kStages - 1 : 0;
     // offsets from the block's first byte, which is 1024 modulo 65536
-    static constexpr uint32_t kMl = (HIF8_CACHE_MAX_SEQS + 2) * 8, kScan = kMl + kWarps * kRows * 8, kPlace = kScan + 32 * 8, kBars = kPlace + kWarps * 8, kFlag = kBars + kWarps * kStages * 16;
+    static constexpr uint32_t kMl = (HIF8_CACHE_MAX_SEQS + 2) * 8, kScan = kMl + kWarps * kRows * 8, kPlace = kScan + 32 * 8, kBars = kPlace + kWarps * 8, kFlag = kBars + kWarps * kStages * 8;
     static constexpr uint32_t kFrontRing = kLutBytes - 1024 - kFrontWarps * kRing, kLut = kLutBytes - 1024, kBackRing = kLut + kLutBytes;
     static constexpr uint32_t kSmem = kBackRing + (kWarps < kBackWarps ? kWarps : kBackWarps) * kRing;
     static_assert(kFlag + 16 <= kFrontRing && kSmem <= 227 * 1024 && kRows * D * 4 <= kRing, "shared memory");
@@ -131,9 +131,9 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
             *reinterpret_cast<uint4*>(lut_words + (i >> 3) * 64 + (i & 7) * 4) = make_uint4(v, v, v, v);
         }
     }
-    const uint32_t bars = raw + S::kBars + warp * S::kStages * 16;  // of stage x: keys at 16 x, values at 16 x + 8
+    const uint32_t bars = raw + S::kBars + warp * S::kStages * 8;
     if (lane == 0) {
-        for (int x = 0; x < 2 * S::kStages; x++) mbar_init(bars + 8 * x, 1);
+        for (int x = 0; x < S::kStages; x++) mbar_init(bars + 8 * x, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (threadIdx.x == 0) *abort_flag = 0;
@@ -207,15 +207,14 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
         const int i = __ffs(b_live) - 1, row = __shfl_sync(0xFFFFFFFFu, b_row, i);
         t0 = lo_chunk + (b_first + i) * kChunk + 16 * gw;
         b_live &= b_live - 1;
-        const uint32_t st = n % S::kStages, at = ring + st * 2 * S::kTile, bar = bars + 16 * st;
+        const uint32_t st = n % S::kStages, at = ring + st * 2 * S::kTile, bar = bars + 8 * st;
         __syncwarp();  // every lane has read what the stage held
         if (elect_one()) {
-            mbar_expect(bar, S::kTile);
+            mbar_expect(bar, 2 * S::kTile);
             tma_load_2d(at, &map_k, 0, row, bar);
             if (D == 256) tma_load_2d(at + 2048, &map_k, 128, row, bar);
-            mbar_expect(bar + 8, S::kTile);
-            tma_load_2d(at + S::kTile, &map_v, 0, row, bar + 8);
-            if (D == 256) tma_load_2d(at + S::kTile + 2048, &map_v, 128, row, bar + 8);
+            tma_load_2d(at + S::kTile, &map_v, 0, row, bar);
+            if (D == 256) tma_load_2d(at + S::kTile + 2048, &map_v, 128, row, bar);
         }
         __syncwarp();
         exps = __shfl_sync(0xFFFFFFFFu, b_exps, i);  // (behind the copies, which need not wait for them)
@@ -303,14 +302,17 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
                 for (int st = 0; st < 4; st++) { qb[i][j][st][0] = w[j][2 * st]; qb[i][j][st][1] = w[j][2 * st + 1]; }
 #pragma unroll
             for (int b = 0; b < 2; b++)  // the scores' columns of this thread: rows 2 t and 2 t + 1 of the tile
-                row_mul[i][b] = fminf(p.scale_log2 * pow2_clamped(-__shfl_sync(0xFFFFFFFFu, e, 4 * (2 * t + b))), 3.0e38f);
+                row_mul[i][b] = fminf(p.scale_log2 * pow2_clamped(-__shfl_sync(0xFFFFFFFFu, e, 4 * (2 * t + b))), 3.0e23f);  // (times 2^48 within the finite floats)
         }
 
-        float m[NT][2], l[NT][2], o[NT][MT][4];
+        // base: the maximum that the weights refer to, 0 before there is one; limit: what an argument may be without a new one; far: a base that an FMA cannot take
+        float m[NT][2], l[NT][2], base[NT][2], limit[NT][2], o[NT][MT][4];
+        bool far = false;
 #pragma unroll
         for (int i = 0; i < NT; i++) {
             m[i][0] = m[i][1] = kNegInf;
-            l[i][0] = l[i][1] = 0.f;
+            l[i][0] = l[i][1] = base[i][0] = base[i][1] = 0.f;
+            limit[i][0] = limit[i][1] = kNegInf;
 #pragma unroll
             for (int x = 0; x < MT; x++)
 #pragma unroll
@@ -319,7 +321,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
 
         while (ahead_t0[0] >= 0) {
             const int t0 = ahead_t0[0], exps = ahead_exps[0];
-            const uint32_t st = use % S::kStages, parity = (use / S::kStages) & 1u, at_k = ring + st * 2 * S::kTile, at_v = at_k + S::kTile, bar = bars + 16 * st;
+            const uint32_t st = use % S::kStages, parity = (use / S::kStages) & 1u, at_k = ring + st * 2 * S::kTile, at_v = at_k + S::kTile, bar = bars + 8 * st;
             ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag, p.status, 61));
             if (!ok) break;
             // scores, transposed: operand row g (+ 8) x rows 2 t, 2 t + 1.  (Two sums, so that a product does not wait for the one in front of it.)
@@ -346,15 +348,21 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
             const bool whole = t0 >= lo_max && t0 + 16 <= hi_min;  // every row sees every token
             const int ke = (int)(signed char)(exps & 0xFF), ve = exps >> 8;
             const float k_mul = pow2f(-ke), v_mul = pow2f(ve), v_add = (float)-ve;
-            float top[NT][2];
+            // Arguments of the exponentials, x - base + 8 in one FMA; the maximum is only looked for when one of them has outgrown the weights' range in FP16
+            // by now (x > base + 6), or there was none before.
+            auto argument = [&](int i, int h, int b, float f) -> float {
+                const float y = sc[i][2 * h + b];
+                return far ? fmaf(y, f, v_add) - base[i][b] + kPShift : fmaf(y, f, v_add - base[i][b] + kPShift);  // (for large scores base - 8 is not exact, the difference is)
+            };
+            float e[NT][4];
             bool grows = false;
 #pragma unroll
             for (int i = 0; i < NT; i++) {
 #pragma unroll
                 for (int b = 0; b < 2; b++) {
-                    const float f = fminf(row_mul[i][b] * k_mul, 3.0e38f);
+                    const float f = row_mul[i][b] * k_mul;
 #pragma unroll
-                    for (int h = 0; h < 2; h++) sc[i][2 * h + b] = fmaf(sc[i][2 * h + b] + sd[i][2 * h + b], f, v_add);
+                    for (int h = 0; h < 2; h++) sc[i][2 * h + b] += sd[i][2 * h + b];
                     if (!whole) {
                         const int row = 8 * i + 2 * t + b, qi = query_of(min(row, n_rows - 1));
                         const int hi = row < n_rows ? min(v.len, hi_of(p, v, qi)) : v.len, lo = row < n_rows ? lo_of(p, v, qi) : 0;  // (nobody reads columns without a row)
@@ -364,42 +372,51 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
                             if (tok < lo || tok >= hi) sc[i][2 * h + b] = kNegInf;
                         }
                     }
-                    float a = fmaxf(sc[i][b], sc[i][2 + b]);
-                    a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 4));
-                    a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 8));
-                    a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 16));
-                    top[i][b] = a;
-                    grows |= a > m[i][b];
+#pragma unroll
+                    for (int h = 0; h < 2; h++) {
+                        e[i][2 * h + b] = argument(i, h, b, f);
+                        grows |= e[i][2 * h + b] > limit[i][b];
+                    }
                 }
             }
             if (__any_sync(0xFFFFFFFFu, grows)) {
+                bool large = false;
 #pragma unroll
                 for (int i = 0; i < NT; i++)
 #pragma unroll
                     for (int b = 0; b < 2; b++) {
-                        const float n = fmaxf(m[i][b], top[i][b]), f = part_factor(m[i][b], n);
+                        const float f = row_mul[i][b] * k_mul;
+                        float a = fmaxf(fmaf(sc[i][b], f, v_add), fmaf(sc[i][2 + b], f, v_add));
+                        a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 4));
+                        a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 8));
+                        a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 16));
+                        const float n = fmaxf(m[i][b], a), g0 = part_factor(m[i][b], n);
                         m[i][b] = n;
-                        l[i][b] *= f;
+                        base[i][b] = n == kNegInf ? 0.f : n;
+                        limit[i][b] = n == kNegInf ? kNegInf : kPLimit;
+                        large |= fabsf(base[i][b]) > 131072.f;
+                        l[i][b] *= g0;
 #pragma unroll
-                        for (int x = 0; x < MT; x++) { o[i][x][b] *= f; o[i][x][2 + b] *= f; }
+                        for (int x = 0; x < MT; x++) { o[i][x][b] *= g0; o[i][x][2 + b] *= g0; }
                     }
+                far = __any_sync(0xFFFFFFFFu, large);
+#pragma unroll
+                for (int i = 0; i < NT; i++)
+#pragma unroll
+                    for (int b = 0; b < 2; b++)
+#pragma unroll
+                        for (int h = 0; h < 2; h++) e[i][2 * h + b] = argument(i, h, b, row_mul[i][b] * k_mul);
             }
             uint32_t pb[NT][2];
 #pragma unroll
             for (int i = 0; i < NT; i++) {
-                float e[4];
 #pragma unroll
-                for (int b = 0; b < 2; b++) {
-                    const float base = m[i][b] == kNegInf ? 0.f : m[i][b];
-                    e[b] = exp2_approx(sc[i][b] - base + kPShift);  // (the difference is exact where it counts; base - 8 is not for large scores)
-                    e[2 + b] = exp2_approx(sc[i][2 + b] - base + kPShift);
-                    l[i][b] = fmaf(e[b] + e[2 + b], v_mul, l[i][b]);
-                }
-                pb[i][0] = transpose_8x8(pack_f16(e[0], e[1]));
-                pb[i][1] = transpose_8x8(pack_f16(e[2], e[3]));
+                for (int y = 0; y < 4; y++) e[i][y] = exp2_approx(e[i][y]);
+#pragma unroll
+                for (int b = 0; b < 2; b++) l[i][b] = fmaf(e[i][b] + e[i][2 + b], v_mul, l[i][b]);
+                pb[i][0] = transpose_8x8(pack_f16(e[i][0], e[i][1]));
+                pb[i][1] = transpose_8x8(pack_f16(e[i][2], e[i][3]));
             }
-            ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar + 8, parity, abort_flag, p.status, 62));
-            if (!ok) break;
             uint32_t vw[4][VB / 4];  // of the tokens in operand rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9
 #pragma unroll
             for (int h = 0; h < 4; h++) {
@@ -446,7 +463,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
 #pragma unroll
             for (int x = 0; x < S::kStages; x++)
                 if (ahead_t0[x] >= 0)
-                    for (int y = 0; y < 2; y++) wait_landed(bars + 16 * ((use + x) % S::kStages) + 8 * y, ((use + x) / S::kStages) & 1u);
+                    wait_landed(bars + 8 * ((use + x) % S::kStages), ((use + x) / S::kStages) & 1u);
             __syncwarp();
         }
 
@@ -511,7 +528,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
 #pragma unroll
         for (int x = 0; x < S::kEarly; x++)
             if (ahead_t0[x] >= 0)
-                for (int y = 0; y < 2; y++) wait_landed(bars + 16 * ((use + x) % S::kStages) + 8 * y, ((use + x) / S::kStages) & 1u);
+                wait_landed(bars + 8 * ((use + x) % S::kStages), ((use + x) / S::kStages) & 1u);
     }
 }
 
