@@ -204,6 +204,18 @@ template <int DT> __device__ __forceinline__ void store_out4(const AttentionPara
     if (p.vectors) *reinterpret_cast<uint2*>(out) = w;
     else { out[0] = (unsigned short)w.x; out[1] = (unsigned short)(w.x >> 16); out[2] = (unsigned short)w.y; out[3] = (unsigned short)(w.y >> 16); }
 }
+template <int DT> __device__ __forceinline__ void store_out8(const AttentionParams& p, long long at, const float (&x)[8])
+{
+    if (p.vectors) *reinterpret_cast<uint4*>(reinterpret_cast<unsigned short*>(p.out) + at) =
+                       make_uint4(pack_out<DT>(x[0], x[1]), pack_out<DT>(x[2], x[3]), pack_out<DT>(x[4], x[5]), pack_out<DT>(x[6], x[7]));
+    else {
+#pragma unroll
+        for (int y = 0; y < 8; y += 4) {
+            const float z[4] = {x[y], x[y + 1], x[y + 2], x[y + 3]};
+            store_out4<DT>(p, at + y, z);
+        }
+    }
+}
 // from a row's maximum, its denominator and the power of two that the weights carry
 __device__ __forceinline__ float lse_of(float m, float l, float shift) { return l == 0.f ? kNegInf : (m - shift + log2f(l)) * kLn2; }
 __device__ __forceinline__ float part_factor(float m, float top) { return m == kNegInf ? 0.f : exp2_approx(m - top); }

@@ -17,11 +17,11 @@ namespace {
 constexpr int kTileRows = 128, kPairRows = 256, kTileTokens = 128;
 constexpr float kShift = 4.f, kLazy = 8.f;
 constexpr int kStages = 4;
-constexpr int kTmaWarp = 8, kMmaWarp = 9, kThreadsA = 12 * 32;
-// Registers: 168 a thread at launch, 64512 in all; the eight warps that hold rows of scores take 208, the third group of four warps (two of them idle) 88.
+constexpr int kTmaWarp = 8, kMmaWarp = 9, kPlanWarp = 10, kThreadsA = 12 * 32;
+// Registers: 168 a thread at launch, 64512 in all; the eight warps that hold rows of scores take 208, the third group of four warps (one of them idle) 88.
 constexpr int kRegsRows = 208, kRegsOther = 88;
 static_assert(256 * kRegsRows + 128 * kRegsOther <= kThreadsA * 168, "no more than the block has");
-constexpr int kMetaRing = 8, kSegRing = 4;
+constexpr int kMetaRing = 8, kSegRing = 4, kSegReaders = 10;  // (the copying warp, the products' and eight of rows)
 
 struct PrefillParams {
     AttentionParams a;
@@ -288,22 +288,23 @@ __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.
 __device__ __forceinline__ bool warp_all(bool x) { return __all_sync(0xFFFFFFFFu, x); }
 __device__ __forceinline__ bool warp_any(bool x) { return __any_sync(0xFFFFFFFFu, x); }
 
-// What the copying warp tells the others of a segment: tiles c0 .. c1 of a unit (a pair of row tiles of a sequence and key head).  tiles == 0: there is no other.
+// What the planning warp tells the others of a segment: tiles c0 .. c1 of a unit (a pair of row tiles of a sequence and key head).  tiles == 0: there is no other.
 struct SegmentInfo {
     int tiles, head, first, n_q, len, r0, n_rows, t0, lo_max, hi_min, whole, from_start;  // t0: first token of the first tile; whole: c0 == 0 and c1 the unit's tiles
-    int pad[4];
+    int q_row, block0, pad[2];                                                          // first row of the packed queries, first block of tokens
 };
 static_assert(sizeof(SegmentInfo) == 64, "read in 16-byte pieces");
 
 template <int D>
 struct PrefillSmem {
+    static constexpr int kQBufs = D == 64 ? 2 : 1;  // (short units, as windows and short prompts have them, wait for their queries otherwise: see the kernel's figures)
     static constexpr uint32_t kQ = kTileRows * D * 2, kStage = kTileTokens * D * 2;
-    static constexpr uint32_t q = 0, stages = 2 * kQ, meta = stages + kStages * kStage, seg = meta + kMetaRing * 128, bars = seg + kSegRing * 64;
-    // barriers: queries there / free, stages full / empty, factors of a tile there, segment told, scores there [2], weights there (half of them, all) [2], sums complete, sums read,
-    // all products ended (after a wait that gave up)
-    static constexpr uint32_t q_full = bars, q_empty = bars + 8, full = bars + 16, empty = full + 8 * kStages, meta_full = empty + 8 * kStages, seg_full = meta_full + 8 * kMetaRing,
-                              s_full = seg_full + 8 * kSegRing, p_half = s_full + 16, p_full = p_half + 16, o_full = p_full + 16, o_empty = o_full + 8, drain = o_empty + 8, tmem_slot = drain + 8,
-                              abort_flag = tmem_slot + 4, total = abort_flag + 4;
+    static constexpr uint32_t q = 0, stages = kQBufs * 2 * kQ, meta = stages + kStages * kStage, seg = meta + kMetaRing * 128, bars = seg + kSegRing * 64;
+    // barriers: queries there / free, stages full / empty, factors of a tile there, segment told / read, scores there [2], weights there (half of them, all) [2], sums complete, sums
+    // read, all products ended (after a wait that gave up)
+    static constexpr uint32_t q_full = bars, q_empty = q_full + 8 * kQBufs, full = q_empty + 8 * kQBufs, empty = full + 8 * kStages, meta_full = empty + 8 * kStages,
+                              seg_full = meta_full + 8 * kMetaRing, seg_empty = seg_full + 8 * kSegRing, s_full = seg_empty + 8 * kSegRing, p_half = s_full + 16, p_full = p_half + 16,
+                              o_full = p_full + 16, o_empty = o_full + 8, drain = o_empty + 8, tmem_slot = drain + 8, abort_flag = tmem_slot + 4, total = abort_flag + 4;
     static constexpr uint32_t kBytes = total + 1024;
     static_assert(kBytes <= 227 * 1024, "shared memory");
 };
@@ -320,11 +321,12 @@ struct Segment {
         const long long per_head = p.tiles_at[p.pairs];
         head = (int)(x0 / per_head);
         const long long x = x0 - head * per_head;
-        int a = 0;  // last pair that starts at or before x (empty ones share their start with the next)
+        int a = 0;  // last pair that starts at or before x (empty ones share their start with the next); one probe a lane and round
         for (int n = p.pairs; n > 1;) {
-            const int half = n >> 1;
-            if (p.tiles_at[a + half] <= x) { a += half; n -= half; }
-            else n = half;
+            const int step = (n + 31) >> 5, i = ((int)threadIdx.x & 31) * step;
+            const int last = 31 - __clz(__ballot_sync(0xFFFFFFFFu, i == 0 || (i < n && p.tiles_at[a + i] <= x)));
+            a += last * step;
+            n = min(step, n - last * step);
         }
         pair = a;
         u = pair_view(p, p.pair_seq[a], a);
@@ -383,10 +385,10 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sm + L::tmem_slot);
     auto bar = [&](uint32_t at, int i = 0) { return base + at + 8u * i; };
     if (threadIdx.x == 0) {
-        mbar_init(bar(L::q_full), 1); mbar_init(bar(L::q_empty), 1);
+        for (int i = 0; i < L::kQBufs; i++) { mbar_init(bar(L::q_full, i), 1); mbar_init(bar(L::q_empty, i), 1); }
         for (int i = 0; i < kStages; i++) { mbar_init(bar(L::full, i), 1); mbar_init(bar(L::empty, i), 1); }
         for (int i = 0; i < kMetaRing; i++) mbar_init(bar(L::meta_full, i), 1);
-        for (int i = 0; i < kSegRing; i++) mbar_init(bar(L::seg_full, i), 1);
+        for (int i = 0; i < kSegRing; i++) { mbar_init(bar(L::seg_full, i), 1); mbar_init(bar(L::seg_empty, i), kSegReaders); }
         for (int i = 0; i < 2; i++) { mbar_init(bar(L::s_full, i), 1); mbar_init(bar(L::p_half, i), 4); mbar_init(bar(L::p_full, i), 4); }
         mbar_init(bar(L::o_full), 1); mbar_init(bar(L::o_empty), 8); mbar_init(bar(L::drain), 1);
         *abort_flag = 0;
@@ -407,57 +409,66 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
     const int me = blockIdx.x;
     bool ok = true;
     uint32_t seg = 0;  // segments so far
-    // the next segment, as the copying warp tells it (four are kept: it is at most one ahead of the products, those one ahead of the rows' warps)
-    auto next_segment = [&](SegmentInfo& g, int where) -> bool {
+    auto next_segment = [&](SegmentInfo& g, int where) -> bool {  // as the planning warp tells it
         ok = warp_all(mbar_wait(bar(L::seg_full, seg % kSegRing), (seg / kSegRing) & 1u, abort_flag, p.a.status, where));
         if (!ok) return false;
         const int4* from = reinterpret_cast<const int4*>(sm + L::seg + (seg % kSegRing) * 64);
-        const int4 a = from[0], b = from[1], c = from[2];
+        const int4 a = from[0], b = from[1], c = from[2], d = from[3];
         g.tiles = a.x; g.head = a.y; g.first = a.z; g.n_q = a.w; g.len = b.x; g.r0 = b.y; g.n_rows = b.z; g.t0 = b.w; g.lo_max = c.x; g.hi_min = c.y; g.whole = c.z; g.from_start = c.w;
+        g.q_row = d.x; g.block0 = d.y;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(L::seg_empty, seg % kSegRing));
         return g.tiles > 0;
     };
 
     // (each branch sets its own count of registers: the compiler works by the smallest that reaches a place)
     if (warp >= kTmaWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
-    if (warp == kTmaWarp) {
+    if (warp == kPlanWarp) {  // up to kSegRing segments ahead: finding one takes a handful of loads that wait for one another
         const long long all = p.tiles_at[p.pairs] * p.a.c.heads;
         const int blocks = (int)min((long long)gridDim.x, all);
         long long x0 = me < blocks ? share_of(all, me, blocks) : 0;
         const long long x_end = me < blocks ? share_of(all, me + 1, blocks) : 0;
-        uint32_t n = 0, tile = 0;  // copies into the ring; tiles so far
-        auto tell = [&](const SegmentInfo& g) {
+        for (bool more = true; more; seg++) {
+            int4 info[4] = {make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0)};
+            more = x0 < x_end;
+            if (more) {
+                const Segment g(p, x0, x_end);
+                if (seg == 0 && lane == 0) p.cut[me] = make_int4(g.pair, g.u.seq, g.head, g.c0);
+                info[0] = make_int4(g.c1 - g.c0, g.head, g.u.v.first, g.u.v.n_q);
+                info[1] = make_int4(g.u.v.len, g.u.r0, g.u.n_rows, g.u.base + (g.u.j0 + g.c0) * kTileTokens);
+                info[2] = make_int4(g.u.lo_max, g.u.hi_min, g.c0 == 0 && g.c1 == g.u.tiles, g.c0 == 0);
+                info[3] = make_int4((int)(g.head * p.rows + (long long)g.u.v.first * p.a.group + g.u.r0), p.block_at[g.u.seq] + g.u.j0 + g.c0, 0, 0);
+                x0 += g.c1 - g.c0;
+            }
+            if (seg >= kSegRing) ok = warp_all(mbar_wait(bar(L::seg_empty, seg % kSegRing), (seg / kSegRing - 1) & 1u, abort_flag, p.a.status, 84));
+            if (!ok) break;
             if (lane == 0) {
                 int4* to = reinterpret_cast<int4*>(sm + L::seg + (seg % kSegRing) * 64);
-                to[0] = make_int4(g.tiles, g.head, g.first, g.n_q);
-                to[1] = make_int4(g.len, g.r0, g.n_rows, g.t0);
-                to[2] = make_int4(g.lo_max, g.hi_min, g.whole, g.from_start);
+                for (int i = 0; i < 4; i++) to[i] = info[i];
                 mbar_arrive(bar(L::seg_full, seg % kSegRing));
             }
             __syncwarp();
-        };
-        SegmentInfo t;
-        while (x0 < x_end) {
-            const Segment g(p, x0, x_end);
-            if (seg == 0 && lane == 0) p.cut[me] = make_int4(g.pair, g.u.seq, g.head, g.c0);
-            t.tiles = g.c1 - g.c0; t.head = g.head; t.first = g.u.v.first; t.n_q = g.u.v.n_q; t.len = g.u.v.len; t.r0 = g.u.r0; t.n_rows = g.u.n_rows;
-            t.t0 = g.u.base + (g.u.j0 + g.c0) * kTileTokens; t.lo_max = g.u.lo_max; t.hi_min = g.u.hi_min; t.whole = g.c0 == 0 && g.c1 == g.u.tiles; t.from_start = g.c0 == 0;
-            tell(t);
-            const bool two = g.u.n_rows > kTileRows;
-            if (seg) ok = warp_all(mbar_wait(bar(L::q_empty), (seg - 1) & 1u, abort_flag, p.a.status, 71));
+        }
+    } else if (warp == kTmaWarp) {
+        uint32_t n = 0, tile = 0;  // copies into the ring; tiles so far
+        SegmentInfo g;
+        while (next_segment(g, 85)) {
+            const bool two = g.n_rows > kTileRows;
+            const uint32_t qb = seg % L::kQBufs;
+            if (seg >= L::kQBufs) ok = warp_all(mbar_wait(bar(L::q_empty, qb), (seg / L::kQBufs - 1) & 1u, abort_flag, p.a.status, 71));
             if (!ok) break;
-            const int q_row = (int)(g.head * p.rows + (long long)g.u.v.first * p.a.group + g.u.r0);
             if (elect_one()) {
-                mbar_expect(bar(L::q_full), two ? 2 * L::kQ : L::kQ);
+                mbar_expect(bar(L::q_full, qb), two ? 2 * L::kQ : L::kQ);
                 for (int i = 0; i < (two ? 2 : 1); i++)
 #pragma unroll
-                    for (int c = 0; c < D / 64; c++) tma_load_2d(base + L::q + i * L::kQ + c * (kTileRows * 128), &map_q, c * 64, q_row + i * kTileRows, bar(L::q_full));
+                    for (int c = 0; c < D / 64; c++)
+                        tma_load_2d(base + L::q + (2 * qb + i) * L::kQ + c * (kTileRows * 128), &map_q, c * 64, g.q_row + i * kTileRows, bar(L::q_full, qb));
             }
             __syncwarp();
             seg++;
-            const int block0 = p.block_at[g.u.seq] + g.u.j0 + g.c0;
-            for (int j = 0; j < t.tiles && ok; j++, tile++) {
-                const int blk = min(block0 + j, p.cap_blocks - 1);  // (beyond: lengths above max_length)
+            for (int j = 0; j < g.tiles && ok; j++, tile++) {
+                const int blk = min(g.block0 + j, p.cap_blocks - 1);  // (beyond: lengths above max_length)
                 const int row = (int)(((long long)g.head * p.cap_blocks + blk) * kTileTokens);
                 for (int kv = 0; kv < 2; kv++, n++) {
                     const uint32_t st = n % kStages;
@@ -477,11 +488,9 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                 }
             }
             if (!ok) break;
-            x0 += t.tiles;
         }
-        if (ok) { t.tiles = 0; tell(t); }
         if (!ok || warp_any(*abort_flag)) {  // copies on their way land before the block's shared memory becomes another's
-            if (seg) wait_landed(bar(L::q_full), (seg - 1) & 1u);
+            for (uint32_t i = seg > L::kQBufs ? seg - L::kQBufs : 0; i < seg; i++) wait_landed(bar(L::q_full, i % L::kQBufs), (i / L::kQBufs) & 1u);
             for (uint32_t i = n > kStages ? n - kStages : 0; i < n; i++) wait_landed(bar(L::full, i % kStages), (i / kStages) & 1u);
             const uint32_t asked = (n + 1) / 2;  // tiles whose keys, and with them factors, were asked for
             for (uint32_t i = asked > kMetaRing ? asked - kMetaRing : 0; i < asked; i++) wait_landed(bar(L::meta_full, i % kMetaRing), (i / kMetaRing) & 1u);
@@ -493,11 +502,12 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
         SegmentInfo g;
         while (next_segment(g, 81)) {
             const int both = g.n_rows > kTileRows ? 2 : 1, tiles = g.tiles;
-            ok = warp_all(mbar_wait(bar(L::q_full), seg & 1u, abort_flag, p.a.status, 73));
+            const uint32_t qb = seg % L::kQBufs;
+            ok = warp_all(mbar_wait(bar(L::q_full, qb), (seg / L::kQBufs) & 1u, abort_flag, p.a.status, 73));
             if (!ok) break;
             auto scores = [&](int i, uint32_t st) {
                 if (elect_one()) {
-                    const uint64_t da = make_smem_desc(base + L::q + i * L::kQ, 16, 1024), db = make_smem_desc(base + L::stages + st * L::kStage, 16, 1024);
+                    const uint64_t da = make_smem_desc(base + L::q + (2 * qb + i) * L::kQ, 16, 1024), db = make_smem_desc(base + L::stages + st * L::kStage, 16, 1024);
 #pragma unroll
                     for (int kk = 0; kk < D / 16; kk++) {
                         const uint64_t off = (uint64_t)((kk / 4) * (kTileRows * 128 / 16) + (kk % 4) * 2);
@@ -543,7 +553,7 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                 if (elect_one()) {
                     tc_commit(bar(L::empty, sv));
                     if (j + 1 < tiles) tc_commit(bar(L::empty, sk));
-                    else { tc_commit(bar(L::o_full)); tc_commit(bar(L::q_empty)); }
+                    else { tc_commit(bar(L::o_full)); tc_commit(bar(L::q_empty, qb)); }
                 }
                 __syncwarp();
                 n += j + 1 < tiles ? 2 : 1;
@@ -587,10 +597,14 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                     for (int c = 0; c < 4; c++) tmem_ld_x32(t_s + 32 * c, sr + 32 * c);
                     tmem_ld_wait();
                     if (t0 < g.lo_max || t0 + kTileTokens > g.hi_min) {  // some row does not see some token
-                        const int lo_c = lo - t0, hi_c = hi - t0;
 #pragma unroll
-                        for (int c = 0; c < 128; c++)
-                            if (c < lo_c || c >= hi_c) sr[c] = __float_as_uint(kNegInf);
+                        for (int c = 0; c < 4; c++) {
+                            const int lo_c = max(0, min(32, lo - t0 - 32 * c)), hi_c = max(0, min(32, hi - t0 - 32 * c));
+                            const uint32_t seen = (uint32_t)((1ull << hi_c) - 1ull) & ~(uint32_t)((1ull << lo_c) - 1ull);  // (a bit a column: one test each)
+#pragma unroll
+                            for (int y = 0; y < 32; y++)
+                                if (!(seen & (1u << y))) sr[32 * c + y] = __float_as_uint(kNegInf);
+                        }
                     }
                     float top = kNegInf;
 #pragma unroll
@@ -683,9 +697,11 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                     if (mine) {
                         if (g.whole) {
 #pragma unroll
-                            for (int y = 0; y < 32; y += 4) {
-                                const float x[4] = {__uint_as_float(o[y]) * inv, __uint_as_float(o[y + 1]) * inv, __uint_as_float(o[y + 2]) * inv, __uint_as_float(o[y + 3]) * inv};
-                                store_out4<DT>(p.a, tok * p.a.out_token + (long long)h * p.a.out_head + 32 * c + y, x);
+                            for (int y = 0; y < 32; y += 8) {
+                                float x[8];
+#pragma unroll
+                                for (int z = 0; z < 8; z++) x[z] = __uint_as_float(o[y + z]) * inv;
+                                store_out8<DT>(p.a, tok * p.a.out_token + (long long)h * p.a.out_head + 32 * c + y, x);
                             }
                         } else {
 #pragma unroll
