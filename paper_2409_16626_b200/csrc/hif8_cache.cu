@@ -33,55 +33,84 @@ struct AppendParams {
 };
 
 // A block of a cache (one page's tokens of one head of K or V) is converted by TEAM threads: their part of it stays in registers between the
-// reduction of its largest magnitude and the conversion, so the source is read once.  256 threads hold 64 KiB of source: pages of 128 tokens of
-// 128 FP32 elements, or of 256 16-bit ones.  A warp where a sequence has few new tokens (a step of decoding has one: 128 elements a block).
+// reduction of its largest magnitude and the conversion, so the source is read once, and the next block's part is on its way meanwhile; what a block has beyond what
+// they hold is read twice, the second time from L2.  A warp holds 2 KiB of a 16-bit source and 4 KiB of FP32, 256 threads 16 KiB and
+// 32 KiB (64 tokens of 128 elements), 512 threads 64 KiB: the smallest team that holds a block of the call takes it (27.7 K tokens of 8 heads, BF16, with the reading call, us: pages of 64 x 128
+// by 256 threads 70; of 128 x 128 by 256 / 512: 108 / 92; of 16 x 64 by 256 threads / a warp: 108 / 44).
+template <int SRC, int TEAM> struct AppendShape {
+    static constexpr int kBlock = TEAM > kThreads ? TEAM : kThreads;                       // threads of a block
+    static constexpr int kHeld = TEAM > kThreads || SRC == HIF8_F32 ? 8 : 4;               // vectors of a unit in a thread's registers
+};
 template <int MODE, int SRC, int TEAM>
-__global__ void __launch_bounds__(kThreads) cache_append_kernel(const AppendParams p)
+__global__ void __launch_bounds__(AppendShape<SRC, TEAM>::kBlock) cache_append_kernel(const AppendParams p)
 {
-    constexpr int PV = SrcTraits<SRC>::kPerVec, kHeld = 8;
+    constexpr int PV = SrcTraits<SRC>::kPerVec, kHeld = AppendShape<SRC, TEAM>::kHeld, kBlock = AppendShape<SRC, TEAM>::kBlock;
     __shared__ SmemTables s;
-    __shared__ uint32_t s_part[kThreads / 32];
-    setup_tables<true, MODE != HIF8_RND_TA, false, MODE, SRC>(s, p.flags);
+    __shared__ uint32_t s_part[2][kBlock / 32];
+    setup_tables<true, MODE != HIF8_RND_TA, false, MODE, SRC, kBlock>(s, p.flags);
     pdl_wait_prior_grid();
     pdl_launch_dependents();
     const int lane = threadIdx.x & 31, member = threadIdx.x % TEAM;
-    const int row_vecs = p.c.dim / PV;
-    for (long long u = (long long)blockIdx.x * (kThreads / TEAM) + threadIdx.x / TEAM; u < p.units; u += (long long)gridDim.x * (kThreads / TEAM)) {
-        const int part = (int)(u % (2 * p.c.heads)), head = part >> 1;
-        const bool is_v = part & 1;
-        Piece pc = find_piece(u / (2 * p.c.heads), p.start, p.lengths, p.n_seqs, p.n_new, p.c.shift, lane);
-        const int page = pc.count ? p.c.page_of(pc.seq, pc.pos >> p.c.shift) : -1;
-        if (page < 0) continue;  // (the same answer in the whole team)
-        const int slot = pc.pos & ((1 << p.c.shift) - 1), n_vec = pc.count * row_vecs;
-        const char* src = reinterpret_cast<const char*>(p.src[is_v]);
-        auto load = [&](int i) -> uint4 {
-            const int t = i / row_vecs;
-            const long long e = (long long)(pc.token + t) * p.token_stride + (long long)head * p.head_stride + (long long)(i - t * row_vecs) * PV;
-            if (p.vectors) return __ldcs(reinterpret_cast<const uint4*>(src + e * (16 / PV)));
-            uint32_t w[4];
+    const int row_vecs = p.c.dim / PV, row_shift = 31 - __clz(row_vecs);
+    UnitWalk walk(p.units, 2 * p.c.heads, (long long)blockIdx.x * (kBlock / TEAM) + threadIdx.x / TEAM, (long long)gridDim.x * (kBlock / TEAM));
+    // the unit that is loaded, in a thread's registers; the one before it is being converted
+    Piece pc;
+    int page = -1, n_vec = 0, n_units = 0;
+    const char* src = nullptr;
+    auto load = [&](const char* from, int i) -> uint4 {
+        const int t = i >> row_shift;
+        const long long e = (long long)t * p.token_stride + (long long)(i - (t << row_shift)) * PV;
+        if (p.vectors) return __ldcs(reinterpret_cast<const uint4*>(from + e * (16 / PV)));
+        uint32_t w[4];
 #pragma unroll
-            for (int j = 0; j < 4; j++)
-                w[j] = SRC == HIF8_F32 ? reinterpret_cast<const uint32_t*>(src)[e + j]
-                                       : (uint32_t)reinterpret_cast<const unsigned short*>(src)[e + 2 * j] | ((uint32_t)reinterpret_cast<const unsigned short*>(src)[e + 2 * j + 1] << 16);
-            return make_uint4(w[0], w[1], w[2], w[3]);
-        };
-        uint4 held[kHeld];
+        for (int j = 0; j < 4; j++)
+            w[j] = SRC == HIF8_F32 ? reinterpret_cast<const uint32_t*>(from)[e + j]
+                                   : (uint32_t)reinterpret_cast<const unsigned short*>(from)[e + 2 * j] | ((uint32_t)reinterpret_cast<const unsigned short*>(from)[e + 2 * j + 1] << 16);
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    };
+    uint4 held[kHeld];
+    auto begin = [&]() {  // the next unit that there is something of; n_vec = 0: there is none
+        n_vec = 0;
+        for (; walk.left > 0; walk.next()) {
+            if (walk.fresh || n_units == 0) {
+                pc = find_piece(walk.number, p.start, p.lengths, p.n_seqs, p.n_new, p.c.shift, lane);
+                page = pc.count ? p.c.page_of(pc.seq, pc.pos >> p.c.shift) : -1;
+            }
+            n_units++;
+            if (page < 0) continue;  // (the same answer in the whole team)
+            n_vec = pc.count << row_shift;
+            src = reinterpret_cast<const char*>(p.src[walk.part & 1]) + ((long long)pc.token * p.token_stride + (long long)(walk.part >> 1) * p.head_stride) * (16 / PV);
 #pragma unroll
-        for (int j = 0; j < kHeld; j++) held[j] = member + j * TEAM < n_vec ? load(member + j * TEAM) : make_uint4(0, 0, 0, 0);
+            for (int j = 0; j < kHeld; j++) held[j] = member + j * TEAM < n_vec ? load(src, member + j * TEAM) : make_uint4(0, 0, 0, 0);
+            return;
+        }
+    };
+    begin();
+    int parity = 0;
+    while (n_vec > 0) {
+        uint4 mine[kHeld];
+#pragma unroll
+        for (int j = 0; j < kHeld; j++) mine[j] = held[j];
+        const int count = n_vec, slot = pc.pos & ((1 << p.c.shift) - 1), head = walk.part >> 1;
+        const bool is_v = walk.part & 1;
+        const char* from = src;
         int* exps = (is_v ? p.c.v_exp : p.c.k_exp) + ((long long)page * p.c.heads + head);
+        uint8_t* dst = (is_v ? p.c.v : p.c.k) + p.c.block_at(page, head) + (long long)slot * p.c.dim;
+        walk.next();
+        begin();
         int e;
         if (slot) e = clamp_cache_exp(*exps);  // the block's first tokens set its exponent
         else {
             uint32_t acc = 0;
 #pragma unroll
-            for (int j = 0; j < kHeld; j++) acc = amax_vector<SRC>(acc, held[j]);
-            for (int i = member + kHeld * TEAM; i < n_vec; i += TEAM) acc = amax_vector<SRC>(acc, load(i));
+            for (int j = 0; j < kHeld; j++) acc = amax_vector<SRC>(acc, mine[j]);
+            for (int i = member + kHeld * TEAM; i < count; i += TEAM) acc = amax_vector<SRC>(acc, load(from, i));
             uint32_t a = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax_value<SRC>(acc)));
-            if (TEAM > 32) {
-                if (lane == 0) s_part[threadIdx.x >> 5] = a;
+            if (TEAM > 32) {  // (two places in turn: whoever is still reading one is waited for at the other's barrier)
+                if (lane == 0) s_part[parity][threadIdx.x >> 5] = a;
                 __syncthreads();
-                a = __reduce_max_sync(0xFFFFFFFFu, lane < TEAM / 32 ? s_part[lane] : 0u);
-                __syncthreads();
+                a = __reduce_max_sync(0xFFFFFFFFu, lane < TEAM / 32 ? s_part[parity][lane] : 0u);
+                parity ^= 1;
             }
             e = clamp_cache_exp(scale_exp_from_amax(a, p.target_exp));
             if (member == 0) *exps = e;
@@ -93,7 +122,6 @@ __global__ void __launch_bounds__(kThreads) cache_append_kernel(const AppendPara
         for (int j = 0; j < 4; j++) scale2[j] = bf16x2_of_pow2(scale);
 #pragma unroll
         for (int j = 0; j < 8; j++) scales[j] = scale;
-        uint8_t* dst = (is_v ? p.c.v : p.c.k) + p.c.block_at(page, head) + (long long)slot * p.c.dim;
         auto convert = [&](int i, const uint4& v) {
             uint2 w;
             if (MODE == HIF8_RND_TA) w = encode_vector_ta<SRC>(v, scale2, scales, s.ta);
@@ -113,25 +141,33 @@ __global__ void __launch_bounds__(kThreads) cache_append_kernel(const AppendPara
         };
 #pragma unroll
         for (int j = 0; j < kHeld; j++)
-            if (member + j * TEAM < n_vec) convert(member + j * TEAM, held[j]);
-        for (int i = member + kHeld * TEAM; i < n_vec; i += TEAM) convert(i, load(i));
+            if (member + j * TEAM < count) convert(member + j * TEAM, mine[j]);
+        for (int i = member + kHeld * TEAM; i < count; i += TEAM) convert(i, load(from, i));
     }
 }
 
-template <int MODE, int SRC>
-void launch_append(const AppendParams& p, bool few, int sms, cudaStream_t st)
+template <int MODE, int SRC, int TEAM>
+void launch_append_team(const AppendParams& p, int sms, cudaStream_t st)
 {
-    const long long per_block = few ? kThreads / 32 : 1, blocks = (p.units + per_block - 1) / per_block, most = (long long)sms * 4;
-    const dim3 grid((unsigned)(blocks < most ? blocks : most));
-    if (few) launch_pdl(cache_append_kernel<MODE, SRC, 32>, grid, st, p);
-    else launch_pdl(cache_append_kernel<MODE, SRC, kThreads>, grid, st, p);
+    constexpr int kBlock = AppendShape<SRC, TEAM>::kBlock;
+    const long long blocks = (p.units * TEAM + kBlock - 1) / kBlock, most = (long long)sms * 4;
+    launch_pdl_threads(kBlock, cache_append_kernel<MODE, SRC, TEAM>, dim3((unsigned)(blocks < most ? blocks : most)), st, p);
+}
+// tokens: what a sequence has in the mean, up to a page
+template <int MODE, int SRC>
+void launch_append(const AppendParams& p, int tokens, int sms, cudaStream_t st)
+{
+    const int vecs = tokens * p.c.dim / SrcTraits<SRC>::kPerVec;
+    if (vecs <= 32 * AppendShape<SRC, 32>::kHeld) launch_append_team<MODE, SRC, 32>(p, sms, st);
+    else if (vecs <= 256 * AppendShape<SRC, 256>::kHeld) launch_append_team<MODE, SRC, 256>(p, sms, st);
+    else launch_append_team<MODE, SRC, 512>(p, sms, st);
 }
 template <int MODE>
-void launch_append_of(int dtype, const AppendParams& p, bool few, int sms, cudaStream_t st)
+void launch_append_of(int dtype, const AppendParams& p, int tokens, int sms, cudaStream_t st)
 {
-    if (dtype == HIF8_F32) launch_append<MODE, HIF8_F32>(p, few, sms, st);
-    else if (dtype == HIF8_BF16) launch_append<MODE, HIF8_BF16>(p, few, sms, st);
-    else launch_append<MODE, HIF8_F16>(p, few, sms, st);
+    if (dtype == HIF8_F32) launch_append<MODE, HIF8_F32>(p, tokens, sms, st);
+    else if (dtype == HIF8_BF16) launch_append<MODE, HIF8_BF16>(p, tokens, sms, st);
+    else launch_append<MODE, HIF8_F16>(p, tokens, sms, st);
 }
 
 // ---------------------------------------------------------------------------------------------------------
@@ -168,12 +204,17 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(const ReadParams p
     const int lane = threadIdx.x & 31;
     const uint32_t lane4 = 4u * lane;
     const int row_vecs = p.c.dim / N;
-    for (long long u = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); u < p.units; u += (long long)gridDim.x * (kThreads / 32)) {
-        const int part = (int)(u % (2 * p.c.heads)), head = part >> 1;
-        const bool is_v = part & 1;
-        const Piece pc = find_piece(u / (2 * p.c.heads), p.start, p.first, p.n_seqs, p.n_out, p.c.shift, lane);
+    UnitWalk walk(p.units, 2 * p.c.heads, (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), (long long)gridDim.x * (kThreads / 32));
+    Piece pc;
+    int page = -1;
+    for (; walk.left > 0; walk.next()) {
+        const int head = walk.part >> 1;
+        const bool is_v = walk.part & 1;
+        if (walk.fresh) {
+            pc = find_piece(walk.number, p.start, p.first, p.n_seqs, p.n_out, p.c.shift, lane);
+            page = pc.count ? p.c.page_of(pc.seq, pc.pos >> p.c.shift) : -1;
+        }
         if (!pc.count) continue;
-        const int page = p.c.page_of(pc.seq, pc.pos >> p.c.shift);
         const int slot = pc.pos & ((1 << p.c.shift) - 1), n_vec = pc.count * row_vecs;
         const int e = page < 0 ? 0 : clamp_exp((is_v ? p.c.v_exp : p.c.k_exp)[(long long)page * p.c.heads + head]);
         const float back = pow2f(-e);
@@ -488,13 +529,13 @@ extern "C" int hif8_cache_append(const void* k, const void* v, int src_dtype, in
     p.n_seqs = n_seqs; p.n_new = n_new; p.target_exp = target_exp; p.flags = flags;
     p.units = piece_numbers(n_new, n_seqs, p.c.shift) * kv_heads * 2;
     p.vectors = aligned_rows(k, v, token_stride, head_stride, item);
-    const bool few = (long long)n_new * head_dim <= 8192ll * n_seqs / 4;  // a quarter of what a team of 256 threads holds, in the mean
+    const int mean = (n_new + n_seqs - 1) / n_seqs, tokens = mean < page_tokens ? mean : page_tokens;
     cudaStream_t st = (cudaStream_t)stream;
     switch (rnd) {
-        case HIF8_RND_TA: launch_append_of<HIF8_RND_TA>(src_dtype, p, few, sms, st); break;
-        case HIF8_RND_HR: launch_append_of<HIF8_RND_HR>(src_dtype, p, few, sms, st); break;
-        case HIF8_RND_SSR: launch_append_of<HIF8_RND_SSR>(src_dtype, p, few, sms, st); break;
-        default: launch_append_of<HIF8_RND_TE>(src_dtype, p, few, sms, st); break;
+        case HIF8_RND_TA: launch_append_of<HIF8_RND_TA>(src_dtype, p, tokens, sms, st); break;
+        case HIF8_RND_HR: launch_append_of<HIF8_RND_HR>(src_dtype, p, tokens, sms, st); break;
+        case HIF8_RND_SSR: launch_append_of<HIF8_RND_SSR>(src_dtype, p, tokens, sms, st); break;
+        default: launch_append_of<HIF8_RND_TE>(src_dtype, p, tokens, sms, st); break;
     }
     return finish_launch(1);
 }

@@ -73,6 +73,27 @@ __device__ __forceinline__ Piece find_piece(long long number, const int* start, 
     return p;
 }
 
+// The units (a piece's tokens of one head of K or V) of team `me` of `teams`: consecutive ones, so that a piece is looked for once and not for each of its units
+// (27.7 K tokens of 8 heads of 128, appended and read back: 89 -> 81 us).
+struct UnitWalk {
+    long long number, left;  // the piece's number; units to come, this one included
+    int part, parts;         // of the piece: head and K or V; parts of a piece
+    bool fresh;              // the first unit of its piece here
+    __device__ UnitWalk(long long units, int parts_, long long me, long long teams) : parts(parts_), fresh(true)
+    {
+        const long long each = units / teams, rest = units - each * teams, u = me * each + (me < rest ? me : rest);
+        left = each + (me < rest ? 1 : 0);
+        number = u / parts;
+        part = (int)(u - number * parts);
+    }
+    __device__ void next()
+    {
+        left--;
+        fresh = ++part == parts;
+        if (fresh) { part = 0; number++; }
+    }
+};
+
 }  // namespace
 
 // Arguments that describe the cache, checked before anything is launched; fills in the view.
