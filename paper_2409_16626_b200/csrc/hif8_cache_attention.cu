@@ -39,32 +39,40 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v)
 //
 // Chunks of 64 tokens of a (sequence, key head, row tile) are dealt out evenly: group g of four warps takes the chunks [T g / G, T (g + 1) / G) of all
 // T, in order.  A unit whose chunks lie in several groups leaves partial sums in the workspace, which a second kernel adds in a fixed order.
+// WIDE: short units are not cut: all warps of a block are one group, which takes whole units, and there is no second kernel (see whole_units).
 // ---------------------------------------------------------------------------------------------------------
-constexpr int kGroupWarps = 4, kChunk = 16 * kGroupWarps;
 constexpr uint32_t kLutBytes = 65536;  // rows of 256 bytes on a 64 KiB boundary: the address is one byte permute away from the code
 
 // groups of a block: what registers and shared memory leave room for (128 elements, NT = 1: three groups of 168 registers a thread 351 us where four take 341)
 constexpr int groups_of(int dim, int nt) { return dim == 256 ? 2 : dim == 128 && nt == 2 ? 3 : 4; }
 
 // Shared memory: [prefix sums, maxima and denominators, barriers, rings] table [rings].  The table lies on a 64 KiB boundary; a block's memory begins
-// 1 KiB behind one.
-template <int D, int NT>
+// 1 KiB behind one.  The upper halves of the table's rows hold the warps' sums while a segment's are joined, a few query rows at a time: the rings
+// go on with the next segment's tiles meanwhile.
+template <int D, int NT, bool WIDE>
 struct RowsShape {
-    static constexpr int kGroups = groups_of(D, NT), kWarps = kGroups * kGroupWarps, kThreads = kWarps * 32;
+    static constexpr int kWarps = 4 * groups_of(D, NT), kThreads = kWarps * 32, kGroupWarps = WIDE ? kWarps : 4, kGroups = kWarps / kGroupWarps, kChunk = 16 * kGroupWarps;
     static constexpr int kRows = 8 * NT;
     static constexpr int kStages = D == 64 ? 4 : 2;
     static constexpr uint32_t kTile = 16 * D;                            // bytes of 16 tokens of K or V
-    static constexpr uint32_t kRing = kStages * 2 * kTile;               // of a warp; at a segment's end its sums lie there
+    static constexpr uint32_t kRing = kStages * 2 * kTile;               // of a warp
     static constexpr int kBackWarps = 98304 / kRing, kFrontWarps = kWarps > kBackWarps ? kWarps - kBackWarps : 0;  // rings behind / in front of the table
+    static constexpr int kGapRows = 256 / kWarps, kJoinRows = D == 64 ? 8 : 4;  // rows of the table whose upper halves are a warp's; query rows that fit there
     static constexpr int kRecord = kRows * (D + 2);                      // floats of a partial result: sums, maxima, denominators
-    // where a warp's sums fit in one stage of its ring, the next segment's first tiles are on their way in the others while the sums are joined
-    static constexpr int kEarly = kRows * D * 4 <= 2 * (int)kTile ? kStages - 1 : 0;
     // offsets from the block's first byte, which is 1024 modulo 65536
-    static constexpr uint32_t kMl = (HIF8_CACHE_MAX_SEQS + 2) * 8, kScan = kMl + kWarps * kRows * 8, kPlace = kScan + 32 * 8, kBars = kPlace + kWarps * 8, kFlag = kBars + kWarps * kStages * 8;
+    static constexpr uint32_t kMl = (HIF8_CACHE_MAX_SEQS + 2) * 8, kScan = kMl + kWarps * kRows * 8, kBars = kScan + 32 * 8, kFlag = kBars + kWarps * kStages * 8,
+                              kMul = (kFlag + 16 + 15) / 16 * 16, kQuery = (kMul + kGroups * kRows * 4 + 15) / 16 * 16,
+                              kQueryBytes = kRows * D * 2;
     static constexpr uint32_t kFrontRing = kLutBytes - 1024 - kFrontWarps * kRing, kLut = kLutBytes - 1024, kBackRing = kLut + kLutBytes;
     static constexpr uint32_t kSmem = kBackRing + (kWarps < kBackWarps ? kWarps : kBackWarps) * kRing;
-    static_assert(kFlag + 16 <= kFrontRing && kSmem <= 227 * 1024 && kRows * D * 4 <= kRing, "shared memory");
+    static_assert(kQuery + kGroups * kQueryBytes <= kFrontRing && kSmem <= 227 * 1024 && kJoinRows * D * 4 <= kGapRows * 128, "shared memory");
     __device__ static uint32_t ring(uint32_t raw, int w) { return raw + (w < kBackWarps ? kBackRing + w * kRing : kFrontRing + (w - kBackWarps) * kRing); }
+    // offset of float4 number f of query row `row` (of the kJoinRows) in warp w's sums: neither writing them from the products' layout nor reading rows meets in a bank
+    __device__ static uint32_t sum_at(int w, int row, int f)
+    {
+        const int i = row * (D / 4) + (f ^ ((row >> 1) & 3) ^ (((f >> (D == 64 ? 1 : 4)) & 1) << 2));
+        return kLut + (uint32_t)(w * kGapRows + (i >> 3)) * 256 + 128 + (uint32_t)(i & 7) * 16;
+    }
 };
 
 // token (of a tile's 16) in row r of the A operand: with rows 2 t and 2 t + 1 the tokens that thread t of a column of threads reads V of
@@ -81,35 +89,33 @@ template <int D> __device__ __forceinline__ uint32_t chunk_at(int token, int chu
     if (D == 64) return (uint32_t)(token * 64 + ((chunk ^ ((token >> 1) & 3)) << 4));
     return (uint32_t)((chunk >> 3) * 2048 + token * 128 + (((chunk & 7) ^ (token & 7)) << 4));
 }
-// place of float4 number f of row `row` in a warp's sums: neither writing them from the products' layout nor reading rows meets in a bank
-template <int D> __device__ __forceinline__ int sum_at(int row, int f) { return row * (D / 4) + (f ^ ((row >> 1) & 3) ^ (((f >> (D == 64 ? 1 : 4)) & 1) << 2)); }
-
-__device__ __forceinline__ void group_sync(int group) { asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(kGroupWarps * 32) : "memory"); }
+__device__ __forceinline__ void group_sync(int group, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(threads) : "memory"); }
 // ... and whether `any` holds in one of the group's threads
-__device__ __forceinline__ bool group_any(int group, bool any)
+__device__ __forceinline__ bool group_any(int group, int threads, bool any)
 {
     uint32_t r;
     asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %3, 0;\n\tbarrier.cta.red.or.pred q, %1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                 : "=r"(r) : "r"(group + 1), "r"(kGroupWarps * 32), "r"((uint32_t)any) : "memory");
+                 : "=r"(r) : "r"(group + 1), "r"(threads), "r"((uint32_t)any) : "memory");
     return r != 0;
 }
 
 // The work of one sequence in chunks
 struct SeqChunks {
     int lo, per_unit, tiles;  // first token (on a chunk), chunks of a unit, row tiles
-    __device__ SeqChunks(const AttentionParams& p, const SeqView& v, int rows)
+    __device__ SeqChunks(const AttentionParams& p, const SeqView& v, int rows, int chunk)
     {
-        lo = v.n_q ? lo_of(p, v, 0) / kChunk * kChunk : 0;
-        per_unit = max(1, (v.len - lo + kChunk - 1) / kChunk);
+        lo = v.n_q ? lo_of(p, v, 0) / chunk * chunk : 0;
+        per_unit = max(1, (v.len - lo + chunk - 1) / chunk);
         tiles = (int)(((long long)v.n_q * p.group + rows - 1) / rows);
     }
 };
 
-template <int D, int NT, int DT>
-__global__ void __launch_bounds__(RowsShape<D, NT>::kThreads, 1)
+template <int D, int NT, int DT, bool WIDE>
+__global__ void __launch_bounds__(RowsShape<D, NT, WIDE>::kThreads, 1)
 cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const AttentionParams p)
 {
-    using S = RowsShape<D, NT>;
+    using S = RowsShape<D, NT, WIDE>;
+    constexpr int GW = S::kGroupWarps, kChunk = S::kChunk;
     constexpr int J = D / 64;                       // blocks of 64 elements of a key
     constexpr int VB = D / 8;                       // bytes of a value row that a thread takes
     constexpr int MT = D / 16;                      // m16 tiles of the output
@@ -117,7 +123,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
     const uint32_t raw = smem_u32(smem_raw);
     long long* s_prefix = reinterpret_cast<long long*>(smem_raw);
     const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int grp = warp / kGroupWarps, gw = warp % kGroupWarps;
+    const int grp = warp / GW, gw = warp % GW;
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_raw + S::kFlag);
     if ((raw & (kLutBytes - 1)) != 1024) {  // (the same answer in every thread of the grid)
         pdl_wait_prior_grid();
@@ -147,9 +153,9 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
         long long mine = 0;
         for (int s = s0; s < s1; s++) {
             const SeqView v = seq_view(p, s);
-            const SeqChunks k(p, v, S::kRows);
+            const SeqChunks k(p, v, S::kRows, kChunk);
             s_prefix[s] = mine;
-            mine += (long long)k.tiles * p.c.heads * k.per_unit;
+            mine += (long long)k.tiles * p.c.heads * (WIDE ? 1 : k.per_unit);
         }
         long long x = mine;
 #pragma unroll
@@ -174,8 +180,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
     const long long x_end = share_of(chunks, me + 1, groups);
     const uint32_t lut = raw + S::kLut + 4u * lane;
     const uint32_t ring = S::ring(raw, warp);
-    float2* all_ml = reinterpret_cast<float2*>(smem_raw + S::kMl) + grp * kGroupWarps * S::kRows;
-    uint32_t* all_place = reinterpret_cast<uint32_t*>(smem_raw + S::kPlace) + grp * kGroupWarps;  // where the warps' sums lie
+    float2* all_ml = reinterpret_cast<float2*>(smem_raw + S::kMl) + grp * GW * S::kRows;
     const int slot_mask = (1 << p.c.shift) - 1;
     // where this thread reads its bytes of a tile: keys of operand rows g and g + 8, the 16-byte chunks t, t + 4, ..; values of four tokens
     const int tok_k = token_of_row<D>(g), piece = piece_of<D>(g);
@@ -183,29 +188,77 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
     bool ok = true;
     const uint32_t magic = 65536u / (uint32_t)p.group + 1u;  // x / group = x magic >> 16 for the x < group + 16 that come up
 
-    // ---- a segment: chunks c0 .. c1 of a unit
-    int s, head, r0, n_rows, q0, h0, c0, c1, per_unit, hi_min, hi_max, lo_min, lo_max, lo_chunk;
-    SeqView v;
-    // Tiles of this warp: lane n holds pool row and exponents of that of the n-th chunk of a batch of 32; a tile without a page, or with no token
-    // that a row sees, is left out.  Tiles are asked for ahead; `ahead` holds first tokens and exponents of those on their way.
+    // ---- a segment: chunks c0 .. c1 of a unit.  The first one is looked for; the others begin at the next unit, which takes no search and hardly a division.  (Looked
+    // for by every warp, a segment took as many instructions as 18 tiles.)
+    struct Segment {
+        SeqView v;
+        int s, head, r0, n_rows, q0, h0, c0, c1, per_unit, lo_chunk, hi_min, hi_max, lo_min, lo_max;  // q0, h0: query and head of the first row
+    };
+    Segment e0;
+    long long left = x_end - x0;  // chunks (units: WIDE) of this group from the segment's first on
+    auto enter = [&]() {          // e0.s: its tokens
+        e0.v = seq_view(p, e0.s);
+        const SeqChunks k(p, e0.v, S::kRows, kChunk);
+        e0.per_unit = k.per_unit; e0.lo_chunk = k.lo;
+    };
+    auto limits = [&]() {
+        e0.c1 = WIDE ? e0.per_unit : (int)min((long long)e0.per_unit, e0.c0 + left);
+        e0.n_rows = min(S::kRows, e0.v.n_q * p.group - e0.r0);
+        e0.q0 = e0.r0 ? e0.r0 / p.group : 0; e0.h0 = e0.r0 - e0.q0 * p.group;
+        const int qb = e0.q0 + (int)((uint32_t)(e0.h0 + e0.n_rows - 1) * magic >> 16);
+        e0.hi_min = min(e0.v.len, hi_of(p, e0.v, e0.q0)); e0.hi_max = min(e0.v.len, hi_of(p, e0.v, qb)); e0.lo_min = lo_of(p, e0.v, e0.q0); e0.lo_max = lo_of(p, e0.v, qb);
+    };
+    auto locate = [&]() {
+        e0.s = 0;
+        for (int n = p.n_seqs; n > 1;) {  // last sequence that starts at or before x0 (those without chunks share their start with the next)
+            const int half = n >> 1;
+            if (s_prefix[e0.s + half] <= x0) { e0.s += half; n -= half; }
+            else n = half;
+        }
+        enter();
+        const long long in_seq = x0 - s_prefix[e0.s], unit = WIDE ? in_seq : div_small(in_seq, e0.per_unit);
+        const int tiles = (int)(((long long)e0.v.n_q * p.group + S::kRows - 1) / S::kRows);
+        e0.c0 = WIDE ? 0 : (int)(in_seq - unit * e0.per_unit);
+        e0.head = (int)div_small(unit, tiles); e0.r0 = (int)(unit - (long long)e0.head * tiles) * S::kRows;
+        limits();
+    };
+    auto advance = [&]() -> bool {  // to the next segment; false: there is none
+        left -= WIDE ? 1 : e0.c1 - e0.c0;
+        if (left <= 0) return false;
+        e0.r0 += S::kRows;
+        if (e0.r0 >= e0.v.n_q * p.group) {
+            e0.r0 = 0;
+            if (++e0.head == p.c.heads) {
+                e0.head = 0;
+                do { e0.s++; enter(); } while (e0.v.n_q == 0 && e0.s + 1 < p.n_seqs);
+            }
+        }
+        e0.c0 = 0;
+        limits();
+        return true;
+    };
+    auto step_of = [&](int h0, int row) -> int { return (int)((uint32_t)(h0 + row) * magic >> 16); };  // queries from the first row's to row `row`'s
+
+    // ---- the copies: tiles of this warp, kStages ahead of the products.  Lane n holds pool row and exponents of the warp's tile in the n-th chunk of a batch of 32;
+    // a tile without a page, or with no token that a row sees, is left out.  `ahead` holds first tokens and exponents of those on their way.
     int b_row = -1, b_exps = 0, b_first = 0;
     uint32_t b_live = 0;
     int ahead_t0[S::kStages], ahead_exps[S::kStages];
     auto load_batch = [&](int c) {
         b_first = c;
-        const int at = lo_chunk + (c + lane) * kChunk + 16 * gw;  // (below 2^31: a length, at most 2^30, and less than 2^12 more)
-        const int page = c + lane < c1 && at < hi_max && at + 16 > lo_min ? p.c.page_of(s, at >> p.c.shift) : -1;
-        const long long e = (long long)max(page, 0) * p.c.heads + head;
+        const int at = e0.lo_chunk + (c + lane) * kChunk + 16 * gw;  // (below 2^31: a length, at most 2^30, and less than 2^14 more)
+        const int page = c + lane < e0.c1 && at < e0.hi_max && at + 16 > e0.lo_min ? p.c.page_of(e0.s, at >> p.c.shift) : -1;
+        const long long e = (long long)max(page, 0) * p.c.heads + e0.head;
         b_exps = page >= 0 ? (clamp_cache_exp(p.c.k_exp[e]) & 0xFF) | clamp_cache_exp(p.c.v_exp[e]) << 8 : 0;
         b_row = (int)(e << p.c.shift) + (at & slot_mask);  // (rows of a pool number less than 2^31)
         b_live = __ballot_sync(0xFFFFFFFFu, page >= 0);
     };
     auto ask = [&](uint32_t n, int& t0, int& exps) {  // the next tile into the place of use n; t0 = -1: there is none
-        while (!b_live && b_first + 32 < c1) load_batch(b_first + 32);
+        while (!b_live && b_first + 32 < e0.c1) load_batch(b_first + 32);
         t0 = -1;
         if (!b_live || !ok) return;
         const int i = __ffs(b_live) - 1, row = __shfl_sync(0xFFFFFFFFu, b_row, i);
-        t0 = lo_chunk + (b_first + i) * kChunk + 16 * gw;
+        t0 = e0.lo_chunk + (b_first + i) * kChunk + 16 * gw;
         b_live &= b_live - 1;
         const uint32_t st = n % S::kStages, at = ring + st * 2 * S::kTile, bar = bars + 8 * st;
         __syncwarp();  // every lane has read what the stage held
@@ -219,90 +272,79 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
         __syncwarp();
         exps = __shfl_sync(0xFFFFFFFFu, b_exps, i);  // (behind the copies, which need not wait for them)
     };
-    auto open = [&]() {  // the segment at x0, its first tiles
-        s = 0;
-        for (int n = p.n_seqs; n > 1;) {  // last sequence that starts at or before x0 (those without chunks share their start with the next)
-            const int half = n >> 1;
-            if (s_prefix[s + half] <= x0) { s += half; n -= half; }
-            else n = half;
-        }
-        v = seq_view(p, s);
-        const SeqChunks k(p, v, S::kRows);
-        const long long in_seq = x0 - s_prefix[s], unit = div_small(in_seq, k.per_unit);
-        per_unit = k.per_unit; lo_chunk = k.lo;
-        c0 = (int)(in_seq - unit * k.per_unit); c1 = (int)min((long long)k.per_unit, c0 + (x_end - x0));
-        head = (int)div_small(unit, k.tiles); r0 = (int)(unit - (long long)head * k.tiles) * S::kRows;
-        n_rows = (int)min((long long)S::kRows, (long long)v.n_q * p.group - r0);
-        q0 = r0 / p.group; h0 = r0 - q0 * p.group;  // query and head of the tile's first row
-        const int qb = q0 + (int)((uint32_t)(h0 + n_rows - 1) * magic >> 16);
-        hi_min = min(v.len, hi_of(p, v, q0)); hi_max = min(v.len, hi_of(p, v, qb)); lo_min = lo_of(p, v, q0); lo_max = lo_of(p, v, qb);
-        load_batch(c0);
+    // ---- the queries of a segment: the group's warps load (behind the first tiles) and convert a share of the rows each, D / 8 lanes to a row
+    constexpr int kRowLanes = D / 8, kRowsStep = GW * 32 / kRowLanes, kSteps = (S::kRows + kRowsStep - 1) / kRowsStep;
+    unsigned char* queries = smem_raw + S::kQuery + grp * S::kQueryBytes;
+    float* muls = reinterpret_cast<float*>(smem_raw + S::kMul) + grp * S::kRows;
+    uint4 q_raw[kSteps];
+    const int q_row = (gw * 32 + lane) / kRowLanes, q_piece = lane % kRowLanes;  // first row, eight elements of it
+    auto begin = [&]() {
+        load_batch(e0.c0);
 #pragma unroll
-        for (int x = 0; x < S::kEarly; x++) ask(use + x, ahead_t0[x], ahead_exps[x]);
+        for (int x = 0; x < S::kStages; x++) ask(use + x, ahead_t0[x], ahead_exps[x]);
+#pragma unroll
+        for (int i = 0; i < kSteps; i++) {
+            const int row = q_row + i * kRowsStep;
+            q_raw[i] = make_uint4(0, 0, 0, 0);
+            if (row < e0.n_rows) {
+                const int step = step_of(e0.h0, row);
+                const unsigned short* src = reinterpret_cast<const unsigned short*>(p.q) + (long long)(e0.v.first + e0.q0 + step) * p.q_token +
+                                            (long long)(e0.head * p.group + e0.h0 + row - step * p.group) * p.q_head + 8 * q_piece;
+                if (p.vectors) q_raw[i] = __ldg(reinterpret_cast<const uint4*>(src));
+                else q_raw[i] = make_uint4((uint32_t)src[0] | (uint32_t)src[1] << 16, (uint32_t)src[2] | (uint32_t)src[3] << 16, (uint32_t)src[4] | (uint32_t)src[5] << 16, (uint32_t)src[6] | (uint32_t)src[7] << 16);
+            }
+        }
     };
-    open();
+    auto convert_queries = [&]() {
+#pragma unroll
+        for (int i = 0; i < kSteps; i++) {
+            const int row = q_row + i * kRowsStep;
+            int e = 0;
+            if (DT == HIF8_BF16) {  // FP16 queries are multiplied as they are
+                float a = amax_value<DT>(amax_vector<DT>(0u, q_raw[i]));
+#pragma unroll
+                for (int d = 1; d < kRowLanes; d *= 2) a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, d));
+                e = query_exp(a);
+                const float f = pow2f(e);
+                auto both = [&](uint32_t w) { return pack_f16(q_value<DT>(w & 0xFFFFu) * f, q_value<DT>(w >> 16) * f); };
+                q_raw[i] = make_uint4(both(q_raw[i].x), both(q_raw[i].y), both(q_raw[i].z), both(q_raw[i].w));
+            }
+            if (row < S::kRows) {
+                *reinterpret_cast<uint4*>(queries + row * D * 2 + 16 * q_piece) = q_raw[i];
+                if (q_piece == 0) muls[row] = fminf(p.scale_log2 * pow2_clamped(-e), 3.0e23f);  // (times 2^48 within the finite floats)
+            }
+        }
+    };
+    locate();
+    begin();
+    convert_queries();
+    group_sync(grp, GW * 32);
     // (what the joining kernel has to know of the unit that this group's first chunk lies in)
-    if (gw == 0 && lane == 0) {
+    if (!WIDE && gw == 0 && lane == 0) {
         int4* cut = p.cut + 2 * me;
-        cut[0] = make_int4(head, r0, c0, per_unit);
-        cut[1] = make_int4(v.first, n_rows, 0, 0);
+        cut[0] = make_int4(e0.head, e0.r0, e0.c0, e0.per_unit);
+        cut[1] = make_int4(e0.v.first, e0.n_rows, 0, 0);
     }
 
     while (true) {
-#pragma unroll
-        for (int x = S::kEarly; x < S::kStages; x++) ask(use + x, ahead_t0[x], ahead_exps[x]);
-        auto query_of = [&](int row) -> int { return q0 + (int)((uint32_t)(h0 + row) * magic >> 16); };
-        auto head_of = [&](int row) -> int { return head * p.group + h0 + row - (int)((uint32_t)(h0 + row) * magic >> 16) * p.group; };
+        const SeqView v = e0.v;
+        const int n_rows = e0.n_rows, hi_min = e0.hi_min, hi_max = e0.hi_max, lo_min = e0.lo_min, lo_max = e0.lo_max;
+        auto query_of = [&](int row) -> int { return e0.q0 + step_of(e0.h0, row); };
 
         // queries: column g of n8 tile i is row r0 + 8 i + g; a thread takes the elements 64 j + 16 t .. + 15
         uint32_t qb[NT][J][4][2];
         float row_mul[NT][2];
 #pragma unroll
         for (int i = 0; i < NT; i++) {
-            uint32_t w[J][8];
-            if (8 * i + g < n_rows) {
-                const long long at = (long long)(v.first + query_of(8 * i + g)) * p.q_token + (long long)head_of(8 * i + g) * p.q_head + 16 * t;
-                const unsigned short* src = reinterpret_cast<const unsigned short*>(p.q) + at;
 #pragma unroll
-                for (int j = 0; j < J; j++) {
-                    if (p.vectors) {
-                        const uint4 a = __ldg(reinterpret_cast<const uint4*>(src + 64 * j)), b = __ldg(reinterpret_cast<const uint4*>(src + 64 * j) + 1);
-                        w[j][0] = a.x; w[j][1] = a.y; w[j][2] = a.z; w[j][3] = a.w; w[j][4] = b.x; w[j][5] = b.y; w[j][6] = b.z; w[j][7] = b.w;
-                    } else {
-#pragma unroll
-                        for (int x = 0; x < 8; x++) w[j][x] = (uint32_t)src[64 * j + 2 * x] | ((uint32_t)src[64 * j + 2 * x + 1] << 16);
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < J; j++)
-#pragma unroll
-                    for (int x = 0; x < 8; x++) w[j][x] = 0u;
-            }
-            int e = 0;
-            if (DT == HIF8_BF16) {  // FP16 queries are multiplied as they are
-                uint32_t acc = 0;
-#pragma unroll
-                for (int j = 0; j < J; j++)
-#pragma unroll
-                    for (int x = 0; x < 8; x++) acc = amax_word<DT>(acc, w[j][x]);
-                float a = amax_value<DT>(acc);
-                a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
-                a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
-                e = query_exp(a);
-                const float f = pow2f(e);
-#pragma unroll
-                for (int j = 0; j < J; j++)
-#pragma unroll
-                    for (int x = 0; x < 8; x++) w[j][x] = pack_f16(q_value<DT>(w[j][x] & 0xFFFFu) * f, q_value<DT>(w[j][x] >> 16) * f);
+            for (int j = 0; j < J; j++) {
+                const uint4* from = reinterpret_cast<const uint4*>(queries + (8 * i + g) * D * 2 + 128 * j + 32 * t);
+                const uint4 a = from[0], b = from[1];
+                qb[i][j][0][0] = a.x; qb[i][j][0][1] = a.y; qb[i][j][1][0] = a.z; qb[i][j][1][1] = a.w;
+                qb[i][j][2][0] = b.x; qb[i][j][2][1] = b.y; qb[i][j][3][0] = b.z; qb[i][j][3][1] = b.w;
             }
 #pragma unroll
-            for (int j = 0; j < J; j++)
-#pragma unroll
-                for (int st = 0; st < 4; st++) { qb[i][j][st][0] = w[j][2 * st]; qb[i][j][st][1] = w[j][2 * st + 1]; }
-#pragma unroll
-            for (int b = 0; b < 2; b++)  // the scores' columns of this thread: rows 2 t and 2 t + 1 of the tile
-                row_mul[i][b] = fminf(p.scale_log2 * pow2_clamped(-__shfl_sync(0xFFFFFFFFu, e, 4 * (2 * t + b))), 3.0e23f);  // (times 2^48 within the finite floats)
+            for (int b = 0; b < 2; b++) row_mul[i][b] = muls[8 * i + 2 * t + b];  // the scores' columns of this thread: rows 2 t and 2 t + 1 of the tile
         }
 
         // base: the maximum that the weights refer to, 0 before there is one; limit: what an argument may be without a new one; far: a base that an FMA cannot take
@@ -459,25 +501,18 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
             ask(use + S::kStages, ahead_t0[S::kStages - 1], ahead_exps[S::kStages - 1]);
             use++;
         }
-        if (!ok) {  // copies on their way land before the ring is used for anything else
+        if (!ok) {  // copies on their way land before the block's shared memory becomes another's
 #pragma unroll
             for (int x = 0; x < S::kStages; x++)
-                if (ahead_t0[x] >= 0)
-                    wait_landed(bars + 8 * ((use + x) % S::kStages), ((use + x) / S::kStages) & 1u);
+                if (ahead_t0[x] >= 0) wait_landed(bars + 8 * ((use + x) % S::kStages), ((use + x) / S::kStages) & 1u);
             __syncwarp();
         }
 
-        // ---- the four warps' sums of the segment, each in its own ring; the next segment's first tiles are asked for before
-        const int done_rows = n_rows, done_q0 = q0, done_h0 = h0, done_head = head, done_first = v.first;
-        const bool is_whole = c0 == 0 && c1 == per_unit;
-        float* record = p.partial + (size_t)(2 * me + (c0 == 0 ? 1 : 0)) * S::kRecord;
-        x0 += c1 - c0;
-        const bool more = x0 < x_end;
-        const uint32_t place = ring - raw + (S::kEarly ? (use + S::kStages - 1) % S::kStages * 2 * S::kTile : 0u);
-#pragma unroll
-        for (int x = 0; x < S::kStages; x++) ahead_t0[x] = -1;
-        __syncwarp();
-        if (more) open();
+        // ---- the four warps' sums of the segment (all warps': WIDE); the next segment's first tiles and queries are asked for meanwhile
+        const int done_q0 = e0.q0, done_h0 = e0.h0, done_head = e0.head;
+        bool more = false;
+        const bool is_whole = e0.c0 == 0 && e0.c1 == e0.per_unit;
+        float* record = p.partial + (size_t)(2 * me + (e0.c0 == 0 ? 1 : 0)) * S::kRecord;
 #pragma unroll
         for (int i = 0; i < NT; i++)
 #pragma unroll
@@ -485,59 +520,82 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
                 l[i][b] += __shfl_xor_sync(0xFFFFFFFFu, l[i][b], 4);
                 l[i][b] += __shfl_xor_sync(0xFFFFFFFFu, l[i][b], 8);
                 l[i][b] += __shfl_xor_sync(0xFFFFFFFFu, l[i][b], 16);
-                const int row = 8 * i + 2 * t + b;
-                if (g == 0) all_ml[gw * S::kRows + row] = make_float2(m[i][b], l[i][b]);
+                if (g == 0) all_ml[gw * S::kRows + 8 * i + 2 * t + b] = make_float2(m[i][b], l[i][b]);
+            }
 #pragma unroll
-                for (int x = 0; x < MT; x += 2) {
-                    const int d = D == 64 ? 8 * piece + 2 * x : 128 * (x / 8) + 16 * piece + 2 * (x % 8);
-                    reinterpret_cast<float4*>(smem_raw + place)[sum_at<D>(row, d / 4)] = make_float4(o[i][x][b], o[i][x][2 + b], o[i][x + 1][b], o[i][x + 1][2 + b]);
+        for (int x = 0; x < S::kStages; x++) ahead_t0[x] = -1;
+#pragma unroll
+        for (int pass = 0; pass < S::kRows / S::kJoinRows; pass++) {
+            if (pass * S::kJoinRows >= n_rows) break;  // (the same in the whole group)
+            if (pass) group_sync(grp, GW * 32);
+#pragma unroll
+            for (int i = 0; i < NT; i++)
+#pragma unroll
+                for (int b = 0; b < 2; b++) {
+                    const int row = 8 * i + 2 * t + b;
+                    if (row / S::kJoinRows == pass) {
+#pragma unroll
+                        for (int x = 0; x < MT; x += 2) {
+                            const int d = D == 64 ? 8 * piece + 2 * x : 128 * (x / 8) + 16 * piece + 2 * (x % 8);
+                            *reinterpret_cast<float4*>(smem_raw + S::sum_at(warp, row % S::kJoinRows, d / 4)) = make_float4(o[i][x][b], o[i][x][2 + b], o[i][x + 1][b], o[i][x + 1][2 + b]);
+                        }
+                    }
+                }
+            group_sync(grp, GW * 32);
+            if (pass == 0) {
+                more = advance();
+                if (more) begin();
+            }
+            const int rows = min(S::kJoinRows, n_rows - pass * S::kJoinRows);
+            for (int i = gw * 32 + lane; i < rows * (D / 4); i += GW * 32) {
+                const int in_pass = i / (D / 4), row = pass * S::kJoinRows + in_pass, f = i % (D / 4);
+                float2 ml[GW];
+                float top = kNegInf, den = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int w = 0; w < GW; w++) { ml[w] = all_ml[w * S::kRows + row]; top = fmaxf(top, ml[w].x); }
+#pragma unroll
+                for (int w = 0; w < GW; w++) {
+                    const float h = part_factor(ml[w].x, top);
+                    den += ml[w].y * h;
+                    const float4 a = *reinterpret_cast<const float4*>(smem_raw + S::sum_at(grp * GW + w, in_pass, f));
+                    x[0] += a.x * h; x[1] += a.y * h; x[2] += a.z * h; x[3] += a.w * h;
+                }
+                if (is_whole) {
+                    const int step = step_of(done_h0, row), h = done_head * p.group + done_h0 + row - step * p.group;
+                    const long long tok = v.first + done_q0 + step;
+                    const float inv = den == 0.f ? 0.f : 1.f / den;
+#pragma unroll
+                    for (int y = 0; y < 4; y++) x[y] *= inv;
+                    store_out4<DT>(p, tok * p.out_token + (long long)h * p.out_head + 4 * f, x);
+                    if (p.lse && f == 0) p.lse[tok * p.heads + h] = lse_of(top, den, kPShift);
+                } else {
+                    *reinterpret_cast<float4*>(record + row * D + 4 * f) = make_float4(x[0], x[1], x[2], x[3]);
+                    if (f == 0) *reinterpret_cast<float2*>(record + S::kRows * D + 2 * row) = make_float2(top, den);
                 }
             }
-        if (lane == 0) all_place[gw] = place;
-        group_sync(grp);
-        for (int i = gw * 32 + lane; i < done_rows * (D / 4); i += kGroupWarps * 32) {
-            const int row = i / (D / 4), f = i % (D / 4);
-            float2 ml[kGroupWarps];
-            float top = kNegInf, den = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int w = 0; w < kGroupWarps; w++) { ml[w] = all_ml[w * S::kRows + row]; top = fmaxf(top, ml[w].x); }
-#pragma unroll
-            for (int w = 0; w < kGroupWarps; w++) {
-                const float h = part_factor(ml[w].x, top);
-                den += ml[w].y * h;
-                const float4 a = reinterpret_cast<const float4*>(smem_raw + all_place[w])[sum_at<D>(row, f)];
-                x[0] += a.x * h; x[1] += a.y * h; x[2] += a.z * h; x[3] += a.w * h;
-            }
-            if (is_whole) {
-                const int step = (int)((uint32_t)(done_h0 + row) * magic >> 16), h = done_head * p.group + done_h0 + row - step * p.group;
-                const long long tok = done_first + done_q0 + step;
-                const float inv = den == 0.f ? 0.f : 1.f / den;
-#pragma unroll
-                for (int y = 0; y < 4; y++) x[y] *= inv;
-                store_out4<DT>(p, tok * p.out_token + (long long)h * p.out_head + 4 * f, x);
-                if (p.lse && f == 0) p.lse[tok * p.heads + h] = lse_of(top, den, kPShift);
-            } else {
-                *reinterpret_cast<float4*>(record + row * D + 4 * f) = make_float4(x[0], x[1], x[2], x[3]);
-                if (f == 0) *reinterpret_cast<float2*>(record + S::kRows * D + 2 * row) = make_float2(top, den);
-            }
         }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the sums' place is the copies' again
-        if (group_any(grp, !ok) || !more) break;
+        if (more) convert_queries();
+        if (group_any(grp, GW * 32, !ok) || !more) break;
     }
     if (!ok || *abort_flag) {
 #pragma unroll
-        for (int x = 0; x < S::kEarly; x++)
-            if (ahead_t0[x] >= 0)
-                wait_landed(bars + 8 * ((use + x) % S::kStages), ((use + x) / S::kStages) & 1u);
+        for (int x = 0; x < S::kStages; x++)
+            if (ahead_t0[x] >= 0) wait_landed(bars + 8 * ((use + x) % S::kStages), ((use + x) / S::kStages) & 1u);
     }
 }
 
 // Block b - 1 joins the unit that the boundary between groups b - 1 and b cuts, if that is the first one to do so; the parts are added in the groups' order.
-constexpr int kCombineThreads = 256;
+// A unit may lie in all groups: the parts' factors come first, then threads share the parts of a result out among them.
+constexpr int kCombineThreads = 512;
 template <int D, int NT, int DT>
 __global__ void __launch_bounds__(kCombineThreads) cache_attention_combine_kernel(const AttentionParams p, int all_groups)
 {
-    using S = RowsShape<D, NT>;
+    using S = RowsShape<D, NT, false>;
+    constexpr int kMostGroups = kMaxBlocks * S::kGroups, kItems = S::kRows * (D / 4);
+    static_assert(kItems <= kCombineThreads, "a thread for every four results");
+    __shared__ float s_factor[kMostGroups * S::kRows];
+    __shared__ float s_top[S::kRows], s_den[S::kRows];
+    __shared__ float4 s_part[kCombineThreads];
     pdl_wait_prior_grid();
     pdl_launch_dependents();
     const int b = (int)blockIdx.x + 1;
@@ -547,30 +605,48 @@ __global__ void __launch_bounds__(kCombineThreads) cache_attention_combine_kerne
     if (b >= groups) return;
     const long long begin = share_of(chunks, b, groups) - cut.z, end = begin + cut.w;
     if (cut.z == 0 || share_of(chunks, b - 1, groups) > begin) return;
-    int parts = 2;  // groups b - 1 .. b - 2 + parts
-    while (b - 1 + parts < groups && share_of(chunks, b - 1 + parts, groups) < end) parts++;
-    const int head = cut.x, r0 = cut.y, first = of.x, n_rows = of.y;
-    auto record = [&](int i) { return p.partial + (size_t)(2 * (b - 1 + i) + (i == 0 ? 1 : 0)) * S::kRecord; };
-    for (int i = threadIdx.x; i < n_rows * (D / 4); i += kCombineThreads) {
-        const int row = i / (D / 4), d = (i - row * (D / 4)) * 4;
-        float top = kNegInf, den = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 2
-        for (int j = 0; j < parts; j++) {
-            const float* r = record(j);
-            const float2 ml = *reinterpret_cast<const float2*>(r + S::kRows * D + 2 * row);
-            const float4 a = *reinterpret_cast<const float4*>(r + row * D + d);
-            const float n = fmaxf(top, ml.x), f = part_factor(top, n), h = part_factor(ml.x, n);
-            den = den * f + ml.y * h;
-            o[0] = o[0] * f + a.x * h; o[1] = o[1] * f + a.y * h; o[2] = o[2] * f + a.z * h; o[3] = o[3] * f + a.w * h;
-            top = n;
-        }
-        const int r = r0 + row, qi = r / p.group, h = head * p.group + r - qi * p.group;
-        const float inv = den == 0.f ? 0.f : 1.f / den;
+    const int parts = owner_of(chunks, end - 1, groups) - (b - 1) + 1;  // groups b - 1 .. b - 2 + parts
+    const int head = cut.x, r0 = cut.y, first = of.x, n_rows = of.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    auto record = [&](int i) -> const float* { return p.partial + (size_t)(2 * (b - 1 + i) + (i == 0 ? 1 : 0)) * S::kRecord; };
+    for (int row = warp; row < n_rows; row += kCombineThreads / 32) {
+        float top = kNegInf, den = 0.f;
+        for (int j = lane; j < parts; j += 32) top = fmaxf(top, record(j)[S::kRows * D + 2 * row]);
 #pragma unroll
-        for (int y = 0; y < 4; y++) o[y] *= inv;
-        store_out4<DT>(p, (long long)(first + qi) * p.out_token + (long long)h * p.out_head + d, o);
-        if (p.lse && d == 0) p.lse[(long long)(first + qi) * p.heads + h] = lse_of(top, den, kPShift);
+        for (int d = 1; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+        for (int j = lane; j < parts; j += 32) {
+            const float2 ml = *reinterpret_cast<const float2*>(record(j) + S::kRows * D + 2 * row);
+            const float h = part_factor(ml.x, top);
+            s_factor[j * S::kRows + row] = h;
+            den += ml.y * h;
+        }
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) den += __shfl_xor_sync(0xFFFFFFFFu, den, d);
+        if (lane == 0) { s_top[row] = top; s_den[row] = den; }
     }
+    __syncthreads();
+    const int items = n_rows * (D / 4), shares = kCombineThreads / items, item = (int)threadIdx.x % items, share = (int)threadIdx.x / items;
+    const int row = item / (D / 4), f = item % (D / 4);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (share < shares) {
+#pragma unroll 4
+        for (int j = share; j < parts; j += shares) {
+            const float4 a = *reinterpret_cast<const float4*>(record(j) + row * D + 4 * f);
+            const float h = s_factor[j * S::kRows + row];
+            o.x += a.x * h; o.y += a.y * h; o.z += a.z * h; o.w += a.w * h;
+        }
+        s_part[threadIdx.x] = o;
+    }
+    __syncthreads();
+    if (share != 0) return;
+    for (int j = 1; j < shares; j++) {
+        const float4 a = s_part[j * items + item];
+        o.x += a.x; o.y += a.y; o.z += a.z; o.w += a.w;
+    }
+    const int r = r0 + row, qi = r / p.group, h = head * p.group + r - qi * p.group;
+    const float den = s_den[row], inv = den == 0.f ? 0.f : 1.f / den;
+    const float x[4] = {o.x * inv, o.y * inv, o.z * inv, o.w * inv};
+    store_out4<DT>(p, (long long)(first + qi) * p.out_token + (long long)h * p.out_head + 4 * f, x);
+    if (p.lse && f == 0) p.lse[(long long)(first + qi) * p.heads + h] = lse_of(s_top[row], den, kPShift);
 }
 
 // Inf and NaN among the values of tokens that only some of a sequence's queries see: the rows that do see them get them here.  (Those that all queries
@@ -653,7 +729,8 @@ PerDevice<DeviceSetup> g_setup;
 template <int D, int NT, int DT>
 cudaError_t allow_shared()
 {
-    return cudaFuncSetAttribute((const void*)cache_attention_rows_kernel<D, NT, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)RowsShape<D, NT>::kSmem);
+    const cudaError_t e = cudaFuncSetAttribute((const void*)cache_attention_rows_kernel<D, NT, DT, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)RowsShape<D, NT, false>::kSmem);
+    return e != cudaSuccess ? e : cudaFuncSetAttribute((const void*)cache_attention_rows_kernel<D, NT, DT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)RowsShape<D, NT, true>::kSmem);
 }
 template <int DT>
 cudaError_t allow_shared_of()
@@ -664,13 +741,22 @@ cudaError_t allow_shared_of()
     return cudaSuccess;
 }
 
-template <int D, int NT, int DT>
-cudaError_t launch_rows(const AttentionParams& p, int sms, cudaStream_t st)
+// Whether units are taken whole by all warps of a block, without a second kernel: where every unit has a block of its own and a warp two tiles of 16 tokens at most.
+// us a call in a graph, 8 key heads of 128, BF16, cut / whole: 1 sequence of 100 tokens 9.1 / 6.6, 16 of up to 500 16.3 / 10.6; three tiles a warp: 1 of 517 10.6 / 11.0, two
+// rounds of blocks: 64 of up to 300 20.3 / 28.9.  (Units and lengths are the host's upper bounds.)
+bool whole_units(const AttentionParams& p, int max_q, int max_length, int rows, int warps, int blocks)
 {
-    using S = RowsShape<D, NT>;
+    const long long units = (max_q <= 1 ? (long long)p.n_seqs : (long long)p.n_q * p.group / rows + p.n_seqs) * p.c.heads;
+    const long long tokens = p.window && p.window + (long long)max_q < max_length ? p.window + (long long)max_q : max_length;
+    return units <= blocks && tokens <= 32 * warps;
+}
+
+template <int D, int NT, int DT, bool WIDE>
+cudaError_t launch_rows_form(const AttentionParams& p, int blocks, cudaStream_t st)
+{
+    using S = RowsShape<D, NT, WIDE>;
     cudaLaunchConfig_t cfg{};
-    const int ctas = sms < kMaxBlocks ? sms : kMaxBlocks;
-    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.gridDim = dim3((unsigned)blocks);
     cfg.blockDim = dim3(S::kThreads);
     cfg.dynamicSmemBytes = S::kSmem;
     cfg.stream = st;
@@ -681,19 +767,25 @@ cudaError_t launch_rows(const AttentionParams& p, int sms, cudaStream_t st)
     cfg.numAttrs = 1;
     CUtensorMap map_k, map_v;
     if (!pool_map(&map_k, p.c.k, p.c) || !pool_map(&map_v, p.c.v, p.c)) return cudaErrorInvalidValue;
-    cudaError_t rc = cudaLaunchKernelEx(&cfg, cache_attention_rows_kernel<D, NT, DT>, map_k, map_v, p);
-    if (rc != cudaSuccess) return rc;
-    const int groups = ctas * S::kGroups;
-    rc = launch_pdl_threads(kCombineThreads, cache_attention_combine_kernel<D, NT, DT>, dim3((unsigned)(groups - 1)), st, p, groups);
-    g_launches.fetch_add(2, std::memory_order_relaxed);
-    return rc;
+    g_launches.fetch_add(WIDE ? 1 : 2, std::memory_order_relaxed);
+    const cudaError_t rc = cudaLaunchKernelEx(&cfg, cache_attention_rows_kernel<D, NT, DT, WIDE>, map_k, map_v, p);
+    if (WIDE || rc != cudaSuccess) return rc;
+    const int groups = blocks * S::kGroups;
+    return launch_pdl_threads(kCombineThreads, cache_attention_combine_kernel<D, NT, DT>, dim3((unsigned)(groups - 1)), st, p, groups);
+}
+template <int D, int NT, int DT>
+cudaError_t launch_rows(const AttentionParams& p, int max_q, int max_length, int sms, cudaStream_t st)
+{
+    const int blocks = sms < kMaxBlocks ? sms : kMaxBlocks;
+    if (whole_units(p, max_q, max_length, 8 * NT, RowsShape<D, NT, true>::kWarps, blocks)) return launch_rows_form<D, NT, DT, true>(p, blocks, st);
+    return launch_rows_form<D, NT, DT, false>(p, blocks, st);
 }
 template <int DT>
-cudaError_t launch_rows_of(const AttentionParams& p, int nt, int sms, cudaStream_t st)
+cudaError_t launch_rows_of(const AttentionParams& p, int nt, int max_q, int max_length, int sms, cudaStream_t st)
 {
-    if (p.c.dim == 64) return nt == 2 ? launch_rows<64, 2, DT>(p, sms, st) : launch_rows<64, 1, DT>(p, sms, st);
-    if (p.c.dim == 128) return nt == 2 ? launch_rows<128, 2, DT>(p, sms, st) : launch_rows<128, 1, DT>(p, sms, st);
-    return launch_rows<256, 1, DT>(p, sms, st);
+    if (p.c.dim == 64) return nt == 2 ? launch_rows<64, 2, DT>(p, max_q, max_length, sms, st) : launch_rows<64, 1, DT>(p, max_q, max_length, sms, st);
+    if (p.c.dim == 128) return nt == 2 ? launch_rows<128, 2, DT>(p, max_q, max_length, sms, st) : launch_rows<128, 1, DT>(p, max_q, max_length, sms, st);
+    return launch_rows<256, 1, DT>(p, max_q, max_length, sms, st);
 }
 
 }  // namespace
@@ -762,7 +854,7 @@ extern "C" int hif8_cache_attention(const void* q, int dtype, int64_t q_token_st
     if (tiles && workspace_bytes >= kHeadBytes + tiles) {
         p.special_flag = p.status + 1;
         rc = launch_prefill(p, dtype, max_length, ws + kHeadBytes, sms, st);
-    } else rc = dtype == HIF8_BF16 ? launch_rows_of<HIF8_BF16>(p, nt, sms, st) : launch_rows_of<HIF8_F16>(p, nt, sms, st);
+    } else rc = dtype == HIF8_BF16 ? launch_rows_of<HIF8_BF16>(p, nt, max_q, max_length, sms, st) : launch_rows_of<HIF8_F16>(p, nt, max_q, max_length, sms, st);
     if (rc == cudaSuccess && max_q > 1 && (p.causal || p.window)) {
         const dim3 grid((unsigned)(head_dim / 16), (unsigned)kv_heads, (unsigned)n_seqs);
         rc = dtype == HIF8_BF16 ? launch_pdl(cache_attention_specials_kernel<HIF8_BF16>, grid, st, p) : launch_pdl(cache_attention_specials_kernel<HIF8_F16>, grid, st, p);

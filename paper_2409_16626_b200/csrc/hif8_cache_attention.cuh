@@ -186,6 +186,8 @@ __device__ __forceinline__ int lo_of(const AttentionParams& p, const SeqView& v,
 __device__ __forceinline__ long long div_small(long long a, int b) { return a >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b); }
 // first chunk of group g
 __host__ __device__ __forceinline__ long long share_of(long long chunks, int g, int groups) { return chunks * g / groups; }
+// ... and the group that chunk x belongs to
+__device__ __forceinline__ int owner_of(long long chunks, long long x, int groups) { return (int)(((x + 1) * groups - 1) / chunks); }
 
 template <int DT> __device__ __forceinline__ float q_value(uint32_t half_word) { return DT == HIF8_BF16 ? __uint_as_float(half_word << 16) : __half2float(__ushort_as_half((unsigned short)half_word)); }
 

@@ -746,20 +746,21 @@ __global__ void __launch_bounds__(kThreads) cache_attention_join_kernel(const Pr
     const PairView u = pair_view(p, cut.y, cut.x);
     const int head = cut.z;
     const long long end = begin + u.tiles;
-    int parts = 2;
-    while (b - 1 + parts < blocks && share_of(all, b - 1 + parts, blocks) < end) parts++;
+    const int parts = owner_of(all, end - 1, blocks) - (b - 1) + 1;
     for (int i = threadIdx.x; i < kJoinRows * (D / 4); i += kThreads) {
         const int row = (int)blockIdx.y * kJoinRows + i / (D / 4), d = i % (D / 4) * 4;
         if (row >= u.n_rows) continue;
+        auto record = [&](int j) -> const float* { return p.a.partial + (size_t)(2 * (b - 1 + j) + (j == 0 ? 1 : 0)) * Record<D>::floats; };
         float top = kNegInf, den = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int j = 0; j < parts; j++) top = fmaxf(top, record(j)[(size_t)kRecordRows * D + 2 * row]);
+#pragma unroll 4
         for (int j = 0; j < parts; j++) {
-            const float* rec = p.a.partial + (size_t)(2 * (b - 1 + j) + (j == 0 ? 1 : 0)) * Record<D>::floats;
-            const float2 ml = *reinterpret_cast<const float2*>(rec + (size_t)kRecordRows * D + 2 * row);
-            const float4 a = *reinterpret_cast<const float4*>(rec + (size_t)row * D + d);
-            const float n = fmaxf(top, ml.x), f = part_factor(top, n), h = part_factor(ml.x, n);
-            den = den * f + ml.y * h;
-            o[0] = o[0] * f + a.x * h; o[1] = o[1] * f + a.y * h; o[2] = o[2] * f + a.z * h; o[3] = o[3] * f + a.w * h;
-            top = n;
+            const float2 ml = *reinterpret_cast<const float2*>(record(j) + (size_t)kRecordRows * D + 2 * row);
+            const float4 a = *reinterpret_cast<const float4*>(record(j) + (size_t)row * D + d);
+            const float h = part_factor(ml.x, top);
+            den += ml.y * h;
+            o[0] += a.x * h; o[1] += a.y * h; o[2] += a.z * h; o[3] += a.w * h;
         }
         const int r = u.r0 + row, qi = r / p.a.group, h = head * p.a.group + r - qi * p.a.group;
         const float inv = den == 0.f ? 0.f : 1.f / den;
