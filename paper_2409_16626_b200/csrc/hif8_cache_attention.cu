@@ -194,7 +194,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
         SeqView v;
         int s, head, r0, n_rows, q0, h0, c0, c1, per_unit, lo_chunk, hi_min, hi_max, lo_min, lo_max;  // q0, h0: query and head of the first row
     };
-    Segment e0;
+    Segment e0{};
     long long left = x_end - x0;  // chunks (units: WIDE) of this group from the segment's first on
     auto enter = [&]() {          // e0.s: its tokens
         e0.v = seq_view(p, e0.s);

@@ -14,14 +14,18 @@
 namespace hif8 {
 namespace {
 
-constexpr int kTileRows = 128, kPairRows = 256, kTileTokens = 128;
+constexpr int kTileRows = 128, kTileTokens = 128;
 constexpr float kShift = 4.f, kLazy = 8.f;
-constexpr int kStages = 4;
+// Row tiles of a block: two, except for heads of 256, whose sums take half of tensor memory: there the two places of scores belong to consecutive tiles of tokens.
+template <int D> struct TileShape {
+    static constexpr int kTiles = D == 256 ? 1 : 2, kUnitRows = kTiles * kTileRows;
+    static constexpr int kStages = D == 256 ? 2 : 4;  // (heads of 256: one for keys, one for values)
+};
 constexpr int kTmaWarp = 8, kMmaWarp = 9, kPlanWarp = 10, kThreadsA = 12 * 32;
 // Registers: 168 a thread at launch, 64512 in all; the eight warps that hold rows of scores take 208, the third group of four warps (one of them idle) 88.
 constexpr int kRegsRows = 208, kRegsOther = 88;
 static_assert(256 * kRegsRows + 128 * kRegsOther <= kThreadsA * 168, "no more than the block has");
-constexpr int kMetaRing = 8, kSegRing = 4, kSegReaders = 10;  // (the copying warp, the products' and eight of rows)
+constexpr int kMetaRing = 8, kSegRing = 4;
 
 struct PrefillParams {
     AttentionParams a;
@@ -37,10 +41,11 @@ struct PrefillParams {
     int* specials;         // set when some token that only some queries see holds Inf or NaN in V
     int cap_blocks, pairs;
     long long rows;        // n_q * group
+    int unit_rows;         // query rows of a unit
 };
 
 // pairs of row tiles of the sequence, and their numbers: from first_pair on (see Piece: no sums over the batch)
-__device__ __forceinline__ long long first_pair(const PrefillParams& p, int s) { return ((long long)start_at(p.a.q_start, s, p.a.n_q) * p.a.group) / kPairRows + s; }
+__device__ __forceinline__ long long first_pair(const PrefillParams& p, int s) { return ((long long)start_at(p.a.q_start, s, p.a.n_q) * p.a.group) / p.unit_rows + s; }
 
 struct PairView {
     int seq, r0, n_rows, base, j0, tiles;  // rows r0 .. of the sequence; first token of its blocks in the workspace; first tile, tiles
@@ -54,8 +59,8 @@ __device__ __forceinline__ PairView pair_view(const PrefillParams& p, int seq, l
     u.v = seq_view(p.a, seq);
     const long long i = number - first_pair(p, seq), rows = (long long)u.v.n_q * p.a.group;
     u.base = lo_of(p.a, u.v, 0) / kTileTokens * kTileTokens;
-    u.r0 = (int)(i * kPairRows);
-    u.n_rows = i < 0 || i * kPairRows >= rows ? 0 : (int)min((long long)kPairRows, rows - i * kPairRows);
+    u.r0 = (int)(i * p.unit_rows);
+    u.n_rows = i < 0 || i * p.unit_rows >= rows ? 0 : (int)min((long long)p.unit_rows, rows - i * p.unit_rows);
     if (!u.n_rows) { u.r0 = u.j0 = u.tiles = u.lo_min = u.lo_max = u.hi_min = u.hi_max = 0; return u; }
     const int qa = u.r0 / p.a.group, qb = (u.r0 + u.n_rows - 1) / p.a.group;
     u.lo_min = lo_of(p.a, u.v, qa); u.lo_max = lo_of(p.a, u.v, qb);
@@ -297,20 +302,23 @@ static_assert(sizeof(SegmentInfo) == 64, "read in 16-byte pieces");
 
 template <int D>
 struct PrefillSmem {
+    static constexpr int kStages = TileShape<D>::kStages, kTiles = TileShape<D>::kTiles;
     static constexpr int kQBufs = D == 64 ? 2 : 1;  // (short units, as windows and short prompts have them, wait for their queries otherwise: see the kernel's figures)
     static constexpr uint32_t kQ = kTileRows * D * 2, kStage = kTileTokens * D * 2;
-    static constexpr uint32_t q = 0, stages = kQBufs * 2 * kQ, meta = stages + kStages * kStage, seg = meta + kMetaRing * 128, bars = seg + kSegRing * 64;
-    // barriers: queries there / free, stages full / empty, factors of a tile there, segment told / read, scores there [2], weights there (half of them, all) [2], sums complete, sums
-    // read, all products ended (after a wait that gave up)
+    static constexpr uint32_t q = 0, stages = kQBufs * kTiles * kQ, meta = stages + kStages * kStage, seg = meta + kMetaRing * 128, bars = seg + kSegRing * 64;
+    // barriers: queries there / free, stages full / empty, factors of a tile there, segment told / read, scores there [2], weights there (half of them, all) [2], sums complete, a tile's products with
+    // values done (one row tile), sums read, all products ended (after a wait that gave up)
     static constexpr uint32_t q_full = bars, q_empty = q_full + 8 * kQBufs, full = q_empty + 8 * kQBufs, empty = full + 8 * kStages, meta_full = empty + 8 * kStages,
                               seg_full = meta_full + 8 * kMetaRing, seg_empty = seg_full + 8 * kSegRing, s_full = seg_empty + 8 * kSegRing, p_half = s_full + 16, p_full = p_half + 16,
-                              o_full = p_full + 16, o_empty = o_full + 8, drain = o_empty + 8, tmem_slot = drain + 8, abort_flag = tmem_slot + 4, total = abort_flag + 4;
+                              o_full = p_full + 16, pv_done = o_full + 8, o_empty = pv_done + 8, drain = o_empty + 8, tmem_slot = drain + 8, abort_flag = tmem_slot + 4, total = abort_flag + 4;
     static constexpr uint32_t kBytes = total + 1024;
     static_assert(kBytes <= 227 * 1024, "shared memory");
 };
 
-constexpr int kRecordRows = kPairRows;
-template <int D> struct Record { static constexpr size_t floats = (size_t)kRecordRows * (D + 2); };
+template <int D> struct Record {
+    static constexpr int kRows = TileShape<D>::kUnitRows;
+    static constexpr size_t floats = (size_t)kRows * (D + 2);
+};
 
 // a segment: tiles c0 .. c1 of a unit
 struct Segment {
@@ -377,6 +385,7 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                                                                              const __grid_constant__ CUtensorMap map_v, const PrefillParams p)
 {
     using L = PrefillSmem<D>;
+    constexpr int kTiles = L::kTiles, kStages = L::kStages;
     extern __shared__ unsigned char smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     unsigned char* sm = smem_raw + (base - smem_u32(smem_raw));
@@ -388,9 +397,9 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
         for (int i = 0; i < L::kQBufs; i++) { mbar_init(bar(L::q_full, i), 1); mbar_init(bar(L::q_empty, i), 1); }
         for (int i = 0; i < kStages; i++) { mbar_init(bar(L::full, i), 1); mbar_init(bar(L::empty, i), 1); }
         for (int i = 0; i < kMetaRing; i++) mbar_init(bar(L::meta_full, i), 1);
-        for (int i = 0; i < kSegRing; i++) { mbar_init(bar(L::seg_full, i), 1); mbar_init(bar(L::seg_empty, i), kSegReaders); }
+        for (int i = 0; i < kSegRing; i++) { mbar_init(bar(L::seg_full, i), 1); mbar_init(bar(L::seg_empty, i), 2 + 4 * kTiles); }  // (read by the copying warp, the products' and the rows')
         for (int i = 0; i < 2; i++) { mbar_init(bar(L::s_full, i), 1); mbar_init(bar(L::p_half, i), 4); mbar_init(bar(L::p_full, i), 4); }
-        mbar_init(bar(L::o_full), 1); mbar_init(bar(L::o_empty), 8); mbar_init(bar(L::drain), 1);
+        mbar_init(bar(L::o_full), 1); mbar_init(bar(L::pv_done), 1); mbar_init(bar(L::o_empty), 4 * kTiles); mbar_init(bar(L::drain), 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -405,7 +414,7 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
     pdl_wait_prior_grid();
     pdl_launch_dependents();
 
-    // tensor memory: scores (and weights over them) of the two tiles at columns 0 and 128, sums at 256 and 384
+    // tensor memory: scores (and weights over them) of the two tiles at columns 0 and 128, sums at 256 and 384 (one row tile: scores of tiles of tokens in turn, sums from 256 on)
     const int me = blockIdx.x;
     bool ok = true;
     uint32_t seg = 0;  // segments so far
@@ -451,7 +460,7 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
             __syncwarp();
         }
     } else if (warp == kTmaWarp) {
-        uint32_t n = 0, tile = 0;  // copies into the ring; tiles so far
+        uint32_t n[2] = {0, 0}, tile = 0;  // copies of keys, of values; tiles so far
         SegmentInfo g;
         while (next_segment(g, 85)) {
             const bool two = g.n_rows > kTileRows;
@@ -463,37 +472,54 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                 for (int i = 0; i < (two ? 2 : 1); i++)
 #pragma unroll
                     for (int c = 0; c < D / 64; c++)
-                        tma_load_2d(base + L::q + (2 * qb + i) * L::kQ + c * (kTileRows * 128), &map_q, c * 64, g.q_row + i * kTileRows, bar(L::q_full, qb));
+                        tma_load_2d(base + L::q + (kTiles * qb + i) * L::kQ + c * (kTileRows * 128), &map_q, c * 64, g.q_row + i * kTileRows, bar(L::q_full, qb));
             }
             __syncwarp();
             seg++;
-            for (int j = 0; j < g.tiles && ok; j++, tile++) {
+            auto copy = [&](int kv, int j, uint32_t st, uint32_t round) {  // keys or values of tile j into stage st, its round-th use
                 const int blk = min(g.block0 + j, p.cap_blocks - 1);  // (beyond: lengths above max_length)
                 const int row = (int)(((long long)g.head * p.cap_blocks + blk) * kTileTokens);
-                for (int kv = 0; kv < 2; kv++, n++) {
-                    const uint32_t st = n % kStages;
-                    if (n >= kStages) ok = warp_all(mbar_wait(bar(L::empty, st), (n / kStages - 1) & 1u, abort_flag, p.a.status, 72));
-                    if (!ok) break;
-                    if (elect_one()) {
-                        const uint32_t to = base + L::stages + st * L::kStage;
-                        mbar_expect(bar(L::full, st), L::kStage);
+                if (round) ok = warp_all(mbar_wait(bar(L::empty, st), (round - 1) & 1u, abort_flag, p.a.status, 72));
+                if (!ok) return;
+                if (elect_one()) {
+                    const uint32_t to = base + L::stages + st * L::kStage;
+                    mbar_expect(bar(L::full, st), L::kStage);
 #pragma unroll
-                        for (int c = 0; c < D / 64; c++) tma_load_2d(to + c * (kTileTokens * 128), kv ? &map_v : &map_k, c * 64, row, bar(L::full, st));
-                        if (!kv) {  // (eight tiles are kept: keys of tile x are only asked for when the scores of tile x - 2 are there, so the rows are at x - 3 at least)
-                            mbar_expect(bar(L::meta_full, tile % kMetaRing), 128);
-                            bulk_load(base + L::meta + (tile % kMetaRing) * 128, p.meta + (row >> 4), 128, bar(L::meta_full, tile % kMetaRing));
-                        }
+                    for (int c = 0; c < D / 64; c++) tma_load_2d(to + c * (kTileTokens * 128), kv ? &map_v : &map_k, c * 64, row, bar(L::full, st));
+                    if (!kv) {  // (eight tiles are kept: keys of tile x are only asked for when the scores of tile x - 2 are there, so the rows are at x - 3 at least)
+                        mbar_expect(bar(L::meta_full, (tile + j) % kMetaRing), 128);
+                        bulk_load(base + L::meta + (tile + j) % kMetaRing * 128, p.meta + (row >> 4), 128, bar(L::meta_full, (tile + j) % kMetaRing));
                     }
-                    __syncwarp();
                 }
-            }
+                __syncwarp();
+                n[kv]++;
+            };
+            // in the order in which the products free the stages: keys and values in turn; with one row tile the scores, and so the keys, are a tile ahead
+            if (kTiles == 2)
+                for (int j = 0; j < g.tiles && ok; j++)
+                    for (int kv = 0; kv < 2 && ok; kv++) copy(kv, j, (n[0] + n[1]) % kStages, (n[0] + n[1]) / kStages);
+            else
+                for (int j = -2; j < g.tiles && ok; j++) {  // K0 | V0 K1 | K2 V1 | K3 V2 ..: (j = -1: V0 needs no wait that K1 does)
+                    if (j == -2) copy(0, 0, 0, n[0]);
+                    else if (j == -1) {
+                        copy(1, 0, 1, n[1]);
+                        if (ok && g.tiles > 1) copy(0, 1, 0, n[0]);
+                    } else {
+                        if (j + 2 < g.tiles) copy(0, j + 2, 0, n[0]);
+                        if (ok && j + 1 < g.tiles) copy(1, j + 1, 1, n[1]);
+                    }
+                }
+            if (ok) tile += g.tiles;
             if (!ok) break;
         }
         if (!ok || warp_any(*abort_flag)) {  // copies on their way land before the block's shared memory becomes another's
             for (uint32_t i = seg > L::kQBufs ? seg - L::kQBufs : 0; i < seg; i++) wait_landed(bar(L::q_full, i % L::kQBufs), (i / L::kQBufs) & 1u);
-            for (uint32_t i = n > kStages ? n - kStages : 0; i < n; i++) wait_landed(bar(L::full, i % kStages), (i / kStages) & 1u);
-            const uint32_t asked = (n + 1) / 2;  // tiles whose keys, and with them factors, were asked for
-            for (uint32_t i = asked > kMetaRing ? asked - kMetaRing : 0; i < asked; i++) wait_landed(bar(L::meta_full, i % kMetaRing), (i / kMetaRing) & 1u);
+            if (kTiles == 2)
+                for (uint32_t all = n[0] + n[1], i = all > kStages ? all - kStages : 0; i < all; i++) wait_landed(bar(L::full, i % kStages), (i / kStages) & 1u);
+            else
+                for (int kv = 0; kv < 2; kv++)
+                    if (n[kv]) wait_landed(bar(L::full, kv), (n[kv] - 1) & 1u);
+            for (uint32_t i = n[0] > kMetaRing ? n[0] - kMetaRing : 0; i < n[0]; i++) wait_landed(bar(L::meta_full, i % kMetaRing), (i / kMetaRing) & 1u);
         }
     } else if (warp == kMmaWarp) {
         const uint32_t id_s = (1u << 4) | ((uint32_t)(kTileTokens >> 3) << 17) | ((uint32_t)(kTileRows >> 4) << 24);     // FP16 x FP16 -> FP32, both K-major
@@ -505,24 +531,69 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
             const uint32_t qb = seg % L::kQBufs;
             ok = warp_all(mbar_wait(bar(L::q_full, qb), (seg / L::kQBufs) & 1u, abort_flag, p.a.status, 73));
             if (!ok) break;
-            auto scores = [&](int i, uint32_t st) {
+            auto scores = [&](int i, uint32_t st, int place) {
                 if (elect_one()) {
-                    const uint64_t da = make_smem_desc(base + L::q + (2 * qb + i) * L::kQ, 16, 1024), db = make_smem_desc(base + L::stages + st * L::kStage, 16, 1024);
+                    const uint64_t da = make_smem_desc(base + L::q + (kTiles * qb + i) * L::kQ, 16, 1024), db = make_smem_desc(base + L::stages + st * L::kStage, 16, 1024);
 #pragma unroll
                     for (int kk = 0; kk < D / 16; kk++) {
                         const uint64_t off = (uint64_t)((kk / 4) * (kTileRows * 128 / 16) + (kk % 4) * 2);
-                        tc_mma_f16(tmem + i * 128, da + off, db + off, id_s, kk > 0);
+                        tc_mma_f16(tmem + place * 128, da + off, db + off, id_s, kk > 0);
                     }
-                    tc_commit(bar(L::s_full, i));
+                    tc_commit(bar(L::s_full, place));
                 }
                 __syncwarp();
             };
+            auto values = [&](int place, int i, uint32_t st, uint32_t parity, bool add) {  // as the weights come: those of the first 64 tokens, and the others
+                const uint64_t dv = make_smem_desc(base + L::stages + st * L::kStage, kTileTokens * 128, 1024);
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    ok = warp_all(mbar_wait(bar(h ? L::p_full : L::p_half, place), parity, abort_flag, p.a.status, 78));
+                    if (!ok) return;
+                    tc_fence_after();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int kk = 4 * h; kk < 4 * h + 4; kk++)
+                            tc_mma_f16_a_tmem(tmem + 256 + i * 128, tmem + place * 128 + kk * 8, dv + (uint64_t)(kk * 128), id_o, add || kk > 0);
+                    }
+                    __syncwarp();
+                }
+            };
+            if constexpr (kTiles == 1) {
+                // scores are a tile ahead of the weights: S0 S1 | P0 V0 S2 | P1 V1 S3 ..
+                auto next_scores = [&]() {
+                    ok = warp_all(mbar_wait(bar(L::full, 0), n & 1u, abort_flag, p.a.status, 74));
+                    if (!ok) return;
+                    tc_fence_after();
+                    scores(0, 0, (int)(n & 1u));
+                    if (elect_one()) tc_commit(bar(L::empty, 0));
+                    __syncwarp();
+                    n++;
+                };
+                next_scores();
+                if (ok && seg) ok = warp_all(mbar_wait(bar(L::o_empty), (seg - 1) & 1u, abort_flag, p.a.status, 75));  // the segment in front of this one has read its sums
+                for (int j = 0; j < tiles && ok; j++) {
+                    if (j + 1 < tiles) next_scores();
+                    if (ok) ok = warp_all(mbar_wait(bar(L::full, 1), uses[0] & 1u, abort_flag, p.a.status, 76));
+                    if (ok) values((int)(uses[0] & 1u), 0, 1, (uses[0] >> 1) & 1u, j > 0);
+                    if (!ok) break;
+                    uses[0]++;
+                    if (elect_one()) {
+                        tc_commit(bar(L::empty, 1));
+                        tc_commit(bar(L::pv_done));
+                        if (j + 1 == tiles) { tc_commit(bar(L::o_full)); tc_commit(bar(L::q_empty, qb)); }
+                    }
+                    __syncwarp();
+                }
+                if (!ok) break;
+                seg++;
+                continue;
+            }
             // keys of the first tile
             uint32_t st = n % kStages;
             ok = warp_all(mbar_wait(bar(L::full, st), (n / kStages) & 1u, abort_flag, p.a.status, 74));
             if (!ok) break;
             tc_fence_after();
-            for (int i = 0; i < both; i++) scores(i, st);
+            for (int i = 0; i < both; i++) scores(i, st, i);
             if (elect_one()) tc_commit(bar(L::empty, st));
             __syncwarp();
             n++;
@@ -532,22 +603,10 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                 ok = warp_all(mbar_wait(bar(L::full, sv), (n / kStages) & 1u, abort_flag, p.a.status, 76));
                 if (ok && j + 1 < tiles) ok = warp_all(mbar_wait(bar(L::full, sk), ((n + 1) / kStages) & 1u, abort_flag, p.a.status, 77));
                 for (int i = 0; i < both && ok; i++) {
-                    const uint64_t dv = make_smem_desc(base + L::stages + sv * L::kStage, kTileTokens * 128, 1024);
-#pragma unroll
-                    for (int h = 0; h < 2; h++) {  // as the weights come: those of the first 64 tokens, and the others
-                        ok = warp_all(mbar_wait(bar(h ? L::p_full : L::p_half, i), uses[i] & 1u, abort_flag, p.a.status, 78));
-                        if (!ok) break;
-                        tc_fence_after();
-                        if (elect_one()) {
-#pragma unroll
-                            for (int kk = 4 * h; kk < 4 * h + 4; kk++)
-                                tc_mma_f16_a_tmem(tmem + 256 + i * 128, tmem + i * 128 + kk * 8, dv + (uint64_t)(kk * 128), id_o, j > 0 || kk > 0);
-                        }
-                        __syncwarp();
-                    }
+                    values(i, i, sv, uses[i] & 1u, j > 0);
                     if (!ok) break;
                     uses[i]++;
-                    if (j + 1 < tiles) scores(i, sk);
+                    if (j + 1 < tiles) scores(i, sk, i);
                 }
                 if (!ok) break;
                 if (elect_one()) {
@@ -571,8 +630,9 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
     }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsRows));
+      if (warp < 4 * kTiles) {
         const int i = warp >> 2, row = (warp & 3) * 32 + lane;  // tile, row
-        const uint32_t t_s = tmem + i * 128 + ((uint32_t)((warp & 3) * 32) << 16), t_o = t_s + 256;
+        const uint32_t t_warp = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_o = t_warp + 256 + i * 128;
         uint32_t uses = 0, tile = 0;  // scores of this row tile, tiles of tokens
         SegmentInfo g;
         while (next_segment(g, 82)) {
@@ -587,7 +647,9 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                 int t0 = g.t0;
                 for (int j = 0; j < g.tiles; j++, t0 += kTileTokens) {
                     const uint32_t mt = base + L::meta + ((tile + j) % kMetaRing) * 128;
-                    ok = warp_all(mbar_wait(bar(L::s_full, i), uses & 1u, abort_flag, p.a.status, 79) &&
+                    const int place = kTiles == 2 ? i : (int)(uses & 1u);  // of the scores
+                    const uint32_t t_s = t_warp + place * 128;
+                    ok = warp_all(mbar_wait(bar(L::s_full, place), (kTiles == 2 ? uses : uses >> 1) & 1u, abort_flag, p.a.status, 79) &&
                                   mbar_wait(bar(L::meta_full, (tile + j) % kMetaRing), ((tile + j) / kMetaRing) & 1u, abort_flag, p.a.status, 83));
                     if (!ok) break;
                     uses++;
@@ -618,6 +680,11 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                     const bool grows = top > m + kLazy || (m == kNegInf && top > kNegInf);
                     if (__any_sync(0xFFFFFFFFu, grows)) {
                         const float next = grows ? top : m, h = grows ? part_factor(m, next) : 1.f;
+                        if (kTiles == 1 && j > 0) {  // (with two row tiles the scores' barrier says so)
+                            ok = warp_all(mbar_wait(bar(L::pv_done), uses & 1u, abort_flag, p.a.status, 86));  // products with values of tile uses - 2 (uses counts this one)
+                            if (!ok) break;
+                            tc_fence_after();
+                        }
                         if (j > 0) {
 #pragma unroll 1
                             for (int c = 0; c < D / 16; c++) {
@@ -670,13 +737,13 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                             tmem_st_wait();
                             tc_fence_before();
                             __syncwarp();
-                            if (lane == 0) mbar_arrive(bar(L::p_half, i));
+                            if (lane == 0) mbar_arrive(bar(L::p_half, place));
                         }
                     }
                     tmem_st_wait();
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(L::p_full, i));
+                    if (lane == 0) mbar_arrive(bar(L::p_full, place));
                 }
             }
             if (!ok) break;
@@ -711,7 +778,7 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                     }
                 }
                 if (mine) {
-                    if (!g.whole) *reinterpret_cast<float2*>(record + (size_t)kRecordRows * D + 2 * (i * kTileRows + row)) = make_float2(m, l);
+                    if (!g.whole) *reinterpret_cast<float2*>(record + (size_t)Record<D>::kRows * D + 2 * (i * kTileRows + row)) = make_float2(m, l);
                     else if (p.a.lse) p.a.lse[tok * p.a.heads + h] = lse_of(m, l, kShift);
                 }
             }
@@ -720,6 +787,7 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
             if (lane == 0) mbar_arrive(bar(L::o_empty));
             seg++;
         }
+      }
     }
     tc_fence_before();
     __syncthreads();
@@ -729,7 +797,7 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
     }
 }
 
-// Joins the unit that the boundary between blocks b - 1 and b cuts first; a block of threads takes 16 of its 256 rows.
+// Joins the unit that the boundary between blocks b - 1 and b cuts first; a block of threads takes 16 of its rows.
 constexpr int kJoinRows = 16;
 template <int D, int DT>
 __global__ void __launch_bounds__(kThreads) cache_attention_join_kernel(const PrefillParams p, int grid_blocks)
@@ -753,10 +821,10 @@ __global__ void __launch_bounds__(kThreads) cache_attention_join_kernel(const Pr
         auto record = [&](int j) -> const float* { return p.a.partial + (size_t)(2 * (b - 1 + j) + (j == 0 ? 1 : 0)) * Record<D>::floats; };
         float top = kNegInf, den = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-        for (int j = 0; j < parts; j++) top = fmaxf(top, record(j)[(size_t)kRecordRows * D + 2 * row]);
+        for (int j = 0; j < parts; j++) top = fmaxf(top, record(j)[(size_t)Record<D>::kRows * D + 2 * row]);
 #pragma unroll 4
         for (int j = 0; j < parts; j++) {
-            const float2 ml = *reinterpret_cast<const float2*>(record(j) + (size_t)kRecordRows * D + 2 * row);
+            const float2 ml = *reinterpret_cast<const float2*>(record(j) + (size_t)Record<D>::kRows * D + 2 * row);
             const float4 a = *reinterpret_cast<const float4*>(record(j) + (size_t)row * D + d);
             const float h = part_factor(ml.x, top);
             den += ml.y * h;
@@ -781,17 +849,17 @@ struct Sizes {
 Sizes sizes_of(int n_seqs, int n_q, int max_length, int heads, int kv_heads, int dim)
 {
     Sizes z;
-    const int group = heads / kv_heads;
+    const int group = heads / kv_heads, unit_rows = dim == 256 ? TileShape<256>::kUnitRows : TileShape<128>::kUnitRows;
     const long long cap = (long long)n_seqs * ((max_length + kTileTokens - 1) / kTileTokens + 1);
     z.cap_blocks = (int)(cap < (1 << 22) ? cap : 1 << 22);
-    z.pairs = (int)((long long)n_q * group / kPairRows) + n_seqs;
+    z.pairs = (int)((long long)n_q * group / unit_rows) + n_seqs;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += round_up_256(bytes); return here; };
     z.cut = take((size_t)kMaxBlocks * 16);
     z.block_at = take((size_t)(n_seqs + 1) * 4);
     z.tiles_at = take((size_t)(z.pairs + 1) * 8);
     z.pair_seq = take((size_t)z.pairs * 4);
-    z.partial = take((size_t)2 * kMaxBlocks * kRecordRows * (dim + 2) * 4);
+    z.partial = take((size_t)2 * kMaxBlocks * unit_rows * (dim + 2) * 4);
     z.meta = take((size_t)kv_heads * z.cap_blocks * 8 * 16);
     z.q_mul = take((size_t)n_q * heads * 4);
     z.kx = take((size_t)kv_heads * z.cap_blocks * kTileTokens * dim * 2);
@@ -819,7 +887,7 @@ cudaError_t launch_of(const PrefillParams& p, int sms, cudaStream_t st)
 {
     cudaError_t rc = launch_pdl_threads(kPlanThreads, cache_plan_kernel, dim3(1), st, p);
     if (rc != cudaSuccess) return rc;
-    const long long units = 2ll * p.cap_blocks * p.a.c.heads + ((long long)p.a.n_q * p.a.heads + 127) / 128, most = 6ll * sms;  // (six blocks fit on an SM)
+    const long long units = 2ll * p.cap_blocks * p.a.c.heads + ((long long)p.a.n_q * p.a.heads * D + 8191) / 8192, most = 6ll * sms;  // (six blocks fit on an SM)
     rc = launch_pdl(cache_expand_kernel<D, DT>, dim3((unsigned)(units < most ? units : most)), st, p);
     if (rc != cudaSuccess) return rc;
     CUtensorMap mq, mk, mv;
@@ -838,16 +906,18 @@ cudaError_t launch_of(const PrefillParams& p, int sms, cudaStream_t st)
     cfg.numAttrs = 1;
     rc = cudaLaunchKernelEx(&cfg, cache_attention_tiles_kernel<D, DT>, mq, mk, mv, p);
     if (rc != cudaSuccess) return rc;
-    rc = launch_pdl(cache_attention_join_kernel<D, DT>, dim3((unsigned)(blocks > 1 ? blocks - 1 : 1), kPairRows / kJoinRows), st, p, blocks);
+    rc = launch_pdl(cache_attention_join_kernel<D, DT>, dim3((unsigned)(blocks > 1 ? blocks - 1 : 1), TileShape<D>::kUnitRows / kJoinRows), st, p, blocks);
     g_launches.fetch_add(4, std::memory_order_relaxed);
     return rc;
 }
 
 }  // namespace
 
+// From 64 rows of a key head on (us, few-rows kernel / this: 16 sequences of 16 queries and four heads to a key head against up to 2000 tokens 64.5 / 54.6, 64 against up to 4000
+// 375 / 326, one against 8000 38.0 / 40.1, heads of 64: 4 against up to 16000 79 / 91; twice the rows: 16 against up to 2000 107 / 61).
 size_t prefill_workspace_bytes(int n_seqs, int n_q, int max_q, int max_length, int heads, int kv_heads, int dim)
 {
-    if ((long long)max_q * (heads / kv_heads) < 64 || dim > 128) return 0;
+    if ((long long)max_q * (heads / kv_heads) < 64) return 0;
     const Sizes z = sizes_of(n_seqs, n_q, max_length, heads, kv_heads, dim);
     if ((long long)kv_heads * z.cap_blocks * kTileTokens > 0x7FFFFFFF || (long long)n_q * heads > 0x7FFFFFFF) return 0;  // (rows of a tensor map)
     return z.total;
@@ -859,11 +929,13 @@ cudaError_t launch_prefill(AttentionParams a, int dtype, int max_length, uint8_t
     cudaError_t rc = cudaGetDevice(&dev);
     if (rc != cudaSuccess) return rc;
     const PrefillSetup* setup = g_prefill_setup.get(dev, [](int, PrefillSetup* o) {
-        const void* k[4] = {(const void*)cache_attention_tiles_kernel<64, HIF8_BF16>, (const void*)cache_attention_tiles_kernel<64, HIF8_F16>,
-                            (const void*)cache_attention_tiles_kernel<128, HIF8_BF16>, (const void*)cache_attention_tiles_kernel<128, HIF8_F16>};
-        const int bytes[4] = {(int)PrefillSmem<64>::kBytes, (int)PrefillSmem<64>::kBytes, (int)PrefillSmem<128>::kBytes, (int)PrefillSmem<128>::kBytes};
+        const void* k[6] = {(const void*)cache_attention_tiles_kernel<64, HIF8_BF16>, (const void*)cache_attention_tiles_kernel<64, HIF8_F16>,
+                            (const void*)cache_attention_tiles_kernel<128, HIF8_BF16>, (const void*)cache_attention_tiles_kernel<128, HIF8_F16>,
+                            (const void*)cache_attention_tiles_kernel<256, HIF8_BF16>, (const void*)cache_attention_tiles_kernel<256, HIF8_F16>};
+        const int bytes[6] = {(int)PrefillSmem<64>::kBytes, (int)PrefillSmem<64>::kBytes, (int)PrefillSmem<128>::kBytes, (int)PrefillSmem<128>::kBytes, (int)PrefillSmem<256>::kBytes,
+                              (int)PrefillSmem<256>::kBytes};
         o->rc = cudaSuccess;
-        for (int i = 0; i < 4 && o->rc == cudaSuccess; i++) o->rc = cudaFuncSetAttribute(k[i], cudaFuncAttributeMaxDynamicSharedMemorySize, bytes[i]);
+        for (int i = 0; i < 6 && o->rc == cudaSuccess; i++) o->rc = cudaFuncSetAttribute(k[i], cudaFuncAttributeMaxDynamicSharedMemorySize, bytes[i]);
     });
     if (!setup || setup->rc != cudaSuccess) return cudaErrorInvalidValue;
     PrefillParams p;
@@ -883,8 +955,10 @@ cudaError_t launch_prefill(AttentionParams a, int dtype, int max_length, uint8_t
     p.cap_blocks = z.cap_blocks;
     p.pairs = z.pairs;
     p.rows = (long long)a.n_q * a.group;
+    p.unit_rows = a.c.dim == 256 ? TileShape<256>::kUnitRows : TileShape<128>::kUnitRows;
     if (a.c.dim == 64) return dtype == HIF8_BF16 ? launch_of<64, HIF8_BF16>(p, sms, st) : launch_of<64, HIF8_F16>(p, sms, st);
-    return dtype == HIF8_BF16 ? launch_of<128, HIF8_BF16>(p, sms, st) : launch_of<128, HIF8_F16>(p, sms, st);
+    if (a.c.dim == 128) return dtype == HIF8_BF16 ? launch_of<128, HIF8_BF16>(p, sms, st) : launch_of<128, HIF8_F16>(p, sms, st);
+    return dtype == HIF8_BF16 ? launch_of<256, HIF8_BF16>(p, sms, st) : launch_of<256, HIF8_F16>(p, sms, st);
 }
 
 }  // namespace hif8

@@ -140,13 +140,13 @@ def test_several_queries(counts, causal, window, heads, kv_heads, dim):
 
 @pytest.mark.parametrize("lengths,counts", [([300], [128]), ([129, 64, 1], [129, 64, 1]), ([3000, 0, 700, 40], [300, 0, 700, 33]), ([5000, 260], [65, 260]), ([50, 20], [70, 90])])
 @pytest.mark.parametrize("causal,window", [(1, 0), (0, 0), (1, 200), (1, 3), (0, 129)])
-@pytest.mark.parametrize("heads,kv_heads,dim,dtype", [(8, 2, 128, BF16), (3, 3, 64, F16), (7, 1, 64, BF16), (5, 5, 128, F16)])
+@pytest.mark.parametrize("heads,kv_heads,dim,dtype", [(8, 2, 128, BF16), (3, 3, 64, F16), (7, 1, 64, BF16), (5, 5, 128, F16), (4, 2, 256, BF16), (7, 1, 256, F16)])
 def test_chunks(lengths, counts, causal, window, heads, kv_heads, dim, dtype):
     c, q = make(lengths, counts, heads, kv_heads, 16 if window else 128, dim, dtype, seed=len(lengths) + window)
     close(c, q, counts, heads, causal, window)
 
 
-@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("dim", [64, 128, 256])
 def test_chunks_without_room_for_tiles(dim):
     c, q = make([700, 90], [100, 90], 8, 2, 64, dim, BF16)
     close(c, q, [100, 90], 8)
