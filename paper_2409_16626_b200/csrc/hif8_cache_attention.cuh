@@ -127,16 +127,17 @@ __device__ __forceinline__ unsigned long long global_ns()
     return t;
 }
 constexpr unsigned long long kWaitLimitNs = 2000000000ull;  // 2 s a wait
-// Bounded wait: false when the barrier did not complete in time, or someone else of the block gave up.
+// Bounded wait: false when the barrier did not complete in time, or someone else of the block gave up.  (The clock is only read when a wait gets long.)
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int where)
 {
-    if (mbar_try_wait(bar, parity)) return true;
-    const unsigned long long t0 = global_ns();
+    unsigned long long t0 = 0;
     for (uint32_t it = 1;; it++) {
         if (mbar_try_wait(bar, parity)) return true;
         if ((it & 63u) == 0) {
             if (*abort_flag) return false;
-            if (global_ns() - t0 > kWaitLimitNs) {
+            const unsigned long long now = global_ns();
+            if (t0 == 0) t0 = now;
+            if (now - t0 > kWaitLimitNs) {
                 *abort_flag = 1;
                 atomicCAS(status, 0, where);
                 return false;
