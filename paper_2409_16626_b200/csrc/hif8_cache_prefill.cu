@@ -641,6 +641,7 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
             SeqView v;
             v.first = g.first; v.n_q = g.n_q; v.len = g.len;
             float m = kNegInf, l = 0.f;
+            bool far = false;  // a maximum that an FMA cannot take off exactly
             if (works) {
                 const int hi = min(v.len, hi_of(p.a, v, qi)), lo = lo_of(p.a, v, qi);
                 const float mul = p.q_mul[g.head * p.rows + (long long)g.first * p.a.group + r];
@@ -657,6 +658,12 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                     uint32_t sr[128];
 #pragma unroll
                     for (int c = 0; c < 4; c++) tmem_ld_x32(t_s + 32 * c, sr + 32 * c);
+                    float f[8], minus_ev[8], weight[8];  // of 16 tokens: factor of a score, -e_v, 2^e_v
+#pragma unroll
+                    for (int x = 0; x < 8; x++) {
+                        const float4 k = lds_f4(mt + 16 * x);
+                        f[x] = fmaxf(fminf(mul * k.x, 3.0e38f), 1.0e-36f); minus_ev[x] = k.y; weight[x] = k.z;
+                    }
                     tmem_ld_wait();
                     if (t0 < g.lo_max || t0 + kTileTokens > g.hi_min) {  // some row does not see some token
 #pragma unroll
@@ -671,11 +678,10 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                     float top = kNegInf;
 #pragma unroll
                     for (int x = 0; x < 8; x++) {
-                        const float4 k = lds_f4(mt + 16 * x);
                         auto a = [&](int y) { return __uint_as_float(sr[16 * x + y]); };
                         const float b0 = max3(a(0), a(1), a(2)), b1 = max3(a(3), a(4), a(5)), b2 = max3(a(6), a(7), a(8)), b3 = max3(a(9), a(10), a(11)), b4 = max3(a(12), a(13), a(14));
                         const float c = max3(max3(b0, b1, a(15)), max3(b2, b3, b4), kNegInf);
-                        top = fmaxf(top, fmaf(c, fmaxf(fminf(mul * k.x, 3.0e38f), 1.0e-36f), k.y));
+                        top = fmaxf(top, fmaf(c, f[x], minus_ev[x]));
                     }
                     const bool grows = top > m + kLazy || (m == kNegInf && top > kNegInf);
                     if (__any_sync(0xFFFFFFFFu, grows)) {
@@ -698,16 +704,15 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                         }
                         l *= h;
                         m = next;
+                        far = __any_sync(0xFFFFFFFFu, fabsf(m) > 131072.f && m != kNegInf);
                     }
                     const float base_m = m == kNegInf ? 0.f : m;
-                    const bool far = __any_sync(0xFFFFFFFFu, fabsf(base_m) > 131072.f);
                     if (far) {  // there -m + 4 - e would lose its last bits: the differences first
 #pragma unroll
                         for (int x = 0; x < 8; x++) {
-                            const float4 k = lds_f4(mt + 16 * x);
-                            const float f = fmaxf(fminf(mul * k.x, 3.0e38f), 1.0e-36f);
 #pragma unroll
-                            for (int y = 0; y < 16; y++) sr[16 * x + y] = __float_as_uint(fmaf(__uint_as_float(sr[16 * x + y]), f, k.y) - base_m);
+                            for (int y = 0; y < 16; y++) sr[16 * x + y] = __float_as_uint(fmaf(__uint_as_float(sr[16 * x + y]), f[x], minus_ev[x]) - base_m);
+                            f[x] = 1.f; minus_ev[x] = base_m;
                         }
                     }
 #pragma unroll
@@ -715,9 +720,8 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                         uint32_t pr[16];
 #pragma unroll
                         for (int x = 2 * c; x < 2 * c + 2; x++) {
-                            const float4 k = lds_f4(mt + 16 * x);
-                            const float f = far ? 1.f : fmaxf(fminf(mul * k.x, 3.0e38f), 1.0e-36f), add = far ? kShift : k.y - base_m + kShift;
-                            const uint64_t f2 = pack2(f, f), a2 = pack2(add, add);
+                            const float add = minus_ev[x] - base_m + kShift;
+                            const uint64_t f2 = pack2(f[x], f[x]), a2 = pack2(add, add);
                             uint64_t sum2 = 0;
 #pragma unroll
                             for (int y = 0; y < 16; y += 2) {
@@ -730,7 +734,7 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                             }
                             float u0, u1;
                             unpack2(sum2, u0, u1);
-                            l = fmaf(u0 + u1, k.z, l);
+                            l = fmaf(u0 + u1, weight[x], l);
                         }
                         tmem_st_x16(t_s + 16 * c, pr);
                         if (c == 1) {  // the products with the first 64 tokens may start
