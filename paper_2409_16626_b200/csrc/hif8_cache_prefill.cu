@@ -736,13 +736,13 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                             unpack2(sum2, u0, u1);
                             l = fmaf(u0 + u1, weight[x], l);
                         }
-                        tmem_st_x16(t_s + 16 * c, pr);
-                        if (c == 1) {  // the products with the first 64 tokens may start
+                        if (c == 2) {  // the products with the first 64 tokens may start: their weights have landed while these were computed
                             tmem_st_wait();
                             tc_fence_before();
                             __syncwarp();
                             if (lane == 0) mbar_arrive(bar(L::p_half, place));
                         }
+                        tmem_st_x16(t_s + 16 * c, pr);
                     }
                     tmem_st_wait();
                     tc_fence_before();
