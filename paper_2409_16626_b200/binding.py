@@ -346,7 +346,8 @@ def hif8_cache_read(k_pages, v_pages, k_exp, v_exp, n_pages, kv_heads, page_toke
 
 
 def hif8_cache_attention_workspace_bytes(n_seqs, n_q, max_q, max_length, heads, kv_heads, head_dim):
-    return int(lib.hif8_cache_attention_workspace_bytes(n_seqs, n_q, max_q, max_length, heads, kv_heads, head_dim))
+    n = _c.hif8_cache_attention_workspace_bytes(n_seqs, n_q, max_q, max_length, heads, kv_heads, head_dim)
+    return int(lib.hif8_cache_attention_workspace_bytes(n_seqs, n_q, max_q, max_length, heads, kv_heads, head_dim)) if n is None else n
 
 
 def hif8_cache_attention(q, dtype, q_token_stride, q_head_stride, d_q_start, d_lengths, n_seqs, n_q, max_q, max_length, k_pages, v_pages, k_exp, v_exp,
@@ -370,7 +371,8 @@ def hif8_cache_fork(k_pages, v_pages, k_exp, v_exp, n_pages, kv_heads, page_toke
 
 
 def hif8_cache_compact_workspace_bytes(n_pages):
-    return int(lib.hif8_cache_compact_workspace_bytes(n_pages))
+    n = _c.hif8_cache_compact_workspace_bytes(n_pages)
+    return int(lib.hif8_cache_compact_workspace_bytes(n_pages)) if n is None else n
 
 
 def hif8_cache_compact(k_pages, v_pages, k_exp, v_exp, n_pages, kv_heads, page_tokens, head_dim, page_table, table_stride, d_lengths, n_seqs, move,

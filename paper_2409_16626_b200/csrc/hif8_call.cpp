@@ -80,18 +80,20 @@ bool convert(PyObject* o, T* out)
 }
 
 template <auto F> struct Entry;
-template <class... A, int (*F)(A...)>
+PyObject* result(int rc) { return PyLong_FromLong(rc); }
+PyObject* result(size_t n) { return PyLong_FromSize_t(n); }
+template <class R, class... A, R (*F)(A...)>
 struct Entry<F> {
     template <size_t... I>
     static PyObject* run(PyObject* const* args, std::index_sequence<I...>)
     {
         std::tuple<A...> a{};
         if (!(convert<A>(args[I], &std::get<I>(a)) && ...)) { PyErr_Clear(); Py_RETURN_NONE; }
-        int rc;
+        R rc;
         Py_BEGIN_ALLOW_THREADS
         rc = F(std::get<I>(a)...);
         Py_END_ALLOW_THREADS
-        return PyLong_FromLong(rc);
+        return result(rc);
     }
     static PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n)
     {
@@ -124,6 +126,7 @@ PyMethodDef methods[] = {
     HIF8_ENTRY(hif8_gemm_channel_scaled), HIF8_ENTRY(hif8_channel_amax_scale_encode), HIF8_ENTRY(hif8_delayed_scale_encode),
     HIF8_ENTRY(hif8_encode_transpose), HIF8_ENTRY(hif8_encode_from_amax), HIF8_ENTRY(hif8_als_update), HIF8_ENTRY(hif8_check_finite),
     HIF8_ENTRY(hif8_cache_append), HIF8_ENTRY(hif8_cache_read), HIF8_ENTRY(hif8_cache_attention), HIF8_ENTRY(hif8_cache_fork), HIF8_ENTRY(hif8_cache_compact),
+    HIF8_ENTRY(hif8_cache_attention_workspace_bytes), HIF8_ENTRY(hif8_cache_compact_workspace_bytes),
     {"set_up", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&set_up)), METH_FASTCALL, nullptr},
     {"set_cuda_ready", &set_cuda_ready, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
