@@ -650,47 +650,58 @@ __global__ void __launch_bounds__(kCombineThreads) cache_attention_combine_kerne
 }
 
 // Inf and NaN among the values of tokens that only some of a sequence's queries see: the rows that do see them get them here.  (Those that all queries
-// see took the ordinary way.)  A block looks through 16 elements of a key head's value rows; there is hardly ever anything to do.
+// see took the ordinary way.)  A block looks through `slices` pieces of 16 elements of a key head's value rows, 256 pieces at a time, and lists what it finds; there
+// is hardly ever anything to do.
 template <int DT>
-__global__ void __launch_bounds__(kThreads) cache_attention_specials_kernel(const AttentionParams p)
+__global__ void __launch_bounds__(kThreads) cache_attention_specials_kernel(const AttentionParams p, int slices)
 {
+    __shared__ int2 s_found[kThreads * 16];  // token, element and code
+    __shared__ int s_count;
     pdl_wait_prior_grid();
     pdl_launch_dependents();
-    const int slice = blockIdx.x, head = blockIdx.y, s = blockIdx.z;
     if (p.special_flag && !*p.special_flag) return;
+    const int head = blockIdx.y, s = blockIdx.z;
     const SeqView v = seq_view(p, s);
     if (v.n_q < 2) return;
-    // tokens that the last query sees or the first, and not both
+    // tokens that the last query sees or the first, and not both: [a0, a1) and [b0, b1)
     const int hi0 = min(v.len, hi_of(p, v, 0)), hi1 = min(v.len, hi_of(p, v, v.n_q - 1)), lo0 = lo_of(p, v, 0), lo1 = lo_of(p, v, v.n_q - 1);
-    const int a0 = lo0, a1 = min(lo1, hi1), b0 = max(hi0, a1), b1 = hi1;  // [a0, a1) and [b0, b1)
-    const int n = max(0, a1 - a0) + max(0, b1 - b0);
-    auto token = [&](int i) { return i < max(0, a1 - a0) ? a0 + i : b0 + (i - max(0, a1 - a0)); };
-    auto codes = [&](int tok) -> uint4 {
-        const int page = p.c.page_of(s, tok >> p.c.shift);
-        if (page < 0) return make_uint4(0, 0, 0, 0);
-        return __ldg(reinterpret_cast<const uint4*>(p.c.v + p.c.block_at(page, head) + (long long)(tok & ((1 << p.c.shift) - 1)) * p.c.dim + 16 * slice));
-    };
-    int found = 0;
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-        const uint4 w = codes(token(i));
-        found |= finite_codes(w.x) != w.x || finite_codes(w.y) != w.y || finite_codes(w.z) != w.z || finite_codes(w.w) != w.w;
-    }
-    if (!__syncthreads_or(found)) return;
-    const long long work = (long long)v.n_q * p.group * 16;
-    for (long long i = threadIdx.x; i < work; i += kThreads) {
-        const int d = (int)(i & 15), r = (int)(i >> 4), qi = r / p.group, h = head * p.group + r - qi * p.group;
-        const int hi = min(v.len, hi_of(p, v, qi)), lo = lo_of(p, v, qi);
-        float add = 0.f;
-        for (int j = 0; j < n; j++) {
-            const int tok = token(j);
-            if (tok < lo || tok >= hi) continue;
-            const uint4 w = codes(tok);
-            const uint32_t word = d < 4 ? w.x : d < 8 ? w.y : d < 12 ? w.z : w.w, c = (word >> (8 * (d & 3))) & 0xFFu;
-            if (c == 0x80u || (c & 0x7Fu) == 0x6Fu) add += __uint_as_float(decode_bits_f32(c));
+    const int a0 = lo0, a1 = min(lo1, hi1), b0 = max(hi0, a1), b1 = hi1, n_a = max(0, a1 - a0);
+    const long long pieces = (long long)(n_a + max(0, b1 - b0)) * slices;
+    if (threadIdx.x == 0) s_count = 0;
+    __syncthreads();
+    for (long long at = 0; at < pieces; at += kThreads) {
+        const long long i = at + threadIdx.x;
+        if (i < pieces) {
+            const int k = (int)(i / slices), d0 = ((int)blockIdx.x * slices + (int)(i - (long long)k * slices)) * 16, tok = k < n_a ? a0 + k : b0 + (k - n_a);
+            const int page = p.c.page_of(s, tok >> p.c.shift);
+            uint4 w = make_uint4(0, 0, 0, 0);
+            if (page >= 0) w = __ldg(reinterpret_cast<const uint4*>(p.c.v + p.c.block_at(page, head) + (long long)(tok & ((1 << p.c.shift) - 1)) * p.c.dim + d0));
+            if (finite_codes(w.x) != w.x || finite_codes(w.y) != w.y || finite_codes(w.z) != w.z || finite_codes(w.w) != w.w)
+                for (int d = 0; d < 16; d++) {
+                    const uint32_t c = ((d < 4 ? w.x : d < 8 ? w.y : d < 12 ? w.z : w.w) >> (8 * (d & 3))) & 0xFFu;
+                    if (c == 0x80u || (c & 0x7Fu) == 0x6Fu) s_found[atomicAdd(&s_count, 1)] = make_int2(tok, (d0 + d) << 8 | (int)c);
+                }
         }
-        if (add != 0.f) {  // (an Inf or a NaN)
-            unsigned short* out = reinterpret_cast<unsigned short*>(p.out) + (long long)(v.first + qi) * p.out_token + (long long)h * p.out_head + 16 * slice + d;
-            *out = (unsigned short)to_bits<DT>(q_value<DT>(*out) + add);
+        __syncthreads();
+        const int found = s_count;
+        __syncthreads();  // (everyone has read it before the next pieces are counted)
+        if (found) {
+            const int width = 16 * slices;
+            const long long work = (long long)v.n_q * p.group * width;
+            for (long long x = threadIdx.x; x < work; x += kThreads) {
+                const int r = (int)(x / width), d = (int)blockIdx.x * width + (int)(x - (long long)r * width), qi = r / p.group, h = head * p.group + r - qi * p.group;
+                const int hi = min(v.len, hi_of(p, v, qi)), lo = lo_of(p, v, qi);
+                float add = 0.f;  // (Inf and NaN: the order of the sum does not matter)
+                for (int j = 0; j < found; j++)
+                    if (s_found[j].y >> 8 == d && s_found[j].x >= lo && s_found[j].x < hi) add += __uint_as_float(decode_bits_f32((uint32_t)s_found[j].y & 0xFFu));
+                if (add != 0.f) {
+                    unsigned short* out = reinterpret_cast<unsigned short*>(p.out) + (long long)(v.first + qi) * p.out_token + (long long)h * p.out_head + d;
+                    *out = (unsigned short)to_bits<DT>(q_value<DT>(*out) + add);
+                }
+            }
+            __syncthreads();
+            if (threadIdx.x == 0) s_count = 0;
+            __syncthreads();
         }
     }
 }
@@ -856,8 +867,9 @@ extern "C" int hif8_cache_attention(const void* q, int dtype, int64_t q_token_st
         rc = launch_prefill(p, dtype, max_length, ws + kHeadBytes, sms, st);
     } else rc = dtype == HIF8_BF16 ? launch_rows_of<HIF8_BF16>(p, nt, max_q, max_length, sms, st) : launch_rows_of<HIF8_F16>(p, nt, max_q, max_length, sms, st);
     if (rc == cudaSuccess && max_q > 1 && (p.causal || p.window)) {
-        const dim3 grid((unsigned)(head_dim / 16), (unsigned)kv_heads, (unsigned)n_seqs);
-        rc = dtype == HIF8_BF16 ? launch_pdl(cache_attention_specials_kernel<HIF8_BF16>, grid, st, p) : launch_pdl(cache_attention_specials_kernel<HIF8_F16>, grid, st, p);
+        const int slices = p.special_flag ? 1 : head_dim / 16;  // (few rows: few tokens to look at)
+        const dim3 grid((unsigned)(head_dim / 16 / slices), (unsigned)kv_heads, (unsigned)n_seqs);
+        rc = dtype == HIF8_BF16 ? launch_pdl(cache_attention_specials_kernel<HIF8_BF16>, grid, st, p, slices) : launch_pdl(cache_attention_specials_kernel<HIF8_F16>, grid, st, p, slices);
         g_launches.fetch_add(1, std::memory_order_relaxed);
     }
     note_status_word(st, p.status);

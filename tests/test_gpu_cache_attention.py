@@ -217,6 +217,20 @@ def test_inf_and_nan_where_they_are_not_seen(counts, causal, window, small):
     close(c, q, counts, 8, causal, window, small=small)
 
 
+@pytest.mark.parametrize("small", [False, True])
+def test_a_later_query_s_values_are_all_special(small):
+    """Every value of the last tokens is Inf or NaN: the queries in front of them keep their results."""
+    c, q = make([400], [120], 4, 2, 16, 64, F16)
+    c.fill(0)
+    clean = attend(c, q, [120], 4, small=small)[0]
+    rng = np.random.default_rng(3)
+    for t in range(330, 400):
+        c.h["v"][c.table[0, t // 16], :, t % 16] = rng.choice([0x80, 0x6F, 0xEF], size=(2, 64))
+    c.upload()
+    out, _ = close(c, q, [120], 4, small=small)
+    assert torch.equal(out[:50], clean[:50]) and not torch.isfinite(out[50:]).any()
+
+
 @pytest.mark.parametrize("counts", [[1, 2], [1, 40]])
 def test_scores_and_spreads_at_the_ends(counts):
     """Large scores (one token takes all), queries and blocks of very different magnitudes, exponents beyond the limit."""
