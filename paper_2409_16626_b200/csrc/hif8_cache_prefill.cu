@@ -9,6 +9,12 @@
 // FP16, written over S, and O += P V accumulates in tensor memory; while one tile's warps work, the tensor cores do the other tile's products.  O is only
 // rescaled when a row's maximum has grown by more than 2^8 (P stays below 2^12), by the warps themselves: the next scores' barrier says that the sums are not in use.
 // The tiles of all units are dealt out evenly over the blocks; a unit that several blocks share leaves FP32 parts, which a last kernel joins in a fixed order.
+//
+// Measured: a chunk of 2048 queries against 16461 tokens, 32/8 heads of 128: 525 us a call (986 TFLOP/s; cuBLAS sustains 1384 here at the same 1000 W), 465 of them in the
+// attention kernel, whose tensor pipe is busy 59 % of the time and the exponentials' unit as long.  A pair of tiles takes 3250 cycles where the products alone take 2048: what a row
+// tile's warps do to its scores (load 90, maximum 380, weights 1650 cycles) and its products (770, and 500 until each side has noticed the other) make a chain
+// as long as that, and two row tiles are what tensor memory holds.  Exponentials as polynomials on the FMA pipe, for an eighth to half of the elements, made it slower (531 ->
+// 534 to 558 us), and so did a warp of its own to issue each row tile's products (540 -> 588).
 #include "hif8_cache_attention.cuh"
 
 namespace hif8 {
@@ -37,7 +43,7 @@ struct PrefillParams {
     int* block_at;         // [n_seqs + 1] first 128-token block of each sequence
     long long* tiles_at;   // [pairs + 1] tiles in front of each pair of row tiles (of one head)
     int* pair_seq;         // [pairs]
-    int4* cut;             // [blocks] pair, sequence, key head and first tile of the block's first segment
+    int4* cut;             // [blocks] two of each: first tile, tiles, key head and first row of the unit that the block's first segment lies in; first query, rows
     int* specials;         // set when some token that only some queries see holds Inf or NaN in V
     int cap_blocks, pairs;
     long long rows;        // n_q * group
@@ -323,7 +329,7 @@ template <int D> struct Record {
 // a segment: tiles c0 .. c1 of a unit
 struct Segment {
     PairView u;
-    int pair, head, c0, c1;
+    int head, c0, c1;
     __device__ Segment(const PrefillParams& p, long long x0, long long x_end)
     {
         const long long per_head = p.tiles_at[p.pairs];
@@ -336,7 +342,6 @@ struct Segment {
             a += last * step;
             n = min(step, n - last * step);
         }
-        pair = a;
         u = pair_view(p, p.pair_seq[a], a);
         c0 = (int)(x - p.tiles_at[a]);
         c1 = (int)min((long long)u.tiles, c0 + (x_end - x0));
@@ -443,7 +448,10 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
             more = x0 < x_end;
             if (more) {
                 const Segment g(p, x0, x_end);
-                if (seg == 0 && lane == 0) p.cut[me] = make_int4(g.pair, g.u.seq, g.head, g.c0);
+                if (seg == 0 && lane == 0) {
+                    p.cut[2 * me] = make_int4(g.c0, g.u.tiles, g.head, g.u.r0);
+                    p.cut[2 * me + 1] = make_int4(g.u.v.first, g.u.n_rows, 0, 0);
+                }
                 info[0] = make_int4(g.c1 - g.c0, g.head, g.u.v.first, g.u.v.n_q);
                 info[1] = make_int4(g.u.v.len, g.u.r0, g.u.n_rows, g.u.base + (g.u.j0 + g.c0) * kTileTokens);
                 info[2] = make_int4(g.u.lo_max, g.u.hi_min, g.c0 == 0 && g.c1 == g.u.tiles, g.c0 == 0);
@@ -808,20 +816,18 @@ __global__ void __launch_bounds__(kThreads) cache_attention_join_kernel(const Pr
 {
     pdl_wait_prior_grid();
     pdl_launch_dependents();
-    const long long per_head = p.tiles_at[p.pairs], all = per_head * p.a.c.heads;
-    const int blocks = (int)min((long long)grid_blocks, all), b = (int)blockIdx.x + 1;
+    const int b = (int)blockIdx.x + 1;
+    const long long all = p.tiles_at[p.pairs] * p.a.c.heads;
+    const int4 cut = p.cut[2 * b], of = p.cut[2 * b + 1];  // the unit that the boundary cuts (of a block that has no tiles: not looked at)
+    const int blocks = (int)min((long long)grid_blocks, all);
     if (b >= blocks) return;
-    const long long x = share_of(all, b, blocks);
-    const int4 cut = p.cut[b];  // the unit that the boundary cuts
-    const long long begin = x - cut.w;
-    if (cut.w == 0 || share_of(all, b - 1, blocks) > begin) return;
-    const PairView u = pair_view(p, cut.y, cut.x);
-    const int head = cut.z;
-    const long long end = begin + u.tiles;
+    const long long begin = share_of(all, b, blocks) - cut.x, end = begin + cut.y;
+    if (cut.x == 0 || share_of(all, b - 1, blocks) > begin) return;
+    const int head = cut.z, r0 = cut.w, first = of.x, n_rows = of.y;
     const int parts = owner_of(all, end - 1, blocks) - (b - 1) + 1;
     for (int i = threadIdx.x; i < kJoinRows * (D / 4); i += kThreads) {
         const int row = (int)blockIdx.y * kJoinRows + i / (D / 4), d = i % (D / 4) * 4;
-        if (row >= u.n_rows) continue;
+        if (row >= n_rows) continue;
         auto record = [&](int j) -> const float* { return p.a.partial + (size_t)(2 * (b - 1 + j) + (j == 0 ? 1 : 0)) * Record<D>::floats; };
         float top = kNegInf, den = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
@@ -834,12 +840,12 @@ __global__ void __launch_bounds__(kThreads) cache_attention_join_kernel(const Pr
             den += ml.y * h;
             o[0] += a.x * h; o[1] += a.y * h; o[2] += a.z * h; o[3] += a.w * h;
         }
-        const int r = u.r0 + row, qi = r / p.a.group, h = head * p.a.group + r - qi * p.a.group;
+        const int r = r0 + row, qi = r / p.a.group, h = head * p.a.group + r - qi * p.a.group;
         const float inv = den == 0.f ? 0.f : 1.f / den;
 #pragma unroll
         for (int y = 0; y < 4; y++) o[y] *= inv;
-        store_out4<DT>(p.a, (long long)(u.v.first + qi) * p.a.out_token + (long long)h * p.a.out_head + d, o);
-        if (p.a.lse && d == 0) p.a.lse[(long long)(u.v.first + qi) * p.a.heads + h] = lse_of(top, den, kShift);
+        store_out4<DT>(p.a, (long long)(first + qi) * p.a.out_token + (long long)h * p.a.out_head + d, o);
+        if (p.a.lse && d == 0) p.a.lse[(long long)(first + qi) * p.a.heads + h] = lse_of(top, den, kShift);
     }
 }
 
@@ -859,7 +865,7 @@ Sizes sizes_of(int n_seqs, int n_q, int max_length, int heads, int kv_heads, int
     z.pairs = (int)((long long)n_q * group / unit_rows) + n_seqs;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += round_up_256(bytes); return here; };
-    z.cut = take((size_t)kMaxBlocks * 16);
+    z.cut = take((size_t)kMaxBlocks * 32);
     z.block_at = take((size_t)(n_seqs + 1) * 4);
     z.tiles_at = take((size_t)(z.pairs + 1) * 8);
     z.pair_seq = take((size_t)z.pairs * 4);
