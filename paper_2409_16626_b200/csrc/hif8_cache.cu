@@ -561,6 +561,7 @@ extern "C" int hif8_cache_read(const uint8_t* k_pages, const uint8_t* v_pages, c
     if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & (item - 1)) return HIF8_ERR_ALIGN;
     const size_t dst_bytes = ((size_t)(n_out - 1) * (size_t)token_stride + (size_t)(kv_heads - 1) * (size_t)head_stride + (size_t)head_dim) * item;
     const size_t pool = (size_t)n_pages * (size_t)p.c.page_bytes();
+    if (k == v) return HIF8_ERR_OVERLAP;  // (k and v may be slices of one tensor otherwise)
     for (const void* d : {(const void*)k, (const void*)v})
         for (const void* s : {(const void*)k_pages, (const void*)v_pages})
             if (ranges_overlap(s, pool, d, dst_bytes)) return HIF8_ERR_OVERLAP;

@@ -855,7 +855,7 @@ extern "C" int hif8_cache_attention(const void* q, int dtype, int64_t q_token_st
     if (!setup || setup->rc != cudaSuccess) return HIF8_ERR_CUDA;
     p.q = q; p.q_token = q_token_stride; p.q_head = q_head_stride; p.q_start = d_q_start; p.lengths = d_lengths; p.n_seqs = n_seqs; p.n_q = n_q; p.heads = heads; p.group = group;
     p.vectors = !((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15u) && !((q_token_stride | q_head_stride | out_token_stride | out_head_stride) & 7);
-    p.scale_log2 = fminf(softmax_scale * kLog2e, 3.0e38f); p.causal = causal != 0; p.window = window;
+    p.scale_log2 = fminf(softmax_scale * kLog2e, 3.0e38f); p.causal = causal != 0; p.window = window < 1 << 30 ? window : 1 << 30;  // (lengths and queries stay below 2^30: positions minus a window stay inside an int)
     p.out = out; p.out_token = out_token_stride; p.out_head = out_head_stride; p.lse = lse;
     uint8_t* ws = reinterpret_cast<uint8_t*>(workspace);
     p.status = reinterpret_cast<int*>(ws);

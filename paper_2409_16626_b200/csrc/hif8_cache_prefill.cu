@@ -852,6 +852,8 @@ __global__ void __launch_bounds__(kThreads) cache_attention_join_kernel(const Pr
 // ---------------------------------------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------------------------------------
+constexpr size_t kMostWorkspace = (size_t)16 << 30;
+
 struct Sizes {
     int cap_blocks, pairs;
     size_t cut, block_at, tiles_at, pair_seq, partial, meta, q_mul, kx, vx, qx, total;  // offsets
@@ -860,9 +862,9 @@ Sizes sizes_of(int n_seqs, int n_q, int max_length, int heads, int kv_heads, int
 {
     Sizes z;
     const int group = heads / kv_heads, unit_rows = dim == 256 ? TileShape<256>::kUnitRows : TileShape<128>::kUnitRows;
-    const long long cap = (long long)n_seqs * ((max_length + kTileTokens - 1) / kTileTokens + 1);
-    z.cap_blocks = (int)(cap < (1 << 22) ? cap : 1 << 22);
-    z.pairs = (int)((long long)n_q * group / unit_rows) + n_seqs;
+    const long long cap = (long long)n_seqs * (((long long)max_length + kTileTokens - 1) / kTileTokens + 1);
+    z.cap_blocks = (int)(cap < 0x7FFFFFFF ? cap : 0x7FFFFFFF);  // (refused by its size long before)
+    z.pairs = (int)((long long)n_q * group / unit_rows) + n_seqs;  // (n_q * group is below 2^30)
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += round_up_256(bytes); return here; };
     z.cut = take((size_t)kMaxBlocks * 32);
@@ -929,7 +931,8 @@ size_t prefill_workspace_bytes(int n_seqs, int n_q, int max_q, int max_length, i
 {
     if ((long long)max_q * (heads / kv_heads) < 64) return 0;
     const Sizes z = sizes_of(n_seqs, n_q, max_length, heads, kv_heads, dim);
-    if ((long long)kv_heads * z.cap_blocks * kTileTokens > 0x7FFFFFFF || (long long)n_q * heads > 0x7FFFFFFF) return 0;  // (rows of a tensor map)
+    // (rows of a tensor map; and no call is asked for more memory than a good part of a device's: the few-rows kernel then takes it)
+    if ((long long)kv_heads * z.cap_blocks * kTileTokens > 0x7FFFFFFF || (long long)n_q * heads > 0x7FFFFFFF || z.total > kMostWorkspace) return 0;
     return z.total;
 }
 

@@ -32,7 +32,7 @@ OWN = {
                (dict(k=16 * M), OVERLAP), (dict(v=32 * M + 16), OVERLAP), (dict(v_pages=16 * M), OVERLAP), (dict(n_new=0), OK), (dict(n_seqs=0), OK)],
     "read": [(dict(dst_dtype=-1), DTYPE), (dict(n_out=-1), SHAPE), (dict(n_seqs=4097), SHAPE), (dict(token_stride=64), SHAPE), (dict(token_stride=0), SHAPE), (dict(head_stride=63), SHAPE),
              (dict(token_stride=64, head_stride=600), SHAPE), (dict(k=None), NULL), (dict(d_first=None), NULL), (dict(d_out_start=None), NULL), (dict(k=64 * M + 2), ALIGN),
-             (dict(k=16 * M + 64), OVERLAP), (dict(n_out=0), OK)],
+             (dict(k=16 * M + 64), OVERLAP), (dict(k=65 * M), OVERLAP), (dict(n_out=0), OK)],
     "fork": [(dict(n_children=-1), SHAPE), (dict(n_children=4097), SHAPE), (dict(table_out_stride=0), SHAPE), (dict(d_lengths=None), NULL), (dict(d_parent=None), NULL),
              (dict(table_out=None), NULL), (dict(d_lengths_out=None), NULL), (dict(table_out=50 * M + 16), OVERLAP), (dict(d_lengths_out=51 * M + 4), OVERLAP), (dict(n_children=0), OK)],
     "compact": [(dict(n_seqs=4097), SHAPE), (dict(d_lengths=None), NULL), (dict(d_n_live=None), NULL), (dict(d_free_pages=None), NULL), (dict(workspace=None), WORKSPACE),
@@ -62,3 +62,10 @@ def test_attention_workspace_bytes():
     size = H.hif8_cache_attention_workspace_bytes
     assert size(4, 4, 1, 1000, 8, 2, 128) > 33000 and size(4, 4, 1, 1000, 8, 3, 128) == 0 and size(4, 4, 1, 1000, 8, 2, 100) == 0 and size(-1, 4, 1, 1000, 8, 2, 128) == 0
     assert size(4, 4, 1, 1000, 8, 2, 128) % 256 == 0
+
+
+def test_attention_workspace_stays_within_a_device():
+    size = H.hif8_cache_attention_workspace_bytes
+    assert size(2048, 1 << 20, 1 << 20, 1 << 30, 64, 1, 128) < (16 << 30) + (1 << 28)
+    assert size(64, 1024, 16, 131072, 64, 8, 128) < 1 << 28     # 34 GB of tiles: not asked for
+    assert size(4, 4096, 1024, 16384, 32, 8, 128) > 4 * 16384 * 8 * 128 * 4

@@ -304,6 +304,67 @@ def test_wrong_bounds_and_starts_stay_inside():
         assert H.hif8_last_device_status() == 0 and (out[0] == 5.0).all() and (out[n + 1] == 5.0).all()
 
 
+def test_wrong_starts_of_chunks_stay_inside():
+    c, q = make([200, 141, 300], [40, 20, 60], 4, 1, 16, 64, BF16)
+    n = 120
+    for longest in (300, 90):  # the second: lengths beyond what the host was told
+        size = H.hif8_cache_attention_workspace_bytes(3, n, 60, longest, 4, 1, 64)
+        ws = torch.full((size + 256,), 0xA5, dtype=torch.uint8, device="cuda")
+        for start in ([0, 70, 30, 120], [-5, 3, 50, 10 ** 9], [120, 120, 120, 120], [0, 120, 0, 120], [119, 0, 3, 120]):
+            out = torch.full((n + 2, 4, 64), 5.0, dtype=torch.bfloat16, device="cuda")
+            lse = torch.full((n + 2, 4), 5.0, device="cuda")
+            H.hif8_cache_attention(q, BF16, 256, 64, torch.tensor(start, dtype=torch.int32, device="cuda"), c.d_lengths, 3, n, 60, longest, *c.args(), 4, 0.1, 1, 0, out[1:], 256, 64,
+                                   lse[1:], ws, size)
+            assert H.hif8_last_device_status() == 0 and (out[0] == 5.0).all() and (out[n + 1] == 5.0).all() and (lse[0] == 5.0).all() and (lse[n + 1] == 5.0).all()
+            assert (ws[size:] == 0xA5).all()
+
+
+@pytest.mark.parametrize("counts", [[1, 1], [30, 40]])
+@pytest.mark.parametrize("causal", [0, 1])
+def test_the_largest_windows_are_none(counts, causal):
+    c, q = make([20, 141], counts, 4, 2, 16, 64, BF16)
+    want = attend(c, q, counts, 4, causal)
+    for window in (2 ** 31 - 1, 2 ** 30, 200):
+        got = attend(c, q, counts, 4, causal, window)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("counts", [[1], [3], [40]])
+def test_a_pool_beyond_four_gigabytes(counts):
+    """The same sequence in a small pool and at the end of one of more than 2^32 bytes."""
+    c, q = make([300], counts, 8, 4, 128, 256, BF16)
+    want = attend(c, q, counts, 8)
+    n_pages = (1 << 32) // (4 * 128 * 256) + 8
+    big = {}
+    for name in ("k", "v", "k_exp", "v_exp"):
+        big[name] = torch.zeros((n_pages,) + c.d[name].shape[1:], dtype=c.d[name].dtype, device="cuda")
+        big[name][-c.shape[0]:] = c.d[name][:c.shape[0]]
+    c.d, c.d_table, c.shape = big, torch.where(c.d_table >= 0, c.d_table + (n_pages - c.shape[0]), -1).int(), (n_pages,) + c.shape[1:]
+    got = attend(c, q, counts, 8)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_two_calls_at_once_on_two_streams():
+    """Each with a workspace of its own; single tokens, and chunks."""
+    for counts in ([1, 1, 1], [50, 3, 90]):
+        c, q = make([700, 3000, 99], counts, 8, 2, 32, 128, BF16)
+        want = attend(c, q, counts, 8)
+        torch.cuda.synchronize()
+        streams, got = [torch.cuda.Stream() for _ in range(2)], [[], []]
+        size = H.hif8_cache_attention_workspace_bytes(3, len(q), max(counts), 3000, 8, 2, 128)
+        ws, st = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(2)], starts(counts)
+        torch.cuda.synchronize()
+        for _ in range(20):
+            for i, stream in enumerate(streams):
+                out, lse = torch.empty_like(q), torch.empty(len(q), 8, device="cuda")
+                H.hif8_cache_attention(q, BF16, q.stride(0), q.stride(1), st, c.d_lengths, 3, len(q), max(counts), 3000, *c.args(), 8, 128 ** -0.5, 1, 0, out, q.stride(0), q.stride(1), lse,
+                                       ws[i], size, stream)
+                got[i].append((out, lse))
+        torch.cuda.synchronize()
+        for out, lse in got[0] + got[1]:
+            assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
 def test_many_sequences_and_shared_pages():
     lengths = [(i * 37) % 150 for i in range(700)]
     lengths[0] = lengths[-1] = 130
@@ -319,23 +380,25 @@ def test_long_sequences_are_shared_out_and_reproducible():
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
 
 
-def test_another_stream_and_a_captured_graph():
-    c, q = make([500, 77], [1, 4], 8, 2, 32, 128, BF16)
-    want, norm = attend(c, q, [1, 4], 8)
+@pytest.mark.parametrize("counts", [[1, 4], [20, 77]])
+def test_another_stream_and_a_captured_graph(counts):
+    c, q = make([500, 77], counts, 8, 2, 32, 128, BF16)
+    n, most = sum(counts), max(counts)
+    want, norm = attend(c, q, counts, 8)
     torch.cuda.synchronize()
     side = torch.cuda.Stream()
     with torch.cuda.stream(side):
-        out, lse = attend(c, q, [1, 4], 8, stream=side)
+        out, lse = attend(c, q, counts, 8, stream=side)
     side.synchronize()
     assert torch.equal(out, want) and torch.equal(lse, norm)
-    size = H.hif8_cache_attention_workspace_bytes(2, 5, 4, 500, 8, 2, 128)
-    ws, st = torch.empty(size, dtype=torch.uint8, device="cuda"), starts([1, 4])
+    size = H.hif8_cache_attention_workspace_bytes(2, n, most, 500, 8, 2, 128)
+    ws, st = torch.empty(size, dtype=torch.uint8, device="cuda"), starts(counts)
     out.zero_()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
-        H.hif8_cache_attention(q, BF16, q.stride(0), q.stride(1), st, c.d_lengths, 2, 5, 4, 500, *c.args(), 8, 128 ** -0.5, 1, 0, out, q.stride(0), q.stride(1), lse, ws, size)
+        H.hif8_cache_attention(q, BF16, q.stride(0), q.stride(1), st, c.d_lengths, 2, n, most, 500, *c.args(), 8, 128 ** -0.5, 1, 0, out, q.stride(0), q.stride(1), lse, ws, size)
     q.neg_()
-    want = attend(c, q, [1, 4], 8)[0]
+    want = attend(c, q, counts, 8)[0]
     for _ in range(2):
         graph.replay()
     torch.cuda.synchronize()
