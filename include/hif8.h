@@ -425,7 +425,8 @@ int hif8_cache_append(const void* k, const void* v, int src_dtype, int64_t token
 
 /*
  * Tokens out of the cache: those of sequence s from position d_first[s] on, d_out_start[s + 1] - d_out_start[s] of them, as
- * value(code) * 2^-e rounded to nearest-even in dst_dtype, to k, v [n_out tokens][kv_heads][head_dim] (rows must not share elements: HIF8_ERR_SHAPE).
+ * value(code) * 2^-e rounded to nearest-even in dst_dtype, to k, v [n_out tokens][kv_heads][head_dim] (rows must not share elements: HIF8_ERR_SHAPE, those of
+ * k with those of v: HIF8_ERR_OVERLAP).
  */
 int hif8_cache_read(const uint8_t* k_pages, const uint8_t* v_pages, const int* k_exp, const int* v_exp, int n_pages, int kv_heads,
                     int page_tokens, int head_dim, const int* page_table, int64_t table_stride, const int* d_first, const int* d_out_start,
@@ -439,7 +440,8 @@ int hif8_cache_read(const uint8_t* k_pages, const uint8_t* v_pages, const int* k
  * positions: query i at p_i = d_lengths[s] - n + i.  It looks at the cached tokens j
  *   causal != 0: j <= p_i;  causal == 0: all;   window > 0: only j > p_i - window (window == 0: no such limit).
  * A query that sees no token (an empty cache, a position below 0, scores that are all -Inf) gives zeros and lse = -Inf.  Tokens that a query does not see never
- * reach its result, Inf and NaN among them, nor do slots behind a sequence's length.  Inf and NaN that it does see propagate as in IEEE arithmetic.
+ * reach its result, Inf and NaN among them, nor do slots behind a sequence's length.  Inf and NaN that it does see propagate as in IEEE arithmetic (and a
+ * weight below the range of FP16 counts as zero).
  * Products of codes are exact and sums are FP32; the weights of the softmax are rounded to FP16.  softmax_scale: positive and finite (HIF8_ERR_SCALE_RANGE).
  * The pool must have a page and less than 2^31 rows (n_pages * kv_heads * page_tokens), and n_q * heads / kv_heads must stay below 2^30 (HIF8_ERR_SHAPE).
  * max_q and max_length: upper bounds of a sequence's queries and tokens, known to the host.  They have to hold (where they do not, results may be wrong, but no

@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(const ReadParams p
         }
         if (!pc.count) continue;
         const int slot = pc.pos & ((1 << p.c.shift) - 1), n_vec = pc.count * row_vecs;
-        const int e = page < 0 ? 0 : clamp_exp((is_v ? p.c.v_exp : p.c.k_exp)[(long long)page * p.c.heads + head]);
+        const int e = page < 0 ? 0 : clamp_cache_exp((is_v ? p.c.v_exp : p.c.k_exp)[(long long)page * p.c.heads + head]);
         const float back = pow2f(-e);
         const uint32_t back2 = bf16x2_of_pow2(back);
         const uint8_t* src = (is_v ? p.c.v : p.c.k) + (page < 0 ? 0ll : p.c.block_at(page, head) + (long long)slot * p.c.dim);
@@ -500,6 +500,24 @@ static bool aligned_rows(const void* a, const void* b, int64_t token_stride, int
 {
     return !((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) & 15u) && !((token_stride * (int64_t)item) & 15) && !((head_stride * (int64_t)item) & 15);
 }
+// Whether a row of one result and a row of another of the same strides, `delta` elements apart, share an element (slices of one tensor do not): for each
+// distance in heads the tokens' distance that comes closest.
+static bool rows_meet(int64_t delta, int64_t token_stride, int64_t head_stride, int n, int heads, int dim)
+{
+    for (int h = 1 - heads; h < heads; h++) {
+        const int64_t rest = delta + h * head_stride;
+        int64_t t = token_stride ? -rest / token_stride : 0;
+        for (int64_t x = t - 1; x <= t + 1; x++) {
+            const int64_t y = x < 1 - n ? 1 - n : x > n - 1 ? n - 1 : x, gap = rest + y * token_stride;
+            if (gap > -dim && gap < dim) return true;
+        }
+    }
+    return false;
+}
+static bool ints_aligned(const void* a, const void* b = nullptr, const void* c = nullptr, const void* d = nullptr)
+{
+    return !((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b) | reinterpret_cast<uintptr_t>(c) | reinterpret_cast<uintptr_t>(d)) & 3u);
+}
 static int finish_launch(int n)
 {
     g_launches.fetch_add((uint64_t)n, std::memory_order_relaxed);
@@ -520,7 +538,7 @@ extern "C" int hif8_cache_append(const void* k, const void* v, int src_dtype, in
     if (n_seqs == 0 || n_new == 0) return HIF8_OK;
     if (!k || !v || !d_new_start || !d_lengths) return HIF8_ERR_NULL;
     const size_t item = dtype_bytes(src_dtype);
-    if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & (item - 1)) return HIF8_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & (item - 1) || !ints_aligned(d_new_start, d_lengths)) return HIF8_ERR_ALIGN;
     const size_t src_bytes = ((size_t)(n_new - 1) * (size_t)token_stride + (size_t)(kv_heads - 1) * (size_t)head_stride + (size_t)head_dim) * item;
     const size_t pool = (size_t)n_pages * (size_t)p.c.page_bytes();
     for (const void* s : {k, v})
@@ -558,10 +576,10 @@ extern "C" int hif8_cache_read(const uint8_t* k_pages, const uint8_t* v_pages, c
     const int64_t n_inner = token_stride < head_stride ? n_out : kv_heads, n_outer = token_stride < head_stride ? kv_heads : n_out;
     if ((n_inner > 1 && inner < head_dim) || (n_outer > 1 && outer < (n_inner - 1) * inner + head_dim)) return HIF8_ERR_SHAPE;
     const size_t item = dtype_bytes(dst_dtype);
-    if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & (item - 1)) return HIF8_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & (item - 1) || !ints_aligned(d_first, d_out_start)) return HIF8_ERR_ALIGN;
     const size_t dst_bytes = ((size_t)(n_out - 1) * (size_t)token_stride + (size_t)(kv_heads - 1) * (size_t)head_stride + (size_t)head_dim) * item;
     const size_t pool = (size_t)n_pages * (size_t)p.c.page_bytes();
-    if (k == v) return HIF8_ERR_OVERLAP;  // (k and v may be slices of one tensor otherwise)
+    if (rows_meet(((intptr_t)v - (intptr_t)k) / (intptr_t)item, token_stride, head_stride, n_out, kv_heads, head_dim)) return HIF8_ERR_OVERLAP;
     for (const void* d : {(const void*)k, (const void*)v})
         for (const void* s : {(const void*)k_pages, (const void*)v_pages})
             if (ranges_overlap(s, pool, d, dst_bytes)) return HIF8_ERR_OVERLAP;
@@ -588,6 +606,7 @@ extern "C" int hif8_cache_fork(uint8_t* k_pages, uint8_t* v_pages, int* k_exp, i
     if (int rc = check_cache(k_pages, v_pages, k_exp, v_exp, n_pages, kv_heads, page_tokens, head_dim, page_table, table_stride, &p.c)) return rc;
     if (n_children == 0) return HIF8_OK;
     if ((n_seqs && !d_lengths) || !d_parent || !table_out || !d_lengths_out) return HIF8_ERR_NULL;
+    if (!ints_aligned(d_lengths, d_parent, d_new_page, table_out) || !ints_aligned(d_lengths_out)) return HIF8_ERR_ALIGN;
     const size_t in_bytes = (size_t)n_seqs * (size_t)table_stride * 4, out_bytes = (size_t)n_children * (size_t)table_out_stride * 4;
     if (ranges_overlap(page_table, in_bytes, table_out, out_bytes) || ranges_overlap(d_lengths, (size_t)n_seqs * 4, d_lengths_out, (size_t)n_children * 4)) return HIF8_ERR_OVERLAP;
     int sms; if (int rc = checked_device(&sms)) return rc;
@@ -611,6 +630,7 @@ extern "C" int hif8_cache_compact(uint8_t* k_pages, uint8_t* v_pages, int* k_exp
     CompactParams p;
     if (int rc = check_cache(k_pages, v_pages, k_exp, v_exp, n_pages, kv_heads, page_tokens, head_dim, page_table, table_stride, &p.c)) return rc;
     if ((n_seqs && !d_lengths) || !d_n_live || (n_pages && !d_free_pages)) return HIF8_ERR_NULL;
+    if (!ints_aligned(d_lengths, d_n_live, d_free_pages)) return HIF8_ERR_ALIGN;
     if (!workspace || workspace_bytes < hif8_cache_compact_workspace_bytes(n_pages) || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return HIF8_ERR_WORKSPACE;
     int sms; if (int rc = checked_device(&sms)) return rc;
     p.table = page_table; p.lengths = d_lengths; p.n_seqs = n_seqs; p.move = move != 0; p.parts = copy_parts(p.c);

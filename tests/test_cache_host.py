@@ -25,18 +25,24 @@ OWN = {
                   (dict(softmax_scale=0.0), RANGE), (dict(softmax_scale=-1.0), RANGE), (dict(softmax_scale=float("nan")), RANGE), (dict(softmax_scale=float("inf")), RANGE),
                   (dict(q=None), NULL), (dict(out=None), NULL), (dict(d_q_start=None), NULL), (dict(d_lengths=None), NULL), (dict(q=64 * M + 1), ALIGN), (dict(lse=67 * M + 2), ALIGN),
                   (dict(out=64 * M + 64), OVERLAP), (dict(out=16 * M), OVERLAP), (dict(out=32 * M), OVERLAP), (dict(workspace=None), WORKSPACE),
-                  (dict(workspace=68 * M + 16), WORKSPACE), (dict(workspace_bytes=1 << 15), WORKSPACE), (dict(n_q=0), OK), (dict(n_seqs=0), OK)],
+                  (dict(workspace=68 * M + 16), WORKSPACE), (dict(workspace_bytes=1 << 15), WORKSPACE), (dict(d_q_start=51 * M + 2), ALIGN), (dict(n_seqs=2049), SHAPE), (dict(n_q=0), OK), (dict(n_seqs=0), OK)],
     "append": [(dict(src_dtype=3), DTYPE), (dict(rnd=H.RND_SR), ROUND), (dict(rnd=7), ROUND), (dict(flags=4), FLAGS), (dict(target_exp=16), RANGE), (dict(target_exp=-23), RANGE),
                (dict(n_seqs=4097), SHAPE), (dict(n_new=-1), SHAPE), (dict(token_stride=-128), SHAPE), (dict(head_stride=-1), SHAPE), (dict(k=None), NULL), (dict(v=None), NULL),
                (dict(d_new_start=None), NULL), (dict(d_lengths=None), NULL), (dict(k=64 * M + 1), ALIGN), (dict(src_dtype=H.F32, v=65 * M + 2), ALIGN),
-               (dict(k=16 * M), OVERLAP), (dict(v=32 * M + 16), OVERLAP), (dict(v_pages=16 * M), OVERLAP), (dict(n_new=0), OK), (dict(n_seqs=0), OK)],
+               (dict(k=16 * M), OVERLAP), (dict(v=32 * M + 16), OVERLAP), (dict(v_pages=16 * M), OVERLAP), (dict(n_new=0), OK), (dict(n_seqs=0), OK),
+               (dict(d_new_start=51 * M + 2), ALIGN), (dict(d_lengths=52 * M + 1), ALIGN), (dict(n_seqs=2049), SHAPE)],
     "read": [(dict(dst_dtype=-1), DTYPE), (dict(n_out=-1), SHAPE), (dict(n_seqs=4097), SHAPE), (dict(token_stride=64), SHAPE), (dict(token_stride=0), SHAPE), (dict(head_stride=63), SHAPE),
              (dict(token_stride=64, head_stride=600), SHAPE), (dict(k=None), NULL), (dict(d_first=None), NULL), (dict(d_out_start=None), NULL), (dict(k=64 * M + 2), ALIGN),
-             (dict(k=16 * M + 64), OVERLAP), (dict(k=65 * M), OVERLAP), (dict(n_out=0), OK)],
+             (dict(k=16 * M + 64), OVERLAP), (dict(k=65 * M), OVERLAP), (dict(n_out=0), OK),
+             (dict(v=64 * M + 4), OVERLAP), (dict(v=64 * M + 252), OVERLAP), (dict(v=64 * M + 256), OVERLAP), (dict(v=64 * M - 128 * 9 * 4), OVERLAP), (dict(v=64 * M + 64 * 19 * 4 + 252), OVERLAP),
+             (dict(token_stride=256, v=64 * M + 256), OVERLAP), (dict(token_stride=256, v=64 * M - 768), OVERLAP), (dict(token_stride=64, head_stride=700, v=64 * M + 4 * 700), OVERLAP),
+             (dict(d_first=51 * M + 1), ALIGN), (dict(d_out_start=52 * M + 2), ALIGN)],
     "fork": [(dict(n_children=-1), SHAPE), (dict(n_children=4097), SHAPE), (dict(table_out_stride=0), SHAPE), (dict(d_lengths=None), NULL), (dict(d_parent=None), NULL),
-             (dict(table_out=None), NULL), (dict(d_lengths_out=None), NULL), (dict(table_out=50 * M + 16), OVERLAP), (dict(d_lengths_out=51 * M + 4), OVERLAP), (dict(n_children=0), OK)],
+             (dict(table_out=None), NULL), (dict(d_lengths_out=None), NULL), (dict(table_out=50 * M + 16), OVERLAP), (dict(d_lengths_out=51 * M + 4), OVERLAP), (dict(n_children=0), OK),
+             (dict(d_parent=52 * M + 2), ALIGN), (dict(d_new_page=53 * M + 2), ALIGN), (dict(table_out=54 * M + 1), ALIGN), (dict(d_lengths_out=55 * M + 2), ALIGN), (dict(n_children=2049), SHAPE)],
     "compact": [(dict(n_seqs=4097), SHAPE), (dict(d_lengths=None), NULL), (dict(d_n_live=None), NULL), (dict(d_free_pages=None), NULL), (dict(workspace=None), WORKSPACE),
-                (dict(workspace_bytes=255), WORKSPACE), (dict(workspace=54 * M + 16), WORKSPACE)],
+                (dict(workspace_bytes=255), WORKSPACE), (dict(workspace=54 * M + 16), WORKSPACE),
+                (dict(d_lengths=51 * M + 2), ALIGN), (dict(d_n_live=52 * M + 2), ALIGN), (dict(d_free_pages=53 * M + 1), ALIGN)],
 }
 
 

@@ -75,6 +75,20 @@ def test_append_extreme_exponents_are_clamped():
     assert {48, -48, 0} <= set(c.h["k_exp"].ravel().tolist())
 
 
+def test_read_takes_exponents_within_the_limits():
+    c = Cache(4, 2, 16, 64, [60], [0], seed=1)
+    c.fill()
+    want = {}
+    for limit in (H.CACHE_EXP_MAX, 100):
+        for name in ("k_exp", "v_exp"):
+            c.h[name][:, 0], c.h[name][:, 1] = limit, -limit
+        c.upload()
+        k, v = torch.empty(60, 2, 64, device="cuda"), torch.empty(60, 2, 64, device="cuda")
+        H.hif8_cache_read(*c.args(), torch.zeros(1, dtype=torch.int32, device="cuda"), starts([60]), 1, 60, k, v, H.F32, 128, 64)
+        want[limit] = torch.stack([k, v])
+    assert torch.equal(want[100], want[H.CACHE_EXP_MAX]) and torch.isfinite(want[100]).all() and (want[100][:, :, 1].abs().amax() > 2.0 ** 40)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("layout", ["fused", "heads_first", "odd"])
 def test_append_and_read_strides(dtype, layout):
