@@ -654,59 +654,78 @@ __global__ void __launch_bounds__(kCombineThreads) cache_attention_combine_kerne
 }
 
 // Inf and NaN among the values of tokens that only some of a sequence's queries see: the rows that do see them get them here.  (Those that all queries
-// see took the ordinary way.)  A block looks through `slices` pieces of 16 elements of a key head's value rows, 256 pieces at a time, and lists what it finds; there
-// is hardly ever anything to do.
+// see took the ordinary way.)  A block looks through `slices` pieces of 16 elements of a key head's value rows, 256 pieces at a time, and keeps a bit for each token,
+// element and kind of what it finds; there is hardly ever anything to do, and if there is, a result takes a few words to look at, however much was found.  Without
+// a window only the first of a kind in an element counts (whoever sees a later one sees that as well): a cache full of NaN does not make the work quadratic.
 template <int DT>
 __global__ void __launch_bounds__(kThreads) cache_attention_specials_kernel(const AttentionParams p, int slices)
 {
-    __shared__ int2 s_found[kThreads * 16];  // token, element and code
-    __shared__ int s_count;
+    constexpr int kWords = kThreads;  // (16 slices by words of tokens: 128, and 256 where 16 slices leave half of each word)
+    __shared__ uint32_t s_found[3][kWords];  // Inf, -Inf, NaN: [elements][tokens / 32]
+    __shared__ uint32_t s_before[256];       // kinds that an element held in earlier rounds
     pdl_wait_prior_grid();
     pdl_launch_dependents();
     if (p.special_flag && !*p.special_flag) return;
     const int head = blockIdx.y, s = blockIdx.z;
     const SeqView v = seq_view(p, s);
     if (v.n_q < 2) return;
-    // tokens that the last query sees or the first, and not both: [a0, a1) and [b0, b1)
+    // tokens that the last query sees or the first, and not both: [a0, a1) and [b0, b1), number k being a0 + k, and b0 + k - n_a from n_a on
     const int hi0 = min(v.len, hi_of(p, v, 0)), hi1 = min(v.len, hi_of(p, v, v.n_q - 1)), lo0 = lo_of(p, v, 0), lo1 = lo_of(p, v, v.n_q - 1);
-    const int a0 = lo0, a1 = min(lo1, hi1), b0 = max(hi0, a1), b1 = hi1, n_a = max(0, a1 - a0);
-    const long long pieces = (long long)(n_a + max(0, b1 - b0)) * slices;
-    if (threadIdx.x == 0) s_count = 0;
+    const int a0 = lo0, a1 = min(lo1, hi1), b0 = max(hi0, a1), b1 = hi1, n_a = max(0, a1 - a0), n = n_a + max(0, b1 - b0);
+    const int step = kThreads / slices, words = (step + 31) / 32, width = 16 * slices;  // tokens at a time
+    for (int i = threadIdx.x; i < 3 * kWords; i += kThreads) s_found[i / kWords][i % kWords] = 0u;
+    s_before[threadIdx.x] = 0u;  // (kThreads == 256, the most elements)
     __syncthreads();
-    for (long long at = 0; at < pieces; at += kThreads) {
-        const long long i = at + threadIdx.x;
-        if (i < pieces) {
-            const int k = (int)(i / slices), d0 = ((int)blockIdx.x * slices + (int)(i - (long long)k * slices)) * 16, tok = k < n_a ? a0 + k : b0 + (k - n_a);
-            const int page = p.c.page_of(s, tok >> p.c.shift);
+    auto token = [&](int k) -> int { return k < n_a ? a0 + k : b0 + (k - n_a); };
+    for (int k0 = 0; k0 < n; k0 += step) {
+        const int kk = (int)threadIdx.x / slices, k = k0 + kk, d0 = ((int)threadIdx.x - kk * slices) * 16;
+        bool any = false;
+        if (k < n) {
+            const int tok = token(k), page = p.c.page_of(s, tok >> p.c.shift);
             uint4 w = make_uint4(0, 0, 0, 0);
-            if (page >= 0) w = __ldg(reinterpret_cast<const uint4*>(p.c.v + p.c.block_at(page, head) + (long long)(tok & ((1 << p.c.shift) - 1)) * p.c.dim + d0));
+            if (page >= 0)
+                w = __ldg(reinterpret_cast<const uint4*>(p.c.v + p.c.block_at(page, head) + (long long)(tok & ((1 << p.c.shift) - 1)) * p.c.dim + (int)blockIdx.x * width + d0));
             if (finite_codes(w.x) != w.x || finite_codes(w.y) != w.y || finite_codes(w.z) != w.z || finite_codes(w.w) != w.w)
                 for (int d = 0; d < 16; d++) {
                     const uint32_t c = ((d < 4 ? w.x : d < 8 ? w.y : d < 12 ? w.z : w.w) >> (8 * (d & 3))) & 0xFFu;
-                    if (c == 0x80u || (c & 0x7Fu) == 0x6Fu) s_found[atomicAdd(&s_count, 1)] = make_int2(tok, (d0 + d) << 8 | (int)c);
+                    const int kind = c == 0x6Fu ? 0 : c == 0xEFu ? 1 : 2;
+                    if ((c == 0x80u || (c & 0x7Fu) == 0x6Fu) && !(s_before[d0 + d] >> kind & 1u)) {
+                        atomicOr(&s_found[kind][(d0 + d) * words + (kk >> 5)], 1u << (kk & 31));
+                        any = true;
+                    }
                 }
+        }
+        if (!__syncthreads_or(any)) continue;
+        // rows of queries that see any of the round's tokens
+        const int tok0 = token(k0), tok1 = token(min(k0 + step, n) - 1), i0 = p.causal ? max(0, tok0 - v.pos(0)) : 0, i1 = p.window ? (int)min((long long)v.n_q, (long long)tok1 + p.window - v.pos(0)) : v.n_q;
+        const long long work = (long long)i1 * p.group * width;
+        for (long long x = (long long)i0 * p.group * width + threadIdx.x; x < work; x += kThreads) {
+            const int r = (int)(x / width), d = (int)(x - (long long)r * width), qi = r / p.group, h = head * p.group + r - qi * p.group;
+            const int hi = min(v.len, hi_of(p, v, qi)), lo = lo_of(p, v, qi);
+            // the numbers it sees, from this round's first: of [a0, a1), of [b0, b1)
+            const int from[2] = {max(lo - a0, 0) - k0, max(lo - b0 + n_a, n_a) - k0}, to[2] = {min(hi - a0, n_a) - k0, hi - b0 + n_a - k0};
+            uint32_t seen[3] = {0u, 0u, 0u};
+            for (int y = 0; y < words; y++) {
+                uint32_t mask = 0u;
+                for (int z = 0; z < 2; z++) {
+                    const int f = max(0, min(32, from[z] - 32 * y)), t = max(0, min(32, to[z] - 32 * y));
+                    if (f < t) mask |= (uint32_t)((1ull << t) - (1ull << f));
+                }
+                for (int z = 0; z < 3; z++) seen[z] |= s_found[z][d * words + y] & mask;
+            }
+            if (seen[0] | seen[1] | seen[2]) {
+                const float add = seen[2] || (seen[0] && seen[1]) ? __uint_as_float(0x7FC00000u) : seen[0] ? -kNegInf : kNegInf;
+                unsigned short* out = reinterpret_cast<unsigned short*>(p.out) + (long long)(v.first + qi) * p.out_token + (long long)h * p.out_head + (int)blockIdx.x * width + d;
+                *out = (unsigned short)to_bits<DT>(q_value<DT>(*out) + add);
+            }
         }
         __syncthreads();
-        const int found = s_count;
-        __syncthreads();  // (everyone has read it before the next pieces are counted)
-        if (found) {
-            const int width = 16 * slices;
-            const long long work = (long long)v.n_q * p.group * width;
-            for (long long x = threadIdx.x; x < work; x += kThreads) {
-                const int r = (int)(x / width), d = (int)blockIdx.x * width + (int)(x - (long long)r * width), qi = r / p.group, h = head * p.group + r - qi * p.group;
-                const int hi = min(v.len, hi_of(p, v, qi)), lo = lo_of(p, v, qi);
-                float add = 0.f;  // (Inf and NaN: the order of the sum does not matter)
-                for (int j = 0; j < found; j++)
-                    if (s_found[j].y >> 8 == d && s_found[j].x >= lo && s_found[j].x < hi) add += __uint_as_float(decode_bits_f32((uint32_t)s_found[j].y & 0xFFu));
-                if (add != 0.f) {
-                    unsigned short* out = reinterpret_cast<unsigned short*>(p.out) + (long long)(v.first + qi) * p.out_token + (long long)h * p.out_head + d;
-                    *out = (unsigned short)to_bits<DT>(q_value<DT>(*out) + add);
-                }
-            }
-            __syncthreads();
-            if (threadIdx.x == 0) s_count = 0;
-            __syncthreads();
+        for (int i = threadIdx.x; i < 3 * width * words; i += kThreads) {
+            const int z = i / (width * words), j = i - z * width * words;
+            if (s_found[z][j] && !p.window) atomicOr(&s_before[j / words], 1u << z);
+            s_found[z][j] = 0u;
         }
+        __syncthreads();
     }
 }
 

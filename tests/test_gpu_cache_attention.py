@@ -231,6 +231,27 @@ def test_a_later_query_s_values_are_all_special(small):
     assert torch.equal(out[:50], clean[:50]) and not torch.isfinite(out[50:]).any()
 
 
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("window", [0, 90, 7])
+@pytest.mark.parametrize("small", [False, True])
+def test_scattered_special_values(dim, window, small):
+    """Inf, -Inf and NaN, of several kinds in some elements, all over the tokens that only some queries see; and nearly everywhere."""
+    counts, lengths = [500, 70], [600, 71]
+    c, q = make(lengths, counts, 4, 2, 32, dim, BF16)
+    c.fill(0)
+    rng = np.random.default_rng(dim + window)
+    for s, n in enumerate(lengths):
+        for i in range(60):
+            t = int(rng.integers(0, n))
+            c.h["v"][c.table[s, t // 32], i % 2, t % 32, int(rng.integers(0, dim)) // 5 * 5] = rng.choice([0x80, 0x6F, 0xEF])
+    c.upload()
+    close(c, q, counts, 4, 1, window, small=small, scale=0.02)
+    c.h["v"][:] = 0x80
+    c.upload()
+    out, _ = attend(c, q, counts, 4, 1, window, small=small)
+    assert torch.isnan(out).all()
+
+
 @pytest.mark.parametrize("counts", [[1, 2], [1, 40]])
 def test_scores_and_spreads_at_the_ends(counts):
     """Large scores (one token takes all), queries and blocks of very different magnitudes, exponents beyond the limit."""
