@@ -476,3 +476,83 @@ def test_serving_steps_together():
         c.upload()
         want, norm = attend(c, q[row:row + 1], [1], heads, scale=0.125)
         assert torch.equal(out[row:row + 1], want) and torch.equal(lse[row:row + 1], norm)
+
+
+@pytest.mark.parametrize("counts", [1, 9])
+def test_as_many_sequences_as_a_call_takes(counts):
+    """2048 of them: single tokens, and with 16 heads to a key head as chunks."""
+    lengths = [(i * 29) % 47 for i in range(H.CACHE_MAX_SEQS)]
+    group = 1 if counts == 1 else 16
+    q_counts = [counts if i % 3 else 0 for i in range(H.CACHE_MAX_SEQS)]
+    c, q = make(lengths, q_counts, group, 1, 16, 64, BF16)
+    out, lse = attend(c, q, q_counts, group)
+    pick = list(range(0, 40)) + list(range(H.CACHE_MAX_SEQS - 40, H.CACHE_MAX_SEQS))
+    at = np.concatenate([[0], np.cumsum(q_counts)])
+    rows = torch.from_numpy(np.concatenate([np.arange(at[s], at[s + 1]) for s in pick])).cuda()
+    few = Cache(1, 1, 16, 64, [0], [0], seed=0)
+    few.dtype, few.shape, few.h, few.lengths, few.table = BF16, c.shape, c.h, [lengths[s] for s in pick], c.table[pick]
+    want, norm, tol, tol_lse = reference(few, q[rows], [q_counts[s] for s in pick], group, 64 ** -0.5, 1, 0)
+    assert ((out[rows].double() - want).abs() <= tol).all()
+    same = torch.isfinite(norm)
+    assert torch.equal(same, torch.isfinite(lse[rows])) and ((lse[rows].double() - norm).abs()[same] <= tol_lse[same]).all()
+
+
+@pytest.mark.parametrize("m", [1, 40])
+def test_a_captured_step_follows_its_inputs(m):
+    """Append, attention, fork, append for the children and compaction in one graph, replayed with other tokens, lengths and parents: what the calls one by one give."""
+    heads, kv, page, dim, width, n_pages = 8, 2, 32, 128, 8, 40
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    size = H.hif8_cache_attention_workspace_bytes(2, 2 * m, m, width * page, heads, kv, dim)
+    compact_size = H.hif8_cache_compact_workspace_bytes(n_pages)
+
+    def fresh():
+        s = {name: torch.full(shape, 5, dtype=t, device="cuda") for name, shape, t in (
+            ("q", (2 * m, heads, dim), torch.bfloat16), ("k", (2 * m, kv, dim), torch.bfloat16), ("v", (2 * m, kv, dim), torch.bfloat16), ("out", (2 * m, heads, dim), torch.bfloat16),
+            ("lse", (2 * m, heads), torch.float32), ("kp", (n_pages, kv, page, dim), torch.uint8), ("vp", (n_pages, kv, page, dim), torch.uint8), ("ke", (n_pages, kv), torch.int32),
+            ("ve", (n_pages, kv), torch.int32), ("table", (2, width), torch.int32), ("lengths", (2,), torch.int32), ("after", (2,), torch.int32), ("parent", (3,), torch.int32),
+            ("new", (3,), torch.int32), ("children", (3, width), torch.int32), ("child_lengths", (3,), torch.int32), ("live", (1,), torch.int32), ("free", (n_pages,), torch.int32),
+            ("ws", (size,), torch.uint8), ("ws2", (compact_size,), torch.uint8))}
+        s["start"], s["one"] = ints([0, m, 2 * m]), ints([0, 1, 1, 2])
+        return s
+
+    def fill(s, seed):
+        g = torch.Generator().manual_seed(seed)
+        for name in ("q", "k", "v"):
+            s[name].copy_(torch.randn(s[name].shape, generator=g))
+        for name in ("kp", "vp"):
+            s[name].copy_(torch.randint(0, 0x60, s[name].shape, generator=g))
+        lengths = [int(x) for x in torch.randint(0, width * page - m - 1, (2,), generator=g)]
+        s["ke"].zero_(), s["ve"].zero_()
+        s["table"].copy_(torch.from_numpy(np.random.default_rng(seed).permutation(n_pages)[:2 * width].reshape(2, width)))
+        s["lengths"].copy_(ints(lengths)), s["after"].copy_(ints([x + m for x in lengths]))
+        s["parent"].copy_(ints([seed % 2, 1, 0]))
+        s["new"].copy_(torch.from_numpy(np.setdiff1d(np.arange(n_pages), s["table"].cpu().numpy())[:3]))
+
+    def step(s):
+        pool = lambda t: (s["kp"], s["vp"], s["ke"], s["ve"], n_pages, kv, page, dim, t, width)  # noqa: E731
+        H.hif8_cache_append(s["k"], s["v"], BF16, kv * dim, dim, s["start"], s["lengths"], 2, 2 * m, *pool(s["table"]))
+        H.hif8_cache_attention(s["q"], BF16, heads * dim, dim, s["start"], s["after"], 2, 2 * m, m, width * page, *pool(s["table"]), heads, 0.1, 1, 50, s["out"], heads * dim, dim, s["lse"],
+                               s["ws"], size)
+        H.hif8_cache_fork(*pool(s["table"]), s["after"], 2, s["parent"], s["new"], 3, s["children"], width, s["child_lengths"])
+        H.hif8_cache_append(s["k"], s["v"], BF16, kv * dim, dim, s["one"], s["child_lengths"], 3, 2 * m, *pool(s["children"]))
+        H.hif8_cache_compact(*pool(s["children"]), s["child_lengths"], 3, 1, s["live"], s["free"], s["ws2"], compact_size)
+
+    captured, plain = fresh(), fresh()
+    fill(captured, 1)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(captured)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(captured)
+    for seed in (2, 3, 4):
+        fill(captured, seed), fill(plain, seed)
+        graph.replay()
+        step(plain)
+        torch.cuda.synchronize()
+        for name in captured:
+            if name not in ("ws", "ws2"):
+                assert torch.equal(captured[name], plain[name]), (seed, name)
+        assert int(captured["live"]) > 0
