@@ -42,10 +42,12 @@ struct PrefillParams {
     float4* meta;          // [heads][cap_blocks * 8]: of 16 tokens: 2^-e_k, -e_v (-Inf: no page), 2^e_v
     int* block_at;         // [n_seqs + 1] first 128-token block of each sequence
     long long* tiles_at;   // [pairs + 1] tiles in front of each pair of row tiles (of one head)
+    int* units_at;         // [pairs] those of the pairs in front that have tiles
     int* pair_seq;         // [pairs]
-    int4* cut;             // [blocks] two of each: first tile, tiles, key head and first row of the unit that the block's first segment lies in; first query, rows
+    long long* bound;      // [blocks + 1] first tile of each block: heads x tiles_at
+    int4* cut;             // [blocks] two of each, of the unit that the block's first tile lies in: tiles in front of that one, tiles, key head, first row; first query, rows, pair
     int* specials;         // set when some token that only some queries see holds Inf or NaN in V
-    int cap_blocks, pairs;
+    int cap_blocks, pairs, blocks;
     long long rows;        // n_q * group
     int unit_rows;         // query rows of a unit
 };
@@ -80,6 +82,9 @@ __device__ __forceinline__ PairView pair_view(const PrefillParams& p, int seq, l
 // Plan
 // ---------------------------------------------------------------------------------------------------------
 constexpr int kPlanThreads = 1024;
+// What is dealt out evenly: two for a tile, three for a unit (its queries, its results, and tiles that are masked; heads of 64: 3600 cycles a tile, 4900 a unit.  By tiles alone blocks
+// of 12 prompts of up to 2047 tokens with a window of 700 had 5 to 12 units and took 128 to 162 thousand cycles).
+constexpr int kTileCost = 2, kUnitCost = 3;
 __device__ __forceinline__ long long plan_prefix(long long v, long long* total, long long* s_warp)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -106,6 +111,8 @@ __device__ __forceinline__ long long plan_prefix(long long v, long long* total, 
 __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const PrefillParams p)
 {
     __shared__ long long s_warp[32];
+    __shared__ long long s_cost[kPlanThreads];  // in front of each pair, and of each: tiles, first row, first query of its sequence, rows
+    __shared__ int4 s_info[kPlanThreads];
     pdl_wait_prior_grid();
     pdl_launch_dependents();
     if (threadIdx.x == 0) { *p.a.status = 0; *p.specials = 0; }
@@ -123,10 +130,12 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const PrefillP
         carry += total;
     }
     if (threadIdx.x == 0) p.block_at[p.a.n_seqs] = (int)min(carry, (long long)p.cap_blocks);
+    long long carry_units = 0;
     carry = 0;
     for (int x0 = 0; x0 < p.pairs; x0 += kPlanThreads) {
         const int x = x0 + threadIdx.x;
         long long n = 0;
+        int4 info = make_int4(0, 0, 0, 0);
         if (x < p.pairs) {
             int s = 0;
             for (int k = p.a.n_seqs; k > 1;) {
@@ -135,13 +144,51 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const PrefillP
                 else k = half;
             }
             p.pair_seq[x] = s;
-            n = pair_view(p, s, x).tiles;
+            const PairView u = pair_view(p, s, x);
+            n = u.tiles;
+            info = make_int4(u.tiles, u.r0, u.v.first, u.n_rows);
         }
         const long long before = carry + plan_prefix(n, &total, s_warp);
         if (x < p.pairs) p.tiles_at[x] = before;
         carry += total;
+        const long long units = carry_units + plan_prefix(n > 0, &total, s_warp);
+        if (x < p.pairs) p.units_at[x] = (int)units;
+        if (x < kPlanThreads) { s_cost[x] = kTileCost * before + kUnitCost * units; s_info[x] = info; }
+        carry_units += total;
     }
     if (threadIdx.x == 0) p.tiles_at[p.pairs] = carry;
+    __syncthreads();
+    // Where each block begins.  (Few pairs, as small calls have them, are looked for in shared memory.)
+    const bool here = p.pairs <= kPlanThreads;
+    const long long cost = kTileCost * carry + kUnitCost * carry_units;  // of a head
+    for (int b = threadIdx.x; b <= p.blocks; b += kPlanThreads) {
+        if (b == p.blocks || !carry) { p.bound[b] = carry * p.a.c.heads; continue; }
+        const long long at = share_of(cost * p.a.c.heads, b, p.blocks);
+        const int head = (int)(at / cost);
+        const long long off = at - head * cost;
+        int a = 0;  // the last pair that begins at or before that (empty ones share their start with the next)
+        for (int k = p.pairs; k > 1;) {
+            const int half = k >> 1;
+            if ((here ? s_cost[a + half] : kTileCost * p.tiles_at[a + half] + kUnitCost * p.units_at[a + half]) <= off) { a += half; k -= half; }
+            else k = half;
+        }
+        int4 of = s_info[here ? a : 0];
+        if (!here) {
+            const PairView u = pair_view(p, p.pair_seq[a], a);
+            of = make_int4(u.tiles, u.r0, u.v.first, u.n_rows);
+        }
+        const int tiles = of.x;
+        const long long tiles_at = p.tiles_at[a], in = off - (here ? s_cost[a] : kTileCost * tiles_at + kUnitCost * p.units_at[a]) - kUnitCost;
+        int c = in <= 0 ? 0 : (int)min((long long)tiles, (in + kTileCost / 2) / kTileCost);
+        if (cost * p.a.c.heads >= 4ll * kTileCost * p.blocks) {  // a tile alone is not worth a segment
+            if (c == 1) c = 0;
+            else if (c && c == tiles - 1) c = tiles;
+        }
+        p.bound[b] = head * carry + tiles_at + c;
+        const bool next = c == tiles;  // it begins with the next unit, whichever that is
+        p.cut[2 * b] = make_int4(next ? 0 : c, tiles, head, of.y);
+        p.cut[2 * b + 1] = make_int4(of.z, of.w, next ? -1 : a, 0);
+    }
 }
 
 // ---------------------------------------------------------------------------------------------------------
@@ -310,13 +357,16 @@ template <int D>
 struct PrefillSmem {
     static constexpr int kStages = TileShape<D>::kStages, kTiles = TileShape<D>::kTiles;
     static constexpr int kQBufs = D == 64 ? 2 : 1;  // (short units, as windows and short prompts have them, wait for their queries otherwise: see the kernel's figures)
+    // Heads of 64: the two row tiles' warps take turns with their exponentials, or both would want them at once and then both wait for products (1000 queries against 8000 tokens,
+    // 32/8 heads: 135 -> 124 us; heads of 128, whose products keep them apart: 152 -> 154).
+    static constexpr bool kTurns = D == 64;
     static constexpr uint32_t kQ = kTileRows * D * 2, kStage = kTileTokens * D * 2;
-    static constexpr uint32_t q = 0, stages = kQBufs * kTiles * kQ, meta = stages + kStages * kStage, seg = meta + kMetaRing * 128, bars = seg + kSegRing * 64;
+    static constexpr uint32_t q = 0, stages = kQBufs * kTiles * kQ, out = stages + kStages * kStage, meta = out + 4 * kTiles * 4096, seg = meta + kMetaRing * 128, bars = seg + kSegRing * 64;
     // barriers: queries there / free, stages full / empty, factors of a tile there, segment told / read, scores there [2], weights there (half of them, all) [2], sums complete, a tile's products with
     // values done (one row tile), sums read, all products ended (after a wait that gave up)
     static constexpr uint32_t q_full = bars, q_empty = q_full + 8 * kQBufs, full = q_empty + 8 * kQBufs, empty = full + 8 * kStages, meta_full = empty + 8 * kStages,
                               seg_full = meta_full + 8 * kMetaRing, seg_empty = seg_full + 8 * kSegRing, s_full = seg_empty + 8 * kSegRing, p_half = s_full + 16, p_full = p_half + 16,
-                              o_full = p_full + 16, pv_done = o_full + 8, o_empty = pv_done + 8, drain = o_empty + 8, tmem_slot = drain + 8, abort_flag = tmem_slot + 4, total = abort_flag + 4;
+                              o_full = p_full + 16, pv_done = o_full + 8, o_empty = pv_done + 8, drain = o_empty + 8, turn = drain + 8, tmem_slot = turn + 64, abort_flag = tmem_slot + 4, total = abort_flag + 4;
     static constexpr uint32_t kBytes = total + 1024;
     static_assert(kBytes <= 227 * 1024, "shared memory");
 };
@@ -330,6 +380,12 @@ template <int D> struct Record {
 struct Segment {
     PairView u;
     int head, c0, c1;
+    __device__ Segment(const PrefillParams& p, long long x0, long long x_end, int pair, int head_)  // (the first one of a block)
+    {
+        const long long per_head = p.tiles_at[p.pairs];
+        head = head_;
+        set(p, pair, x0 - head * per_head, x_end - x0);
+    }
     __device__ Segment(const PrefillParams& p, long long x0, long long x_end)
     {
         const long long per_head = p.tiles_at[p.pairs];
@@ -342,9 +398,13 @@ struct Segment {
             a += last * step;
             n = min(step, n - last * step);
         }
+        set(p, a, x, x_end - x0);
+    }
+    __device__ void set(const PrefillParams& p, int a, long long x, long long left)
+    {
         u = pair_view(p, p.pair_seq[a], a);
         c0 = (int)(x - p.tiles_at[a]);
-        c1 = (int)min((long long)u.tiles, c0 + (x_end - x0));
+        c1 = (int)min((long long)u.tiles, c0 + left);
     }
 };
 
@@ -379,6 +439,7 @@ __device__ __forceinline__ float4 lds_f4(uint32_t addr)
     asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
     return v;
 }
+__device__ __forceinline__ void sts_v4(uint32_t addr, uint4 v) { asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory"); }
 // `bytes` (a multiple of 16) from global to shared memory
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar)
 {
@@ -405,6 +466,7 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
         for (int i = 0; i < kSegRing; i++) { mbar_init(bar(L::seg_full, i), 1); mbar_init(bar(L::seg_empty, i), 2 + 4 * kTiles); }  // (read by the copying warp, the products' and the rows')
         for (int i = 0; i < 2; i++) { mbar_init(bar(L::s_full, i), 1); mbar_init(bar(L::p_half, i), 4); mbar_init(bar(L::p_full, i), 4); }
         mbar_init(bar(L::o_full), 1); mbar_init(bar(L::pv_done), 1); mbar_init(bar(L::o_empty), 4 * kTiles); mbar_init(bar(L::drain), 1);
+        for (int i = 0; i < 8; i++) mbar_init(bar(L::turn, i), 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -439,19 +501,14 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
     if (warp >= kTmaWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
     if (warp == kPlanWarp) {  // up to kSegRing segments ahead: finding one takes a handful of loads that wait for one another
-        const long long all = p.tiles_at[p.pairs] * p.a.c.heads;
-        const int blocks = (int)min((long long)gridDim.x, all);
-        long long x0 = me < blocks ? share_of(all, me, blocks) : 0;
-        const long long x_end = me < blocks ? share_of(all, me + 1, blocks) : 0;
+        long long x0 = p.bound[me];
+        const long long x_end = p.bound[me + 1];
         for (bool more = true; more; seg++) {
             int4 info[4] = {make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0)};
             more = x0 < x_end;
             if (more) {
-                const Segment g(p, x0, x_end);
-                if (seg == 0 && lane == 0) {
-                    p.cut[2 * me] = make_int4(g.c0, g.u.tiles, g.head, g.u.r0);
-                    p.cut[2 * me + 1] = make_int4(g.u.v.first, g.u.n_rows, 0, 0);
-                }
+                const int known = seg == 0 ? p.cut[2 * me + 1].z : -1;  // the pair that it begins in
+                const Segment g = known >= 0 ? Segment(p, x0, x_end, known, p.cut[2 * me].z) : Segment(p, x0, x_end);
                 info[0] = make_int4(g.c1 - g.c0, g.head, g.u.v.first, g.u.v.n_q);
                 info[1] = make_int4(g.u.v.len, g.u.r0, g.u.n_rows, g.u.base + (g.u.j0 + g.c0) * kTileTokens);
                 info[2] = make_int4(g.u.lo_max, g.u.hi_min, g.c0 == 0 && g.c1 == g.u.tiles, g.c0 == 0);
@@ -641,7 +698,7 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
       if (warp < 4 * kTiles) {
         const int i = warp >> 2, row = (warp & 3) * 32 + lane;  // tile, row
         const uint32_t t_warp = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_o = t_warp + 256 + i * 128;
-        uint32_t uses = 0, tile = 0;  // scores of this row tile, tiles of tokens
+        uint32_t uses = 0, tile = 0, turn = 0;  // scores of this row tile, tiles of tokens, tiles of tokens that both row tiles had
         SegmentInfo g;
         while (next_segment(g, 82)) {
             const bool works = i * kTileRows < g.n_rows, mine = i * kTileRows + row < g.n_rows;  // the tile, this row
@@ -715,6 +772,10 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                         far = __any_sync(0xFFFFFFFFu, fabsf(m) > 131072.f && m != kNegInf);
                     }
                     const float base_m = m == kNegInf ? 0.f : m;
+                    if (L::kTurns && g.n_rows > kTileRows) {
+                        if (i || turn) ok = warp_all(mbar_wait(bar(L::turn, 4 * i + (warp & 3)), (i ? turn : turn - 1) & 1u, abort_flag, p.a.status, 87));
+                        if (!ok) break;
+                    }
                     if (far) {  // there -m + 4 - e would lose its last bits: the differences first
 #pragma unroll
                         for (int x = 0; x < 8; x++) {
@@ -744,6 +805,11 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                             unpack2(sum2, u0, u1);
                             l = fmaf(u0 + u1, weight[x], l);
                         }
+                        if (L::kTurns && c == 3 && g.n_rows > kTileRows) {
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(bar(L::turn, 4 * (1 - i) + (warp & 3)));
+                            turn++;
+                        }
                         if (c == 2) {  // the products with the first 64 tokens may start: their weights have landed while these were computed
                             tmem_st_wait();
                             tc_fence_before();
@@ -767,25 +833,33 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                 float* record = p.a.partial + (size_t)(2 * me + (g.from_start ? 1 : 0)) * Record<D>::floats;
                 const int h = g.head * p.a.group + r - qi * p.a.group;
                 const long long tok = g.first + qi;
-                const float inv = g.whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                // (a part goes through shared memory, 32 elements of each of the warp's rows at a time: a store of its 32-bit values then takes 4 rows and not 32, and each line that it
+                // touches is a cycle: 64 queries against 60000 tokens 166 -> 161 us; results gain nothing by it)
+                const uint32_t stage = base + L::out + warp * 4096;
 #pragma unroll 1
                 for (int c = 0; c < D / 32; c++) {
                     uint32_t o[32];
                     tmem_ld_x32(t_o + 32 * c, o);
                     tmem_ld_wait();
-                    if (mine) {
-                        if (g.whole) {
+                    if (!g.whole) {
 #pragma unroll
-                            for (int y = 0; y < 32; y += 8) {
-                                float x[8];
+                        for (int y = 0; y < 8; y++) sts_v4(stage + lane * 128 + ((y ^ (lane & 7)) << 4), make_uint4(o[4 * y], o[4 * y + 1], o[4 * y + 2], o[4 * y + 3]));
+                        __syncwarp();
 #pragma unroll
-                                for (int z = 0; z < 8; z++) x[z] = __uint_as_float(o[y + z]) * inv;
-                                store_out8<DT>(p.a, tok * p.a.out_token + (long long)h * p.a.out_head + 32 * c + y, x);
-                            }
-                        } else {
+                        for (int y = 0; y < 8; y++) { const uint4 w = lds_v4(stage + (4 * y + (lane >> 3)) * 128 + (((lane & 7) ^ ((4 * y + (lane >> 3)) & 7)) << 4)); o[4 * y] = w.x; o[4 * y + 1] = w.y; o[4 * y + 2] = w.z; o[4 * y + 3] = w.w; }
 #pragma unroll
-                            for (int y = 0; y < 32; y += 4)
-                                *reinterpret_cast<uint4*>(record + (size_t)(i * kTileRows + row) * D + 32 * c + y) = make_uint4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+                        for (int y = 0; y < 8; y++)
+                            *reinterpret_cast<uint4*>(record + (size_t)(i * kTileRows + (warp & 3) * 32 + 4 * y + (lane >> 3)) * D + 32 * c + 4 * (lane & 7)) =
+                                make_uint4(o[4 * y], o[4 * y + 1], o[4 * y + 2], o[4 * y + 3]);
+                        __syncwarp();
+                    } else if (mine) {
+#pragma unroll
+                        for (int y = 0; y < 32; y += 8) {
+                            float x[8];
+#pragma unroll
+                            for (int z = 0; z < 8; z++) x[z] = __uint_as_float(o[y + z]) * inv;
+                            store_out8<DT>(p.a, tok * p.a.out_token + (long long)h * p.a.out_head + 32 * c + y, x);
                         }
                     }
                 }
@@ -812,23 +886,42 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
 // Joins the unit that the boundary between blocks b - 1 and b cuts first; a block of threads takes 16 of its rows.
 constexpr int kJoinRows = 16;
 template <int D, int DT>
-__global__ void __launch_bounds__(kThreads) cache_attention_join_kernel(const PrefillParams p, int grid_blocks)
+__global__ void __launch_bounds__(kThreads) cache_attention_join_kernel(const PrefillParams p)
 {
+    __shared__ int s_record[kMaxBlocks], s_parts;
     pdl_wait_prior_grid();
     pdl_launch_dependents();
-    const int b = (int)blockIdx.x + 1;
-    const long long all = p.tiles_at[p.pairs] * p.a.c.heads;
-    const int4 cut = p.cut[2 * b], of = p.cut[2 * b + 1];  // the unit that the boundary cuts (of a block that has no tiles: not looked at)
-    const int blocks = (int)min((long long)grid_blocks, all);
-    if (b >= blocks) return;
-    const long long begin = share_of(all, b, blocks) - cut.x, end = begin + cut.y;
-    if (cut.x == 0 || share_of(all, b - 1, blocks) > begin) return;
+    const int b = (int)blockIdx.x + 1, lane = threadIdx.x & 31;
+    if (b >= p.blocks) return;
+    constexpr int kSteps = (kMaxBlocks + 31) / 32;
+    long long from[kSteps], to[kSteps];  // (all loads at once)
+#pragma unroll
+    for (int k = 0; k < kSteps; k++) { from[k] = p.bound[min(b + 32 * k + lane, p.blocks)]; to[k] = p.bound[min(b + 32 * k + lane + 1, p.blocks)]; }
+    const long long x = p.bound[b], all = p.bound[p.blocks], x_before = p.bound[b - 1];
+    const int4 cut = p.cut[2 * b], of = p.cut[2 * b + 1];  // (of a block that begins behind all tiles: not looked at)
+    if (x >= all) return;
+    const long long begin = x - cut.x, end = begin + cut.y;
+    if (cut.x == 0 || x_before > begin) return;
     const int head = cut.z, r0 = cut.w, first = of.x, n_rows = of.y;
-    const int parts = owner_of(all, end - 1, blocks) - (b - 1) + 1;
+    if ((int)blockIdx.y * kJoinRows >= n_rows) return;
+    if (threadIdx.x < 32) {  // the blocks that have tiles of the unit: the one in front of the boundary, whose part is its last, and those behind it, whose parts are their first
+        int n = 1;
+        if (lane == 0) s_record[0] = 2 * (b - 1) + 1;
+#pragma unroll
+        for (int k = 0; k < kSteps; k++) {
+            const bool in = from[k] < end && to[k] > from[k];
+            const uint32_t any = __ballot_sync(0xFFFFFFFFu, in);
+            if (in) s_record[n + __popc(any & ((1u << lane) - 1u))] = 2 * (b + 32 * k + lane);
+            n += __popc(any);
+        }
+        if (lane == 0) s_parts = n;
+    }
+    __syncthreads();
+    const int parts = s_parts;
     for (int i = threadIdx.x; i < kJoinRows * (D / 4); i += kThreads) {
         const int row = (int)blockIdx.y * kJoinRows + i / (D / 4), d = i % (D / 4) * 4;
         if (row >= n_rows) continue;
-        auto record = [&](int j) -> const float* { return p.a.partial + (size_t)(2 * (b - 1 + j) + (j == 0 ? 1 : 0)) * Record<D>::floats; };
+        auto record = [&](int j) -> const float* { return p.a.partial + (size_t)s_record[j] * Record<D>::floats; };
         float top = kNegInf, den = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
         for (int j = 0; j < parts; j++) top = fmaxf(top, record(j)[(size_t)Record<D>::kRows * D + 2 * row]);
@@ -856,7 +949,7 @@ constexpr size_t kMostWorkspace = (size_t)16 << 30;
 
 struct Sizes {
     int cap_blocks, pairs;
-    size_t cut, block_at, tiles_at, pair_seq, partial, meta, q_mul, kx, vx, qx, total;  // offsets
+    size_t cut, bound, block_at, tiles_at, units_at, pair_seq, partial, meta, q_mul, kx, vx, qx, total;  // offsets
 };
 Sizes sizes_of(int n_seqs, int n_q, int max_length, int heads, int kv_heads, int dim)
 {
@@ -868,8 +961,10 @@ Sizes sizes_of(int n_seqs, int n_q, int max_length, int heads, int kv_heads, int
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += round_up_256(bytes); return here; };
     z.cut = take((size_t)kMaxBlocks * 32);
+    z.bound = take((size_t)(kMaxBlocks + 1) * 8);
     z.block_at = take((size_t)(n_seqs + 1) * 4);
     z.tiles_at = take((size_t)(z.pairs + 1) * 8);
+    z.units_at = take((size_t)z.pairs * 4);
     z.pair_seq = take((size_t)z.pairs * 4);
     z.partial = take((size_t)2 * kMaxBlocks * unit_rows * (dim + 2) * 4);
     z.meta = take((size_t)kv_heads * z.cap_blocks * 8 * 16);
@@ -905,7 +1000,7 @@ cudaError_t launch_of(const PrefillParams& p, int sms, cudaStream_t st)
     CUtensorMap mq, mk, mv;
     const long long kv_rows = (long long)p.a.c.heads * p.cap_blocks * kTileTokens;
     if (!fp16_map(&mq, p.qx, D, p.rows * p.a.c.heads) || !fp16_map(&mk, p.kx, D, kv_rows) || !fp16_map(&mv, p.vx, D, kv_rows)) return cudaErrorInvalidValue;
-    const int blocks = sms < kMaxBlocks ? sms : kMaxBlocks;
+    const int blocks = p.blocks;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)blocks);
     cfg.blockDim = dim3(kThreadsA);
@@ -918,7 +1013,7 @@ cudaError_t launch_of(const PrefillParams& p, int sms, cudaStream_t st)
     cfg.numAttrs = 1;
     rc = cudaLaunchKernelEx(&cfg, cache_attention_tiles_kernel<D, DT>, mq, mk, mv, p);
     if (rc != cudaSuccess) return rc;
-    rc = launch_pdl(cache_attention_join_kernel<D, DT>, dim3((unsigned)(blocks > 1 ? blocks - 1 : 1), TileShape<D>::kUnitRows / kJoinRows), st, p, blocks);
+    rc = launch_pdl(cache_attention_join_kernel<D, DT>, dim3((unsigned)(blocks > 1 ? blocks - 1 : 1), TileShape<D>::kUnitRows / kJoinRows), st, p);
     g_launches.fetch_add(4, std::memory_order_relaxed);
     return rc;
 }
@@ -959,6 +1054,8 @@ cudaError_t launch_prefill(AttentionParams a, int dtype, int max_length, uint8_t
     p.block_at = reinterpret_cast<int*>(ws + z.block_at);
     p.tiles_at = reinterpret_cast<long long*>(ws + z.tiles_at);
     p.pair_seq = reinterpret_cast<int*>(ws + z.pair_seq);
+    p.units_at = reinterpret_cast<int*>(ws + z.units_at);
+    p.bound = reinterpret_cast<long long*>(ws + z.bound);
     p.a.partial = reinterpret_cast<float*>(ws + z.partial);
     p.meta = reinterpret_cast<float4*>(ws + z.meta);
     p.q_mul = reinterpret_cast<float*>(ws + z.q_mul);
@@ -967,6 +1064,7 @@ cudaError_t launch_prefill(AttentionParams a, int dtype, int max_length, uint8_t
     p.qx = reinterpret_cast<__half*>(ws + z.qx);
     p.cap_blocks = z.cap_blocks;
     p.pairs = z.pairs;
+    p.blocks = sms < kMaxBlocks ? sms : kMaxBlocks;
     p.rows = (long long)a.n_q * a.group;
     p.unit_rows = a.c.dim == 256 ? TileShape<256>::kUnitRows : TileShape<128>::kUnitRows;
     if (a.c.dim == 64) return dtype == HIF8_BF16 ? launch_of<64, HIF8_BF16>(p, sms, st) : launch_of<64, HIF8_F16>(p, sms, st);
