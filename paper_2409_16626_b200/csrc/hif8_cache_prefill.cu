@@ -1,6 +1,6 @@
 // Attention over the HiF8 key/value cache for many query rows (chunks of prompts): bound by the products, so it runs on the tensor cores (tcgen05).
 //
-// Three steps.  (1) plan: where each sequence's tokens lie in the workspace, and how many tiles of 128 tokens each pair of row tiles has to look at.
+// Three steps.  (1) plan: where each sequence's tokens lie in the workspace, how many tiles of 128 tokens each pair of row tiles has to look at, and where blocks begin.
 // (2) expand: the codes of K and V that are looked at and the queries become FP16 tiles in the workspace (exact, see hif8_cache_attention.cu; the queries
 // packed by key head, with the power of two they are scaled by aside), once for all rows that use them: 5 bytes of traffic a code, 3 % of the time of
 // a chunk of 2048 queries against 16 K tokens.  Decoding inside the product kernel was not built: with 256 query rows to a tile of keys its lookups and stores
@@ -8,9 +8,9 @@
 // (3) attention: a block holds two tiles of 128 query rows.  For each, S = Q K^T goes to tensor memory, four warps (a thread a row) turn it into P = 2^(x - m + 4) in
 // FP16, written over S, and O += P V accumulates in tensor memory; while one tile's warps work, the tensor cores do the other tile's products.  O is only
 // rescaled when a row's maximum has grown by more than 2^8 (P stays below 2^12), by the warps themselves: the next scores' barrier says that the sums are not in use.
-// The tiles of all units are dealt out evenly over the blocks; a unit that several blocks share leaves FP32 parts, which a last kernel joins in a fixed order.
+// All units are dealt out over the blocks by a cost of their tiles and of themselves; a unit that several blocks share leaves FP32 parts, which a last kernel joins in a fixed order.
 //
-// Measured: a chunk of 2048 queries against 16461 tokens, 32/8 heads of 128: 525 us a call (986 TFLOP/s; cuBLAS sustains 1384 here at the same 1000 W), 465 of them in the
+// Measured: a chunk of 2048 queries against 16461 tokens, 32/8 heads of 128: 520 us a call (995 TFLOP/s; cuBLAS sustains 1384 here at the same 1000 W), 465 of them in the
 // attention kernel, whose tensor pipe is busy 59 % of the time and the exponentials' unit as long.  A pair of tiles takes 3250 cycles where the products alone take 2048: what a row
 // tile's warps do to its scores (load 90, maximum 380, weights 1650 cycles) and its products (770, and 500 until each side has noticed the other) make a chain
 // as long as that, and two row tiles are what tensor memory holds.  Exponentials as polynomials on the FMA pipe, for an eighth to half of the elements, made it slower (531 ->
@@ -945,7 +945,7 @@ __global__ void __launch_bounds__(kThreads) cache_attention_join_kernel(const Pr
 // ---------------------------------------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------------------------------------
-constexpr size_t kMostWorkspace = (size_t)16 << 30;
+constexpr size_t kMostWorkspace = (size_t)16 << 30;  // beyond, the few-rows kernel takes the call
 
 struct Sizes {
     int cap_blocks, pairs;
