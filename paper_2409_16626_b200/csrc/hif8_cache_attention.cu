@@ -394,6 +394,9 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
             const bool whole = t0 >= lo_max && t0 + 16 <= hi_min;  // every row sees every token
             const int ke = (int)(signed char)(exps & 0xFF), ve = exps >> 8;
             const float k_mul = pow2f(-ke), v_mul = pow2f(ve), v_add = (float)-ve;
+            // Factor of a score: not below 1e-36, where scores count as nothing anyway (a product of codes is below 2^40).  A factor of 0 would turn the -Inf of a token that
+            // a row does not see into NaN.
+            auto factor = [&](int i, int b) -> float { return fmaxf(row_mul[i][b] * k_mul, 1.0e-36f); };
             // Arguments of the exponentials, x - base + 8 in one FMA; the maximum is only looked for when one of them has outgrown the weights' range in FP16
             // by now (x > base + 6), or there was none before.
             auto argument = [&](int i, int h, int b, float f) -> float {
@@ -406,7 +409,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
             for (int i = 0; i < NT; i++) {
 #pragma unroll
                 for (int b = 0; b < 2; b++) {
-                    const float f = row_mul[i][b] * k_mul;
+                    const float f = factor(i, b);
 #pragma unroll
                     for (int h = 0; h < 2; h++) sc[i][2 * h + b] += sd[i][2 * h + b];
                     if (!whole) {
@@ -431,7 +434,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
                 for (int i = 0; i < NT; i++)
 #pragma unroll
                     for (int b = 0; b < 2; b++) {
-                        const float f = row_mul[i][b] * k_mul;
+                        const float f = factor(i, b);
                         float a = fmaxf(fmaf(sc[i][b], f, v_add), fmaf(sc[i][2 + b], f, v_add));
                         a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 4));
                         a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 8));
@@ -451,7 +454,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
 #pragma unroll
                     for (int b = 0; b < 2; b++)
 #pragma unroll
-                        for (int h = 0; h < 2; h++) e[i][2 * h + b] = argument(i, h, b, row_mul[i][b] * k_mul);
+                        for (int h = 0; h < 2; h++) e[i][2 * h + b] = argument(i, h, b, factor(i, b));
             }
             uint32_t pb[NT][2];
 #pragma unroll

@@ -1,0 +1,28 @@
+"""Attention over the HiF8 key/value cache where factors, weights and values lie at the ends of their ranges.
+
+Each case goes through both kernels: few query rows, and chunks (a workspace without room for tiles takes a chunk through the first).
+Tolerances are those of test_gpu_cache_attention, derived there."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2409_16626_b200 as H
+from cache_util import VALUES
+from test_gpu_cache_attention import BF16, F16, attend, close, make, reference
+
+pytestmark = pytest.mark.gpu
+FORMS = [([1, 1], False), ([3, 2], False), ([70, 40], True), ([70, 40], False)]  # queries of each sequence, least workspace
+
+
+@pytest.mark.parametrize("counts,small", FORMS)
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("q_exp,k_exp,scale", [(-112, 24, None), (-120, 48, None), (-90, 48, None), (-70, 48, 1e-10), (0, 0, 1e-40), (-60, -48, 1e-40)])
+def test_factors_of_scores_that_vanish(counts, small, dim, q_exp, k_exp, scale):
+    """Tokens that a row does not see stay unseen however small the factor of its scores is: the result is a plain mean."""
+    c, q = make([70, 333], counts, 8, 2, 32, dim, BF16, seed=dim)
+    c.h["k_exp"][:] = k_exp
+    c.upload()
+    out, lse = close(c, (q.float() * 2.0 ** q_exp).bfloat16(), counts, 8, scale=scale, small=small)
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
