@@ -315,7 +315,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
             }
             if (row < S::kRows) {
                 *reinterpret_cast<uint4*>(queries + row * D * 2 + 16 * q_piece) = q_raw[i];
-                if (q_piece == 0) muls[row] = fminf(p.scale_log2 * pow2_clamped(-e), 3.0e23f);  // (times 2^48 within the finite floats)
+                if (q_piece == 0) muls[row] = query_factor(p.scale_log2, e);
             }
         }
     };
@@ -393,10 +393,8 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
             }
             const bool whole = t0 >= lo_max && t0 + 16 <= hi_min;  // every row sees every token
             const int ke = (int)(signed char)(exps & 0xFF), ve = exps >> 8;
-            const float k_mul = pow2f(-ke), v_mul = pow2f(ve), v_add = (float)-ve;
-            // Factor of a score: not below 1e-36, where scores count as nothing anyway (a product of codes is below 2^40).  A factor of 0 would turn the -Inf of a token that
-            // a row does not see into NaN.
-            auto factor = [&](int i, int b) -> float { return fmaxf(row_mul[i][b] * k_mul, 1.0e-36f); };
+            const float k_mul = pow2f(kMulShift - ke), v_mul = pow2f(ve), v_add = (float)-ve;
+            auto factor = [&](int i, int b) -> float { return score_factor(row_mul[i][b], k_mul); };
             // Arguments of the exponentials, x - base + 8 in one FMA; the maximum is only looked for when one of them has outgrown the weights' range in FP16
             // by now (x > base + 6), or there was none before.
             auto argument = [&](int i, int h, int b, float f) -> float {

@@ -168,6 +168,13 @@ __device__ __forceinline__ float pow2_clamped(int a) { return pow2f(max(-126, mi
 // is below 2^-38 of it.
 __device__ __forceinline__ int query_exp(float amax) { return scale_exp_from_amax(__float_as_uint(amax), 14); }
 
+// Factor of a score: softmax scale / ln 2, the inverses of the powers of two of the query row (e) and of the block (its exponent).  The row's part and the block's
+// share a power of two, 2^-kMulShift and 2^(kMulShift - e_k), so that neither leaves the floats where the product does not.  The product stays in [1e-36, 3e38]: below, scores count as
+// nothing anyway (a product of codes is below 2^40); a factor of 0 would turn the -Inf of a token that a row does not see into NaN, and so would Inf a score of 0.
+constexpr int kMulShift = 24;
+__device__ __forceinline__ float query_factor(float scale_log2, int e) { return fminf(scale_log2 * pow2_clamped(-e - kMulShift), 3.0e38f); }
+__device__ __forceinline__ float score_factor(float row, float block) { return fmaxf(fminf(row * block, 3.0e38f), 1.0e-36f); }
+
 // What query rows may look at.  A row is a query and one of the heads that share a key head: row r of a sequence's n_q * group belongs to query r / group.
 struct SeqView {
     int first, n_q, len;  // first query of the batch, queries, tokens in the cache

@@ -38,7 +38,7 @@ struct PrefillParams {
     __half* kx;            // [heads][cap_blocks * 128][dim]
     __half* vx;
     __half* qx;            // [heads][n_q * group][dim]
-    float* q_mul;          // [heads][n_q * group]: softmax scale / ln 2 times the inverse of the power of two of the row
+    float* q_mul;          // [heads][n_q * group]: the row's part of a score's factor (query_factor)
     float4* meta;          // [heads][cap_blocks * 8]: of 16 tokens: 2^-e_k, -e_v (-Inf: no page), 2^e_v
     int* block_at;         // [n_seqs + 1] first 128-token block of each sequence
     long long* tiles_at;   // [pairs + 1] tiles in front of each pair of row tiles (of one head)
@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(kThreads) cache_expand_kernel(const PrefillPar
             if (!is_v && lane == 0) {
                 const long long e = (long long)max(page, 0) * c.heads + head;
                 const int ke = page >= 0 ? clamp_cache_exp(c.k_exp[e]) : 0, ve = page >= 0 ? clamp_cache_exp(c.v_exp[e]) : 0;
-                p.meta[row >> 4] = make_float4(pow2f(-ke), page >= 0 ? (float)-ve : kNegInf, pow2f(ve), 0.f);
+                p.meta[row >> 4] = make_float4(pow2f(kMulShift - ke), page >= 0 ? (float)-ve : kNegInf, pow2f(ve), 0.f);
             }
 #pragma unroll
             for (int i = 0; i < kSteps; i++) {
@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(kThreads) cache_expand_kernel(const PrefillPar
             }
             if (r[x] < rows) {
                 *reinterpret_cast<uint4*>(p.qx + to[x] * D + 8 * (lane % kLanes)) = w[x];
-                if (lane % kLanes == 0) p.q_mul[to[x]] = fminf(p.a.scale_log2 * pow2_clamped(-e), 3.0e38f);
+                if (lane % kLanes == 0) p.q_mul[to[x]] = query_factor(p.a.scale_log2, e);
             }
         }
     }
@@ -727,7 +727,7 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
 #pragma unroll
                     for (int x = 0; x < 8; x++) {
                         const float4 k = lds_f4(mt + 16 * x);
-                        f[x] = fmaxf(fminf(mul * k.x, 3.0e38f), 1.0e-36f); minus_ev[x] = k.y; weight[x] = k.z;
+                        f[x] = score_factor(mul, k.x); minus_ev[x] = k.y; weight[x] = k.z;
                     }
                     tmem_ld_wait();
                     if (t0 < g.lo_max || t0 + kTileTokens > g.hi_min) {  // some row does not see some token

@@ -26,3 +26,15 @@ def test_factors_of_scores_that_vanish(counts, small, dim, q_exp, k_exp, scale):
     c.upload()
     out, lse = close(c, (q.float() * 2.0 ** q_exp).bfloat16(), counts, 8, scale=scale, small=small)
     assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("counts,small", FORMS)
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("q_exp,k_exp,scale", [(100, 0, None), (120, 48, None), (90, -9, 0.5), (80, 40, 1e10), (120, 48, 1e10)])
+def test_factors_of_scores_beyond_the_ordinary(counts, small, dim, q_exp, k_exp, scale):
+    """Queries of up to 2^120: the logarithms of the sums are those of the formula on either kernel."""
+    c, q = make([70, 333], counts, 8, 2, 32, dim, BF16, seed=dim)
+    c.h["k_exp"][:] = k_exp
+    c.upload()
+    out, lse = close(c, (q.float() * 2.0 ** q_exp).bfloat16(), counts, 8, scale=scale, small=small)
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
