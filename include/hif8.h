@@ -442,7 +442,10 @@ int hif8_cache_read(const uint8_t* k_pages, const uint8_t* v_pages, const int* k
  * A query that sees no token (an empty cache, a position below 0, scores that are all -Inf) gives zeros and lse = -Inf.  Tokens that a query does not see never
  * reach its result, Inf and NaN among them, nor do slots behind a sequence's length.  Inf and NaN that it does see propagate as in IEEE arithmetic (and a
  * weight below the range of FP16 counts as zero).
- * Products of codes are exact and sums are FP32; the weights of the softmax are rounded to FP16.  softmax_scale: positive and finite (HIF8_ERR_SCALE_RANGE).
+ * Products of codes are exact and sums are FP32; the weights of the softmax are rounded to FP16 as they multiply codes: w_j = exp(s_ij) 2^-e, e the exponent of the
+ * block of v_j (of 16 tokens whose values are all zero: HIF8_CACHE_EXP_MAX).  Down to 2^-18 of the largest w_j that a query sees they have 11 bits, below that
+ * steps of 2^-28 of it (fewer than 64 query rows of a key head: 2^-22, 2^-32): where blocks of very different exponents meet, elements in which the larger one is zero have fewer bits.
+ * softmax_scale: positive and finite (HIF8_ERR_SCALE_RANGE).
  * The pool must have a page and less than 2^31 rows (n_pages * kv_heads * page_tokens), and n_q * heads / kv_heads must stay below 2^30 (HIF8_ERR_SHAPE).
  * max_q and max_length: upper bounds of a sequence's queries and tokens, known to the host.  They have to hold (where they do not, results may be wrong, but no
  * memory beside the arguments' is touched).

@@ -393,7 +393,8 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
             }
             const bool whole = t0 >= lo_max && t0 + 16 <= hi_min;  // every row sees every token
             const int ke = (int)(signed char)(exps & 0xFF), ve = exps >> 8;
-            const float k_mul = pow2f(kMulShift - ke), v_mul = pow2f(ve), v_add = (float)-ve;
+            const float k_mul = pow2f(kMulShift - ke);
+            float v_mul = pow2f(ve), v_add = (float)-ve;
             auto factor = [&](int i, int b) -> float { return score_factor(row_mul[i][b], k_mul); };
             // Arguments of the exponentials, x - base + 8 in one FMA; the maximum is only looked for when one of them has outgrown the weights' range in FP16
             // by now (x > base + 6), or there was none before.
@@ -427,6 +428,19 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
                 }
             }
             if (__any_sync(0xFFFFFFFFu, grows)) {
+                // A tile whose values are zeros has no say in what the weights refer to: they count as values of the largest exponent.  (What it adds to the sums is 0 in any case;
+                // zeros have exponent 0, which would push the weights of small values in other blocks out of FP16.)
+                uint32_t some = 0u;
+#pragma unroll
+                for (int y = 0; y < D / 32; y++) {
+                    const int tok = t0 + (D == 64 ? 8 * y + (lane >> 2) : (4 * y + (lane >> 3)) & 15);
+                    const uint4 w = lds_v4(at_v + 512 * y + 16 * lane);
+                    if (tok >= lo_min && tok < hi_max) some |= w.x | w.y | w.z | w.w;
+                }
+                if (!__any_sync(0xFFFFFFFFu, some != 0u)) {
+                    v_add = -(float)HIF8_CACHE_EXP_MAX;
+                    v_mul = pow2f(HIF8_CACHE_EXP_MAX);
+                }
                 bool large = false;
 #pragma unroll
                 for (int i = 0; i < NT; i++)

@@ -32,6 +32,8 @@ constexpr int kTmaWarp = 8, kMmaWarp = 9, kPlanWarp = 10, kThreadsA = 12 * 32;
 constexpr int kRegsRows = 208, kRegsOther = 88;
 static_assert(256 * kRegsRows + 128 * kRegsOther <= kThreadsA * 168, "no more than the block has");
 constexpr int kMetaRing = 8, kSegRing = 4;
+__device__ __forceinline__ bool warp_all(bool x) { return __all_sync(0xFFFFFFFFu, x); }
+__device__ __forceinline__ bool warp_any(bool x) { return __any_sync(0xFFFFFFFFu, x); }
 
 struct PrefillParams {
     AttentionParams a;
@@ -230,11 +232,8 @@ __global__ void __launch_bounds__(kThreads) cache_expand_kernel(const PrefillPar
             uint2 w[kSteps];
 #pragma unroll
             for (int i = 0; i < kSteps; i++) w[i] = page >= 0 ? __ldg(reinterpret_cast<const uint2*>(src) + lane + 32 * i) : make_uint2(0, 0);
-            if (!is_v && lane == 0) {
-                const long long e = (long long)max(page, 0) * c.heads + head;
-                const int ke = page >= 0 ? clamp_cache_exp(c.k_exp[e]) : 0, ve = page >= 0 ? clamp_cache_exp(c.v_exp[e]) : 0;
-                p.meta[row >> 4] = make_float4(pow2f(kMulShift - ke), page >= 0 ? (float)-ve : kNegInf, pow2f(ve), 0.f);
-            }
+            const int exponent = page >= 0 ? clamp_cache_exp((is_v ? c.v_exp : c.k_exp)[(long long)page * c.heads + head]) : 0;
+            bool some = false;  // of the values is not zero
 #pragma unroll
             for (int i = 0; i < kSteps; i++) {
                 // tokens that no query sees are not there; of V where only some queries see them, Inf and NaN are left to cache_attention_specials_kernel
@@ -245,8 +244,17 @@ __global__ void __launch_bounds__(kThreads) cache_expand_kernel(const PrefillPar
                     if (f.x != w[i].x || f.y != w[i].y) *p.specials = 1;
                     w[i] = f;
                 }
+                some |= (w[i].x | w[i].y) != 0u;
                 const uint2 a = lane_lookup4(table, w[i].x, 4u * lane), b = lane_lookup4(table, w[i].y, 4u * lane);
                 dst[lane + 32 * i] = make_uint4(a.x, a.y, b.x, b.y);
+            }
+            // Values that are zeros have no say in what the weights refer to: they count as values of the largest exponent.  (Their blocks have exponent 0, which would push
+            // the weights of small values in other blocks out of FP16.)
+            const int ve = warp_any(some) ? exponent : HIF8_CACHE_EXP_MAX;
+            if (lane == 0) {
+                float* meta = reinterpret_cast<float*>(p.meta + (row >> 4));
+                if (is_v) *reinterpret_cast<float2*>(meta) = make_float2(page >= 0 ? (float)-ve : kNegInf, pow2f(ve));
+                else meta[2] = pow2f(kMulShift - exponent);
             }
             continue;
         }
@@ -343,8 +351,6 @@ __device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t* r)
 }
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ bool warp_all(bool x) { return __all_sync(0xFFFFFFFFu, x); }
-__device__ __forceinline__ bool warp_any(bool x) { return __any_sync(0xFFFFFFFFu, x); }
 
 // What the planning warp tells the others of a segment: tiles c0 .. c1 of a unit (a pair of row tiles of a sequence and key head).  tiles == 0: there is no other.
 struct SegmentInfo {
@@ -727,7 +733,7 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
 #pragma unroll
                     for (int x = 0; x < 8; x++) {
                         const float4 k = lds_f4(mt + 16 * x);
-                        f[x] = score_factor(mul, k.x); minus_ev[x] = k.y; weight[x] = k.z;
+                        f[x] = score_factor(mul, k.z); minus_ev[x] = k.x; weight[x] = k.y;
                     }
                     tmem_ld_wait();
                     if (t0 < g.lo_max || t0 + kTileTokens > g.hi_min) {  // some row does not see some token
