@@ -440,8 +440,8 @@ int hif8_cache_read(const uint8_t* k_pages, const uint8_t* v_pages, const int* k
  * positions: query i at p_i = d_lengths[s] - n + i.  It looks at the cached tokens j
  *   causal != 0: j <= p_i;  causal == 0: all;   window > 0: only j > p_i - window (window == 0: no such limit).
  * A query that sees no token (an empty cache, a position below 0, scores that are all -Inf) gives zeros and lse = -Inf.  Tokens that a query does not see never
- * reach its result, Inf and NaN among them, nor do slots behind a sequence's length.  Inf and NaN that it does see propagate as in IEEE arithmetic (and a
- * weight below the range of FP16 counts as zero).
+ * reach its result, Inf and NaN among them, nor do slots behind a sequence's length.  Inf and NaN of queries and keys propagate through the scores as
+ * in IEEE arithmetic.  Inf and NaN among the values that a query sees reach that element of its result whatever the tokens' weights are (also none): Inf of its sign, NaN of a NaN or of both signs.
  * Products of codes are exact and sums are FP32; the weights of the softmax are rounded to FP16 as they multiply codes: w_j = exp(s_ij) 2^-e, e the exponent of the
  * block of v_j (of 16 tokens whose values are all zero: HIF8_CACHE_EXP_MAX).  Down to 2^-18 of the largest w_j that a query sees they have 11 bits, below that
  * steps of 2^-28 of it (fewer than 64 query rows of a key head: 2^-22, 2^-32): where blocks of very different exponents meet, elements in which the larger one is zero have fewer bits.

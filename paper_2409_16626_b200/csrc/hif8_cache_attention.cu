@@ -103,6 +103,50 @@ __device__ __forceinline__ bool group_any(int group, int threads, bool any)
     return r != 0;
 }
 
+// Inf and NaN among the values that a query sees reach its result whatever their weights are.  Products with Inf tell that one is there, and which where the weights are not zero; a weight
+// that is (below FP16's range, or of a score of -Inf) makes NaN of it.  So where a result is NaN and its denominator is not, the column is read again: four elements of query `tok` of the
+// batch, from d on, x what the products gave.  NaN, or Inf of both signs, ends the search.  (In a function of its own: there is hardly ever anything to do.  8 sequences of 131072 tokens whose
+// values are all Inf, most weights 0: 33 ms instead of 0.4; all NaN: 0.43.)
+__device__ __noinline__ float4 seen_specials(const AttentionParams& p, int tok, int head, int d, float4 x)
+{
+    const uint32_t need = (x.x != x.x ? 0xFFu : 0u) | (x.y != x.y ? 0xFF00u : 0u) | (x.z != x.z ? 0xFF0000u : 0u) | (x.w != x.w ? 0xFF000000u : 0u);
+    int s = 0;
+    for (int n = p.n_seqs; n > 1;) {  // the last sequence that starts at or before the query
+        const int half = n >> 1;
+        if (start_at(p.q_start, s + half, p.n_q) <= tok) { s += half; n -= half; }
+        else n = half;
+    }
+    const SeqView v = seq_view(p, s);
+    const int lo = lo_of(p, v, tok - v.first), hi = min(v.len, hi_of(p, v, tok - v.first)), mask = (1 << p.c.shift) - 1;
+    uint32_t inf = 0u, minus = 0u, nan = 0u;
+    for (int t = lo; t < hi && need & ~(nan | (inf & minus));) {
+        const int page = p.c.page_of(s, t >> p.c.shift), n = min(hi - t, mask + 1 - (t & mask));
+        if (page >= 0) {
+            const uint8_t* at = p.c.v + p.c.block_at(page, head) + (long long)(t & mask) * p.c.dim + d;
+#pragma unroll 8
+            for (int i = 0; i < n; i++) {
+                const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(at + i * p.c.dim));
+                inf |= __vcmpeq4(w, 0x6F6F6F6Fu); minus |= __vcmpeq4(w, 0xEFEFEFEFu); nan |= __vcmpeq4(w, 0x80808080u);
+            }
+        }
+        t += n;
+    }
+    nan |= inf & minus;
+    auto result = [&](float y, int shift) -> float {
+        if (!(need >> shift & 1u) || nan >> shift & 1u) return y;
+        return inf >> shift & 1u ? -kNegInf : minus >> shift & 1u ? kNegInf : y;
+    };
+    return make_float4(result(x.x, 0), result(x.y, 8), result(x.z, 16), result(x.w, 24));
+}
+__device__ __forceinline__ void resolve_specials(const AttentionParams& p, int tok, int head, int d, float den, float (&x)[4])
+{
+    const float any = (x[0] + x[1]) + (x[2] + x[3]);
+    if (any != any && den == den) {
+        const float4 y = seen_specials(p, tok, head, d, make_float4(x[0], x[1], x[2], x[3]));
+        x[0] = y.x; x[1] = y.y; x[2] = y.z; x[3] = y.w;
+    }
+}
+
 // The work of one sequence in chunks
 struct SeqChunks {
     int lo, per_unit, tiles;  // first token (on a chunk), chunks of a unit, row tiles
@@ -116,7 +160,7 @@ struct SeqChunks {
 
 template <int D, int NT, int DT, bool WIDE>
 __global__ void __launch_bounds__(RowsShape<D, NT, WIDE>::kThreads, 1)
-cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const AttentionParams p)
+cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttentionParams p)
 {
     using S = RowsShape<D, NT, WIDE>;
     constexpr int GW = S::kGroupWarps, kChunk = S::kChunk;
@@ -585,6 +629,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
                     const float inv = den == 0.f ? 0.f : 1.f / den;
 #pragma unroll
                     for (int y = 0; y < 4; y++) x[y] *= inv;
+                    resolve_specials(p, (int)tok, done_head, 4 * f, den, x);
                     store_out4<DT>(p, tok * p.out_token + (long long)h * p.out_head + 4 * f, x);
                     if (p.lse && f == 0) p.lse[tok * p.heads + h] = lse_of(top, den, kPShift);
                 } else {
@@ -607,7 +652,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __g
 // A unit may lie in all groups: the parts' factors come first, then threads share the parts of a result out among them.
 constexpr int kCombineThreads = 512;
 template <int D, int NT, int DT>
-__global__ void __launch_bounds__(kCombineThreads) cache_attention_combine_kernel(const AttentionParams p, int all_groups)
+__global__ void __launch_bounds__(kCombineThreads) cache_attention_combine_kernel(const __grid_constant__ AttentionParams p, int all_groups)
 {
     using S = RowsShape<D, NT, false>;
     constexpr int kMostGroups = kMaxBlocks * S::kGroups, kItems = S::kRows * (D / 4);
@@ -663,13 +708,14 @@ __global__ void __launch_bounds__(kCombineThreads) cache_attention_combine_kerne
     }
     const int r = r0 + row, qi = r / p.group, h = head * p.group + r - qi * p.group;
     const float den = s_den[row], inv = den == 0.f ? 0.f : 1.f / den;
-    const float x[4] = {o.x * inv, o.y * inv, o.z * inv, o.w * inv};
+    float x[4] = {o.x * inv, o.y * inv, o.z * inv, o.w * inv};
+    resolve_specials(p, first + qi, head, 4 * f, den, x);
     store_out4<DT>(p, (long long)(first + qi) * p.out_token + (long long)h * p.out_head + 4 * f, x);
     if (p.lse && f == 0) p.lse[(long long)(first + qi) * p.heads + h] = lse_of(s_top[row], den, kPShift);
 }
 
 // Inf and NaN among the values of tokens that only some of a sequence's queries see: the rows that do see them get them here.  (Those that all queries
-// see took the ordinary way.)  A block looks through `slices` pieces of 16 elements of a key head's value rows, 256 pieces at a time, and keeps a bit for each token,
+// see take the ordinary way with few rows; chunks leave all of them out of the products, and set a flag where there are some.)  A block looks through `slices` pieces of 16 elements of a key head's value rows, 256 pieces at a time, and keeps a bit for each token,
 // element and kind of what it finds; there is hardly ever anything to do, and if there is, a result takes a few words to look at, however much was found.  Without
 // a window only the first of a kind in an element counts (whoever sees a later one sees that as well): a cache full of NaN does not make the work quadratic.
 template <int DT>
@@ -683,9 +729,9 @@ __global__ void __launch_bounds__(kThreads) cache_attention_specials_kernel(cons
     if (p.special_flag && !*p.special_flag) return;
     const int head = blockIdx.y, s = blockIdx.z;
     const SeqView v = seq_view(p, s);
-    if (v.n_q < 2) return;
-    // tokens that the last query sees or the first, and not both: [a0, a1) and [b0, b1), number k being a0 + k, and b0 + k - n_a from n_a on
-    const int hi0 = min(v.len, hi_of(p, v, 0)), hi1 = min(v.len, hi_of(p, v, v.n_q - 1)), lo0 = lo_of(p, v, 0), lo1 = lo_of(p, v, v.n_q - 1);
+    if (v.n_q < (p.special_flag ? 1 : 2)) return;
+    // tokens that the last query sees or the first, and not both (chunks: that any sees): [a0, a1) and [b0, b1), number k being a0 + k, and b0 + k - n_a from n_a on
+    const int hi1 = min(v.len, hi_of(p, v, v.n_q - 1)), lo0 = lo_of(p, v, 0), hi0 = p.special_flag ? lo0 : min(v.len, hi_of(p, v, 0)), lo1 = p.special_flag ? lo0 : lo_of(p, v, v.n_q - 1);
     const int a0 = lo0, a1 = min(lo1, hi1), b0 = max(hi0, a1), b1 = hi1, n_a = max(0, a1 - a0), n = n_a + max(0, b1 - b0);
     const int step = kThreads / slices, words = (step + 31) / 32, width = 16 * slices;  // tokens at a time
     for (int i = threadIdx.x; i < 3 * kWords; i += kThreads) s_found[i / kWords][i % kWords] = 0u;
@@ -904,7 +950,7 @@ extern "C" int hif8_cache_attention(const void* q, int dtype, int64_t q_token_st
         p.special_flag = p.status + 1;
         rc = launch_prefill(p, dtype, max_length, ws + kHeadBytes, sms, st);
     } else rc = dtype == HIF8_BF16 ? launch_rows_of<HIF8_BF16>(p, nt, max_q, max_length, sms, st) : launch_rows_of<HIF8_F16>(p, nt, max_q, max_length, sms, st);
-    if (rc == cudaSuccess && max_q > 1 && (p.causal || p.window)) {
+    if (rc == cudaSuccess && (p.special_flag || (max_q > 1 && (p.causal || p.window)))) {
         const int slices = p.special_flag ? 1 : head_dim / 16;  // (few rows: few tokens to look at)
         const dim3 grid((unsigned)(head_dim / 16 / slices), (unsigned)kv_heads, (unsigned)n_seqs);
         rc = dtype == HIF8_BF16 ? launch_pdl(cache_attention_specials_kernel<HIF8_BF16>, grid, st, p, slices) : launch_pdl(cache_attention_specials_kernel<HIF8_F16>, grid, st, p, slices);

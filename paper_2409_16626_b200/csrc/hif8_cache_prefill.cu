@@ -48,7 +48,7 @@ struct PrefillParams {
     int* pair_seq;         // [pairs]
     long long* bound;      // [blocks + 1] first tile of each block: heads x tiles_at
     int4* cut;             // [blocks] two of each, of the unit that the block's first tile lies in: tiles in front of that one, tiles, key head, first row; first query, rows, pair
-    int* specials;         // set when some token that only some queries see holds Inf or NaN in V
+    int* specials;         // set when some token that a query sees holds Inf or NaN in V
     int cap_blocks, pairs, blocks;
     long long rows;        // n_q * group
     int unit_rows;         // query rows of a unit
@@ -236,10 +236,11 @@ __global__ void __launch_bounds__(kThreads) cache_expand_kernel(const PrefillPar
             bool some = false;  // of the values is not zero
 #pragma unroll
             for (int i = 0; i < kSteps; i++) {
-                // tokens that no query sees are not there; of V where only some queries see them, Inf and NaN are left to cache_attention_specials_kernel
+                // tokens that no query sees are not there; Inf and NaN of V are left to cache_attention_specials_kernel (0 times them would reach queries that do not see them, and
+                // make NaN of an Inf)
                 const int tok = t0 + (lane + 32 * i) * 8 / D;
                 if (tok < lo0 || tok >= hi1) w[i] = make_uint2(0, 0);
-                else if (is_v && (tok >= hi0 || tok < lo1)) {
+                else if (is_v) {
                     const uint2 f = make_uint2(finite_codes(w[i].x), finite_codes(w[i].y));
                     if (f.x != w[i].x || f.y != w[i].y) *p.specials = 1;
                     w[i] = f;

@@ -71,3 +71,84 @@ def test_zeros_only():
         c.upload()
         out, _ = close(c, q, counts, 8)
         assert (out == 0).all()
+
+
+def expect_specials(c, q, counts, heads, window, scale, **kw):
+    """Where a query sees Inf or NaN among an element's values, the result is that Inf, or NaN of NaN or both signs, whatever the weights are; elsewhere what the other values give."""
+    out, lse = attend(c, q, counts, heads, 1, window, scale, **kw)
+    scale = q.shape[2] ** -0.5 if scale is None else scale
+    stale, c.h["v"] = c.h["v"], np.where(np.isfinite(VALUES[c.h["v"]]), c.h["v"], 0).astype(np.uint8)
+    want, norm, tol, tol_lse = reference(c, q, counts, heads // c.shape[1], scale, 1, window)
+    c.h["v"] = stale
+    _, kv, page, _ = c.shape
+    special, at = torch.zeros_like(want, dtype=torch.bool), 0
+    for s, (n, m) in enumerate(zip(c.lengths, counts)):
+        codes = c.h["v"][c.table[s, :-(-n // page)]].transpose(1, 0, 2, 3).reshape(kv, -1, c.shape[3])[:, :n]
+        pos, key = np.arange(n - m, n)[:, None], np.arange(n)
+        seen = torch.from_numpy((key <= pos) & ((key > pos - window) if window else True)).cuda().double()
+        kinds = [(torch.einsum("qt,htd->qhd", seen, torch.from_numpy(codes == code).cuda().double()) > 0).repeat_interleave(heads // kv, 1) for code in (0x6F, 0xEF, 0x80)]
+        rows = slice(at, at + m)
+        special[rows] = kinds[0] | kinds[1] | kinds[2]
+        value = torch.where(kinds[2] | (kinds[0] & kinds[1]), math.nan, torch.where(kinds[0], math.inf, -math.inf))
+        want[rows] = torch.where(special[rows], value, want[rows])
+        at += m
+    got = out.double()
+    assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isinf(got), torch.isinf(want))
+    assert torch.equal(got[torch.isinf(want)], want[torch.isinf(want)])
+    assert ((got - want).abs()[~special] <= tol[~special]).all()
+    assert torch.equal(torch.isfinite(norm), torch.isfinite(lse)) and ((lse.double() - norm).abs() <= tol_lse)[torch.isfinite(norm)].all()
+    return special
+
+
+@pytest.mark.parametrize("counts,small", FORMS)
+@pytest.mark.parametrize("dim,dtype", [(64, F16), (128, BF16), (256, BF16)])
+@pytest.mark.parametrize("window", [0, 50])
+@pytest.mark.parametrize("kinds", [[0x6F], [0xEF, 0x6F], [0x80, 0xEF], [0x6F, 0xEF, 0x80]])
+def test_inf_and_nan_among_values_whatever_their_weights(counts, small, dim, dtype, window, kinds):
+    """Weights from one that takes all down to none that FP32 could hold; specials in tokens that all queries see, that some see, and that none sees any more."""
+    lengths = [70, 333]
+    c, q = make(lengths, counts, 8, 2, 32, dim, dtype, seed=dim + window)
+    c.fill(0)
+    rng = np.random.default_rng(dim + len(kinds))
+    for s, n in enumerate(lengths):
+        for i in range(24):
+            t = int(rng.integers(0, n))
+            c.h["v"][c.table[s, t // 32], i % 2, t % 32, int(rng.integers(0, dim // 4))] = rng.choice(kinds)
+        t = n - 1
+        c.h["v"][c.table[s, t // 32], :, t % 32, dim - 1] = kinds[0]
+    c.upload()
+    for scale in (4.0, 0.02):
+        assert expect_specials(c, q, counts, 8, window, scale, small=small).any()
+
+
+@pytest.mark.parametrize("small", [False, True])
+def test_inf_among_values_of_tokens_of_no_weight(small):
+    """Every score is -Inf: zeros, and Inf where a value is."""
+    for counts in ([1, 1], [70, 40]):
+        c, q = make([70, 333], counts, 8, 2, 32, 64, BF16)
+        c.fill(0)
+        c.h["k"][:, :, :, 3] = 0xEF
+        c.h["v"][c.table[1, 2], :, 5, 7] = 0x6F
+        c.upload()
+        q[:, :, 3] = 1.0
+        out, lse = attend(c, q, counts, 8, small=small)
+        assert (lse == -math.inf).all()
+        want = torch.zeros_like(out)
+        want[counts[0]:, :, 7] = math.inf
+        assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("kinds", [[0x6F], [0x80], [0x6F, 0xEF, 0x80]])
+def test_specials_in_a_long_sequence_that_is_shared_out(kinds):
+    """Single tokens over sequences that many groups of warps share: what each part and their sums make of Inf."""
+    lengths = [20000, 300, 9000]
+    c, q = make(lengths, [1, 1, 2], 8, 1, 128, 128, BF16)
+    c.fill(0)
+    rng = np.random.default_rng(5)
+    for s, n in enumerate(lengths):
+        for i in range(40):
+            t = int(rng.integers(0, n))
+            c.h["v"][c.table[s, t // 128], 0, t % 128, int(rng.integers(0, 40))] = rng.choice(kinds)
+    c.upload()
+    for scale in (2.0, 0.01):
+        assert expect_specials(c, q, [1, 1, 2], 8, 0, scale).any()
