@@ -452,7 +452,7 @@ int hif8_cache_read(const uint8_t* k_pages, const uint8_t* v_pages, const int* k
  * out must not overlap q or the pages.  workspace: hif8_cache_attention_workspace_bytes(...) bytes of the same arguments, 256-byte aligned, contents irrelevant on entry and
  * undefined on return, for one call at a time (two captured graphs that may run at the same time need one each).  Its first int is a device status word as for hif8_gemm
  * (hif8_gemm_status, hif8_last_device_status).  From 64 query rows of a key head on (max_q * heads / kv_heads) the size has room for FP16 tiles of what is looked
- * at, up to 16 GiB; a smaller workspace, down to the size for fewer rows, gives the same results more slowly.  Where the sum over a sequence's tokens is shared, the parts are added in a fixed order: results are reproducible.
+ * at, up to 16 GiB; a smaller workspace, down to the size for max_q = 1, gives results within the same bounds more slowly.  Where the sum over a sequence's tokens is shared, the parts are added in a fixed order: results are reproducible.
  */
 int hif8_cache_attention(const void* q, int dtype, int64_t q_token_stride, int64_t q_head_stride, const int* d_q_start, const int* d_lengths,
                          int n_seqs, int n_q, int max_q, int max_length, const uint8_t* k_pages, const uint8_t* v_pages, const int* k_exp,

@@ -923,7 +923,9 @@ extern "C" int hif8_cache_attention(const void* q, int dtype, int64_t q_token_st
     const size_t pool = (size_t)n_pages * (size_t)p.c.page_bytes();
     if (ranges_overlap(q, q_bytes, out, out_bytes) || ranges_overlap(k_pages, pool, out, out_bytes) || ranges_overlap(v_pages, pool, out, out_bytes)) return HIF8_ERR_OVERLAP;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return HIF8_ERR_WORKSPACE;
-    const int group = heads / kv_heads, nt = row_tiles_of(max_q, group, head_dim);
+    const int group = heads / kv_heads;
+    int nt = row_tiles_of(max_q, group, head_dim);
+    if (workspace_bytes < kHeadBytes + partial_bytes(head_dim, nt)) nt = row_tiles_of(1, group, head_dim);  // (the workspace of single tokens takes any call)
     if (workspace_bytes < kHeadBytes + partial_bytes(head_dim, nt)) return HIF8_ERR_WORKSPACE;
     int sms; if (int rc = checked_device(&sms)) return rc;
     int dev = 0;

@@ -9,7 +9,7 @@ import pytest
 import torch
 
 import paper_2409_16626_b200 as H
-from cache_util import VALUES
+from cache_util import VALUES, starts
 from test_gpu_cache_attention import BF16, F16, attend, close, make, reference
 
 pytestmark = pytest.mark.gpu
@@ -152,3 +152,24 @@ def test_specials_in_a_long_sequence_that_is_shared_out(kinds):
     c.upload()
     for scale in (2.0, 0.01):
         assert expect_specials(c, q, [1, 1, 2], 8, 0, scale).any()
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("heads,kv_heads,m", [(8, 2, 100), (4, 1, 17), (16, 1, 4)])
+def test_the_least_workspace_of_a_chunk(dim, heads, kv_heads, m):
+    """A chunk with the workspace of single tokens: the same results as with one for its own bounds, within the tolerance; a byte less is refused."""
+    lengths, counts = [300, 45], [m, 3]
+    c, q = make(lengths, counts, heads, kv_heads, 32, dim, BF16)
+    want, norm, tol, tol_lse = reference(c, q, counts, heads // kv_heads, dim ** -0.5, 1, 0)
+    size = H.hif8_cache_attention_workspace_bytes(2, len(q), 1, 300, heads, kv_heads, dim)
+    assert size < H.hif8_cache_attention_workspace_bytes(2, len(q), m, 300, heads, kv_heads, dim)
+    ws = torch.full((size + 256,), 0xA5, dtype=torch.uint8, device="cuda")
+    out, lse = torch.full_like(q, 9.0), torch.full((len(q), heads), 9.0, device="cuda")
+
+    def call(size):
+        return H.hif8_cache_attention(q, BF16, q.stride(0), q.stride(1), starts(counts), c.d_lengths, 2, len(q), m, 300, *c.args(), heads, dim ** -0.5, 1, 0, out, q.stride(0), q.stride(1), lse,
+                                      ws, size, check=False)
+    assert call(size - 1) == 8 and (out == 9.0).all()
+    assert call(size) == 0 and H.hif8_last_device_status() == 0
+    assert ((out.double() - want).abs() <= tol).all() and ((lse.double() - norm).abs() <= tol_lse).all()
+    assert (ws[size:] == 0xA5).all()
