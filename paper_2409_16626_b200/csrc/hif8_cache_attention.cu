@@ -838,12 +838,16 @@ cudaError_t allow_shared_of()
 
 // Whether units are taken whole by all warps of a block, without a second kernel: where every unit has a block of its own and a warp two tiles of 16 tokens at most.
 // us a call in a graph, 8 key heads of 128, BF16, cut / whole: 1 sequence of 100 tokens 9.1 / 6.6, 16 of up to 500 16.3 / 10.6; three tiles a warp: 1 of 517 10.6 / 11.0, two
-// rounds of blocks: 64 of up to 300 20.3 / 28.9.  (Units and lengths are the host's upper bounds.)
+// rounds of blocks: 64 of up to 300 20.3 / 28.9, 32 of up to 100, 4 key heads and 32 heads to each 16.1 / 21.4.  Heads of 256, whose blocks have two groups of warps and not four, four rounds
+// too unless all tokens are one chunk of a group: 16 sequences, 8 key heads, 16 heads to each (two rounds), of up to 60 tokens 12.6 / 15.4, 100 20.2 / 15.7, 250 25.8 / 19.9; 32 (four) of up to
+// 250 38.9 / 36.2, 48 (six) 51.8 / 51.1.  (Units and lengths are the host's upper bounds.)
 bool whole_units(const AttentionParams& p, int max_q, int max_length, int rows, int warps, int blocks)
 {
-    const long long units = (max_q <= 1 ? (long long)p.n_seqs : (long long)p.n_q * p.group / rows + p.n_seqs) * p.c.heads;
+    // (row tiles of all sequences: as many as the longest has for each, or one more for each than full ones)
+    const long long each = ((long long)max_q * p.group + rows - 1) / rows * p.n_seqs, full = (long long)p.n_q * p.group / rows + p.n_seqs;
+    const long long units = (each < full ? each : full) * p.c.heads;
     const long long tokens = p.window && p.window + (long long)max_q < max_length ? p.window + (long long)max_q : max_length;
-    return units <= blocks && tokens <= 32 * warps;
+    return units <= (p.c.dim == 256 && tokens > 64 ? 4ll : 1ll) * blocks && tokens <= 32 * warps;
 }
 
 template <int D, int NT, int DT, bool WIDE>

@@ -173,3 +173,17 @@ def test_the_least_workspace_of_a_chunk(dim, heads, kv_heads, m):
     assert call(size) == 0 and H.hif8_last_device_status() == 0
     assert ((out.double() - want).abs() <= tol).all() and ((lse.double() - norm).abs() <= tol_lse).all()
     assert (ws[size:] == 0xA5).all()
+
+
+@pytest.mark.parametrize("dim,heads,kv_heads,seqs,shortest,launches", [(256, 64, 4, 16, 20, 1), (256, 128, 8, 16, 20, 2), (256, 128, 8, 16, 70, 1), (256, 128, 8, 40, 70, 2), (128, 128, 4, 16, 20, 1),
+                                                                      (128, 128, 4, 32, 20, 2), (64, 16, 4, 30, 20, 1)])
+def test_units_are_taken_whole_where_they_fit_the_blocks(dim, heads, kv_heads, seqs, shortest, launches):
+    """Single tokens of several row tiles a key head: one launch where the row tiles of all sequences and key heads fit a round of blocks (heads of 256, more than 64 tokens: four), two otherwise."""
+    if torch.cuda.get_device_properties(0).multi_processor_count < 148:
+        pytest.skip("fewer blocks than the cases assume")
+    lengths = [shortest + i for i in range(seqs)]
+    c, q = make(lengths, [1] * seqs, heads, kv_heads, 64, dim, BF16)
+    close(c, q, [1] * seqs, heads)
+    before = H.hif8_launch_count()
+    attend(c, q, [1] * seqs, heads)
+    assert H.hif8_launch_count() - before == launches
