@@ -402,7 +402,7 @@ int hif8_pts_status(const void* workspace, hif8_stream_t stream);
  * attended to, and read back as zeros.  Sequences may share pages that no call of append writes to.
  * A ragged batch of tokens (new ones, queries, ones to read) lies sequence by sequence; d_*_start [n_seqs + 1] says where each begins,
  * in ascending order, and the last entry where the last one ends.  Tokens and heads of such a batch are token_stride and head_stride elements
- * apart, those of a head contiguous.  16-byte aligned pointers and strides take the vectorised path, others a slower one with identical results.
+ * apart, those of a head contiguous.  What a call writes must not overlap what else it writes or reads (HIF8_ERR_OVERLAP); rows of K and of V may be slices of one tensor.  16-byte aligned pointers and strides take the vectorised path, others a slower one with identical results.
  */
 #define HIF8_CACHE_MAX_SEQS 2048
 #define HIF8_CACHE_MAX_HEADS 128
@@ -416,7 +416,7 @@ int hif8_pts_status(const void* workspace, hif8_stream_t stream);
  *   from amax down to amax / 128 where the format has three mantissa bits, and leaves later tokens of the block 2^12 times that before they overflow.
  *   code = To_HiF8_<rnd>(x * 2^e), rnd one of HIF8_RND_TA, _HR, _SSR, _TE (HIF8_ERR_ROUND for _SR: what a cache holds does not depend on draws).
  * k, v: [n_new tokens][kv_heads][head_dim] of src_dtype.  The pages and exponents of the tokens are written, nothing else; d_lengths stays as it is.
- * No page may receive tokens of two sequences of the same call.
+ * No page may receive tokens of two sequences, or of two places of a row, of the same call.
  */
 int hif8_cache_append(const void* k, const void* v, int src_dtype, int64_t token_stride, int64_t head_stride, const int* d_new_start,
                       const int* d_lengths, int n_seqs, int n_new, uint8_t* k_pages, uint8_t* v_pages, int* k_exp, int* v_exp, int n_pages,
@@ -449,7 +449,7 @@ int hif8_cache_read(const uint8_t* k_pages, const uint8_t* v_pages, const int* k
  * The pool must have a page and less than 2^31 rows (n_pages * kv_heads * page_tokens), and n_q * heads / kv_heads must stay below 2^30 (HIF8_ERR_SHAPE).
  * max_q and max_length: upper bounds of a sequence's queries and tokens, known to the host.  They have to hold (where they do not, results may be wrong, but no
  * memory beside the arguments' is touched).
- * out must not overlap q or the pages.  workspace: hif8_cache_attention_workspace_bytes(...) bytes of the same arguments, 256-byte aligned, contents irrelevant on entry and
+ * workspace: hif8_cache_attention_workspace_bytes(...) bytes of the same arguments, 256-byte aligned, contents irrelevant on entry and
  * undefined on return, for one call at a time (two captured graphs that may run at the same time need one each).  Its first int is a device status word as for hif8_gemm
  * (hif8_gemm_status, hif8_last_device_status).  From 64 query rows of a key head on (max_q * heads / kv_heads) the size has room for FP16 tiles of what is looked
  * at, up to 16 GiB; a smaller workspace, down to the size for max_q = 1, gives results within the same bounds more slowly.  Where the sum over a sequence's tokens is shared, the parts are added in a fixed order: results are reproducible.
@@ -466,8 +466,7 @@ size_t hif8_cache_attention_workspace_bytes(int n_seqs, int n_q, int max_q, int 
  * apart) becomes row d_parent[i] of page_table as far as that sequence has tokens, -1 behind, and d_lengths_out[i] its length.  Where the last page is
  * partly filled and d_new_page[i] is a page, its contents and exponents are copied there and the child's row names the copy; full pages are shared, and so
  * is the last one where d_new_page[i] is none (or d_new_page NULL): for the child that keeps it.  Of children that name the same new page the first gets it.
- * New pages must be free: no page of a row.  table_out and d_lengths_out must not overlap page_table and d_lengths (HIF8_ERR_OVERLAP), so that any child
- * may continue any parent.  A parent that is none (outside 0 .. n_seqs - 1) gives an empty child.  A length beyond table_out_stride pages is cut there.
+ * New pages must be free: no page of a row.  (The rows go to a table of their own so that any child may continue any parent.)  A parent that is none (outside 0 .. n_seqs - 1) gives an empty child.  A length beyond table_out_stride pages is cut there.
  */
 int hif8_cache_fork(uint8_t* k_pages, uint8_t* v_pages, int* k_exp, int* v_exp, int n_pages, int kv_heads, int page_tokens, int head_dim,
                     const int* page_table, int64_t table_stride, const int* d_lengths, int n_seqs, const int* d_parent, const int* d_new_page,

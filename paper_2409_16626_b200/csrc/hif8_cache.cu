@@ -540,11 +540,10 @@ extern "C" int hif8_cache_append(const void* k, const void* v, int src_dtype, in
     const size_t item = dtype_bytes(src_dtype);
     if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & (item - 1) || !ints_aligned(d_new_start, d_lengths)) return HIF8_ERR_ALIGN;
     const size_t src_bytes = ((size_t)(n_new - 1) * (size_t)token_stride + (size_t)(kv_heads - 1) * (size_t)head_stride + (size_t)head_dim) * item;
-    const size_t pool = (size_t)n_pages * (size_t)p.c.page_bytes();
-    for (const void* s : {k, v})
-        for (const void* d : {(const void*)k_pages, (const void*)v_pages})
-            if (ranges_overlap(s, src_bytes, d, pool)) return HIF8_ERR_OVERLAP;
-    if (ranges_overlap(k_pages, pool, v_pages, pool)) return HIF8_ERR_OVERLAP;
+    const size_t pool = p.c.pool_bytes(), exps = p.c.exp_bytes();
+    if (written_over({{k_pages, pool}, {v_pages, pool}, {k_exp, exps}, {v_exp, exps}},
+                     {{k, src_bytes}, {v, src_bytes}, {page_table, p.c.table_bytes(n_seqs)}, {d_new_start, (size_t)(n_seqs + 1) * 4}, {d_lengths, (size_t)n_seqs * 4}}))
+        return HIF8_ERR_OVERLAP;
     int sms; if (int rc = checked_device(&sms)) return rc;
     p.src[0] = k; p.src[1] = v; p.token_stride = token_stride; p.head_stride = head_stride; p.start = d_new_start; p.lengths = d_lengths;
     p.n_seqs = n_seqs; p.n_new = n_new; p.target_exp = target_exp; p.flags = flags;
@@ -578,11 +577,12 @@ extern "C" int hif8_cache_read(const uint8_t* k_pages, const uint8_t* v_pages, c
     const size_t item = dtype_bytes(dst_dtype);
     if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & (item - 1) || !ints_aligned(d_first, d_out_start)) return HIF8_ERR_ALIGN;
     const size_t dst_bytes = ((size_t)(n_out - 1) * (size_t)token_stride + (size_t)(kv_heads - 1) * (size_t)head_stride + (size_t)head_dim) * item;
-    const size_t pool = (size_t)n_pages * (size_t)p.c.page_bytes();
+    const size_t pool = p.c.pool_bytes(), exps = p.c.exp_bytes();
     if (rows_meet(((intptr_t)v - (intptr_t)k) / (intptr_t)item, token_stride, head_stride, n_out, kv_heads, head_dim)) return HIF8_ERR_OVERLAP;
-    for (const void* d : {(const void*)k, (const void*)v})
-        for (const void* s : {(const void*)k_pages, (const void*)v_pages})
-            if (ranges_overlap(s, pool, d, dst_bytes)) return HIF8_ERR_OVERLAP;
+    for (const void* d : {k, v})
+        if (written_over({{d, dst_bytes}}, {{k_pages, pool}, {v_pages, pool}, {k_exp, exps}, {v_exp, exps}, {page_table, p.c.table_bytes(n_seqs)}, {d_first, (size_t)n_seqs * 4},
+                                            {d_out_start, (size_t)(n_seqs + 1) * 4}}))
+            return HIF8_ERR_OVERLAP;
     int sms; if (int rc = checked_device(&sms)) return rc;
     p.dst[0] = k; p.dst[1] = v; p.token_stride = token_stride; p.head_stride = head_stride; p.start = d_out_start; p.first = d_first;
     p.n_seqs = n_seqs; p.n_out = n_out;
@@ -607,8 +607,10 @@ extern "C" int hif8_cache_fork(uint8_t* k_pages, uint8_t* v_pages, int* k_exp, i
     if (n_children == 0) return HIF8_OK;
     if ((n_seqs && !d_lengths) || !d_parent || !table_out || !d_lengths_out) return HIF8_ERR_NULL;
     if (!ints_aligned(d_lengths, d_parent, d_new_page, table_out) || !ints_aligned(d_lengths_out)) return HIF8_ERR_ALIGN;
-    const size_t in_bytes = (size_t)n_seqs * (size_t)table_stride * 4, out_bytes = (size_t)n_children * (size_t)table_out_stride * 4;
-    if (ranges_overlap(page_table, in_bytes, table_out, out_bytes) || ranges_overlap(d_lengths, (size_t)n_seqs * 4, d_lengths_out, (size_t)n_children * 4)) return HIF8_ERR_OVERLAP;
+    const size_t pool = d_new_page ? p.c.pool_bytes() : 0, exps = d_new_page ? p.c.exp_bytes() : 0, each = (size_t)n_children * 4;
+    if (written_over({{table_out, each * (size_t)table_out_stride}, {d_lengths_out, each}, {k_pages, pool}, {v_pages, pool}, {k_exp, exps}, {v_exp, exps}},
+                     {{page_table, p.c.table_bytes(n_seqs)}, {d_lengths, (size_t)n_seqs * 4}, {d_parent, each}, {d_new_page, d_new_page ? each : 0}}))
+        return HIF8_ERR_OVERLAP;
     int sms; if (int rc = checked_device(&sms)) return rc;
     p.lengths = d_lengths; p.parent = d_parent; p.new_page = d_new_page; p.table_out = table_out; p.out_stride = table_out_stride; p.lengths_out = d_lengths_out;
     p.n_seqs = n_seqs; p.n_children = n_children; p.parts = copy_parts(p.c);
@@ -632,6 +634,11 @@ extern "C" int hif8_cache_compact(uint8_t* k_pages, uint8_t* v_pages, int* k_exp
     if ((n_seqs && !d_lengths) || !d_n_live || (n_pages && !d_free_pages)) return HIF8_ERR_NULL;
     if (!ints_aligned(d_lengths, d_n_live, d_free_pages)) return HIF8_ERR_ALIGN;
     if (!workspace || workspace_bytes < hif8_cache_compact_workspace_bytes(n_pages) || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return HIF8_ERR_WORKSPACE;
+    const size_t pool = move ? p.c.pool_bytes() : 0, exps = move ? p.c.exp_bytes() : 0, table = p.c.table_bytes(n_seqs), lengths = (size_t)n_seqs * 4;
+    if (written_over({{d_n_live, 4}, {d_free_pages, (size_t)n_pages * 4}, {workspace, hif8_cache_compact_workspace_bytes(n_pages)}, {k_pages, pool}, {v_pages, pool}, {k_exp, exps}, {v_exp, exps},
+                      {page_table, move ? table : 0}},
+                     {{page_table, move ? 0 : table}, {d_lengths, lengths}}))
+        return HIF8_ERR_OVERLAP;
     int sms; if (int rc = checked_device(&sms)) return rc;
     p.table = page_table; p.lengths = d_lengths; p.n_seqs = n_seqs; p.move = move != 0; p.parts = copy_parts(p.c);
     p.words = (n_pages + 31) / 32;

@@ -7,8 +7,10 @@
 #include <cuda_runtime.h>
 
 #include <cstdint>
+#include <initializer_list>
 
 #include "hif8.h"
+#include "hif8_internal.cuh"
 
 namespace hif8 {
 
@@ -22,6 +24,9 @@ struct CacheView {
     int pages, heads, shift, dim;  // shift: log2 of the tokens of a page
 
     __host__ __device__ long long page_bytes() const { return ((long long)heads * dim) << shift; }
+    size_t pool_bytes() const { return (size_t)pages * (size_t)page_bytes(); }
+    size_t exp_bytes() const { return (size_t)pages * (size_t)heads * sizeof(int); }
+    size_t table_bytes(int seqs) const { return (size_t)seqs * (size_t)table_stride * sizeof(int); }
     // first byte of a block: one page's tokens of one head
     __device__ long long block_at(int page, int head) const { return ((long long)page * heads + head) * dim << shift; }
     // page of the tokens block << shift .. of a sequence; -1 where the table names none
@@ -95,6 +100,19 @@ struct UnitWalk {
 };
 
 }  // namespace
+
+// Whether something that a call writes lies where it writes something else, or reads.
+struct ByteRange { const void* at; size_t bytes; };
+inline bool written_over(std::initializer_list<ByteRange> written, std::initializer_list<ByteRange> read)
+{
+    for (const ByteRange* w = written.begin(); w != written.end(); w++) {
+        for (const ByteRange* o = w + 1; o != written.end(); o++)
+            if (ranges_overlap(w->at, w->bytes, o->at, o->bytes)) return true;
+        for (const ByteRange& r : read)
+            if (ranges_overlap(w->at, w->bytes, r.at, r.bytes)) return true;
+    }
+    return false;
+}
 
 // Arguments that describe the cache, checked before anything is launched; fills in the view.
 inline int check_cache(const void* k, const void* v, const void* k_exp, const void* v_exp, int n_pages, int kv_heads, int page_tokens, int head_dim, const void* table,

@@ -924,13 +924,18 @@ extern "C" int hif8_cache_attention(const void* q, int dtype, int64_t q_token_st
     if ((n_inner > 1 && inner < head_dim) || (n_outer > 1 && outer < (n_inner - 1) * inner + head_dim)) return HIF8_ERR_SHAPE;
     const size_t q_bytes = ((size_t)(n_q - 1) * (size_t)q_token_stride + (size_t)(heads - 1) * (size_t)q_head_stride + (size_t)head_dim) * 2;
     const size_t out_bytes = ((size_t)(n_q - 1) * (size_t)out_token_stride + (size_t)(heads - 1) * (size_t)out_head_stride + (size_t)head_dim) * 2;
-    const size_t pool = (size_t)n_pages * (size_t)p.c.page_bytes();
-    if (ranges_overlap(q, q_bytes, out, out_bytes) || ranges_overlap(k_pages, pool, out, out_bytes) || ranges_overlap(v_pages, pool, out, out_bytes)) return HIF8_ERR_OVERLAP;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return HIF8_ERR_WORKSPACE;
     const int group = heads / kv_heads;
     int nt = row_tiles_of(max_q, group, head_dim);
     if (workspace_bytes < kHeadBytes + partial_bytes(head_dim, nt)) nt = row_tiles_of(1, group, head_dim);  // (the workspace of single tokens takes any call)
     if (workspace_bytes < kHeadBytes + partial_bytes(head_dim, nt)) return HIF8_ERR_WORKSPACE;
+    const size_t tiles = prefill_workspace_bytes(n_seqs, n_q, max_q, max_length, heads, kv_heads, head_dim);
+    const bool chunk = tiles && workspace_bytes >= kHeadBytes + tiles;
+    const size_t pool = p.c.pool_bytes(), exps = p.c.exp_bytes();
+    if (written_over({{out, out_bytes}, {lse, lse ? (size_t)n_q * (size_t)heads * 4 : 0}, {workspace, kHeadBytes + (chunk ? tiles : partial_bytes(head_dim, nt))}},
+                     {{q, q_bytes}, {k_pages, pool}, {v_pages, pool}, {k_exp, exps}, {v_exp, exps}, {page_table, p.c.table_bytes(n_seqs)}, {d_q_start, (size_t)(n_seqs + 1) * 4},
+                      {d_lengths, (size_t)n_seqs * 4}}))
+        return HIF8_ERR_OVERLAP;
     int sms; if (int rc = checked_device(&sms)) return rc;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return HIF8_ERR_CUDA;
@@ -949,10 +954,9 @@ extern "C" int hif8_cache_attention(const void* q, int dtype, int64_t q_token_st
     p.cut = reinterpret_cast<int4*>(ws + kHeadBytes);
     p.partial = reinterpret_cast<float*>(ws + kHeadBytes + round_up_256((size_t)kMaxBlocks * groups_of(head_dim, nt) * 32));
     cudaStream_t st = (cudaStream_t)stream;
-    const size_t tiles = prefill_workspace_bytes(n_seqs, n_q, max_q, max_length, heads, kv_heads, head_dim);
     cudaError_t rc;
     p.special_flag = nullptr;
-    if (tiles && workspace_bytes >= kHeadBytes + tiles) {
+    if (chunk) {
         p.special_flag = p.status + 1;
         rc = launch_prefill(p, dtype, max_length, ws + kHeadBytes, sms, st);
     } else rc = dtype == HIF8_BF16 ? launch_rows_of<HIF8_BF16>(p, nt, max_q, max_length, sms, st) : launch_rows_of<HIF8_F16>(p, nt, max_q, max_length, sms, st);
