@@ -737,11 +737,15 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                         f[x] = score_factor(mul, k.z); minus_ev[x] = k.x; weight[x] = k.y;
                     }
                     tmem_ld_wait();
-                    if (t0 < g.lo_max || t0 + kTileTokens > g.hi_min) {  // some row does not see some token
+                    float least = minus_ev[0];
+#pragma unroll
+                    for (int x = 1; x < 8; x++) least = fminf(least, minus_ev[x]);
+                    if (t0 < g.lo_max || t0 + kTileTokens > g.hi_min || least == kNegInf) {  // some row does not see some token (of no page: an infinite query makes NaN of its zeros)
 #pragma unroll
                         for (int c = 0; c < 4; c++) {
+                            const uint32_t there = (minus_ev[2 * c] == kNegInf ? 0u : 0xFFFFu) | (minus_ev[2 * c + 1] == kNegInf ? 0u : 0xFFFF0000u);
                             const int lo_c = max(0, min(32, lo - t0 - 32 * c)), hi_c = max(0, min(32, hi - t0 - 32 * c));
-                            const uint32_t seen = (uint32_t)((1ull << hi_c) - 1ull) & ~(uint32_t)((1ull << lo_c) - 1ull);  // (a bit a column: one test each)
+                            const uint32_t seen = there & (uint32_t)((1ull << hi_c) - 1ull) & ~(uint32_t)((1ull << lo_c) - 1ull);  // (a bit a column: one test each)
 #pragma unroll
                             for (int y = 0; y < 32; y++)
                                 if (!(seen & (1u << y))) sr[32 * c + y] = __float_as_uint(kNegInf);

@@ -187,3 +187,17 @@ def test_units_are_taken_whole_where_they_fit_the_blocks(dim, heads, kv_heads, s
     before = H.hif8_launch_count()
     attend(c, q, [1] * seqs, heads)
     assert H.hif8_launch_count() - before == launches
+
+
+@pytest.mark.parametrize("counts,small", FORMS)
+@pytest.mark.parametrize("dim", [64, 256])
+def test_infinite_queries_do_not_see_entries_that_name_no_page(counts, small, dim):
+    """Every score of such a query is -Inf: zeros, as if the missing pages were not there."""
+    c, q = make([100, 333], counts, 8, 2, 16, dim, BF16)
+    c.h["k"][:, :, :, 3] = 0xC8
+    c.table[0, 1] = c.table[1, 0] = c.table[1, 7] = -1
+    c.upload()
+    q[::2, :, 3] = math.inf
+    out, lse = attend(c, q, counts, 8, small=small)
+    assert (out[::2] == 0).all() and (lse[::2] == -math.inf).all()
+    assert (out[1::2] != 0).any(-1).all() and torch.isfinite(lse[1::2]).all()
