@@ -368,8 +368,9 @@ struct CompactParams {
 };
 constexpr int kRankThreads = 1024;
 // Up to that many table entries and pages one block marks and ranks, a launch instead of three; beyond, its single SM takes longer to read the table
-// than the other launches cost.
-constexpr long long kMarkHereEntries = 1 << 16;
+// than the other launches cost (us a call that moves nothing, one launch / three: 2048 entries and 1024 pages 5.9 / 6.3, 4096 and 2048 6.7 / 6.7, 8192 and 4096 9.5 / 8.3, 65536 and 32768
+// 50 / 28).
+constexpr long long kMarkHereEntries = 1 << 12;
 constexpr int kMarkHereWords = 8192;
 
 __device__ __forceinline__ void mark_entry(const CompactParams& p, long long e, uint32_t* bits)
