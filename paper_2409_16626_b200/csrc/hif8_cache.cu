@@ -2,8 +2,8 @@
 // pages (fork), and live pages moved together (compact).  Attention over the cache is in hif8_cache_attention.cu.
 //
 // All four are bound by the bytes they move; small calls by launches and by how many loads wait for one another.  Measured (us, of the measured copy bandwidth):
-// 27.7 K tokens of prompts, 8 heads of 128, BF16, appended and read back 70 (75 %), 128 single tokens 8.4 on the device for both calls; 512 samples forked, pages of 128 tokens
-// 26 (81 %); 3.6 K pages of 64 tokens moved 173 (83 %).
+// 27.7 K tokens of prompts, 8 heads of 128, BF16, appended and read back 71 (73 %; alone 41 and 38), FP32 57 and 67 (76 and 65 %), 128 single tokens 8.4 on the device for both calls; 512
+// samples forked, pages of 128 tokens 26 (82 %); 3.6 K pages of 64 tokens moved 170 (84 %).
 #include <cuda_runtime.h>
 
 #include <atomic>

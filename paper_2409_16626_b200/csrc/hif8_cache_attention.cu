@@ -36,7 +36,7 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v)
 // values with a copy for every lane takes a byte permute and a conflict-free lookup a code.  The tensor-memory path would write every decoded value to
 // shared memory and read it again, and shared-memory traffic is what comes next after DRAM here.  (Loads straight into registers, a tile ahead, did not
 // cover the latency: 8 sequences of up to 131072 tokens, 64/8 heads of 128: 480 us, 400 of them without any lookup.)
-// Measured (us, of the measured copy bandwidth): those sequences 311 (4.8 TB/s, 74 %), 64 of up to 4096 tokens, 32/8 heads 72 (4.1 TB/s, 63 %).  Of a tile's 220 cycles an SM the
+// Measured (us, of the measured copy bandwidth): those sequences 311 (4.8 TB/s, 73 %), 64 of up to 4096 tokens, 32/8 heads 74 (4.0 TB/s, 60 %; heads of 64 57, of 256 145).  Of a tile's 220 cycles an SM the
 // shared-memory pipe is busy 165 (128 lookups and 32 wavefronts of bytes); 430 instructions a tile and warp leave the schedulers busy 62 % of the time.
 // Which of the 16 tokens or the elements meet in a product is the operands' own business as long as both agree: a thread's bytes are read 16 at a time, and
 // tokens and pieces are dealt to the threads so that the reads of a swizzled tile never meet in a bank (see token_of_row, piece_of).

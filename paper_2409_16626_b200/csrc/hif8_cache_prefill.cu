@@ -10,7 +10,7 @@
 // rescaled when a row's maximum has grown by more than 2^8 (P stays below 2^12), by the warps themselves: the next scores' barrier says that the sums are not in use.
 // All units are dealt out over the blocks by a cost of their tiles and of themselves; a unit that several blocks share leaves FP32 parts, which a last kernel joins in a fixed order.
 //
-// Measured: a chunk of 2048 queries against 16461 tokens, 32/8 heads of 128: 520 us a call (995 TFLOP/s; cuBLAS sustains 1384 here at the same 1000 W), 465 of them in the
+// Measured: a chunk of 2048 queries against 16461 tokens, 32/8 heads of 128: 515 to 520 us a call (1000 TFLOP/s; cuBLAS sustains 1346 to 1384 here at the same 1000 W), 465 of them in the
 // attention kernel, whose tensor pipe is busy 59 % of the time and the exponentials' unit as long.  A pair of tiles takes 3250 cycles where the products alone take 2048: what a row
 // tile's warps do to its scores (load 90, maximum 380, weights 1650 cycles) and its products (770, and 500 until each side has noticed the other) make a chain
 // as long as that, and two row tiles are what tensor memory holds.  Exponentials as polynomials on the FMA pipe, for an eighth to half of the elements, made it slower (531 ->
@@ -85,7 +85,8 @@ __device__ __forceinline__ PairView pair_view(const PrefillParams& p, int seq, l
 // ---------------------------------------------------------------------------------------------------------
 constexpr int kPlanThreads = 1024;
 // What is dealt out evenly: two for a tile, three for a unit (its queries, its results, and tiles that are masked; heads of 64: 3600 cycles a tile, 4900 a unit.  By tiles alone blocks
-// of 12 prompts of up to 2047 tokens with a window of 700 had 5 to 12 units and took 128 to 162 thousand cycles).
+// of 12 prompts of up to 2047 tokens with a window of 700 had 5 to 12 units and took 128 to 162 thousand cycles.  us with two / three / four / five for a unit: heads of 128, 8 prompts of 1000
+// 180 / 175 / 174 / 174, 8 of 2000 449 / 443 / 444 / 446, 30 of up to 500 147 / 145 / 145 / 148; of 64, 8 of 2000 328 / 326 / 330 / 333; of 256, 4 of 2000 240 / 232 / 231 / 233).
 constexpr int kTileCost = 2, kUnitCost = 3;
 __device__ __forceinline__ long long plan_prefix(long long v, long long* total, long long* s_warp)
 {
@@ -365,7 +366,7 @@ struct PrefillSmem {
     static constexpr int kStages = TileShape<D>::kStages, kTiles = TileShape<D>::kTiles;
     static constexpr int kQBufs = D == 64 ? 2 : 1;  // (short units, as windows and short prompts have them, wait for their queries otherwise: see the kernel's figures)
     // Heads of 64: the two row tiles' warps take turns with their exponentials, or both would want them at once and then both wait for products (1000 queries against 8000 tokens,
-    // 32/8 heads: 135 -> 124 us; heads of 128, whose products keep them apart: 152 -> 154).
+    // 32/8 heads: 136 -> 122 us; heads of 128, whose products keep them apart: 152 -> 154).
     static constexpr bool kTurns = D == 64;
     static constexpr uint32_t kQ = kTileRows * D * 2, kStage = kTileTokens * D * 2;
     static constexpr uint32_t q = 0, stages = kQBufs * kTiles * kQ, out = stages + kStages * kStage, meta = out + 4 * kTiles * 4096, seg = meta + kMetaRing * 128, bars = seg + kSegRing * 64;
@@ -846,7 +847,7 @@ __global__ void __launch_bounds__(kThreadsA, 1) cache_attention_tiles_kernel(con
                 const long long tok = g.first + qi;
                 const float inv = l == 0.f ? 0.f : 1.f / l;
                 // (a part goes through shared memory, 32 elements of each of the warp's rows at a time: a store of its 32-bit values then takes 4 rows and not 32, and each line that it
-                // touches is a cycle: 64 queries against 60000 tokens 166 -> 161 us; results gain nothing by it)
+                // touches is a cycle: 64 queries against 60000 tokens 162 -> 157 us; results gain nothing by it)
                 const uint32_t stage = base + L::out + warp * 4096;
 #pragma unroll 1
                 for (int c = 0; c < D / 32; c++) {
@@ -1031,8 +1032,11 @@ cudaError_t launch_of(const PrefillParams& p, int sms, cudaStream_t st)
 
 }  // namespace
 
-// From 64 rows of a key head on (us, few-rows kernel / this: 16 sequences of 16 queries and four heads to a key head against up to 2000 tokens 64.5 / 54.6, 64 against up to 4000
-// 375 / 326, one against 8000 38.0 / 40.1, heads of 64: 4 against up to 16000 79 / 91; twice the rows: 16 against up to 2000 107 / 61).
+// From 64 rows of a key head on.  us, few-rows kernel / this, with 48, 64 and 96 rows (four heads to a key head, 8 key heads):
+//   heads of 128: 16 sequences of up to 2000 tokens 62 / 65, 76 / 65, 104 / 66; 4 of up to 16000 95 / 110, 120 / 111, 165 / 111; one of 8000 40.8 / 41.9, 41.7 / 42.3, 51.5 / 42.2
+//   heads of 64:  16 of up to 2000 41.8 / 48.3, 49.4 / 48.1, 66 / 49; 4 of up to 16000 62 / 82, 76 / 82, 102 / 81; one of 1000 16.8 / 20.5, 17.7 / 20.9, 19.6 / 21.0
+//   heads of 256: 16 of up to 2000 137 / 99, 177 / 100, 256 / 103; one of 1000 27 / 31, 29 / 31, 33 / 32
+// (Few and long sequences of heads of 64 lose a little at 64 rows, and heads of 256 would gain from fewer rows on.)
 size_t prefill_workspace_bytes(int n_seqs, int n_q, int max_q, int max_length, int heads, int kv_heads, int dim)
 {
     if ((long long)max_q * (heads / kv_heads) < 64) return 0;
