@@ -489,6 +489,89 @@ int hif8_cache_compact(uint8_t* k_pages, uint8_t* v_pages, int* k_exp, int* v_ex
 size_t hif8_cache_compact_workspace_bytes(int n_pages);
 
 
+/*
+ * Block-scaled matrices: one power-of-two scale for each block of 128 (the finest of the scalings that Sections 5 and 6 name is a channel's).
+ *
+ * A matrix [rows, cols] of codes, rows ld bytes apart, has an exponent e for each block of block_rows x HIF8_BLOCK elements (block_rows 1, for activations
+ * and their gradients, or HIF8_BLOCK, for weights): d_exp[(r / block_rows) * exp_stride + c / HIF8_BLOCK], exp_stride >= ceil(cols / HIF8_BLOCK).  A code
+ * stands for value(code) * 2^-e.  Exponents lie, and are taken, within [-HIF8_BLOCK_EXP_MAX, HIF8_BLOCK_EXP_MAX]: within them what a code stands for is exact in BF16.
+ * Matrices of values have rows ld elements apart.  Rows must not overlap one another, nor what a call writes anything else that it writes or reads
+ * (HIF8_ERR_OVERLAP) but for what a call names.  Pointers are aligned to their elements (HIF8_ERR_ALIGN); rows on 16-byte boundaries (of codes: 8) take the vectorised path, others a slower one with identical
+ * results.  A matrix has less than 2^31 groups of eight columns (HIF8_ERR_SHAPE).
+ */
+#define HIF8_BLOCK 128
+#define HIF8_BLOCK_EXP_MAX 96
+
+/*
+ * Values -> block-scaled codes, one pass:
+ *   e = clamp(target_exp - floor(log2 amax)) with the block's largest finite magnitude, 0 for zeros;  dst = To_HiF8_<rnd>(src * 2^e)
+ * target_exp in [-22, 15]: 3 puts what lies from amax down to amax / 128 where the format has three mantissa bits.
+ * HIF8_RND_SR draws the word of index r * cols + c, as hif8_encode does.
+ */
+int hif8_block_encode(const void* src, int src_dtype, int64_t ld_src, int64_t rows, int64_t cols, int block_rows, uint8_t* dst, int64_t ld_dst, int* d_exp,
+                      int64_t exp_stride, int target_exp, int rnd, unsigned flags, uint64_t seed, hif8_stream_t stream);
+
+/* Block-scaled codes -> values: value(src) * 2^-e, rounded to nearest-even in dst_dtype (only FP16 needs it). */
+int hif8_block_decode(const uint8_t* src, int64_t ld_src, const int* d_exp, int64_t exp_stride, int64_t rows, int64_t cols, int block_rows, void* dst, int dst_dtype,
+                      int64_t ld_dst, hif8_stream_t stream);
+
+/*
+ * Root-mean-square norm with the residual's addition, its result in block-scaled codes (blocks of 1 x 128): what stands in front of a product.
+ *   h = x + residual, rounded to dtype (residual NULL: h = x);  r = 1 / sqrt(mean_c h^2 + eps);  dst, d_exp = the codes of h * r * weight (see hif8_block_encode)
+ * x, residual, h (may be NULL; may be x or residual itself, with the same ld) [rows, cols], weight [cols]: all of `dtype`.  d_rstd [rows] (may be NULL): r, for the gradient.
+ * cols at most HIF8_NORM_MAX_COLS (HIF8_ERR_SHAPE); eps >= 0 and finite (HIF8_ERR_SCALE_RANGE).  Squares are added in FP32, products are FP32 and rounded once, to the codes.
+ * rnd one of HIF8_RND_TA, _HR, _SSR, _TE (HIF8_ERR_ROUND for _SR).  Inf and NaN propagate within their row as in IEEE arithmetic.
+ */
+#define HIF8_NORM_MAX_COLS 32768
+int hif8_rmsnorm_encode(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, int dtype, const void* weight, float eps, int64_t rows, int64_t cols,
+                        void* h, int64_t ld_h, float* d_rstd, uint8_t* dst, int64_t ld_dst, int* d_exp, int64_t exp_stride, int target_exp, int rnd, unsigned flags,
+                        hif8_stream_t stream);
+
+/*
+ * Its gradient (the rounding to codes passes it on as it is):  with u = h * r
+ *   dx = r * (weight * dy - u * mean_c(weight * dy * u)) + dh      the gradient of x and of residual; dh (NULL: 0): that of h from behind
+ *   d_weight_grad[c] (+)= sum over rows of dy * u                  FP32, added to what is there when accumulate != 0; NULL: not wanted
+ * dy, h, dh, dx [rows, cols] of dtype; dx may be dy or dh itself, with the same ld.  Sums are FP32 in a fixed order: results are reproducible.
+ * workspace (for d_weight_grad): hif8_rmsnorm_backward_workspace_bytes(rows, cols) bytes, 256-byte aligned, contents irrelevant on entry and undefined on return, for one call at a time.
+ */
+int hif8_rmsnorm_backward(const void* dy, int64_t ld_dy, const void* h, int64_t ld_h, const void* dh, int64_t ld_dh, int dtype, const void* weight, const float* d_rstd,
+                          int64_t rows, int64_t cols, void* dx, int64_t ld_dx, float* d_weight_grad, int accumulate, void* workspace, size_t workspace_bytes,
+                          hif8_stream_t stream);
+size_t hif8_rmsnorm_backward_workspace_bytes(int64_t rows, int64_t cols);
+
+/*
+ * The product of block-scaled operands, and with it the gradients' products:
+ *   C[m,n] (+)= sum_k value(A(m,k)) 2^-ea * value(W(k,n)) 2^-ew
+ * Aq is stored [M,K] (a_is_km = 0) or [K,M], Wq [K,N] (w_is_nk = 0) or [N,K]; either operand's blocks (a_block_rows, w_block_rows: 1 or HIF8_BLOCK) lie on the
+ * matrix as it is stored, so what one call made of a tensor serves all its products:
+ *   forward  Y[T,N'] = X W^T:   A = X [T,K'] (1),  W = [N',K'] (128), w_is_nk = 1
+ *   dX[T,K'] = dY W:            A = dY [T,N'] (1), the same W, w_is_nk = 0
+ *   dW[N',K'] += dY^T X:        A = dY, a_is_km = 1, W = X [T,K'] (1), w_is_nk = 0, accumulate = 1
+ * M, N and K are any positive numbers.  C [M,N] of HIF8_BF16 or HIF8_F32, 16-byte aligned with rows a multiple of 16 bytes apart (HIF8_ERR_ALIGN); what lies behind
+ * column N of a row stays as it is.  Products are exact in FP32 unless they leave its range (beyond it Inf, below 2^-126 possibly 0); sums are FP32, in a fixed order.
+ * NaN and Inf codes propagate as in IEEE arithmetic.  accumulate as in hif8_gemm_ex.
+ * workspace: hif8_gemm_block_workspace_bytes(...) bytes of the same arguments, 256-byte aligned, contents irrelevant on entry and undefined on return, for one call at a time; its first int is a device status
+ * word as for hif8_gemm (hif8_gemm_status, hif8_last_device_status).
+ */
+int hif8_gemm_block(const uint8_t* Aq, int64_t lda, int a_is_km, const int* d_exp_a, int64_t exp_stride_a, int a_block_rows, const uint8_t* Wq, int64_t ldw,
+                    int w_is_nk, const int* d_exp_w, int64_t exp_stride_w, int w_block_rows, void* C, int64_t ldc, int c_dtype, int M, int N, int K, int accumulate,
+                    void* workspace, size_t workspace_bytes, hif8_stream_t stream);
+size_t hif8_gemm_block_workspace_bytes(int M, int N, int K, int a_is_km, int w_is_nk, int w_block_rows);
+
+/*
+ * The global norm of all gradients and clipping, behind a backward pass under a loss scale of 2^s (Section 5.1, ALS):
+ *   *d_norm = sqrt(sum g^2) * 2^-s over all elements of all tensors;  dst = g * 2^-s * min(1, max_norm / norm), rounded once to the tensor's type
+ * A list of tensors in device memory: d_src [n_tensors] addresses, d_dst the same for the results (NULL, or equal entries: in place; otherwise no result may overlap a
+ * gradient), d_dtype [n_tensors] element formats, d_start [n_tensors + 1] running sums of the tensors' numbers of elements, from 0 to n_elements.  (They have to be right: the library
+ * cannot check them; a tensor of no known format is left out.)  Addresses are aligned to their elements; 16-byte aligned ones take the vectorised path.
+ *   d_scale_exp: device int s, the first int of the state of hif8_als_state_init, for instance (NULL: 0);  max_norm > 0, +Inf for no clipping (HIF8_ERR_SCALE_RANGE).
+ *   A norm beyond FP32 is stored as +Inf and clipped to all the same.  Gradients that are not all finite: nothing is written to dst, *d_norm = +Inf and *d_found_inf |= 1 (as hif8_check_finite; either pointer may be NULL).
+ * Squares are summed in FP64 in a fixed order: results are reproducible.  workspace: hif8_grad_clip_workspace_bytes() bytes, 256-byte aligned, for one call at a time.
+ */
+int hif8_grad_clip(const uint64_t* d_src, const uint64_t* d_dst, const int* d_dtype, const int64_t* d_start, int n_tensors, int64_t n_elements, const int* d_scale_exp,
+                   float max_norm, float* d_norm, int* d_found_inf, void* workspace, size_t workspace_bytes, hif8_stream_t stream);
+size_t hif8_grad_clip_workspace_bytes(void);
+
 /* bytes of device workspace a call needs (which = HIF8_WS_*; n = element count; for HIF8_WS_GEMM: 0 for the
  * minimum, or M*K + K*N for the decode-once path) */
 size_t hif8_workspace_bytes(int which, size_t n);

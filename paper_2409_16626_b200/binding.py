@@ -22,6 +22,7 @@ OK = 0
 SCALE_STATE_BYTES, SCALE_HISTORY_MAX = 1024, 32
 ALS_STATE_BYTES = 64
 CACHE_MAX_SEQS, CACHE_MAX_HEADS, CACHE_MAX_GROUP, CACHE_EXP_MAX = 2048, 128, 64, 48
+BLOCK, BLOCK_EXP_MAX, NORM_MAX_COLS = 128, 96, 32768
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libhif8.so")
@@ -29,7 +30,8 @@ EXPORTS = ["hif8_encode", "hif8_decode", "hif8_amax", "hif8_amax_scale_encode", 
            "hif8_pts_status", "hif8_selftest_wait_timeout", "hif8_channel_amax_scale_encode", "hif8_gemm_channel_scaled",
            "hif8_scale_state_init", "hif8_delayed_scale_encode", "hif8_gemm_ex", "hif8_encode_transpose", "hif8_als_state_init", "hif8_als_update", "hif8_check_finite", "hif8_encode_from_amax",
            "hif8_amax_scale_encode_static", "hif8_encode_f32_patterns", "hif8_last_device_status", "hif8_selftest_host_caches", "hif8_cache_append", "hif8_cache_read", "hif8_cache_attention", "hif8_cache_attention_workspace_bytes", "hif8_cache_fork", "hif8_cache_compact",
-           "hif8_cache_compact_workspace_bytes", "hif8_gemm_path_policy", "hif8_workspace_bytes", "hif8_status_string", "hif8_launch_count"]
+           "hif8_cache_compact_workspace_bytes", "hif8_block_encode", "hif8_block_decode", "hif8_rmsnorm_encode", "hif8_rmsnorm_backward", "hif8_rmsnorm_backward_workspace_bytes",
+           "hif8_gemm_block", "hif8_gemm_block_workspace_bytes", "hif8_grad_clip", "hif8_grad_clip_workspace_bytes", "hif8_gemm_path_policy", "hif8_workspace_bytes", "hif8_status_string", "hif8_launch_count"]
 
 for _path in (LIB_PATH, CALL_PATH):
     if not os.path.exists(_path):
@@ -105,6 +107,24 @@ lib.hif8_cache_compact.argtypes = _cache + [_vp, _i, _i, _vp, _vp, _vp, _sz, _vp
 lib.hif8_cache_compact.restype = _i
 lib.hif8_cache_compact_workspace_bytes.argtypes = [_i]
 lib.hif8_cache_compact_workspace_bytes.restype = _sz
+lib.hif8_block_encode.argtypes = [_vp, _i, _i64, _i64, _i64, _i, _vp, _i64, _vp, _i64, _i, _i, _u, _u64, _vp]
+lib.hif8_block_encode.restype = _i
+lib.hif8_block_decode.argtypes = [_vp, _i64, _vp, _i64, _i64, _i64, _i, _vp, _i, _i64, _vp]
+lib.hif8_block_decode.restype = _i
+lib.hif8_rmsnorm_encode.argtypes = [_vp, _i64, _vp, _i64, _i, _vp, C.c_float, _i64, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _i, _i, _u, _vp]
+lib.hif8_rmsnorm_encode.restype = _i
+lib.hif8_rmsnorm_backward.argtypes = [_vp, _i64, _vp, _i64, _vp, _i64, _i, _vp, _vp, _i64, _i64, _vp, _i64, _vp, _i, _vp, _sz, _vp]
+lib.hif8_rmsnorm_backward.restype = _i
+lib.hif8_rmsnorm_backward_workspace_bytes.argtypes = [_i64, _i64]
+lib.hif8_rmsnorm_backward_workspace_bytes.restype = _sz
+lib.hif8_gemm_block.argtypes = [_vp, _i64, _i, _vp, _i64, _i, _vp, _i64, _i, _vp, _i64, _i, _vp, _i64, _i, _i, _i, _i, _i, _vp, _sz, _vp]
+lib.hif8_gemm_block.restype = _i
+lib.hif8_gemm_block_workspace_bytes.argtypes = [_i] * 6
+lib.hif8_gemm_block_workspace_bytes.restype = _sz
+lib.hif8_grad_clip.argtypes = [_vp, _vp, _vp, _vp, _i, _i64, _vp, C.c_float, _vp, _vp, _vp, _sz, _vp]
+lib.hif8_grad_clip.restype = _i
+lib.hif8_grad_clip_workspace_bytes.argtypes = []
+lib.hif8_grad_clip_workspace_bytes.restype = _sz
 lib.hif8_workspace_bytes.argtypes = [_i, _sz]
 lib.hif8_workspace_bytes.restype = _sz
 lib.hif8_status_string.argtypes = [_i]
@@ -382,6 +402,67 @@ def hif8_cache_compact(k_pages, v_pages, k_exp, v_exp, n_pages, kv_heads, page_t
             d_free_pages, workspace, workspace_bytes, stream)
     rc = _c.hif8_cache_compact(*args)
     return _check(_via_ctypes("hif8_cache_compact", args) if rc is None else rc, check)
+
+
+def hif8_block_encode(src, src_dtype, ld_src, rows, cols, block_rows, dst, ld_dst, d_exp, exp_stride, target_exp=3, rnd=RND_TA, flags=0, seed=0, stream=None, check=True):
+    """Values to codes with a scale for each block of 1 x 128 or 128 x 128."""
+    args = (src, src_dtype, ld_src, rows, cols, block_rows, dst, ld_dst, d_exp, exp_stride, target_exp, rnd, flags, seed, stream)
+    rc = _c.hif8_block_encode(*args)
+    return _check(_via_ctypes("hif8_block_encode", args) if rc is None else rc, check)
+
+
+def hif8_block_decode(src, ld_src, d_exp, exp_stride, rows, cols, block_rows, dst, dst_dtype, ld_dst, stream=None, check=True):
+    """Codes with a scale for each block back to values."""
+    args = (src, ld_src, d_exp, exp_stride, rows, cols, block_rows, dst, dst_dtype, ld_dst, stream)
+    rc = _c.hif8_block_decode(*args)
+    return _check(_via_ctypes("hif8_block_decode", args) if rc is None else rc, check)
+
+
+def hif8_rmsnorm_encode(x, ld_x, residual, ld_residual, dtype, weight, eps, rows, cols, h, ld_h, d_rstd, dst, ld_dst, d_exp, exp_stride, target_exp=3, rnd=RND_TA, flags=0,
+                        stream=None, check=True):
+    """The residual's addition and the root-mean-square norm, the result as codes with a scale for each 1 x 128."""
+    args = (x, ld_x, residual, ld_residual, dtype, weight, eps, rows, cols, h, ld_h, d_rstd, dst, ld_dst, d_exp, exp_stride, target_exp, rnd, flags, stream)
+    rc = _c.hif8_rmsnorm_encode(*args)
+    return _check(_via_ctypes("hif8_rmsnorm_encode", args) if rc is None else rc, check)
+
+
+def hif8_rmsnorm_backward_workspace_bytes(rows, cols):
+    n = _c.hif8_rmsnorm_backward_workspace_bytes(rows, cols)
+    return int(lib.hif8_rmsnorm_backward_workspace_bytes(rows, cols)) if n is None else n
+
+
+def hif8_rmsnorm_backward(dy, ld_dy, h, ld_h, dh, ld_dh, dtype, weight, d_rstd, rows, cols, dx, ld_dx, d_weight_grad=None, accumulate=0, workspace=None, workspace_bytes=0,
+                          stream=None, check=True):
+    """The gradients of hif8_rmsnorm_encode's x (and residual) and weight."""
+    args = (dy, ld_dy, h, ld_h, dh, ld_dh, dtype, weight, d_rstd, rows, cols, dx, ld_dx, d_weight_grad, int(accumulate), workspace, workspace_bytes, stream)
+    rc = _c.hif8_rmsnorm_backward(*args)
+    return _check(_via_ctypes("hif8_rmsnorm_backward", args) if rc is None else rc, check)
+
+
+def hif8_gemm_block_workspace_bytes(M, N, K, a_is_km, w_is_nk, w_block_rows):
+    n = _c.hif8_gemm_block_workspace_bytes(M, N, K, a_is_km, w_is_nk, w_block_rows)
+    return int(lib.hif8_gemm_block_workspace_bytes(M, N, K, int(a_is_km), int(w_is_nk), w_block_rows)) if n is None else n
+
+
+def hif8_gemm_block(Aq, lda, a_is_km, d_exp_a, exp_stride_a, a_block_rows, Wq, ldw, w_is_nk, d_exp_w, exp_stride_w, w_block_rows, Cmat, ldc, c_dtype, M, N, K, accumulate=0,
+                    workspace=None, workspace_bytes=0, stream=None, check=True):
+    """The product of two matrices of codes with a scale for each block."""
+    args = (Aq, lda, int(a_is_km), d_exp_a, exp_stride_a, a_block_rows, Wq, ldw, int(w_is_nk), d_exp_w, exp_stride_w, w_block_rows, Cmat, ldc, c_dtype, M, N, K, int(accumulate),
+            workspace, workspace_bytes, stream)
+    rc = _c.hif8_gemm_block(*args)
+    return _check(_via_ctypes("hif8_gemm_block", args) if rc is None else rc, check)
+
+
+def hif8_grad_clip_workspace_bytes():
+    n = _c.hif8_grad_clip_workspace_bytes()
+    return int(lib.hif8_grad_clip_workspace_bytes()) if n is None else n
+
+
+def hif8_grad_clip(d_src, d_dst, d_dtype, d_start, n_tensors, n_elements, d_scale_exp, max_norm, d_norm, d_found_inf, workspace, workspace_bytes, stream=None, check=True):
+    """The global norm of a list of gradients under a loss scale, and the gradients unscaled and clipped to it."""
+    args = (d_src, d_dst, d_dtype, d_start, n_tensors, n_elements, d_scale_exp, max_norm, d_norm, d_found_inf, workspace, workspace_bytes, stream)
+    rc = _c.hif8_grad_clip(*args)
+    return _check(_via_ctypes("hif8_grad_clip", args) if rc is None else rc, check)
 
 
 # the names that the package itself offers (see the package's __getattr__)

@@ -1,0 +1,384 @@
+// Block-scaled matrices: conversion to HiF8 with one power-of-two scale for each 1 x 128 or 128 x 128 elements, back, and into BF16 as
+// operands of a product.
+//
+//   e = clamp(target_exp - floor(log2 amax)),  code = To_HiF8(x 2^e),  x ~ value(code) 2^-e
+//
+// All of it is bound by memory: every element is read once.  Sixteen threads hold a block's width, eight elements each, so a block's maximum
+// takes four exchanges within half a warp; a block of 128 rows is one thread block's, held in registers between its maximum and its codes.
+#include "hif8_block.cuh"
+
+namespace hif8 {
+namespace {
+
+struct EncodeParams {
+    const void* src;
+    long long ld_src;
+    BlockCodes m;
+    FastDiv across;       // blocks of a row
+    unsigned units;       // 1 x 128: blocks of the matrix; 128 x 128: the same
+    int target_exp;
+    unsigned flags;
+    unsigned long long seed;
+    bool vectors, codes8;  // rows of the source start on 16-byte boundaries, those of the codes on 8-byte ones
+};
+
+// eight elements -> codes; `flat`: the flat index of the first one (stochastic rounding draws by it)
+template <int SRC, int MODE>
+__device__ __forceinline__ uint2 encode_eight(const Eight<SRC>& e, float scale, const SmemTables& sm, unsigned long long flat, unsigned long long seed)
+{
+    if (MODE == HIF8_RND_TA && SRC == HIF8_BF16) {
+        const uint32_t s2 = bf16x2_of_pow2(scale);
+        const uint32_t scales2[4] = {s2, s2, s2, s2};
+        const float scales[8] = {scale, scale, scale, scale, scale, scale, scale, scale};
+        return encode_vector_ta<SRC>(e.v[0], scales2, scales, sm.ta);
+    }
+    uint32_t w[2] = {0u, 0u};
+    uint4 draws = make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        float x; uint32_t raw, word = 0;
+        unpack_eight<SRC>(e, i, x, raw);
+        if (MODE == HIF8_RND_SR) {
+            const unsigned long long at = flat + i;
+            if (i == 0 || (at & 3u) == 0) draws = philox4x32_10((uint32_t)(at >> 2), (uint32_t)(at >> 34), (uint32_t)seed, (uint32_t)(seed >> 32));
+            word = philox_word(draws, (unsigned)at & 3u);
+        }
+        w[i >> 2] |= (encode_one<MODE, SRC>(x, raw, scale, sm.ta, sm.thr, word) & 0xFFu) << (8 * (i & 3));
+    }
+    return make_uint2(w[0], w[1]);
+}
+
+template <int SRC>
+__device__ __forceinline__ uint32_t amax_of_eight(const Eight<SRC>& e)
+{
+    uint32_t m = amax_vector<SRC>(0u, e.v[0]);
+    if (SRC == HIF8_F32) m = amax_vector<SRC>(m, e.v[sizeof(e.v) / 16 - 1]);
+    return __float_as_uint(amax_value<SRC>(m));
+}
+
+// Blocks of 1 x 128: a warp takes 2 UN consecutive ones at a time, half a warp every other one.
+template <int SRC, int MODE, int UN>
+__global__ void __launch_bounds__(kThreads) block_row_encode_kernel(const EncodeParams p)
+{
+    __shared__ SmemTables sm;
+    setup_tables<true, MODE != HIF8_RND_TA, false, MODE, SRC>(sm, p.flags);
+    pdl_wait_prior_grid();
+    pdl_launch_dependents();
+    constexpr size_t item = SRC == HIF8_F32 ? 4 : 2;
+    const unsigned lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, half = lane >> 4, at = (lane & 15u) * 8u;
+    const unsigned warps = gridDim.x * (kThreads / 32);
+    for (unsigned long long first = (unsigned long long)(blockIdx.x * (kThreads / 32) + warp) * (2 * UN); first < p.units; first += (unsigned long long)warps * (2 * UN)) {
+        unsigned row[UN], blk[UN];
+        Eight<SRC> e[UN];
+#pragma unroll
+        for (int j = 0; j < UN; j++) {
+            const unsigned u = (unsigned)first + half + 2 * j;
+            row[j] = p.across.div(u); blk[j] = u - row[j] * p.across.d;
+            const long long c = (long long)blk[j] * 128 + at;
+            e[j] = load_eight<SRC>(reinterpret_cast<const char*>(p.src) + (size_t)row[j] * (size_t)p.ld_src * item, u < p.units ? c : p.m.cols, p.m.cols, p.vectors);
+        }
+#pragma unroll
+        for (int j = 0; j < UN; j++) {
+            const uint32_t top = half_warp_max(amax_of_eight<SRC>(e[j]));
+            const int se = block_exp_from_amax(top, p.target_exp);
+            if ((unsigned)first + half + 2 * j >= p.units) continue;
+            const long long c = (long long)blk[j] * 128 + at;
+            if (c < p.m.cols) {
+                const uint2 w = encode_eight<SRC, MODE>(e[j], pow2f(se), sm, (unsigned long long)row[j] * (unsigned long long)p.m.cols + (unsigned long long)c, p.seed);
+                store_codes8(p.m.codes + (size_t)row[j] * (size_t)p.m.ld, c, p.m.cols, p.codes8, w);
+            }
+            if (at == 0) p.m.exps[(size_t)row[j] * (size_t)p.m.exp_stride + blk[j]] = se;
+        }
+    }
+}
+
+// Blocks of 128 x 128: a thread block takes one at a time, half a warp eight of its rows.
+template <int SRC, int MODE>
+__global__ void __launch_bounds__(kThreads) block_tile_encode_kernel(const EncodeParams p)
+{
+    __shared__ SmemTables sm;
+    __shared__ uint32_t s_top[2][kThreads / 32];
+    setup_tables<true, MODE != HIF8_RND_TA, false, MODE, SRC>(sm, p.flags);
+    pdl_wait_prior_grid();
+    pdl_launch_dependents();
+    constexpr size_t item = SRC == HIF8_F32 ? 4 : 2;
+    constexpr int kRows = 128 / (kThreads / 16);
+    const unsigned at = (threadIdx.x & 15u) * 8u, r0 = threadIdx.x >> 4;
+    int turn = 0;
+    for (unsigned u = blockIdx.x; u < p.units; u += gridDim.x, turn ^= 1) {
+        const unsigned down = p.across.div(u), blk = u - down * p.across.d;
+        const long long c = (long long)blk * 128 + at, row = (long long)down * 128 + r0;
+        Eight<SRC> e[kRows];
+        uint32_t top = 0;
+#pragma unroll
+        for (int j = 0; j < kRows; j++) {
+            const long long r = row + j * (kThreads / 16);
+            e[j] = load_eight<SRC>(reinterpret_cast<const char*>(p.src) + (size_t)r * (size_t)p.ld_src * item, r < p.m.rows ? c : p.m.cols, p.m.cols, p.vectors);
+        }
+#pragma unroll
+        for (int j = 0; j < kRows; j++) top = max(top, amax_of_eight<SRC>(e[j]));
+        top = __reduce_max_sync(0xFFFFFFFFu, top);
+        if ((threadIdx.x & 31u) == 0) s_top[turn][threadIdx.x >> 5] = top;
+        __syncthreads();  // (two sets of words in turn: whoever still reads the other one has not passed this barrier)
+        top = 0;
+#pragma unroll
+        for (int w = 0; w < kThreads / 32; w++) top = max(top, s_top[turn][w]);
+        const int se = block_exp_from_amax(top, p.target_exp);
+        if (threadIdx.x == 0) p.m.exps[(size_t)down * (size_t)p.m.exp_stride + blk] = se;
+        const float scale = pow2f(se);
+        if (c < p.m.cols) {
+#pragma unroll
+            for (int j = 0; j < kRows; j++) {
+                const long long r = row + j * (kThreads / 16);
+                if (r >= p.m.rows) continue;
+                const uint2 w = encode_eight<SRC, MODE>(e[j], scale, sm, (unsigned long long)r * (unsigned long long)p.m.cols + (unsigned long long)c, p.seed);
+                store_codes8(p.m.codes + (size_t)r * (size_t)p.m.ld, c, p.m.cols, p.codes8, w);
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// codes -> values
+// ------------------------------------------------------------------------------------------------
+struct DecodeParams {
+    BlockCodes m;
+    void* dst;
+    long long ld_dst, rows_out, cols_out;
+    FastDiv chunks;      // groups of eight columns of a row that is written
+    unsigned units;      // such groups
+    bool codes8, vectors;  // rows of the codes start on 8-byte boundaries, those written on 16-byte ones
+    uint32_t* clear_word;
+};
+
+__device__ __forceinline__ int exp_at(const BlockCodes& m, long long r, long long c)
+{
+    return clamp_block_exp(__ldg(m.exps + (size_t)(r >> m.shift) * (size_t)m.exp_stride + (size_t)(c >> 7)));
+}
+
+// four codes through a table of one word per code (LANE: a copy per lane), as two words of two BF16
+template <bool LANE>
+__device__ __forceinline__ uint2 bf16_of_four(const uint32_t* table, uint32_t w, uint32_t lane4)
+{
+    if (LANE) return lane_lookup4(table, w, lane4);
+    return make_uint2(table[w & 0xFFu] | (table[(w >> 8) & 0xFFu] << 16), table[(w >> 16) & 0xFFu] | (table[w >> 24] << 16));
+}
+
+template <int DST>
+__device__ __forceinline__ Eight<DST> scaled_eight(uint2 lo, uint2 hi, int e)
+{
+    if (DST == HIF8_BF16) {  // (exact, no subnormals: |e| is at most 96)
+        const uint32_t s = bf16x2_of_pow2(pow2f(-e));
+        Eight<DST> r;
+        r.v[0] = make_uint4(mul_bf16x2(lo.x, s), mul_bf16x2(lo.y, s), mul_bf16x2(hi.x, s), mul_bf16x2(hi.y, s));
+        return r;
+    }
+    const uint32_t w[4] = {lo.x, lo.y, hi.x, hi.y};
+    const float s = pow2f(-e);
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) x[i] = __uint_as_float((i & 1) ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16) * s;
+    return pack_eight<DST>(x);
+}
+
+// LANE: a copy of the table for each lane.  One table for all costs a warp several wavefronts a lookup; filling 32 copies costs a block more than a
+// small matrix takes.
+template <int DST, bool LANE, int UN>
+__global__ void __launch_bounds__(kThreads) block_decode_kernel(const DecodeParams p)
+{
+    __shared__ __align__(16) uint32_t table[LANE ? kLaneTableWords : 256];
+    if (LANE) fill_lane_table(table, decode_bits_f32(threadIdx.x) >> 16);
+    else table[threadIdx.x] = decode_bits_f32(threadIdx.x) >> 16;
+    __syncthreads();
+    pdl_wait_prior_grid();
+    pdl_launch_dependents();
+    if (p.clear_word && blockIdx.x == 0 && threadIdx.x == 0) *p.clear_word = 0u;
+    const uint32_t lane4 = (threadIdx.x & 31u) * 4u;
+    for (unsigned long long base = (unsigned long long)blockIdx.x * (kThreads * UN) + threadIdx.x; base < p.units; base += (unsigned long long)gridDim.x * (kThreads * UN)) {
+        uint2 v[UN];
+        int e[UN];
+#pragma unroll
+        for (int j = 0; j < UN; j++) {
+            const unsigned u = (unsigned)base + j * kThreads;
+            const unsigned row = p.chunks.div(u), c = (u - row * p.chunks.d) * 8u;
+            const bool inside = u < p.units && row < p.m.rows && c < p.m.cols;
+            v[j] = inside ? load_codes8(p.m.codes + (size_t)row * (size_t)p.m.ld, c, p.m.cols, p.codes8) : make_uint2(0u, 0u);
+            e[j] = inside ? exp_at(p.m, row, c) : 0;
+        }
+#pragma unroll
+        for (int j = 0; j < UN; j++) {
+            const unsigned u = (unsigned)base + j * kThreads;
+            if (u >= p.units) continue;
+            const unsigned row = p.chunks.div(u), c = (u - row * p.chunks.d) * 8u;
+            const Eight<DST> x = scaled_eight<DST>(bf16_of_four<LANE>(table, v[j].x, lane4), bf16_of_four<LANE>(table, v[j].y, lane4), e[j]);
+            store_eight<DST>(reinterpret_cast<char*>(p.dst) + (size_t)row * (size_t)p.ld_dst * (DST == HIF8_F32 ? 4 : 2), c, p.cols_out, p.vectors, x);
+        }
+    }
+}
+
+// Codes [rows, cols] -> BF16 [cols, ld_dst], transposed: tiles of 64 rows by 64 columns.  A thread takes two rows' eight columns and puts a column's two
+// values into one word, lines of 33 words apart: eight row pairs and four groups of columns to a warp meet in no bank, and read whole 32-byte sectors.
+constexpr int kFlipRows = 64, kFlipCols = 64, kFlipLine = kFlipRows / 2 + 1;
+template <bool LANE>
+__global__ void __launch_bounds__(kThreads) block_decode_transpose_kernel(const DecodeParams p)
+{
+    __shared__ __align__(16) uint32_t table[LANE ? kLaneTableWords : 256];
+    __shared__ uint32_t tile[kFlipCols * kFlipLine];
+    if (LANE) fill_lane_table(table, decode_bits_f32(threadIdx.x) >> 16);
+    else table[threadIdx.x] = decode_bits_f32(threadIdx.x) >> 16;
+    __syncthreads();
+    pdl_wait_prior_grid();
+    pdl_launch_dependents();
+    if (p.clear_word && blockIdx.x == 0 && threadIdx.x == 0) *p.clear_word = 0u;
+    const unsigned lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    const uint32_t lane4 = lane * 4u;
+    for (unsigned t = blockIdx.x; t < p.units; t += gridDim.x) {  // p.chunks: tiles across
+        const unsigned down = p.chunks.div(t), across = t - down * p.chunks.d;
+        const long long r0 = (long long)down * kFlipRows, c0 = (long long)across * kFlipCols;
+        uint2 v[2];
+        int e[2];
+        const unsigned group = (warp & 1u) * 4u + (lane & 3u), pair = (warp >> 1) * 8u + (lane >> 2);  // eight groups of columns by 32 row pairs
+        const long long c = c0 + group * 8u;
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const long long r = r0 + 2 * pair + i;
+            const bool inside = r < p.m.rows && c < p.m.cols;
+            v[i] = inside ? load_codes8(p.m.codes + (size_t)r * (size_t)p.m.ld, c, p.m.cols, p.codes8) : make_uint2(0u, 0u);
+            e[i] = inside ? exp_at(p.m, r, c) : 0;
+        }
+        const Eight<HIF8_BF16> a = scaled_eight<HIF8_BF16>(bf16_of_four<LANE>(table, v[0].x, lane4), bf16_of_four<LANE>(table, v[0].y, lane4), e[0]);
+        const Eight<HIF8_BF16> b = scaled_eight<HIF8_BF16>(bf16_of_four<LANE>(table, v[1].x, lane4), bf16_of_four<LANE>(table, v[1].y, lane4), e[1]);
+        const uint32_t x[4] = {a.v[0].x, a.v[0].y, a.v[0].z, a.v[0].w}, y[4] = {b.v[0].x, b.v[0].y, b.v[0].z, b.v[0].w};
+#pragma unroll
+        for (int i = 0; i < 8; i++) tile[(group * 8 + i) * kFlipLine + pair] = __byte_perm(x[i >> 1], y[i >> 1], (i & 1) ? 0x7632 : 0x5410);
+        __syncthreads();
+        for (unsigned k = warp; k < kFlipCols; k += kThreads / 32) {
+            const long long at = c0 + k, r = r0 + 2 * lane;
+            if (at < p.m.cols && r < p.rows_out) *reinterpret_cast<uint32_t*>(reinterpret_cast<unsigned short*>(p.dst) + (size_t)at * (size_t)p.ld_dst + r) = tile[k * kFlipLine + lane];
+        }
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// host side
+// ------------------------------------------------------------------------------------------------
+int finish(int launches)
+{
+    g_launches.fetch_add((uint64_t)launches, std::memory_order_relaxed);
+    return cudaGetLastError() == cudaSuccess ? HIF8_OK : HIF8_ERR_CUDA;
+}
+
+template <int SRC, int MODE>
+void launch_encode(const EncodeParams& p, int sms, cudaStream_t st)
+{
+    if (p.m.shift == 7) {
+        const unsigned most = (unsigned)sms * 6u;
+        launch_pdl(block_tile_encode_kernel<SRC, MODE>, dim3(p.units < most ? p.units : most), st, p);
+        return;
+    }
+    // (a warp that has one pair of blocks waits for memory once; with four pairs, which large matrices need to keep memory busy, it converts them one after the other)
+    const unsigned most = (unsigned)sms * 8u, blocks1 = (p.units + 15u) / 16u, blocks4 = (p.units + 63u) / 64u;
+    if (blocks1 <= most) launch_pdl(block_row_encode_kernel<SRC, MODE, 1>, dim3(blocks1), st, p);
+    else launch_pdl(block_row_encode_kernel<SRC, MODE, 4>, dim3(blocks4 < most ? blocks4 : most), st, p);
+}
+template <int SRC>
+void launch_encode_mode(int rnd, const EncodeParams& p, int sms, cudaStream_t st)
+{
+    switch (rnd) {
+        case HIF8_RND_TA: return launch_encode<SRC, HIF8_RND_TA>(p, sms, st);
+        case HIF8_RND_HR: return launch_encode<SRC, HIF8_RND_HR>(p, sms, st);
+        case HIF8_RND_SSR: return launch_encode<SRC, HIF8_RND_SSR>(p, sms, st);
+        case HIF8_RND_TE: return launch_encode<SRC, HIF8_RND_TE>(p, sms, st);
+        default: return launch_encode<SRC, HIF8_RND_SR>(p, sms, st);
+    }
+}
+
+template <int DST>
+void launch_decode(const DecodeParams& p, int sms, cudaStream_t st)
+{
+    const unsigned most = (unsigned)sms * 6u, few = (p.units + kThreads - 1) / kThreads, blocks = (p.units + 4 * kThreads - 1) / (4 * kThreads);
+    if (few <= (unsigned)sms * 8u) launch_pdl(block_decode_kernel<DST, false, 1>, dim3(few), st, p);
+    else launch_pdl(block_decode_kernel<DST, true, 4>, dim3(blocks < most ? blocks : most), st, p);
+}
+
+}  // namespace
+
+int expand_block_codes(const BlockCodes& m, void* dst, long long ld_dst, long long rows_out, long long cols_out, bool transposed, uint32_t* clear_word, cudaStream_t st)
+{
+    int sms; if (int rc = checked_device(&sms)) return rc;
+    DecodeParams p{};
+    p.m = m; p.dst = dst; p.ld_dst = ld_dst; p.rows_out = rows_out; p.cols_out = cols_out; p.clear_word = clear_word;
+    p.codes8 = aligned_to(m.codes, 8) && (m.rows <= 1 || (m.ld & 7) == 0);
+    p.vectors = true;
+    const long long across = transposed ? (cols_out + kFlipCols - 1) / kFlipCols : (cols_out + 7) / 8;
+    const long long down = transposed ? (rows_out + kFlipRows - 1) / kFlipRows : rows_out;
+    if (across > 0x7FFFFFFFll / (down > 0 ? down : 1)) return HIF8_ERR_SHAPE;
+    p.chunks = FastDiv((uint32_t)across); p.units = (unsigned)(across * down);
+    if (transposed) {
+        const unsigned most = (unsigned)sms * 4u;
+        if (p.units <= (unsigned)sms * 2u) launch_pdl(block_decode_transpose_kernel<false>, dim3(p.units), st, p);
+        else launch_pdl(block_decode_transpose_kernel<true>, dim3(p.units < most ? p.units : most), st, p);
+    } else launch_decode<HIF8_BF16>(p, sms, st);
+    return finish(1);
+}
+
+}  // namespace hif8
+
+using namespace hif8;
+
+extern "C" int hif8_block_encode(const void* src, int src_dtype, int64_t ld_src, int64_t rows, int64_t cols, int block_rows, uint8_t* dst, int64_t ld_dst, int* d_exp,
+                                 int64_t exp_stride, int target_exp, int rnd, unsigned flags, uint64_t seed, hif8_stream_t stream)
+{
+    if (bad_dtype(src_dtype)) return HIF8_ERR_DTYPE;
+    if (rnd < HIF8_RND_TA || rnd > HIF8_RND_SR) return HIF8_ERR_ROUND;
+    if (flags & ~(unsigned)(HIF8_FLAG_SATURATE | HIF8_FLAG_NAN_TO_ZERO)) return HIF8_ERR_FLAGS;
+    if (target_exp < -22 || target_exp > 15) return HIF8_ERR_SCALE_RANGE;
+    if (rows < 0 || cols < 0 || (block_rows != 1 && block_rows != HIF8_BLOCK)) return HIF8_ERR_SHAPE;
+    EncodeParams p{};
+    p.m = BlockCodes{dst, ld_dst, d_exp, exp_stride, rows, cols, block_rows == 1 ? 0 : 7};
+    if (ld_src < cols || ld_dst < cols || exp_stride < p.m.blocks_across()) return HIF8_ERR_SHAPE;
+    if (rows == 0 || cols == 0) return HIF8_OK;
+    if (!src || !dst || !d_exp) return HIF8_ERR_NULL;
+    if (p.m.blocks_across() > 0x7FFFFFFFll / p.m.blocks_down()) return HIF8_ERR_SHAPE;
+    const size_t item = dtype_bytes(src_dtype);
+    if (!aligned_to(src, item) || !aligned_to(d_exp, sizeof(int))) return HIF8_ERR_ALIGN;
+    if (written_over({{dst, p.m.code_bytes()}, {d_exp, p.m.exp_bytes()}}, {{src, matrix_bytes(rows, cols, ld_src, item)}})) return HIF8_ERR_OVERLAP;
+    int sms; if (int rc = checked_device(&sms)) return rc;
+    p.src = src; p.ld_src = ld_src; p.target_exp = target_exp; p.flags = flags; p.seed = seed;
+    p.across = FastDiv((uint32_t)p.m.blocks_across()); p.units = (unsigned)(p.m.blocks_across() * p.m.blocks_down());
+    p.vectors = vector_rows(src, rows, ld_src, item);
+    p.codes8 = aligned_to(dst, 8) && (rows <= 1 || (ld_dst & 7) == 0);
+    cudaStream_t st = (cudaStream_t)stream;
+    if (src_dtype == HIF8_F32) launch_encode_mode<HIF8_F32>(rnd, p, sms, st);
+    else if (src_dtype == HIF8_BF16) launch_encode_mode<HIF8_BF16>(rnd, p, sms, st);
+    else launch_encode_mode<HIF8_F16>(rnd, p, sms, st);
+    return finish(1);
+}
+
+extern "C" int hif8_block_decode(const uint8_t* src, int64_t ld_src, const int* d_exp, int64_t exp_stride, int64_t rows, int64_t cols, int block_rows, void* dst, int dst_dtype,
+                                 int64_t ld_dst, hif8_stream_t stream)
+{
+    if (bad_dtype(dst_dtype)) return HIF8_ERR_DTYPE;
+    if (rows < 0 || cols < 0 || (block_rows != 1 && block_rows != HIF8_BLOCK)) return HIF8_ERR_SHAPE;
+    DecodeParams p{};
+    p.m = BlockCodes{const_cast<uint8_t*>(src), ld_src, const_cast<int*>(d_exp), exp_stride, rows, cols, block_rows == 1 ? 0 : 7};
+    if (ld_src < cols || ld_dst < cols || exp_stride < p.m.blocks_across()) return HIF8_ERR_SHAPE;
+    if (rows == 0 || cols == 0) return HIF8_OK;
+    if (!src || !dst || !d_exp) return HIF8_ERR_NULL;
+    const long long across = (cols + 7) / 8;
+    if (across > 0x7FFFFFFFll / rows) return HIF8_ERR_SHAPE;
+    const size_t item = dtype_bytes(dst_dtype);
+    if (!aligned_to(dst, item) || !aligned_to(d_exp, sizeof(int))) return HIF8_ERR_ALIGN;
+    if (written_over({{dst, matrix_bytes(rows, cols, ld_dst, item)}}, {{src, p.m.code_bytes()}, {d_exp, p.m.exp_bytes()}})) return HIF8_ERR_OVERLAP;
+    int sms; if (int rc = checked_device(&sms)) return rc;
+    p.dst = dst; p.ld_dst = ld_dst; p.rows_out = rows; p.cols_out = cols;
+    p.chunks = FastDiv((uint32_t)across); p.units = (unsigned)(across * rows);
+    p.codes8 = aligned_to(src, 8) && (rows <= 1 || (ld_src & 7) == 0);
+    p.vectors = vector_rows(dst, rows, ld_dst, item);
+    cudaStream_t st = (cudaStream_t)stream;
+    if (dst_dtype == HIF8_F32) launch_decode<HIF8_F32>(p, sms, st);
+    else if (dst_dtype == HIF8_BF16) launch_decode<HIF8_BF16>(p, sms, st);
+    else launch_decode<HIF8_F16>(p, sms, st);
+    return finish(1);
+}

@@ -1,0 +1,153 @@
+// What the kernels of block-scaled matrices share: a thread's eight neighbouring elements of a row, sixteen threads to a block's width.
+#pragma once
+#include "hif8_block_types.cuh"
+#include "hif8_device.cuh"
+
+namespace hif8 {
+namespace {
+
+// n / d for n < 2^31 by a multiplication and a shift (Granlund and Montgomery, 1994)
+struct FastDiv {
+    uint32_t d, mul, shift;
+    FastDiv() = default;
+    explicit FastDiv(uint32_t d_) : d(d_), shift(0)
+    {
+        while ((1ull << shift) < d) shift++;
+        mul = (uint32_t)((((1ull << shift) - d) << 32) / d + 1);
+    }
+    __device__ __forceinline__ uint32_t div(uint32_t n) const { return (__umulhi(mul, n) + n) >> shift; }
+};
+
+__device__ __forceinline__ int clamp_block_exp(int e) { return max(-HIF8_BLOCK_EXP_MAX, min(HIF8_BLOCK_EXP_MAX, e)); }
+__device__ __forceinline__ int block_exp_from_amax(uint32_t amax_bits, int target_exp) { return clamp_block_exp(scale_exp_from_amax(amax_bits, target_exp)); }
+
+// largest of the values of sixteen threads (the lower or the upper half of a warp)
+__device__ __forceinline__ uint32_t half_warp_max(uint32_t v)
+{
+#pragma unroll
+    for (int d = 8; d; d >>= 1) v = max(v, __shfl_xor_sync(0xFFFFFFFFu, v, d));
+    return v;
+}
+
+// Eight elements c .. c + 7 of a row of `cols`, zeros behind its end: 16 bytes, of FP32 32.  `vectors`: the row starts on a 16-byte boundary (and c is a multiple of 8).
+// KEEP: they will be read again.
+template <int DT> struct Eight { uint4 v[DT == HIF8_F32 ? 2 : 1]; };
+template <int DT, bool KEEP = false>
+__device__ __forceinline__ Eight<DT> load_eight(const void* row, long long c, long long cols, bool vectors)
+{
+    Eight<DT> e;
+    if (KEEP && vectors && c + 8 <= cols) {
+        const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(row) + c * (DT == HIF8_F32 ? 4 : 2));
+        e.v[0] = __ldg(p);
+        if (DT == HIF8_F32) e.v[sizeof(e.v) / 16 - 1] = __ldg(p + 1);
+        return e;
+    }
+    if (DT == HIF8_F32) {
+        const float* p = reinterpret_cast<const float*>(row) + c;
+        if (vectors && c + 8 <= cols) {
+            e.v[0] = __ldcs(reinterpret_cast<const uint4*>(p));
+            e.v[sizeof(e.v) / 16 - 1] = __ldcs(reinterpret_cast<const uint4*>(p) + 1);
+        } else {
+            uint32_t w[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) w[i] = c + i < cols ? __float_as_uint(__ldcs(p + i)) : 0u;
+            e.v[0] = make_uint4(w[0], w[1], w[2], w[3]);
+            e.v[sizeof(e.v) / 16 - 1] = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+    } else {
+        const unsigned short* p = reinterpret_cast<const unsigned short*>(row) + c;
+        if (vectors && c + 8 <= cols) e.v[0] = __ldcs(reinterpret_cast<const uint4*>(p));
+        else {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const uint32_t lo = c + 2 * i < cols ? __ldcs(p + 2 * i) : 0, hi = c + 2 * i + 1 < cols ? __ldcs(p + 2 * i + 1) : 0;
+                w[i] = lo | (hi << 16);
+            }
+            e.v[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+    return e;
+}
+template <int DT>
+__device__ __forceinline__ void unpack_eight(const Eight<DT>& e, int i, float& x, uint32_t& raw)
+{
+    if (DT == HIF8_F32) unpack<DT>(e.v[i >> 2], i & 3, x, raw);
+    else unpack<DT>(e.v[0], i, x, raw);
+}
+template <int DT>
+__device__ __forceinline__ float value_of_eight(const Eight<DT>& e, int i)
+{
+    float x; uint32_t raw;
+    unpack_eight<DT>(e, i, x, raw);
+    return x;
+}
+// eight values, rounded to nearest even
+template <int DT>
+__device__ __forceinline__ Eight<DT> pack_eight(const float (&x)[8])
+{
+    Eight<DT> e;
+    uint32_t w[8];
+    if (DT == HIF8_F32) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) w[i] = __float_as_uint(x[i]);
+        e.v[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        e.v[sizeof(e.v) / 16 - 1] = make_uint4(w[4], w[5], w[6], w[7]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            if (DT == HIF8_BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(x[2 * i + 1]), "f"(x[2 * i]));
+            else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(x[2 * i + 1]), "f"(x[2 * i]));
+        }
+        e.v[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    return e;
+}
+template <int DT>
+__device__ __forceinline__ void store_eight(void* row, long long c, long long cols, bool vectors, const Eight<DT>& e)
+{
+    if (DT == HIF8_F32) {
+        float* p = reinterpret_cast<float*>(row) + c;
+        if (vectors && c + 8 <= cols) {
+            *reinterpret_cast<uint4*>(p) = e.v[0];
+            reinterpret_cast<uint4*>(p)[1] = e.v[sizeof(e.v) / 16 - 1];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                if (c + i < cols) p[i] = value_of_eight<DT>(e, i);
+        }
+    } else {
+        unsigned short* p = reinterpret_cast<unsigned short*>(row) + c;
+        if (vectors && c + 8 <= cols) *reinterpret_cast<uint4*>(p) = e.v[0];
+        else {
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                float x; uint32_t raw;
+                unpack_eight<DT>(e, i, x, raw);
+                if (c + i < cols) p[i] = (unsigned short)raw;
+            }
+        }
+    }
+}
+// eight codes; `vectors`: the row starts on an 8-byte boundary
+__device__ __forceinline__ void store_codes8(uint8_t* row, long long c, long long cols, bool vectors, uint2 w)
+{
+    if (vectors && c + 8 <= cols) *reinterpret_cast<uint2*>(row + c) = w;
+    else {
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            if (c + i < cols) row[c + i] = (uint8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
+    }
+}
+__device__ __forceinline__ uint2 load_codes8(const uint8_t* row, long long c, long long cols, bool vectors)
+{
+    if (vectors && c + 8 <= cols) return __ldcs(reinterpret_cast<const uint2*>(row + c));
+    uint32_t w[2] = {0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+        if (c + i < cols) w[i >> 2] |= (uint32_t)row[c + i] << (8 * (i & 3));
+    return make_uint2(w[0], w[1]);
+}
+
+}  // namespace
+}  // namespace hif8

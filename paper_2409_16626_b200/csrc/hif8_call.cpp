@@ -127,6 +127,8 @@ PyMethodDef methods[] = {
     HIF8_ENTRY(hif8_encode_transpose), HIF8_ENTRY(hif8_encode_from_amax), HIF8_ENTRY(hif8_als_update), HIF8_ENTRY(hif8_check_finite),
     HIF8_ENTRY(hif8_cache_append), HIF8_ENTRY(hif8_cache_read), HIF8_ENTRY(hif8_cache_attention), HIF8_ENTRY(hif8_cache_fork), HIF8_ENTRY(hif8_cache_compact),
     HIF8_ENTRY(hif8_cache_attention_workspace_bytes), HIF8_ENTRY(hif8_cache_compact_workspace_bytes),
+    HIF8_ENTRY(hif8_block_encode), HIF8_ENTRY(hif8_block_decode), HIF8_ENTRY(hif8_rmsnorm_encode), HIF8_ENTRY(hif8_rmsnorm_backward), HIF8_ENTRY(hif8_gemm_block),
+    HIF8_ENTRY(hif8_grad_clip), HIF8_ENTRY(hif8_rmsnorm_backward_workspace_bytes), HIF8_ENTRY(hif8_gemm_block_workspace_bytes), HIF8_ENTRY(hif8_grad_clip_workspace_bytes),
     {"set_up", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&set_up)), METH_FASTCALL, nullptr},
     {"set_cuda_ready", &set_cuda_ready, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};

@@ -496,6 +496,26 @@ __device__ __forceinline__ void stage_chunk_bf16(uint32_t box, int row, int piec
         sts_v4(line + ((uint32_t)((piece0 + i) ^ (row & 7)) << 4), make_uint4(pk[0], pk[1], pk[2], pk[3]));
     }
 }
+// What of a 32-column chunk of one row lies behind the last whole 16 bytes of the row: stored (FP32 C: or added) element by element.
+__device__ __forceinline__ void store_ragged(const GemmParams& p, int row, int col, const uint32_t (&r)[32], float f1, float f2)
+{
+    if (row >= p.M) return;
+    const int first = p.c_is_f32 ? p.N & ~3 : p.N & ~7;
+#pragma unroll
+    for (int i = 0; i < 32; i++) {  // (constant indices: see add_chunk_bf16)
+        if (col + i < first || col + i >= p.N) continue;
+        const long long at = (long long)row * p.ldc + col + i;
+        float v = __uint_as_float(r[i]) * f1 * f2;
+        if (p.c_is_f32) {
+            float* c = reinterpret_cast<float*>(p.C) + at;
+            *c = p.accumulate ? *c + v : v;
+        } else {
+            uint32_t b;
+            asm("cvt.rn.bf16x2.f32 %0, %1, %1;" : "=r"(b) : "f"(v));
+            reinterpret_cast<unsigned short*>(p.C)[at] = (unsigned short)b;
+        }
+    }
+}
 // tile store shared -> global (clipped at the edges of the matrix); the caller commits and waits for the group
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int c0, int c1)
 {
@@ -1755,7 +1775,9 @@ struct SmemLayout2 {
 constexpr uint32_t kSmemBytes2 = SmemLayout2::total + 1024;
 static_assert(kSmemBytes2 <= 227 * 1024, "shared memory of one CTA");
 
-template <bool W_IS_NK>
+// RAGGED: rows of C end inside 16 bytes.  A tile store clips at the end of the tensor map's rows in whole 16-byte pieces only, so the map ends in front of the
+// last one and the warp writes what is left itself.
+template <bool W_IS_NK, bool RAGGED>
 __global__ void __launch_bounds__(kThreadsP, 1)
 bf16_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_c,
                       const GemmParams p)
@@ -1892,6 +1914,8 @@ bf16_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
             tile_coords(t - b * tiles_one, tiles_m2, tiles_n2, tile_m, tile_n, group);
             const int row0 = tile_m * 2 * BM + (int)rank * BM + warp * 32, row = row0 + lane, n0 = tile_n * BN;
             const int pieces = p.c_by_tma && row0 < p.M ? (min(BN, p.N - n0) + piece_cols - 1) / piece_cols : 0;
+            // (RAGGED: pieces that the tensor map of C has a column of)
+            const int mapped = !RAGGED ? pieces : min(pieces, (max(0, (p.c_is_f32 ? p.N & ~3 : p.N & ~7) - n0) + piece_cols - 1) / piece_cols);
             auto fetch_old = [&](int i) {  // lane 0; the staging piece is free
                 const uint32_t bar = bar_old(2 * warp + (i & 1));
                 mbar_arrive_expect_tx(bar, kOutBytes);
@@ -1900,7 +1924,7 @@ bf16_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
             };
             if (p.c_by_tma && p.accumulate && lane == 0) {
                 asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                for (int i = 0; i < min(2, pieces); i++) fetch_old(i);
+                for (int i = 0; i < min(2, mapped); i++) fetch_old(i);
             }
             if (!mbar_wait(bar_acc_full(acc), (uint32_t)(use & 1), abort_flag, p.status, 24)) break;
             tc_fence_after();
@@ -1923,6 +1947,8 @@ bf16_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                     tmem_ld_32x32b_x32(tlane + i * 32, r);
                     tmem_ld_wait();
                     if (p.d_sw_channel) apply_channel_scale(p, n0 + i * 32, lane, sa, r);
+                    if (RAGGED && n0 + i * 32 + 32 > p.N) store_ragged(p, row, n0 + i * 32, r, f1, f2);
+                    if (RAGGED && i >= mapped) continue;
                     if (p.accumulate) {
                         if (!mbar_wait(bar_old(2 * warp + (i & 1)), (n_old >> (i & 1)) & 1, abort_flag, p.status, 25)) break;
                         n_old ^= 1u << (i & 1);
@@ -1946,15 +1972,17 @@ bf16_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                         tmem_ld_32x32b_x32(tlane + i * 64 + h * 32, r);
                         tmem_ld_wait();
                         if (p.d_sw_channel) apply_channel_scale(p, n0 + i * 64 + h * 32, lane, sa, r);
+                        if (RAGGED && n0 + i * 64 + h * 32 + 32 > p.N) store_ragged(p, row, n0 + i * 64 + h * 32, r, f1, f2);
                         stage_chunk_bf16(buf, lane, 4 * h, r, f1, f2);
                     }
                 }
+                if (RAGGED && i >= mapped) continue;
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) {
                     tma_store_2d(&map_c, buf, n0 + i * piece_cols, row0);
                     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                    if (p.accumulate && i + 2 < pieces) {
+                    if (p.accumulate && i + 2 < mapped) {
                         asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                         fetch_old(i + 2);
                     }
@@ -2107,6 +2135,7 @@ EncodeTiledFn encode_tiled_fn()
 struct MapKey {
     const void* ptr;
     uint64_t inner, rows, count, ld;  // ld: row pitch in elements (2-D) or distance between stacked matrices (3-D)
+    uint64_t pitch;                   // 3-D: row pitch in elements
     uint32_t box_inner, box_rows;
     uint32_t kind;                    // 0: bytes, 2-D; 1: BF16, 2-D, 128-byte swizzle; 2: BF16, 3-D stack, 128-byte swizzle;
                                       // 3: bytes, 2-D, 64-byte swizzle; 4: bytes, 2-D, 128-byte swizzle; 5: FP32, 2-D, 128-byte swizzle;
@@ -2122,7 +2151,7 @@ bool encode_map(const MapKey& k, CUtensorMap* map)
     const bool bf16 = k.kind == 1 || k.kind == 2;
     if (k.kind == 2) {
         cuuint64_t dims[3] = {k.inner, k.rows, k.count};
-        cuuint64_t strides[2] = {k.inner * 2u, (k.count > 1 ? k.ld : k.inner * k.rows) * 2u};
+        cuuint64_t strides[2] = {k.pitch * 2u, (k.count > 1 ? k.ld : k.pitch * k.rows) * 2u};
         cuuint32_t box[3] = {k.box_inner, k.box_rows, 1};
         cuuint32_t estr[3] = {1, 1, 1};
         return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(k.ptr), dims, strides, box, estr,
@@ -2169,13 +2198,13 @@ bool make_map_f32(CUtensorMap* map, const void* ptr, uint64_t inner, uint64_t ro
     return g_map_cache.lookup_or_make(k, map, encode_map);
 }
 
-// BF16 stack of `count` matrices [rows, inner], `stack_stride` elements apart (box: one matrix deep)
+// BF16 stack of `count` matrices [rows, inner], `stack_stride` elements apart (box: one matrix deep), rows `pitch` elements apart (0: contiguous)
 bool make_map3(CUtensorMap* map, const void* ptr, uint64_t inner, uint64_t rows, uint64_t count, uint64_t stack_stride,
-               uint32_t box_inner, uint32_t box_rows)
+               uint32_t box_inner, uint32_t box_rows, uint64_t pitch = 0)
 {
     MapKey k;
     std::memset(&k, 0, sizeof k);
-    k.ptr = ptr; k.inner = inner; k.rows = rows; k.count = count; k.ld = count > 1 ? stack_stride : 0; k.box_inner = box_inner;
+    k.ptr = ptr; k.inner = inner; k.rows = rows; k.count = count; k.ld = count > 1 ? stack_stride : 0; k.pitch = pitch ? pitch : inner; k.box_inner = box_inner;
     k.box_rows = box_rows; k.kind = 2u;
     return g_map_cache.lookup_or_make(k, map, encode_map);
 }
@@ -2218,10 +2247,11 @@ bool gemm_kernels_ready(int dev, int* sm_count_out, const int** wd_clusters = nu
         out->sm_count = 0;
         std::memset(out->wd_clusters, 0, sizeof out->wd_clusters);
         std::memset(out->nw_clusters, 0, sizeof out->nw_clusters);
-        const void* pair[2] = {(const void*)bf16_gemm_pair_kernel<false>, (const void*)bf16_gemm_pair_kernel<true>};
+        const void* pair[4] = {(const void*)bf16_gemm_pair_kernel<false, false>, (const void*)bf16_gemm_pair_kernel<true, false>,
+                               (const void*)bf16_gemm_pair_kernel<false, true>, (const void*)bf16_gemm_pair_kernel<true, true>};
         const void* wd[24];
         weights_kernels<kOneGroup>(wd); weights_kernels<kGroups>(wd + 6); weights_kernels<kFarRows>(wd + 12); weights_kernels<kParts>(wd + 18);
-        for (int i = 0; i < 2 && out->rc == cudaSuccess; i++)
+        for (int i = 0; i < 4 && out->rc == cudaSuccess; i++)
             out->rc = cudaFuncSetAttribute(pair[i], cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes2);
         for (int i = 0; i < 24 && out->rc == cudaSuccess; i++)
             out->rc = cudaFuncSetAttribute(wd[i], cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytesMax);
@@ -2297,7 +2327,7 @@ void note_status_word(cudaStream_t st, const int* word)
 }
 
 int launch_bf16_pair_gemm(const void* a_bf, const void* w_bf, int w_is_nk, GemmParams p, cudaStream_t st,
-                          long long a_stack_stride, long long w_stack_stride)
+                          long long a_stack_stride, long long w_stack_stride, long long a_pitch, long long w_pitch)
 {
     int dev = 0, sm_count = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || !gemm_kernels_ready(dev, &sm_count)) return HIF8_ERR_CUDA;
@@ -2310,17 +2340,19 @@ int launch_bf16_pair_gemm(const void* a_bf, const void* w_bf, int w_is_nk, GemmP
     if (nb > 1 && ((a_stack_stride & 7) || (w_stack_stride & 7))) return HIF8_ERR_ALIGN;  // 16-byte strides
     CUtensorMap ma, mw;
     // A boxes: this CTA's 128 rows of [M,K]
-    if (!make_map3(&ma, a_bf, (uint64_t)K, (uint64_t)M, nb, (uint64_t)a_stack_stride, BK, BM)) return HIF8_ERR_CUDA;
+    if (!make_map3(&ma, a_bf, (uint64_t)K, (uint64_t)M, nb, (uint64_t)a_stack_stride, BK, BM, (uint64_t)a_pitch)) return HIF8_ERR_CUDA;
     // W boxes are one CTA's half of the 256-column tile: 128 rows of [N,K], or two boxes of 64 columns of [K,N]
-    const bool okw = w_is_nk ? make_map3(&mw, w_bf, (uint64_t)K, (uint64_t)N, nb, (uint64_t)w_stack_stride, BK, BN / 2)
-                             : make_map3(&mw, w_bf, (uint64_t)N, (uint64_t)K, nb, (uint64_t)w_stack_stride, 64, BK);
+    const bool okw = w_is_nk ? make_map3(&mw, w_bf, (uint64_t)K, (uint64_t)N, nb, (uint64_t)w_stack_stride, BK, BN / 2, (uint64_t)w_pitch)
+                             : make_map3(&mw, w_bf, (uint64_t)N, (uint64_t)K, nb, (uint64_t)w_stack_stride, 64, BK, (uint64_t)w_pitch);
     if (!okw) return HIF8_ERR_CUDA;
     // the result through tile stores, except the squared error and BF16 sums
     CUtensorMap mc = ma;  // (a valid map in any case; only used when c_by_tma is set)
     p.c_by_tma = (!p.err_sum && (p.c_is_f32 || !p.accumulate)) ? 1 : 0;
-    if (p.c_by_tma) {
-        const bool okc = p.c_is_f32 ? make_map_f32(&mc, p.C, (uint64_t)N, (uint64_t)M, (uint64_t)p.ldc, 32)
-                                    : make_map(&mc, p.C, (uint64_t)N, (uint64_t)M, (uint64_t)p.ldc, 64, 32, true);
+    const int whole = p.c_is_f32 ? N & ~3 : N & ~7;
+    const bool ragged = p.c_by_tma && whole != N;
+    if (p.c_by_tma && whole > 0) {
+        const bool okc = p.c_is_f32 ? make_map_f32(&mc, p.C, (uint64_t)whole, (uint64_t)M, (uint64_t)p.ldc, 32)
+                                    : make_map(&mc, p.C, (uint64_t)whole, (uint64_t)M, (uint64_t)p.ldc, 64, 32, true);
         if (!okc) return HIF8_ERR_CUDA;
     }
     const int pairs = (int)(tiles2 < sm_count / 2 ? tiles2 : sm_count / 2);
@@ -2335,8 +2367,10 @@ int launch_bf16_pair_gemm(const void* a_bf, const void* w_bf, int w_is_nk, GemmP
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr; cfg.numAttrs = 2;
-    const cudaError_t lrc = w_is_nk ? cudaLaunchKernelEx(&cfg, bf16_gemm_pair_kernel<true>, ma, mw, mc, p)
-                                    : cudaLaunchKernelEx(&cfg, bf16_gemm_pair_kernel<false>, ma, mw, mc, p);
+    const cudaError_t lrc = ragged ? (w_is_nk ? cudaLaunchKernelEx(&cfg, bf16_gemm_pair_kernel<true, true>, ma, mw, mc, p)
+                                              : cudaLaunchKernelEx(&cfg, bf16_gemm_pair_kernel<false, true>, ma, mw, mc, p))
+                                   : (w_is_nk ? cudaLaunchKernelEx(&cfg, bf16_gemm_pair_kernel<true, false>, ma, mw, mc, p)
+                                              : cudaLaunchKernelEx(&cfg, bf16_gemm_pair_kernel<false, false>, ma, mw, mc, p));
     g_launches.fetch_add(1, std::memory_order_relaxed);
     return (lrc == cudaSuccess && cudaGetLastError() == cudaSuccess) ? HIF8_OK : HIF8_ERR_CUDA;
 }

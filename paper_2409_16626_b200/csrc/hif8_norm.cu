@@ -1,0 +1,439 @@
+// Root-mean-square norm in front of a block-scaled product, with the residual's addition and HiF8 codes as its result, and its gradient.
+//
+//   h = x + residual (rounded to their type),  r = 1 / sqrt(mean(h^2) + eps),  y = h r w  ->  codes with a scale for each 1 x 128
+//   dx = r (w dy - u mean(w dy u)) + dh,  u = h r;     dw_j = sum_i dy_ij u_ij
+//
+// Both are bound by memory.  A row is held in registers between its sum and its results (a group of 32 to 1024 threads per row, up to 32 elements a
+// thread), so every tensor is read or written once.  Sums, the norm's factor and the weight's gradient are FP32.
+#include "hif8_block.cuh"
+#include "hif8_host_cache.h"
+
+namespace hif8 {
+namespace {
+
+constexpr int kNormEights = 4;  // groups of eight elements that a thread holds of a row
+
+struct NormParams {
+    const void* x;
+    const void* residual;  // or null
+    const void* weight;
+    void* h;               // or null
+    float* rstd;           // or null
+    long long ld_x, ld_res, ld_h, rows, cols;
+    float eps;
+    BlockCodes m;
+    int lg;                // log2 of the threads of a row
+    int target_exp;
+    unsigned flags;
+    bool vec_x, vec_res, vec_h, vec_w, codes8;  // rows on boundaries of 16 bytes (codes: 8)
+};
+
+// Sum over the 1 << lg threads of a row, the same bits in each of them; `s_part`: one of two sets of a word per warp, used in turn, so nobody still reads
+// it from the use before the last one, which the barrier of the last one stands behind.
+__device__ __forceinline__ float row_sum(float v, float* s_part, int lg, int group, bool alone)
+{
+#pragma unroll
+    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+    if (lg == 5) return v;
+    if ((threadIdx.x & 31u) == 0) s_part[threadIdx.x >> 5] = v;
+    if (alone) __syncthreads();
+    else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(1 << lg) : "memory");
+    const int n = 1 << (lg - 5);
+    const float* part = s_part + (group << (lg - 5));
+    if (n == 2) return part[0] + part[1];
+    v = 0.f;
+    for (int i = 0; i < n; i += 4) {
+        const float4 q = *reinterpret_cast<const float4*>(part + i);
+        v += (q.x + q.y) + (q.z + q.w);
+    }
+    return v;
+}
+
+template <int DT> __device__ __forceinline__ const char* row_at(const void* base, long long row, long long ld)
+{
+    return reinterpret_cast<const char*>(base) + (size_t)row * (size_t)ld * (DT == HIF8_F32 ? 4 : 2);
+}
+
+template <int DT, int MODE, int BLOCK>
+__global__ void __launch_bounds__(BLOCK) norm_encode_kernel(const NormParams p)
+{
+    constexpr int NV = kNormEights;
+    __shared__ SmemTables sm;
+    __shared__ __align__(16) float s_part[2][BLOCK / 32];
+    setup_tables<true, MODE != HIF8_RND_TA, false, MODE, HIF8_F32, BLOCK>(sm, p.flags);
+    pdl_wait_prior_grid();
+    pdl_launch_dependents();
+    const int gs = 1 << p.lg, group = threadIdx.x >> p.lg, t = threadIdx.x & (gs - 1), groups = BLOCK >> p.lg;
+    int turn = 0;
+    for (long long row = (long long)blockIdx.x * groups + group; row - group < p.rows; row += (long long)gridDim.x * groups, turn ^= 1) {
+        const bool live = row < p.rows;  // a group behind the last row only takes part in the exchanges
+        Eight<DT> h[NV];
+        float sum = 0.f;
+        const long long end = live ? p.cols : 0;
+#pragma unroll
+        for (int j = 0; j < NV; j++) h[j] = load_eight<DT>(row_at<DT>(p.x, row, p.ld_x), (j * gs + t) * 8, end, p.vec_x);
+        if (p.residual) {
+            Eight<DT> r[NV];
+#pragma unroll
+            for (int j = 0; j < NV; j++) r[j] = load_eight<DT>(row_at<DT>(p.residual, row, p.ld_res), (j * gs + t) * 8, end, p.vec_res);
+#pragma unroll
+            for (int j = 0; j < NV; j++) {
+                float s[8];
+#pragma unroll
+                for (int i = 0; i < 8; i++) s[i] = value_of_eight<DT>(h[j], i) + value_of_eight<DT>(r[j], i);
+                h[j] = pack_eight<DT>(s);
+            }
+        }
+        if (p.h) {
+#pragma unroll
+            for (int j = 0; j < NV; j++) store_eight<DT>(const_cast<char*>(row_at<DT>(p.h, row, p.ld_h)), (j * gs + t) * 8, end, p.vec_h, h[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < NV; j++)
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float v = value_of_eight<DT>(h[j], i);
+                sum = fmaf(v, v, sum);
+            }
+        sum = row_sum(sum, s_part[turn], p.lg, group, groups == 1);
+        const float rstd = __frsqrt_rn(sum / (float)p.cols + p.eps);
+        if (p.rstd && t == 0 && live) p.rstd[row] = rstd;
+#pragma unroll
+        for (int j = 0; j < NV; j++) {
+            const long long c = (j * gs + t) * 8;
+            if ((c & ~127ll) >= end) continue;  // (the same for a block's sixteen threads, and so is what follows for half a warp)
+            const Eight<DT> w = load_eight<DT, true>(p.weight, c, p.cols, p.vec_w);
+            float y[8], top = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                y[i] = value_of_eight<DT>(h[j], i) * rstd * value_of_eight<DT>(w, i);
+                if (c + i >= p.cols) y[i] = 0.f;
+                top = amax_step(top, y[i]);
+            }
+            uint32_t m = __float_as_uint(top);
+            const unsigned mask = 0xFFFFu << (threadIdx.x & 16u);
+#pragma unroll
+            for (int d = 8; d; d >>= 1) m = max(m, __shfl_xor_sync(mask, m, d));
+            const int se = block_exp_from_amax(m, p.target_exp);
+            if ((t & 15) == 0) p.m.exps[(size_t)row * (size_t)p.m.exp_stride + (size_t)(c >> 7)] = se;
+            const float scale = pow2f(se);
+            uint32_t code[2] = {0u, 0u};
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                uint32_t k;
+                if (MODE == HIF8_RND_TA) {
+                    k = ta_magnitude_code(y[i], scale, sm.ta);
+                    k |= (k + 0x7Fu) & (__float_as_uint(y[i]) >> 24) & 0x80u;
+                } else k = encode_one<MODE, HIF8_F32>(y[i], __float_as_uint(y[i]), scale, sm.ta, sm.thr, 0u) & 0xFFu;
+                code[i >> 2] |= k << (8 * (i & 3));
+            }
+            store_codes8(p.m.codes + (size_t)row * (size_t)p.m.ld, c, p.cols, p.codes8, make_uint2(code[0], code[1]));
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// gradient
+// ------------------------------------------------------------------------------------------------
+struct NormBackwardParams {
+    const void* dy;
+    const void* h;
+    const void* dh;      // or null
+    const void* weight;
+    const float* rstd;
+    void* dx;
+    float* part;         // [blocks][cols] shares of the weight's gradient, or null
+    long long ld_dy, ld_h, ld_dh, ld_dx, rows, cols;
+    int lg;
+    bool vec_dy, vec_h, vec_dh, vec_dx, vec_w;
+};
+
+// A thread has the same columns of every row it works on, so it keeps their sums of dy u: in registers, of rows of 1024 threads (which have 64 registers each) in
+// shared memory.
+template <int DT, int BLOCK>
+__global__ void __launch_bounds__(BLOCK) norm_backward_kernel(const NormBackwardParams p)
+{
+    constexpr int NV = kNormEights;
+    constexpr bool kFar = BLOCK == 1024;
+    extern __shared__ __align__(16) float s_acc[];  // BLOCK x 32: kFar: the threads' sums; blocks of 256: to join their groups
+    __shared__ __align__(16) float s_part[2][BLOCK / 32];
+    pdl_wait_prior_grid();
+    pdl_launch_dependents();
+    const int gs = 1 << p.lg, group = threadIdx.x >> p.lg, t = threadIdx.x & (gs - 1), groups = BLOCK >> p.lg;
+    float acc[kFar ? 1 : NV][8];
+    if (!kFar) {
+#pragma unroll
+        for (int j = 0; j < (kFar ? 1 : NV); j++)
+#pragma unroll
+            for (int i = 0; i < 8; i++) acc[j][i] = 0.f;
+    } else {
+        for (int k = 0; k < NV * 8; k++) s_acc[k * BLOCK + threadIdx.x] = 0.f;
+    }
+    const float inv = 1.f / (float)p.cols;
+    int turn = 0;
+    for (long long row = (long long)blockIdx.x * groups + group; row - group < p.rows; row += (long long)gridDim.x * groups, turn ^= 1) {
+        const bool live = row < p.rows;
+        const long long end = live ? p.cols : 0;
+        Eight<DT> dy[NV], h[NV], dh[NV];
+#pragma unroll
+        for (int j = 0; j < NV; j++) dy[j] = load_eight<DT>(row_at<DT>(p.dy, row, p.ld_dy), (j * gs + t) * 8, end, p.vec_dy);
+#pragma unroll
+        for (int j = 0; j < NV; j++) h[j] = load_eight<DT>(row_at<DT>(p.h, row, p.ld_h), (j * gs + t) * 8, end, p.vec_h);
+        const float rstd = live ? __ldg(p.rstd + row) : 0.f;
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < NV; j++) {
+            const Eight<DT> w = load_eight<DT, true>(p.weight, (j * gs + t) * 8, p.cols, p.vec_w);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float d = value_of_eight<DT>(dy[j], i), u = value_of_eight<DT>(h[j], i) * rstd;
+                sum = fmaf(d * value_of_eight<DT>(w, i), u, sum);
+                if (!kFar) acc[j % (kFar ? 1 : NV)][i] = fmaf(d, u, acc[j % (kFar ? 1 : NV)][i]);
+                else s_acc[(j * 8 + i) * BLOCK + threadIdx.x] = fmaf(d, u, s_acc[(j * 8 + i) * BLOCK + threadIdx.x]);
+            }
+        }
+        if (p.dh) {
+#pragma unroll
+            for (int j = 0; j < NV; j++) dh[j] = load_eight<DT>(row_at<DT>(p.dh, row, p.ld_dh), (j * gs + t) * 8, end, p.vec_dh);
+        }
+        const float mean = row_sum(sum, s_part[turn], p.lg, group, groups == 1) * inv;
+#pragma unroll
+        for (int j = 0; j < NV; j++) {
+            const Eight<DT> w = load_eight<DT, true>(p.weight, (j * gs + t) * 8, p.cols, p.vec_w);
+            float g[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float u = value_of_eight<DT>(h[j], i) * rstd, wdy = value_of_eight<DT>(dy[j], i) * value_of_eight<DT>(w, i);
+                g[i] = rstd * fmaf(-u, mean, wdy);
+                if (p.dh) g[i] += value_of_eight<DT>(dh[j], i);
+            }
+            store_eight<DT>(const_cast<char*>(row_at<DT>(p.dx, row, p.ld_dx)), (j * gs + t) * 8, end, p.vec_dx, pack_eight<DT>(g));
+        }
+    }
+    if (!p.part) return;
+    float* out = p.part + (size_t)blockIdx.x * (size_t)p.cols;
+    if (kFar) {
+        for (int k = 0; k < NV * 8; k++) {
+            const long long c = ((k >> 3) * gs + t) * 8 + (k & 7);
+            if (c < p.cols) out[c] = s_acc[k * BLOCK + threadIdx.x];
+        }
+        return;
+    }
+    if (groups == 1) {
+#pragma unroll
+        for (int j = 0; j < (kFar ? 1 : NV); j++)
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const long long c = (j * gs + t) * 8 + i;
+                if (c < p.cols) out[c] = acc[j][i];
+            }
+        return;
+    }
+    // the groups' sums, in their order
+    const int width = gs * NV * 8;
+#pragma unroll
+    for (int j = 0; j < (kFar ? 1 : NV); j++)
+#pragma unroll
+        for (int i = 0; i < 8; i += 4)
+            *reinterpret_cast<float4*>(s_acc + group * width + (j * gs + t) * 8 + i) = make_float4(acc[j][i], acc[j][i + 1], acc[j][i + 2], acc[j][i + 3]);
+    __syncthreads();
+    for (int c = threadIdx.x; c < width && c < p.cols; c += BLOCK) {
+        float v = 0.f;
+        for (int g = 0; g < groups; g++) v += s_acc[g * width + c];
+        out[c] = v;
+    }
+}
+
+// dweight_j (+)= the blocks' shares, in their order: 32 columns by eight slices of the blocks
+__global__ void __launch_bounds__(kThreads) norm_weight_grad_kernel(const float* __restrict__ part, int blocks, long long cols, float* dweight, int accumulate)
+{
+    __shared__ float s_sum[kThreads / 32][32];
+    pdl_wait_prior_grid();
+    pdl_launch_dependents();
+    const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, per = (blocks + kThreads / 32 - 1) / (kThreads / 32);
+    const long long c = (long long)blockIdx.x * 32 + lane;
+    float v = 0.f;
+    if (c < cols) {
+        const int from = slice * per, to = min(blocks, from + per);
+#pragma unroll 8
+        for (int b = from; b < to; b++) v += part[(size_t)b * (size_t)cols + c];
+    }
+    s_sum[slice][lane] = v;
+    __syncthreads();
+    if (slice == 0 && c < cols) {
+        v = 0.f;
+#pragma unroll
+        for (int s = 0; s < kThreads / 32; s++) v += s_sum[s][lane];
+        dweight[c] = accumulate ? dweight[c] + v : v;
+    }
+}
+
+int finish(int launches)
+{
+    g_launches.fetch_add((uint64_t)launches, std::memory_order_relaxed);
+    return cudaGetLastError() == cudaSuccess ? HIF8_OK : HIF8_ERR_CUDA;
+}
+
+// log2 of the threads that share a row: up to 32 elements each, or eight, with few rows, whose time is that of one row
+int row_threads_log2(long long rows, long long cols, int few)
+{
+    const long long eights = (cols + 7) / 8, want = rows <= few ? eights : (eights + kNormEights - 1) / kNormEights;
+    int lg = 5;
+    while (lg < 10 && (1ll << lg) < want) lg++;
+    return lg;
+}
+
+// blocks of the gradient's kernel: as many as are resident, which the shares of the weight's gradient in the workspace go by
+long long backward_blocks(long long rows, int lg)
+{
+    const int groups = lg < 8 ? 1 << (8 - lg) : 1;
+    const long long need = (rows + groups - 1) / groups, most = lg <= 8 ? 2 * 148 : 148;
+    return need < most ? need : most;
+}
+constexpr int kFewRows = 148;
+
+template <int DT, int MODE>
+void launch_norm(const NormParams& p, int sms, cudaStream_t st)
+{
+    const int groups = p.lg < 8 ? 1 << (8 - p.lg) : 1;
+    const long long need = (p.rows + groups - 1) / groups, most = (long long)sms * (p.lg <= 8 ? 4 : p.lg == 9 ? 2 : 1);
+    const dim3 grid((unsigned)(need < most ? need : most));
+    if (p.lg <= 8) launch_pdl_threads(256, norm_encode_kernel<DT, MODE, 256>, grid, st, p);
+    else if (p.lg == 9) launch_pdl_threads(512, norm_encode_kernel<DT, MODE, 512>, grid, st, p);
+    else launch_pdl_threads(1024, norm_encode_kernel<DT, MODE, 1024>, grid, st, p);
+}
+template <int DT>
+void launch_norm_mode(int rnd, const NormParams& p, int sms, cudaStream_t st)
+{
+    switch (rnd) {
+        case HIF8_RND_TA: return launch_norm<DT, HIF8_RND_TA>(p, sms, st);
+        case HIF8_RND_HR: return launch_norm<DT, HIF8_RND_HR>(p, sms, st);
+        case HIF8_RND_SSR: return launch_norm<DT, HIF8_RND_SSR>(p, sms, st);
+        default: return launch_norm<DT, HIF8_RND_TE>(p, sms, st);
+    }
+}
+
+template <int DT, int BLOCK>
+bool launch_backward_block(const NormBackwardParams& p, long long blocks, cudaStream_t st)
+{
+    const size_t bytes = BLOCK == 512 ? 0 : (size_t)BLOCK * kNormEights * 8 * sizeof(float);
+    if (bytes > 48 * 1024) {  // a fact of the device, set by its first such call
+        static PerDevice<cudaError_t> ready;
+        int dev = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess) return false;
+        const cudaError_t* rc = ready.get(dev, [&](int, cudaError_t* out) {
+            *out = cudaFuncSetAttribute(norm_backward_kernel<DT, BLOCK>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        });
+        if (!rc || *rc != cudaSuccess) return false;
+    }
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3(BLOCK);
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, norm_backward_kernel<DT, BLOCK>, p) == cudaSuccess;
+}
+template <int DT>
+bool launch_backward(const NormBackwardParams& p, long long blocks, cudaStream_t st)
+{
+    if (p.lg <= 8) return launch_backward_block<DT, 256>(p, blocks, st);
+    if (p.lg == 9) return launch_backward_block<DT, 512>(p, blocks, st);
+    return launch_backward_block<DT, 1024>(p, blocks, st);
+}
+
+// the same rows (a result in the place of an operand), or no byte in common
+bool same_or_apart(const void* dst, size_t dst_bytes, long long ld_dst, const void* src, size_t src_bytes, long long ld_src, long long rows)
+{
+    return (dst == src && (ld_dst == ld_src || rows <= 1)) || !ranges_overlap(dst, dst_bytes, src, src_bytes);
+}
+
+}  // namespace
+}  // namespace hif8
+
+using namespace hif8;
+
+extern "C" int hif8_rmsnorm_encode(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, int dtype, const void* weight, float eps, int64_t rows, int64_t cols,
+                                   void* h, int64_t ld_h, float* d_rstd, uint8_t* dst, int64_t ld_dst, int* d_exp, int64_t exp_stride, int target_exp, int rnd, unsigned flags,
+                                   hif8_stream_t stream)
+{
+    if (bad_dtype(dtype)) return HIF8_ERR_DTYPE;
+    if (rnd != HIF8_RND_TA && rnd != HIF8_RND_HR && rnd != HIF8_RND_SSR && rnd != HIF8_RND_TE) return HIF8_ERR_ROUND;
+    if (flags & ~(unsigned)(HIF8_FLAG_SATURATE | HIF8_FLAG_NAN_TO_ZERO)) return HIF8_ERR_FLAGS;
+    if (target_exp < -22 || target_exp > 15 || !(eps >= 0.f && eps <= 3.402823466e38f)) return HIF8_ERR_SCALE_RANGE;
+    if (rows < 0 || cols < 0 || cols > HIF8_NORM_MAX_COLS || rows > 0x7FFFFFFFll * 32) return HIF8_ERR_SHAPE;
+    NormParams p{};
+    p.m = BlockCodes{dst, ld_dst, d_exp, exp_stride, rows, cols, 0};
+    if (ld_x < cols || (residual && ld_residual < cols) || (h && ld_h < cols) || ld_dst < cols || exp_stride < p.m.blocks_across()) return HIF8_ERR_SHAPE;
+    if (rows == 0 || cols == 0) return HIF8_OK;
+    if (!x || !weight || !dst || !d_exp) return HIF8_ERR_NULL;
+    const size_t item = dtype_bytes(dtype);
+    if (!aligned_to(x, item) || !aligned_to(residual, item) || !aligned_to(weight, item) || !aligned_to(h, item) || !aligned_to(d_rstd, 4) || !aligned_to(d_exp, 4)) return HIF8_ERR_ALIGN;
+    const size_t x_bytes = matrix_bytes(rows, cols, ld_x, item), r_bytes = residual ? matrix_bytes(rows, cols, ld_residual, item) : 0, h_bytes = h ? matrix_bytes(rows, cols, ld_h, item) : 0;
+    const size_t w_bytes = (size_t)cols * item, rstd_bytes = d_rstd ? (size_t)rows * 4 : 0;
+    if (written_over({{dst, p.m.code_bytes()}, {d_exp, p.m.exp_bytes()}, {d_rstd, rstd_bytes}}, {{x, x_bytes}, {residual, r_bytes}, {weight, w_bytes}, {h, h_bytes}}) ||
+        written_over({{h, h_bytes}}, {{weight, w_bytes}}) || !same_or_apart(h, h_bytes, ld_h, x, x_bytes, ld_x, rows) ||
+        !same_or_apart(h, h_bytes, ld_h, residual, r_bytes, ld_residual, rows))
+        return HIF8_ERR_OVERLAP;
+    int sms; if (int rc = checked_device(&sms)) return rc;
+    p.x = x; p.residual = residual; p.weight = weight; p.h = h; p.rstd = d_rstd; p.ld_x = ld_x; p.ld_res = ld_residual; p.ld_h = ld_h; p.rows = rows; p.cols = cols;
+    p.eps = eps; p.target_exp = target_exp; p.flags = flags;
+    p.lg = row_threads_log2(rows, cols, kFewRows);
+    p.vec_x = vector_rows(x, rows, ld_x, item); p.vec_res = vector_rows(residual, rows, ld_residual, item); p.vec_h = vector_rows(h, rows, ld_h, item); p.vec_w = aligned_to(weight, 16);
+    p.codes8 = aligned_to(dst, 8) && (rows <= 1 || (ld_dst & 7) == 0);
+    cudaStream_t st = (cudaStream_t)stream;
+    if (dtype == HIF8_F32) launch_norm_mode<HIF8_F32>(rnd, p, sms, st);
+    else if (dtype == HIF8_BF16) launch_norm_mode<HIF8_BF16>(rnd, p, sms, st);
+    else launch_norm_mode<HIF8_F16>(rnd, p, sms, st);
+    return finish(1);
+}
+
+extern "C" size_t hif8_rmsnorm_backward_workspace_bytes(int64_t rows, int64_t cols)
+{
+    if (rows <= 0 || cols <= 0 || cols > HIF8_NORM_MAX_COLS) return 0;
+    return ((size_t)backward_blocks(rows, row_threads_log2(rows, cols, 0)) * (size_t)cols * sizeof(float) + 255) & ~(size_t)255;
+}
+
+extern "C" int hif8_rmsnorm_backward(const void* dy, int64_t ld_dy, const void* h, int64_t ld_h, const void* dh, int64_t ld_dh, int dtype, const void* weight, const float* d_rstd,
+                                     int64_t rows, int64_t cols, void* dx, int64_t ld_dx, float* d_weight_grad, int accumulate, void* workspace, size_t workspace_bytes,
+                                     hif8_stream_t stream)
+{
+    if (bad_dtype(dtype)) return HIF8_ERR_DTYPE;
+    if (rows < 0 || cols < 0 || cols > HIF8_NORM_MAX_COLS || rows > 0x7FFFFFFFll * 32) return HIF8_ERR_SHAPE;
+    if (ld_dy < cols || ld_h < cols || (dh && ld_dh < cols) || ld_dx < cols) return HIF8_ERR_SHAPE;
+    if (cols == 0) return HIF8_OK;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (!aligned_to(d_weight_grad, 4)) return HIF8_ERR_ALIGN;
+    if (rows == 0) {  // no row: a gradient of zeros
+        if (d_weight_grad && !accumulate && cudaMemsetAsync(d_weight_grad, 0, (size_t)cols * 4, st) != cudaSuccess) return HIF8_ERR_CUDA;
+        return HIF8_OK;
+    }
+    if (!dy || !h || !weight || !d_rstd || !dx) return HIF8_ERR_NULL;
+    const size_t item = dtype_bytes(dtype);
+    if (!aligned_to(dy, item) || !aligned_to(h, item) || !aligned_to(dh, item) || !aligned_to(weight, item) || !aligned_to(dx, item) || !aligned_to(d_rstd, 4)) return HIF8_ERR_ALIGN;
+    NormBackwardParams p{};
+    p.lg = row_threads_log2(rows, cols, 0);
+    const long long blocks = backward_blocks(rows, p.lg);
+    const size_t need = d_weight_grad ? hif8_rmsnorm_backward_workspace_bytes(rows, cols) : 0;
+    if (need && (!workspace || workspace_bytes < need || !aligned_to(workspace, 256))) return HIF8_ERR_WORKSPACE;
+    const size_t dy_bytes = matrix_bytes(rows, cols, ld_dy, item), h_bytes = matrix_bytes(rows, cols, ld_h, item), dh_bytes = dh ? matrix_bytes(rows, cols, ld_dh, item) : 0;
+    const size_t dx_bytes = matrix_bytes(rows, cols, ld_dx, item), w_bytes = (size_t)cols * item, dw_bytes = d_weight_grad ? (size_t)cols * 4 : 0;
+    if (written_over({{d_weight_grad, dw_bytes}, {workspace, need}},
+                     {{dy, dy_bytes}, {h, h_bytes}, {dh, dh_bytes}, {weight, w_bytes}, {d_rstd, (size_t)rows * 4}, {dx, dx_bytes}}) ||
+        written_over({{dx, dx_bytes}}, {{h, h_bytes}, {weight, w_bytes}, {d_rstd, (size_t)rows * 4}}) || !same_or_apart(dx, dx_bytes, ld_dx, dy, dy_bytes, ld_dy, rows) ||
+        !same_or_apart(dx, dx_bytes, ld_dx, dh, dh_bytes, ld_dh, rows))
+        return HIF8_ERR_OVERLAP;
+    int sms; if (int rc = checked_device(&sms)) return rc;
+    p.dy = dy; p.h = h; p.dh = dh; p.weight = weight; p.rstd = d_rstd; p.dx = dx; p.part = d_weight_grad ? reinterpret_cast<float*>(workspace) : nullptr;
+    p.ld_dy = ld_dy; p.ld_h = ld_h; p.ld_dh = ld_dh; p.ld_dx = ld_dx; p.rows = rows; p.cols = cols;
+    p.vec_dy = vector_rows(dy, rows, ld_dy, item); p.vec_h = vector_rows(h, rows, ld_h, item); p.vec_dh = vector_rows(dh, rows, ld_dh, item); p.vec_dx = vector_rows(dx, rows, ld_dx, item);
+    p.vec_w = aligned_to(weight, 16);
+    const bool ok = dtype == HIF8_F32 ? launch_backward<HIF8_F32>(p, blocks, st) : dtype == HIF8_BF16 ? launch_backward<HIF8_BF16>(p, blocks, st) : launch_backward<HIF8_F16>(p, blocks, st);
+    if (!ok) return HIF8_ERR_CUDA;
+    if (p.part)
+        launch_pdl(norm_weight_grad_kernel, dim3((unsigned)((cols + 31) / 32)), st, reinterpret_cast<const float*>(workspace), (int)blocks, (long long)cols, d_weight_grad, accumulate);
+    return finish(p.part ? 2 : 1);
+}
