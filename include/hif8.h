@@ -547,8 +547,8 @@ size_t hif8_rmsnorm_backward_workspace_bytes(int64_t rows, int64_t cols);
  *   forward  Y[T,N'] = X W^T:   A = X [T,K'] (1),  W = [N',K'] (128), w_is_nk = 1
  *   dX[T,K'] = dY W:            A = dY [T,N'] (1), the same W, w_is_nk = 0
  *   dW[N',K'] += dY^T X:        A = dY, a_is_km = 1, W = X [T,K'] (1), w_is_nk = 0, accumulate = 1
- * M, N and K are any positive numbers.  C [M,N] of HIF8_BF16 or HIF8_F32, 16-byte aligned with rows a multiple of 16 bytes apart (HIF8_ERR_ALIGN); what lies behind
- * column N of a row stays as it is.  Products are exact in FP32 unless they leave its range (beyond it Inf, below 2^-126 possibly 0); sums are FP32, in a fixed order.
+ * M, N and K are any positive numbers; all three matrices are 16-byte aligned with rows a multiple of 16 bytes apart (HIF8_ERR_ALIGN).  C [M,N] of HIF8_BF16 or HIF8_F32; what lies
+ * behind column N of a row stays as it is.  Products are exact in FP32 unless they leave its range (beyond it Inf, below 2^-126 possibly 0); sums are FP32, in a fixed order.
  * NaN and Inf codes propagate as in IEEE arithmetic.  accumulate as in hif8_gemm_ex.
  * workspace: hif8_gemm_block_workspace_bytes(...) bytes of the same arguments, 256-byte aligned, contents irrelevant on entry and undefined on return, for one call at a time; its first int is a device status
  * word as for hif8_gemm (hif8_gemm_status, hif8_last_device_status).

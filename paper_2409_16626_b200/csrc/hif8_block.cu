@@ -148,7 +148,8 @@ struct DecodeParams {
     FastDiv chunks;      // groups of eight columns of a row that is written
     unsigned units;      // such groups
     bool codes8, vectors;  // rows of the codes start on 8-byte boundaries, those written on 16-byte ones
-    uint32_t* clear_word;
+    uint32_t* clear;
+    unsigned clear_words;
 };
 
 __device__ __forceinline__ int exp_at(const BlockCodes& m, long long r, long long c)
@@ -192,7 +193,8 @@ __global__ void __launch_bounds__(kThreads) block_decode_kernel(const DecodePara
     __syncthreads();
     pdl_wait_prior_grid();
     pdl_launch_dependents();
-    if (p.clear_word && blockIdx.x == 0 && threadIdx.x == 0) *p.clear_word = 0u;
+    if (blockIdx.x == 0)
+        for (unsigned i = threadIdx.x; i < p.clear_words; i += kThreads) p.clear[i] = 0u;
     const uint32_t lane4 = (threadIdx.x & 31u) * 4u;
     for (unsigned long long base = (unsigned long long)blockIdx.x * (kThreads * UN) + threadIdx.x; base < p.units; base += (unsigned long long)gridDim.x * (kThreads * UN)) {
         uint2 v[UN];
@@ -229,7 +231,8 @@ __global__ void __launch_bounds__(kThreads) block_decode_transpose_kernel(const 
     __syncthreads();
     pdl_wait_prior_grid();
     pdl_launch_dependents();
-    if (p.clear_word && blockIdx.x == 0 && threadIdx.x == 0) *p.clear_word = 0u;
+    if (blockIdx.x == 0)
+        for (unsigned i = threadIdx.x; i < p.clear_words; i += kThreads) p.clear[i] = 0u;
     const unsigned lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     const uint32_t lane4 = lane * 4u;
     for (unsigned t = blockIdx.x; t < p.units; t += gridDim.x) {  // p.chunks: tiles across
@@ -304,11 +307,12 @@ void launch_decode(const DecodeParams& p, int sms, cudaStream_t st)
 
 }  // namespace
 
-int expand_block_codes(const BlockCodes& m, void* dst, long long ld_dst, long long rows_out, long long cols_out, bool transposed, uint32_t* clear_word, cudaStream_t st)
+int expand_block_codes(const BlockCodes& m, void* dst, long long ld_dst, long long rows_out, long long cols_out, bool transposed, uint32_t* clear, unsigned clear_words,
+                       cudaStream_t st)
 {
     int sms; if (int rc = checked_device(&sms)) return rc;
     DecodeParams p{};
-    p.m = m; p.dst = dst; p.ld_dst = ld_dst; p.rows_out = rows_out; p.cols_out = cols_out; p.clear_word = clear_word;
+    p.m = m; p.dst = dst; p.ld_dst = ld_dst; p.rows_out = rows_out; p.cols_out = cols_out; p.clear = clear; p.clear_words = clear_words;
     p.codes8 = aligned_to(m.codes, 8) && (m.rows <= 1 || (m.ld & 7) == 0);
     p.vectors = true;
     const long long across = transposed ? (cols_out + kFlipCols - 1) / kFlipCols : (cols_out + 7) / 8;

@@ -27,10 +27,40 @@ struct BlockCodes {
     size_t exp_bytes() const { return rows > 0 ? ((size_t)(blocks_down() - 1) * (size_t)exp_stride + (size_t)blocks_across()) * sizeof(int) : 0; }
 };
 
+// What the workspace of a block-scaled product holds behind the status word: the activations as BF16, and either the weights as BF16 too, or the narrow kernel's
+// tickets and partial sums.  (Sizes follow from the arguments alone, so that they can be asked for without a device.)
+struct BlockWorkspace {
+    static constexpr size_t kStatus = 256;
+    static constexpr int kNarrowRows = 64;   // up to so many rows the weight-streaming kernel takes the product
+    static constexpr int kExpandRows = 512;  // from so many on there is room to expand the weights too
+    long long a_pitch, w_pitch;              // elements between rows of the BF16 copies
+    size_t a_bytes, w_bytes, narrow_bytes;   // w_bytes, narrow_bytes: 0 where there is none
+    bool in_kernel;                          // the weights' layout lets the kernels that decode weights take the product
+    BlockWorkspace(int M, int N, int K, bool w_is_nk, int w_block_rows)
+    {
+        auto pad8 = [](long long n) { return (n + 7) & ~7ll; };
+        auto pad256 = [](size_t n) { return (n + 255) & ~(size_t)255; };
+        in_kernel = w_block_rows == HIF8_BLOCK && (K & 15) == 0;
+        a_pitch = pad8(K);
+        w_pitch = pad8(w_is_nk ? K : N);
+        a_bytes = pad256((size_t)M * (size_t)a_pitch * 2);
+        const bool narrow = in_kernel && M <= kNarrowRows;
+        w_bytes = in_kernel && M < kExpandRows ? 0 : pad256((size_t)(w_is_nk ? N : K) * (size_t)w_pitch * 2);
+        // partial sums of 128 columns by the rows: a slice for each block of up to 160 and two more for each slab, which two blocks may share
+        const size_t slabs = ((size_t)N + 127) / 128;
+        narrow_bytes = narrow ? pad256(slabs * 16) + (160 + 3 * slabs) * (size_t)((M + 15) & ~15) * 512 : 0;
+    }
+    size_t bytes() const { return kStatus + a_bytes + w_bytes + narrow_bytes; }
+};
+
+// C of `p` from block-scaled operands, the rest of `p` filled in here; the arguments have been checked.
+struct GemmParams;
+int launch_block_gemm(const BlockCodes& a, bool a_is_km, const BlockCodes& w, bool w_is_nk, const GemmParams& p, const BlockWorkspace& sizes, void* workspace, cudaStream_t st);
+
 // Codes of a product's operand, decoded into BF16 with their blocks' scales (exact: four significant bits, exponents within -118 .. 111):
 // dst [rows_out, cols_out], or with `transposed` element (r, c) at dst[c][r]; rows and columns beyond the matrix become zeros.  cols_out (transposed:
-// rows_out) and ld_dst are multiples of 8, dst is 16-byte aligned.  The launch also clears *clear_word (may be null).
-int expand_block_codes(const BlockCodes& m, void* dst, long long ld_dst, long long rows_out, long long cols_out, bool transposed, uint32_t* clear_word, cudaStream_t st);
+// rows_out) and ld_dst are multiples of 8, dst is 16-byte aligned.  The launch also clears clear_words words.
+int expand_block_codes(const BlockCodes& m, void* dst, long long ld_dst, long long rows_out, long long cols_out, bool transposed, uint32_t* clear, unsigned clear_words, cudaStream_t st);
 
 namespace {
 

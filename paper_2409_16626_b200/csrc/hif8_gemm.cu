@@ -29,6 +29,7 @@
 #include <type_traits>
 
 #include "hif8.h"
+#include "hif8_block_types.cuh"
 #include "hif8_host_cache.h"
 #include "hif8_internal.cuh"
 
@@ -428,6 +429,23 @@ __device__ __forceinline__ uint4 decode8(uint2 v, uint32_t lut_lane)
     return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+// 2^-e of a block of weights as two BF16 values (a code's value times it is exact)
+__device__ __forceinline__ uint32_t block_scale2(int e)
+{
+    return (uint32_t)(127 - max(-HIF8_BLOCK_EXP_MAX, min(HIF8_BLOCK_EXP_MAX, e))) * 0x00800080u;
+}
+__device__ __forceinline__ void scale_words(uint32_t (&o)[32], uint32_t scale2)
+{
+#pragma unroll
+    for (int i = 0; i < 32; i++) o[i] = mul_bf16x2(o[i], scale2);
+}
+
 // Groups of `group` tile-rows sweep N together: their W tiles stay in L2 (8 in the weights kernel, whose kGroupPieces is the same number; the pair kernel says its own).
 __device__ __forceinline__ void tile_coords(int t, int tiles_m, int tiles_n, int& tile_m, int& tile_n, int group = 8)
 {
@@ -712,7 +730,8 @@ __global__ void __launch_bounds__(kExpandThreads) expand_activations_stream_kern
     }
 }
 
-template <bool W_IS_NK, bool ACT_BF16, bool CLUSTER, bool WIDE>
+// SCALED: the weights have an exponent for each 128 x 128, which is what a pair block is; the activations carry theirs in their BF16 copy.
+template <bool W_IS_NK, bool ACT_BF16, bool CLUSTER, bool WIDE, bool SCALED = false>
 __global__ void __launch_bounds__(kThreadsN, 1)
 hif8_gemm_narrow_kernel(const __grid_constant__ CUtensorMap map_act, const __grid_constant__ CUtensorMap map_w, const GemmParams p, int mp,
                         const NarrowPlan plan)
@@ -903,8 +922,18 @@ hif8_gemm_narrow_kernel(const __grid_constant__ CUtensorMap map_act, const __gri
         int s8 = group >> 1;  // byte stage of the group's next k-block, and the parity of its round
         uint32_t ph8 = 0;
         const int h = group & 1;  // which k-block of its pair block
+        int sc_slab = slab0, sc_pb = pb0 + (group >> 1);  // SCALED: the pair block's place
+        auto block_exp = [&]() {
+            while (sc_pb >= num_pb) { sc_pb -= num_pb; sc_slab++; }
+            return __ldg(p.w_exp + (W_IS_NK ? (long long)sc_slab * p.w_exp_stride + sc_pb : (long long)sc_pb * p.w_exp_stride + sc_slab));
+        };
+        int e_next = 0;
+        if (SCALED && group < n_it) e_next = block_exp();
         for (int it = group; it < n_it && ok; it += kDecodeGroups) {
             const int s = it % S, r = it / S;
+            const uint32_t scale2 = SCALED ? block_scale2(e_next) : 0u;
+            sc_pb += 2;
+            if (SCALED && it + kDecodeGroups < n_it) e_next = block_exp();  // (the next one, on its way while this k-block is decoded)
             ok = mbar_wait(bar_u8_full(s8), ph8, abort_flag, p.status, 33);
             if (ok && r > 0) ok = mbar_wait(bar_bf_empty(s), (r - 1) & 1, abort_flag, p.status, 34);
             if (!ok) {
@@ -957,6 +986,7 @@ hif8_gemm_narrow_kernel(const __grid_constant__ CUtensorMap map_act, const __gri
                     o[8 * jj + 0] = lo.x; o[8 * jj + 1] = lo.y; o[8 * jj + 2] = lo.z; o[8 * jj + 3] = lo.w;
                     o[8 * jj + 4] = hi.x; o[8 * jj + 5] = hi.y; o[8 * jj + 6] = hi.z; o[8 * jj + 7] = hi.w;
                 }
+                if (SCALED) scale_words(o, scale2);
                 tmem_st_32x32b_x32(st_base, o);
             } else {
 #pragma unroll
@@ -967,6 +997,10 @@ hif8_gemm_narrow_kernel(const __grid_constant__ CUtensorMap map_act, const __gri
                         const uint4 lo = decode8<kLutShiftN>(make_uint2(v.x, v.y), lut), hi = decode8<kLutShiftN>(make_uint2(v.z, v.w), lut);
                         uint32_t* d = o + 16 * c + 8 * i;
                         d[0] = lo.x; d[1] = lo.y; d[2] = lo.z; d[3] = lo.w; d[4] = hi.x; d[5] = hi.y; d[6] = hi.z; d[7] = hi.w;
+                    }
+                    if (SCALED) {
+#pragma unroll
+                        for (int i = 0; i < 16; i++) o[16 * c + i] = mul_bf16x2(o[16 * c + i], scale2);
                     }
                     tmem_st_16x256b_x4(st_base + ((uint32_t)(16 * c) << 16), o + 16 * c);
                 }
@@ -1332,7 +1366,8 @@ __device__ __forceinline__ void store_columns(unsigned char* out, Pitch pitch, i
 enum WeightsForm { kOneGroup, kGroups, kFarRows, kParts };  // up to eight pieces (or sixteen, see launch_weights_gemm); more; the rows of C 4 GiB apart or more (any number of pieces); parts of tiles
 constexpr int kGroupPieces = 8;
 
-template <bool W_IS_NK, int ACT, int FORM>
+// SCALED (expanded activations only): as in the narrow kernel, a k-block of 128 k and a CTA's 128 columns is a block of weights.
+template <bool W_IS_NK, int ACT, int FORM, bool SCALED = false>
 __global__ void __launch_bounds__(kThreadsWd, 1)
 hif8_gemm_weights_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_act, const GemmParams p, const TilePlan tp)
 {
@@ -1551,6 +1586,18 @@ hif8_gemm_weights_kernel(const __grid_constant__ CUtensorMap map_w, const __grid
         constexpr int kGaveUp = 1 << 30;
         int it = decodes ? group : kGaveUp, tile_it = 0, local = 0;  // next k-block of the group; first k-block of the tile to finish next
         bool joined = !decodes;
+        // SCALED: exponent of the weight block of this CTA's x-th k-block, over all its tiles (0 where there is none)
+        auto block_exp = [&](int x) {
+            const int i = x / n_kb, tile = t0 + i * t_step, kb = kb0 + x - i * n_kb;
+            if (tile >= t_end) return 0;
+            int slab, m0;
+            place(tile, slab, m0);
+            const int cb = 2 * slab + (int)half;
+            if (cb * BM >= p.N) return 0;
+            return __ldg(p.w_exp + (W_IS_NK ? (long long)cb * p.w_exp_stride + kb : (long long)kb * p.w_exp_stride + cb));
+        };
+        int e_next = 0;
+        if (SCALED && decodes) e_next = block_exp(it);
         for (int t = t0; t < t_end;) {
             // the group's k-blocks of this tile, and one of the next
             const int n_it_known = t + t_step < t_end ? tile_it + 2 * n_kb : tile_it + n_kb;
@@ -1559,6 +1606,8 @@ hif8_gemm_weights_kernel(const __grid_constant__ CUtensorMap map_w, const __grid
                 bool ok = mbar_wait(bar_u8_full(s), r & 1, abort_flag, p.status, 43);
                 if (ok && r > 0) ok = mbar_wait(bar_bf_empty(s), (r - 1) & 1, abort_flag, p.status, 44);
                 if (!ok) { it += kGaveUp; continue; }  // (no further k-block: gives up at the next wait)
+                const uint32_t scale2 = SCALED ? block_scale2(e_next) : 0u;
+                if (SCALED) e_next = block_exp(it + kDecodeGroups);  // (the next one, on its way while this k-block is decoded)
                 const uint32_t w8 = lay.u8(s), dst = tlane + (uint32_t)(s * (KB / 2));
                 if (ACT != kActExpanded) {
                     // activations as bytes: the tile's 8-byte chunks, up to eight per thread (it lies in a row, [M,K] or [K,M]), two at a time and in
@@ -1618,6 +1667,7 @@ hif8_gemm_weights_kernel(const __grid_constant__ CUtensorMap map_w, const __grid
                         o[8 * j + 0] = lo.x; o[8 * j + 1] = lo.y; o[8 * j + 2] = lo.z; o[8 * j + 3] = lo.w;
                         o[8 * j + 4] = hi.x; o[8 * j + 5] = hi.y; o[8 * j + 6] = hi.z; o[8 * j + 7] = hi.w;
                     }
+                    if (SCALED) scale_words(o, scale2);
                     if (W_IS_NK) tmem_st_32x32b_x32(dst + (uint32_t)(h * (BK / 2)), o);
                     else if (KB == 2 * BK) {
                         tmem_st_16x256b_x4(dst + ((uint32_t)(16 * h) << 16), o);
@@ -2220,11 +2270,11 @@ struct GemmDeviceSetup {
 };
 PerDevice<GemmDeviceSetup> g_gemm_setup;
 
-template <bool ACT_BF16, bool WIDE>
+template <bool ACT_BF16, bool WIDE, bool SCALED = false>
 void narrow_kernels(const void** k)
 {
-    k[0] = (const void*)hif8_gemm_narrow_kernel<false, ACT_BF16, false, WIDE>; k[1] = (const void*)hif8_gemm_narrow_kernel<true, ACT_BF16, false, WIDE>;
-    k[2] = (const void*)hif8_gemm_narrow_kernel<false, ACT_BF16, true, WIDE>; k[3] = (const void*)hif8_gemm_narrow_kernel<true, ACT_BF16, true, WIDE>;
+    k[0] = (const void*)hif8_gemm_narrow_kernel<false, ACT_BF16, false, WIDE, SCALED>; k[1] = (const void*)hif8_gemm_narrow_kernel<true, ACT_BF16, false, WIDE, SCALED>;
+    k[2] = (const void*)hif8_gemm_narrow_kernel<false, ACT_BF16, true, WIDE, SCALED>; k[3] = (const void*)hif8_gemm_narrow_kernel<true, ACT_BF16, true, WIDE, SCALED>;
 }
 template <int FORM>
 void weights_kernels(const void** k)
@@ -2232,6 +2282,7 @@ void weights_kernels(const void** k)
     k[0] = (const void*)hif8_gemm_weights_kernel<false, kActExpanded, FORM>; k[1] = (const void*)hif8_gemm_weights_kernel<true, kActExpanded, FORM>;
     k[2] = (const void*)hif8_gemm_weights_kernel<false, kActRows, FORM>; k[3] = (const void*)hif8_gemm_weights_kernel<true, kActRows, FORM>;
     k[4] = (const void*)hif8_gemm_weights_kernel<false, kActColumns, FORM>; k[5] = (const void*)hif8_gemm_weights_kernel<true, kActColumns, FORM>;
+    k[6] = (const void*)hif8_gemm_weights_kernel<false, kActExpanded, FORM, true>; k[7] = (const void*)hif8_gemm_weights_kernel<true, kActExpanded, FORM, true>;
 }
 
 template <int MT>
@@ -2249,11 +2300,11 @@ bool gemm_kernels_ready(int dev, int* sm_count_out, const int** wd_clusters = nu
         std::memset(out->nw_clusters, 0, sizeof out->nw_clusters);
         const void* pair[4] = {(const void*)bf16_gemm_pair_kernel<false, false>, (const void*)bf16_gemm_pair_kernel<true, false>,
                                (const void*)bf16_gemm_pair_kernel<false, true>, (const void*)bf16_gemm_pair_kernel<true, true>};
-        const void* wd[24];
-        weights_kernels<kOneGroup>(wd); weights_kernels<kGroups>(wd + 6); weights_kernels<kFarRows>(wd + 12); weights_kernels<kParts>(wd + 18);
+        const void* wd[32];
+        weights_kernels<kOneGroup>(wd); weights_kernels<kGroups>(wd + 8); weights_kernels<kFarRows>(wd + 16); weights_kernels<kParts>(wd + 24);
         for (int i = 0; i < 4 && out->rc == cudaSuccess; i++)
             out->rc = cudaFuncSetAttribute(pair[i], cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes2);
-        for (int i = 0; i < 24 && out->rc == cudaSuccess; i++)
+        for (int i = 0; i < 32 && out->rc == cudaSuccess; i++)
             out->rc = cudaFuncSetAttribute(wd[i], cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytesMax);
         for (int s = 1; s <= kWdMaxSplit && out->rc == cudaSuccess; s *= 2) {
             cudaLaunchConfig_t cfg{};
@@ -2264,9 +2315,9 @@ bool gemm_kernels_ready(int dev, int* sm_count_out, const int** wd_clusters = nu
             cfg.attrs = attr; cfg.numAttrs = 1;
             out->rc = cudaOccupancyMaxActiveClusters(&out->wd_clusters[s], wd[1], &cfg);
         }
-        const void* narrow[12];
-        narrow_kernels<false, true>(narrow); narrow_kernels<true, true>(narrow + 4); narrow_kernels<false, false>(narrow + 8);
-        for (int i = 0; i < 12 && out->rc == cudaSuccess; i++)
+        const void* narrow[16];
+        narrow_kernels<false, true>(narrow); narrow_kernels<true, true>(narrow + 4); narrow_kernels<false, false>(narrow + 8); narrow_kernels<true, true, true>(narrow + 12);
+        for (int i = 0; i < 16 && out->rc == cudaSuccess; i++)
             out->rc = cudaFuncSetAttribute(narrow[i], cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytesMax);
         for (int s = 1; s <= kNwMaxSplit && out->rc == cudaSuccess; s *= 2) {
             cudaLaunchConfig_t cfg{};
@@ -2466,6 +2517,10 @@ template <int ACT, int FORM>
 static cudaError_t launch_weights_form(const cudaLaunchConfig_t& cfg, int w_is_nk, const CUtensorMap& map_w, const CUtensorMap& map_act, const GemmParams& p,
                                        const TilePlan& tp)
 {
+    if constexpr (ACT == kActExpanded)
+        if (p.w_exp)
+            return w_is_nk ? cudaLaunchKernelEx(&cfg, hif8_gemm_weights_kernel<true, ACT, FORM, true>, map_w, map_act, p, tp)
+                           : cudaLaunchKernelEx(&cfg, hif8_gemm_weights_kernel<false, ACT, FORM, true>, map_w, map_act, p, tp);
     return w_is_nk ? cudaLaunchKernelEx(&cfg, hif8_gemm_weights_kernel<true, ACT, FORM>, map_w, map_act, p, tp)
                    : cudaLaunchKernelEx(&cfg, hif8_gemm_weights_kernel<false, ACT, FORM>, map_w, map_act, p, tp);
 }
@@ -2531,20 +2586,49 @@ static int launch_weights_gemm(const uint8_t* Wq, int64_t ldw, int w_is_nk, cons
     return cudaGetLastError() == cudaSuccess ? HIF8_OK : HIF8_ERR_CUDA;
 }
 
-template <bool W_IS_NK, bool ACT_BF16, bool WIDE>
+template <bool W_IS_NK, bool ACT_BF16, bool WIDE, bool SCALED = false>
 static cudaError_t launch_narrow_form(const cudaLaunchConfig_t& cfg, bool cluster, const CUtensorMap& map_act, const CUtensorMap& map_w, const GemmParams& p,
                                       int mp, const NarrowPlan& plan)
 {
-    return cluster ? cudaLaunchKernelEx(&cfg, hif8_gemm_narrow_kernel<W_IS_NK, ACT_BF16, true, WIDE>, map_act, map_w, p, mp, plan)
-                   : cudaLaunchKernelEx(&cfg, hif8_gemm_narrow_kernel<W_IS_NK, ACT_BF16, false, WIDE>, map_act, map_w, p, mp, plan);
+    return cluster ? cudaLaunchKernelEx(&cfg, hif8_gemm_narrow_kernel<W_IS_NK, ACT_BF16, true, WIDE, SCALED>, map_act, map_w, p, mp, plan)
+                   : cudaLaunchKernelEx(&cfg, hif8_gemm_narrow_kernel<W_IS_NK, ACT_BF16, false, WIDE, SCALED>, map_act, map_w, p, mp, plan);
 }
 template <bool W_IS_NK>
 static cudaError_t launch_narrow_kernel(const cudaLaunchConfig_t& cfg, bool cluster, bool act_bf16, const CUtensorMap& map_act, const CUtensorMap& map_w,
                                         const GemmParams& p, int mp, const NarrowPlan& plan)
 {
+    if (p.w_exp) return launch_narrow_form<W_IS_NK, true, true, true>(cfg, cluster, map_act, map_w, p, mp, plan);  // (activations in BF16)
     if (act_bf16) return launch_narrow_form<W_IS_NK, true, true>(cfg, cluster, map_act, map_w, p, mp, plan);
     return mp <= kNwWideBytesM ? launch_narrow_form<W_IS_NK, false, true>(cfg, cluster, map_act, map_w, p, mp, plan)
                                : launch_narrow_form<W_IS_NK, false, false>(cfg, cluster, map_act, map_w, p, mp, plan);
+}
+
+// act_bf16: the launch right in front expands the activations and lets its dependents start at once; this one waits for its completion once its own set-up is done.
+static int launch_narrow(const NarrowPlan& plan, long long grid, bool act_bf16, const CUtensorMap& map_act, const CUtensorMap& map_ws, const GemmParams& p, int mp, int w_is_nk,
+                         cudaStream_t st)
+{
+    cudaLaunchConfig_t cn{};
+    cn.gridDim = dim3((unsigned)grid);
+    cn.blockDim = dim3(kThreadsN);
+    cn.dynamicSmemBytes = kSmemBytesMax;
+    cn.stream = st;
+    cudaLaunchAttribute an[2];
+    int n_an = 0;
+    if (act_bf16) {
+        an[n_an].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        an[n_an++].val.programmaticStreamSerializationAllowed = 1;
+    }
+    if (plan.split > 1) {
+        an[n_an].id = cudaLaunchAttributeClusterDimension;
+        an[n_an].val.clusterDim.x = (unsigned)plan.split; an[n_an].val.clusterDim.y = 1; an[n_an++].val.clusterDim.z = 1;
+    }
+    cn.attrs = an; cn.numAttrs = (unsigned)n_an;
+    const bool cluster = plan.split > 1;
+    const cudaError_t rc = w_is_nk ? launch_narrow_kernel<true>(cn, cluster, act_bf16, map_act, map_ws, p, mp, plan)
+                                   : launch_narrow_kernel<false>(cn, cluster, act_bf16, map_act, map_ws, p, mp, plan);
+    if (rc != cudaSuccess) return HIF8_ERR_CUDA;
+    g_launches.fetch_add(1, std::memory_order_relaxed);
+    return cudaGetLastError() == cudaSuccess ? HIF8_OK : HIF8_ERR_CUDA;
 }
 
 // How the warp kernel divides a product, and what that takes in cycles from call to results.  The terms are fitted to 670 measured
@@ -2834,31 +2918,7 @@ static int gemm_entry(const uint8_t* Aq, int64_t lda, int a_is_km, const uint8_t
         }
         plan.clear_status = !act_bf16 && !plan.tickets;
         if (!act_bf16 && plan.tickets && cudaMemsetAsync(workspace, 0, clear_bytes, st) != cudaSuccess) return HIF8_ERR_CUDA;
-        cudaLaunchConfig_t cn{};
-        cn.gridDim = dim3((unsigned)grid);
-        cn.blockDim = dim3(kThreadsN);
-        cn.dynamicSmemBytes = kSmemBytesMax;
-        cn.stream = st;
-        // with the preparing kernel right in front: programmatic stream serialization (that kernel lets its dependents start
-        // at once; this one waits for its completion once its own set-up is done)
-        cudaLaunchAttribute an[2];
-        int n_an = 0;
-        if (act_bf16) {
-            an[n_an].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-            an[n_an++].val.programmaticStreamSerializationAllowed = 1;
-        }
-        if (plan.split > 1) {
-            an[n_an].id = cudaLaunchAttributeClusterDimension;
-            an[n_an].val.clusterDim.x = (unsigned)plan.split; an[n_an].val.clusterDim.y = 1; an[n_an++].val.clusterDim.z = 1;
-        }
-        cn.attrs = an; cn.numAttrs = (unsigned)n_an;
-        cudaError_t nrc;
-        const bool cluster = plan.split > 1;
-        nrc = w_is_nk ? launch_narrow_kernel<true>(cn, cluster, act_bf16, map_act, map_ws, p, mp, plan)
-                      : launch_narrow_kernel<false>(cn, cluster, act_bf16, map_act, map_ws, p, mp, plan);
-        if (nrc != cudaSuccess) return HIF8_ERR_CUDA;
-        g_launches.fetch_add(1, std::memory_order_relaxed);
-        return cudaGetLastError() == cudaSuccess ? HIF8_OK : HIF8_ERR_CUDA;
+        return launch_narrow(plan, grid, act_bf16, map_act, map_ws, p, mp, w_is_nk, st);
     }
 
     if (choice.form == kFormWeights && choice.weights.act != kActExpanded) return launch_weights_gemm(Wq, ldw, w_is_nk, choice.weights, Aq, lda, p, wd_clusters, st);
@@ -2875,6 +2935,68 @@ static int gemm_entry(const uint8_t* Aq, int64_t lda, int a_is_km, const uint8_t
     // million codes that costs more than such a table saves, 2758 x 2816 x 848 21.1 -> 22.3 us)
     rc = decode_codes(Wq, w_bf, HIF8_BF16, (size_t)K * N, 0, (size_t)1 << 23, st);
     return rc != HIF8_OK ? rc : launch_bf16_pair_gemm(a_bf, w_bf, w_is_nk, p, st);
+}
+
+// Block-scaled operands.  The activations are expanded to BF16 with their scales in front, whatever the kernel.  Weights with a scale for each 128 x 128 and K a
+// multiple of 16 are decoded in the kernel: up to 64 rows by the narrow one, beyond by the weights one, until expanding them pays (as for
+// hif8_gemm, with more to win back: 3 bytes an element).  Other weights (activations of a gradient's product, with a scale for each 1 x 128) are expanded too.
+int hif8::launch_block_gemm(const BlockCodes& a, bool a_is_km, const BlockCodes& w, bool w_is_nk, const GemmParams& params, const BlockWorkspace& sizes, void* workspace, cudaStream_t st)
+{
+    GemmParams p = params;
+    const int M = p.M, N = p.N, K = p.K;
+    int dev = 0, sm_count = 0;
+    const int *wd_clusters = nullptr, *nw_clusters = nullptr;
+    if (cudaGetDevice(&dev) != cudaSuccess || !gemm_kernels_ready(dev, &sm_count, &wd_clusters, &nw_clusters)) return HIF8_ERR_CUDA;
+    unsigned char* wsb = reinterpret_cast<unsigned char*>(workspace) + BlockWorkspace::kStatus;
+    unsigned char* a_bf = wsb;
+    const long long a_rows = a_is_km ? sizes.a_pitch : M, a_cols = a_is_km ? M : sizes.a_pitch;
+    auto expand_a = [&](size_t clear_bytes) {
+        return expand_block_codes(a, a_bf, sizes.a_pitch, a_rows, a_cols, a_is_km, reinterpret_cast<uint32_t*>(workspace), (unsigned)(clear_bytes / 4), st);
+    };
+    if (sizes.in_kernel && M <= BlockWorkspace::kNarrowRows) {
+        p.w_exp = w.exps; p.w_exp_stride = w.exp_stride;
+        const int mp = (M + 15) & ~15;
+        const long long slabs = (N + BM - 1) / BM, num_pb = (K + BK2 - 1) / BK2, total = slabs * num_pb;
+        if (total > 0x3FFFFFFF) return HIF8_ERR_SHAPE;
+        const NarrowTiling nt(M, N, K, sm_count, nw_clusters, true);
+        NarrowPlan plan{};
+        plan.split = nt.split;
+        long long grid = slabs * plan.split;
+        size_t clear_bytes = 4;
+        const size_t ticket_bytes = (((size_t)slabs * kEpiWarps * 4) + 255) & ~(size_t)255, part_bytes = (size_t)slabs * nt.pmax * mp * BM * 4;
+        a_bf = wsb + sizes.narrow_bytes;
+        if (nt.ranges && ticket_bytes + part_bytes <= sizes.narrow_bytes) {
+            plan.tickets = reinterpret_cast<unsigned*>(wsb);
+            plan.part = reinterpret_cast<float*>(wsb + ticket_bytes);
+            plan.pmax = (int)nt.pmax;
+            plan.split = 0;
+            grid = nt.grid;
+            clear_bytes = BlockWorkspace::kStatus + ticket_bytes;  // the tickets follow the status word
+        }
+        if (grid > 0x7FFFFFFFll) return HIF8_ERR_SHAPE;
+        plan.q = (int)(total / grid); plan.rem = (int)(total % grid);
+        CUtensorMap map_act, map_ws;
+        if (!make_map(&map_act, a_bf, (uint64_t)K, (uint64_t)M, (uint64_t)sizes.a_pitch, BK, (uint32_t)mp, true)) return HIF8_ERR_CUDA;
+        const bool okn = w_is_nk ? make_map(&map_ws, w.codes, (uint64_t)K, (uint64_t)N, (uint64_t)w.ld, BK2, BM, false, 128)
+                                 : make_map(&map_ws, w.codes, (uint64_t)N, (uint64_t)K, (uint64_t)w.ld, BM, BK2, false, 128, true);
+        if (!okn) return HIF8_ERR_CUDA;
+        if (int rc = expand_a(clear_bytes)) return rc;
+        return launch_narrow(plan, grid, true, map_act, map_ws, p, mp, w_is_nk, st);
+    }
+    if (sizes.in_kernel) {
+        const WeightsTiling tl(M, N, K, kActExpanded, a_is_km, wd_clusters);
+        const long long pair_rounds = ((long long)((M + 2 * BM - 1) / (2 * BM)) * ((N + BN - 1) / BN) + sm_count / 2 - 1) / (sm_count / 2);
+        const double expand_w = 6000.0 + 3.0 * (double)K * N / 3300.0, pair_cycles = (double)pair_rounds * ((K + BK - 1) / BK * 545.0 + 500.0);
+        if (sizes.w_bytes == 0 || expand_w + pair_cycles >= 1.03 * tl.cost.all(tl.tiles)) {
+            p.w_exp = w.exps; p.w_exp_stride = w.exp_stride;
+            if (int rc = expand_a(4)) return rc;
+            return launch_weights_gemm(w.codes, w.ld, w_is_nk, tl, a_bf, K, p, wd_clusters, st);
+        }
+    }
+    unsigned char* w_bf = a_bf + sizes.a_bytes;
+    if (int rc = expand_a(4)) return rc;
+    if (int rc = expand_block_codes(w, w_bf, sizes.w_pitch, w.rows, sizes.w_pitch, false, nullptr, 0, st)) return rc;
+    return launch_bf16_pair_gemm(a_bf, w_bf, w_is_nk, p, st, 0, 0, sizes.a_pitch, sizes.w_pitch);
 }
 
 extern "C" int hif8_gemm(const uint8_t* Aq, int64_t lda, const uint8_t* Wq, int64_t ldw, int w_is_nk, void* C, int64_t ldc,

@@ -40,7 +40,7 @@ REFUSED = {
                  (dict(dx=20 * M), OVERLAP), (dict(d_weight_grad=21 * M + 4), OVERLAP), (dict(d_weight_grad=64 * M), OVERLAP), (dict(workspace=16 * M), OVERLAP), (dict(cols=0), OK)],
     "gemm": [(dict(c_dtype=H.F16), DTYPE), (dict(M=-1), SHAPE), (dict(K=0), SHAPE), (dict(a_block_rows=2), SHAPE), (dict(w_block_rows=64), SHAPE), (dict(lda=249), SHAPE), (dict(ldw=249), SHAPE),
              (dict(ldc=56), SHAPE), (dict(exp_stride_a=1), SHAPE), (dict(exp_stride_w=1), SHAPE), (dict(a_is_km=1, lda=49), SHAPE), (dict(w_is_nk=0, ldw=59), SHAPE), (dict(Aq=None), NULL), (dict(Wq=None), NULL),
-             (dict(Cmat=None), NULL), (dict(d_exp_a=None), NULL), (dict(d_exp_w=None), NULL), (dict(Cmat=20 * M + 8), ALIGN), (dict(ldc=61), ALIGN), (dict(d_exp_a=17 * M + 2), ALIGN),
+             (dict(Cmat=None), NULL), (dict(d_exp_a=None), NULL), (dict(d_exp_w=None), NULL), (dict(Cmat=20 * M + 8), ALIGN), (dict(Aq=16 * M + 8), ALIGN), (dict(Wq=18 * M + 1), ALIGN), (dict(lda=264), ALIGN), (dict(ldw=257), ALIGN), (dict(ldc=61), ALIGN), (dict(d_exp_a=17 * M + 2), ALIGN),
              (dict(d_exp_w=19 * M + 1), ALIGN), (dict(workspace=None), WORKSPACE), (dict(workspace=64 * M + 16), WORKSPACE), (dict(workspace_bytes=255), WORKSPACE), (dict(Cmat=16 * M), OVERLAP),
              (dict(Cmat=18 * M), OVERLAP), (dict(Cmat=19 * M), OVERLAP), (dict(Cmat=64 * M + 256), OVERLAP), (dict(workspace=16 * M), OVERLAP), (dict(M=0), OK), (dict(N=0), OK)],
     "clip": [(dict(max_norm=0.0), RANGE), (dict(max_norm=-1.0), RANGE), (dict(max_norm=float("nan")), RANGE), (dict(n_tensors=-1), SHAPE), (dict(n_elements=-1), SHAPE), (dict(n_elements=1 << 51), SHAPE),

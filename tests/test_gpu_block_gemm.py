@@ -72,8 +72,8 @@ def test_blocks_and_layouts(w_is_nk, ab, wb, a_is_km, c_dtype, accumulate):
     check(20, 392, 528, a_is_km, ab, w_is_nk, wb, c_dtype, accumulate, seed=4)
 
 
-@pytest.mark.parametrize("how", [dict(lda=304, ldw=320), dict(lda=301, ldw=303), dict(a_offset=16, w_offset=32), dict(a_offset=1, w_offset=3), dict(ldc=272), dict(lda=304, w_offset=5)])
-@pytest.mark.parametrize("M", [7, 150])
+@pytest.mark.parametrize("how", [dict(lda=304, ldw=320), dict(a_offset=16, w_offset=32), dict(ldc=272), dict(lda=1024, w_offset=48, ldc=1000)])
+@pytest.mark.parametrize("M", [7, 150, 600])
 def test_strides_and_alignments(M, how):
     check(M, 256, 288, seed=5, **how)
 
