@@ -19,7 +19,8 @@ struct EncodeParams {
     int target_exp;
     unsigned flags;
     unsigned long long seed;
-    bool vectors, codes8;  // rows of the source start on 16-byte boundaries, those of the codes on 8-byte ones
+    bool vectors, vectors32, codes8, codes16;  // rows of the source start on boundaries of 16 and 32 bytes, those of the codes of 8 and 16
+    bool late;             // the next launch may start at the end (see launch_encode)
 };
 
 // eight elements -> codes; `flat`: the flat index of the first one (stochastic rounding draws by it)
@@ -56,51 +57,78 @@ __device__ __forceinline__ uint32_t amax_of_eight(const Eight<SRC>& e)
     return __float_as_uint(amax_value<SRC>(m));
 }
 
-// Blocks of 1 x 128: a warp takes 2 UN consecutive ones at a time, half a warp every other one.
-template <int SRC, int MODE, int UN>
-__global__ void __launch_bounds__(kThreads) block_row_encode_kernel(const EncodeParams p)
+// Sixteen neighbouring elements of a row, from column c on; `vectors32`: the row starts on a 32-byte boundary
+template <int DT> struct Sixteen { Eight<DT> lo, hi; };
+template <int DT>
+__device__ __forceinline__ Sixteen<DT> load_sixteen(const void* row, long long c, long long cols, bool vectors, bool vectors32)
+{
+    Sixteen<DT> s;
+    if (vectors32 && c + 16 <= cols) {
+        const char* p = reinterpret_cast<const char*>(row) + c * (DT == HIF8_F32 ? 4 : 2);
+        auto get = [](const char* from, uint4& a, uint4& b) {
+            asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "l"(from));
+        };
+        constexpr int last = sizeof(s.lo.v) / 16 - 1;
+        if (DT == HIF8_F32) {
+            get(p, s.lo.v[0], s.lo.v[last]);
+            get(p + 32, s.hi.v[0], s.hi.v[last]);
+        } else get(p, s.lo.v[0], s.hi.v[0]);
+        return s;
+    }
+    s.lo = load_eight<DT>(row, c, cols, vectors);
+    s.hi = load_eight<DT>(row, c + 8, cols, vectors);
+    return s;
+}
+
+// Blocks of 1 x 128: eight threads to a block, four blocks to a warp and step.  Issue slots are what it costs beside the bytes: with sixteen threads of eight elements each, four
+// steps in flight, it took 17.6 instructions an element (16384 x 8192, us: BF16 94.6, FP16 89.8, FP32 109.7; so 70.9, 68.9 and 100.0; with two steps in flight and fewer blocks
+// 73.0, 71.3 and 101.0).
+constexpr int row_blocks(int src, int mode) { return mode == HIF8_RND_SR ? 2 : src == HIF8_F32 ? 5 : 6; }
+template <int SRC, int MODE>
+__global__ void __launch_bounds__(kThreads, row_blocks(SRC, MODE)) block_row_encode_kernel(const EncodeParams p)
 {
     __shared__ SmemTables sm;
     setup_tables<true, MODE != HIF8_RND_TA, false, MODE, SRC>(sm, p.flags);
     pdl_wait_prior_grid();
-    pdl_launch_dependents();
+    if (!p.late) pdl_launch_dependents();
     constexpr size_t item = SRC == HIF8_F32 ? 4 : 2;
-    const unsigned lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, half = lane >> 4, at = (lane & 15u) * 8u;
-    const unsigned warps = gridDim.x * (kThreads / 32);
-    for (unsigned long long first = (unsigned long long)(blockIdx.x * (kThreads / 32) + warp) * (2 * UN); first < p.units; first += (unsigned long long)warps * (2 * UN)) {
-        unsigned row[UN], blk[UN];
-        Eight<SRC> e[UN];
+    const unsigned lane = threadIdx.x & 31u, part = lane >> 3, at = (lane & 7u) * 16u;
+    const unsigned warp = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), warps = gridDim.x * (kThreads / 32);
+    for (unsigned long long first = (unsigned long long)warp * 4; first < p.units; first += (unsigned long long)warps * 4) {
+        const unsigned u = (unsigned)first + part, row = p.across.div(u), blk = u - row * p.across.d;
+        const long long c = (long long)blk * 128 + at;
+        const Sixteen<SRC> e = load_sixteen<SRC>(reinterpret_cast<const char*>(p.src) + (size_t)row * (size_t)p.ld_src * item, u < p.units ? c : p.m.cols, p.m.cols, p.vectors, p.vectors32);
+        uint32_t top = max(amax_of_eight<SRC>(e.lo), amax_of_eight<SRC>(e.hi));
 #pragma unroll
-        for (int j = 0; j < UN; j++) {
-            const unsigned u = (unsigned)first + half + 2 * j;
-            row[j] = p.across.div(u); blk[j] = u - row[j] * p.across.d;
-            const long long c = (long long)blk[j] * 128 + at;
-            e[j] = load_eight<SRC>(reinterpret_cast<const char*>(p.src) + (size_t)row[j] * (size_t)p.ld_src * item, u < p.units ? c : p.m.cols, p.m.cols, p.vectors);
-        }
-#pragma unroll
-        for (int j = 0; j < UN; j++) {
-            const uint32_t top = half_warp_max(amax_of_eight<SRC>(e[j]));
-            const int se = block_exp_from_amax(top, p.target_exp);
-            if ((unsigned)first + half + 2 * j >= p.units) continue;
-            const long long c = (long long)blk[j] * 128 + at;
-            if (c < p.m.cols) {
-                const uint2 w = encode_eight<SRC, MODE>(e[j], pow2f(se), sm, (unsigned long long)row[j] * (unsigned long long)p.m.cols + (unsigned long long)c, p.seed);
-                store_codes8(p.m.codes + (size_t)row[j] * (size_t)p.m.ld, c, p.m.cols, p.codes8, w);
-            }
-            if (at == 0) p.m.exps[(size_t)row[j] * (size_t)p.m.exp_stride + blk[j]] = se;
+        for (int d = 4; d; d >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+        const int se = block_exp_from_amax(top, p.target_exp);
+        if (u >= p.units) continue;
+        if (at == 0) p.m.exps[(size_t)row * (size_t)p.m.exp_stride + blk] = se;
+        if (c >= p.m.cols) continue;
+        const float scale = pow2f(se);
+        const unsigned long long flat = (unsigned long long)row * (unsigned long long)p.m.cols + (unsigned long long)c;
+        const uint2 lo = encode_eight<SRC, MODE>(e.lo, scale, sm, flat, p.seed), hi = encode_eight<SRC, MODE>(e.hi, scale, sm, flat + 8, p.seed);
+        uint8_t* out = p.m.codes + (size_t)row * (size_t)p.m.ld;
+        if (p.codes16 && c + 16 <= p.m.cols) *reinterpret_cast<uint4*>(out + c) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+        else {
+            store_codes8(out, c, p.m.cols, p.codes8, lo);
+            store_codes8(out, c + 8, p.m.cols, p.codes8, hi);
         }
     }
+    if (p.late) pdl_launch_dependents();
 }
 
 // Blocks of 128 x 128: a thread block takes one at a time, half a warp eight of its rows.
+constexpr int tile_blocks(int src) { return src == HIF8_F32 ? 2 : 4; }
 template <int SRC, int MODE>
-__global__ void __launch_bounds__(kThreads) block_tile_encode_kernel(const EncodeParams p)
+__global__ void __launch_bounds__(kThreads, tile_blocks(SRC)) block_tile_encode_kernel(const EncodeParams p)
 {
     __shared__ SmemTables sm;
     __shared__ uint32_t s_top[2][kThreads / 32];
     setup_tables<true, MODE != HIF8_RND_TA, false, MODE, SRC>(sm, p.flags);
     pdl_wait_prior_grid();
-    pdl_launch_dependents();
+    if (!p.late) pdl_launch_dependents();
     constexpr size_t item = SRC == HIF8_F32 ? 4 : 2;
     constexpr int kRows = 128 / (kThreads / 16);
     const unsigned at = (threadIdx.x & 15u) * 8u, r0 = threadIdx.x >> 4;
@@ -136,6 +164,7 @@ __global__ void __launch_bounds__(kThreads) block_tile_encode_kernel(const Encod
             }
         }
     }
+    if (p.late) pdl_launch_dependents();
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -145,11 +174,12 @@ struct DecodeParams {
     BlockCodes m;
     void* dst;
     long long ld_dst, rows_out, cols_out;
-    FastDiv chunks;      // groups of eight columns of a row that is written
+    FastDiv chunks;      // groups of sixteen columns of a row that is written
     unsigned units;      // such groups
-    bool codes8, vectors;  // rows of the codes start on 8-byte boundaries, those written on 16-byte ones
+    bool codes8, codes16, vectors, vectors32;  // rows of the codes start on boundaries of 8 and of 16 bytes, those written of 16 and of 32
     uint32_t* clear;
     unsigned clear_words;
+    bool late;           // the next launch may start at the end (see launch_decode)
 };
 
 __device__ __forceinline__ int exp_at(const BlockCodes& m, long long r, long long c)
@@ -182,40 +212,87 @@ __device__ __forceinline__ Eight<DST> scaled_eight(uint2 lo, uint2 hi, int e)
     return pack_eight<DST>(x);
 }
 
+// sixteen values of a row: two words of 32 bytes (FP32) or one, whole sectors a lane where the row lies so
+template <int DST>
+__device__ __forceinline__ void store_sixteen(void* row, unsigned c, long long cols, bool vectors, bool vectors32, const Eight<DST>& lo, const Eight<DST>& hi)
+{
+    if (vectors32 && c + 16 <= cols) {
+        char* p = reinterpret_cast<char*>(row) + (size_t)c * (DST == HIF8_F32 ? 4 : 2);
+        auto put = [](char* to, const uint4& a, const uint4& b) {
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                         ::"l"(to), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
+        };
+        constexpr int last = sizeof(lo.v) / 16 - 1;
+        if (DST == HIF8_F32) {
+            put(p, lo.v[0], lo.v[last]);
+            put(p + 32, hi.v[0], hi.v[last]);
+        } else put(p, lo.v[0], hi.v[0]);
+        return;
+    }
+    store_eight<DST>(row, c, cols, vectors, lo);
+    store_eight<DST>(row, c + 8, cols, vectors, hi);
+}
+
 // LANE: a copy of the table for each lane.  One table for all costs a warp several wavefronts a lookup; filling 32 copies costs a block more than a
-// small matrix takes.
+// small matrix takes.  The next groups' codes are on their way while those at hand are looked up.
 template <int DST, bool LANE, int UN>
-__global__ void __launch_bounds__(kThreads) block_decode_kernel(const DecodeParams p)
+__global__ void __launch_bounds__(kThreads, LANE ? 6 : 4) block_decode_kernel(const DecodeParams p)
 {
     __shared__ __align__(16) uint32_t table[LANE ? kLaneTableWords : 256];
     if (LANE) fill_lane_table(table, decode_bits_f32(threadIdx.x) >> 16);
     else table[threadIdx.x] = decode_bits_f32(threadIdx.x) >> 16;
     __syncthreads();
     pdl_wait_prior_grid();
-    pdl_launch_dependents();
+    if (!p.late) pdl_launch_dependents();
     if (blockIdx.x == 0)
         for (unsigned i = threadIdx.x; i < p.clear_words; i += kThreads) p.clear[i] = 0u;
     const uint32_t lane4 = (threadIdx.x & 31u) * 4u;
-    for (unsigned long long base = (unsigned long long)blockIdx.x * (kThreads * UN) + threadIdx.x; base < p.units; base += (unsigned long long)gridDim.x * (kThreads * UN)) {
-        uint2 v[UN];
-        int e[UN];
+    constexpr size_t item = DST == HIF8_F32 ? 4 : 2;
+    struct Group {
+        uint4 v;
+        int e;
+        unsigned row, col;
+    };
+    auto load = [&](unsigned long long u64) {
+        Group g;
+        g.v = make_uint4(0u, 0u, 0u, 0u);
+        g.e = 0; g.row = 0; g.col = 0;
+        if (u64 >= p.units) return g;
+        const unsigned u = (unsigned)u64;
+        g.row = p.chunks.div(u); g.col = (u - g.row * p.chunks.d) * 16u;
+        if (g.row < p.m.rows && g.col < p.m.cols) {
+            const uint8_t* at = p.m.codes + (size_t)g.row * (size_t)p.m.ld;
+            g.e = exp_at(p.m, g.row, g.col);
+            if (p.codes16 && g.col + 16 <= p.m.cols) g.v = __ldcs(reinterpret_cast<const uint4*>(at + g.col));
+            else {
+                const uint2 lo = load_codes8(at, g.col, p.m.cols, p.codes8), hi = load_codes8(at, g.col + 8, p.m.cols, p.codes8);
+                g.v = make_uint4(lo.x, lo.y, hi.x, hi.y);
+            }
+        }
+        return g;
+    };
+    const unsigned long long step = (unsigned long long)gridDim.x * (kThreads * UN);
+    unsigned long long base = (unsigned long long)blockIdx.x * (kThreads * UN) + threadIdx.x;
+    Group next[UN];
+#pragma unroll
+    for (int j = 0; j < UN; j++) next[j] = load(base + j * kThreads);
+    for (; base < p.units; base += step) {
+        Group now[UN];
 #pragma unroll
         for (int j = 0; j < UN; j++) {
-            const unsigned u = (unsigned)base + j * kThreads;
-            const unsigned row = p.chunks.div(u), c = (u - row * p.chunks.d) * 8u;
-            const bool inside = u < p.units && row < p.m.rows && c < p.m.cols;
-            v[j] = inside ? load_codes8(p.m.codes + (size_t)row * (size_t)p.m.ld, c, p.m.cols, p.codes8) : make_uint2(0u, 0u);
-            e[j] = inside ? exp_at(p.m, row, c) : 0;
+            now[j] = next[j];
+            if (LANE) next[j] = load(base + step + j * kThreads);
         }
 #pragma unroll
         for (int j = 0; j < UN; j++) {
-            const unsigned u = (unsigned)base + j * kThreads;
-            if (u >= p.units) continue;
-            const unsigned row = p.chunks.div(u), c = (u - row * p.chunks.d) * 8u;
-            const Eight<DST> x = scaled_eight<DST>(bf16_of_four<LANE>(table, v[j].x, lane4), bf16_of_four<LANE>(table, v[j].y, lane4), e[j]);
-            store_eight<DST>(reinterpret_cast<char*>(p.dst) + (size_t)row * (size_t)p.ld_dst * (DST == HIF8_F32 ? 4 : 2), c, p.cols_out, p.vectors, x);
+            if (base + j * kThreads >= p.units) continue;
+            const Eight<DST> lo = scaled_eight<DST>(bf16_of_four<LANE>(table, now[j].v.x, lane4), bf16_of_four<LANE>(table, now[j].v.y, lane4), now[j].e);
+            const Eight<DST> hi = scaled_eight<DST>(bf16_of_four<LANE>(table, now[j].v.z, lane4), bf16_of_four<LANE>(table, now[j].v.w, lane4), now[j].e);
+            store_sixteen<DST>(reinterpret_cast<char*>(p.dst) + (size_t)now[j].row * (size_t)p.ld_dst * item, now[j].col, p.cols_out, p.vectors, p.vectors32, lo, hi);
         }
+        if (!LANE) break;  // (as many threads as groups)
     }
+    if (p.late) pdl_launch_dependents();
 }
 
 // Codes [rows, cols] -> BF16 [cols, ld_dst], transposed: tiles of 64 rows by 64 columns.  A thread takes two rows' eight columns and puts a column's two
@@ -272,18 +349,20 @@ int finish(int launches)
     return cudaGetLastError() == cudaSuccess ? HIF8_OK : HIF8_ERR_CUDA;
 }
 
+// Large matrices: as many blocks as are resident, since a second round of blocks as long as the first one would find the device half empty.  (Blocks of the next launch
+// that only wait take the places that are free, and sit unevenly when they start: behind launches of several rounds they come at the end.)
 template <int SRC, int MODE>
-void launch_encode(const EncodeParams& p, int sms, cudaStream_t st)
+void launch_encode(EncodeParams p, int sms, cudaStream_t st)
 {
     if (p.m.shift == 7) {
-        const unsigned most = (unsigned)sms * 6u;
-        launch_pdl(block_tile_encode_kernel<SRC, MODE>, dim3(p.units < most ? p.units : most), st, p);
+        const unsigned most = (unsigned)(sms * tile_blocks(SRC));
+        p.late = p.units > most;
+        launch_pdl(block_tile_encode_kernel<SRC, MODE>, dim3(p.late ? most : p.units), st, p);
         return;
     }
-    // (a warp that has one pair of blocks waits for memory once; with four pairs, which large matrices need to keep memory busy, it converts them one after the other)
-    const unsigned most = (unsigned)sms * 8u, blocks1 = (p.units + 15u) / 16u, blocks4 = (p.units + 63u) / 64u;
-    if (blocks1 <= most) launch_pdl(block_row_encode_kernel<SRC, MODE, 1>, dim3(blocks1), st, p);
-    else launch_pdl(block_row_encode_kernel<SRC, MODE, 4>, dim3(blocks4 < most ? blocks4 : most), st, p);
+    const unsigned blocks = (p.units + 31u) / 32u, most = (unsigned)(sms * row_blocks(SRC, MODE));
+    p.late = blocks > most;
+    launch_pdl(block_row_encode_kernel<SRC, MODE>, dim3(p.late ? most : blocks), st, p);
 }
 template <int SRC>
 void launch_encode_mode(int rnd, const EncodeParams& p, int sms, cudaStream_t st)
@@ -298,11 +377,14 @@ void launch_encode_mode(int rnd, const EncodeParams& p, int sms, cudaStream_t st
 }
 
 template <int DST>
-void launch_decode(const DecodeParams& p, int sms, cudaStream_t st)
+void launch_decode(DecodeParams p, int sms, cudaStream_t st)
 {
-    const unsigned most = (unsigned)sms * 6u, few = (p.units + kThreads - 1) / kThreads, blocks = (p.units + 4 * kThreads - 1) / (4 * kThreads);
-    if (few <= (unsigned)sms * 8u) launch_pdl(block_decode_kernel<DST, false, 1>, dim3(few), st, p);
-    else launch_pdl(block_decode_kernel<DST, true, 4>, dim3(blocks < most ? blocks : most), st, p);
+    const unsigned most = (unsigned)sms * 6u, few = (p.units + kThreads - 1) / kThreads;
+    if (few <= (unsigned)sms * 4u) launch_pdl(block_decode_kernel<DST, false, 1>, dim3(few), st, p);
+    else {
+        p.late = true;
+        launch_pdl(block_decode_kernel<DST, true, 1>, dim3(few < most ? few : most), st, p);
+    }
 }
 
 }  // namespace
@@ -313,9 +395,9 @@ int expand_block_codes(const BlockCodes& m, void* dst, long long ld_dst, long lo
     int sms; if (int rc = checked_device(&sms)) return rc;
     DecodeParams p{};
     p.m = m; p.dst = dst; p.ld_dst = ld_dst; p.rows_out = rows_out; p.cols_out = cols_out; p.clear = clear; p.clear_words = clear_words;
-    p.codes8 = aligned_to(m.codes, 8) && (m.rows <= 1 || (m.ld & 7) == 0);
-    p.vectors = true;
-    const long long across = transposed ? (cols_out + kFlipCols - 1) / kFlipCols : (cols_out + 7) / 8;
+    p.codes8 = aligned_to(m.codes, 8) && (m.rows <= 1 || (m.ld & 7) == 0); p.codes16 = aligned_to(m.codes, 16) && (m.rows <= 1 || (m.ld & 15) == 0);
+    p.vectors = true; p.vectors32 = aligned_to(dst, 32) && (ld_dst & 15) == 0;
+    const long long across = transposed ? (cols_out + kFlipCols - 1) / kFlipCols : (cols_out + 15) / 16;
     const long long down = transposed ? (rows_out + kFlipRows - 1) / kFlipRows : rows_out;
     if (across > 0x7FFFFFFFll / (down > 0 ? down : 1)) return HIF8_ERR_SHAPE;
     p.chunks = FastDiv((uint32_t)across); p.units = (unsigned)(across * down);
@@ -352,7 +434,8 @@ extern "C" int hif8_block_encode(const void* src, int src_dtype, int64_t ld_src,
     p.src = src; p.ld_src = ld_src; p.target_exp = target_exp; p.flags = flags; p.seed = seed;
     p.across = FastDiv((uint32_t)p.m.blocks_across()); p.units = (unsigned)(p.m.blocks_across() * p.m.blocks_down());
     p.vectors = vector_rows(src, rows, ld_src, item);
-    p.codes8 = aligned_to(dst, 8) && (rows <= 1 || (ld_dst & 7) == 0);
+    p.vectors32 = aligned_to(src, 32) && (rows <= 1 || ((size_t)ld_src * item & 31u) == 0);
+    p.codes8 = aligned_to(dst, 8) && (rows <= 1 || (ld_dst & 7) == 0); p.codes16 = aligned_to(dst, 16) && (rows <= 1 || (ld_dst & 15) == 0);
     cudaStream_t st = (cudaStream_t)stream;
     if (src_dtype == HIF8_F32) launch_encode_mode<HIF8_F32>(rnd, p, sms, st);
     else if (src_dtype == HIF8_BF16) launch_encode_mode<HIF8_BF16>(rnd, p, sms, st);
@@ -370,7 +453,7 @@ extern "C" int hif8_block_decode(const uint8_t* src, int64_t ld_src, const int* 
     if (ld_src < cols || ld_dst < cols || exp_stride < p.m.blocks_across()) return HIF8_ERR_SHAPE;
     if (rows == 0 || cols == 0) return HIF8_OK;
     if (!src || !dst || !d_exp) return HIF8_ERR_NULL;
-    const long long across = (cols + 7) / 8;
+    const long long across = (cols + 15) / 16;
     if (across > 0x7FFFFFFFll / rows) return HIF8_ERR_SHAPE;
     const size_t item = dtype_bytes(dst_dtype);
     if (!aligned_to(dst, item) || !aligned_to(d_exp, sizeof(int))) return HIF8_ERR_ALIGN;
@@ -378,8 +461,8 @@ extern "C" int hif8_block_decode(const uint8_t* src, int64_t ld_src, const int* 
     int sms; if (int rc = checked_device(&sms)) return rc;
     p.dst = dst; p.ld_dst = ld_dst; p.rows_out = rows; p.cols_out = cols;
     p.chunks = FastDiv((uint32_t)across); p.units = (unsigned)(across * rows);
-    p.codes8 = aligned_to(src, 8) && (rows <= 1 || (ld_src & 7) == 0);
-    p.vectors = vector_rows(dst, rows, ld_dst, item);
+    p.codes8 = aligned_to(src, 8) && (rows <= 1 || (ld_src & 7) == 0); p.codes16 = aligned_to(src, 16) && (rows <= 1 || (ld_src & 15) == 0);
+    p.vectors = vector_rows(dst, rows, ld_dst, item); p.vectors32 = aligned_to(dst, 32) && (rows <= 1 || ((size_t)ld_dst * item & 31u) == 0);
     cudaStream_t st = (cudaStream_t)stream;
     if (dst_dtype == HIF8_F32) launch_decode<HIF8_F32>(p, sms, st);
     else if (dst_dtype == HIF8_BF16) launch_decode<HIF8_BF16>(p, sms, st);

@@ -30,12 +30,19 @@ __device__ __forceinline__ uint32_t half_warp_max(uint32_t v)
 }
 
 // Eight elements c .. c + 7 of a row of `cols`, zeros behind its end: 16 bytes, of FP32 32.  `vectors`: the row starts on a 16-byte boundary (and c is a multiple of 8).
-// KEEP: they will be read again.
+// KEEP: they will be read again.  WHOLE: the row does so and `cols` is a multiple of 8, so no element is looked at by itself.
 template <int DT> struct Eight { uint4 v[DT == HIF8_F32 ? 2 : 1]; };
-template <int DT, bool KEEP = false>
+template <int DT, bool KEEP = false, bool WHOLE = false>
 __device__ __forceinline__ Eight<DT> load_eight(const void* row, long long c, long long cols, bool vectors)
 {
     Eight<DT> e;
+    if (WHOLE) {
+        const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(row) + (unsigned)c * (DT == HIF8_F32 ? 4u : 2u));
+        const bool in = (int)c < (int)cols;
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(e.v) / 16); i++) e.v[i] = !in ? make_uint4(0, 0, 0, 0) : KEEP ? __ldg(p + i) : __ldcs(p + i);
+        return e;
+    }
     if (KEEP && vectors && c + 8 <= cols) {
         const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(row) + c * (DT == HIF8_F32 ? 4 : 2));
         e.v[0] = __ldg(p);
@@ -103,9 +110,17 @@ __device__ __forceinline__ Eight<DT> pack_eight(const float (&x)[8])
     }
     return e;
 }
-template <int DT>
+template <int DT, bool WHOLE = false>
 __device__ __forceinline__ void store_eight(void* row, long long c, long long cols, bool vectors, const Eight<DT>& e)
 {
+    if (WHOLE) {
+        uint4* p = reinterpret_cast<uint4*>(reinterpret_cast<char*>(row) + (unsigned)c * (DT == HIF8_F32 ? 4u : 2u));
+        if ((int)c < (int)cols) {
+#pragma unroll
+            for (int i = 0; i < (int)(sizeof(e.v) / 16); i++) p[i] = e.v[i];
+        }
+        return;
+    }
     if (DT == HIF8_F32) {
         float* p = reinterpret_cast<float*>(row) + c;
         if (vectors && c + 8 <= cols) {

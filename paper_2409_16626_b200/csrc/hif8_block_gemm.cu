@@ -6,9 +6,8 @@ using namespace hif8;
 
 extern "C" size_t hif8_gemm_block_workspace_bytes(int M, int N, int K, int a_is_km, int w_is_nk, int w_block_rows)
 {
-    (void)a_is_km;
     if (M <= 0 || N <= 0 || K <= 0) return BlockWorkspace::kStatus;
-    return BlockWorkspace(M, N, K, w_is_nk != 0, w_block_rows).bytes();
+    return BlockWorkspace(M, N, K, a_is_km != 0, w_is_nk != 0, w_block_rows).bytes();
 }
 
 extern "C" int hif8_gemm_block(const uint8_t* Aq, int64_t lda, int a_is_km, const int* d_exp_a, int64_t exp_stride_a, int a_block_rows, const uint8_t* Wq, int64_t ldw,
@@ -25,7 +24,7 @@ extern "C" int hif8_gemm_block(const uint8_t* Aq, int64_t lda, int a_is_km, cons
     if (!Aq || !Wq || !C || !d_exp_a || !d_exp_w) return HIF8_ERR_NULL;
     const size_t c_item = c_dtype == HIF8_F32 ? 4 : 2;
     if (!aligned_to(Aq, 16) || !aligned_to(Wq, 16) || ((lda | ldw) & 15) || !aligned_to(C, 16) || ((ldc * c_item) & 15) || !aligned_to(d_exp_a, 4) || !aligned_to(d_exp_w, 4)) return HIF8_ERR_ALIGN;
-    const BlockWorkspace plan(M, N, K, w_is_nk != 0, w_block_rows);
+    const BlockWorkspace plan(M, N, K, a_is_km != 0, w_is_nk != 0, w_block_rows);
     if (!workspace || workspace_bytes < plan.bytes() || !aligned_to(workspace, 256)) return HIF8_ERR_WORKSPACE;
     if (written_over({{C, matrix_bytes(M, N, ldc, c_item)}, {workspace, plan.bytes()}}, {{Aq, a.code_bytes()}, {Wq, w.code_bytes()}, {d_exp_a, a.exp_bytes()}, {d_exp_w, w.exp_bytes()}}))
         return HIF8_ERR_OVERLAP;

@@ -33,17 +33,19 @@ struct BlockWorkspace {
     static constexpr size_t kStatus = 256;
     static constexpr int kNarrowRows = 64;   // up to so many rows the weight-streaming kernel takes the product
     static constexpr int kExpandRows = 512;  // from so many on there is room to expand the weights too
-    long long a_pitch, w_pitch;              // elements between rows of the BF16 copies
+    long long a_pitch, a_pitch_km, w_pitch;  // elements between rows of the BF16 copies (of A as [M,K], as [K,M])
     size_t a_bytes, w_bytes, narrow_bytes;   // w_bytes, narrow_bytes: 0 where there is none
     bool in_kernel;                          // the weights' layout lets the kernels that decode weights take the product
-    BlockWorkspace(int M, int N, int K, bool w_is_nk, int w_block_rows)
+    BlockWorkspace(int M, int N, int K, bool a_is_km, bool w_is_nk, int w_block_rows)
     {
         auto pad8 = [](long long n) { return (n + 7) & ~7ll; };
         auto pad256 = [](size_t n) { return (n + 255) & ~(size_t)255; };
         in_kernel = w_block_rows == HIF8_BLOCK && (K & 15) == 0;
         a_pitch = pad8(K);
+        a_pitch_km = pad8(M);
         w_pitch = pad8(w_is_nk ? K : N);
         a_bytes = pad256((size_t)M * (size_t)a_pitch * 2);
+        if (a_is_km && (size_t)K * (size_t)a_pitch_km * 2 > a_bytes) a_bytes = pad256((size_t)K * (size_t)a_pitch_km * 2);
         const bool narrow = in_kernel && M <= kNarrowRows;
         w_bytes = in_kernel && M < kExpandRows ? 0 : pad256((size_t)(w_is_nk ? N : K) * (size_t)w_pitch * 2);
         // partial sums of 128 columns by the rows: a slice for each block of up to 160 and two more for each slab, which two blocks may share

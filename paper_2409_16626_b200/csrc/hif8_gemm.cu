@@ -1827,7 +1827,8 @@ static_assert(kSmemBytes2 <= 227 * 1024, "shared memory of one CTA");
 
 // RAGGED: rows of C end inside 16 bytes.  A tile store clips at the end of the tensor map's rows in whole 16-byte pieces only, so the map ends in front of the
 // last one and the warp writes what is left itself.
-template <bool W_IS_NK, bool RAGGED>
+// A_IS_KM: A as [K,M], its tiles two boxes of 64 columns like those of W as [K,N].
+template <bool W_IS_NK, bool RAGGED, bool A_IS_KM>
 __global__ void __launch_bounds__(kThreadsP, 1)
 bf16_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_c,
                       const GemmParams p)
@@ -1883,7 +1884,11 @@ bf16_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
         const uint32_t full = map_to_cta(bar_full(s), 0);
         if (loads_a) {
             if (leader) mbar_arrive_expect_tx(bar_full(s), 2 * kStageBytes2);  // bytes of both CTAs, both operands
-            tma_load_3d_pair(dst_a, &map_a, kb * BK, m0, ia, full);
+            if (!A_IS_KM) tma_load_3d_pair(dst_a, &map_a, kb * BK, m0, ia, full);
+            else {
+#pragma unroll
+                for (int c = 0; c < BM / 64; c++) tma_load_3d_pair(dst_a + c * 8192, &map_a, m0 + c * 64, kb * BK, ia, full);
+            }
         } else if (W_IS_NK) tma_load_3d_pair(dst_b, &map_w, kb * BK, n0, iw, full);
         else {
 #pragma unroll
@@ -1915,7 +1920,7 @@ bf16_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
     } else if (warp == kMmaWarp) {
         if (leader) {
             // M = 256 over the pair, N = 256
-            const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((W_IS_NK ? 0u : 1u) << 16) |
+            const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((A_IS_KM ? 1u : 0u) << 15) | ((W_IS_NK ? 0u : 1u) << 16) |
                                    ((uint32_t)(BN >> 3) << 17) | ((uint32_t)((2 * BM) >> 4) << 24);
             int local = 0, s = 0;
             uint32_t ph = 0;
@@ -1931,11 +1936,11 @@ bf16_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                     if (!ok) break;
                     tc_fence_after();
                     const uint32_t a_addr = base + s * kStageBytes2, b_addr = a_addr + kABfBytes;
-                    const uint64_t da = make_smem_desc(a_addr, 16, 1024), db = W_IS_NK ? make_smem_desc(b_addr, 16, 1024) : make_smem_desc(b_addr, 8192, 1024);
+                    const uint64_t da = A_IS_KM ? make_smem_desc(a_addr, 8192, 1024) : make_smem_desc(a_addr, 16, 1024), db = W_IS_NK ? make_smem_desc(b_addr, 16, 1024) : make_smem_desc(b_addr, 8192, 1024);
                     if (elect_one()) {
 #pragma unroll
                         for (int kk = 0; kk < BK / 16; kk++)
-                            tc_mma_bf16_pair(d_tmem, da + (uint64_t)(kk * 2), db + (uint64_t)(kk * (W_IS_NK ? 2 : 128)), idesc, (kb > 0 || kk > 0) ? 1u : 0u);
+                            tc_mma_bf16_pair(d_tmem, da + (uint64_t)(kk * (A_IS_KM ? 128 : 2)), db + (uint64_t)(kk * (W_IS_NK ? 2 : 128)), idesc, (kb > 0 || kk > 0) ? 1u : 0u);
                         tc_commit_pair(bar_empty(s));
                     }
                     progress++;
@@ -2285,6 +2290,12 @@ void weights_kernels(const void** k)
     k[6] = (const void*)hif8_gemm_weights_kernel<false, kActExpanded, FORM, true>; k[7] = (const void*)hif8_gemm_weights_kernel<true, kActExpanded, FORM, true>;
 }
 
+template <bool RAGGED, bool A_IS_KM>
+void pair_kernels(const void** k)
+{
+    k[0] = (const void*)bf16_gemm_pair_kernel<false, RAGGED, A_IS_KM>; k[1] = (const void*)bf16_gemm_pair_kernel<true, RAGGED, A_IS_KM>;
+}
+
 template <int MT>
 void warp_kernels(const void** k)
 {
@@ -2298,11 +2309,11 @@ bool gemm_kernels_ready(int dev, int* sm_count_out, const int** wd_clusters = nu
         out->sm_count = 0;
         std::memset(out->wd_clusters, 0, sizeof out->wd_clusters);
         std::memset(out->nw_clusters, 0, sizeof out->nw_clusters);
-        const void* pair[4] = {(const void*)bf16_gemm_pair_kernel<false, false>, (const void*)bf16_gemm_pair_kernel<true, false>,
-                               (const void*)bf16_gemm_pair_kernel<false, true>, (const void*)bf16_gemm_pair_kernel<true, true>};
+        const void* pair[8];
+        pair_kernels<false, false>(pair); pair_kernels<true, false>(pair + 2); pair_kernels<false, true>(pair + 4); pair_kernels<true, true>(pair + 6);
         const void* wd[32];
         weights_kernels<kOneGroup>(wd); weights_kernels<kGroups>(wd + 8); weights_kernels<kFarRows>(wd + 16); weights_kernels<kParts>(wd + 24);
-        for (int i = 0; i < 4 && out->rc == cudaSuccess; i++)
+        for (int i = 0; i < 8 && out->rc == cudaSuccess; i++)
             out->rc = cudaFuncSetAttribute(pair[i], cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes2);
         for (int i = 0; i < 32 && out->rc == cudaSuccess; i++)
             out->rc = cudaFuncSetAttribute(wd[i], cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytesMax);
@@ -2378,7 +2389,7 @@ void note_status_word(cudaStream_t st, const int* word)
 }
 
 int launch_bf16_pair_gemm(const void* a_bf, const void* w_bf, int w_is_nk, GemmParams p, cudaStream_t st,
-                          long long a_stack_stride, long long w_stack_stride, long long a_pitch, long long w_pitch)
+                          long long a_stack_stride, long long w_stack_stride, long long a_pitch, long long w_pitch, bool a_is_km)
 {
     int dev = 0, sm_count = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || !gemm_kernels_ready(dev, &sm_count)) return HIF8_ERR_CUDA;
@@ -2390,8 +2401,10 @@ int launch_bf16_pair_gemm(const void* a_bf, const void* w_bf, int w_is_nk, GemmP
     if (M <= 0 || N <= 0 || K <= 0 || tiles2 > 0x3FFFFFFF) return HIF8_ERR_SHAPE;
     if (nb > 1 && ((a_stack_stride & 7) || (w_stack_stride & 7))) return HIF8_ERR_ALIGN;  // 16-byte strides
     CUtensorMap ma, mw;
-    // A boxes: this CTA's 128 rows of [M,K]
-    if (!make_map3(&ma, a_bf, (uint64_t)K, (uint64_t)M, nb, (uint64_t)a_stack_stride, BK, BM, (uint64_t)a_pitch)) return HIF8_ERR_CUDA;
+    // A boxes: this CTA's 128 rows of [M,K], or two boxes of 64 columns of [K,M]
+    const bool oka = a_is_km ? make_map3(&ma, a_bf, (uint64_t)M, (uint64_t)K, nb, (uint64_t)a_stack_stride, 64, BK, (uint64_t)a_pitch)
+                             : make_map3(&ma, a_bf, (uint64_t)K, (uint64_t)M, nb, (uint64_t)a_stack_stride, BK, BM, (uint64_t)a_pitch);
+    if (!oka) return HIF8_ERR_CUDA;
     // W boxes are one CTA's half of the 256-column tile: 128 rows of [N,K], or two boxes of 64 columns of [K,N]
     const bool okw = w_is_nk ? make_map3(&mw, w_bf, (uint64_t)K, (uint64_t)N, nb, (uint64_t)w_stack_stride, BK, BN / 2, (uint64_t)w_pitch)
                              : make_map3(&mw, w_bf, (uint64_t)N, (uint64_t)K, nb, (uint64_t)w_stack_stride, 64, BK, (uint64_t)w_pitch);
@@ -2418,10 +2431,10 @@ int launch_bf16_pair_gemm(const void* a_bf, const void* w_bf, int w_is_nk, GemmP
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr; cfg.numAttrs = 2;
-    const cudaError_t lrc = ragged ? (w_is_nk ? cudaLaunchKernelEx(&cfg, bf16_gemm_pair_kernel<true, true>, ma, mw, mc, p)
-                                              : cudaLaunchKernelEx(&cfg, bf16_gemm_pair_kernel<false, true>, ma, mw, mc, p))
-                                   : (w_is_nk ? cudaLaunchKernelEx(&cfg, bf16_gemm_pair_kernel<true, false>, ma, mw, mc, p)
-                                              : cudaLaunchKernelEx(&cfg, bf16_gemm_pair_kernel<false, false>, ma, mw, mc, p));
+    const void* kernel[8];
+    pair_kernels<false, false>(kernel); pair_kernels<true, false>(kernel + 2); pair_kernels<false, true>(kernel + 4); pair_kernels<true, true>(kernel + 6);
+    void* args[] = {&ma, &mw, &mc, &p};
+    const cudaError_t lrc = cudaLaunchKernelExC(&cfg, kernel[(a_is_km ? 4 : 0) + (ragged ? 2 : 0) + (w_is_nk ? 1 : 0)], args);
     g_launches.fetch_add(1, std::memory_order_relaxed);
     return (lrc == cudaSuccess && cudaGetLastError() == cudaSuccess) ? HIF8_OK : HIF8_ERR_CUDA;
 }
@@ -2993,10 +3006,12 @@ int hif8::launch_block_gemm(const BlockCodes& a, bool a_is_km, const BlockCodes&
             return launch_weights_gemm(w.codes, w.ld, w_is_nk, tl, a_bf, K, p, wd_clusters, st);
         }
     }
+    // both operands expanded as they are stored
     unsigned char* w_bf = a_bf + sizes.a_bytes;
-    if (int rc = expand_a(4)) return rc;
+    const long long a_pitch = a_is_km ? sizes.a_pitch_km : sizes.a_pitch;
+    if (int rc = expand_block_codes(a, a_bf, a_pitch, a.rows, a_pitch, false, reinterpret_cast<uint32_t*>(workspace), 1, st)) return rc;
     if (int rc = expand_block_codes(w, w_bf, sizes.w_pitch, w.rows, sizes.w_pitch, false, nullptr, 0, st)) return rc;
-    return launch_bf16_pair_gemm(a_bf, w_bf, w_is_nk, p, st, 0, 0, sizes.a_pitch, sizes.w_pitch);
+    return launch_bf16_pair_gemm(a_bf, w_bf, w_is_nk, p, st, 0, 0, a_pitch, sizes.w_pitch, a_is_km);
 }
 
 extern "C" int hif8_gemm(const uint8_t* Aq, int64_t lda, const uint8_t* Wq, int64_t ldw, int w_is_nk, void* C, int64_t ldc,

@@ -30,12 +30,12 @@ struct GemmParams {
     int c_by_tma;             // pair kernel: results leave through pieces staged in shared memory and tile stores (all but BF16 sums and the squared error)
 };
 
-// C (or the squared error) from operands that are already BF16 in device memory: a_bf [M,K], w_bf [K,N] or (w_is_nk) [N,K],
+// C (or the squared error) from operands that are already BF16 in device memory: a_bf [M,K] or (a_is_km) [K,M], w_bf [K,N] or (w_is_nk) [N,K],
 // both contiguous unless a pitch is given.  Fills in the tile counts of `p`; p.status must point at a zeroed device int.
 // In a batch the variants of an operand are `*_stack_stride` elements apart (multiples of 8).  `*_pitch`: elements between an operand's rows (a multiple
 // of 8; 0: contiguous).
 int launch_bf16_pair_gemm(const void* a_bf, const void* w_bf, int w_is_nk, GemmParams p, cudaStream_t st,
-                          long long a_stack_stride = 0, long long w_stack_stride = 0, long long a_pitch = 0, long long w_pitch = 0);
+                          long long a_stack_stride = 0, long long w_stack_stride = 0, long long a_pitch = 0, long long w_pitch = 0, bool a_is_km = false);
 
 // dst[c][r] = BF16 value of the HiF8 byte src[r][c]; src [rows, cols] contiguous (rows a multiple of 8, cols of 16), both
 // pointers 16-byte aligned.  The launch also clears the device word `clear_word` (may be null).

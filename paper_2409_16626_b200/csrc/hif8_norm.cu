@@ -25,6 +25,7 @@ struct NormParams {
     int lg;                // log2 of the threads of a row
     int target_exp;
     unsigned flags;
+    bool late;             // the next launch may start at the end: its blocks sit unevenly when they come under launches of several rounds
     bool vec_x, vec_res, vec_h, vec_w, codes8;  // rows on boundaries of 16 bytes (codes: 8)
 };
 
@@ -54,39 +55,64 @@ template <int DT> __device__ __forceinline__ const char* row_at(const void* base
     return reinterpret_cast<const char*>(base) + (size_t)row * (size_t)ld * (DT == HIF8_F32 ? 4 : 2);
 }
 
-template <int DT, int MODE, int BLOCK>
-__global__ void __launch_bounds__(BLOCK) norm_encode_kernel(const NormParams p)
+// x + residual, rounded once.  (16-bit types packed: the sum in FP32 rounded to them is the same, since a sum that FP32 rounds has one term far below half a step of the other.)
+template <int DT> __device__ __forceinline__ uint32_t add_word(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    if (DT == HIF8_F32) return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+    if (DT == HIF8_BF16) asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    else asm("add.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+template <int DT> __device__ __forceinline__ Eight<DT> add_eight(const Eight<DT>& a, const Eight<DT>& b)
+{
+    Eight<DT> r;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(r.v) / 16); i++)
+        r.v[i] = make_uint4(add_word<DT>(a.v[i].x, b.v[i].x), add_word<DT>(a.v[i].y, b.v[i].y), add_word<DT>(a.v[i].z, b.v[i].z), add_word<DT>(a.v[i].w, b.v[i].w));
+    return r;
+}
+
+__device__ __forceinline__ uint32_t half_max(uint32_t m)  // of the sixteen threads of a block of 128
+{
+    const unsigned mask = 0xFFFFu << (threadIdx.x & 16u);
+#pragma unroll
+    for (int d = 8; d; d >>= 1) m = max(m, __shfl_xor_sync(mask, m, d));
+    return m;
+}
+
+// Issue slots are what a row costs beside its bytes: columns behind the row's end are zeros already when they are loaded, a block's maximum leaves Inf out only where there is
+// one, and the code table is read with the sign.
+// WHOLE: every row on a 16-byte boundary (codes: 8), columns a multiple of 8.
+constexpr int norm_blocks(int dtype, int block, bool whole) { return dtype == HIF8_F32 || !whole ? (block < 512 ? 512 / block : 1) : 1024 / block; }
+template <int DT, int MODE, int BLOCK, bool WHOLE>
+__global__ void __launch_bounds__(BLOCK, norm_blocks(DT, BLOCK, WHOLE)) norm_encode_kernel(const NormParams p)
 {
     constexpr int NV = kNormEights;
     __shared__ SmemTables sm;
     __shared__ __align__(16) float s_part[2][BLOCK / 32];
     setup_tables<true, MODE != HIF8_RND_TA, false, MODE, HIF8_F32, BLOCK>(sm, p.flags);
     pdl_wait_prior_grid();
-    pdl_launch_dependents();
+    if (!p.late) pdl_launch_dependents();
     const int gs = 1 << p.lg, group = threadIdx.x >> p.lg, t = threadIdx.x & (gs - 1), groups = BLOCK >> p.lg;
     int turn = 0;
     for (long long row = (long long)blockIdx.x * groups + group; row - group < p.rows; row += (long long)gridDim.x * groups, turn ^= 1) {
         const bool live = row < p.rows;  // a group behind the last row only takes part in the exchanges
+        const int end = live ? (int)p.cols : 0;
         Eight<DT> h[NV];
         float sum = 0.f;
-        const long long end = live ? p.cols : 0;
 #pragma unroll
-        for (int j = 0; j < NV; j++) h[j] = load_eight<DT>(row_at<DT>(p.x, row, p.ld_x), (j * gs + t) * 8, end, p.vec_x);
+        for (int j = 0; j < NV; j++) h[j] = load_eight<DT, false, WHOLE>(row_at<DT>(p.x, row, p.ld_x), (j * gs + t) * 8, end, p.vec_x);
         if (p.residual) {
             Eight<DT> r[NV];
 #pragma unroll
-            for (int j = 0; j < NV; j++) r[j] = load_eight<DT>(row_at<DT>(p.residual, row, p.ld_res), (j * gs + t) * 8, end, p.vec_res);
+            for (int j = 0; j < NV; j++) r[j] = load_eight<DT, false, WHOLE>(row_at<DT>(p.residual, row, p.ld_res), (j * gs + t) * 8, end, p.vec_res);
 #pragma unroll
-            for (int j = 0; j < NV; j++) {
-                float s[8];
-#pragma unroll
-                for (int i = 0; i < 8; i++) s[i] = value_of_eight<DT>(h[j], i) + value_of_eight<DT>(r[j], i);
-                h[j] = pack_eight<DT>(s);
-            }
+            for (int j = 0; j < NV; j++) h[j] = add_eight<DT>(h[j], r[j]);
         }
         if (p.h) {
 #pragma unroll
-            for (int j = 0; j < NV; j++) store_eight<DT>(const_cast<char*>(row_at<DT>(p.h, row, p.ld_h)), (j * gs + t) * 8, end, p.vec_h, h[j]);
+            for (int j = 0; j < NV; j++) store_eight<DT, WHOLE>(const_cast<char*>(row_at<DT>(p.h, row, p.ld_h)), (j * gs + t) * 8, end, p.vec_h, h[j]);
         }
 #pragma unroll
         for (int j = 0; j < NV; j++)
@@ -98,38 +124,44 @@ __global__ void __launch_bounds__(BLOCK) norm_encode_kernel(const NormParams p)
         sum = row_sum(sum, s_part[turn], p.lg, group, groups == 1);
         const float rstd = __frsqrt_rn(sum / (float)p.cols + p.eps);
         if (p.rstd && t == 0 && live) p.rstd[row] = rstd;
+        uint8_t* codes = p.m.codes + (size_t)row * (size_t)p.m.ld;
+        int* exps = p.m.exps + (size_t)row * (size_t)p.m.exp_stride;
 #pragma unroll
         for (int j = 0; j < NV; j++) {
-            const long long c = (j * gs + t) * 8;
-            if ((c & ~127ll) >= end) continue;  // (the same for a block's sixteen threads, and so is what follows for half a warp)
-            const Eight<DT> w = load_eight<DT, true>(p.weight, c, p.cols, p.vec_w);
+            const int c = (j * gs + t) * 8;
+            if ((c & ~127) >= end) continue;  // (the same for a block's sixteen threads, and so is what follows for half a warp)
+            const Eight<DT> w = load_eight<DT, true, WHOLE>(p.weight, c, p.cols, p.vec_w);
             float y[8], top = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 y[i] = value_of_eight<DT>(h[j], i) * rstd * value_of_eight<DT>(w, i);
-                if (c + i >= p.cols) y[i] = 0.f;
-                top = amax_step(top, y[i]);
+                top = fmaxf(top, fabsf(y[i]));  // (a NaN is passed over)
             }
-            uint32_t m = __float_as_uint(top);
-            const unsigned mask = 0xFFFFu << (threadIdx.x & 16u);
+            uint32_t m = half_max(__float_as_uint(top));
+            if (m >= 0x7F800000u) {
+                top = 0.f;
 #pragma unroll
-            for (int d = 8; d; d >>= 1) m = max(m, __shfl_xor_sync(mask, m, d));
+                for (int i = 0; i < 8; i++) top = amax_step(top, y[i]);
+                m = half_max(__float_as_uint(top));
+            }
             const int se = block_exp_from_amax(m, p.target_exp);
-            if ((t & 15) == 0) p.m.exps[(size_t)row * (size_t)p.m.exp_stride + (size_t)(c >> 7)] = se;
+            if ((t & 15) == 0) exps[c >> 7] = se;
             const float scale = pow2f(se);
-            uint32_t code[2] = {0u, 0u};
+            uint32_t k[8];
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                uint32_t k;
-                if (MODE == HIF8_RND_TA) {
-                    k = ta_magnitude_code(y[i], scale, sm.ta);
-                    k |= (k + 0x7Fu) & (__float_as_uint(y[i]) >> 24) & 0x80u;
-                } else k = encode_one<MODE, HIF8_F32>(y[i], __float_as_uint(y[i]), scale, sm.ta, sm.thr, 0u) & 0xFFu;
-                code[i >> 2] |= k << (8 * (i & 3));
+                if (MODE == HIF8_RND_TA) k[i] = sm.ta[__float_as_uint(y[i] * scale) >> 19];
+                else k[i] = encode_one<MODE, HIF8_F32>(y[i], __float_as_uint(y[i]), scale, sm.ta, sm.thr, 0u);
             }
-            store_codes8(p.m.codes + (size_t)row * (size_t)p.m.ld, c, p.cols, p.codes8, make_uint2(code[0], code[1]));
+            const uint2 word = make_uint2(__byte_perm(__byte_perm(k[0], k[1], 0x0040), __byte_perm(k[2], k[3], 0x0040), 0x5410),
+                                          __byte_perm(__byte_perm(k[4], k[5], 0x0040), __byte_perm(k[6], k[7], 0x0040), 0x5410));
+            if (WHOLE) {
+                if (c < end) *reinterpret_cast<uint2*>(codes + c) = word;
+            }
+            else store_codes8(codes, c, end, p.codes8, word);
         }
     }
+    if (p.late) pdl_launch_dependents();
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -148,14 +180,20 @@ struct NormBackwardParams {
     bool vec_dy, vec_h, vec_dh, vec_dx, vec_w;
 };
 
-// A thread has the same columns of every row it works on, so it keeps their sums of dy u: in registers, of rows of 1024 threads (which have 64 registers each) in
-// shared memory.
-template <int DT, int BLOCK>
-__global__ void __launch_bounds__(BLOCK) norm_backward_kernel(const NormBackwardParams p)
+// Its values are unpacked again behind this: kept unpacked over a barrier they take registers that the kernels do not have.
+template <int DT> __device__ __forceinline__ void packed_again(Eight<DT>& e)
 {
-    constexpr int NV = kNormEights;
-    constexpr bool kFar = BLOCK == 1024;
-    extern __shared__ __align__(16) float s_acc[];  // BLOCK x 32: kFar: the threads' sums; blocks of 256: to join their groups
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(e.v) / 16); i++) asm volatile("" : "+r"(e.v[i].x), "+r"(e.v[i].y), "+r"(e.v[i].z), "+r"(e.v[i].w));
+}
+
+// A thread has the same columns of every row it works on, so it keeps their sums of dy u: in registers (NV = 2), of rows beyond 16384 columns (NV = 4, 1024 threads with 64
+// registers each) in shared memory.
+template <int DT, int BLOCK, int NV, bool WHOLE>
+__global__ void __launch_bounds__(BLOCK, norm_blocks(DT, BLOCK, WHOLE)) norm_backward_kernel(const NormBackwardParams p)
+{
+    constexpr bool kFar = NV > 2;
+    extern __shared__ __align__(16) float s_acc[];  // BLOCK x 8 NV: kFar: the threads' sums; blocks of 256: to join their groups
     __shared__ __align__(16) float s_part[2][BLOCK / 32];
     pdl_wait_prior_grid();
     pdl_launch_dependents();
@@ -173,17 +211,21 @@ __global__ void __launch_bounds__(BLOCK) norm_backward_kernel(const NormBackward
     int turn = 0;
     for (long long row = (long long)blockIdx.x * groups + group; row - group < p.rows; row += (long long)gridDim.x * groups, turn ^= 1) {
         const bool live = row < p.rows;
-        const long long end = live ? p.cols : 0;
+        const int end = live ? (int)p.cols : 0;
         Eight<DT> dy[NV], h[NV], dh[NV];
 #pragma unroll
-        for (int j = 0; j < NV; j++) dy[j] = load_eight<DT>(row_at<DT>(p.dy, row, p.ld_dy), (j * gs + t) * 8, end, p.vec_dy);
+        for (int j = 0; j < NV; j++) dy[j] = load_eight<DT, false, WHOLE>(row_at<DT>(p.dy, row, p.ld_dy), (j * gs + t) * 8, end, p.vec_dy);
 #pragma unroll
-        for (int j = 0; j < NV; j++) h[j] = load_eight<DT>(row_at<DT>(p.h, row, p.ld_h), (j * gs + t) * 8, end, p.vec_h);
+        for (int j = 0; j < NV; j++) h[j] = load_eight<DT, false, WHOLE>(row_at<DT>(p.h, row, p.ld_h), (j * gs + t) * 8, end, p.vec_h);
         const float rstd = live ? __ldg(p.rstd + row) : 0.f;
+        if (p.dh) {
+#pragma unroll
+            for (int j = 0; j < NV; j++) dh[j] = load_eight<DT, false, WHOLE>(row_at<DT>(p.dh, row, p.ld_dh), (j * gs + t) * 8, end, p.vec_dh);
+        }
         float sum = 0.f;
 #pragma unroll
         for (int j = 0; j < NV; j++) {
-            const Eight<DT> w = load_eight<DT, true>(p.weight, (j * gs + t) * 8, p.cols, p.vec_w);
+            const Eight<DT> w = load_eight<DT, true, WHOLE>(p.weight, (j * gs + t) * 8, p.cols, p.vec_w);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 const float d = value_of_eight<DT>(dy[j], i), u = value_of_eight<DT>(h[j], i) * rstd;
@@ -192,14 +234,14 @@ __global__ void __launch_bounds__(BLOCK) norm_backward_kernel(const NormBackward
                 else s_acc[(j * 8 + i) * BLOCK + threadIdx.x] = fmaf(d, u, s_acc[(j * 8 + i) * BLOCK + threadIdx.x]);
             }
         }
-        if (p.dh) {
-#pragma unroll
-            for (int j = 0; j < NV; j++) dh[j] = load_eight<DT>(row_at<DT>(p.dh, row, p.ld_dh), (j * gs + t) * 8, end, p.vec_dh);
-        }
         const float mean = row_sum(sum, s_part[turn], p.lg, group, groups == 1) * inv;
+        const void* weight = p.weight;
+        asm volatile("" : "+l"(weight));
 #pragma unroll
         for (int j = 0; j < NV; j++) {
-            const Eight<DT> w = load_eight<DT, true>(p.weight, (j * gs + t) * 8, p.cols, p.vec_w);
+            packed_again<DT>(dy[j]);
+            packed_again<DT>(h[j]);
+            const Eight<DT> w = load_eight<DT, true, WHOLE>(weight, (j * gs + t) * 8, p.cols, p.vec_w);
             float g[8];
 #pragma unroll
             for (int i = 0; i < 8; i++) {
@@ -207,14 +249,14 @@ __global__ void __launch_bounds__(BLOCK) norm_backward_kernel(const NormBackward
                 g[i] = rstd * fmaf(-u, mean, wdy);
                 if (p.dh) g[i] += value_of_eight<DT>(dh[j], i);
             }
-            store_eight<DT>(const_cast<char*>(row_at<DT>(p.dx, row, p.ld_dx)), (j * gs + t) * 8, end, p.vec_dx, pack_eight<DT>(g));
+            store_eight<DT, WHOLE>(const_cast<char*>(row_at<DT>(p.dx, row, p.ld_dx)), (j * gs + t) * 8, end, p.vec_dx, pack_eight<DT>(g));
         }
     }
     if (!p.part) return;
     float* out = p.part + (size_t)blockIdx.x * (size_t)p.cols;
     if (kFar) {
         for (int k = 0; k < NV * 8; k++) {
-            const long long c = ((k >> 3) * gs + t) * 8 + (k & 7);
+            const int c = ((k >> 3) * gs + t) * 8 + (k & 7);
             if (c < p.cols) out[c] = s_acc[k * BLOCK + threadIdx.x];
         }
         return;
@@ -224,7 +266,7 @@ __global__ void __launch_bounds__(BLOCK) norm_backward_kernel(const NormBackward
         for (int j = 0; j < (kFar ? 1 : NV); j++)
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                const long long c = (j * gs + t) * 8 + i;
+                const int c = (j * gs + t) * 8 + i;
                 if (c < p.cols) out[c] = acc[j][i];
             }
         return;
@@ -244,13 +286,14 @@ __global__ void __launch_bounds__(BLOCK) norm_backward_kernel(const NormBackward
     }
 }
 
-// dweight_j (+)= the blocks' shares, in their order: 32 columns by eight slices of the blocks
-__global__ void __launch_bounds__(kThreads) norm_weight_grad_kernel(const float* __restrict__ part, int blocks, long long cols, float* dweight, int accumulate)
+// dweight_j (+)= the blocks' shares, in their order: 32 columns by 32 slices of the blocks
+constexpr int kShareThreads = 1024;
+__global__ void __launch_bounds__(kShareThreads) norm_weight_grad_kernel(const float* __restrict__ part, int blocks, long long cols, float* dweight, int accumulate)
 {
-    __shared__ float s_sum[kThreads / 32][32];
+    __shared__ float s_sum[32][33];
     pdl_wait_prior_grid();
     pdl_launch_dependents();
-    const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, per = (blocks + kThreads / 32 - 1) / (kThreads / 32);
+    const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, per = (blocks + 31) / 32;
     const long long c = (long long)blockIdx.x * 32 + lane;
     float v = 0.f;
     if (c < cols) {
@@ -260,12 +303,11 @@ __global__ void __launch_bounds__(kThreads) norm_weight_grad_kernel(const float*
     }
     s_sum[slice][lane] = v;
     __syncthreads();
-    if (slice == 0 && c < cols) {
-        v = 0.f;
+    v = s_sum[lane][slice];  // a warp adds a column's 32 sums
 #pragma unroll
-        for (int s = 0; s < kThreads / 32; s++) v += s_sum[s][lane];
-        dweight[c] = accumulate ? dweight[c] + v : v;
-    }
+    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+    const long long own = (long long)blockIdx.x * 32 + slice;
+    if (lane == 0 && own < cols) dweight[own] = accumulate ? dweight[own] + v : v;
 }
 
 int finish(int launches)
@@ -283,24 +325,39 @@ int row_threads_log2(long long rows, long long cols, int few)
     return lg;
 }
 
-// blocks of the gradient's kernel: as many as are resident, which the shares of the weight's gradient in the workspace go by
+// The gradient's kernel: sixteen elements a thread, 32 where 1024 threads are too few; as many blocks as are resident, which the shares of the weight's gradient in the
+// workspace go by.
+int backward_threads_log2(long long cols)
+{
+    int lg = 5;
+    while (lg < 10 && (16ll << lg) < cols) lg++;
+    return lg;
+}
 long long backward_blocks(long long rows, int lg)
 {
     const int groups = lg < 8 ? 1 << (8 - lg) : 1;
-    const long long need = (rows + groups - 1) / groups, most = lg <= 8 ? 2 * 148 : 148;
+    const long long need = (rows + groups - 1) / groups, most = 148 * (lg <= 8 ? 4 : lg == 9 ? 2 : 1);
     return need < most ? need : most;
 }
 constexpr int kFewRows = 148;
 
+template <int DT, int MODE, bool WHOLE>
+void launch_norm(NormParams p, int sms, cudaStream_t st)
+{
+    const int groups = p.lg < 8 ? 1 << (8 - p.lg) : 1;
+    const long long need = (p.rows + groups - 1) / groups, most = (long long)sms * norm_blocks(DT, p.lg <= 8 ? 256 : p.lg == 9 ? 512 : 1024, WHOLE);
+    const dim3 grid((unsigned)(need < most ? need : most));
+    p.late = need > most;
+    if (p.lg <= 8) launch_pdl_threads(256, norm_encode_kernel<DT, MODE, 256, WHOLE>, grid, st, p);
+    else if (p.lg == 9) launch_pdl_threads(512, norm_encode_kernel<DT, MODE, 512, WHOLE>, grid, st, p);
+    else launch_pdl_threads(1024, norm_encode_kernel<DT, MODE, 1024, WHOLE>, grid, st, p);
+}
 template <int DT, int MODE>
 void launch_norm(const NormParams& p, int sms, cudaStream_t st)
 {
-    const int groups = p.lg < 8 ? 1 << (8 - p.lg) : 1;
-    const long long need = (p.rows + groups - 1) / groups, most = (long long)sms * (p.lg <= 8 ? 4 : p.lg == 9 ? 2 : 1);
-    const dim3 grid((unsigned)(need < most ? need : most));
-    if (p.lg <= 8) launch_pdl_threads(256, norm_encode_kernel<DT, MODE, 256>, grid, st, p);
-    else if (p.lg == 9) launch_pdl_threads(512, norm_encode_kernel<DT, MODE, 512>, grid, st, p);
-    else launch_pdl_threads(1024, norm_encode_kernel<DT, MODE, 1024>, grid, st, p);
+    const bool whole = (p.cols & 7) == 0 && p.vec_x && p.vec_w && p.codes8 && (!p.residual || p.vec_res) && (!p.h || p.vec_h);
+    if (whole) launch_norm<DT, MODE, true>(p, sms, st);
+    else launch_norm<DT, MODE, false>(p, sms, st);
 }
 template <int DT>
 void launch_norm_mode(int rnd, const NormParams& p, int sms, cudaStream_t st)
@@ -313,16 +370,16 @@ void launch_norm_mode(int rnd, const NormParams& p, int sms, cudaStream_t st)
     }
 }
 
-template <int DT, int BLOCK>
+template <int DT, int BLOCK, int NV, bool WHOLE>
 bool launch_backward_block(const NormBackwardParams& p, long long blocks, cudaStream_t st)
 {
-    const size_t bytes = BLOCK == 512 ? 0 : (size_t)BLOCK * kNormEights * 8 * sizeof(float);
+    const size_t bytes = BLOCK == 256 || NV > 2 ? (size_t)BLOCK * NV * 8 * sizeof(float) : 0;
     if (bytes > 48 * 1024) {  // a fact of the device, set by its first such call
         static PerDevice<cudaError_t> ready;
         int dev = 0;
         if (cudaGetDevice(&dev) != cudaSuccess) return false;
         const cudaError_t* rc = ready.get(dev, [&](int, cudaError_t* out) {
-            *out = cudaFuncSetAttribute(norm_backward_kernel<DT, BLOCK>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+            *out = cudaFuncSetAttribute(norm_backward_kernel<DT, BLOCK, NV, WHOLE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
         });
         if (!rc || *rc != cudaSuccess) return false;
     }
@@ -335,14 +392,20 @@ bool launch_backward_block(const NormBackwardParams& p, long long blocks, cudaSt
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr; cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, norm_backward_kernel<DT, BLOCK>, p) == cudaSuccess;
+    return cudaLaunchKernelEx(&cfg, norm_backward_kernel<DT, BLOCK, NV, WHOLE>, p) == cudaSuccess;
+}
+template <int DT, bool WHOLE>
+bool launch_backward(const NormBackwardParams& p, long long blocks, cudaStream_t st)
+{
+    if (p.lg <= 8) return launch_backward_block<DT, 256, 2, WHOLE>(p, blocks, st);
+    if (p.lg == 9) return launch_backward_block<DT, 512, 2, WHOLE>(p, blocks, st);
+    return p.cols <= 16384 ? launch_backward_block<DT, 1024, 2, WHOLE>(p, blocks, st) : launch_backward_block<DT, 1024, 4, WHOLE>(p, blocks, st);
 }
 template <int DT>
 bool launch_backward(const NormBackwardParams& p, long long blocks, cudaStream_t st)
 {
-    if (p.lg <= 8) return launch_backward_block<DT, 256>(p, blocks, st);
-    if (p.lg == 9) return launch_backward_block<DT, 512>(p, blocks, st);
-    return launch_backward_block<DT, 1024>(p, blocks, st);
+    const bool whole = (p.cols & 7) == 0 && p.vec_dy && p.vec_h && p.vec_dx && p.vec_w && (!p.dh || p.vec_dh);
+    return whole ? launch_backward<DT, true>(p, blocks, st) : launch_backward<DT, false>(p, blocks, st);
 }
 
 // the same rows (a result in the place of an operand), or no byte in common
@@ -394,7 +457,7 @@ extern "C" int hif8_rmsnorm_encode(const void* x, int64_t ld_x, const void* resi
 extern "C" size_t hif8_rmsnorm_backward_workspace_bytes(int64_t rows, int64_t cols)
 {
     if (rows <= 0 || cols <= 0 || cols > HIF8_NORM_MAX_COLS) return 0;
-    return ((size_t)backward_blocks(rows, row_threads_log2(rows, cols, 0)) * (size_t)cols * sizeof(float) + 255) & ~(size_t)255;
+    return ((size_t)backward_blocks(rows, backward_threads_log2(cols)) * (size_t)cols * sizeof(float) + 255) & ~(size_t)255;
 }
 
 extern "C" int hif8_rmsnorm_backward(const void* dy, int64_t ld_dy, const void* h, int64_t ld_h, const void* dh, int64_t ld_dh, int dtype, const void* weight, const float* d_rstd,
@@ -415,7 +478,7 @@ extern "C" int hif8_rmsnorm_backward(const void* dy, int64_t ld_dy, const void* 
     const size_t item = dtype_bytes(dtype);
     if (!aligned_to(dy, item) || !aligned_to(h, item) || !aligned_to(dh, item) || !aligned_to(weight, item) || !aligned_to(dx, item) || !aligned_to(d_rstd, 4)) return HIF8_ERR_ALIGN;
     NormBackwardParams p{};
-    p.lg = row_threads_log2(rows, cols, 0);
+    p.lg = backward_threads_log2(cols);
     const long long blocks = backward_blocks(rows, p.lg);
     const size_t need = d_weight_grad ? hif8_rmsnorm_backward_workspace_bytes(rows, cols) : 0;
     if (need && (!workspace || workspace_bytes < need || !aligned_to(workspace, 256))) return HIF8_ERR_WORKSPACE;
@@ -434,6 +497,6 @@ extern "C" int hif8_rmsnorm_backward(const void* dy, int64_t ld_dy, const void* 
     const bool ok = dtype == HIF8_F32 ? launch_backward<HIF8_F32>(p, blocks, st) : dtype == HIF8_BF16 ? launch_backward<HIF8_BF16>(p, blocks, st) : launch_backward<HIF8_F16>(p, blocks, st);
     if (!ok) return HIF8_ERR_CUDA;
     if (p.part)
-        launch_pdl(norm_weight_grad_kernel, dim3((unsigned)((cols + 31) / 32)), st, reinterpret_cast<const float*>(workspace), (int)blocks, (long long)cols, d_weight_grad, accumulate);
+        launch_pdl_threads(kShareThreads, norm_weight_grad_kernel, dim3((unsigned)((cols + 31) / 32)), st, reinterpret_cast<const float*>(workspace), (int)blocks, (long long)cols, d_weight_grad, accumulate);
     return finish(p.part ? 2 : 1);
 }
