@@ -2300,6 +2300,7 @@ template <int MT>
 void warp_kernels(const void** k)
 {
     k[0] = (const void*)hif8_gemm_warp_kernel<false, false, MT>; k[1] = (const void*)hif8_gemm_warp_kernel<true, false, MT>;
+    k[2] = (const void*)hif8_gemm_warp_kernel<false, false, MT, true>; k[3] = (const void*)hif8_gemm_warp_kernel<true, false, MT, true>;
 }
 
 bool gemm_kernels_ready(int dev, int* sm_count_out, const int** wd_clusters = nullptr, const int** nw_clusters = nullptr, const int** wp_clusters = nullptr)
@@ -2340,10 +2341,10 @@ bool gemm_kernels_ready(int dev, int* sm_count_out, const int** wd_clusters = nu
             out->rc = cudaOccupancyMaxActiveClusters(&out->nw_clusters[s], narrow[7], &cfg);  // (all of them take the same)
         }
         std::memset(out->wp_clusters, 0, sizeof out->wp_clusters);
-        const void* wp[8];
-        warp_kernels<1>(wp); warp_kernels<2>(wp + 2); warp_kernels<4>(wp + 4);
-        wp[6] = (const void*)hif8_gemm_warp_kernel<false, true, 4>; wp[7] = (const void*)hif8_gemm_warp_kernel<true, true, 4>;
-        for (int i = 0; i < 8 && out->rc == cudaSuccess; i++)
+        const void* wp[14];
+        warp_kernels<1>(wp); warp_kernels<2>(wp + 4); warp_kernels<4>(wp + 8);
+        wp[12] = (const void*)hif8_gemm_warp_kernel<false, true, 4>; wp[13] = (const void*)hif8_gemm_warp_kernel<true, true, 4>;
+        for (int i = 0; i < 14 && out->rc == cudaSuccess; i++)
             out->rc = cudaFuncSetAttribute(wp[i], cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytesMax);
         for (int s = 1; s <= kWarpMaxCluster && out->rc == cudaSuccess; s++) {
             cudaLaunchConfig_t cfg{};
@@ -2352,7 +2353,7 @@ bool gemm_kernels_ready(int dev, int* sm_count_out, const int** wd_clusters = nu
             attr[0].val.clusterDim.x = s; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
             cfg.gridDim = dim3(s); cfg.blockDim = dim3(kWarpThreads); cfg.dynamicSmemBytes = kSmemBytesMax;
             cfg.attrs = attr; cfg.numAttrs = 1;
-            out->rc = cudaOccupancyMaxActiveClusters(&out->wp_clusters[s], wp[7], &cfg);
+            out->rc = cudaOccupancyMaxActiveClusters(&out->wp_clusters[s], wp[13], &cfg);
         }
         if (out->rc == cudaSuccess) out->rc = cudaDeviceGetAttribute(&out->sm_count, cudaDevAttrMultiProcessorCount, d);
     });
@@ -2706,6 +2707,9 @@ template <int MT>
 static cudaError_t launch_warp_kernel(const cudaLaunchConfig_t& cfg, bool w_is_nk, const uint8_t* A, long long lda, const uint8_t* W, long long ldw,
                                       const GemmParams& p, const WarpPlan& plan)
 {
+    if (p.w_exp)
+        return w_is_nk ? cudaLaunchKernelEx(&cfg, hif8_gemm_warp_kernel<true, false, MT, true>, A, lda, W, ldw, p, plan)
+                       : cudaLaunchKernelEx(&cfg, hif8_gemm_warp_kernel<false, false, MT, true>, A, lda, W, ldw, p, plan);
     return w_is_nk ? cudaLaunchKernelEx(&cfg, hif8_gemm_warp_kernel<true, false, MT>, A, lda, W, ldw, p, plan)
                    : cudaLaunchKernelEx(&cfg, hif8_gemm_warp_kernel<false, false, MT>, A, lda, W, ldw, p, plan);
 }
@@ -2950,61 +2954,101 @@ static int gemm_entry(const uint8_t* Aq, int64_t lda, int a_is_km, const uint8_t
     return rc != HIF8_OK ? rc : launch_bf16_pair_gemm(a_bf, w_bf, w_is_nk, p, st);
 }
 
-// Block-scaled operands.  The activations are expanded to BF16 with their scales in front, whatever the kernel.  Weights with a scale for each 128 x 128 and K a
-// multiple of 16 are decoded in the kernel: up to 64 rows by the narrow one, beyond by the weights one, until expanding them pays (as for
-// hif8_gemm, with more to win back: 3 bytes an element).  Other weights (activations of a gradient's product, with a scale for each 1 x 128) are expanded too.
+// Which kernel takes a block-scaled product whose weights have a scale for each 128 x 128 (K a multiple of 16): as for hif8_gemm, by the same costs.  room: the workspace has
+// room to expand the weights.
+struct BlockKey {
+    int M, N, K, dev, a_is_km, w_is_nk, policy, pad;
+};
+struct BlockChoice {
+    GemmForm form;
+    WarpTiling warp;
+    WeightsTiling weights;
+};
+static LruCache<BlockKey, BlockChoice, 64> g_block_choices;
+
+static void choose_block(const BlockKey& k, int sm_count, const int* wd_clusters, const int* nw_clusters, const int* wp_clusters, bool room, BlockChoice* out)
+{
+    const bool narrow = k.M <= BlockWorkspace::kNarrowRows;
+    out->form = narrow ? kFormNarrow : kFormWeights;
+    double other;
+    if (!narrow) {
+        out->weights = WeightsTiling(k.M, k.N, k.K, kActExpanded, k.a_is_km, wd_clusters);
+        const long long pair_rounds = ((long long)((k.M + 2 * BM - 1) / (2 * BM)) * ((k.N + BN - 1) / BN) + sm_count / 2 - 1) / (sm_count / 2);
+        const double expand_w = 6000.0 + 3.0 * (double)k.K * k.N / 3300.0, pair_cycles = (double)pair_rounds * ((k.K + BK - 1) / BK * 545.0 + 500.0);
+        if (room && k.policy != HIF8_GEMM_PATH_EXPAND_A && (k.policy == HIF8_GEMM_PATH_EXPAND_BOTH || expand_w + pair_cycles < 1.03 * out->weights.cost.all(out->weights.tiles))) {
+            out->form = kFormPair;
+            return;
+        }
+        other = out->weights.cycles;
+    } else other = NarrowTiling(k.M, k.N, k.K, sm_count, nw_clusters, true).cycles + 6000.0;
+    if (k.a_is_km || (k.policy != HIF8_GEMM_PATH_AUTO && k.policy != HIF8_GEMM_PATH_WARP)) return;
+    out->warp = WarpTiling(k.M, k.N, k.K, k.w_is_nk, false, wp_clusters, k.policy == HIF8_GEMM_PATH_WARP ? 1e30 : other / 1.2);
+    if (out->warp.mt > 0) out->form = kFormWarp;
+}
+
+// Block-scaled operands.  Where the weights have a scale for each 128 x 128 and K is a multiple of 16 they are decoded in the kernel: few rows and a small weight by the warp
+// kernel, which takes the activations' codes too; the others have the activations expanded to BF16 with their scales in front, up to 64 rows for the narrow kernel, beyond
+// for the weights kernel, until expanding the weights pays.  Other weights (a gradient's activations, with a scale for each 1 x 128) are expanded whatever the size.
 int hif8::launch_block_gemm(const BlockCodes& a, bool a_is_km, const BlockCodes& w, bool w_is_nk, const GemmParams& params, const BlockWorkspace& sizes, void* workspace, cudaStream_t st)
 {
     GemmParams p = params;
     const int M = p.M, N = p.N, K = p.K;
     int dev = 0, sm_count = 0;
-    const int *wd_clusters = nullptr, *nw_clusters = nullptr;
-    if (cudaGetDevice(&dev) != cudaSuccess || !gemm_kernels_ready(dev, &sm_count, &wd_clusters, &nw_clusters)) return HIF8_ERR_CUDA;
+    const int *wd_clusters = nullptr, *nw_clusters = nullptr, *wp_clusters = nullptr;
+    if (cudaGetDevice(&dev) != cudaSuccess || !gemm_kernels_ready(dev, &sm_count, &wd_clusters, &nw_clusters, &wp_clusters)) return HIF8_ERR_CUDA;
     unsigned char* wsb = reinterpret_cast<unsigned char*>(workspace) + BlockWorkspace::kStatus;
     unsigned char* a_bf = wsb;
     const long long a_rows = a_is_km ? sizes.a_pitch : M, a_cols = a_is_km ? M : sizes.a_pitch;
     auto expand_a = [&](size_t clear_bytes) {
         return expand_block_codes(a, a_bf, sizes.a_pitch, a_rows, a_cols, a_is_km, reinterpret_cast<uint32_t*>(workspace), (unsigned)(clear_bytes / 4), st);
     };
-    if (sizes.in_kernel && M <= BlockWorkspace::kNarrowRows) {
-        p.w_exp = w.exps; p.w_exp_stride = w.exp_stride;
-        const int mp = (M + 15) & ~15;
-        const long long slabs = (N + BM - 1) / BM, num_pb = (K + BK2 - 1) / BK2, total = slabs * num_pb;
-        if (total > 0x3FFFFFFF) return HIF8_ERR_SHAPE;
-        const NarrowTiling nt(M, N, K, sm_count, nw_clusters, true);
-        NarrowPlan plan{};
-        plan.split = nt.split;
-        long long grid = slabs * plan.split;
-        size_t clear_bytes = 4;
-        const size_t ticket_bytes = (((size_t)slabs * kEpiWarps * 4) + 255) & ~(size_t)255, part_bytes = (size_t)slabs * nt.pmax * mp * BM * 4;
-        a_bf = wsb + sizes.narrow_bytes;
-        if (nt.ranges && ticket_bytes + part_bytes <= sizes.narrow_bytes) {
-            plan.tickets = reinterpret_cast<unsigned*>(wsb);
-            plan.part = reinterpret_cast<float*>(wsb + ticket_bytes);
-            plan.pmax = (int)nt.pmax;
-            plan.split = 0;
-            grid = nt.grid;
-            clear_bytes = BlockWorkspace::kStatus + ticket_bytes;  // the tickets follow the status word
-        }
-        if (grid > 0x7FFFFFFFll) return HIF8_ERR_SHAPE;
-        plan.q = (int)(total / grid); plan.rem = (int)(total % grid);
-        CUtensorMap map_act, map_ws;
-        if (!make_map(&map_act, a_bf, (uint64_t)K, (uint64_t)M, (uint64_t)sizes.a_pitch, BK, (uint32_t)mp, true)) return HIF8_ERR_CUDA;
-        const bool okn = w_is_nk ? make_map(&map_ws, w.codes, (uint64_t)K, (uint64_t)N, (uint64_t)w.ld, BK2, BM, false, 128)
-                                 : make_map(&map_ws, w.codes, (uint64_t)N, (uint64_t)K, (uint64_t)w.ld, BM, BK2, false, 128, true);
-        if (!okn) return HIF8_ERR_CUDA;
-        if (int rc = expand_a(clear_bytes)) return rc;
-        return launch_narrow(plan, grid, true, map_act, map_ws, p, mp, w_is_nk, st);
-    }
     if (sizes.in_kernel) {
-        const WeightsTiling tl(M, N, K, kActExpanded, a_is_km, wd_clusters);
-        const long long pair_rounds = ((long long)((M + 2 * BM - 1) / (2 * BM)) * ((N + BN - 1) / BN) + sm_count / 2 - 1) / (sm_count / 2);
-        const double expand_w = 6000.0 + 3.0 * (double)K * N / 3300.0, pair_cycles = (double)pair_rounds * ((K + BK - 1) / BK * 545.0 + 500.0);
-        if (sizes.w_bytes == 0 || expand_w + pair_cycles >= 1.03 * tl.cost.all(tl.tiles)) {
-            p.w_exp = w.exps; p.w_exp_stride = w.exp_stride;
-            if (int rc = expand_a(4)) return rc;
-            return launch_weights_gemm(w.codes, w.ld, w_is_nk, tl, a_bf, K, p, wd_clusters, st);
+        p.w_exp = w.exps; p.w_exp_stride = w.exp_stride;
+        p.a_exp = a.exps; p.a_exp_stride = a.exp_stride; p.a_exp_shift = a.shift;
+        BlockKey key;
+        std::memset(&key, 0, sizeof key);
+        key.M = M; key.N = N; key.K = K; key.dev = dev; key.a_is_km = a_is_km; key.w_is_nk = w_is_nk;
+        key.policy = g_path_policy.load(std::memory_order_relaxed);
+        BlockChoice choice;
+        if (!g_block_choices.find(key, &choice)) {
+            choose_block(key, sm_count, wd_clusters, nw_clusters, wp_clusters, sizes.w_bytes != 0, &choice);
+            g_block_choices.put(key, choice);
         }
+        if (choice.form == kFormWarp) return launch_warp_gemm(a.codes, a.ld, 0, w.codes, w.ld, w_is_nk, p, choice.warp, st);
+        if (choice.form == kFormNarrow) {
+            const int mp = (M + 15) & ~15;
+            const long long slabs = (N + BM - 1) / BM, num_pb = (K + BK2 - 1) / BK2, total = slabs * num_pb;
+            if (total > 0x3FFFFFFF) return HIF8_ERR_SHAPE;
+            const NarrowTiling nt(M, N, K, sm_count, nw_clusters, true);
+            NarrowPlan plan{};
+            plan.split = nt.split;
+            long long grid = slabs * plan.split;
+            size_t clear_bytes = 4;
+            const size_t ticket_bytes = (((size_t)slabs * kEpiWarps * 4) + 255) & ~(size_t)255, part_bytes = (size_t)slabs * nt.pmax * mp * BM * 4;
+            a_bf = wsb + sizes.narrow_bytes;
+            if (nt.ranges && ticket_bytes + part_bytes <= sizes.narrow_bytes) {
+                plan.tickets = reinterpret_cast<unsigned*>(wsb);
+                plan.part = reinterpret_cast<float*>(wsb + ticket_bytes);
+                plan.pmax = (int)nt.pmax;
+                plan.split = 0;
+                grid = nt.grid;
+                clear_bytes = BlockWorkspace::kStatus + ticket_bytes;  // the tickets follow the status word
+            }
+            if (grid > 0x7FFFFFFFll) return HIF8_ERR_SHAPE;
+            plan.q = (int)(total / grid); plan.rem = (int)(total % grid);
+            CUtensorMap map_act, map_ws;
+            if (!make_map(&map_act, a_bf, (uint64_t)K, (uint64_t)M, (uint64_t)sizes.a_pitch, BK, (uint32_t)mp, true)) return HIF8_ERR_CUDA;
+            const bool okn = w_is_nk ? make_map(&map_ws, w.codes, (uint64_t)K, (uint64_t)N, (uint64_t)w.ld, BK2, BM, false, 128)
+                                     : make_map(&map_ws, w.codes, (uint64_t)N, (uint64_t)K, (uint64_t)w.ld, BM, BK2, false, 128, true);
+            if (!okn) return HIF8_ERR_CUDA;
+            if (int rc = expand_a(clear_bytes)) return rc;
+            return launch_narrow(plan, grid, true, map_act, map_ws, p, mp, w_is_nk, st);
+        }
+        if (choice.form == kFormWeights) {
+            if (int rc = expand_a(4)) return rc;
+            return launch_weights_gemm(w.codes, w.ld, w_is_nk, choice.weights, a_bf, K, p, wd_clusters, st);
+        }
+        p.w_exp = nullptr;
     }
     // both operands expanded as they are stored
     unsigned char* w_bf = a_bf + sizes.a_bytes;

@@ -103,7 +103,9 @@ __device__ __forceinline__ float lds_volatile_f32(uint32_t addr)
     return v;
 }
 
-template <bool W_IS_NK, bool A_IS_KM, int MT>
+// SCALED: block-scaled operands, A as [M,K] with any blocks, the weights' of 128 x 128: a unit's columns and 64 k lie in one block, whose scale is multiplied
+// onto the decoded words.
+template <bool W_IS_NK, bool A_IS_KM, int MT, bool SCALED = false>
 __global__ void __launch_bounds__(kWarpThreads, 1)
 hif8_gemm_warp_kernel(const uint8_t* __restrict__ A, long long lda, const uint8_t* __restrict__ W, long long ldw, const GemmParams p, const WarpPlan plan)
 {
@@ -182,6 +184,24 @@ hif8_gemm_warp_kernel(const uint8_t* __restrict__ A, long long lda, const uint8_
         for (int s = 0; s < 4; s++)
 #pragma unroll
             for (int i = 0; i < MT; i++) b[j][s][i][0] = 0u;  // the codes, until they are decoded
+    int e_act[SCALED ? CH : 1][SCALED ? MT : 1];  // exponents of the activations' blocks
+    if (SCALED) {
+#pragma unroll
+        for (int j = 0; j < (SCALED ? CH : 1); j++)
+#pragma unroll
+            for (int i = 0; i < (SCALED ? MT : 1); i++) e_act[j][i] = 0;
+    }
+    // exponent of the weights' block of column n and the slice's j-th 64 k
+    auto weight_exp = [&](int n, int j) {
+        if (n >= p.N || j >= plan.chunks || 64 * j >= k_len) return 0;
+        const long long kb = (k0 + 64 * j) >> 7, nb = n >> 7;
+        return __ldg(p.w_exp + (W_IS_NK ? nb * p.w_exp_stride + kb : kb * p.w_exp_stride + nb));
+    };
+    int e_w[SCALED ? CH : 1];  // of the unit to work on next
+    if (SCALED) {
+#pragma unroll
+        for (int j = 0; j < (SCALED ? CH : 1); j++) e_w[j] = n_it > 0 ? weight_exp(n_next, j) : 0;
+    }
     if (n_it > 0) {
 #pragma unroll
         for (int j = 0; j < CH; j++) {
@@ -192,6 +212,7 @@ hif8_gemm_warp_kernel(const uint8_t* __restrict__ A, long long lda, const uint8_
                     const int m = m0 + 8 * i + g;
                     const uint8_t* src = A + (long long)m * lda + k0 + 64 * j;
                     if (m >= p.M) continue;
+                    if (SCALED && 64 * j < k_len) e_act[j][i] = __ldg(p.a_exp + (long long)(m >> p.a_exp_shift) * p.a_exp_stride + ((k0 + 64 * j) >> 7));
                     if ((k_blocks >> j) & 1) {
                         const uint4 x = __ldg(reinterpret_cast<const uint4*>(src + 16 * t));
                         b[j][0][i][0] = x.x; b[j][1][i][0] = x.y; b[j][2][i][0] = x.z; b[j][3][i][0] = x.w;
@@ -234,7 +255,14 @@ hif8_gemm_warp_kernel(const uint8_t* __restrict__ A, long long lda, const uint8_
                         for (int i = 0; i < 4; i++) w[i] = o[i];
                     }
 #pragma unroll
-                    for (int i = 0; i < MT; i++) decode4(w[i], lut, b[j][s][i][0], b[j][s][i][1]);
+                    for (int i = 0; i < MT; i++) {
+                        decode4(w[i], lut, b[j][s][i][0], b[j][s][i][1]);
+                        if (SCALED) {
+                            const uint32_t scale2 = block_scale2(e_act[SCALED ? j : 0][SCALED ? i : 0]);
+                            b[j][s][i][0] = mul_bf16x2(b[j][s][i][0], scale2);
+                            b[j][s][i][1] = mul_bf16x2(b[j][s][i][1], scale2);
+                        }
+                    }
                 }
             }
         }
@@ -280,6 +308,8 @@ hif8_gemm_warp_kernel(const uint8_t* __restrict__ A, long long lda, const uint8_
         for (int j = 0; j < CH; j++) {
             if (j < plan.chunks) {
                 uint32_t x[kSlotWords];
+                const uint32_t scale2 = SCALED ? block_scale2(e_w[SCALED ? j : 0]) : 0u;
+                if (SCALED && it + 1 < n_it) e_w[SCALED ? j : 0] = weight_exp(n_next, j);
                 if (W_IS_NK) {
 #pragma unroll
                     for (int i = 0; i < kSlotWords; i++) x[i] = v[j][i];
@@ -304,6 +334,7 @@ hif8_gemm_warp_kernel(const uint8_t* __restrict__ A, long long lda, const uint8_
                         uint32_t a0, a1, a2, a3;
                         decode4(codes[u][0], lut, a0, a2);
                         decode4(codes[u][1], lut, a1, a3);
+                        if (SCALED) { a0 = mul_bf16x2(a0, scale2); a1 = mul_bf16x2(a1, scale2); a2 = mul_bf16x2(a2, scale2); a3 = mul_bf16x2(a3, scale2); }
 #pragma unroll
                         for (int i = 0; i < MT; i++) mma_16816(acc[u][i], a0, a1, a2, a3, b[j][s][i][0], b[j][s][i][1]);
                     }

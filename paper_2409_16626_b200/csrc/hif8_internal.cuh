@@ -27,6 +27,10 @@ struct GemmParams {
     // block-scaled weights (kernels with SCALED): the exponent of 128 k by 128 columns, [N,K] weights: [column block][k block], [K,N]: [k block][column block]
     const int* w_exp;
     long long w_exp_stride;
+    // ... and the warp kernel's activations [M,K]: of 1 << a_exp_shift rows by 128 k
+    const int* a_exp;
+    long long a_exp_stride;
+    int a_exp_shift;
     int c_by_tma;             // pair kernel: results leave through pieces staged in shared memory and tile stores (all but BF16 sums and the squared error)
 };
 

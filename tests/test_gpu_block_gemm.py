@@ -6,6 +6,7 @@ import torch
 
 import block_util as B
 import paper_2409_16626_b200 as H
+from gpu_util import gemm_path
 
 pytestmark = pytest.mark.gpu
 
@@ -58,8 +59,11 @@ SIZES = [(1, 128, 128), (1, 4096, 512), (5, 300, 1040), (17, 257, 2064), (48, 10
 @pytest.mark.parametrize("w_is_nk", [0, 1])
 @pytest.mark.parametrize("c_dtype", [H.F32, H.BF16])
 @pytest.mark.parametrize("M,N,K", SIZES)
-def test_forward_sizes(M, N, K, c_dtype, w_is_nk):
-    check(M, N, K, w_is_nk=w_is_nk, c_dtype=c_dtype, seed=M + N + K)
+@pytest.mark.parametrize("path", [H.GEMM_PATH_AUTO, H.GEMM_PATH_WARP, H.GEMM_PATH_NO_WARP, H.GEMM_PATH_EXPAND_BOTH])
+def test_forward_sizes(M, N, K, c_dtype, w_is_nk, path):
+    """Every kernel that a product may be given to, where it can take it."""
+    with gemm_path(path):
+        check(M, N, K, w_is_nk=w_is_nk, c_dtype=c_dtype, seed=M + N + K)
 
 
 @pytest.mark.parametrize("accumulate", [0, 1])
@@ -70,6 +74,9 @@ def test_forward_sizes(M, N, K, c_dtype, w_is_nk):
 def test_blocks_and_layouts(w_is_nk, ab, wb, a_is_km, c_dtype, accumulate):
     check(131, 264, 300, a_is_km, ab, w_is_nk, wb, c_dtype, accumulate, seed=3)
     check(20, 392, 528, a_is_km, ab, w_is_nk, wb, c_dtype, accumulate, seed=4)
+    with gemm_path(H.GEMM_PATH_NO_WARP):
+        check(20, 392, 528, a_is_km, ab, w_is_nk, wb, c_dtype, accumulate, seed=5)
+        check(300, 392, 528, a_is_km, ab, w_is_nk, wb, c_dtype, accumulate, seed=6)
 
 
 @pytest.mark.parametrize("how", [dict(lda=304, ldw=320), dict(a_offset=16, w_offset=32), dict(ldc=272), dict(lda=1024, w_offset=48, ldc=1000)])
