@@ -2,17 +2,22 @@
 //
 //   norm = sqrt(sum g^2) 2^-s,   out = g 2^-s min(1, max_norm / norm)
 //
-// Two launches: sums of squares, a share of all elements to a block, and the scaling, in front of which every block adds the shares up in the same order. Both
-// are bound by memory.  Gradients are a list of tensors; the elements of all of them in a row are what blocks share out, so that a list of many small tensors
-// and few large ones takes the time of its bytes.  Squares are added in FP32 over 16 bytes and in FP64 from there on (vectors whose sum leaves FP32's comfortable
-// range: in FP64 altogether), so the norm is as exact as FP32 can say, and the squares of finite gradients do not overflow.
+// Two launches: sums of squares, a share of the list to a block, and the scaling, in front of which every block adds the shares up in the same order. Both are bound by
+// memory.  A share is a stretch of the list of all elements, in which each tensor takes kTensorCost places more than it has elements, for what it costs to come to one: so
+// neither many small tensors nor few large ones leave blocks idle.  A block fetches the descriptors of its tensors together, works on long pieces with all threads and on short ones
+// with a warp each.  (Tensors one after the other, each with its descriptor's latency: 3000 tensors of 10 elements 362 us, CLIP_MANY_US; 2.7 M elements in 28 matrices and 9 vectors
+// 21.5 us, CLIP_SMALL_US.)  Squares are added in FP32 over 16 bytes and in FP64 from there on (vectors whose sum leaves FP32's comfortable range: in FP64 altogether), so the
+// norm is as exact as FP32 can say, and the squares of finite gradients do not overflow.
 #include "hif8_block.cuh"
 
 namespace hif8 {
 namespace {
 
-constexpr int kClipBlocks = 1024;   // shares of the sum at most
-constexpr int kClipUnroll = 4;
+constexpr int kClipBlocks = 1024;   // shares at most
+constexpr int kClipPerSM = 4;
+constexpr int kClipUnroll = 2;      // words of 32 bytes a thread has in flight
+constexpr long long kTensorCost = 1024, kShare = 2048;  // (a share's least length)
+constexpr long long kLongPiece = 2048;                  // from so many elements on a piece is the whole block's
 
 struct ClipParams {
     const uint64_t* src;
@@ -20,7 +25,7 @@ struct ClipParams {
     const int* dtypes;
     const int64_t* start;
     int tensors;
-    long long total, per;   // elements; elements of a block's share
+    long long total, cost, per;   // elements; places of the list; places of a block's share
     const int* scale_exp;
     float max_norm;
     float* norm_out;
@@ -29,23 +34,24 @@ struct ClipParams {
     int parts;
 };
 
-// Where the elements from .. to - 1 of the whole list lie in one tensor: its elements lo .. hi - 1 (shares start on multiples of eight within it).
-struct Segment {
+// Elements lo .. hi - 1 of a tensor (shares start on multiples of sixteen within it)
+struct Piece16 {
     uint64_t src, dst;
     long long lo, hi;
     int dtype;
 };
 
 __device__ __forceinline__ long long start_of(const ClipParams& p, int t) { return max(0ll, min((long long)p.start[t], p.total)); }
+__device__ __forceinline__ long long place_of(const ClipParams& p, int t) { return start_of(p, t) + kTensorCost * t; }
 
-// the last tensor that starts at or in front of `at` (a warp together, one probe a lane and round)
+// the last tensor whose places start at or in front of `at` (a warp together, one probe a lane and round)
 __device__ __forceinline__ int find_tensor(const ClipParams& p, long long at)
 {
     const int lane = threadIdx.x & 31;
     int lo = 0, n = p.tensors;
     while (n > 1) {
         const int step = (n + 31) >> 5, i = lo + lane * step;
-        const bool below = lane * step < n && (lane == 0 || start_of(p, i) <= at);
+        const bool below = lane * step < n && (lane == 0 || place_of(p, i) <= at);
         const int last = 31 - __clz(__ballot_sync(0xFFFFFFFFu, below));
         lo += last * step;
         n = min(step, n - last * step);
@@ -53,16 +59,53 @@ __device__ __forceinline__ int find_tensor(const ClipParams& p, long long at)
     return lo;
 }
 
-__device__ __forceinline__ Segment segment_of(const ClipParams& p, int t, long long from, long long to)
+// What of tensor t lies at the places from .. to - 1; false if its places start behind them
+__device__ __forceinline__ bool piece_of(const ClipParams& p, int t, long long from, long long to, Piece16& s)
 {
-    Segment s;
-    const long long b = start_of(p, t), e = start_of(p, t + 1), n = max(0ll, e - b);
+    if (t >= p.tensors) return false;
+    const long long b = start_of(p, t), e = start_of(p, t + 1), n = max(0ll, e - b), first = b + kTensorCost * (t + 1);  // place of its first element
     s.src = p.src[t];
     s.dst = p.dst ? p.dst[t] : s.src;
     s.dtype = p.dtypes[t];
-    s.lo = from <= b ? 0 : min(n, (from - b + 7) & ~7ll);
-    s.hi = to <= b ? 0 : min(n, (to - b + 7) & ~7ll);
-    return s;
+    s.lo = from <= first ? 0 : min(n, (from - first + 15) & ~15ll);
+    s.hi = to <= first ? 0 : min(n, (to - first + 15) & ~15ll);
+    return b + kTensorCost * t < to;
+}
+
+// f(piece, thread, threads) for the pieces of this block's share; first: find_tensor of its beginning
+template <class F>
+__device__ __forceinline__ void for_pieces(const ClipParams& p, long long from, long long to, int first, F&& f)
+{
+    __shared__ Piece16 s_piece[kThreads];
+    for (int batch = first; batch < p.tensors; batch += kThreads) {
+        Piece16 mine;
+        const bool in = piece_of(p, batch + (int)threadIdx.x, from, to, mine);
+        if (in) s_piece[threadIdx.x] = mine;
+        const int n = __syncthreads_count(in);  // (starts are in order: those in the share come first)
+        const int warp = threadIdx.x >> 5;
+#pragma unroll 1
+        for (int i = 0; i < n + (kThreads / 32) * ((n + kThreads / 32 - 1) / (kThreads / 32)); i += i < n ? 1 : kThreads / 32) {  // long ones, then a warp's short ones
+            const bool alone = i >= n;
+            const int k = alone ? i - n + warp : i;
+            if (k >= n) continue;
+            const Piece16 s = s_piece[k];
+            if ((s.hi - s.lo < kLongPiece) != alone) continue;
+            f(s, alone ? (int)(threadIdx.x & 31u) : (int)threadIdx.x, alone ? 32 : kThreads);
+        }
+        if (n < kThreads) break;
+        __syncthreads();
+    }
+}
+
+__device__ __forceinline__ void load_32(const void* from, uint4& a, uint4& b)
+{
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "l"(from));
+}
+__device__ __forceinline__ void store_32(void* to, const uint4& a, const uint4& b)
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(to), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
 }
 
 template <int DT> __device__ __forceinline__ double squares(const uint4& v)
@@ -89,24 +132,28 @@ template <int DT> __device__ __forceinline__ double squares(const uint4& v)
     return d;
 }
 
-template <int DT> __device__ __forceinline__ double segment_squares(const Segment& s)
+template <int DT> __device__ __forceinline__ double piece_squares(const Piece16& s, int thread, int threads)
 {
-    constexpr int PV = SrcTraits<DT>::kPerVec;
+    constexpr int PW = 2 * SrcTraits<DT>::kPerVec;  // elements of 32 bytes
     double sum = 0.0;
     long long tail = s.lo;
-    if ((s.src & 15u) == 0) {
-        const uint4* v4 = reinterpret_cast<const uint4*>(s.src);
-        const long long end = s.hi / PV;
-        for (long long base = s.lo / PV + threadIdx.x; base < end; base += kThreads * kClipUnroll) {
-            uint4 v[kClipUnroll];
+    if ((s.src & 31u) == 0) {
+        const char* from = reinterpret_cast<const char*>(s.src);
+        const long long end = s.hi / PW;
+        for (long long base = s.lo / PW + thread; base < end; base += threads * kClipUnroll) {
+            uint4 v[kClipUnroll][2];
 #pragma unroll
-            for (int j = 0; j < kClipUnroll; j++) v[j] = base + j * kThreads < end ? v4[base + j * kThreads] : make_uint4(0, 0, 0, 0);
+            for (int j = 0; j < kClipUnroll; j++) {
+                v[j][0] = v[j][1] = make_uint4(0, 0, 0, 0);
+                if (base + j * threads < end) load_32(from + (base + j * threads) * 32, v[j][0], v[j][1]);
+            }
 #pragma unroll
-            for (int j = 0; j < kClipUnroll; j++) sum += squares<DT>(v[j]);
+            for (int j = 0; j < kClipUnroll; j++) sum += squares<DT>(v[j][0]) + squares<DT>(v[j][1]);
         }
-        tail = end * PV;
+        tail = max(s.lo, end * PW);
     }
-    for (long long i = tail + threadIdx.x; i < s.hi; i += kThreads) {
+#pragma unroll 1
+    for (long long i = tail + thread; i < s.hi; i += threads) {
         float x; uint32_t raw;
         load_scalar<DT>(reinterpret_cast<const void*>(s.src), (unsigned long long)i, x, raw);
         sum = fma((double)x, (double)x, sum);
@@ -126,22 +173,19 @@ __device__ __forceinline__ double block_sum(double v, double* s_part)
     return v;
 }
 
-__global__ void __launch_bounds__(kThreads) grad_squares_kernel(const ClipParams p)
+__global__ void __launch_bounds__(kThreads, kClipPerSM) grad_squares_kernel(const ClipParams p)
 {
     __shared__ double s_part[kThreads / 32];
     pdl_wait_prior_grid();
     pdl_launch_dependents();
-    const long long from = (long long)blockIdx.x * p.per, to = min(p.total, from + p.per);
+    const long long from = (long long)blockIdx.x * p.per, to = min(p.cost, from + p.per);
     double sum = 0.0;
-    if (from < to) {
-        for (int t = find_tensor(p, from); t < p.tensors && start_of(p, t) < to; t++) {
-            const Segment s = segment_of(p, t, from, to);
-            if (s.lo >= s.hi) continue;
-            if (s.dtype == HIF8_F32) sum += segment_squares<HIF8_F32>(s);
-            else if (s.dtype == HIF8_BF16) sum += segment_squares<HIF8_BF16>(s);
-            else if (s.dtype == HIF8_F16) sum += segment_squares<HIF8_F16>(s);
-        }
-    }
+    if (from < to)
+        for_pieces(p, from, to, find_tensor(p, from), [&](const Piece16& s, int thread, int threads) {
+            if (s.dtype == HIF8_F32) sum += piece_squares<HIF8_F32>(s, thread, threads);
+            else if (s.dtype == HIF8_BF16) sum += piece_squares<HIF8_BF16>(s, thread, threads);
+            else if (s.dtype == HIF8_F16) sum += piece_squares<HIF8_F16>(s, thread, threads);
+        });
     sum = block_sum(sum, s_part);
     if (threadIdx.x == 0) p.part[blockIdx.x] = sum;
 }
@@ -154,39 +198,43 @@ struct Factor {
 
 template <int DT> __device__ __forceinline__ uint4 scaled(const uint4& v, const Factor& f)
 {
-    constexpr int PV = SrcTraits<DT>::kPerVec;
-    uint32_t w[4] = {0u, 0u, 0u, 0u};
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int k = 0; k < PV; k++) {
-        float x; uint32_t raw;
-        unpack<DT>(v, k, x, raw);
-        const uint32_t b = to_bits<DT>(f.of(x));
-        if (DT == HIF8_F32) w[k] = b;
-        else w[k >> 1] |= b << (16 * (k & 1));
+    for (int k = 0; k < 4; k++) {
+        if (DT == HIF8_F32) w[k] = __float_as_uint(f.of(__uint_as_float(w[k])));
+        else if (DT == HIF8_BF16) {
+            const float lo = f.of(__uint_as_float(w[k] << 16)), hi = f.of(__uint_as_float(w[k] & 0xFFFF0000u));
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[k]) : "f"(hi), "f"(lo));
+        } else {
+            const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
+            asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w[k]) : "f"(f.of(x.y)), "f"(f.of(x.x)));
+        }
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // (from its end: what the first launch read last may still be in L2)
-template <int DT> __device__ __forceinline__ void scale_segment(const Segment& s, const Factor& f)
+template <int DT> __device__ __forceinline__ void scale_piece(const Piece16& s, const Factor& f, int thread, int threads)
 {
-    constexpr int PV = SrcTraits<DT>::kPerVec;
+    constexpr int PW = 2 * SrcTraits<DT>::kPerVec;
     long long tail = s.lo;
-    if (((s.src | s.dst) & 15u) == 0) {
-        const uint4* v4 = reinterpret_cast<const uint4*>(s.src);
-        uint4* o4 = reinterpret_cast<uint4*>(s.dst);
-        const long long first = s.lo / PV, end = s.hi / PV;
-        for (long long base = end - 1 - threadIdx.x; base >= first; base -= kThreads * kClipUnroll) {
-            uint4 v[kClipUnroll];
-#pragma unroll
-            for (int j = 0; j < kClipUnroll; j++) v[j] = base - j * kThreads >= first ? __ldcs(v4 + base - j * kThreads) : make_uint4(0, 0, 0, 0);
+    if (((s.src | s.dst) & 31u) == 0) {
+        const char* from = reinterpret_cast<const char*>(s.src);
+        char* to = reinterpret_cast<char*>(s.dst);
+        const long long first = s.lo / PW, end = s.hi / PW;
+        for (long long base = end - 1 - thread; base >= first; base -= threads * kClipUnroll) {
+            uint4 v[kClipUnroll][2];
 #pragma unroll
             for (int j = 0; j < kClipUnroll; j++)
-                if (base - j * kThreads >= first) __stcs(o4 + base - j * kThreads, scaled<DT>(v[j], f));
+                if (base - j * threads >= first) load_32(from + (base - j * threads) * 32, v[j][0], v[j][1]);
+#pragma unroll
+            for (int j = 0; j < kClipUnroll; j++)
+                if (base - j * threads >= first) store_32(to + (base - j * threads) * 32, scaled<DT>(v[j][0], f), scaled<DT>(v[j][1], f));
         }
-        tail = end * PV;
+        tail = max(s.lo, end * PW);
     }
-    for (long long i = tail + threadIdx.x; i < s.hi; i += kThreads) {
+#pragma unroll 1
+    for (long long i = tail + thread; i < s.hi; i += threads) {
         float x; uint32_t raw;
         load_scalar<DT>(reinterpret_cast<const void*>(s.src), (unsigned long long)i, x, raw);
         const uint32_t b = to_bits<DT>(f.of(x));
@@ -195,9 +243,12 @@ template <int DT> __device__ __forceinline__ void scale_segment(const Segment& s
     }
 }
 
-__global__ void __launch_bounds__(kThreads) grad_scale_kernel(const ClipParams p)
+__global__ void __launch_bounds__(kThreads, kClipPerSM) grad_scale_kernel(const ClipParams p)
 {
     __shared__ double s_part[kThreads / 32];
+    // (the list is none of the first launch's results, and what wrote it is over since that one runs)
+    const long long from = (long long)blockIdx.x * p.per, to = min(p.cost, from + p.per);
+    const int first = from < to ? find_tensor(p, from) : 0;
     pdl_wait_prior_grid();
     pdl_launch_dependents();
     double sum = 0.0;
@@ -218,15 +269,13 @@ __global__ void __launch_bounds__(kThreads) grad_scale_kernel(const ClipParams p
     const int k1 = max(-126, min(125, k));  // (m rounded to FP32 may be 2)
     const Factor f{(float)m * pow2f(k1), pow2f(k - k1)};
     const bool same = f.f == 1.f && f.p == 1.f;  // in place there is nothing to do
-    const long long from = (long long)blockIdx.x * p.per, to = min(p.total, from + p.per);
-    if (from >= to) return;
-    for (int t = find_tensor(p, to - 1); t >= 0 && start_of(p, t + 1) > from; t--) {
-        const Segment s = segment_of(p, t, from, to);
-        if (s.lo >= s.hi || (same && s.src == s.dst)) continue;
-        if (s.dtype == HIF8_F32) scale_segment<HIF8_F32>(s, f);
-        else if (s.dtype == HIF8_BF16) scale_segment<HIF8_BF16>(s, f);
-        else if (s.dtype == HIF8_F16) scale_segment<HIF8_F16>(s, f);
-    }
+    if (from < to)
+        for_pieces(p, from, to, first, [&](const Piece16& s, int thread, int threads) {
+            if (same && s.src == s.dst) return;
+            if (s.dtype == HIF8_F32) scale_piece<HIF8_F32>(s, f, thread, threads);
+            else if (s.dtype == HIF8_BF16) scale_piece<HIF8_BF16>(s, f, thread, threads);
+            else if (s.dtype == HIF8_F16) scale_piece<HIF8_F16>(s, f, thread, threads);
+        });
 }
 
 }  // namespace
@@ -255,12 +304,12 @@ extern "C" int hif8_grad_clip(const uint64_t* d_src, const uint64_t* d_dst, cons
     ClipParams p{};
     p.src = d_src; p.dst = d_dst; p.dtypes = d_dtype; p.start = d_start; p.tensors = n_tensors; p.total = n_tensors ? n_elements : 0;
     p.scale_exp = d_scale_exp; p.max_norm = max_norm; p.norm_out = d_norm; p.found = d_found_inf; p.part = reinterpret_cast<double*>(workspace);
-    // a share: 2048 elements or more, a multiple of that
-    long long blocks = (p.total + 2047) / 2048;
-    const long long most = (long long)sms * 6 < kClipBlocks ? (long long)sms * 6 : kClipBlocks;
+    p.cost = n_tensors ? n_elements + kTensorCost * n_tensors : 0;
+    long long blocks = (p.cost + kShare - 1) / kShare;
+    const long long most = (long long)sms * kClipPerSM < kClipBlocks ? (long long)sms * kClipPerSM : kClipBlocks;
     if (blocks > most) blocks = most;
     if (blocks < 1) blocks = 1;
-    p.per = ((p.total + blocks - 1) / blocks + 2047) / 2048 * 2048;
+    p.per = ((p.cost + blocks - 1) / blocks + 63) / 64 * 64;
     p.parts = (int)blocks;
     cudaStream_t st = (cudaStream_t)stream;
     launch_pdl(grad_squares_kernel, dim3((unsigned)blocks), st, p);
