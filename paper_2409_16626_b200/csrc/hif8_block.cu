@@ -181,6 +181,11 @@ struct DecodeParams {
     unsigned clear_words;
     bool late;           // the next launch may start at the end (see launch_decode)
 };
+// One matrix, or two (a product's operands) in one launch: the groups of the second follow those of the first.
+template <bool TWO> struct DecodeJob {
+    DecodeParams m[TWO ? 2 : 1];
+    unsigned units;
+};
 
 __device__ __forceinline__ int exp_at(const BlockCodes& m, long long r, long long c)
 {
@@ -235,17 +240,17 @@ __device__ __forceinline__ void store_sixteen(void* row, unsigned c, long long c
 
 // LANE: a copy of the table for each lane.  One table for all costs a warp several wavefronts a lookup; filling 32 copies costs a block more than a
 // small matrix takes.  The next groups' codes are on their way while those at hand are looked up.
-template <int DST, bool LANE, int UN>
-__global__ void __launch_bounds__(kThreads, LANE ? 6 : 4) block_decode_kernel(const DecodeParams p)
+template <int DST, bool LANE, bool TWO>
+__global__ void __launch_bounds__(kThreads, LANE ? 6 : 4) block_decode_kernel(const __grid_constant__ DecodeJob<TWO> job)
 {
     __shared__ __align__(16) uint32_t table[LANE ? kLaneTableWords : 256];
     if (LANE) fill_lane_table(table, decode_bits_f32(threadIdx.x) >> 16);
     else table[threadIdx.x] = decode_bits_f32(threadIdx.x) >> 16;
     __syncthreads();
     pdl_wait_prior_grid();
-    if (!p.late) pdl_launch_dependents();
+    if (!job.m[0].late) pdl_launch_dependents();
     if (blockIdx.x == 0)
-        for (unsigned i = threadIdx.x; i < p.clear_words; i += kThreads) p.clear[i] = 0u;
+        for (unsigned i = threadIdx.x; i < job.m[0].clear_words; i += kThreads) job.m[0].clear[i] = 0u;
     const uint32_t lane4 = (threadIdx.x & 31u) * 4u;
     constexpr size_t item = DST == HIF8_F32 ? 4 : 2;
     struct Group {
@@ -253,12 +258,15 @@ __global__ void __launch_bounds__(kThreads, LANE ? 6 : 4) block_decode_kernel(co
         int e;
         unsigned row, col;
     };
+    auto which = [&](unsigned long long u) { return TWO && u >= job.m[0].units ? 1 : 0; };
     auto load = [&](unsigned long long u64) {
         Group g;
         g.v = make_uint4(0u, 0u, 0u, 0u);
         g.e = 0; g.row = 0; g.col = 0;
-        if (u64 >= p.units) return g;
-        const unsigned u = (unsigned)u64;
+        if (u64 >= job.units) return g;
+        const int k = which(u64);
+        const DecodeParams& p = job.m[k];
+        const unsigned u = (unsigned)(u64 - (k ? job.m[0].units : 0u));
         g.row = p.chunks.div(u); g.col = (u - g.row * p.chunks.d) * 16u;
         if (g.row < p.m.rows && g.col < p.m.cols) {
             const uint8_t* at = p.m.codes + (size_t)g.row * (size_t)p.m.ld;
@@ -271,28 +279,19 @@ __global__ void __launch_bounds__(kThreads, LANE ? 6 : 4) block_decode_kernel(co
         }
         return g;
     };
-    const unsigned long long step = (unsigned long long)gridDim.x * (kThreads * UN);
-    unsigned long long base = (unsigned long long)blockIdx.x * (kThreads * UN) + threadIdx.x;
-    Group next[UN];
-#pragma unroll
-    for (int j = 0; j < UN; j++) next[j] = load(base + j * kThreads);
-    for (; base < p.units; base += step) {
-        Group now[UN];
-#pragma unroll
-        for (int j = 0; j < UN; j++) {
-            now[j] = next[j];
-            if (LANE) next[j] = load(base + step + j * kThreads);
-        }
-#pragma unroll
-        for (int j = 0; j < UN; j++) {
-            if (base + j * kThreads >= p.units) continue;
-            const Eight<DST> lo = scaled_eight<DST>(bf16_of_four<LANE>(table, now[j].v.x, lane4), bf16_of_four<LANE>(table, now[j].v.y, lane4), now[j].e);
-            const Eight<DST> hi = scaled_eight<DST>(bf16_of_four<LANE>(table, now[j].v.z, lane4), bf16_of_four<LANE>(table, now[j].v.w, lane4), now[j].e);
-            store_sixteen<DST>(reinterpret_cast<char*>(p.dst) + (size_t)now[j].row * (size_t)p.ld_dst * item, now[j].col, p.cols_out, p.vectors, p.vectors32, lo, hi);
-        }
+    const unsigned long long step = (unsigned long long)gridDim.x * kThreads;
+    unsigned long long base = (unsigned long long)blockIdx.x * kThreads + threadIdx.x;
+    Group next = load(base);
+    for (; base < job.units; base += step) {
+        const Group now = next;
+        if (LANE) next = load(base + step);
+        const DecodeParams& p = job.m[which(base)];
+        const Eight<DST> lo = scaled_eight<DST>(bf16_of_four<LANE>(table, now.v.x, lane4), bf16_of_four<LANE>(table, now.v.y, lane4), now.e);
+        const Eight<DST> hi = scaled_eight<DST>(bf16_of_four<LANE>(table, now.v.z, lane4), bf16_of_four<LANE>(table, now.v.w, lane4), now.e);
+        store_sixteen<DST>(reinterpret_cast<char*>(p.dst) + (size_t)now.row * (size_t)p.ld_dst * item, now.col, p.cols_out, p.vectors, p.vectors32, lo, hi);
         if (!LANE) break;  // (as many threads as groups)
     }
-    if (p.late) pdl_launch_dependents();
+    if (job.m[0].late) pdl_launch_dependents();
 }
 
 // Codes [rows, cols] -> BF16 [cols, ld_dst], transposed: tiles of 64 rows by 64 columns.  A thread takes two rows' eight columns and puts a column's two
@@ -376,36 +375,50 @@ void launch_encode_mode(int rnd, const EncodeParams& p, int sms, cudaStream_t st
     }
 }
 
-template <int DST>
-void launch_decode(DecodeParams p, int sms, cudaStream_t st)
+template <int DST, bool TWO>
+void launch_decode(DecodeJob<TWO> job, int sms, cudaStream_t st)
 {
-    const unsigned most = (unsigned)sms * 6u, few = (p.units + kThreads - 1) / kThreads;
-    if (few <= (unsigned)sms * 4u) launch_pdl(block_decode_kernel<DST, false, 1>, dim3(few), st, p);
-    else {
-        p.late = true;
-        launch_pdl(block_decode_kernel<DST, true, 1>, dim3(few < most ? few : most), st, p);
-    }
+    job.units = job.m[0].units + (TWO ? job.m[TWO ? 1 : 0].units : 0u);
+    const unsigned most = (unsigned)sms * 6u, few = (job.units + kThreads - 1) / kThreads;
+    if (few <= (unsigned)sms * 4u) {
+        job.m[0].late = false;
+        launch_pdl(block_decode_kernel<DST, false, TWO>, dim3(few), st, job);
+    } else launch_pdl(block_decode_kernel<DST, true, TWO>, dim3(few < most ? few : most), st, job);
+}
+
+// a product's operand, to be decoded as it is stored (or transposed); false: too large
+bool operand_job(const BlockOperand& o, DecodeParams* p)
+{
+    *p = DecodeParams{};
+    p->m = o.m; p->dst = o.dst; p->ld_dst = o.ld_dst; p->rows_out = o.rows_out; p->cols_out = o.cols_out;
+    p->codes8 = aligned_to(o.m.codes, 8) && (o.m.rows <= 1 || (o.m.ld & 7) == 0); p->codes16 = aligned_to(o.m.codes, 16) && (o.m.rows <= 1 || (o.m.ld & 15) == 0);
+    p->vectors = true; p->vectors32 = aligned_to(o.dst, 32) && (o.ld_dst & 15) == 0;
+    const long long across = o.transposed ? (o.cols_out + kFlipCols - 1) / kFlipCols : (o.cols_out + 15) / 16;
+    const long long down = o.transposed ? (o.rows_out + kFlipRows - 1) / kFlipRows : o.rows_out;
+    if (across > 0x3FFFFFFFll / (down > 0 ? down : 1)) return false;
+    p->chunks = FastDiv((uint32_t)across); p->units = (unsigned)(across * down);
+    return true;
 }
 
 }  // namespace
 
-int expand_block_codes(const BlockCodes& m, void* dst, long long ld_dst, long long rows_out, long long cols_out, bool transposed, uint32_t* clear, unsigned clear_words,
-                       cudaStream_t st)
+int expand_block_codes(const BlockOperand& a, const BlockOperand* w, uint32_t* clear, unsigned clear_words, cudaStream_t st)
 {
     int sms; if (int rc = checked_device(&sms)) return rc;
-    DecodeParams p{};
-    p.m = m; p.dst = dst; p.ld_dst = ld_dst; p.rows_out = rows_out; p.cols_out = cols_out; p.clear = clear; p.clear_words = clear_words;
-    p.codes8 = aligned_to(m.codes, 8) && (m.rows <= 1 || (m.ld & 7) == 0); p.codes16 = aligned_to(m.codes, 16) && (m.rows <= 1 || (m.ld & 15) == 0);
-    p.vectors = true; p.vectors32 = aligned_to(dst, 32) && (ld_dst & 15) == 0;
-    const long long across = transposed ? (cols_out + kFlipCols - 1) / kFlipCols : (cols_out + 15) / 16;
-    const long long down = transposed ? (rows_out + kFlipRows - 1) / kFlipRows : rows_out;
-    if (across > 0x7FFFFFFFll / (down > 0 ? down : 1)) return HIF8_ERR_SHAPE;
-    p.chunks = FastDiv((uint32_t)across); p.units = (unsigned)(across * down);
-    if (transposed) {
+    DecodeJob<true> two{};
+    if (!operand_job(a, &two.m[0]) || (w && !operand_job(*w, &two.m[1]))) return HIF8_ERR_SHAPE;
+    two.m[0].clear = clear; two.m[0].clear_words = clear_words;
+    if (w) launch_decode<HIF8_BF16, true>(two, sms, st);
+    else if (a.transposed) {
+        const DecodeParams& p = two.m[0];
         const unsigned most = (unsigned)sms * 4u;
         if (p.units <= (unsigned)sms * 2u) launch_pdl(block_decode_transpose_kernel<false>, dim3(p.units), st, p);
         else launch_pdl(block_decode_transpose_kernel<true>, dim3(p.units < most ? p.units : most), st, p);
-    } else launch_decode<HIF8_BF16>(p, sms, st);
+    } else {
+        DecodeJob<false> one{};
+        one.m[0] = two.m[0];
+        launch_decode<HIF8_BF16, false>(one, sms, st);
+    }
     return finish(1);
 }
 
@@ -448,7 +461,9 @@ extern "C" int hif8_block_decode(const uint8_t* src, int64_t ld_src, const int* 
 {
     if (bad_dtype(dst_dtype)) return HIF8_ERR_DTYPE;
     if (rows < 0 || cols < 0 || (block_rows != 1 && block_rows != HIF8_BLOCK)) return HIF8_ERR_SHAPE;
-    DecodeParams p{};
+    DecodeJob<false> job{};
+    DecodeParams& p = job.m[0];
+    p.late = true;
     p.m = BlockCodes{const_cast<uint8_t*>(src), ld_src, const_cast<int*>(d_exp), exp_stride, rows, cols, block_rows == 1 ? 0 : 7};
     if (ld_src < cols || ld_dst < cols || exp_stride < p.m.blocks_across()) return HIF8_ERR_SHAPE;
     if (rows == 0 || cols == 0) return HIF8_OK;
@@ -464,8 +479,8 @@ extern "C" int hif8_block_decode(const uint8_t* src, int64_t ld_src, const int* 
     p.codes8 = aligned_to(src, 8) && (rows <= 1 || (ld_src & 7) == 0); p.codes16 = aligned_to(src, 16) && (rows <= 1 || (ld_src & 15) == 0);
     p.vectors = vector_rows(dst, rows, ld_dst, item); p.vectors32 = aligned_to(dst, 32) && (rows <= 1 || ((size_t)ld_dst * item & 31u) == 0);
     cudaStream_t st = (cudaStream_t)stream;
-    if (dst_dtype == HIF8_F32) launch_decode<HIF8_F32>(p, sms, st);
-    else if (dst_dtype == HIF8_BF16) launch_decode<HIF8_BF16>(p, sms, st);
-    else launch_decode<HIF8_F16>(p, sms, st);
+    if (dst_dtype == HIF8_F32) launch_decode<HIF8_F32, false>(job, sms, st);
+    else if (dst_dtype == HIF8_BF16) launch_decode<HIF8_BF16, false>(job, sms, st);
+    else launch_decode<HIF8_F16, false>(job, sms, st);
     return finish(1);
 }

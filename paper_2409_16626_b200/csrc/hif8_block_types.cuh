@@ -59,10 +59,17 @@ struct BlockWorkspace {
 struct GemmParams;
 int launch_block_gemm(const BlockCodes& a, bool a_is_km, const BlockCodes& w, bool w_is_nk, const GemmParams& p, const BlockWorkspace& sizes, void* workspace, cudaStream_t st);
 
-// Codes of a product's operand, decoded into BF16 with their blocks' scales (exact: four significant bits, exponents within -118 .. 111):
+// A product's operand to be decoded into BF16 with its blocks' scales (exact: four significant bits, exponents within -118 .. 111):
 // dst [rows_out, cols_out], or with `transposed` element (r, c) at dst[c][r]; rows and columns beyond the matrix become zeros.  cols_out (transposed:
-// rows_out) and ld_dst are multiples of 8, dst is 16-byte aligned.  The launch also clears clear_words words.
-int expand_block_codes(const BlockCodes& m, void* dst, long long ld_dst, long long rows_out, long long cols_out, bool transposed, uint32_t* clear, unsigned clear_words, cudaStream_t st);
+// rows_out) and ld_dst are multiples of 8, dst is 16-byte aligned.
+struct BlockOperand {
+    BlockCodes m;
+    void* dst;
+    long long ld_dst, rows_out, cols_out;
+    bool transposed;
+};
+// One launch for an operand, or for two as they are stored; it also clears clear_words words.
+int expand_block_codes(const BlockOperand& a, const BlockOperand* w, uint32_t* clear, unsigned clear_words, cudaStream_t st);
 
 namespace {
 

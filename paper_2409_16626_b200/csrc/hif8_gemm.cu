@@ -2998,9 +2998,9 @@ int hif8::launch_block_gemm(const BlockCodes& a, bool a_is_km, const BlockCodes&
     if (cudaGetDevice(&dev) != cudaSuccess || !gemm_kernels_ready(dev, &sm_count, &wd_clusters, &nw_clusters, &wp_clusters)) return HIF8_ERR_CUDA;
     unsigned char* wsb = reinterpret_cast<unsigned char*>(workspace) + BlockWorkspace::kStatus;
     unsigned char* a_bf = wsb;
-    const long long a_rows = a_is_km ? sizes.a_pitch : M, a_cols = a_is_km ? M : sizes.a_pitch;
     auto expand_a = [&](size_t clear_bytes) {
-        return expand_block_codes(a, a_bf, sizes.a_pitch, a_rows, a_cols, a_is_km, reinterpret_cast<uint32_t*>(workspace), (unsigned)(clear_bytes / 4), st);
+        const BlockOperand op{a, a_bf, sizes.a_pitch, a_is_km ? sizes.a_pitch : M, a_is_km ? M : sizes.a_pitch, a_is_km};
+        return expand_block_codes(op, nullptr, reinterpret_cast<uint32_t*>(workspace), (unsigned)(clear_bytes / 4), st);
     };
     if (sizes.in_kernel) {
         p.w_exp = w.exps; p.w_exp_stride = w.exp_stride;
@@ -3053,8 +3053,8 @@ int hif8::launch_block_gemm(const BlockCodes& a, bool a_is_km, const BlockCodes&
     // both operands expanded as they are stored
     unsigned char* w_bf = a_bf + sizes.a_bytes;
     const long long a_pitch = a_is_km ? sizes.a_pitch_km : sizes.a_pitch;
-    if (int rc = expand_block_codes(a, a_bf, a_pitch, a.rows, a_pitch, false, reinterpret_cast<uint32_t*>(workspace), 1, st)) return rc;
-    if (int rc = expand_block_codes(w, w_bf, sizes.w_pitch, w.rows, sizes.w_pitch, false, nullptr, 0, st)) return rc;
+    const BlockOperand op_a{a, a_bf, a_pitch, a.rows, a_pitch, false}, op_w{w, w_bf, sizes.w_pitch, w.rows, sizes.w_pitch, false};
+    if (int rc = expand_block_codes(op_a, &op_w, reinterpret_cast<uint32_t*>(workspace), 1, st)) return rc;
     return launch_bf16_pair_gemm(a_bf, w_bf, w_is_nk, p, st, 0, 0, a_pitch, sizes.w_pitch, a_is_km);
 }
 
