@@ -221,6 +221,11 @@ __global__ void __launch_bounds__(BLOCK, norm_blocks(DT, BLOCK, WHOLE)) norm_bac
         if (p.dh) {
 #pragma unroll
             for (int j = 0; j < NV; j++) dh[j] = load_eight<DT, false, WHOLE>(row_at<DT>(p.dh, row, p.ld_dh), (j * gs + t) * 8, end, p.vec_dh);
+        } else {
+#pragma unroll
+            for (int j = 0; j < NV; j++)
+#pragma unroll
+                for (int i = 0; i < (int)(sizeof(dh[j].v) / 16); i++) dh[j].v[i] = make_uint4(0, 0, 0, 0);
         }
         float sum = 0.f;
 #pragma unroll
@@ -228,13 +233,13 @@ __global__ void __launch_bounds__(BLOCK, norm_blocks(DT, BLOCK, WHOLE)) norm_bac
             const Eight<DT> w = load_eight<DT, true, WHOLE>(p.weight, (j * gs + t) * 8, p.cols, p.vec_w);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                const float d = value_of_eight<DT>(dy[j], i), u = value_of_eight<DT>(h[j], i) * rstd;
-                sum = fmaf(d * value_of_eight<DT>(w, i), u, sum);
-                if (!kFar) acc[j % (kFar ? 1 : NV)][i] = fmaf(d, u, acc[j % (kFar ? 1 : NV)][i]);
-                else s_acc[(j * 8 + i) * BLOCK + threadIdx.x] = fmaf(d, u, s_acc[(j * 8 + i) * BLOCK + threadIdx.x]);
+                const float d = value_of_eight<DT>(dy[j], i), x = value_of_eight<DT>(h[j], i), du = d * rstd;
+                sum = fmaf(d * value_of_eight<DT>(w, i), x, sum);
+                if (!kFar) acc[j % (kFar ? 1 : NV)][i] = fmaf(du, x, acc[j % (kFar ? 1 : NV)][i]);
+                else s_acc[(j * 8 + i) * BLOCK + threadIdx.x] = fmaf(du, x, s_acc[(j * 8 + i) * BLOCK + threadIdx.x]);
             }
         }
-        const float mean = row_sum(sum, s_part[turn], p.lg, group, groups == 1) * inv;
+        const float mean = row_sum(sum, s_part[turn], p.lg, group, groups == 1) * rstd * inv, factor = -rstd * mean;
         const void* weight = p.weight;
         asm volatile("" : "+l"(weight));
 #pragma unroll
@@ -244,10 +249,9 @@ __global__ void __launch_bounds__(BLOCK, norm_blocks(DT, BLOCK, WHOLE)) norm_bac
             const Eight<DT> w = load_eight<DT, true, WHOLE>(weight, (j * gs + t) * 8, p.cols, p.vec_w);
             float g[8];
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const float u = value_of_eight<DT>(h[j], i) * rstd, wdy = value_of_eight<DT>(dy[j], i) * value_of_eight<DT>(w, i);
-                g[i] = rstd * fmaf(-u, mean, wdy);
-                if (p.dh) g[i] += value_of_eight<DT>(dh[j], i);
+            for (int i = 0; i < 8; i++) {  // r (w dy - u mean) + dh
+                const float wdy = value_of_eight<DT>(dy[j], i) * value_of_eight<DT>(w, i);
+                g[i] = fmaf(rstd, fmaf(factor, value_of_eight<DT>(h[j], i), wdy), value_of_eight<DT>(dh[j], i));
             }
             store_eight<DT, WHOLE>(const_cast<char*>(row_at<DT>(p.dx, row, p.ld_dx)), (j * gs + t) * 8, end, p.vec_dx, pack_eight<DT>(g));
         }
