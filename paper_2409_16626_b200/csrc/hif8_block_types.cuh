@@ -40,7 +40,7 @@ struct BlockWorkspace {
     {
         auto pad8 = [](long long n) { return (n + 7) & ~7ll; };
         auto pad256 = [](size_t n) { return (n + 255) & ~(size_t)255; };
-        in_kernel = w_block_rows == HIF8_BLOCK && (K & 15) == 0;
+        in_kernel = w_block_rows == HIF8_BLOCK;
         a_pitch = pad8(K);
         a_pitch_km = pad8(M);
         w_pitch = pad8(w_is_nk ? K : N);

@@ -97,14 +97,21 @@ __device__ __forceinline__ void for_pieces(const ClipParams& p, long long from, 
     }
 }
 
-__device__ __forceinline__ void load_32(const void* from, uint4& a, uint4& b)
+// 32 bytes; `whole`: on a boundary of that many, and not of 16 only
+__device__ __forceinline__ void load_32(const void* from, uint4& a, uint4& b, bool whole)
 {
-    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+    if (!whole) {
+        a = reinterpret_cast<const uint4*>(from)[0];
+        b = reinterpret_cast<const uint4*>(from)[1];
+    } else asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "l"(from));
 }
-__device__ __forceinline__ void store_32(void* to, const uint4& a, const uint4& b)
+__device__ __forceinline__ void store_32(void* to, const uint4& a, const uint4& b, bool whole)
 {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+    if (!whole) {
+        reinterpret_cast<uint4*>(to)[0] = a;
+        reinterpret_cast<uint4*>(to)[1] = b;
+    } else asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                  ::"l"(to), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
 }
 
@@ -137,7 +144,8 @@ template <int DT> __device__ __forceinline__ double piece_squares(const Piece16&
     constexpr int PW = 2 * SrcTraits<DT>::kPerVec;  // elements of 32 bytes
     double sum = 0.0;
     long long tail = s.lo;
-    if ((s.src & 31u) == 0) {
+    if ((s.src & 15u) == 0) {
+        const bool whole = (s.src & 16u) == 0;
         const char* from = reinterpret_cast<const char*>(s.src);
         const long long end = s.hi / PW;
         for (long long base = s.lo / PW + thread; base < end; base += threads * kClipUnroll) {
@@ -145,7 +153,7 @@ template <int DT> __device__ __forceinline__ double piece_squares(const Piece16&
 #pragma unroll
             for (int j = 0; j < kClipUnroll; j++) {
                 v[j][0] = v[j][1] = make_uint4(0, 0, 0, 0);
-                if (base + j * threads < end) load_32(from + (base + j * threads) * 32, v[j][0], v[j][1]);
+                if (base + j * threads < end) load_32(from + (base + j * threads) * 32, v[j][0], v[j][1], whole);
             }
 #pragma unroll
             for (int j = 0; j < kClipUnroll; j++) sum += squares<DT>(v[j][0]) + squares<DT>(v[j][1]);
@@ -218,7 +226,8 @@ template <int DT> __device__ __forceinline__ void scale_piece(const Piece16& s, 
 {
     constexpr int PW = 2 * SrcTraits<DT>::kPerVec;
     long long tail = s.lo;
-    if (((s.src | s.dst) & 31u) == 0) {
+    if (((s.src | s.dst) & 15u) == 0) {
+        const bool whole = ((s.src | s.dst) & 16u) == 0;
         const char* from = reinterpret_cast<const char*>(s.src);
         char* to = reinterpret_cast<char*>(s.dst);
         const long long first = s.lo / PW, end = s.hi / PW;
@@ -226,10 +235,10 @@ template <int DT> __device__ __forceinline__ void scale_piece(const Piece16& s, 
             uint4 v[kClipUnroll][2];
 #pragma unroll
             for (int j = 0; j < kClipUnroll; j++)
-                if (base - j * threads >= first) load_32(from + (base - j * threads) * 32, v[j][0], v[j][1]);
+                if (base - j * threads >= first) load_32(from + (base - j * threads) * 32, v[j][0], v[j][1], whole);
 #pragma unroll
             for (int j = 0; j < kClipUnroll; j++)
-                if (base - j * threads >= first) store_32(to + (base - j * threads) * 32, scaled<DT>(v[j][0], f), scaled<DT>(v[j][1], f));
+                if (base - j * threads >= first) store_32(to + (base - j * threads) * 32, scaled<DT>(v[j][0], f), scaled<DT>(v[j][1], f), whole);
         }
         tail = max(s.lo, end * PW);
     }

@@ -1586,18 +1586,28 @@ hif8_gemm_weights_kernel(const __grid_constant__ CUtensorMap map_w, const __grid
         constexpr int kGaveUp = 1 << 30;
         int it = decodes ? group : kGaveUp, tile_it = 0, local = 0;  // next k-block of the group; first k-block of the tile to finish next
         bool joined = !decodes;
-        // SCALED: exponent of the weight block of this CTA's x-th k-block, over all its tiles (0 where there is none)
-        auto block_exp = [&](int x) {
-            const int i = x / n_kb, tile = t0 + i * t_step, kb = kb0 + x - i * n_kb;
-            if (tile >= t_end) return 0;
-            int slab, m0;
-            place(tile, slab, m0);
-            const int cb = 2 * slab + (int)half;
-            if (cb * BM >= p.N) return 0;
-            return __ldg(p.w_exp + (W_IS_NK ? (long long)cb * p.w_exp_stride + kb : (long long)kb * p.w_exp_stride + cb));
+        // SCALED: the exponent of the weight block of the group's next k-block, one after the other over all tiles of this CTA (0 where there is none).  (Its place worked out
+        // from the k-block's number each time took the decode warps a fifth of their instructions, 333 x 32000 x 4096 103 us, SCALED_US.)
+        int e_tile = t0, e_kb = kb0 + group;
+        bool e_there = false;
+        const int* e_row = nullptr;
+        auto block_exp = [&]() {
+            bool fresh = !e_row;
+            while (e_kb >= kb1) { e_kb -= n_kb; e_tile += t_step; fresh = true; }
+            if (e_tile >= t_end) return 0;
+            if (fresh) {
+                int slab, m0;
+                place(e_tile, slab, m0);
+                const int cb = 2 * slab + (int)half;
+                e_row = p.w_exp + (W_IS_NK ? (long long)cb * p.w_exp_stride : cb);
+                e_there = cb * BM < p.N;
+            }
+            const int e = e_there ? __ldg(e_row + (W_IS_NK ? e_kb : (long long)e_kb * p.w_exp_stride)) : 0;
+            e_kb += kDecodeGroups;
+            return e;
         };
         int e_next = 0;
-        if (SCALED && decodes) e_next = block_exp(it);
+        if (SCALED && decodes) e_next = block_exp();
         for (int t = t0; t < t_end;) {
             // the group's k-blocks of this tile, and one of the next
             const int n_it_known = t + t_step < t_end ? tile_it + 2 * n_kb : tile_it + n_kb;
@@ -1607,7 +1617,7 @@ hif8_gemm_weights_kernel(const __grid_constant__ CUtensorMap map_w, const __grid
                 if (ok && r > 0) ok = mbar_wait(bar_bf_empty(s), (r - 1) & 1, abort_flag, p.status, 44);
                 if (!ok) { it += kGaveUp; continue; }  // (no further k-block: gives up at the next wait)
                 const uint32_t scale2 = SCALED ? block_scale2(e_next) : 0u;
-                if (SCALED) e_next = block_exp(it + kDecodeGroups);  // (the next one, on its way while this k-block is decoded)
+                if (SCALED) e_next = block_exp();  // (the next one, on its way while this k-block is decoded)
                 const uint32_t w8 = lay.u8(s), dst = tlane + (uint32_t)(s * (KB / 2));
                 if (ACT != kActExpanded) {
                     // activations as bytes: the tile's 8-byte chunks, up to eight per thread (it lies in a row, [M,K] or [K,M]), two at a time and in
@@ -2576,7 +2586,7 @@ static int launch_weights_gemm(const uint8_t* Wq, int64_t ldw, int w_is_nk, cons
     for (int i = 0; i < (rem ? 2 : 1); i++) {
         const TilePlan& tp = launch[i];
         CUtensorMap map_act;
-        const bool oka = act == kActExpanded ? make_map3(&map_act, a, (uint64_t)K, (uint64_t)M, 1, 0, BK, (uint32_t)tp.bn / 2)
+        const bool oka = act == kActExpanded ? make_map3(&map_act, a, (uint64_t)K, (uint64_t)M, 1, 0, BK, (uint32_t)tp.bn / 2, (uint64_t)lda)
                          : act == kActRows   ? make_map(&map_act, a, (uint64_t)K, (uint64_t)M, (uint64_t)lda, BK, (uint32_t)tp.bn / 2)
                                              : make_map(&map_act, a, (uint64_t)M, (uint64_t)K, (uint64_t)lda, (uint32_t)tp.bn / 2, BK);
         if (!oka) return HIF8_ERR_CUDA;
@@ -2954,7 +2964,7 @@ static int gemm_entry(const uint8_t* Aq, int64_t lda, int a_is_km, const uint8_t
     return rc != HIF8_OK ? rc : launch_bf16_pair_gemm(a_bf, w_bf, w_is_nk, p, st);
 }
 
-// Which kernel takes a block-scaled product whose weights have a scale for each 128 x 128 (K a multiple of 16): as for hif8_gemm, by the same costs.  room: the workspace has
+// Which kernel takes a block-scaled product whose weights have a scale for each 128 x 128: as for hif8_gemm, by the same costs.  room: the workspace has
 // room to expand the weights.
 struct BlockKey {
     int M, N, K, dev, a_is_km, w_is_nk, policy, pad;
@@ -2982,11 +2992,11 @@ static void choose_block(const BlockKey& k, int sm_count, const int* wd_clusters
         other = out->weights.cycles;
     } else other = NarrowTiling(k.M, k.N, k.K, sm_count, nw_clusters, true).cycles + 6000.0;
     if (k.a_is_km || (k.policy != HIF8_GEMM_PATH_AUTO && k.policy != HIF8_GEMM_PATH_WARP)) return;
-    out->warp = WarpTiling(k.M, k.N, k.K, k.w_is_nk, false, wp_clusters, k.policy == HIF8_GEMM_PATH_WARP ? 1e30 : other / 1.2);
+    out->warp = WarpTiling(k.M, k.N, k.K, k.w_is_nk, false, wp_clusters, k.policy == HIF8_GEMM_PATH_WARP ? 1e30 : other / 1.35);  // (scales cost it more than the others)
     if (out->warp.mt > 0) out->form = kFormWarp;
 }
 
-// Block-scaled operands.  Where the weights have a scale for each 128 x 128 and K is a multiple of 16 they are decoded in the kernel: few rows and a small weight by the warp
+// Block-scaled operands.  Where the weights have a scale for each 128 x 128 they are decoded in the kernel: few rows and a small weight by the warp
 // kernel, which takes the activations' codes too; the others have the activations expanded to BF16 with their scales in front, up to 64 rows for the narrow kernel, beyond
 // for the weights kernel, until expanding the weights pays.  Other weights (a gradient's activations, with a scale for each 1 x 128) are expanded whatever the size.
 int hif8::launch_block_gemm(const BlockCodes& a, bool a_is_km, const BlockCodes& w, bool w_is_nk, const GemmParams& params, const BlockWorkspace& sizes, void* workspace, cudaStream_t st)
@@ -3046,7 +3056,7 @@ int hif8::launch_block_gemm(const BlockCodes& a, bool a_is_km, const BlockCodes&
         }
         if (choice.form == kFormWeights) {
             if (int rc = expand_a(4)) return rc;
-            return launch_weights_gemm(w.codes, w.ld, w_is_nk, choice.weights, a_bf, K, p, wd_clusters, st);
+            return launch_weights_gemm(w.codes, w.ld, w_is_nk, choice.weights, a_bf, sizes.a_pitch, p, wd_clusters, st);
         }
         p.w_exp = nullptr;
     }

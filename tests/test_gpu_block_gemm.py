@@ -66,6 +66,19 @@ def test_forward_sizes(M, N, K, c_dtype, w_is_nk, path):
         check(M, N, K, w_is_nk=w_is_nk, c_dtype=c_dtype, seed=M + N + K)
 
 
+@pytest.mark.parametrize("K", list(range(241, 257)) + list(range(17, 32)))
+@pytest.mark.parametrize("w_is_nk", [0, 1])
+def test_sums_end_anywhere(K, w_is_nk):
+    """What lies behind the last k of a row (codes of NaN here) is not part of the sum, in any kernel."""
+    for path in (H.GEMM_PATH_WARP, H.GEMM_PATH_NO_WARP):
+        with gemm_path(path):
+            check(5, 132, K, w_is_nk=w_is_nk, seed=K)
+            check(40, 264, K, w_is_nk=w_is_nk, seed=K)
+            check(100, 132, K, w_is_nk=w_is_nk, seed=K)
+    with gemm_path(H.GEMM_PATH_EXPAND_BOTH):
+        check(520, 132, K, w_is_nk=w_is_nk, seed=K)
+
+
 @pytest.mark.parametrize("accumulate", [0, 1])
 @pytest.mark.parametrize("c_dtype", [H.F32, H.BF16])
 @pytest.mark.parametrize("a_is_km", [0, 1])

@@ -25,7 +25,7 @@ class Layer:
         self.q, self.e = new(T, 272, t=torch.uint8), new(T, 3, t=torch.int32)
         self.wq, self.we = new(F, 272, t=torch.uint8), new(5, 3, t=torch.int32)
         self.dq, self.de = new(T, 528, t=torch.uint8), new(T, 5, t=torch.int32)
-        size = max(H.hif8_gemm_block_workspace_bytes(T, F, D, 0, 1, 128), H.hif8_gemm_block_workspace_bytes(T, D, F, 0, 0, 128), H.hif8_gemm_block_workspace_bytes(F, D, T, 1, 0, 1))
+        size = max(H.hif8_gemm_block_workspace_bytes(1, F, D, 0, 1, 128), H.hif8_gemm_block_workspace_bytes(T, F, D, 0, 1, 128), H.hif8_gemm_block_workspace_bytes(T, D, F, 0, 0, 128), H.hif8_gemm_block_workspace_bytes(F, D, T, 1, 0, 1))
         self.ws = torch.empty(size, dtype=torch.uint8, device="cuda")
         self.nws = torch.empty(H.hif8_rmsnorm_backward_workspace_bytes(T, D), dtype=torch.uint8, device="cuda")
         self.cws = torch.empty(H.hif8_grad_clip_workspace_bytes(), dtype=torch.uint8, device="cuda")
