@@ -334,6 +334,7 @@ int hif8_gemm_status(const void* workspace, hif8_stream_t stream);
  *   HIF8_GEMM_PATH_NO_WARP      as AUTO, without the kernel for few rows and a small weight (nor do the two above take it)
  *   HIF8_GEMM_PATH_WARP         that kernel; HIF8_ERR_SHAPE for a product that it cannot take (K too long for its registers, far
  *                               too large a product, [K,N] weights with N no multiple of four)
+ * Products of block-scaled operands (hif8_gemm_block) go by the same setting where the kernel can take them and the workspace has room, and are not refused otherwise.
  * Up to 64 rows of A given as [M,K] take the weight-streaming kernel under the first three.  Process-wide; returns the
  * previous setting, or HIF8_ERR_FLAGS (4, which is no setting) for an unknown one.  What it computes does not depend on it,
  * only the order of the FP32 sums does.

@@ -5,8 +5,8 @@
 // Two launches: sums of squares, a share of the list to a block, and the scaling, in front of which every block adds the shares up in the same order. Both are bound by
 // memory.  A share is a stretch of the list of all elements, in which each tensor takes kTensorCost places more than it has elements, for what it costs to come to one: so
 // neither many small tensors nor few large ones leave blocks idle.  A block fetches the descriptors of its tensors together, works on long pieces with all threads and on short ones
-// with a warp each.  (Tensors one after the other, each with its descriptor's latency: 3000 tensors of 10 elements 362 us, CLIP_MANY_US; 2.7 M elements in 28 matrices and 9 vectors
-// 21.5 us, CLIP_SMALL_US.)  Squares are added in FP32 over 16 bytes and in FP64 from there on (vectors whose sum leaves FP32's comfortable range: in FP64 altogether), so the
+// with a warp each.  (Tensors one after the other, each with its descriptor's latency: 3000 tensors of 10 elements 362 us, 11.4; 2.7 M elements in 28 matrices and 9 vectors
+// 21.5 us, 14.2.)  Squares are added in FP32 over 16 bytes and in FP64 from there on (vectors whose sum leaves FP32's comfortable range: in FP64 altogether), so the
 // norm is as exact as FP32 can say, and the squares of finite gradients do not overflow.
 #include "hif8_block.cuh"
 

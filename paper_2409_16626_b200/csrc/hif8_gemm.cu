@@ -1587,7 +1587,7 @@ hif8_gemm_weights_kernel(const __grid_constant__ CUtensorMap map_w, const __grid
         int it = decodes ? group : kGaveUp, tile_it = 0, local = 0;  // next k-block of the group; first k-block of the tile to finish next
         bool joined = !decodes;
         // SCALED: the exponent of the weight block of the group's next k-block, one after the other over all tiles of this CTA (0 where there is none).  (Its place worked out
-        // from the k-block's number each time took the decode warps a fifth of their instructions, 333 x 32000 x 4096 103 us, SCALED_US.)
+        // from the k-block's number each time cost 333 x 4096 x 4096 20.9 us, so 20.0.)
         int e_tile = t0, e_kb = kb0 + group;
         bool e_there = false;
         const int* e_row = nullptr;

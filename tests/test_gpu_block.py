@@ -124,3 +124,19 @@ def test_on_another_stream_and_in_a_graph():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(q[:, :500], want[:, :500]) and torch.equal(e, we) and torch.equal(back, first)
+
+
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_rows_far_apart(block_rows):
+    """Offsets beyond 32 bits: 2^31 elements of the source, 2^32 bytes of codes and 2^30 exponents between rows."""
+    x = matrix(3, 200, H.BF16, 17)
+    src = torch.zeros(2 * 2 ** 31 + 200, dtype=torch.bfloat16, device="cuda")
+    torch.as_strided(src, (3, 200), (2 ** 31, 1)).copy_(x)
+    q, e = torch.zeros(2 * 2 ** 32 + 200, dtype=torch.uint8, device="cuda"), torch.zeros(2 * 2 ** 30 + 2, dtype=torch.int32, device="cuda")
+    H.hif8_block_encode(src, H.BF16, 2 ** 31, 3, 200, block_rows, q, 2 ** 32, e, 2 ** 30)
+    codes, exps = B.encode(x, H.BF16, block_rows)
+    down = exps.shape[0]
+    assert np.array_equal(torch.as_strided(q, (3, 200), (2 ** 32, 1)).cpu().numpy(), codes) and np.array_equal(torch.as_strided(e, (down, 2), (2 ** 30, 1)).cpu().numpy(), exps)
+    src.zero_()
+    H.hif8_block_decode(q, 2 ** 32, e, 2 ** 30, 3, 200, block_rows, src, H.BF16, 2 ** 31)
+    assert torch.equal(torch.as_strided(src, (3, 200), (2 ** 31, 1)).cpu(), torch.from_numpy(B.meant(codes, exps, block_rows)).bfloat16())

@@ -174,3 +174,24 @@ def test_captured(M):
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(C, want)
+
+
+def test_rows_far_apart():
+    """Offsets beyond 32 bits: rows of codes 2^31 bytes apart, rows of C 2^32 bytes."""
+    for M, N, K in ((3, 40, 256), (2, 300, 512)):
+        a, ae, av = operand(M, K, 1, 51)
+        w, we, wv = operand(N, K, 128, 52)
+        far = torch.zeros((M - 1) * 2 ** 31 + K, dtype=torch.uint8, device="cuda")
+        fa = torch.as_strided(far, (M, K), (2 ** 31, 1))
+        fa.copy_(a)
+        out = torch.zeros((M - 1) * 2 ** 30 + N, device="cuda")
+        n = H.hif8_gemm_block_workspace_bytes(M, N, K, 0, 1, 128)
+        ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+        for path in (H.GEMM_PATH_WARP, H.GEMM_PATH_NO_WARP):
+            out.fill_(7)
+            with gemm_path(path):
+                H.hif8_gemm_block(fa, 2 ** 31, 0, ae, ae.stride(0), 1, w, w.stride(0), 1, we, we.stride(0), 128, out, 2 ** 30, H.F32, M, N, K, 0, ws, n)
+            C = torch.as_strided(out, (M, N), (2 ** 30, 1))
+            assert np.all(np.abs(C.cpu().double().numpy() - av @ wv.T) <= bound(K) * (np.abs(av) @ np.abs(wv.T)))
+            assert float(out[N]) == 7 and float(out[2 ** 30 - 1]) == 7
+        del far, out

@@ -215,3 +215,45 @@ def test_results_are_reproducible():
     r = B.norm(h, None, w, EPS, H.BF16)[1].astype(np.float32)
     a, b = gradient(dy, h, None, w, r, H.BF16), gradient(dy, h, None, w, r, H.BF16)
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_rows_far_apart():
+    """Offsets beyond 32 bits: rows 2^31 elements apart."""
+    x, r, w = inputs(2, 300, H.BF16, 51)
+    far = [torch.zeros(2 ** 31 + 300, dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+    rows = [torch.as_strided(t, (2, 300), (2 ** 31, 1)) for t in far]
+    rows[0].copy_(x)
+    rows[1].copy_(r)
+    q, e, rstd = torch.zeros(2 ** 32 + 300, dtype=torch.uint8, device="cuda"), torch.zeros(2, 3, dtype=torch.int32, device="cuda"), torch.zeros(2, device="cuda")
+    H.hif8_rmsnorm_encode(far[0], 2 ** 31, far[1], 2 ** 31, H.BF16, w.cuda(), EPS, 2, 300, far[2], 2 ** 31, rstd, q, 2 ** 32, e, 3)
+    h, r1, codes, exps = call(x, r, w, H.BF16)
+    assert torch.equal(rows[2].cpu(), h) and np.array_equal(torch.as_strided(q, (2, 300), (2 ** 32, 1)).cpu().numpy(), codes) and np.array_equal(e.cpu().numpy(), exps)
+    want = gradient(x, h, r, w, r1, H.BF16)[0]
+    H.hif8_rmsnorm_backward(far[0], 2 ** 31, far[2], 2 ** 31, far[1], 2 ** 31, H.BF16, w.cuda(), rstd, 2, 300, far[0], 2 ** 31)
+    assert torch.equal(rows[0].cpu(), want)
+
+
+def test_streams_and_graphs():
+    h, dy, w = inputs(200, 1000, H.F16, 61)
+    r = B.norm(h, None, w, EPS, H.F16)[1].astype(np.float32)
+    want, wdw = gradient(dy, h, None, w, r, H.F16)
+    n = H.hif8_rmsnorm_backward_workspace_bytes(200, 1000)
+    d = [t.cuda() for t in (dy, h, w, torch.from_numpy(r))]
+    made = [(torch.zeros(200, 1000, dtype=torch.float16, device="cuda"), torch.zeros(1000, device="cuda"), torch.empty(n, dtype=torch.uint8, device="cuda")) for _ in range(3)]
+    torch.cuda.synchronize()
+
+    def run(i, stream=None):
+        dx, dw, ws = made[i]
+        H.hif8_rmsnorm_backward(d[0], 1000, d[1], 1000, None, 0, H.F16, d[2], d[3], 200, 1000, dx, 1000, dw, 0, ws, n, stream)
+
+    for i in range(2):                                       # two streams at once, a workspace each
+        run(i, torch.cuda.Stream())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(2)
+    made[2][2].fill_(0xFF)
+    graph.replay()
+    torch.cuda.synchronize()
+    for dx, dw, _ in made:
+        assert torch.equal(dx.cpu(), want) and torch.equal(dw.cpu(), wdw)
