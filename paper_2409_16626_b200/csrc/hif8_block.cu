@@ -340,6 +340,42 @@ __global__ void __launch_bounds__(kThreads) block_decode_transpose_kernel(const 
 }
 
 // ------------------------------------------------------------------------------------------------
+// parts of a product's sum
+// ------------------------------------------------------------------------------------------------
+// C (+)= the parts, added in their order: a thread has four columns of a row, every part's on its way before the first is added
+template <bool F32>
+__global__ void __launch_bounds__(kThreads) add_parts_kernel(const float4* __restrict__ parts, int n, long long part4, unsigned units, FastDiv quads, void* C, long long ldc, int N,
+                                                             int accumulate)
+{
+    pdl_wait_prior_grid();
+    pdl_launch_dependents();
+    const unsigned u = blockIdx.x * kThreads + threadIdx.x;
+    if (u >= units) return;
+    const unsigned row = quads.div(u), c = (u - row * quads.d) * 4u;  // (quads: groups of four columns of a part's row)
+    float4 v[BlockWorkspace::kMaxSplit];
+#pragma unroll
+    for (int i = 0; i < BlockWorkspace::kMaxSplit; i++)
+        if (i < n) v[i] = __ldcs(parts + (size_t)i * (size_t)part4 + u);
+    float x[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+#pragma unroll
+    for (int i = 1; i < BlockWorkspace::kMaxSplit; i++)
+        if (i < n) { x[0] += v[i].x; x[1] += v[i].y; x[2] += v[i].z; x[3] += v[i].w; }
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        if ((int)c + i >= N) continue;
+        const long long at = (long long)row * ldc + c + i;
+        if (F32) {
+            float* out = reinterpret_cast<float*>(C) + at;
+            *out = accumulate ? *out + x[i] : x[i];
+        } else {
+            unsigned short* out = reinterpret_cast<unsigned short*>(C) + at;
+            const float y = accumulate ? __uint_as_float((uint32_t)*out << 16) + x[i] : x[i];
+            *out = __bfloat16_as_ushort(__float2bfloat16_rn(y));
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
 // host side
 // ------------------------------------------------------------------------------------------------
 int finish(int launches)
@@ -419,6 +455,18 @@ int expand_block_codes(const BlockOperand& a, const BlockOperand* w, uint32_t* c
         one.m[0] = two.m[0];
         launch_decode<HIF8_BF16, false>(one, sms, st);
     }
+    return finish(1);
+}
+
+int add_product_parts(const float* parts, int n, long long rows, long long cols, const GemmParams& p, cudaStream_t st)
+{
+    const long long units = (long long)p.M * (cols / 4);  // (rows of a part in front of the padding ones)
+    if (n > BlockWorkspace::kMaxSplit || units > 0x7FFFFFFFll) return HIF8_ERR_SHAPE;
+    const FastDiv quads((uint32_t)(cols / 4));
+    const dim3 grid((unsigned)((units + kThreads - 1) / kThreads));
+    const float4* from = reinterpret_cast<const float4*>(parts);
+    if (p.c_is_f32) launch_pdl(add_parts_kernel<true>, grid, st, from, n, rows * cols / 4, (unsigned)units, quads, p.C, p.ldc, p.N, p.accumulate);
+    else launch_pdl(add_parts_kernel<false>, grid, st, from, n, rows * cols / 4, (unsigned)units, quads, p.C, p.ldc, p.N, p.accumulate);
     return finish(1);
 }
 

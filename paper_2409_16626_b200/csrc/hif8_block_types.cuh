@@ -27,36 +27,65 @@ struct BlockCodes {
     size_t exp_bytes() const { return rows > 0 ? ((size_t)(blocks_down() - 1) * (size_t)exp_stride + (size_t)blocks_across()) * sizeof(int) : 0; }
 };
 
-// What the workspace of a block-scaled product holds behind the status word: the activations as BF16, and either the weights as BF16 too, or the narrow kernel's
-// tickets and partial sums.  (Sizes follow from the arguments alone, so that they can be asked for without a device.)
+// What the workspace of a block-scaled product holds behind the status word: the activations as BF16, and either the weights as BF16 too and the parts of a divided sum, or
+// the narrow kernel's tickets and partial sums.  (Sizes follow from the arguments alone, so that they can be asked for without a device.)
 struct BlockWorkspace {
     static constexpr size_t kStatus = 256;
     static constexpr int kNarrowRows = 64;   // up to so many rows the weight-streaming kernel takes the product
     static constexpr int kExpandRows = 512;  // from so many on there is room to expand the weights too
+    static constexpr int kPairs = 74, kMaxSplit = 16;
     long long a_pitch, a_pitch_km, w_pitch;  // elements between rows of the BF16 copies (of A as [M,K], as [K,M])
-    size_t a_bytes, w_bytes, narrow_bytes;   // w_bytes, narrow_bytes: 0 where there is none
-    bool in_kernel;                          // the weights' layout lets the kernels that decode weights take the product
+    size_t a_bytes, w_bytes, narrow_bytes, part_bytes;   // 0 where there is none
+    bool in_kernel;                          // the weights' blocks let the kernels that decode weights take the product
+    int split;                               // parts of the sum, 1: not divided
+    long long w_rows;                        // of the weights' copy
+    long long part_k, part_rows, part_cols;  // of a part: its k (the operands' copies end with zeros), rows and columns of its FP32 result; 0 if there is one
     BlockWorkspace(int M, int N, int K, bool a_is_km, bool w_is_nk, int w_block_rows)
     {
         auto pad8 = [](long long n) { return (n + 7) & ~7ll; };
         auto pad256 = [](size_t n) { return (n + 255) & ~(size_t)255; };
         in_kernel = w_block_rows == HIF8_BLOCK;
-        a_pitch = pad8(K);
+        split = 1;
+        part_k = part_rows = part_cols = 0;
+        part_bytes = 0;
+        if (!in_kernel) {
+            // Cycles of the pair kernel's 64 k, of the parts written and read again and of the launch that adds them (gradients of 192 x 512 over 2810 rows 22.6 us, so 13.1; 256 x 256 over 8192 47.6 and 15.9).
+            const long long tiles = (long long)((M + 255) / 256) * ((N + 255) / 256), kb = (K + 63) / 64;
+            const double part = 8.0 * (double)M * (double)N / 2500.0;
+            double least = 545.0 * (double)kb;
+            for (int s = 2; s <= kMaxSplit && tiles * s <= kPairs && kb / s >= 2; s++) {
+                const double t = 545.0 * (double)((kb + s - 1) / s) + part * s + 5000.0;
+                if (t < least) { least = t; split = s; }
+            }
+            if (split > 1) {
+                part_k = (kb + split - 1) / split * 64;
+                split = (int)((kb * 64 + part_k - 1) / part_k);
+                part_rows = (M + 31) & ~31ll;
+                part_cols = pad8(N);
+                part_bytes = pad256((size_t)split * (size_t)part_rows * (size_t)part_cols * 4);
+            }
+        }
+        const long long k_rows = split > 1 ? part_k * split : K;  // of what is stored with k as rows; and its row length otherwise
+        a_pitch = pad8(k_rows);
         a_pitch_km = pad8(M);
-        w_pitch = pad8(w_is_nk ? K : N);
+        w_pitch = pad8(w_is_nk ? k_rows : N);
         a_bytes = pad256((size_t)M * (size_t)a_pitch * 2);
-        if (a_is_km && (size_t)K * (size_t)a_pitch_km * 2 > a_bytes) a_bytes = pad256((size_t)K * (size_t)a_pitch_km * 2);
+        if (a_is_km && (size_t)k_rows * (size_t)a_pitch_km * 2 > a_bytes) a_bytes = pad256((size_t)k_rows * (size_t)a_pitch_km * 2);
         const bool narrow = in_kernel && M <= kNarrowRows;
-        w_bytes = in_kernel && M < kExpandRows ? 0 : pad256((size_t)(w_is_nk ? N : K) * (size_t)w_pitch * 2);
+        w_rows = !w_is_nk ? k_rows : split > 1 ? part_cols : N;
+        w_bytes = in_kernel && M < kExpandRows ? 0 : pad256((size_t)w_rows * (size_t)w_pitch * 2);
         // partial sums of 128 columns by the rows: a slice for each block of up to 160 and two more for each slab, which two blocks may share
         const size_t slabs = ((size_t)N + 127) / 128;
         narrow_bytes = narrow ? pad256(slabs * 16) + (160 + 3 * slabs) * (size_t)((M + 15) & ~15) * 512 : 0;
     }
-    size_t bytes() const { return kStatus + a_bytes + w_bytes + narrow_bytes; }
+    size_t bytes() const { return kStatus + a_bytes + w_bytes + narrow_bytes + part_bytes; }
 };
 
-// C of `p` from block-scaled operands, the rest of `p` filled in here; the arguments have been checked.
+// C of `p` (+)= the sum of n FP32 matrices of `rows` x `cols` in a row, in their order
 struct GemmParams;
+int add_product_parts(const float* parts, int n, long long rows, long long cols, const GemmParams& p, cudaStream_t st);
+
+// C of `p` from block-scaled operands, the rest of `p` filled in here; the arguments have been checked.
 int launch_block_gemm(const BlockCodes& a, bool a_is_km, const BlockCodes& w, bool w_is_nk, const GemmParams& p, const BlockWorkspace& sizes, void* workspace, cudaStream_t st);
 
 // A product's operand to be decoded into BF16 with its blocks' scales (exact: four significant bits, exponents within -118 .. 111):

@@ -1838,7 +1838,9 @@ static_assert(kSmemBytes2 <= 227 * 1024, "shared memory of one CTA");
 // RAGGED: rows of C end inside 16 bytes.  A tile store clips at the end of the tensor map's rows in whole 16-byte pieces only, so the map ends in front of the
 // last one and the warp writes what is left itself.
 // A_IS_KM: A as [K,M], its tiles two boxes of 64 columns like those of W as [K,N].
-template <bool W_IS_NK, bool RAGGED, bool A_IS_KM>
+// SPLIT: few tiles with a long sum: p.split parts of it as products of their own, which a launch behind this one adds up.
+enum PairForm { kPairPlain, kPairRagged, kPairSplit };
+template <bool W_IS_NK, int FORM, bool A_IS_KM>
 __global__ void __launch_bounds__(kThreadsP, 1)
 bf16_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_c,
                       const GemmParams p)
@@ -1857,6 +1859,7 @@ bf16_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
     auto bar_old = [&](int i) { return bars + 8u * (2 * kStages2 + 4 + i); };        // per epilogue warp and staging piece
     volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + SmemLayout2::abort_flag);
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sm + SmemLayout2::tmem_slot);
+    constexpr bool RAGGED = FORM == kPairRagged, SPLIT = FORM == kPairSplit;
     const int num_kb = (p.K + BK - 1) / BK;
     // Up to K = 4096 the A tiles of sixteen tile-rows (32 MiB) stay in L2 beside the W tiles, and W is read half as often; beyond, those of eight (8192 x 28672
     // x 8192 in a sequence of calls 2600 us, with sixteen 2655, with four 2676; x 4096 1255 and with sixteen 1240; 3000 x 11008 x 4096 203.5 and 197.9).
@@ -1865,7 +1868,7 @@ bf16_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
     // a batch of n x n products (A variant ia, W variant iw) is one list of tiles: product b = ia * n + iw owns tiles
     // [b * tiles_one, (b + 1) * tiles_one)
     const int tiles_one = tiles_m2 * tiles_n2, nb = p.batch_n > 0 ? p.batch_n : 1;
-    const int tiles = tiles_one * nb * nb, pairs = gridDim.x >> 1, pair_id = blockIdx.x >> 1;
+    const int tiles = SPLIT ? tiles_one * p.split : tiles_one * nb * nb, pairs = gridDim.x >> 1, pair_id = blockIdx.x >> 1;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages2; s++) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); }
@@ -1913,7 +1916,7 @@ bf16_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
             bool ok = true, wrapped = false;
             for (int t = pair_id; t < tiles && ok; t += pairs) {
                 int tile_m, tile_n;
-                const int b = t / tiles_one, ia = b / nb, iw = b - ia * nb;
+                const int b = t / tiles_one, ia = SPLIT ? b : b / nb, iw = SPLIT ? b : b - ia * nb;
                 tile_coords(t - b * tiles_one, tiles_m2, tiles_n2, tile_m, tile_n, group);
                 const int m0 = tile_m * 2 * BM + (int)rank * BM, n0 = tile_n * BN + (int)rank * (BN / 2);
                 for (int kb = 0; kb < num_kb; kb++) {
@@ -1975,7 +1978,7 @@ bf16_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
         for (int t = pair_id; t < tiles; t += pairs, local++) {
             const int acc = local & 1, use = local >> 1;
             int tile_m, tile_n;
-            const int b = t / tiles_one, ia = b / nb, iw = b - ia * nb;
+            const int b = t / tiles_one, ia = SPLIT ? b : b / nb, iw = SPLIT ? b : b - ia * nb;
             tile_coords(t - b * tiles_one, tiles_m2, tiles_n2, tile_m, tile_n, group);
             const int row0 = tile_m * 2 * BM + (int)rank * BM + warp * 32, row = row0 + lane, n0 = tile_n * BN;
             const int pieces = p.c_by_tma && row0 < p.M ? (min(BN, p.N - n0) + piece_cols - 1) / piece_cols : 0;
@@ -2045,7 +2048,7 @@ bf16_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) {
-                    tma_store_2d(&map_c, buf, n0 + i * piece_cols, row0);
+                    tma_store_2d(&map_c, buf, n0 + i * piece_cols, SPLIT ? row0 + b * p.part_rows : row0);
                     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     if (p.accumulate && i + 2 < mapped) {
                         asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
@@ -2119,9 +2122,9 @@ bf16_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
 #pragma unroll 1
                 for (int i = progress; i < top; i++) {
                     int tile_m, tile_n;
-                    const int t = pair_id + i / num_kb * pairs, b = t / tiles_one, ia = b / nb;
+                    const int t = pair_id + i / num_kb * pairs, b = t / tiles_one, ia = SPLIT ? b : b / nb;
                     tile_coords(t - b * tiles_one, tiles_m2, tiles_n2, tile_m, tile_n, group);
-                    copy_block(tile_m * 2 * BM + (int)rank * BM, tile_n * BN + (int)rank * (BN / 2), ia, b - ia * nb, i % num_kb, i % kStages2);
+                    copy_block(tile_m * 2 * BM + (int)rank * BM, tile_n * BN + (int)rank * (BN / 2), ia, SPLIT ? b : b - ia * nb, i % num_kb, i % kStages2);
                 }
                 if (leader && loads_a)
                     for (int i = max(0, top - kStages2); i < top; i++) wait_landed(bar_full(i % kStages2), i, kStages2);
@@ -2300,10 +2303,17 @@ void weights_kernels(const void** k)
     k[6] = (const void*)hif8_gemm_weights_kernel<false, kActExpanded, FORM, true>; k[7] = (const void*)hif8_gemm_weights_kernel<true, kActExpanded, FORM, true>;
 }
 
-template <bool RAGGED, bool A_IS_KM>
+// [A as [K,M]][form][W as [N,K]]
+constexpr int kPairKernels = 12;
+template <bool A_IS_KM, int FORM>
+void pair_kernels_of(const void** k)
+{
+    k[0] = (const void*)bf16_gemm_pair_kernel<false, FORM, A_IS_KM>; k[1] = (const void*)bf16_gemm_pair_kernel<true, FORM, A_IS_KM>;
+}
 void pair_kernels(const void** k)
 {
-    k[0] = (const void*)bf16_gemm_pair_kernel<false, RAGGED, A_IS_KM>; k[1] = (const void*)bf16_gemm_pair_kernel<true, RAGGED, A_IS_KM>;
+    pair_kernels_of<false, kPairPlain>(k); pair_kernels_of<false, kPairRagged>(k + 2); pair_kernels_of<false, kPairSplit>(k + 4);
+    pair_kernels_of<true, kPairPlain>(k + 6); pair_kernels_of<true, kPairRagged>(k + 8); pair_kernels_of<true, kPairSplit>(k + 10);
 }
 
 template <int MT>
@@ -2320,11 +2330,11 @@ bool gemm_kernels_ready(int dev, int* sm_count_out, const int** wd_clusters = nu
         out->sm_count = 0;
         std::memset(out->wd_clusters, 0, sizeof out->wd_clusters);
         std::memset(out->nw_clusters, 0, sizeof out->nw_clusters);
-        const void* pair[8];
-        pair_kernels<false, false>(pair); pair_kernels<true, false>(pair + 2); pair_kernels<false, true>(pair + 4); pair_kernels<true, true>(pair + 6);
+        const void* pair[kPairKernels];
+        pair_kernels(pair);
         const void* wd[32];
         weights_kernels<kOneGroup>(wd); weights_kernels<kGroups>(wd + 8); weights_kernels<kFarRows>(wd + 16); weights_kernels<kParts>(wd + 24);
-        for (int i = 0; i < 8 && out->rc == cudaSuccess; i++)
+        for (int i = 0; i < kPairKernels && out->rc == cudaSuccess; i++)
             out->rc = cudaFuncSetAttribute(pair[i], cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes2);
         for (int i = 0; i < 32 && out->rc == cudaSuccess; i++)
             out->rc = cudaFuncSetAttribute(wd[i], cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytesMax);
@@ -2405,10 +2415,10 @@ int launch_bf16_pair_gemm(const void* a_bf, const void* w_bf, int w_is_nk, GemmP
     int dev = 0, sm_count = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || !gemm_kernels_ready(dev, &sm_count)) return HIF8_ERR_CUDA;
     const int M = p.M, N = p.N, K = p.K;
-    const uint64_t nb = p.batch_n > 0 ? (uint64_t)p.batch_n : 1;
+    const uint64_t nb = p.split > 1 ? (uint64_t)p.split : p.batch_n > 0 ? (uint64_t)p.batch_n : 1;  // operands in a stack
     p.tiles_m = (M + BM - 1) / BM;
     p.tiles_n = (N + BN - 1) / BN;
-    const long long tiles2 = (long long)((M + 2 * BM - 1) / (2 * BM)) * p.tiles_n * (long long)(nb * nb);
+    const long long tiles2 = (long long)((M + 2 * BM - 1) / (2 * BM)) * p.tiles_n * (long long)(p.split > 1 ? nb : nb * nb);
     if (M <= 0 || N <= 0 || K <= 0 || tiles2 > 0x3FFFFFFF) return HIF8_ERR_SHAPE;
     if (nb > 1 && ((a_stack_stride & 7) || (w_stack_stride & 7))) return HIF8_ERR_ALIGN;  // 16-byte strides
     CUtensorMap ma, mw;
@@ -2426,7 +2436,7 @@ int launch_bf16_pair_gemm(const void* a_bf, const void* w_bf, int w_is_nk, GemmP
     const int whole = p.c_is_f32 ? N & ~3 : N & ~7;
     const bool ragged = p.c_by_tma && whole != N;
     if (p.c_by_tma && whole > 0) {
-        const bool okc = p.c_is_f32 ? make_map_f32(&mc, p.C, (uint64_t)whole, (uint64_t)M, (uint64_t)p.ldc, 32)
+        const bool okc = p.c_is_f32 ? make_map_f32(&mc, p.C, (uint64_t)whole, (uint64_t)(p.split > 1 ? p.split * (long long)p.part_rows : M), (uint64_t)p.ldc, 32)
                                     : make_map(&mc, p.C, (uint64_t)whole, (uint64_t)M, (uint64_t)p.ldc, 64, 32, true);
         if (!okc) return HIF8_ERR_CUDA;
     }
@@ -2442,10 +2452,11 @@ int launch_bf16_pair_gemm(const void* a_bf, const void* w_bf, int w_is_nk, GemmP
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr; cfg.numAttrs = 2;
-    const void* kernel[8];
-    pair_kernels<false, false>(kernel); pair_kernels<true, false>(kernel + 2); pair_kernels<false, true>(kernel + 4); pair_kernels<true, true>(kernel + 6);
+    const void* kernel[kPairKernels];
+    pair_kernels(kernel);
     void* args[] = {&ma, &mw, &mc, &p};
-    const cudaError_t lrc = cudaLaunchKernelExC(&cfg, kernel[(a_is_km ? 4 : 0) + (ragged ? 2 : 0) + (w_is_nk ? 1 : 0)], args);
+    const int form = p.split > 1 ? kPairSplit : ragged ? kPairRagged : kPairPlain;
+    const cudaError_t lrc = cudaLaunchKernelExC(&cfg, kernel[(a_is_km ? 6 : 0) + 2 * form + (w_is_nk ? 1 : 0)], args);
     g_launches.fetch_add(1, std::memory_order_relaxed);
     return (lrc == cudaSuccess && cudaGetLastError() == cudaSuccess) ? HIF8_OK : HIF8_ERR_CUDA;
 }
@@ -3060,12 +3071,18 @@ int hif8::launch_block_gemm(const BlockCodes& a, bool a_is_km, const BlockCodes&
         }
         p.w_exp = nullptr;
     }
-    // both operands expanded as they are stored
+    // both operands expanded as they are stored; few tiles with a long sum in parts of it, behind which a launch adds them up
     unsigned char* w_bf = a_bf + sizes.a_bytes;
-    const long long a_pitch = a_is_km ? sizes.a_pitch_km : sizes.a_pitch;
-    const BlockOperand op_a{a, a_bf, a_pitch, a.rows, a_pitch, false}, op_w{w, w_bf, sizes.w_pitch, w.rows, sizes.w_pitch, false};
+    const long long a_pitch = a_is_km ? sizes.a_pitch_km : sizes.a_pitch, part = sizes.part_k;
+    const BlockOperand op_a{a, a_bf, a_pitch, a_is_km && part ? part * sizes.split : a.rows, a_pitch, false};
+    const BlockOperand op_w{w, w_bf, sizes.w_pitch, sizes.w_rows, sizes.w_pitch, false};
     if (int rc = expand_block_codes(op_a, &op_w, reinterpret_cast<uint32_t*>(workspace), 1, st)) return rc;
-    return launch_bf16_pair_gemm(a_bf, w_bf, w_is_nk, p, st, 0, 0, a_pitch, sizes.w_pitch, a_is_km);
+    if (sizes.split == 1) return launch_bf16_pair_gemm(a_bf, w_bf, w_is_nk, p, st, 0, 0, a_pitch, sizes.w_pitch, a_is_km);
+    GemmParams q = p;
+    float* parts = reinterpret_cast<float*>(w_bf + sizes.w_bytes);
+    q.C = parts; q.c_is_f32 = 1; q.accumulate = 0; q.N = (int)sizes.part_cols; q.ldc = sizes.part_cols; q.K = (int)part; q.split = sizes.split; q.part_rows = (int)sizes.part_rows;
+    if (int rc = launch_bf16_pair_gemm(a_bf, w_bf, w_is_nk, q, st, a_is_km ? part * a_pitch : part, w_is_nk ? part : part * sizes.w_pitch, a_pitch, sizes.w_pitch, a_is_km)) return rc;
+    return add_product_parts(parts, sizes.split, sizes.part_rows, sizes.part_cols, p, st);
 }
 
 extern "C" int hif8_gemm(const uint8_t* Aq, int64_t lda, const uint8_t* Wq, int64_t ldw, int w_is_nk, void* C, int64_t ldc,

@@ -24,6 +24,8 @@ struct GemmParams {
     // batch_n = n > 0: n x n products in one launch, A variant ia with W variant iw for product ia * n + iw; d_sa / d_sw
     // are then arrays of n exponents and err_sum an array of n * n sums
     int batch_n;
+    // split = n > 1 (pair kernel): K is a part of the sum; part i of A and of W (their stacks) goes to the rows from i * part_rows on of C, in FP32
+    int split, part_rows;
     // block-scaled weights (kernels with SCALED): the exponent of 128 k by 128 columns, [N,K] weights: [column block][k block], [K,N]: [k block][column block]
     const int* w_exp;
     long long w_exp_stride;

@@ -176,6 +176,15 @@ def test_captured(M):
     assert torch.equal(C, want)
 
 
+@pytest.mark.parametrize("M,N,K", [(192, 512, 2810), (64, 72, 5000), (300, 7, 1000), (1, 1, 4096), (257, 520, 1537), (33, 1000, 700), (1500, 700, 3000)])
+@pytest.mark.parametrize("a_is_km,w_is_nk", [(0, 0), (0, 1), (1, 0), (1, 1)])
+@pytest.mark.parametrize("c_dtype", [H.F32, H.BF16])
+@pytest.mark.parametrize("accumulate", [0, 1])
+def test_long_sums_of_few_tiles(M, N, K, a_is_km, w_is_nk, c_dtype, accumulate):
+    """Sums that are divided: parts that end with zeros, added up in order."""
+    check(M, N, K, a_is_km, 1, w_is_nk, 1, c_dtype, accumulate, seed=M)
+
+
 def test_rows_far_apart():
     """Offsets beyond 32 bits: rows of codes 2^31 bytes apart, rows of C 2^32 bytes."""
     for M, N, K in ((3, 40, 256), (2, 300, 512)):
