@@ -32,12 +32,13 @@ struct BlockCodes {
 struct BlockWorkspace {
     static constexpr size_t kStatus = 256;
     static constexpr int kNarrowRows = 64;   // up to so many rows the weight-streaming kernel takes the product
-    static constexpr int kExpandRows = 512;  // from so many on there is room to expand the weights too
+    static constexpr int kExpandRows = 512;  // from so many on there is room to expand the weights too, and where the tiles are few and the sum is long
     static constexpr int kPairs = 74, kMaxSplit = 16;
     long long a_pitch, a_pitch_km, w_pitch;  // elements between rows of the BF16 copies (of A as [M,K], as [K,M])
     size_t a_bytes, w_bytes, narrow_bytes, part_bytes;   // 0 where there is none
     bool in_kernel;                          // the weights' blocks let the kernels that decode weights take the product
     int split;                               // parts of the sum, 1: not divided
+    double cycles;                           // of a round of tiles of the pair kernel, with what joins the parts
     long long w_rows;                        // of the weights' copy
     long long part_k, part_rows, part_cols;  // of a part: its k (the operands' copies end with zeros), rows and columns of its FP32 result; 0 if there is one
     BlockWorkspace(int M, int N, int K, bool a_is_km, bool w_is_nk, int w_block_rows)
@@ -46,16 +47,18 @@ struct BlockWorkspace {
         auto pad256 = [](size_t n) { return (n + 255) & ~(size_t)255; };
         in_kernel = w_block_rows == HIF8_BLOCK;
         split = 1;
+        cycles = 0.0;
         part_k = part_rows = part_cols = 0;
         part_bytes = 0;
-        if (!in_kernel) {
+        const long long tiles = (long long)((M + 255) / 256) * ((N + 255) / 256), kb = (K + 63) / 64;
+        const bool expand = !in_kernel || M >= kExpandRows || (M > kNarrowRows && 2 * tiles <= kPairs && kb >= 16);  // room for the weights' copy
+        if (expand) {
             // Cycles of the pair kernel's 64 k, of the parts written and read again and of the launch that adds them (gradients of 192 x 512 over 2810 rows 22.6 us, so 13.1; 256 x 256 over 8192 47.6 and 15.9).
-            const long long tiles = (long long)((M + 255) / 256) * ((N + 255) / 256), kb = (K + 63) / 64;
             const double part = 8.0 * (double)M * (double)N / 2500.0;
-            double least = 545.0 * (double)kb;
+            cycles = 545.0 * (double)kb;
             for (int s = 2; s <= kMaxSplit && tiles * s <= kPairs && kb / s >= 2; s++) {
                 const double t = 545.0 * (double)((kb + s - 1) / s) + part * s + 5000.0;
-                if (t < least) { least = t; split = s; }
+                if (t < cycles) { cycles = t; split = s; }
             }
             if (split > 1) {
                 part_k = (kb + split - 1) / split * 64;
@@ -73,7 +76,7 @@ struct BlockWorkspace {
         if (a_is_km && (size_t)k_rows * (size_t)a_pitch_km * 2 > a_bytes) a_bytes = pad256((size_t)k_rows * (size_t)a_pitch_km * 2);
         const bool narrow = in_kernel && M <= kNarrowRows;
         w_rows = !w_is_nk ? k_rows : split > 1 ? part_cols : N;
-        w_bytes = in_kernel && M < kExpandRows ? 0 : pad256((size_t)w_rows * (size_t)w_pitch * 2);
+        w_bytes = !expand ? 0 : pad256((size_t)w_rows * (size_t)w_pitch * 2);
         // partial sums of 128 columns by the rows: a slice for each block of up to 160 and two more for each slab, which two blocks may share
         const size_t slabs = ((size_t)N + 127) / 128;
         narrow_bytes = narrow ? pad256(slabs * 16) + (160 + 3 * slabs) * (size_t)((M + 15) & ~15) * 512 : 0;

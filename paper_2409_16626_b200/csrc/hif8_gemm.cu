@@ -2975,8 +2975,7 @@ static int gemm_entry(const uint8_t* Aq, int64_t lda, int a_is_km, const uint8_t
     return rc != HIF8_OK ? rc : launch_bf16_pair_gemm(a_bf, w_bf, w_is_nk, p, st);
 }
 
-// Which kernel takes a block-scaled product whose weights have a scale for each 128 x 128: as for hif8_gemm, by the same costs.  room: the workspace has
-// room to expand the weights.
+// Which kernel takes a block-scaled product whose weights have a scale for each 128 x 128: as for hif8_gemm, by the same costs.
 struct BlockKey {
     int M, N, K, dev, a_is_km, w_is_nk, policy, pad;
 };
@@ -2987,7 +2986,7 @@ struct BlockChoice {
 };
 static LruCache<BlockKey, BlockChoice, 64> g_block_choices;
 
-static void choose_block(const BlockKey& k, int sm_count, const int* wd_clusters, const int* nw_clusters, const int* wp_clusters, bool room, BlockChoice* out)
+static void choose_block(const BlockKey& k, int sm_count, const int* wd_clusters, const int* nw_clusters, const int* wp_clusters, const BlockWorkspace& sizes, BlockChoice* out)
 {
     const bool narrow = k.M <= BlockWorkspace::kNarrowRows;
     out->form = narrow ? kFormNarrow : kFormWeights;
@@ -2995,8 +2994,10 @@ static void choose_block(const BlockKey& k, int sm_count, const int* wd_clusters
     if (!narrow) {
         out->weights = WeightsTiling(k.M, k.N, k.K, kActExpanded, k.a_is_km, wd_clusters);
         const long long pair_rounds = ((long long)((k.M + 2 * BM - 1) / (2 * BM)) * ((k.N + BN - 1) / BN) + sm_count / 2 - 1) / (sm_count / 2);
-        const double expand_w = 6000.0 + 3.0 * (double)k.K * k.N / 3300.0, pair_cycles = (double)pair_rounds * ((k.K + BK - 1) / BK * 545.0 + 500.0);
-        if (room && k.policy != HIF8_GEMM_PATH_EXPAND_A && (k.policy == HIF8_GEMM_PATH_EXPAND_BOTH || expand_w + pair_cycles < 1.03 * out->weights.cost.all(out->weights.tiles))) {
+        // (the weights are expanded in the launch that expands the activations)
+        const double expand_w = 2000.0 + 3.0 * (double)k.K * k.N / 3300.0, pair_cycles = sizes.split > 1 ? sizes.cycles + 500.0 : (double)pair_rounds * ((k.K + BK - 1) / BK * 545.0 + 500.0);
+        if (sizes.w_bytes != 0 && k.policy != HIF8_GEMM_PATH_EXPAND_A &&
+            (k.policy == HIF8_GEMM_PATH_EXPAND_BOTH || expand_w + pair_cycles < 1.03 * out->weights.cost.all(out->weights.tiles))) {
             out->form = kFormPair;
             return;
         }
@@ -3032,7 +3033,7 @@ int hif8::launch_block_gemm(const BlockCodes& a, bool a_is_km, const BlockCodes&
         key.policy = g_path_policy.load(std::memory_order_relaxed);
         BlockChoice choice;
         if (!g_block_choices.find(key, &choice)) {
-            choose_block(key, sm_count, wd_clusters, nw_clusters, wp_clusters, sizes.w_bytes != 0, &choice);
+            choose_block(key, sm_count, wd_clusters, nw_clusters, wp_clusters, sizes, &choice);
             g_block_choices.put(key, choice);
         }
         if (choice.form == kFormWarp) return launch_warp_gemm(a.codes, a.ld, 0, w.codes, w.ld, w_is_nk, p, choice.warp, st);
