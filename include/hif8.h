@@ -564,7 +564,7 @@ size_t hif8_gemm_block_workspace_bytes(int M, int N, int K, int a_is_km, int w_i
  *   *d_norm = sqrt(sum g^2) * 2^-s over all elements of all tensors;  dst = g * 2^-s * min(1, max_norm / norm), rounded once to the tensor's type
  * A list of tensors in device memory: d_src [n_tensors] addresses, d_dst the same for the results (NULL, or equal entries: in place; otherwise no result may overlap a
  * gradient), d_dtype [n_tensors] element formats, d_start [n_tensors + 1] running sums of the tensors' numbers of elements, from 0 to n_elements.  (They have to be right: the library
- * cannot check them; a tensor of no known format is left out.)  Addresses are aligned to their elements; 16-byte aligned ones take the vectorised path.
+ * cannot check them.  A tensor of no known format, or at an address that is 0 or not aligned to its elements, is left out.)  16-byte aligned addresses take the vectorised path.
  *   d_scale_exp: device int s, the first int of the state of hif8_als_state_init, for instance (NULL: 0);  max_norm > 0, +Inf for no clipping (HIF8_ERR_SCALE_RANGE).
  *   A norm beyond FP32 is stored as +Inf and clipped to all the same.  Gradients that are not all finite: nothing is written to dst, *d_norm = +Inf and *d_found_inf |= 1 (as hif8_check_finite; either pointer may be NULL).
  * Squares are summed in FP64 in a fixed order: results are reproducible.  workspace: hif8_grad_clip_workspace_bytes() bytes, 256-byte aligned, for one call at a time.

@@ -3,8 +3,8 @@
 //
 //   e = clamp(target_exp - floor(log2 amax)),  code = To_HiF8(x 2^e),  x ~ value(code) 2^-e
 //
-// All of it is bound by memory: every element is read once.  Sixteen threads hold a block's width, eight elements each, so a block's maximum
-// takes four exchanges within half a warp; a block of 128 rows is one thread block's, held in registers between its maximum and its codes.
+// All of it is bound by memory: every element is read once.  Eight threads hold a block of 1 x 128, sixteen elements each, so its maximum takes three exchanges; a block of
+// 128 x 128 is one thread block's, held in registers between its maximum and its codes.
 #include "hif8_block.cuh"
 
 namespace hif8 {
@@ -115,6 +115,47 @@ __global__ void __launch_bounds__(kThreads, row_blocks(SRC, MODE)) block_row_enc
             store_codes8(out, c, p.m.cols, p.codes8, lo);
             store_codes8(out, c + 8, p.m.cols, p.codes8, hi);
         }
+    }
+    if (p.late) pdl_launch_dependents();
+}
+
+// The same where rows lie on no such boundaries: a warp takes two neighbouring blocks of a row at a time, spread over its lanes (see load_spread).
+template <int SRC, int MODE>
+__global__ void __launch_bounds__(kThreads, row_blocks(SRC, MODE)) block_row_encode_spread_kernel(const EncodeParams p)
+{
+    __shared__ SmemTables sm;
+    setup_tables<true, MODE != HIF8_RND_TA, false, MODE, SRC>(sm, p.flags);
+    pdl_wait_prior_grid();
+    if (!p.late) pdl_launch_dependents();
+    constexpr size_t item = SRC == HIF8_F32 ? 4 : 2;
+    const int lane = threadIdx.x & 31, cols = (int)p.m.cols;
+    const unsigned warp = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), warps = gridDim.x * (kThreads / 32);
+    for (unsigned long long u = warp; u < p.units; u += warps) {  // p.across: pairs of blocks of a row
+        const unsigned row = p.across.div((unsigned)u), pair = (unsigned)u - row * p.across.d;
+        const int c = (int)pair * 256 + lane;
+        const Eight<SRC> e = load_spread<SRC>(reinterpret_cast<const char*>(p.src) + (size_t)row * (size_t)p.ld_src * item, c, cols);
+        int se[2];
+        uint32_t code[2] = {0u, 0u};
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            float top = 0.f;
+#pragma unroll
+            for (int i = 4 * k; i < 4 * k + 4; i++) top = amax_step(top, value_of_eight<SRC>(e, i));
+            se[k] = block_exp_from_amax(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top)), p.target_exp);
+            const float scale = pow2f(se[k]);
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                float x; uint32_t raw, word = 0;
+                unpack_eight<SRC>(e, 4 * k + i, x, raw);
+                if (MODE == HIF8_RND_SR) {
+                    const unsigned long long at = (unsigned long long)row * (unsigned long long)p.m.cols + (unsigned long long)(c + 32 * (4 * k + i));
+                    word = philox_word(philox4x32_10((uint32_t)(at >> 2), (uint32_t)(at >> 34), (uint32_t)p.seed, (uint32_t)(p.seed >> 32)), (unsigned)at & 3u);
+                }
+                code[k] |= (encode_one<MODE, SRC>(x, raw, scale, sm.ta, sm.thr, word) & 0xFFu) << (8 * i);
+            }
+        }
+        store_codes_spread(p.m.codes + (size_t)row * (size_t)p.m.ld, c, cols, make_uint2(code[0], code[1]));
+        if (lane < 2 && (int)pair * 256 + 128 * lane < cols) p.m.exps[(size_t)row * (size_t)p.m.exp_stride + 2 * pair + lane] = lane ? se[1] : se[0];
     }
     if (p.late) pdl_launch_dependents();
 }
@@ -294,6 +335,40 @@ __global__ void __launch_bounds__(kThreads, LANE ? 6 : 4) block_decode_kernel(co
     if (job.m[0].late) pdl_launch_dependents();
 }
 
+// The same to rows that lie on no 16-byte boundary, or from such: a warp takes 512 columns of a row, spread over its lanes: sixteen codes each, their exponents four.
+template <int DST>
+__global__ void __launch_bounds__(kThreads, 6) block_decode_spread_kernel(const DecodeParams p)
+{
+    __shared__ __align__(16) uint32_t table[kLaneTableWords];
+    fill_lane_table(table, decode_bits_f32(threadIdx.x));
+    __syncthreads();
+    pdl_wait_prior_grid();
+    const uint32_t lane4 = (threadIdx.x & 31u) * 4u;
+    const int lane = threadIdx.x & 31, cols = (int)p.m.cols;
+    const unsigned warp = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), warps = gridDim.x * (kThreads / 32);
+    for (unsigned long long u = warp; u < p.units; u += warps) {  // p.chunks: stretches of 512 columns of a row
+        const unsigned row = p.chunks.div((unsigned)u);
+        const int c = (int)((unsigned)u - row * p.chunks.d) * 512 + lane;
+        const uint8_t* from = p.m.codes + (size_t)row * (size_t)p.m.ld;
+        uint32_t code[16];
+        float scale[4];
+#pragma unroll
+        for (int i = 0; i < 16; i++) code[i] = c + 32 * i < cols ? __ldcs(from + c + 32 * i) : 0u;
+#pragma unroll
+        for (int k = 0; k < 4; k++) scale[k] = pow2f(c + 128 * k < cols ? -exp_at(p.m, row, c + 128 * k) : 0);
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            if (c + 32 * i >= cols) continue;
+            const float x = __uint_as_float(lane_lookup<0>(table, code[i], lane4)) * scale[i >> 2];
+            const size_t at = (size_t)row * (size_t)p.ld_dst + (size_t)(c + 32 * i);
+            if (DST == HIF8_F32) reinterpret_cast<float*>(p.dst)[at] = x;
+            else if (DST == HIF8_BF16) reinterpret_cast<unsigned short*>(p.dst)[at] = (unsigned short)to_bits<HIF8_BF16>(x);
+            else reinterpret_cast<unsigned short*>(p.dst)[at] = (unsigned short)to_bits<HIF8_F16>(x);
+        }
+    }
+    pdl_launch_dependents();
+}
+
 // Codes [rows, cols] -> BF16 [cols, ld_dst], transposed: tiles of 64 rows by 64 columns.  A thread takes two rows' eight columns and puts a column's two
 // values into one word, lines of 33 words apart: eight row pairs and four groups of columns to a warp meet in no bank, and read whole 32-byte sectors.
 constexpr int kFlipRows = 64, kFlipCols = 64, kFlipLine = kFlipRows / 2 + 1;
@@ -395,7 +470,16 @@ void launch_encode(EncodeParams p, int sms, cudaStream_t st)
         launch_pdl(block_tile_encode_kernel<SRC, MODE>, dim3(p.late ? most : p.units), st, p);
         return;
     }
-    const unsigned blocks = (p.units + 31u) / 32u, most = (unsigned)(sms * row_blocks(SRC, MODE));
+    const unsigned most = (unsigned)(sms * row_blocks(SRC, MODE));
+    if (!(p.vectors && p.codes8) && p.m.cols >= 384 && p.m.cols < 0x7FFFFF00ll) {  // (a warp's two blocks have to be there: rows of 100 BF16 values 90 us, spread 179)
+        const long long pairs = (p.m.cols + 255) / 256, units = pairs * p.m.rows;  // (no more than blocks of the matrix)
+        p.across = FastDiv((uint32_t)pairs); p.units = (unsigned)units;
+        const unsigned blocks = (p.units + 7u) / 8u;
+        p.late = blocks > most;
+        launch_pdl(block_row_encode_spread_kernel<SRC, MODE>, dim3(p.late ? most : blocks), st, p);
+        return;
+    }
+    const unsigned blocks = (p.units + 31u) / 32u;
     p.late = blocks > most;
     launch_pdl(block_row_encode_kernel<SRC, MODE>, dim3(p.late ? most : blocks), st, p);
 }
@@ -527,6 +611,16 @@ extern "C" int hif8_block_decode(const uint8_t* src, int64_t ld_src, const int* 
     p.codes8 = aligned_to(src, 8) && (rows <= 1 || (ld_src & 7) == 0); p.codes16 = aligned_to(src, 16) && (rows <= 1 || (ld_src & 15) == 0);
     p.vectors = vector_rows(dst, rows, ld_dst, item); p.vectors32 = aligned_to(dst, 32) && (rows <= 1 || ((size_t)ld_dst * item & 31u) == 0);
     cudaStream_t st = (cudaStream_t)stream;
+    if (!(p.vectors && p.codes8) && cols < 0x7FFFFE00ll) {
+        const long long stretches = (cols + 511) / 512;
+        p.chunks = FastDiv((uint32_t)stretches); p.units = (unsigned)(stretches * rows);
+        const unsigned most = (unsigned)sms * 6u, blocks = (p.units + 7u) / 8u;
+        const dim3 grid(blocks < most ? blocks : most);
+        if (dst_dtype == HIF8_F32) launch_pdl(block_decode_spread_kernel<HIF8_F32>, grid, st, p);
+        else if (dst_dtype == HIF8_BF16) launch_pdl(block_decode_spread_kernel<HIF8_BF16>, grid, st, p);
+        else launch_pdl(block_decode_spread_kernel<HIF8_F16>, grid, st, p);
+        return finish(1);
+    }
     if (dst_dtype == HIF8_F32) launch_decode<HIF8_F32, false>(job, sms, st);
     else if (dst_dtype == HIF8_BF16) launch_decode<HIF8_BF16, false>(job, sms, st);
     else launch_decode<HIF8_F16, false>(job, sms, st);

@@ -144,6 +144,65 @@ __device__ __forceinline__ void store_eight(void* row, long long c, long long co
         }
     }
 }
+// The same of rows that lie on no 16-byte boundary: element i is column c + 32 i, c the warp's first column plus the lane, so that a warp reads and writes whole lines, an
+// element a lane and instruction.  (Eight neighbouring elements a thread, one by one, took four to nine times as long as rows that are aligned.)
+template <int DT, bool KEEP = false>
+__device__ __forceinline__ Eight<DT> load_spread(const void* row, int c, int cols)
+{
+    Eight<DT> e;
+    uint32_t w[8];
+    auto get = [&](int i) -> uint32_t {
+        if (DT == HIF8_F32) {
+            const uint32_t* p = reinterpret_cast<const uint32_t*>(row) + c + 32 * i;
+            return KEEP ? __ldg(p) : __ldcs(p);
+        }
+        const unsigned short* p = reinterpret_cast<const unsigned short*>(row) + c + 32 * i;
+        return KEEP ? __ldg(p) : __ldcs(p);
+    };
+    if ((c | 31) + 224 < cols) {  // (the same for a warp)
+#pragma unroll
+        for (int i = 0; i < 8; i++) w[i] = get(i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++) w[i] = c + 32 * i >= cols ? 0u : get(i);
+    }
+    constexpr int last = sizeof(e.v) / 16 - 1;
+    if (DT == HIF8_F32) {
+        e.v[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        e.v[last] = make_uint4(w[4], w[5], w[6], w[7]);
+    } else
+        e.v[0] = make_uint4(__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410), __byte_perm(w[4], w[5], 0x5410), __byte_perm(w[6], w[7], 0x5410));
+    return e;
+}
+template <int DT>
+__device__ __forceinline__ void store_spread(void* row, int c, int cols, const Eight<DT>& e)
+{
+    auto put = [&](int i) {
+        float x; uint32_t raw;
+        unpack_eight<DT>(e, i, x, raw);
+        if (DT == HIF8_F32) reinterpret_cast<uint32_t*>(row)[c + 32 * i] = raw;
+        else reinterpret_cast<unsigned short*>(row)[c + 32 * i] = (unsigned short)raw;
+    };
+    if ((c | 31) + 224 < cols) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) put(i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            if (c + 32 * i < cols) put(i);
+    }
+}
+__device__ __forceinline__ void store_codes_spread(uint8_t* row, int c, int cols, uint2 w)
+{
+    if ((c | 31) + 224 < cols) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) row[c + 32 * i] = (uint8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            if (c + 32 * i < cols) row[c + 32 * i] = (uint8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
+    }
+}
 // eight codes; `vectors`: the row starts on an 8-byte boundary
 __device__ __forceinline__ void store_codes8(uint8_t* row, long long c, long long cols, bool vectors, uint2 w)
 {

@@ -69,6 +69,7 @@ __device__ __forceinline__ bool piece_of(const ClipParams& p, int t, long long f
     s.dtype = p.dtypes[t];
     s.lo = from <= first ? 0 : min(n, (from - first + 15) & ~15ll);
     s.hi = to <= first ? 0 : min(n, (to - first + 15) & ~15ll);
+    if (!s.src || !s.dst || ((s.src | s.dst) & (s.dtype == HIF8_F32 ? 3u : 1u))) s.hi = s.lo;  // (no address of such elements: left out)
     return b + kTensorCost * t < to;
 }
 

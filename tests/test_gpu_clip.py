@@ -132,9 +132,17 @@ def test_zeros_and_nothing():
         assert float(g.norm) == 0
 
 
-def test_an_unknown_format_is_left_out():
+@pytest.mark.parametrize("what", ["format", "address", "no address", "no result"])
+def test_what_is_no_tensor_is_left_out(what):
     g = Gradients([1000, 50, 70], [H.F32, H.BF16, H.F32], 13)
-    g.d_dtype[0] = 9
+    if what == "format":
+        g.d_dtype[0] = 9
+    elif what == "address":
+        g.d_src[0] += 2
+    elif what == "no address":
+        g.d_src[0] = 0
+    else:
+        g.d_dst[0] = 0
     g.call(1e9)
     want = np.sqrt(sum(float((x.double() ** 2).sum()) for x in g.host[1:]))
     assert abs(float(g.norm) - want) < 1e-5 * want and bool((g.dst[:g.where[1]] == 0xA5).all())
