@@ -611,7 +611,7 @@ extern "C" int hif8_block_decode(const uint8_t* src, int64_t ld_src, const int* 
     p.codes8 = aligned_to(src, 8) && (rows <= 1 || (ld_src & 7) == 0); p.codes16 = aligned_to(src, 16) && (rows <= 1 || (ld_src & 15) == 0);
     p.vectors = vector_rows(dst, rows, ld_dst, item); p.vectors32 = aligned_to(dst, 32) && (rows <= 1 || ((size_t)ld_dst * item & 31u) == 0);
     cudaStream_t st = (cudaStream_t)stream;
-    if (!(p.vectors && p.codes8) && cols < 0x7FFFFE00ll) {
+    if (!(p.vectors && p.codes8) && cols >= 96 && cols < 0x7FFFFE00ll) {  // (2^26 codes, rows of 20: 247 us, spread 1470; of 100 337 and 322, of 1001 360 and 93)
         const long long stretches = (cols + 511) / 512;
         p.chunks = FastDiv((uint32_t)stretches); p.units = (unsigned)(stretches * rows);
         const unsigned most = (unsigned)sms * 6u, blocks = (p.units + 7u) / 8u;

@@ -80,9 +80,10 @@ __device__ __forceinline__ void for_pieces(const ClipParams& p, long long from, 
 {
     __shared__ Piece16 s_piece[kThreads];
     for (int batch = first; batch < p.tensors; batch += kThreads) {
-        Piece16 mine;
+        Piece16 mine{};
         const bool in = piece_of(p, batch + (int)threadIdx.x, from, to, mine);
-        if (in) s_piece[threadIdx.x] = mine;
+        if (!in) mine.hi = mine.lo;  // (starts that are in no order: nothing)
+        s_piece[threadIdx.x] = mine;
         const int n = __syncthreads_count(in);  // (starts are in order: those in the share come first)
         const int warp = threadIdx.x >> 5;
 #pragma unroll 1
