@@ -498,7 +498,7 @@ size_t hif8_cache_compact_workspace_bytes(int n_pages);
  * stands for value(code) * 2^-e.  Exponents lie, and are taken, within [-HIF8_BLOCK_EXP_MAX, HIF8_BLOCK_EXP_MAX]: within them what a code stands for is exact in BF16.
  * Matrices of values have rows ld elements apart.  Rows must not overlap one another, nor what a call writes anything else that it writes or reads
  * (HIF8_ERR_OVERLAP) but for what a call names.  Pointers are aligned to their elements (HIF8_ERR_ALIGN); rows on 16-byte boundaries (of codes: 8) take the vectorised path, others a slower one with identical
- * results.  A matrix has less than 2^31 groups of eight columns (HIF8_ERR_SHAPE).
+ * results (but that a norm adds its row in another order).  A matrix has less than 2^31 groups of eight columns (HIF8_ERR_SHAPE).
  */
 #define HIF8_BLOCK 128
 #define HIF8_BLOCK_EXP_MAX 96

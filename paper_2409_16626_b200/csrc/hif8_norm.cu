@@ -3,7 +3,7 @@
 //   h = x + residual (rounded to their type),  r = 1 / sqrt(mean(h^2) + eps),  y = h r w  ->  codes with a scale for each 1 x 128
 //   dx = r (w dy - u mean(w dy u)) + dh,  u = h r;     dw_j = sum_i dy_ij u_ij
 //
-// Both are bound by memory.  A row is held in registers between its sum and its results (a group of 32 to 1024 threads per row, up to 32 elements a
+// Both are bound by memory.  A row is held in registers between its sum and its results (16 to 1024 threads per row, up to 32 elements a
 // thread), so every tensor is read or written once.  Sums, the norm's factor and the weight's gradient are FP32.
 #include "hif8_block.cuh"
 #include "hif8_host_cache.h"

@@ -140,3 +140,44 @@ def test_rows_far_apart(block_rows):
     src.zero_()
     H.hif8_block_decode(q, 2 ** 32, e, 2 ** 30, 3, 200, block_rows, src, H.BF16, 2 ** 31)
     assert torch.equal(torch.as_strided(src, (3, 200), (2 ** 31, 1)).cpu(), torch.from_numpy(B.meant(codes, exps, block_rows)).bfloat16())
+
+
+@pytest.mark.parametrize("block_rows", [1, 128])
+@pytest.mark.parametrize("dtype", [H.F32, H.BF16, H.F16])
+@pytest.mark.parametrize("rows,cols", [(1, 95), (2, 97), (3, 383), (3, 385), (5, 390), (2, 512), (130, 513), (3, 1101), (1, 4097)])
+def test_unaligned_rows(rows, cols, dtype, block_rows):
+    check(matrix(rows, cols, dtype, rows + cols), dtype, block_rows, ld=cols | 1, offset=1, ld_q=cols + 3, q_offset=3, exp_pad=1)
+
+
+@pytest.mark.parametrize("dtype", [H.F32, H.BF16, H.F16])
+@pytest.mark.parametrize("rnd", list(MODES))
+def test_roundings_of_unaligned_rows(rnd, dtype):
+    check(matrix(9, 700, dtype, 19), dtype, 1, ld=701, offset=3, ld_q=703, q_offset=1, target=6, rnd=rnd, seed=0x1234567890)
+
+
+@pytest.mark.parametrize("flags", [0, 1, 2, 3])
+@pytest.mark.parametrize("dtype", [H.F32, H.BF16, H.F16])
+def test_inf_nan_and_zeros_in_unaligned_rows(dtype, flags):
+    x = matrix(6, 600, dtype, 21)
+    x[0, 5], x[1, 140], x[2, 599], x[3, 0] = float("inf"), float("-inf"), float("nan"), float("nan")
+    x[4] = 0
+    x[5, 128:256] = float("nan")
+    check(x, dtype, 1, flags=flags, ld=601, offset=1, ld_q=605, q_offset=1)
+
+
+@pytest.mark.parametrize("dtype", [H.F32, H.BF16, H.F16])
+def test_many_unaligned_rows_are_those_of_aligned_ones(dtype):
+    """More rows than are taken at once."""
+    x = torch.randn(9000, 1500, generator=torch.Generator().manual_seed(23)).to(B.TORCH[dtype]).cuda()
+    q, e = B.encoded(x, dtype, 1)
+    src = torch.zeros(1 + 9000 * 1503, dtype=x.dtype, device="cuda")
+    codes, exps = torch.zeros(1 + 9000 * 1501, dtype=torch.uint8, device="cuda"), torch.zeros_like(e)
+    far, out = torch.as_strided(src, (9000, 1500), (1503, 1), 1), torch.as_strided(codes, (9000, 1500), (1501, 1), 1)
+    far.copy_(x)
+    H.hif8_block_encode(far.data_ptr(), dtype, 1503, 9000, 1500, 1, out.data_ptr(), 1501, exps, exps.stride(0))
+    assert torch.equal(out, q[:, :1500]) and torch.equal(exps, e)
+    back = torch.empty(9000, 1500, dtype=x.dtype, device="cuda")
+    H.hif8_block_decode(q, q.stride(0), e, e.stride(0), 9000, 1500, 1, back, dtype, 1500)
+    src.zero_()
+    H.hif8_block_decode(out.data_ptr(), 1501, exps, exps.stride(0), 9000, 1500, 1, far.data_ptr(), dtype, 1503)
+    assert torch.equal(far, back) and bool((torch.as_strided(src, (8999, 3), (1503, 1), 1501) == 0).all())

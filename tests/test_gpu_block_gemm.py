@@ -204,3 +204,11 @@ def test_rows_far_apart():
             assert np.all(np.abs(C.cpu().double().numpy() - av @ wv.T) <= bound(K) * (np.abs(av) @ np.abs(wv.T)))
             assert float(out[N]) == 7 and float(out[2 ** 30 - 1]) == 7
         del far, out
+
+
+@pytest.mark.parametrize("M,N,K", [(2304, 2304, 130), (4600, 2302, 70), (2500, 4099, 200)])
+@pytest.mark.parametrize("c_dtype", [H.F32, H.BF16])
+@pytest.mark.parametrize("accumulate", [0, 1])
+def test_several_tiles_to_a_pair(M, N, K, c_dtype, accumulate):
+    check(M, N, K, 1, 1, 0, 1, c_dtype, accumulate, seed=K)
+    check(M, N, K, 0, 1, 1, 1, c_dtype, accumulate, seed=K)

@@ -174,3 +174,11 @@ def test_captured_and_reproducible():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(g.dst, first) and float(g.norm) == norm
+
+
+@pytest.mark.parametrize("sizes,dtypes", [([45_000_003], [H.BF16]), ([13_000_001, 9_000_000, 77], ALL)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_long_shares(sizes, dtypes, in_place):
+    g = Gradients(sizes, dtypes, 9)
+    g.call(1.0, 4, in_place=in_place)
+    g.check(1.0, 4, g.src if in_place else None)

@@ -257,3 +257,23 @@ def test_streams_and_graphs():
     torch.cuda.synchronize()
     for dx, dw, _ in made:
         assert torch.equal(dx.cpu(), want) and torch.equal(dw.cpu(), wdw)
+
+
+@pytest.mark.parametrize("dtype", [H.F32, H.BF16, H.F16])
+@pytest.mark.parametrize("rows,cols", [(3, 31), (40, 250), (600, 129), (7, 1025), (150, 2050), (149, 5003), (2, 12291), (151, 16383), (150, 32767)])
+def test_unaligned_rows(rows, cols, dtype):
+    x, r, w = inputs(rows, cols, dtype, rows)
+    check(x, r, w, dtype, ld=cols | 1, offset=1, ld_q=cols + 3, q_offset=5, w_offset=1)
+
+
+@pytest.mark.parametrize("dtype", [H.F32, H.BF16, H.F16])
+@pytest.mark.parametrize("in_place", [None, "dy", "dh"])
+@pytest.mark.parametrize("rows,cols", [(3, 31), (1300, 129), (7, 1025), (650, 2050), (310, 5003), (2, 12291), (151, 16383), (150, 32767)])
+def test_gradient_of_unaligned_rows(rows, cols, in_place, dtype):
+    check_gradient(rows, cols, dtype, True, rows, ld=cols | 1, offset=1, in_place=in_place)
+
+
+@pytest.mark.parametrize("dtype", [H.F32, H.BF16, H.F16])
+@pytest.mark.parametrize("rows,cols", [(2600, 128), (1300, 520), (700, 4096), (400, 8200), (310, 12288), (310, 16384), (150, 32768)])
+def test_gradient_in_several_rounds(rows, cols, dtype):
+    check_gradient(rows, cols, dtype, True, rows)
