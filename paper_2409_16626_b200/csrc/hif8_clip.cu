@@ -5,8 +5,8 @@
 // Two launches: sums of squares, a share of the list to a block, and the scaling, in front of which every block adds the shares up in the same order. Both are bound by
 // memory.  A share is a stretch of the list of all elements, in which each tensor takes kTensorCost places more than it has elements, for what it costs to come to one: so
 // neither many small tensors nor few large ones leave blocks idle.  A block fetches the descriptors of its tensors together, works on long pieces with all threads and on short ones
-// with a warp each.  (Tensors one after the other, each with its descriptor's latency: 3000 tensors of 10 elements 362 us, 11.4; 2.7 M elements in 28 matrices and 9 vectors
-// 21.5 us, 14.2.)  Squares are added in FP32 over 16 bytes and in FP64 from there on (vectors whose sum leaves FP32's comfortable range: in FP64 altogether), so the
+// with a warp each.  (Tensors one after the other, each with its descriptor's latency: 3000 tensors of 10 elements 362 us, 11.5; 2.7 M elements in 28 matrices and 9 vectors
+// 21.5 us, 11.8.)  Squares are added in FP32 over 16 bytes and in FP64 from there on (vectors whose sum leaves FP32's comfortable range: in FP64 altogether), so the
 // norm is as exact as FP32 can say, and the squares of finite gradients do not overflow.
 #include "hif8_block.cuh"
 
@@ -14,10 +14,12 @@ namespace hif8 {
 namespace {
 
 constexpr int kClipBlocks = 1024;   // shares at most
-constexpr int kClipPerSM = 4;
-constexpr int kClipUnroll = 2;      // words of 32 bytes a thread has in flight
+// Blocks an SM, and words of 32 bytes that a thread has in flight: sums of squares, results.  (436000000 BF16 elements: so 403 us; 4, 2 and 2 440, which spilled; 2, 8 and 4 411;
+// 2, 4 and 3 412; 2, 6 and 2 408.  20000000 16.9 and 18.9, 1000 5.6 and 6.4.)
+constexpr int kClipPerSM = 2;
+constexpr int kSquaresUnroll = 6, kScaleUnroll = 3;
 constexpr long long kTensorCost = 1024, kShare = 2048;  // (a share's least length)
-constexpr int kKeepWords = 3584;    // of a piece's end stay in L2 for the second launch, which begins there: 66 MB over the blocks
+constexpr int kKeepWords = 7168;    // of a piece's end stay in L2 for the second launch, which begins there: 68 MB over the blocks
 constexpr long long kLongPiece = 2048;                  // from so many elements on a piece is the whole block's
 
 struct ClipParams {
@@ -101,7 +103,7 @@ __device__ __forceinline__ void for_pieces(const ClipParams& p, long long from, 
 }
 
 // 32 bytes; `whole`: on a boundary of that many, and not of 16 only.  GONE: not to be kept in L2.  What the first launch reads in front of a piece's end and what the second one
-// writes is not: 436000000 BF16 elements 454 -> 440 us, 20000000 20.3 -> 19.0 (with 40 to 130 MB kept 441 to 443).
+// writes is not: 436000000 BF16 elements 454 -> 440 us, 20000000 20.3 -> 19.0 (with four blocks an SM; 40 to 130 MB kept: 441 to 443).
 template <bool GONE> __device__ __forceinline__ void load_32(const void* from, uint4& a, uint4& b, bool whole)
 {
     if (!whole) {
@@ -157,17 +159,17 @@ template <int DT> __device__ __forceinline__ double piece_squares(const Piece16&
         const bool whole = (s.src & 16u) == 0;
         const char* from = reinterpret_cast<const char*>(s.src);
         const long long end = s.hi / PW;
-        for (long long base = s.lo / PW + thread; base < end; base += threads * kClipUnroll) {
-            uint4 v[kClipUnroll][2];
+        for (long long base = s.lo / PW + thread; base < end; base += threads * kSquaresUnroll) {
+            uint4 v[kSquaresUnroll][2];
 #pragma unroll
-            for (int j = 0; j < kClipUnroll; j++) {
+            for (int j = 0; j < kSquaresUnroll; j++) {
                 v[j][0] = v[j][1] = make_uint4(0, 0, 0, 0);
                 if (base + j * threads >= end) continue;
                 if (base < end - kKeepWords) load_32<true>(from + (base + j * threads) * 32, v[j][0], v[j][1], whole);
                 else load_32<false>(from + (base + j * threads) * 32, v[j][0], v[j][1], whole);
             }
 #pragma unroll
-            for (int j = 0; j < kClipUnroll; j++) sum += squares<DT>(v[j][0]) + squares<DT>(v[j][1]);
+            for (int j = 0; j < kSquaresUnroll; j++) sum += squares<DT>(v[j][0]) + squares<DT>(v[j][1]);
         }
         tail = max(s.lo, end * PW);
     }
@@ -242,13 +244,13 @@ template <int DT> __device__ __forceinline__ void scale_piece(const Piece16& s, 
         const char* from = reinterpret_cast<const char*>(s.src);
         char* to = reinterpret_cast<char*>(s.dst);
         const long long first = s.lo / PW, end = s.hi / PW;
-        for (long long base = end - 1 - thread; base >= first; base -= threads * kClipUnroll) {
-            uint4 v[kClipUnroll][2];
+        for (long long base = end - 1 - thread; base >= first; base -= threads * kScaleUnroll) {
+            uint4 v[kScaleUnroll][2];
 #pragma unroll
-            for (int j = 0; j < kClipUnroll; j++)
+            for (int j = 0; j < kScaleUnroll; j++)
                 if (base - j * threads >= first) load_32<false>(from + (base - j * threads) * 32, v[j][0], v[j][1], whole);
 #pragma unroll
-            for (int j = 0; j < kClipUnroll; j++)
+            for (int j = 0; j < kScaleUnroll; j++)
                 if (base - j * threads >= first) store_32(to + (base - j * threads) * 32, scaled<DT>(v[j][0], f), scaled<DT>(v[j][1], f), whole);
         }
         tail = max(s.lo, end * PW);
