@@ -91,6 +91,10 @@ int add_product_parts(const float* parts, int n, long long rows, long long cols,
 // C of `p` from block-scaled operands, the rest of `p` filled in here; the arguments have been checked.
 int launch_block_gemm(const BlockCodes& a, bool a_is_km, const BlockCodes& w, bool w_is_nk, const GemmParams& p, const BlockWorkspace& sizes, void* workspace, cudaStream_t st);
 
+// The same for few rows of A [M,K] and weights [N,K] with scales for each 128 x 128, codes of both operands decoded in the kernel; and its cycles (1e30: it has no form for these).
+double block_rows_cycles(int M, int N, int K, int sms);
+int launch_block_rows(const BlockCodes& a, const BlockCodes& w, const GemmParams& p, cudaStream_t st);
+
 // A product's operand to be decoded into BF16 with its blocks' scales (exact: four significant bits, exponents within -118 .. 111):
 // dst [rows_out, cols_out], or with `transposed` element (r, c) at dst[c][r]; rows and columns beyond the matrix become zeros.  cols_out (transposed:
 // rows_out) and ld_dst are multiples of 8, dst is 16-byte aligned.

@@ -2815,7 +2815,7 @@ struct NarrowTiling {
 // Which kernel takes a product, and how it divides it: a function of the sizes, the layouts and what the workspace has room for, so
 // it is kept for the 64 used last.  (The search over divisions takes 0.5 us on the host, 2 us at most: products of 1 to 8192 rows, N and K 16
 // to 28672.  It runs outside the lock, so that threads with new sizes do not wait for one another.)
-enum GemmForm { kFormWarp, kFormNarrow, kFormWeights, kFormPair };
+enum GemmForm { kFormWarp, kFormNarrow, kFormWeights, kFormPair, kFormRows };
 struct GemmKey {
     int M, N, K, dev, w_is_nk, a_is_km, room, policy;
 };
@@ -3012,6 +3012,10 @@ static void choose_block(const BlockKey& k, int sm_count, const int* wd_clusters
         }
         other = out->weights.cycles;
     } else other = NarrowTiling(k.M, k.N, k.K, sm_count, nw_clusters, true).cycles + 6000.0;
+    if (k.w_is_nk && !k.a_is_km && k.policy != HIF8_GEMM_PATH_EXPAND_A && k.policy != HIF8_GEMM_PATH_EXPAND_BOTH) {
+        const double rows = block_rows_cycles(k.M, k.N, k.K, sm_count);
+        if (rows < 0.93 * other) { other = rows; out->form = kFormRows; }
+    }
     if (k.a_is_km || (k.policy != HIF8_GEMM_PATH_AUTO && k.policy != HIF8_GEMM_PATH_WARP)) return;
     out->warp = WarpTiling(k.M, k.N, k.K, k.w_is_nk, false, wp_clusters, k.policy == HIF8_GEMM_PATH_WARP ? 1e30 : other / 1.35);  // (scales cost it more than the others)
     if (out->warp.mt > 0) out->form = kFormWarp;
@@ -3046,6 +3050,7 @@ int hif8::launch_block_gemm(const BlockCodes& a, bool a_is_km, const BlockCodes&
             g_block_choices.put(key, choice);
         }
         if (choice.form == kFormWarp) return launch_warp_gemm(a.codes, a.ld, 0, w.codes, w.ld, w_is_nk, p, choice.warp, st);
+        if (choice.form == kFormRows) return launch_block_rows(a, w, p, st);
         if (choice.form == kFormNarrow) {
             const int mp = (M + 15) & ~15;
             const long long slabs = (N + BM - 1) / BM, num_pb = (K + BK2 - 1) / BK2, total = slabs * num_pb;

@@ -212,3 +212,41 @@ def test_rows_far_apart():
 def test_several_tiles_to_a_pair(M, N, K, c_dtype, accumulate):
     check(M, N, K, 1, 1, 0, 1, c_dtype, accumulate, seed=K)
     check(M, N, K, 0, 1, 1, 1, c_dtype, accumulate, seed=K)
+
+
+@pytest.mark.parametrize("M", [1, 2, 3, 4])
+@pytest.mark.parametrize("N,K", [(1, 4096), (7, 130), (131, 512), (300, 1000), (1000, 2064), (2500, 513), (517, 4097), (260, 5000), (140, 8192), (130, 9000), (72, 16384), (20000, 272)])
+@pytest.mark.parametrize("c_dtype,accumulate", [(H.F32, 1), (H.BF16, 0), (H.BF16, 1)])
+def test_single_tokens(M, N, K, c_dtype, accumulate):
+    with gemm_path(H.GEMM_PATH_NO_WARP):
+        check(M, N, K, 0, 1 if M % 2 else 128, 1, 128, c_dtype, accumulate, seed=N + K)
+        check(M, N, K, 0, 1, 1, 128, c_dtype, accumulate, seed=N, lda=-(-K // 16) * 16 + 32, ldw=-(-K // 16) * 16 + 16, a_offset=16, w_offset=48, ldc=-(-N // 8) * 8 + 8)
+
+
+@pytest.mark.parametrize("M", [1, 2])
+def test_single_tokens_with_exponents_at_their_limits(M):
+    a, ae, av = operand(M, 700, 1, 11, spread=0)
+    w, we, wv = operand(264, 700, 128, 12, spread=0)
+    with gemm_path(H.GEMM_PATH_NO_WARP):
+        for ea, ew in ((96, -96), (-96, 96), (500, -1000), (-(1 << 31), (1 << 31) - 1)):
+            C = B.product(a, torch.full_like(ae, ea), 0, 1, w, torch.full_like(we, ew), 1, 128, M, 264, 700)[:, :264]
+            assert np.all(np.abs(C.cpu().double().numpy() - av @ wv.T) <= 1e-5 * (np.abs(av) @ np.abs(wv.T)))
+        # activations that leave FP32 with both scales, products that do not: 2^111 and 2^20 by weights of 2^-22 .. 2^-16
+        rng = np.random.default_rng(3)
+        big, small = rng.choice([0x6E, 0xEE, 0x08, 0x30], size=(M, 700)).astype(np.uint8), (rng.integers(1, 8, size=(264, 700)) + 128 * rng.integers(0, 2, size=(264, 700))).astype(np.uint8)
+        a[:], w[:] = torch.from_numpy(big).cuda(), torch.from_numpy(small).cuda()
+        C = B.product(a, torch.full_like(ae, -96), 0, 1, w, torch.full_like(we, -20), 1, 128, M, 264, 700)[:, :264].cpu().double().numpy()
+        av, wv = B.VALUES[big] * 2.0 ** 96, B.VALUES[small] * 2.0 ** 20
+        assert np.all(np.isfinite(C)) and np.all(np.abs(C - av @ wv.T) <= 1e-5 * (np.abs(av) @ np.abs(wv.T)))
+
+
+@pytest.mark.parametrize("M", [1, 2])
+def test_inf_and_nan_of_single_tokens(M):
+    a, ae, _ = operand(M, 523, 1, 21)
+    w, we, _ = operand(130, 523, 128, 22)
+    a[0, 200], w[5, 7] = 0x6F, 0x80                      # Inf in a row, NaN in a column
+    w[:, 200] = 0x08                                     # (Inf times a positive value)
+    with gemm_path(H.GEMM_PATH_NO_WARP):
+        C = B.product(a, ae, 0, 1, w, we, 1, 128, M, 130, 523)[:, :130]
+    assert bool(torch.isnan(C[:, 5]).all()) and bool((C[0, :5] == float("inf")).all()) and bool((C[0, 6:] == float("inf")).all())
+    assert M == 1 or bool(torch.isfinite(C[1, :5]).all() and torch.isfinite(C[1, 6:]).all())
