@@ -3022,7 +3022,7 @@ static void choose_block(const BlockKey& k, int sm_count, const int* wd_clusters
 }
 
 // Block-scaled operands.  Where the weights have a scale for each 128 x 128 they are decoded in the kernel: few rows and a small weight by the warp
-// kernel, which takes the activations' codes too; the others have the activations expanded to BF16 with their scales in front, up to 64 rows for the narrow kernel, beyond
+// kernel, one or two rows and a large one by the kernel for single tokens, which take the activations' codes too; the others have the activations expanded to BF16 with their scales in front, up to 64 rows for the narrow kernel, beyond
 // for the weights kernel, until expanding the weights pays.  Other weights (a gradient's activations, with a scale for each 1 x 128) are expanded whatever the size.
 int hif8::launch_block_gemm(const BlockCodes& a, bool a_is_km, const BlockCodes& w, bool w_is_nk, const GemmParams& params, const BlockWorkspace& sizes, void* workspace, cudaStream_t st)
 {
