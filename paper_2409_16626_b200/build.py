@@ -25,7 +25,7 @@ def _stale():
     if not os.path.exists(LIB) or not os.path.exists(CALL):
         return True
     t = min(os.path.getmtime(LIB), os.path.getmtime(CALL))
-    deps = sources() + [CALL_SRC] + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(ROOT, "include", "*.h"))
+    deps = sources() + [CALL_SRC] + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(ROOT, "include", "*.h"))
     return any(os.path.getmtime(d) > t for d in deps)
 
 

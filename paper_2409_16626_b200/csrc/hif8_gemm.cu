@@ -32,6 +32,7 @@
 #include "hif8_block_types.cuh"
 #include "hif8_host_cache.h"
 #include "hif8_internal.cuh"
+#include "hif8_pair_pieces.h"
 
 namespace hif8 {
 extern std::atomic<uint64_t> g_launches;
@@ -1976,6 +1977,7 @@ bf16_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
         };
         const int piece_cols = p.c_is_f32 ? 32 : 64;
         const uint32_t staging = base + SmemLayout2::out + (uint32_t)warp * 2 * kOutBytes;  // this warp's two pieces
+        PiecePlaces places;
         uint32_t n_old = 0, n_fetched = 0;  // old pieces waited for and (lane 0) asked for, over all tiles: parities of the buffers
         for (int t = pair_id; t < tiles; t += pairs, local++) {
             const int acc = local & 1, use = local >> 1;
@@ -1989,7 +1991,7 @@ bf16_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
             // The last tile's pieces have a place each: behind its MMAs the stages are free.  (Two in turn, each waiting for the one before it to have left and, where it is
             // added to C, for the old one to arrive: 1536 x 768 over 777 rows added to C 14.2 us, now 13.6, 4096 x 1024 over 1024 rows 17.9 and 17.1; not added the same.)
             const bool last = t + pairs >= tiles;
-            auto place_of = [&](int i) { return last ? i : i & 1; };
+            auto place_of = [&](int i) { return PiecePlaces::place_of(i, last); };
             auto buffer_of = [&](int i) { return place_of(i) < 2 ? staging + (uint32_t)place_of(i) * kOutBytes : base + (uint32_t)(warp * (kPieces - 2) + i - 2) * kOutBytes; };
             auto fetch_old = [&](int i) {  // lane 0; the piece's place is free
                 const uint32_t bar = bar_old(kPieces * warp + place_of(i));
@@ -2015,8 +2017,11 @@ bf16_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
 #pragma unroll 1
             for (int i = 0; i < pieces; i++) {
                 const uint32_t buf = buffer_of(i), line = buf + (uint32_t)lane * 128u;
-                if (!p.accumulate && place_of(i) < 2) {  // the store of two pieces ago has been read out
-                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                if (!p.accumulate && place_of(i) < 2) {  // the last store from this place has been read out
+                    if (lane == 0) {
+                        if (places.may_still_read(place_of(i)) == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                        else asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                    }
                     __syncwarp();
                 }
                 if (p.c_is_f32) {
@@ -2056,6 +2061,7 @@ bf16_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                 if (RAGGED && i >= mapped) continue;
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
+                places.stored(place_of(i));
                 if (lane == 0) {
                     tma_store_2d(&map_c, buf, n0 + i * piece_cols, SPLIT ? row0 + b * p.part_rows : row0);
                     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
