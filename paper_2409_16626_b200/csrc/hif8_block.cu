@@ -260,10 +260,10 @@ __device__ __forceinline__ Eight<DST> scaled_eight(uint2 lo, uint2 hi, int e)
 
 // sixteen values of a row: two words of 32 bytes (FP32) or one, whole sectors a lane where the row lies so
 template <int DST>
-__device__ __forceinline__ void store_sixteen(void* row, unsigned c, long long cols, bool vectors, bool vectors32, const Eight<DST>& lo, const Eight<DST>& hi)
+__device__ __forceinline__ void store_sixteen(void* row, long long c, long long cols, bool vectors, bool vectors32, const Eight<DST>& lo, const Eight<DST>& hi)
 {
     if (vectors32 && c + 16 <= cols) {
-        char* p = reinterpret_cast<char*>(row) + (size_t)c * (DST == HIF8_F32 ? 4 : 2);
+        char* p = reinterpret_cast<char*>(row) + c * (DST == HIF8_F32 ? 4 : 2);
         auto put = [](char* to, const uint4& a, const uint4& b) {
             asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                          ::"l"(to), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
@@ -297,24 +297,25 @@ __global__ void __launch_bounds__(kThreads, LANE ? 6 : 4) block_decode_kernel(co
     struct Group {
         uint4 v;
         int e;
-        unsigned row, col;
+        unsigned row, chunk;  // (of sixteen columns: a row may have more than 2^32)
     };
     auto which = [&](unsigned long long u) { return TWO && u >= job.m[0].units ? 1 : 0; };
     auto load = [&](unsigned long long u64) {
         Group g;
         g.v = make_uint4(0u, 0u, 0u, 0u);
-        g.e = 0; g.row = 0; g.col = 0;
+        g.e = 0; g.row = 0; g.chunk = 0;
         if (u64 >= job.units) return g;
         const int k = which(u64);
         const DecodeParams& p = job.m[k];
         const unsigned u = (unsigned)(u64 - (k ? job.m[0].units : 0u));
-        g.row = p.chunks.div(u); g.col = (u - g.row * p.chunks.d) * 16u;
-        if (g.row < p.m.rows && g.col < p.m.cols) {
+        g.row = p.chunks.div(u); g.chunk = u - g.row * p.chunks.d;
+        const long long col = (long long)g.chunk * 16;
+        if (g.row < p.m.rows && col < p.m.cols) {
             const uint8_t* at = p.m.codes + (size_t)g.row * (size_t)p.m.ld;
-            g.e = exp_at(p.m, g.row, g.col);
-            if (p.codes16 && g.col + 16 <= p.m.cols) g.v = __ldcs(reinterpret_cast<const uint4*>(at + g.col));
+            g.e = exp_at(p.m, g.row, col);
+            if (p.codes16 && col + 16 <= p.m.cols) g.v = __ldcs(reinterpret_cast<const uint4*>(at + col));
             else {
-                const uint2 lo = load_codes8(at, g.col, p.m.cols, p.codes8), hi = load_codes8(at, g.col + 8, p.m.cols, p.codes8);
+                const uint2 lo = load_codes8(at, col, p.m.cols, p.codes8), hi = load_codes8(at, col + 8, p.m.cols, p.codes8);
                 g.v = make_uint4(lo.x, lo.y, hi.x, hi.y);
             }
         }
@@ -329,7 +330,7 @@ __global__ void __launch_bounds__(kThreads, LANE ? 6 : 4) block_decode_kernel(co
         const DecodeParams& p = job.m[which(base)];
         const Eight<DST> lo = scaled_eight<DST>(bf16_of_four<LANE>(table, now.v.x, lane4), bf16_of_four<LANE>(table, now.v.y, lane4), now.e);
         const Eight<DST> hi = scaled_eight<DST>(bf16_of_four<LANE>(table, now.v.z, lane4), bf16_of_four<LANE>(table, now.v.w, lane4), now.e);
-        store_sixteen<DST>(reinterpret_cast<char*>(p.dst) + (size_t)now.row * (size_t)p.ld_dst * item, now.col, p.cols_out, p.vectors, p.vectors32, lo, hi);
+        store_sixteen<DST>(reinterpret_cast<char*>(p.dst) + (size_t)now.row * (size_t)p.ld_dst * item, (long long)now.chunk * 16, p.cols_out, p.vectors, p.vectors32, lo, hi);
         if (!LANE) break;  // (as many threads as groups)
     }
     if (job.m[0].late) pdl_launch_dependents();
