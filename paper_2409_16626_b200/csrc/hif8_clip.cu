@@ -287,9 +287,10 @@ __global__ void __launch_bounds__(kThreads, kClipPerSM) grad_scale_kernel(const 
     const double c = norm > (double)p.max_norm ? (double)p.max_norm / norm : 1.0;
     int k;
     const double m = frexp(c, &k) * 2.0;
-    k = max(-252, min(250, k - 1 - se));
-    const int k1 = max(-126, min(125, k));  // (m rounded to FP32 may be 2)
-    const Factor f{(float)m * pow2f(k1), pow2f(k - k1)};
+    k -= 1 + se;                                  // at most 126, and at least -302: a limit of 2^-149 and a norm of 2^128 times the root of the number of elements
+    int k1 = max(-126, min(125, k));              // (m rounded to FP32 may be 2)
+    if (k - k1 < -149) k1 = k + 149;              // (results of at most four of FP32's last steps, of whose factor the last bits go)
+    const Factor f{ldexpf((float)m, k1), ldexpf(1.f, k - k1)};
     const bool same = f.f == 1.f && f.p == 1.f;  // in place there is nothing to do
     if (from < to)
         for_pieces(p, from, to, first, [&](const Piece16& s, int thread, int threads) {
