@@ -498,7 +498,7 @@ size_t hif8_cache_compact_workspace_bytes(int n_pages);
  * stands for value(code) * 2^-e.  Exponents lie, and are taken, within [-HIF8_BLOCK_EXP_MAX, HIF8_BLOCK_EXP_MAX]: within them what a code stands for is exact in BF16.
  * Matrices of values have rows ld elements apart.  Rows must not overlap one another, nor what a call writes anything else that it writes or reads
  * (HIF8_ERR_OVERLAP) but for what a call names.  Pointers are aligned to their elements (HIF8_ERR_ALIGN); rows on 16-byte boundaries (of codes: 8) take the vectorised path, others a slower one with identical
- * results (but that a norm adds its row in another order).  A matrix has less than 2^31 groups of eight columns (HIF8_ERR_SHAPE).
+ * results (but that a norm adds its row in another order).  Each call says how large a matrix may be (HIF8_ERR_SHAPE beyond).
  */
 #define HIF8_BLOCK 128
 #define HIF8_BLOCK_EXP_MAX 96
@@ -507,12 +507,12 @@ size_t hif8_cache_compact_workspace_bytes(int n_pages);
  * Values -> block-scaled codes, one pass:
  *   e = clamp(target_exp - floor(log2 amax)) with the block's largest finite magnitude, 0 for zeros;  dst = To_HiF8_<rnd>(src * 2^e)
  * target_exp in [-22, 15]: 3 puts what lies from amax down to amax / 128 where the format has three mantissa bits.
- * HIF8_RND_SR draws the word of index r * cols + c, as hif8_encode does.
+ * HIF8_RND_SR draws the word of index r * cols + c, as hif8_encode does.  At most 2^31 - 1 blocks.
  */
 int hif8_block_encode(const void* src, int src_dtype, int64_t ld_src, int64_t rows, int64_t cols, int block_rows, uint8_t* dst, int64_t ld_dst, int* d_exp,
                       int64_t exp_stride, int target_exp, int rnd, unsigned flags, uint64_t seed, hif8_stream_t stream);
 
-/* Block-scaled codes -> values: value(src) * 2^-e, rounded to nearest-even in dst_dtype (only FP16 needs it). */
+/* Block-scaled codes -> values: value(src) * 2^-e, rounded to nearest-even in dst_dtype (only FP16 needs it).  At most 2^31 - 1 groups of sixteen columns (rows * ceil(cols / 16)). */
 int hif8_block_decode(const uint8_t* src, int64_t ld_src, const int* d_exp, int64_t exp_stride, int64_t rows, int64_t cols, int block_rows, void* dst, int dst_dtype,
                       int64_t ld_dst, hif8_stream_t stream);
 
@@ -520,7 +520,7 @@ int hif8_block_decode(const uint8_t* src, int64_t ld_src, const int* d_exp, int6
  * Root-mean-square norm with the residual's addition, its result in block-scaled codes (blocks of 1 x 128): what stands in front of a product.
  *   h = x + residual, rounded to dtype (residual NULL: h = x);  r = 1 / sqrt(mean_c h^2 + eps);  dst, d_exp = the codes of h * r * weight (see hif8_block_encode)
  * x, residual, h (may be NULL; may be x or residual itself, with the same ld) [rows, cols], weight [cols]: all of `dtype`.  d_rstd [rows] (may be NULL): r, for the gradient.
- * cols at most HIF8_NORM_MAX_COLS (HIF8_ERR_SHAPE); eps >= 0 and finite (HIF8_ERR_SCALE_RANGE).  Squares are added in FP32, products are FP32 and rounded once, to the codes.
+ * cols at most HIF8_NORM_MAX_COLS, rows at most 32 * (2^31 - 1) (HIF8_ERR_SHAPE); eps >= 0 and finite (HIF8_ERR_SCALE_RANGE).  Squares are added in FP32, products are FP32 and rounded once, to the codes.
  * rnd one of HIF8_RND_TA, _HR, _SSR, _TE (HIF8_ERR_ROUND for _SR).  Inf and NaN propagate within their row as in IEEE arithmetic.
  */
 #define HIF8_NORM_MAX_COLS 32768
@@ -548,7 +548,8 @@ size_t hif8_rmsnorm_backward_workspace_bytes(int64_t rows, int64_t cols);
  *   forward  Y[T,N'] = X W^T:   A = X [T,K'] (1),  W = [N',K'] (128), w_is_nk = 1
  *   dX[T,K'] = dY W:            A = dY [T,N'] (1), the same W, w_is_nk = 0
  *   dW[N',K'] += dY^T X:        A = dY, a_is_km = 1, W = X [T,K'] (1), w_is_nk = 0, accumulate = 1
- * M, N and K are any positive numbers; all three matrices are 16-byte aligned with rows a multiple of 16 bytes apart (HIF8_ERR_ALIGN).  C [M,N] of HIF8_BF16 or HIF8_F32; what lies
+ * M, N and K are any numbers from 1 to 2^31 - 4096 (0: nothing is done for M or N, HIF8_ERR_SHAPE for K).  An operand that is expanded in any case has at most 2^30 - 2^20 groups of sixteen
+ * columns: weights with scales for each 1 x 128, and A but where it is [K,M] beside weights with scales for each 128 x 128 (HIF8_ERR_SHAPE).  All three matrices are 16-byte aligned with rows a multiple of 16 bytes apart (HIF8_ERR_ALIGN).  C [M,N] of HIF8_BF16 or HIF8_F32; what lies
  * behind column N of a row stays as it is.  Products are exact in FP32 unless they leave its range (beyond it Inf, below 2^-126 possibly 0); sums are FP32, in a fixed order.
  * NaN and Inf codes propagate as in IEEE arithmetic.  accumulate as in hif8_gemm_ex.
  * workspace: hif8_gemm_block_workspace_bytes(...) bytes of the same arguments, 256-byte aligned, contents irrelevant on entry and undefined on return, for one call at a time; its first int is a device status

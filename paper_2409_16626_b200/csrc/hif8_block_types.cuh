@@ -34,8 +34,11 @@ struct BlockWorkspace {
     static constexpr int kNarrowRows = 64;   // up to so many rows the weight-streaming kernel takes the product
     static constexpr int kExpandRows = 512;  // from so many on there is room to expand the weights too, and where the tiles are few and the sum is long
     static constexpr int kPairs = 74, kMaxSplit = 16;
+    static constexpr int kMostDim = 0x7FFFF000;                        // M, N and K: what is rounded up to tiles of them stays below 2^31
+    static constexpr long long kMostGroups = (1ll << 30) - (1ll << 20);  // groups of sixteen columns of an operand that is expanded (with the rows or groups that parts of a sum are filled up to: 2^30)
     long long a_pitch, a_pitch_km, w_pitch;  // elements between rows of the BF16 copies (of A as [M,K], as [K,M])
     size_t a_bytes, w_bytes, narrow_bytes, part_bytes;   // 0 where there is none
+    bool fits;                               // operands that are expanded in any case have no more groups than that
     bool in_kernel;                          // the weights' blocks let the kernels that decode weights take the product
     int split;                               // parts of the sum, 1: not divided
     double cycles;                           // of a round of tiles of the pair kernel, with what joins the parts
@@ -50,8 +53,11 @@ struct BlockWorkspace {
         cycles = 0.0;
         part_k = part_rows = part_cols = 0;
         part_bytes = 0;
-        const long long tiles = (long long)((M + 255) / 256) * ((N + 255) / 256), kb = (K + 63) / 64;
-        const bool expand = !in_kernel || M >= kExpandRows || (M > kNarrowRows && 2 * tiles <= kPairs && kb >= 16);  // room for the weights' copy
+        auto groups_fit = [](long long rows, long long cols) { return rows * ((cols + 15) / 16) <= kMostGroups; };
+        const bool a_fits = a_is_km ? groups_fit(K, M) : groups_fit(M, K), w_fits = w_is_nk ? groups_fit(N, K) : groups_fit(K, N);
+        fits = in_kernel ? a_fits || a_is_km : a_fits && w_fits;  // (beside weights that are decoded in the kernel, an A as [K,M] is transposed by tiles)
+        const long long tiles = (((long long)M + 255) / 256) * (((long long)N + 255) / 256), kb = ((long long)K + 63) / 64;
+        const bool expand = !in_kernel || (a_fits && w_fits && (M >= kExpandRows || (M > kNarrowRows && 2 * tiles <= kPairs && kb >= 16)));  // room for the weights' copy
         if (expand) {
             // Cycles of the pair kernel's 64 k, of the parts written and read again and of the launch that adds them (gradients of 192 x 512 over 2810 rows 22.6 us, so 13.1; 256 x 256 over 8192 47.6 and 15.9).
             const double part = 8.0 * (double)M * (double)N / 2500.0;
@@ -63,7 +69,7 @@ struct BlockWorkspace {
             if (split > 1) {
                 part_k = (kb + split - 1) / split * 64;
                 split = (int)((kb * 64 + part_k - 1) / part_k);
-                part_rows = (M + 31) & ~31ll;
+                part_rows = ((long long)M + 31) & ~31ll;
                 part_cols = pad8(N);
                 part_bytes = pad256((size_t)split * (size_t)part_rows * (size_t)part_cols * 4);
             }
