@@ -498,7 +498,7 @@ size_t hif8_cache_compact_workspace_bytes(int n_pages);
  * stands for value(code) * 2^-e.  Exponents lie, and are taken, within [-HIF8_BLOCK_EXP_MAX, HIF8_BLOCK_EXP_MAX]: within them what a code stands for is exact in BF16.
  * Matrices of values have rows ld elements apart.  Rows must not overlap one another, nor what a call writes anything else that it writes or reads
  * (HIF8_ERR_OVERLAP) but for what a call names.  Pointers are aligned to their elements (HIF8_ERR_ALIGN); rows on 16-byte boundaries (of codes: 8) take the vectorised path, others a slower one with identical
- * results (but that a norm adds its row in another order).  Each call says how large a matrix may be (HIF8_ERR_SHAPE beyond).
+ * results but for the order in which a norm adds its row (see hif8_rmsnorm_encode).  Each call says how large a matrix may be (HIF8_ERR_SHAPE beyond).
  */
 #define HIF8_BLOCK 128
 #define HIF8_BLOCK_EXP_MAX 96
@@ -521,6 +521,8 @@ int hif8_block_decode(const uint8_t* src, int64_t ld_src, const int* d_exp, int6
  *   h = x + residual, rounded to dtype (residual NULL: h = x);  r = 1 / sqrt(mean_c h^2 + eps);  dst, d_exp = the codes of h * r * weight (see hif8_block_encode)
  * x, residual, h (may be NULL; may be x or residual itself, with the same ld) [rows, cols], weight [cols]: all of `dtype`.  d_rstd [rows] (may be NULL): r, for the gradient.
  * cols at most HIF8_NORM_MAX_COLS, rows at most 32 * (2^31 - 1) (HIF8_ERR_SHAPE); eps >= 0 and finite (HIF8_ERR_SCALE_RANGE).  Squares are added in FP32, products are FP32 and rounded once, to the codes.
+ * The order in which a row's squares are added depends on its alignment and, from 513 to 8192 columns, on whether the call has more than 148 rows: r then differs in its last bits, and a code whose
+ * value lies on the border of two.  Within one call all rows are added alike.  A row whose squares add up to more than FP32 holds has r 0; squares below FP32 count as 0.
  * rnd one of HIF8_RND_TA, _HR, _SSR, _TE (HIF8_ERR_ROUND for _SR).  Inf and NaN propagate within their row as in IEEE arithmetic.
  */
 #define HIF8_NORM_MAX_COLS 32768
@@ -551,7 +553,8 @@ size_t hif8_rmsnorm_backward_workspace_bytes(int64_t rows, int64_t cols);
  * M, N and K are any numbers from 1 to 2^31 - 4096 (0: nothing is done for M or N, HIF8_ERR_SHAPE for K).  An operand that is expanded in any case has at most 2^30 - 2^20 groups of sixteen
  * columns: weights with scales for each 1 x 128, and A but where it is [K,M] beside weights with scales for each 128 x 128 (HIF8_ERR_SHAPE).  All three matrices are 16-byte aligned with rows a multiple of 16 bytes apart (HIF8_ERR_ALIGN).  C [M,N] of HIF8_BF16 or HIF8_F32; what lies
  * behind column N of a row stays as it is.  Products are exact in FP32 unless they leave its range (beyond it Inf, below 2^-126 possibly 0); sums are FP32, in a fixed order.
- * NaN and Inf codes propagate as in IEEE arithmetic.  accumulate as in hif8_gemm_ex.
+ * NaN and Inf codes propagate as in IEEE arithmetic.  accumulate as in hif8_gemm_ex.  Which kernel takes a product, and with it the order of its sums, depends on M, N and K.
+ * Codes are read in whole pieces of 16 bytes: of the last one of a row the bytes behind its end too, whatever they hold (they have no effect, and lie in the same aligned 16 bytes as the row's end).
  * workspace: hif8_gemm_block_workspace_bytes(...) bytes of the same arguments, 256-byte aligned, contents irrelevant on entry and undefined on return, for one call at a time; its first int is a device status
  * word as for hif8_gemm (hif8_gemm_status, hif8_last_device_status).
  */
@@ -562,13 +565,15 @@ size_t hif8_gemm_block_workspace_bytes(int M, int N, int K, int a_is_km, int w_i
 
 /*
  * The global norm of all gradients and clipping, behind a backward pass under a loss scale of 2^s (Section 5.1, ALS):
- *   *d_norm = sqrt(sum g^2) * 2^-s over all elements of all tensors;  dst = g * 2^-s * min(1, max_norm / norm), rounded once to the tensor's type
+ *   *d_norm = sqrt(sum g^2) * 2^-s over all elements of all tensors;  dst = g * (2^-s * min(1, max_norm / norm))
  * A list of tensors in device memory: d_src [n_tensors] addresses, d_dst the same for the results (NULL, or equal entries: in place; otherwise no result may overlap a
  * gradient), d_dtype [n_tensors] element formats, d_start [n_tensors + 1] running sums of the tensors' numbers of elements, from 0 to n_elements.  (They have to be right: the library
- * cannot check them.  A tensor of no known format, or at an address that is 0 or not aligned to its elements, is left out.)  16-byte aligned addresses take the vectorised path.
+ * cannot check them.  A tensor of no known format, or at an address that is 0 or not aligned to its elements, is left out.)  No two tensors of the list may
+ * overlap.  16-byte aligned addresses take the vectorised path.
  *   d_scale_exp: device int s, the first int of the state of hif8_als_state_init, for instance (NULL: 0);  max_norm > 0, +Inf for no clipping (HIF8_ERR_SCALE_RANGE).
  *   A norm beyond FP32 is stored as +Inf and clipped to all the same.  Gradients that are not all finite: nothing is written to dst, *d_norm = +Inf and *d_found_inf |= 1 (as hif8_check_finite; either pointer may be NULL).
- * Squares are summed in FP64 in a fixed order: results are reproducible.  workspace: hif8_grad_clip_workspace_bytes() bytes, 256-byte aligned, for one call at a time.
+ * Squares are added in FP32 within 16 bytes of a tensor and in FP64 from there on, in a fixed order: results are reproducible, and the norm is within 5 * 2^-24 of the exact one.  The factor is rounded to FP32,
+ * its product with g to FP32 too, and for 16-bit tensors once more to their type.  workspace: hif8_grad_clip_workspace_bytes() bytes, 256-byte aligned, for one call at a time.
  */
 int hif8_grad_clip(const uint64_t* d_src, const uint64_t* d_dst, const int* d_dtype, const int64_t* d_start, int n_tensors, int64_t n_elements, const int* d_scale_exp,
                    float max_norm, float* d_norm, int* d_found_inf, void* workspace, size_t workspace_bytes, hif8_stream_t stream);

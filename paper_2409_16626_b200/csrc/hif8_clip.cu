@@ -6,8 +6,9 @@
 // memory.  A share is a stretch of the list of all elements, in which each tensor takes kTensorCost places more than it has elements, for what it costs to come to one: so
 // neither many small tensors nor few large ones leave blocks idle.  A block fetches the descriptors of its tensors together, works on long pieces with all threads and on short ones
 // with a warp each.  (Tensors one after the other, each with its descriptor's latency: 3000 tensors of 10 elements 362 us, 11.5; 2.7 M elements in 28 matrices and 9 vectors
-// 21.5 us, 11.8.)  Squares are added in FP32 over 16 bytes and in FP64 from there on (vectors whose sum leaves FP32's comfortable range: in FP64 altogether), so the
-// norm is as exact as FP32 can say, and the squares of finite gradients do not overflow.
+// 21.5 us, 11.8.)  Squares are added in FP32 over 16 bytes and in FP64 from there on (vectors whose sum leaves FP32's comfortable range: in FP64 altogether): the
+// norm is within 5 * 2^-24 of the exact one, and the squares of finite gradients do not overflow.  (FP64 from the first square on would take a conversion and an FP64 multiply-add
+// for each element.)
 #include "hif8_block.cuh"
 
 namespace hif8 {
@@ -211,7 +212,7 @@ __global__ void __launch_bounds__(kThreads, kClipPerSM) grad_squares_kernel(cons
     if (threadIdx.x == 0) p.part[blockIdx.x] = sum;
 }
 
-// x f p, p a power of two that is 1 unless f p is no normal FP32: one rounding (below 2^-126, and only then, a second)
+// x f p, p a power of two that is 1 unless f p is no normal FP32: one rounding to FP32 (below 2^-126, and only then, a second); a 16-bit tensor's type is the next
 struct Factor {
     float f, p;
     __device__ __forceinline__ float of(float x) const { return x * f * p; }
