@@ -21,14 +21,6 @@ struct FastDiv {
 __device__ __forceinline__ int clamp_block_exp(int e) { return max(-HIF8_BLOCK_EXP_MAX, min(HIF8_BLOCK_EXP_MAX, e)); }
 __device__ __forceinline__ int block_exp_from_amax(uint32_t amax_bits, int target_exp) { return clamp_block_exp(scale_exp_from_amax(amax_bits, target_exp)); }
 
-// largest of the values of sixteen threads (the lower or the upper half of a warp)
-__device__ __forceinline__ uint32_t half_warp_max(uint32_t v)
-{
-#pragma unroll
-    for (int d = 8; d; d >>= 1) v = max(v, __shfl_xor_sync(0xFFFFFFFFu, v, d));
-    return v;
-}
-
 // Eight elements c .. c + 7 of a row of `cols`, zeros behind its end: 16 bytes, of FP32 32.  `vectors`: the row starts on a 16-byte boundary (and c is a multiple of 8).
 // KEEP: they will be read again.  WHOLE: the row does so and `cols` is a multiple of 8, so no element is looked at by itself.
 template <int DT> struct Eight { uint4 v[DT == HIF8_F32 ? 2 : 1]; };
@@ -43,12 +35,7 @@ __device__ __forceinline__ Eight<DT> load_eight(const void* row, long long c, lo
         for (int i = 0; i < (int)(sizeof(e.v) / 16); i++) e.v[i] = !in ? make_uint4(0, 0, 0, 0) : KEEP ? __ldg(p + i) : __ldcs(p + i);
         return e;
     }
-    if (KEEP && vectors && c + 8 <= cols) {
-        const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(row) + c * (DT == HIF8_F32 ? 4 : 2));
-        e.v[0] = __ldg(p);
-        if (DT == HIF8_F32) e.v[sizeof(e.v) / 16 - 1] = __ldg(p + 1);
-        return e;
-    }
+    static_assert(WHOLE || !KEEP, "what is read again is read in whole rows");
     if (DT == HIF8_F32) {
         const float* p = reinterpret_cast<const float*>(row) + c;
         if (vectors && c + 8 <= cols) {

@@ -26,7 +26,6 @@ struct NormParams {
     int target_exp;
     unsigned flags;
     bool late;             // the next launch may start at the end: its blocks sit unevenly when they come under launches of several rounds
-    bool vec_x, vec_res, vec_h, vec_w, codes8;  // rows on boundaries of 16 bytes (codes: 8)
 };
 
 // How a row is shared out: ALONE, one block to a row, any number `gs` of threads in whole warps; otherwise 1 << lg threads of a block of 256, 16 of them only where HALF.
@@ -218,7 +217,6 @@ struct NormBackwardParams {
     float* part;         // [blocks][cols] shares of the weight's gradient, or null
     long long ld_dy, ld_h, ld_dh, ld_dx, rows, cols;
     int gs, lg;
-    bool vec_dy, vec_h, vec_dh, vec_dx, vec_w;
 };
 
 // Its values are unpacked again behind this: kept unpacked over a barrier they take registers that the kernels do not have.
@@ -445,20 +443,19 @@ void launch_norm(NormParams p, int sms, cudaStream_t st)
     else launch_pdl_threads(plan.threads, norm_encode_kernel<DT, MODE, 1024, kNormEights, WHOLE>, grid, st, p);
 }
 template <int DT, int MODE>
-void launch_norm(const NormParams& p, int sms, cudaStream_t st)
+void launch_norm(const NormParams& p, bool whole, int sms, cudaStream_t st)
 {
-    const bool whole = (p.cols & 7) == 0 && p.vec_x && p.vec_w && p.codes8 && (!p.residual || p.vec_res) && (!p.h || p.vec_h);
     if (whole) launch_norm<DT, MODE, true>(p, sms, st);
     else launch_norm<DT, MODE, false>(p, sms, st);
 }
 template <int DT>
-void launch_norm_mode(int rnd, const NormParams& p, int sms, cudaStream_t st)
+void launch_norm_mode(int rnd, const NormParams& p, bool whole, int sms, cudaStream_t st)
 {
     switch (rnd) {
-        case HIF8_RND_TA: return launch_norm<DT, HIF8_RND_TA>(p, sms, st);
-        case HIF8_RND_HR: return launch_norm<DT, HIF8_RND_HR>(p, sms, st);
-        case HIF8_RND_SSR: return launch_norm<DT, HIF8_RND_SSR>(p, sms, st);
-        default: return launch_norm<DT, HIF8_RND_TE>(p, sms, st);
+        case HIF8_RND_TA: return launch_norm<DT, HIF8_RND_TA>(p, whole, sms, st);
+        case HIF8_RND_HR: return launch_norm<DT, HIF8_RND_HR>(p, whole, sms, st);
+        case HIF8_RND_SSR: return launch_norm<DT, HIF8_RND_SSR>(p, whole, sms, st);
+        default: return launch_norm<DT, HIF8_RND_TE>(p, whole, sms, st);
     }
 }
 
@@ -544,12 +541,13 @@ extern "C" int hif8_rmsnorm_encode(const void* x, int64_t ld_x, const void* resi
     int sms; if (int rc = checked_device(&sms)) return rc;
     p.x = x; p.residual = residual; p.weight = weight; p.h = h; p.rstd = d_rstd; p.ld_x = ld_x; p.ld_res = ld_residual; p.ld_h = ld_h; p.rows = rows; p.cols = cols;
     p.eps = eps; p.target_exp = target_exp; p.flags = flags;
-    p.vec_x = vector_rows(x, rows, ld_x, item); p.vec_res = vector_rows(residual, rows, ld_residual, item); p.vec_h = vector_rows(h, rows, ld_h, item); p.vec_w = aligned_to(weight, 16);
-    p.codes8 = aligned_to(dst, 8) && (rows <= 1 || (ld_dst & 7) == 0);
+    // every row on a 16-byte boundary (codes: 8)
+    const bool whole = (cols & 7) == 0 && vector_rows(x, rows, ld_x, item) && aligned_to(weight, 16) && aligned_to(dst, 8) && (rows <= 1 || (ld_dst & 7) == 0) &&
+                       (!residual || vector_rows(residual, rows, ld_residual, item)) && (!h || vector_rows(h, rows, ld_h, item));
     cudaStream_t st = (cudaStream_t)stream;
-    if (dtype == HIF8_F32) launch_norm_mode<HIF8_F32>(rnd, p, sms, st);
-    else if (dtype == HIF8_BF16) launch_norm_mode<HIF8_BF16>(rnd, p, sms, st);
-    else launch_norm_mode<HIF8_F16>(rnd, p, sms, st);
+    if (dtype == HIF8_F32) launch_norm_mode<HIF8_F32>(rnd, p, whole, sms, st);
+    else if (dtype == HIF8_BF16) launch_norm_mode<HIF8_BF16>(rnd, p, whole, sms, st);
+    else launch_norm_mode<HIF8_F16>(rnd, p, whole, sms, st);
     return finish(1);
 }
 
@@ -589,9 +587,8 @@ extern "C" int hif8_rmsnorm_backward(const void* dy, int64_t ld_dy, const void* 
     int sms; if (int rc = checked_device(&sms)) return rc;
     p.dy = dy; p.h = h; p.dh = dh; p.weight = weight; p.rstd = d_rstd; p.dx = dx; p.part = d_weight_grad ? reinterpret_cast<float*>(workspace) : nullptr;
     p.ld_dy = ld_dy; p.ld_h = ld_h; p.ld_dh = ld_dh; p.ld_dx = ld_dx; p.rows = rows; p.cols = cols;
-    p.vec_dy = vector_rows(dy, rows, ld_dy, item); p.vec_h = vector_rows(h, rows, ld_h, item); p.vec_dh = vector_rows(dh, rows, ld_dh, item); p.vec_dx = vector_rows(dx, rows, ld_dx, item);
-    p.vec_w = aligned_to(weight, 16);
-    const bool whole = (cols & 7) == 0 && p.vec_dy && p.vec_h && p.vec_dx && p.vec_w && (!dh || p.vec_dh);
+    const bool whole = (cols & 7) == 0 && vector_rows(dy, rows, ld_dy, item) && vector_rows(h, rows, ld_h, item) && vector_rows(dx, rows, ld_dx, item) && aligned_to(weight, 16) &&
+                       (!dh || vector_rows(dh, rows, ld_dh, item));
     const long long blocks = backward_blocks(rows, backward_plan(cols, dtype, whole));
     const bool ok = dtype == HIF8_F32 ? launch_backward<HIF8_F32>(p, whole, blocks, st) : dtype == HIF8_BF16 ? launch_backward<HIF8_BF16>(p, whole, blocks, st) : launch_backward<HIF8_F16>(p, whole, blocks, st);
     if (!ok) return HIF8_ERR_CUDA;
