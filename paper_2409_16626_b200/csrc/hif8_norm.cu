@@ -407,7 +407,7 @@ struct RowPlan {
 };
 constexpr int kFewRows = 148;
 
-// The gradient's kernel: as many blocks as are resident.  (FP32 of up to 4096 columns, eight elements a thread: 16384 x 4096 184 -> 174 us, 65536 x 1024 170 -> 166.)
+// The gradient's kernel: as many blocks as are resident.  (FP32 of up to 4096 columns, eight elements a thread: 16384 x 4096 181 -> 171 us, 65536 x 1024 170 -> 165.)
 RowPlan backward_plan(long long cols, int dtype, bool whole) { return RowPlan(cols, dtype == HIF8_F32 && cols <= 4096 ? 1 : cols <= 16384 ? 2 : 4, whole, false); }
 long long backward_blocks(long long rows, const RowPlan& plan)
 {
