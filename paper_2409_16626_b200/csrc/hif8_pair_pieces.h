@@ -8,13 +8,14 @@
 
 namespace hif8 {
 
-// Two places in turn, from the first one on in each tile; the last tile's pieces have one each, and those from the third on have held no piece before.
+// Two places in turn, from the first one on in each tile; the last tile's pieces have one each, and those from the third on have held no piece before.  Within a tile all but the newest
+// store have read when a piece is written, which lies in the other place.
 struct PiecePlaces {
-    int newest = -1;  // place of the store committed last
+    int newest = -1;  // place of the store committed last, in the tiles before
     static HIF8_PIECES_FN int place_of(int piece, bool last_tile) { return last_tile ? piece : piece & 1; }
-    // Stores that may still read when a piece is written to `place`: the newest, but for the first piece behind a tile with an odd number of them, which comes to the newest's own place.
+    // Stores that may still read when a tile begins with `place`: the newest, unless the tile before had an odd number of them, so that it lies in this very place.
     HIF8_PIECES_FN int may_still_read(int place) const { return place == newest ? 0 : 1; }
-    HIF8_PIECES_FN void stored(int place) { newest = place; }
+    HIF8_PIECES_FN void stored(int place) { newest = place; }  // by the last store of a tile
 };
 
 }  // namespace hif8

@@ -18,15 +18,19 @@ static int first_clash(const std::vector<int>& tiles, bool staged, bool always_o
 {
     hif8::PiecePlaces places;
     std::deque<int> reading;
-    for (size_t t = 0; t < tiles.size(); t++)
+    auto wait = [&](int may_read) { while ((int)reading.size() > may_read) reading.pop_front(); };
+    for (size_t t = 0; t < tiles.size(); t++) {
+        const bool last = t + 1 == tiles.size();
+        wait(always_one ? 1 << 30 : places.may_still_read(hif8::PiecePlaces::place_of(0, last)) == 0 ? 0 : 1 << 30);
         for (int i = 0; i < tiles[t] + (staged ? 1 : 0); i++) {
-            const int place = hif8::PiecePlaces::place_of(i, t + 1 == tiles.size());
-            if (place < 2)
-                while ((int)reading.size() > (always_one ? 1 : places.may_still_read(place))) reading.pop_front();
+            const int place = hif8::PiecePlaces::place_of(i, last);
+            if (place < 2) wait(1);
             for (int p : reading)
                 if (p == place) return (int)t + 1;
-            if (i < tiles[t]) { places.stored(place); reading.push_back(place); }
+            if (i < tiles[t]) reading.push_back(place);
         }
+        if (tiles[t] > 0) places.stored(hif8::PiecePlaces::place_of(tiles[t] - 1, last));
+    }
     return 0;
 }
 
@@ -74,5 +78,6 @@ def test_the_kernel_waits_so():
     text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "hif8_gemm.cu")).read())
     start = re.search(r"\nbf16_gemm_pair_kernel\(const __grid_constant__", text).end()
     body = text[start:text.find("\n}\n", start)]
-    assert body.count("wait_group.read 1") == 1 and "if (places.may_still_read(place_of(i)) == 0)" in body[:body.find("wait_group.read 1")]
-    assert body.find("places.may_still_read(") < body.find("sts_v4(at") < body.find("places.stored(place_of(i))") < body.find("tma_store_2d(")
+    first, each, write, store, told = (body.find(t) for t in ('places.may_still_read(place_of(0)) == 0) asm volatile("cp.async.bulk.wait_group.read 0;"', "wait_group.read 1", "sts_v4(at", "tma_store_2d(",
+                                                              "if (mapped > 0) places.stored(place_of(mapped - 1));"))
+    assert 0 < first < each < write < store < told and body.count("wait_group.read 1") == 1
