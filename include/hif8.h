@@ -551,7 +551,7 @@ size_t hif8_rmsnorm_backward_workspace_bytes(int64_t rows, int64_t cols);
  *   dX[T,K'] = dY W:            A = dY [T,N'] (1), the same W, w_is_nk = 0
  *   dW[N',K'] += dY^T X:        A = dY, a_is_km = 1, W = X [T,K'] (1), w_is_nk = 0, accumulate = 1
  * M, N and K are any numbers from 1 to 2^31 - 4096 (0: nothing is done for M or N, HIF8_ERR_SHAPE for K).  An operand that is expanded in any case has at most 2^30 - 2^20 groups of sixteen
- * columns: weights with scales for each 1 x 128, and A but where it is [K,M] beside weights with scales for each 128 x 128 (HIF8_ERR_SHAPE).  All three matrices are 16-byte aligned with rows a multiple of 16 bytes apart (HIF8_ERR_ALIGN).  C [M,N] of HIF8_BF16 or HIF8_F32; what lies
+ * columns: weights with scales for each 1 x 128 (as [N,K]: N up to the next multiple of eight), and A but where it is [K,M] beside weights with scales for each 128 x 128 (HIF8_ERR_SHAPE).  All three matrices are 16-byte aligned with rows a multiple of 16 bytes apart (HIF8_ERR_ALIGN).  C [M,N] of HIF8_BF16 or HIF8_F32; what lies
  * behind column N of a row stays as it is.  Products are exact in FP32 unless they leave its range (beyond it Inf, below 2^-126 possibly 0); sums are FP32, in a fixed order.
  * NaN and Inf codes propagate as in IEEE arithmetic.  accumulate as in hif8_gemm_ex.  Which kernel takes a product, and with it the order of its sums, depends on M, N and K.
  * Codes are read in whole pieces of 16 bytes: of the last one of a row the bytes behind its end too, whatever they hold (they have no effect, and lie in the same aligned 16 bytes as the row's end).

@@ -54,7 +54,7 @@ struct BlockWorkspace {
         part_k = part_rows = part_cols = 0;
         part_bytes = 0;
         auto groups_fit = [](long long rows, long long cols) { return rows * ((cols + 15) / 16) <= kMostGroups; };
-        const bool a_fits = a_is_km ? groups_fit(K, M) : groups_fit(M, K), w_fits = w_is_nk ? groups_fit(N, K) : groups_fit(K, N);
+        const bool a_fits = a_is_km ? groups_fit(K, M) : groups_fit(M, K), w_fits = w_is_nk ? groups_fit(pad8(N), K) : groups_fit(K, N);  // (parts of a sum have rows of W for whole groups of eight columns)
         fits = in_kernel ? a_fits || a_is_km : a_fits && w_fits;  // (beside weights that are decoded in the kernel, an A as [K,M] is transposed by tiles)
         const long long tiles = (((long long)M + 255) / 256) * (((long long)N + 255) / 256), kb = ((long long)K + 63) / 64;
         const bool expand = !in_kernel || (a_fits && w_fits && (M >= kExpandRows || (M > kNarrowRows && 2 * tiles <= kPairs && kb >= 16)));  // room for the weights' copy

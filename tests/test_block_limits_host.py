@@ -41,7 +41,7 @@ def gemm(m, n, k, a_is_km=0, w_is_nk=1, w_block_rows=128):
     (gemm(1, 1, 2 ** 31 - 1), SHAPE), (gemm(2 ** 31 - 1, 1, 1, 1), SHAPE), (gemm(1, 2 ** 31 - 1, 1), SHAPE),
     (gemm(EXPANDED, 1, 16), ALIGN), (gemm(EXPANDED, 1, 17), SHAPE), (gemm(EXPANDED + 1, 1, 1), SHAPE), (gemm(EXPANDED + 1, 1, 1, 1), ALIGN), (gemm(16, 1, EXPANDED + 1, 1), ALIGN),
     (gemm(16, 1, EXPANDED, 1, 1, 1), ALIGN), (gemm(16, 1, EXPANDED + 1, 1, 1, 1), SHAPE), (gemm(1, EXPANDED, 16, 0, 1, 1), ALIGN), (gemm(1, EXPANDED + 1, 16, 0, 1, 1), SHAPE),
-    (gemm(1, 16, EXPANDED, 0, 0, 1), ALIGN), (gemm(1, 17, EXPANDED, 0, 0, 1), SHAPE), (gemm(1, EXPANDED + 1, 16), ALIGN)])
+    (gemm(1, 1, EXPANDED * 2, 0, 1, 1), ALIGN), (gemm(1, 1, EXPANDED * 2 + 1, 0, 1, 1), SHAPE), (gemm(1, 9, EXPANDED + 1, 0, 1, 1), SHAPE), (gemm(1, 16, EXPANDED, 0, 0, 1), ALIGN), (gemm(1, 17, EXPANDED, 0, 0, 1), SHAPE), (gemm(1, EXPANDED + 1, 16), ALIGN)])
 def test_limits(call, status):
     name, change = call
     fn, good = CALLS[name]
